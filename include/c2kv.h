@@ -402,6 +402,127 @@ c2kv_status c2kv_extract_attention(c2kv_ctx* ctx, int32_t n_layers, const void* 
                                    const void* v, int32_t n_tokens, int32_t ratio_k, void* out,
                                    float* lse);
 
+/*
+ * Paged caches -- a cache that grows by rows of generated or prompt tokens, in pages of the
+ * caller's memory that belong to no request in particular (the paper has no counterpart; this is
+ * what a serving program keeps once its chunks are composed).  A page holds page_size rows of
+ * every KV head; row j of request r is row j % page_size of page table[r][j / page_size].
+ *
+ * Pages hold the context's type (C2KV_PAGES_NATIVE) or 8-bit codes (C2KV_PAGES_E4M3: sign, 4 bits
+ * of exponent, 3 of fraction), with one fp32 scale for each row of each KV head of K and of V: a
+ * row x is kept as the scale s = max|x| / 448 and the codes nearest to x / s (formed as x times
+ * the rounded 1 / s), and stands for code * s.  A scale of its own for every row lets rows be
+ * appended without touching earlier ones.  A row of magnitudes below 2^-100 is kept as zero.  A
+ * row with an infinity or a NaN is kept with scale NaN and codes 0: queries that see it give NaN,
+ * the others are not touched by it.  The library writes no NaN code (0x7f, 0xff).
+ *
+ * The pages and their scales are laid out head by head, so that one head's rows of a page are one
+ * run; a page may lie anywhere (page_stride), in an allocation that holds other layers' pages too.
+ */
+#define C2KV_PAGES_NATIVE 0
+#define C2KV_PAGES_E4M3   1
+typedef struct c2kv_pages {
+    void*   k;                 /* device [n_pages][Hkv][page_size][d], 16-byte aligned           */
+    void*   v;
+    float*  k_scale;           /* device [n_pages][Hkv][page_size], 16-byte aligned (E4M3 only)  */
+    float*  v_scale;
+    int64_t page_stride;       /* elements from page to page of k and v, a multiple of 16 bytes;
+                                  0 = Hkv * page_size * d                                        */
+    int64_t scale_stride;      /* scales from page to page, a multiple of 4; 0 = Hkv * page_size */
+    int32_t n_pages;
+    int32_t page_size;         /* 16, 32, 64 or 128                                              */
+    int32_t format;            /* C2KV_PAGES_*                                                   */
+} c2kv_pages;
+
+/*
+ * c2kv_paged_append -- write new tokens' K and V into their requests' pages: tokens
+ * [new_ptr[r], new_ptr[r + 1]) become rows start[r], start[r] + 1, .. of request r.  K turns by
+ * turn[t] positions first (RoPE of a pre-RoPE row at position turn[t]; slots stand for several
+ * positions, so a row's position is the caller's to say), or is taken as it is where turn is NULL
+ * (rows of a composed cache, turned already).
+ *
+ *   batch        : requests B >= 1.
+ *   table        : device int32 [B] rows of table_width page numbers, table_stride apart.
+ *   new_ptr      : host int32 [B + 1], non-decreasing from 0; a request may have no new token.
+ *   start        : host int32 [B].
+ *   k, v         : device [T][Hkv][d] in the context's type, tokens kv_stride elements apart
+ *                  (0 = Hkv * d; rows of a fused projection are further apart).
+ *   turn         : device int32 [T], or NULL.
+ * A page number outside [0, n_pages) is refused by the kernel: the row is not written, and
+ * c2kv_sync returns ERR_DEVICE_BOUNDS.  Recorded by the trace as C2KV_PROF_SUFFIX.
+ * Errors: ERR_ARG, ERR_DTYPE (page format), ERR_CUDA.
+ */
+c2kv_status c2kv_paged_append(c2kv_ctx* ctx, const c2kv_pages* pages, int32_t batch, const int32_t* table,
+                              int32_t table_width, int64_t table_stride, const int32_t* new_ptr,
+                              const int32_t* start, const void* k, const void* v, int64_t kv_stride,
+                              const int32_t* turn);
+
+/*
+ * c2kv_paged_gather -- the way back: rows start[r] .. of every request into a dense block in the
+ * context's type, request r's at tokens [row_ptr[r], row_ptr[r + 1]).  K turns by turn[t] (NULL: as
+ * it is): by minus its position it becomes the pre-RoPE row that c2kv_compress_chunk stores, so an
+ * answer can be kept as a chunk.  Rows of a refused page (see above) read as zero.
+ *   k_out, v_out : device [T][Hkv][d], tokens out_stride elements apart (0 = Hkv * d).
+ * Recorded by the trace as C2KV_PROF_COMPOSE.  Errors: as c2kv_paged_append.
+ */
+c2kv_status c2kv_paged_gather(c2kv_ctx* ctx, const c2kv_pages* pages, int32_t batch, const int32_t* table,
+                              int32_t table_width, int64_t table_stride, const int32_t* row_ptr,
+                              const int32_t* start, void* k_out, void* v_out, int64_t out_stride,
+                              const int32_t* turn);
+
+/*
+ * c2kv_paged_attend -- attention of each request's newest tokens (one generated token, a few
+ * drafted ones, a chunk of a prompt) over its pages, their own rows among them (append first).
+ * Queries [q_ptr[r], q_ptr[r + 1]) are the last ones of request r's n_keys[r] rows: query t sits
+ * at row i = n_keys[r] - (q_ptr[r + 1] - t) and
+ *     O[t, h] = softmax_j( R(turn_t) Q_t,h . K_j,h/G / sqrt(d) ) V_j,h/G    over rows j <= i,
+ *                                                    j > i - window where window > 0
+ * (G = Hq / Hkv, any).  A query that sees no row (i < 0) gives zeros, and lse -inf.  Rows that no
+ * query sees are never read into a result, whatever they hold.
+ *
+ *   batch, table, table_width, table_stride : as c2kv_paged_append.
+ *   q_ptr        : host int32 [B + 1], non-decreasing from 0; a request may have no query.
+ *   n_keys       : host int32 [B] rows of each request, >= 0.
+ *   q            : device [T][Hq][d], tokens q_stride elements apart (0 = Hq * d).
+ *   turn         : device int32 [T] positions of the queries, or NULL (turned already).
+ *   out          : device [T][Hq][d] (context dtype).
+ *   lse          : device [Hq][T] fp32 natural-log softmax normaliser, or NULL.
+ * A page number outside [0, n_pages) is refused by the kernel: its rows are not seen, and
+ * c2kv_sync returns ERR_DEVICE_BOUNDS.  Recorded by the trace as C2KV_PROF_ATTN.
+ * Errors: ERR_ARG, ERR_DTYPE (page format), ERR_NOMEM, ERR_CUDA.
+ */
+c2kv_status c2kv_paged_attend(c2kv_ctx* ctx, const c2kv_pages* pages, int32_t batch, const int32_t* table,
+                              int32_t table_width, int64_t table_stride, const int32_t* q_ptr,
+                              const int32_t* n_keys, int32_t window, const void* q, int64_t q_stride,
+                              const int32_t* turn, void* out, float* lse);
+
+/*
+ * c2kv_verify_drafts -- how many of each request's drafted tokens the target's probabilities
+ * accept, and the token that follows them, so that the tokens kept are distributed as the target's
+ * own.  Draft t (token x, row t of q) is accepted while u_accept[t] * q[t][x] < p[row][x] (the
+ * product rounded to fp32).  At the first refusal the next token is drawn from max(p - q, 0) of
+ * that row; after the last draft from p of the row after it.  The draw is exact: weights are cut
+ * to whole multiples of 2^-44 (above 1: 1; NaN and negative: 0), u to a whole multiple k of 2^-24,
+ * and the token is the lowest index whose running sum passes floor(sum * k / 2^24).  Where nothing
+ * is left of p over q, p itself is taken; -1 where p has no weight either.
+ *
+ *   draft_ptr    : host int32 [B + 1], non-decreasing from 0; a request may have no draft.
+ *   vocab        : 1 <= V <= 2^19.
+ *   tokens       : device int32 [T] drafted tokens.  One outside [0, V) is refused, and c2kv_sync
+ *                  returns ERR_DEVICE_BOUNDS.
+ *   p            : device fp32 [T + B][V], rows p_stride apart (0 = V): request r's rows are
+ *                  draft_ptr[r] + r .. draft_ptr[r + 1] + r, one more than its drafts.
+ *   q            : device fp32 [T][V], rows q_stride apart (0 = V), or NULL for drafts made without
+ *                  probabilities (q = 1 at the token, 0 elsewhere).
+ *   u_accept     : device fp32 [T] in [0, 1);  u_next : device fp32 [B] in [0, 1).
+ *   n_accepted, next_token : device int32 [B].
+ * Not recorded by the trace.  Errors: ERR_ARG, ERR_CUDA.
+ */
+c2kv_status c2kv_verify_drafts(c2kv_ctx* ctx, int32_t batch, const int32_t* draft_ptr, int32_t vocab,
+                               const int32_t* tokens, const float* p, int64_t p_stride, const float* q,
+                               int64_t q_stride, const float* u_accept, const float* u_next,
+                               int32_t* n_accepted, int32_t* next_token);
+
 /* c2kv_cache_release -- free a composed cache (stream-ordered). */
 c2kv_status c2kv_cache_release(c2kv_ctx* ctx, c2kv_cache* cache);
 

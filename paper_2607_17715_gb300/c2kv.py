@@ -32,6 +32,7 @@ MODE_MEANPOOL, MODE_PROVIDED, MODE_STORED, MODE_HOST = 0, 1, 2, 3
 ATTN_AUTO, ATTN_SIMT, ATTN_TC = 0, 1, 2
 FUSE_AUTO, FUSE_NEVER, FUSE_ALWAYS = 0, 1, 2
 STORAGE_LOCAL_ROPE, STORAGE_PRE_ROPE = 0, 1
+PAGES_NATIVE, PAGES_E4M3 = 0, 1
 PROF_COMPOSE, PROF_COMPRESS, PROF_SUFFIX, PROF_ATTN, PROF_COMBINE, PROF_DECODE = 0, 1, 2, 3, 4, 5
 PROF_EXTRACT, PROF_FUSED = 6, 7
 PROF_KINDS = 8
@@ -72,7 +73,14 @@ class c2kv_cache_desc(ctypes.Structure):
                 ("l_req", _P32), ("capacity", _P32), ("suffix_capacity", ctypes.c_int32)]
 
 
-_VP, _I32 = ctypes.c_void_p, ctypes.c_int32
+_VP, _I32, _I64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+
+
+class c2kv_pages(ctypes.Structure):
+    _fields_ = [("k", _VP), ("v", _VP), ("k_scale", _VP), ("v_scale", _VP), ("page_stride", _I64),
+                ("scale_stride", _I64), ("n_pages", _I32), ("page_size", _I32), ("format", _I32)]
+
+
 _SIGS = {
     "c2kv_abi_version": (_I32, []),
     "c2kv_create": (_I32, [ctypes.POINTER(c2kv_config), _VP, ctypes.POINTER(_VP)]),
@@ -89,6 +97,10 @@ _SIGS = {
     "c2kv_attend_noalloc": (_I32, [_VP, _VP, _I32, _VP, _VP, _VP, _I32, _VP, _VP]),
     "c2kv_decode": (_I32, [_VP, _VP, _I32, _VP, _VP, _VP, _P32, _VP, _VP]),
     "c2kv_extract_attention": (_I32, [_VP, _I32, _VP, _VP, _VP, _I32, _I32, _VP, _VP]),
+    "c2kv_paged_append": (_I32, [_VP, _VP, _I32, _VP, _I32, _I64, _P32, _P32, _VP, _VP, _I64, _VP]),
+    "c2kv_paged_gather": (_I32, [_VP, _VP, _I32, _VP, _I32, _I64, _P32, _P32, _VP, _VP, _I64, _VP]),
+    "c2kv_paged_attend": (_I32, [_VP, _VP, _I32, _VP, _I32, _I64, _P32, _P32, _I32, _VP, _I64, _VP, _VP, _VP]),
+    "c2kv_verify_drafts": (_I32, [_VP, _I32, _P32, _I32, _VP, _VP, _I64, _VP, _I64, _VP, _VP, _VP, _VP]),
     "c2kv_cache_release": (_I32, [_VP, _VP]),
     "c2kv_sync": (_I32, [_VP]),
     "c2kv_last_error": (ctypes.c_char_p, [_VP]),
@@ -256,6 +268,95 @@ def c2kv_extract_attention(ctx, n_layers, q, k, v, n_tokens, ratio_k, out, lse=N
     """SIF-masked extraction attention over [document tokens; C2 tokens] of one chunk."""
     _check(_lib.c2kv_extract_attention(ctx, n_layers, _ptr(q), _ptr(k), _ptr(v), n_tokens,
                                        ratio_k, _ptr(out), _ptr(lse)), ctx)
+
+
+def make_pages(k, v, k_scale=None, v_scale=None):
+    """Describe pages in torch tensors: k, v [n_pages, Hkv, page_size, d] in the context's type, or
+    8-bit (torch.float8_e4m3fn or uint8 codes) with fp32 scales [n_pages, Hkv, page_size].  The
+    description keeps the tensors."""
+    n, _, rows, d = k.shape
+    eight = k.element_size() == 1
+    for x, inner in ((k, (rows * d, d, 1)), (v, (rows * d, d, 1)), (k_scale, (rows, 1)), (v_scale, (rows, 1))):
+        if x is not None and x.stride()[1:] != inner:
+            raise ValueError("a page must be one dense block of its heads' rows")
+    if v.shape != k.shape or v.dtype != k.dtype or (n > 1 and v.stride(0) != k.stride(0)):
+        raise ValueError("k and v pages must have one shape, type and stride")
+    if eight and (k_scale is None or v_scale is None or k_scale.shape != k.shape[:3] or v_scale.shape != k.shape[:3] or
+                  k_scale.element_size() != 4 or v_scale.element_size() != 4 or
+                  (n > 1 and v_scale.stride(0) != k_scale.stride(0))):
+        raise ValueError("8-bit pages need fp32 scales [n_pages, Hkv, page_size], of one stride")
+    p = c2kv_pages(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), k.stride(0) if n > 1 else 0,
+                   k_scale.stride(0) if eight and n > 1 else 0, n, rows, PAGES_E4M3 if eight else PAGES_NATIVE)
+    p.keep = (k, v, k_scale, v_scale)
+    p.address = ctypes.addressof(p)
+    return p
+
+
+def _table(table, batch, rows):
+    """Address, width and row stride of a table of page numbers (a torch int32 tensor [B, width]) for
+    the requests that a call's host arrays describe."""
+    b, w = table.shape
+    if b != batch or len(rows) != batch:
+        raise ValueError("the table, the ranges and the rows must describe one batch")
+    if table.element_size() != 4 or (w > 1 and table.stride(1) != 1):
+        raise ValueError("a table's rows must be dense int32")
+    return table.data_ptr(), w, table.stride(0) if b > 1 else w
+
+
+def c2kv_paged_append(ctx, pages, table, new_ptr, start, k, v, turn=None):
+    """Write new tokens k, v [T, Hkv, d] into their requests' pages, K turned by turn [T]."""
+    ptr, ptr_p = _i32(new_ptr)
+    st, st_p = _i32(start)
+    batch = len(ptr) - 1
+    tb, w, ts = _table(table, batch, st)
+    _check(_lib.c2kv_paged_append(ctx, pages.address, batch, tb, w, ts, ptr_p, st_p, _ptr(k), _ptr(v),
+                                  _token_stride(k, v), _ptr(turn)), ctx)
+
+
+def c2kv_paged_gather(ctx, pages, table, row_ptr, start, k_out, v_out, turn=None):
+    """Read rows of the pages back into k_out, v_out [T, Hkv, d], K turned by turn [T]."""
+    ptr, ptr_p = _i32(row_ptr)
+    st, st_p = _i32(start)
+    batch = len(ptr) - 1
+    tb, w, ts = _table(table, batch, st)
+    _check(_lib.c2kv_paged_gather(ctx, pages.address, batch, tb, w, ts, ptr_p, st_p, _ptr(k_out), _ptr(v_out),
+                                  _token_stride(k_out, v_out), _ptr(turn)), ctx)
+
+
+def c2kv_paged_attend(ctx, pages, table, q_ptr, n_keys, q, out, lse=None, turn=None, window=0):
+    """Attention of each request's newest tokens q [T, Hq, d] over its n_keys rows."""
+    ptr, ptr_p = _i32(q_ptr)
+    nk, nk_p = _i32(n_keys)
+    batch = len(ptr) - 1
+    tb, w, ts = _table(table, batch, nk)
+    _check(_lib.c2kv_paged_attend(ctx, pages.address, batch, tb, w, ts, ptr_p, nk_p, window, _ptr(q),
+                                  _token_stride(q), _ptr(turn), _ptr(out), _ptr(lse)), ctx)
+
+
+def c2kv_verify_drafts(ctx, draft_ptr, tokens, p, q, u_accept, u_next, n_accepted, next_token):
+    """Accept drafted tokens against the target's probabilities p [T + B, V] and the draft's q [T, V]
+    (None: drafts without probabilities), and draw the token that follows them."""
+    ptr, ptr_p = _i32(draft_ptr)
+    _check(_lib.c2kv_verify_drafts(ctx, len(ptr) - 1, ptr_p, p.shape[1], _ptr(tokens), _ptr(p), _row_stride(p), _ptr(q),
+                                   _row_stride(q), _ptr(u_accept), _ptr(u_next), _ptr(n_accepted), _ptr(next_token)), ctx)
+
+
+def _token_stride(*tensors):
+    """Elements between tokens of torch tensors [T, heads, d] whose heads are dense (0: as they are)."""
+    s = 0
+    for x in tensors:
+        t, h, d = x.shape
+        if (h > 1 and x.stride(1) != d) or x.stride(2) != 1:
+            raise ValueError("a token's heads must be one dense block")
+        mine = x.stride(0) if t > 1 else 0
+        if s and mine and mine != s:
+            raise ValueError("tensors of one call must have one token stride")
+        s = mine or s
+    return s
+
+
+def _row_stride(x):
+    return 0 if x is None or x.shape[0] < 2 else x.stride(0)
 
 
 def c2kv_cache_release(ctx, cache):

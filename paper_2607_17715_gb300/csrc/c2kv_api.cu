@@ -1808,6 +1808,30 @@ MemKind mem_kind(const void* p) {
     return MemKind::kUnknown;
 }
 
+bool context_view(const c2kv_ctx* c, ContextView* v) {
+    if (!c || !v) return false;
+    *v = ContextView{c->cfg.n_q_heads, c->cfg.n_kv_heads, c->cfg.head_dim, c->cfg.dtype, c->sms, c->stream, c->d_err, &c->turns};
+    return true;
+}
+
+TraceScope::TraceScope(c2kv_ctx* c, int kind) : ctx_(c), kind_(kind), begin_(nullptr) {
+    if (!c->prof) return;
+    cudaEvent_t a = prof_event(c);
+    if (a) cudaEventRecord(a, c->stream);
+    begin_ = a;
+}
+
+TraceScope::~TraceScope() {
+    if (!begin_) return;
+    cudaEvent_t a = static_cast<cudaEvent_t>(begin_), b = prof_event(ctx_);
+    if (!b) {
+        ctx_->prof_free.push_back(a);
+        return;
+    }
+    cudaEventRecord(b, ctx_->stream);
+    ctx_->prof_recs.push_back({kind_, a, b});
+}
+
 int32_t set_last_error(c2kv_ctx* c, int32_t code, const char* msg) {
     if (c) c->err = msg ? msg : "";
     return code;

@@ -377,4 +377,26 @@ bool attend_view(const c2kv_ctx* ctx, const c2kv_cache* cache, AttendView* v);
 void note_suffix_written(c2kv_cache* cache, int32_t l0, int32_t n, int32_t n_suffix);
 // Records `msg` as the context's last error and returns `code`.
 int32_t set_last_error(c2kv_ctx* ctx, int32_t code, const char* msg);
+
+// What entry points outside c2kv_api.cu need of a context (the paged calls); false for no context.
+struct ContextView {
+    int32_t n_q_heads, n_kv_heads, head_dim, dtype, sms;
+    cudaStream_t stream;
+    int32_t* err;
+    const RopeTurns* turns;
+};
+bool context_view(const c2kv_ctx* ctx, ContextView* v);
+// Brackets the launches made in its lifetime with the trace's events, when a trace is on.
+class TraceScope {
+public:
+    TraceScope(c2kv_ctx* ctx, int kind);
+    ~TraceScope();
+    TraceScope(const TraceScope&) = delete;
+    TraceScope& operator=(const TraceScope&) = delete;
+
+private:
+    c2kv_ctx* ctx_;
+    int kind_;
+    void* begin_;            // cudaEvent_t, or null
+};
 }  // namespace c2kv

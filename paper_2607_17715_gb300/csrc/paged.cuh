@@ -1,0 +1,147 @@
+// Paged caches: parameters and launchers shared by the paged calls' translation units.
+//
+// A page holds page_size rows of every KV head, head-major ([Hkv][page_size][d]), so that one
+// head's rows of a page are one contiguous run: what an attention CTA, which works on one KV
+// head, reads.  Row j of request r lives in page table[r][j / page_size].
+#pragma once
+
+#include "internal.cuh"
+
+namespace c2kv {
+
+// Requests a launch carries in its parameter block: a launch's latency grows by about 0.4 us for
+// each KB of parameters, so calls of few requests take the small block.
+constexpr int kPagedFew = 32;
+constexpr int kPagedMany = 256;
+
+struct PageView {
+    void* k;                 // [n_pages][Hkv][page_size][d]: the context's type, or E4M3 codes
+    void* v;
+    float* k_scale;          // [n_pages][Hkv][page_size] (E4M3)
+    float* v_scale;
+    const int32_t* table;    // [batch][table_stride]: page of rows j * page_size ..
+    int64_t page_stride;     // elements between pages
+    int64_t scale_stride;    // scales between pages
+    int64_t table_stride;
+    int32_t n_pages;
+    int32_t page_shift;      // log2(page_size)
+};
+
+// Rows of new (or old) tokens moved between a dense block [T][Hkv][d] and pages.
+template <int kReq>
+struct PagedMove {
+    PageView pg;
+    void* k;                 // dense [T] rows, stride elements apart
+    void* v;
+    int64_t stride;
+    const int32_t* turn;     // [T] positions that K turns by, or null
+    int32_t* err;            // device error word: bit 0 = index refused
+    int32_t batch;
+    int32_t b0;              // table row of the launch's first request
+    int32_t hkv;
+    int32_t tokens_per_cta;
+    int32_t t0;              // first token of this launch
+    int32_t t1;              // one past its last
+    RopeTurns rope;
+    int32_t ptr[kReq + 1];   // tokens [ptr[r], ptr[r + 1]) are request r's ...
+    int32_t start[kReq];     // ... rows start[r] ..
+};
+
+// Moves tokens [ptr[0], ptr[batch]) of the call's `batch` requests, kPagedMany requests a launch.
+struct PagedMoveCall {
+    PageView pg;
+    void* k;
+    void* v;
+    int64_t stride;
+    const int32_t* turn;
+    int32_t* err;
+    int32_t hkv;
+    int32_t batch;
+    const int32_t* ptr;      // host [batch + 1]
+    const int32_t* start;    // host [batch]
+    const RopeTurns* rope;
+};
+cudaError_t launch_paged_append(const PagedMoveCall& c, int dtype, int d, bool codes, cudaStream_t s);
+cudaError_t launch_paged_gather(const PagedMoveCall& c, int dtype, int d, bool codes, cudaStream_t s);
+
+// One request of an attention launch: queries [q0, q0 + nq) are the last nq of its n_keys rows.
+struct PagedReq {
+    int32_t q0;
+    int32_t nq;
+    int32_t n_keys;
+    int32_t item0;           // first work item of the request
+};
+
+template <int kReq>
+struct PagedAttn {
+    PageView pg;
+    const void* q;           // [T] rows of [Hq][d], q_stride elements apart, before RoPE
+    void* out;               // [T][Hq][d]
+    float* lse;              // [Hq][T] natural log, or null
+    const int32_t* turn;     // [T] positions that the queries turn by, or null
+    int32_t* err;
+    int64_t q_stride;
+    int64_t n_tokens;        // T
+    int32_t batch;
+    int32_t b0;
+    int32_t hq;
+    int32_t hkv;
+    int32_t window;          // a query sees at most the last `window` rows up to its own (0: all)
+    float scale_log2;        // log2(e) / sqrt(d)
+    RopeTurns rope;
+    PagedReq req[kReq];
+};
+
+struct PagedAttnCall {
+    PageView pg;
+    const void* q;
+    void* out;
+    float* lse;
+    const int32_t* turn;
+    int32_t* err;
+    int64_t q_stride;
+    int32_t hq;
+    int32_t hkv;
+    int32_t window;
+    int32_t batch;
+    const int32_t* ptr;      // host [batch + 1]
+    const int32_t* n_keys;   // host [batch]
+    const RopeTurns* rope;
+};
+cudaError_t launch_paged_attn(const PagedAttnCall& c, int dtype, int d, bool codes, cudaStream_t s);
+
+// Drafted tokens against the target's probabilities (verify.cu).
+template <int kReq>
+struct VerifyParams {
+    const int32_t* tokens;   // [T] drafted tokens
+    const float* p;          // target's probabilities, p_stride apart: request r's rows ptr[r] + r ..
+    const float* q;          // draft's, q_stride apart, or null (a draft that is sure of its tokens)
+    const float* u_accept;   // [T]
+    const float* u_next;     // [B]
+    int32_t* n_accepted;     // [B]
+    int32_t* next_token;     // [B]
+    int32_t* err;
+    int64_t p_stride;
+    int64_t q_stride;
+    int32_t vocab;
+    int32_t b0;
+    int32_t ptr[kReq + 1];
+};
+struct VerifyCall {
+    const int32_t* tokens;
+    const float* p;
+    const float* q;
+    const float* u_accept;
+    const float* u_next;
+    int32_t* n_accepted;
+    int32_t* next_token;
+    int32_t* err;
+    int64_t p_stride;
+    int64_t q_stride;
+    int32_t vocab;
+    int32_t batch;
+    const int32_t* ptr;      // host [batch + 1]
+};
+cudaError_t launch_verify(const VerifyCall& c, cudaStream_t s);
+
+}  // namespace c2kv

@@ -1,0 +1,220 @@
+// Verification of drafted tokens (c2kv_verify_drafts): how many of a request's drafts the target's
+// probabilities accept, and the token that follows them, from given random numbers.
+//
+// Draft i (token x) is accepted while u_i q_i(x) < p_i(x).  At the first refusal the next token comes
+// from max(p - q, 0), after the last draft from p, by inverse CDF: weights are whole multiples of
+// 2^-44, so their sums are the same in any order and the drawn token does not depend on how the
+// vocabulary is split.
+//
+// Two rows of the vocabulary are read once a request, which bounds the call at HBM's rate for a batch
+// and at the chain draft -> probabilities -> sum -> search for one request.  A cluster of CTAs shares a
+// request: each warp sums one contiguous stretch, the CTAs exchange their totals through distributed
+// shared memory, and the warp whose stretch holds the goal reads that stretch again (from L2).
+#include "paged.cuh"
+
+#include <algorithm>
+
+namespace c2kv {
+namespace {
+
+constexpr int kVerThreads = 512;
+constexpr int kVerWarps = kVerThreads / 32;
+constexpr int kMaxCluster = 8;
+
+__device__ __forceinline__ uint64_t warp_sum(uint64_t x) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+
+// A weight in [0, 1] as a multiple of 2^-44, cut off; NaN counts as 0 (fmaxf gives its other operand).
+__device__ __forceinline__ uint64_t whole(float w) {
+    return __float2ull_rz(fminf(fmaxf(w, 0.f), 1.f) * 0x1p44f);
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+// The 8 bytes at this CTA's shared address `local`, in the cluster's CTA `rank`.
+__device__ __forceinline__ uint64_t ld_peer(const uint64_t* local, uint32_t rank) {
+    const uint32_t a = static_cast<uint32_t>(__cvta_generic_to_shared(local));
+    uint32_t peer;
+    uint64_t v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(peer) : "r"(a), "r"(rank));
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(peer) : "memory");
+    return v;
+}
+
+// Weight of token i: what p leaves over q (q may be null), or p without the refused token `drop`.
+struct Row {
+    const float* p;
+    const float* q;
+    int drop;
+    __device__ __forceinline__ uint64_t at(int i) const {
+        const float w = q ? __ldg(p + i) - __ldg(q + i) : __ldg(p + i);
+        return i == drop ? 0 : whole(w);
+    }
+};
+
+// The sum of a warp's stretch [a, b), each lane's part summed over eight loads at a time.
+__device__ __forceinline__ uint64_t stretch_sum(const Row& w, int a, int b, int lane) {
+    uint64_t sum = 0;
+    int i = a + lane;
+    for (; i + 7 * 32 < b; i += 8 * 32) {
+        float x[8], y[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            x[u] = __ldg(w.p + i + 32 * u);
+            y[u] = w.q ? __ldg(w.q + i + 32 * u) : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) sum += i + 32 * u == w.drop ? 0 : whole(x[u] - y[u]);
+    }
+    for (; i < b; i += 32) sum += w.at(i);
+    return warp_sum(sum);
+}
+
+template <int kReq>
+__global__ void __launch_bounds__(kVerThreads) verify_kernel(const __grid_constant__ VerifyParams<kReq> P) {
+    __shared__ uint64_t s_warp[kVerWarps];
+    __shared__ uint64_t s_total;
+    __shared__ int s_accepted;
+    const uint32_t rank = cluster_rank(), n_cta = cluster_size();
+    const int r = blockIdx.x / n_cta, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int lo = P.ptr[r], n = P.ptr[r + 1] - lo, V = P.vocab;
+    const int64_t p_row = (int64_t)lo + P.b0 + r;         // the request's first row of p
+    if (warp == 0) {
+        int a = 0;
+        for (; a < n; a += 32) {
+            bool yes = true;
+            if (a + lane < n) {
+                const int x = __ldg(P.tokens + lo + a + lane);
+                yes = x >= 0 && x < V;
+                if (!yes) {
+                    if (rank == 0) atomicOr(P.err, 1);
+                } else {
+                    const float px = __ldg(P.p + (p_row + a + lane) * P.p_stride + x);
+                    const float qx = P.q ? __ldg(P.q + (int64_t)(lo + a + lane) * P.q_stride + x) : 1.f;
+                    yes = __fmul_rn(__ldg(P.u_accept + lo + a + lane), qx) < px;
+                }
+            }
+            const uint32_t no = __ballot_sync(0xffffffffu, !yes);
+            if (no) {
+                a += __ffs(no) - 1;
+                break;
+            }
+        }
+        if (lane == 0) s_accepted = min(a, n);
+    }
+    __syncthreads();
+    const int acc = s_accepted;
+    Row w{P.p + (p_row + acc) * P.p_stride, nullptr, -1};
+    if (acc < n) {
+        if (P.q) w.q = P.q + (int64_t)(lo + acc) * P.q_stride;
+        else w.drop = __ldg(P.tokens + lo + acc);
+    }
+    // warps of the cluster take stretches of whole 32-element lines, in order
+    const int warps = kVerWarps * (int)n_cta;
+    const int per = ((V + warps - 1) / warps + 31) / 32 * 32;
+    const int64_t first = (int64_t)((int)rank * kVerWarps + warp) * per;
+    const int a = (int)min((int64_t)V, first), b = (int)min((int64_t)V, first + per);
+    uint64_t before = 0, total = 0;
+    for (int pass = 0; pass < 2; ++pass) {
+        const uint64_t mine = stretch_sum(w, a, b, lane);
+        if (lane == 0) s_warp[warp] = mine;
+        __syncthreads();
+        if (warp == 0) {
+            const uint64_t t = warp_sum(lane < kVerWarps ? s_warp[lane] : 0);
+            if (lane == 0) s_total = t;
+        }
+        cluster_sync();
+        before = total = 0;
+        for (uint32_t c = 0; c < n_cta; ++c) {
+            const uint64_t t = ld_peer(&s_total, c);
+            total += t;
+            if (c < rank) before += t;
+        }
+        cluster_sync();                    // read by all before anyone writes or leaves
+        if (total != 0 || pass == 1) break;
+        // nothing is left of p over q (a refusal that rounding made): p itself
+        w.q = nullptr;
+        w.drop = -1;
+    }
+    if (rank == 0 && threadIdx.x == 0) {
+        P.n_accepted[P.b0 + r] = acc;
+        if (total == 0) P.next_token[P.b0 + r] = -1;
+    }
+    if (total == 0) return;
+    const float uf = __ldg(P.u_next + P.b0 + r) * 0x1p24f;
+    const uint64_t u = min((uint64_t)__float2ull_rz(fmaxf(uf, 0.f)), (uint64_t)0xffffff);
+    const uint64_t goal = (total >> 24) * u + (((total & 0xffffff) * u) >> 24);
+    for (int i = 0; i < warp; ++i) before += s_warp[i];
+    if (goal < before || goal >= before + s_warp[warp]) return;
+    // the first token of the stretch whose running sum passes the goal
+    for (int i = a; i < b; i += 32) {
+        const uint64_t x = i + lane < b ? w.at(i + lane) : 0;
+        uint64_t upto = x;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint64_t y = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += y;
+        }
+        const uint32_t past = __ballot_sync(0xffffffffu, before + upto > goal);
+        if (past) {
+            if (lane == __ffs(past) - 1) P.next_token[P.b0 + r] = i + lane;
+            return;
+        }
+        before += __shfl_sync(0xffffffffu, upto, 31);
+    }
+}
+
+template <int kReq>
+cudaError_t launch(const VerifyCall& c, cudaStream_t s) {
+    for (int b0 = 0; b0 < c.batch; b0 += kReq) {
+        const int nb = std::min(c.batch - b0, kReq);
+        VerifyParams<kReq> P;
+        P.tokens = c.tokens;
+        P.p = c.p;
+        P.q = c.q;
+        P.u_accept = c.u_accept;
+        P.u_next = c.u_next;
+        P.n_accepted = c.n_accepted;
+        P.next_token = c.next_token;
+        P.err = c.err;
+        P.p_stride = c.p_stride;
+        P.q_stride = c.q_stride;
+        P.vocab = c.vocab;
+        P.b0 = b0;
+        for (int i = 0; i <= nb; ++i) P.ptr[i] = c.ptr[b0 + i];
+        cudaLaunchConfig_t cfg{};
+        cudaLaunchAttribute at{};
+        at.id = cudaLaunchAttributeClusterDimension;
+        at.val.clusterDim = {kMaxCluster, 1, 1};
+        cfg.gridDim = dim3(nb * kMaxCluster);
+        cfg.blockDim = dim3(kVerThreads);
+        cfg.stream = s;
+        cfg.attrs = &at;
+        cfg.numAttrs = 1;
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, verify_kernel<kReq>, P);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace
+
+cudaError_t launch_verify(const VerifyCall& c, cudaStream_t s) {
+    return c.batch <= kPagedFew ? launch<kPagedFew>(c, s) : launch<kPagedMany>(c, s);
+}
+
+}  // namespace c2kv
