@@ -73,6 +73,15 @@ struct c2kv_ctx {
     // launches (each unit's last split sets its counter back), cleared again after a device error
     uint32_t* tickets = nullptr;
     size_t tickets_cap = 0;
+    // scratch of the paged calls, one for each stream that they ran on (grown rarely)
+    struct Workspace {
+        cudaStream_t stream = nullptr;
+        void* p = nullptr;
+        size_t bytes = 0;
+        uint32_t* counters = nullptr;
+        size_t n = 0;
+    };
+    std::vector<Workspace> workspaces;
     c2kv::RopeTurns turns{};
     // second stream and events of the pipelined compose + attend (host-resident chunks)
     cudaStream_t aux = nullptr;
@@ -367,6 +376,10 @@ c2kv_status c2kv_destroy(c2kv_ctx* c) {
         if (c->pool_v) cudaFree(c->pool_v);
         if (c->d_err) cudaFree(c->d_err);
         if (c->tickets) cudaFree(c->tickets);
+        for (auto& w : c->workspaces) {
+            if (w.p) cudaFree(w.p);
+            if (w.counters) cudaFree(w.counters);
+        }
         delete c;
         return C2KV_OK;
     } catch (...) {
@@ -1700,6 +1713,8 @@ c2kv_status c2kv_sync(c2kv_ctx* c) {
         cudaMemset(c->d_err, 0, sizeof(int32_t));
         // a launch that gave up may have left split-merge counters part-way
         if (c->tickets) cudaMemsetAsync(c->tickets, 0, c->tickets_cap * sizeof(uint32_t), c->stream);
+        for (auto& w : c->workspaces)
+            if (w.counters && w.stream == c->stream) cudaMemsetAsync(w.counters, 0, w.n * sizeof(uint32_t), c->stream);
         return fail(c, C2KV_ERR_DEVICE_BOUNDS, "sync: a kernel refused an out-of-range index (flags 0x%x)", word);
     }
     return C2KV_OK;
@@ -1812,6 +1827,45 @@ bool context_view(const c2kv_ctx* c, ContextView* v) {
     if (!c || !v) return false;
     *v = ContextView{c->cfg.n_q_heads, c->cfg.n_kv_heads, c->cfg.head_dim, c->cfg.dtype, c->sms, c->stream, c->d_err, &c->turns};
     return true;
+}
+
+cudaError_t context_workspace(c2kv_ctx* c, size_t bytes, size_t counters, void** p, uint32_t** cnt) {
+    auto w = std::find_if(c->workspaces.begin(), c->workspaces.end(),
+                          [&](const c2kv_ctx::Workspace& x) { return x.stream == c->stream; });
+    if (w == c->workspaces.end()) {
+        c->workspaces.emplace_back();
+        w = c->workspaces.end() - 1;
+        w->stream = c->stream;
+    }
+    cudaError_t e = cudaSuccess;
+    if (w->bytes < bytes || w->n < counters) e = cudaStreamSynchronize(c->stream);   // it may be in use
+    if (e == cudaSuccess && w->bytes < bytes) {
+        if (w->p) cudaFree(w->p);
+        w->p = nullptr;
+        w->bytes = 0;
+        const size_t cap = std::max(bytes + bytes / 4, (size_t)4 << 20);
+        e = cudaMalloc(&w->p, cap);
+        if (e == cudaSuccess) w->bytes = cap;
+        else w->p = nullptr;
+    }
+    if (e == cudaSuccess && w->n < counters) {
+        if (w->counters) cudaFree(w->counters);
+        w->counters = nullptr;
+        w->n = 0;
+        const size_t cap = std::max<size_t>(2 * counters, 4096);
+        void* q = nullptr;
+        e = cudaMalloc(&q, cap * sizeof(uint32_t));
+        if (e == cudaSuccess) e = cudaMemsetAsync(q, 0, cap * sizeof(uint32_t), c->stream);
+        if (e == cudaSuccess) {
+            w->counters = static_cast<uint32_t*>(q);
+            w->n = cap;
+        } else if (q) {
+            cudaFree(q);
+        }
+    }
+    *p = w->p;
+    *cnt = w->counters;
+    return e;
 }
 
 TraceScope::TraceScope(c2kv_ctx* c, int kind) : ctx_(c), kind_(kind), begin_(nullptr) {

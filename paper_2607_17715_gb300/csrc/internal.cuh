@@ -386,6 +386,9 @@ struct ContextView {
     const RopeTurns* turns;
 };
 bool context_view(const c2kv_ctx* ctx, ContextView* v);
+// At least `bytes` of device memory and `counters` counters, zero between launches, for work on the
+// context's current stream: kept for the stream, so that calls on different streams do not share them.
+cudaError_t context_workspace(c2kv_ctx* ctx, size_t bytes, size_t counters, void** p, uint32_t** c);
 // Brackets the launches made in its lifetime with the trace's events, when a trace is on.
 class TraceScope {
 public:

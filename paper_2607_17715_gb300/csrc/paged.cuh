@@ -67,9 +67,12 @@ cudaError_t launch_paged_gather(const PagedMoveCall& c, int dtype, int d, bool c
 // One request of an attention launch: queries [q0, q0 + nq) are the last nq of its n_keys rows.
 struct PagedReq {
     int32_t q0;
-    int32_t nq;
+    int32_t nq;              // at least 1
     int32_t n_keys;
+    int32_t row;             // its row of the table
     int32_t item0;           // first work item of the request
+    int32_t splits;          // stretches that its keys are cut into
+    int32_t unit0;           // first unit (row tile of a KV head)
 };
 
 template <int kReq>
@@ -83,7 +86,6 @@ struct PagedAttn {
     int64_t q_stride;
     int64_t n_tokens;        // T
     int32_t batch;
-    int32_t b0;
     int32_t hq;
     int32_t hkv;
     int32_t window;          // a query sees at most the last `window` rows up to its own (0: all)
@@ -93,6 +95,7 @@ struct PagedAttn {
 };
 
 struct PagedAttnCall {
+    c2kv_ctx* ctx;           // whose workspace holds the partials of split keys
     PageView pg;
     const void* q;
     void* out;
@@ -109,6 +112,27 @@ struct PagedAttnCall {
     const RopeTurns* rope;
 };
 cudaError_t launch_paged_attn(const PagedAttnCall& c, int dtype, int d, bool codes, cudaStream_t s);
+// bf16 queries of n requests on mma.sync (paged_mma.cu).
+cudaError_t launch_paged_mma(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
+
+template <int kReq>
+void fill_paged(PagedAttn<kReq>& P, const PagedAttnCall& c, int d, const PagedReq* req, int n) {
+    P.pg = c.pg;
+    P.q = c.q;
+    P.out = c.out;
+    P.lse = c.lse;
+    P.turn = c.turn;
+    P.err = c.err;
+    P.q_stride = c.q_stride;
+    P.n_tokens = c.ptr[c.batch];
+    P.batch = n;
+    P.hq = c.hq;
+    P.hkv = c.hkv;
+    P.window = c.window;
+    P.scale_log2 = (float)(1.4426950408889634 / __builtin_sqrt((double)d));
+    P.rope = *c.rope;
+    for (int i = 0; i < n; ++i) P.req[i] = req[i];
+}
 
 // Drafted tokens against the target's probabilities (verify.cu).
 template <int kReq>

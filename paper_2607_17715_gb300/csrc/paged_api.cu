@@ -170,6 +170,7 @@ c2kv_status c2kv_paged_attend(c2kv_ctx* ctx, const c2kv_pages* pages, int32_t ba
             return refuse(ctx, C2KV_ERR_ARG, "%s: q, out must be 16-byte aligned", what);
         st = check_device(ctx, what, {pages->k, pages->v, a.pg.k_scale, a.pg.v_scale, table, q, out, lse, turn});
         if (st != C2KV_OK) return st;
+        a.ctx = ctx;
         a.q = q;
         a.out = out;
         a.lse = lse;

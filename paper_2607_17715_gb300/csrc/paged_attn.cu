@@ -3,6 +3,7 @@
 #include "paged_row.cuh"
 
 #include <algorithm>
+#include <vector>
 
 namespace c2kv {
 namespace {
@@ -24,7 +25,7 @@ __global__ void __launch_bounds__(kRowWarps * 32) paged_row_kernel(const __grid_
     const int lo = P.window ? max(0, hi - P.window) : 0;
     float q[C], o[C], m, l;
     lane_query<T, D>(P, t, h, lane, q);
-    row_attend<T, D, kCodes>(P, q, r, hk, lo + warp, hi, kRowWarps, lane, m, l, o);
+    row_attend<T, D, kCodes>(P, q, R.row, hk, lo + warp, hi, kRowWarps, lane, m, l, o);
     if (lane == 0) {
         s_m[warp] = m;
         s_l[warp] = l;
@@ -50,35 +51,13 @@ __global__ void __launch_bounds__(kRowWarps * 32) paged_row_kernel(const __grid_
     if (P.lse && lane == 0) P.lse[(int64_t)h * P.n_tokens + t] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
 }
 
-template <int kReq>
-void fill(PagedAttn<kReq>& P, const PagedAttnCall& c, int d, int b0, int nb) {
-    P.pg = c.pg;
-    P.q = c.q;
-    P.out = c.out;
-    P.lse = c.lse;
-    P.turn = c.turn;
-    P.err = c.err;
-    P.q_stride = c.q_stride;
-    P.n_tokens = c.ptr[c.batch];
-    P.batch = nb;
-    P.b0 = b0;
-    P.hq = c.hq;
-    P.hkv = c.hkv;
-    P.window = c.window;
-    P.scale_log2 = (float)(1.4426950408889634 / __builtin_sqrt((double)d));
-    P.rope = *c.rope;
-    for (int i = 0; i < nb; ++i)
-        P.req[i] = PagedReq{c.ptr[b0 + i], c.ptr[b0 + i + 1] - c.ptr[b0 + i], c.n_keys[b0 + i], 0};
-}
-
 template <typename T, int D, bool kCodes, int kReq>
-cudaError_t launch_rows(const PagedAttnCall& c, cudaStream_t s) {
-    for (int b0 = 0; b0 < c.batch; b0 += kReq) {
-        const int nb = std::min(c.batch - b0, kReq);
+cudaError_t launch_rows(const PagedAttnCall& c, const PagedReq* req, int n, cudaStream_t s) {
+    for (int b0 = 0; b0 < n; b0 += kReq) {
+        const int nb = std::min(n - b0, kReq);
         PagedAttn<kReq> P;
-        fill(P, c, D, b0, nb);
-        const int tokens = c.ptr[b0 + nb] - c.ptr[b0];
-        if (!tokens) continue;
+        fill_paged(P, c, D, req + b0, nb);
+        const int tokens = req[b0 + nb - 1].q0 + req[b0 + nb - 1].nq - req[b0].q0;
         paged_row_kernel<T, D, kCodes, kReq><<<tokens * c.hq, kRowWarps * 32, 0, s>>>(P);
         const cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
@@ -87,17 +66,23 @@ cudaError_t launch_rows(const PagedAttnCall& c, cudaStream_t s) {
 }
 
 template <typename T, int D>
-cudaError_t rows_of(const PagedAttnCall& c, bool codes, cudaStream_t s) {
-    const bool few = c.batch <= kPagedFew;
-    if (codes) return few ? launch_rows<T, D, true, kPagedFew>(c, s) : launch_rows<T, D, true, kPagedMany>(c, s);
-    return few ? launch_rows<T, D, false, kPagedFew>(c, s) : launch_rows<T, D, false, kPagedMany>(c, s);
+cudaError_t rows_of(const PagedAttnCall& c, const PagedReq* req, int n, bool codes, cudaStream_t s) {
+    const bool few = n <= kPagedFew;
+    if (codes) return few ? launch_rows<T, D, true, kPagedFew>(c, req, n, s) : launch_rows<T, D, true, kPagedMany>(c, req, n, s);
+    return few ? launch_rows<T, D, false, kPagedFew>(c, req, n, s) : launch_rows<T, D, false, kPagedMany>(c, req, n, s);
 }
 
 }  // namespace
 
 cudaError_t launch_paged_attn(const PagedAttnCall& c, int dtype, int d, bool codes, cudaStream_t s) {
-    if (dtype == kDtypeF32) return d == 128 ? rows_of<float, 128>(c, codes, s) : rows_of<float, 64>(c, codes, s);
-    return d == 128 ? rows_of<__nv_bfloat16, 128>(c, codes, s) : rows_of<__nv_bfloat16, 64>(c, codes, s);
+    std::vector<PagedReq> req;
+    req.reserve(c.batch);
+    for (int r = 0; r < c.batch; ++r)
+        if (c.ptr[r + 1] > c.ptr[r]) req.push_back(PagedReq{c.ptr[r], c.ptr[r + 1] - c.ptr[r], c.n_keys[r], r, 0, 1, 0});
+    const int n = (int)req.size();
+    if (dtype == kDtypeF32)
+        return d == 128 ? rows_of<float, 128>(c, req.data(), n, codes, s) : rows_of<float, 64>(c, req.data(), n, codes, s);
+    return launch_paged_mma(c, req.data(), n, d, codes, s);
 }
 
 }  // namespace c2kv
