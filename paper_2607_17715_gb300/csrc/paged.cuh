@@ -115,6 +115,9 @@ cudaError_t launch_paged_attn(const PagedAttnCall& c, int dtype, int d, bool cod
 // bf16 queries of n requests on mma.sync (paged_mma.cu).
 cudaError_t launch_paged_mma(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
 
+// bf16 queries of n requests on tcgen05 (paged_tc.cu).
+cudaError_t launch_paged_tc(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
+
 template <int kReq>
 void fill_paged(PagedAttn<kReq>& P, const PagedAttnCall& c, int d, const PagedReq* req, int n) {
     P.pg = c.pg;

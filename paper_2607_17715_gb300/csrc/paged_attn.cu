@@ -9,6 +9,7 @@ namespace c2kv {
 namespace {
 
 constexpr int kRowWarps = 4;
+constexpr int kMmaRows = 64;             // query rows of a KV head up to which mma.sync takes a request
 
 // One query row a CTA, its keys dealt to four warps.
 template <typename T, int D, bool kCodes, int kReq>
@@ -82,7 +83,13 @@ cudaError_t launch_paged_attn(const PagedAttnCall& c, int dtype, int d, bool cod
     const int n = (int)req.size();
     if (dtype == kDtypeF32)
         return d == 128 ? rows_of<float, 128>(c, req.data(), n, codes, s) : rows_of<float, 64>(c, req.data(), n, codes, s);
-    return launch_paged_mma(c, req.data(), n, d, codes, s);
+    // requests of many rows on tcgen05, those of few on mma.sync
+    std::vector<PagedReq> few, many;
+    for (const PagedReq& q : req) ((int64_t)q.nq * (c.hq / c.hkv) > kMmaRows ? many : few).push_back(q);
+    cudaError_t e = cudaSuccess;
+    if (!many.empty()) e = launch_paged_tc(c, many.data(), (int)many.size(), d, codes, s);
+    if (e == cudaSuccess && !few.empty()) e = launch_paged_mma(c, few.data(), (int)few.size(), d, codes, s);
+    return e;
 }
 
 }  // namespace c2kv
