@@ -1829,6 +1829,9 @@ bool context_view(const c2kv_ctx* c, ContextView* v) {
     return true;
 }
 
+cudaError_t context_alloc(c2kv_ctx* c, void** p, size_t bytes) { return pool_alloc(c, p, bytes); }
+void context_free(c2kv_ctx* c, void* p) { pool_free(c, p); }
+
 cudaError_t context_workspace(c2kv_ctx* c, size_t bytes, size_t counters, void** p, uint32_t** cnt) {
     auto w = std::find_if(c->workspaces.begin(), c->workspaces.end(),
                           [&](const c2kv_ctx::Workspace& x) { return x.stream == c->stream; });

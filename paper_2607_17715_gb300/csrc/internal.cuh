@@ -386,6 +386,8 @@ struct ContextView {
     const RopeTurns* turns;
 };
 bool context_view(const c2kv_ctx* ctx, ContextView* v);
+cudaError_t context_alloc(c2kv_ctx* ctx, void** p, size_t bytes);    // stream-ordered, from the context's memory pool
+void context_free(c2kv_ctx* ctx, void* p);
 // At least `bytes` of device memory and `counters` counters, zero between launches, for work on the
 // context's current stream: kept for the stream, so that calls on different streams do not share them.
 cudaError_t context_workspace(c2kv_ctx* ctx, size_t bytes, size_t counters, void** p, uint32_t** c);

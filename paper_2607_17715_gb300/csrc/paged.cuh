@@ -115,8 +115,24 @@ cudaError_t launch_paged_attn(const PagedAttnCall& c, int dtype, int d, bool cod
 // bf16 queries of n requests on mma.sync (paged_mma.cu).
 cudaError_t launch_paged_mma(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
 
-// bf16 queries of n requests on tcgen05 (paged_tc.cu).
-cudaError_t launch_paged_tc(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
+// Tensor map of pages [n_pages][Hkv][page_size][d], elements of 16 bits or codes of 8.
+bool encode_page_map(CUtensorMap* tm, const void* base, const PageView& pg, int hkv, int d, bool codes, int box_channels,
+                     int box_rows, CUtensorMapSwizzle swizzle);
+// bf16 queries of n requests over 16-bit pages on tcgen05 (paged_tc.cu).
+cudaError_t launch_paged_tc(const PagedAttnCall& c, const PagedReq* req, int n, int d, cudaStream_t s);
+// E4M3 pages of n requests as 16-bit ones (paged_move.cu): request i's pages become pages first[i] .. of
+// `to`, of one size with them, and row i of to.table names them (-1 for a page that is none).
+struct PagedExpandCall {
+    PageView from, to;
+    int32_t* err;
+    int32_t hkv;
+    int32_t n;
+    const PagedReq* req;
+    const int32_t* page0;    // first page of each request that any query sees ...
+    const int32_t* pages;    // ... how many from there on
+    const int32_t* first;    // ... and the page of `to` that it becomes
+};
+cudaError_t launch_paged_expand(const PagedExpandCall& c, int d, cudaStream_t s);
 
 template <int kReq>
 void fill_paged(PagedAttn<kReq>& P, const PagedAttnCall& c, int d, const PagedReq* req, int n) {

@@ -73,6 +73,64 @@ cudaError_t rows_of(const PagedAttnCall& c, const PagedReq* req, int n, bool cod
     return few ? launch_rows<T, D, false, kPagedFew>(c, req, n, s) : launch_rows<T, D, false, kPagedMany>(c, req, n, s);
 }
 
+// Requests of many rows on tcgen05.  Their 8-bit pages are expanded to 16 bits first, in scratch that the
+// stream hands back; requests go in groups so that the scratch stays small beside the cache.
+constexpr int64_t kExpandBytes = (int64_t)512 << 20;
+
+cudaError_t launch_many(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s) {
+    if (!codes) return launch_paged_tc(c, req, n, d, s);
+    const int shift = c.pg.page_shift;
+    const int64_t page_bytes = ((int64_t)c.hkv << shift) * d * 2;
+    for (int b0 = 0; b0 < n;) {
+        std::vector<PagedReq> part;
+        std::vector<int32_t> page0, pages, first;
+        int64_t total = 0, width = 1;
+        for (; b0 < n; ++b0) {
+            const PagedReq& q = req[b0];
+            const int64_t seen = c.window ? std::max<int64_t>(0, (int64_t)q.n_keys - q.nq + 1 - c.window) : 0;   // the first row that a query sees
+            const int32_t lo = (int32_t)(seen >> shift), hi = (int32_t)(((int64_t)q.n_keys + (1 << shift) - 1) >> shift);
+            if (!part.empty() && (total + hi - lo) * page_bytes * 2 > kExpandBytes) break;
+            page0.push_back(lo);
+            pages.push_back(std::max(0, hi - lo));
+            first.push_back((int32_t)total);
+            total += pages.back();
+            width = std::max<int64_t>(width, hi);
+            part.push_back(q);
+        }
+        const int m = (int)part.size();
+        const size_t half = (size_t)std::max<int64_t>(1, total) * page_bytes;
+        void* p = nullptr;
+        cudaError_t e = context_alloc(c.ctx, &p, 2 * half + (size_t)m * width * 4);
+        if (e == cudaErrorMemoryAllocation) {           // no room: code by code, slower
+            (void)cudaGetLastError();
+            e = launch_paged_mma(c, part.data(), m, d, true, s);
+            if (e != cudaSuccess) return e;
+            continue;
+        }
+        if (e != cudaSuccess) return e;
+        PagedExpandCall x{};
+        x.from = c.pg;
+        x.to = PageView{p, static_cast<char*>(p) + half, nullptr, nullptr,
+                        reinterpret_cast<const int32_t*>(static_cast<char*>(p) + 2 * half), page_bytes / 2, 0, width,
+                        (int32_t)std::max<int64_t>(1, total), shift};
+        x.err = c.err;
+        x.hkv = c.hkv;
+        x.n = m;
+        x.req = part.data();
+        x.page0 = page0.data();
+        x.pages = pages.data();
+        x.first = first.data();
+        e = launch_paged_expand(x, d, s);
+        PagedAttnCall a = c;
+        a.pg = x.to;
+        for (int i = 0; i < m; ++i) part[i].row = i;
+        if (e == cudaSuccess) e = launch_paged_tc(a, part.data(), m, d, s);
+        context_free(c.ctx, p);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
 }  // namespace
 
 cudaError_t launch_paged_attn(const PagedAttnCall& c, int dtype, int d, bool codes, cudaStream_t s) {
@@ -87,7 +145,7 @@ cudaError_t launch_paged_attn(const PagedAttnCall& c, int dtype, int d, bool cod
     std::vector<PagedReq> few, many;
     for (const PagedReq& q : req) ((int64_t)q.nq * (c.hq / c.hkv) > kMmaRows ? many : few).push_back(q);
     cudaError_t e = cudaSuccess;
-    if (!many.empty()) e = launch_paged_tc(c, many.data(), (int)many.size(), d, codes, s);
+    if (!many.empty()) e = launch_many(c, many.data(), (int)many.size(), d, codes, s);
     if (e == cudaSuccess && !few.empty()) e = launch_paged_mma(c, few.data(), (int)few.size(), d, codes, s);
     return e;
 }

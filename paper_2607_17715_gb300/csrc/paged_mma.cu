@@ -184,10 +184,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2) paged_mma_kernel(const __grid_
         pages0 = pages1 = -1;
         if (i0 + lane >= n_it) return;
         const int key = (b0 + warp + (i0 + lane) * kWarps) * kBlk;
-        const bool two = boxes == 2 && key + 16 < k_hi;
-        pages0 = __ldg(table + (key >> P.pg.page_shift));
+        // (a page that a window has left behind may be gone from the table)
+        const bool one = boxes == 1 || key + 16 > k_lo, two = boxes == 2 && key + 16 < k_hi;
+        if (one) pages0 = __ldg(table + (key >> P.pg.page_shift));
         if (two) pages1 = __ldg(table + ((key + 16) >> P.pg.page_shift));
-        if (pages0 < 0 || pages0 >= P.pg.n_pages) {
+        if (one && (pages0 < 0 || pages0 >= P.pg.n_pages)) {
             atomicOr(P.err, 1);
             pages0 = -1;
         }
@@ -644,16 +645,6 @@ __global__ void __launch_bounds__(kWarps * 32, 2) paged_mma_kernel(const __grid_
 
 // ------------------------------------------------------------------ host side
 
-bool page_map(CUtensorMap* tm, const void* base, const PageView& pg, int hkv, int d, bool codes, int box_channels, int box_rows,
-              CUtensorMapSwizzle swizzle) {
-    const cuuint64_t eb = codes ? 1 : 2, rows = 1ull << pg.page_shift;
-    const cuuint64_t dims[4] = {(cuuint64_t)d, rows, (cuuint64_t)hkv, (cuuint64_t)pg.n_pages};
-    const cuuint64_t strides[3] = {d * eb, rows * d * eb, (cuuint64_t)pg.page_stride * eb};
-    const cuuint32_t box[4] = {(cuuint32_t)box_channels, (cuuint32_t)box_rows, 1, 1};
-    return encode_tensor_map(tm, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, base, dims, strides,
-                             box, swizzle);
-}
-
 template <int D, bool kCodes, int MT, int kReq>
 cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStream_t s) {
     using L = Lay<D, kCodes>;
@@ -713,8 +704,8 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
             X.part_lse = reinterpret_cast<float*>(static_cast<char*>(p) + o_bytes);
         }
         const auto swizzle = L::RB == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE;
-        if (!page_map(&X.tm_k, c.pg.k, c.pg, c.hkv, D, kCodes, L::BC, X.box_rows, swizzle) ||
-            !page_map(&X.tm_v, c.pg.v, c.pg, c.hkv, D, kCodes, L::BC, X.box_rows, swizzle))
+        if (!encode_page_map(&X.tm_k, c.pg.k, c.pg, c.hkv, D, kCodes, L::BC, X.box_rows, swizzle) ||
+            !encode_page_map(&X.tm_v, c.pg.v, c.pg, c.hkv, D, kCodes, L::BC, X.box_rows, swizzle))
             return cudaErrorInvalidValue;
         kernel<<<(unsigned)items, kWarps * 32, L::kSmem, s>>>(X);
         e = cudaGetLastError();
@@ -733,6 +724,16 @@ cudaError_t by_rows(const PagedAttnCall& c, const PagedReq* req, int n, cudaStre
 }
 
 }  // namespace
+
+bool encode_page_map(CUtensorMap* tm, const void* base, const PageView& pg, int hkv, int d, bool codes, int box_channels, int box_rows,
+              CUtensorMapSwizzle swizzle) {
+    const cuuint64_t eb = codes ? 1 : 2, rows = 1ull << pg.page_shift;
+    const cuuint64_t dims[4] = {(cuuint64_t)d, rows, (cuuint64_t)hkv, (cuuint64_t)pg.n_pages};
+    const cuuint64_t strides[3] = {d * eb, rows * d * eb, (cuuint64_t)pg.page_stride * eb};
+    const cuuint32_t box[4] = {(cuuint32_t)box_channels, (cuuint32_t)box_rows, 1, 1};
+    return encode_tensor_map(tm, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, base, dims, strides,
+                             box, swizzle);
+}
 
 cudaError_t launch_paged_mma(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s) {
     if (d == 128) return codes ? by_rows<128, true>(c, req, n, s) : by_rows<128, false>(c, req, n, s);

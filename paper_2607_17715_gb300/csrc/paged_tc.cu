@@ -5,13 +5,12 @@
 // tensor memory, and each tile's softmax (a warpgroup, a row a thread) runs beside the other tile's
 // products.  The tensor cores bound it, four products of 2 M multiply-adds a key tile and CTA.
 //
-// Loader threads bring the keys, not TMA: a tile of 128 keys is gathered from up to eight pages, rows
-// that no query may feel (past the last key, or of a page that is none) have to be zero in V whatever
-// memory holds, and E4M3 codes are turned to f16 on the way.  A row's scale is applied there, relative
-// to the power of two above the largest scale of its tile: f16 keeps 11 bits, and the tiles' powers of
-// two come back in the softmax, K's as a factor of the scores, V's as an offset of the exponent (the
-// running maximum is of score + offset, so that weights of every tile fit f16; the sum of weights
-// takes the offset back).  Queries are scaled to f16's range a row.  16-bit pages keep bf16 throughout.
+// A tile of 128 keys is gathered from up to eight pages by TMA, swizzled, straight into the operands'
+// tiles; rows of V that no query may feel (past the last key, or of a page that is none) are zeroed
+// there, whatever memory holds.  E4M3 pages are expanded to 16 bits first, once a call (see expand): to
+// turn codes in this kernel takes every CTA of a head the same work again, and its three idle warps
+// needed twice the time of the products (the conversion instruction is slow): 249 us against 124 for
+// 1216 tokens over 8384 rows.
 #include "paged.cuh"
 #include "paged_row.cuh"
 #include "per_device.cuh"
@@ -22,7 +21,7 @@
 #include <math_constants.h>
 
 #include <algorithm>
-#include <cuda_fp16.h>
+#include <climits>
 
 namespace c2kv {
 namespace {
@@ -30,78 +29,46 @@ namespace {
 constexpr int BM = 128;                  // rows of a query tile
 constexpr int BN = 128;                  // keys of a tile
 constexpr int kPair = 2 * BM;
-constexpr int kK = 3, kV = 2;            // stages of K and of V tiles
-constexpr int kUnits = 8;                // tiles whose powers of two are kept: more than K's stages
+constexpr int kUnits = 8;                // tiles whose notes are kept: more than K has stages
 
-// Warps 0..3 load, 4..7 and 8..11 are the softmax of tiles A and B, warp 12 issues the products.  The
-// softmax holds a row of scores in registers: 160 a thread, which warps 12..15 give.
-constexpr int kThreads = 512;
-constexpr int kRegsSoftmax = 160, kRegsLoad = 128, kRegsRest = 64;
-static_assert(128 * kRegsLoad + 256 * kRegsSoftmax + 128 * kRegsRest <= kThreads * 128, "register split");
+// Warp 0 issues the products, warp 1 loads, 4..7 and 8..11 are the softmax of tiles A and B, which holds
+// a row of scores in registers.
+constexpr int kThreads = 384;
+constexpr int kLaunchRegs = 168, kRegsLow = 136, kRegsSoftmax = 184;
+static_assert(128 * kRegsLow + 256 * kRegsSoftmax <= kThreads * kLaunchRegs, "register split");
 
 constexpr uint32_t kTmemCols = 512;      // S_A, S_B (P over their first halves), O_A, O_B
 constexpr uint32_t kColO = 256;
 
-enum { kBarKF = 0, kBarKE = kBarKF + kK, kBarVF = kBarKE + kK, kBarVE = kBarVF + kV, kBarS = kBarVE + kV, kBarP = kBarS + 2,
-       kBarO = kBarP + 2, kBarQ, kBars };
-
 template <int D>
 struct Tc {
-    static constexpr int kTile = BN * D * 2;               // bytes of a 16-bit tile
+    static constexpr int kK = 3, kV = 2;                   // stages of K and of V tiles
+    static constexpr int kTile = BN * D * 2;               // bytes of a tile
     static constexpr int kHalf = BN * 128;                 // of its 64-channel block
-    static constexpr int kTail = 8 * kBars + 16 + 16 * kUnits + 4 * kPair;
-    static constexpr int kSmem = 1024 /*align*/ + (2 + kK + kV) * kTile + kTail;
+    // barriers: tile landed / free (K, V), scores, weights, O, queries, and a V tile before its zeros
+    static constexpr int KF = 0, KE = KF + kK, VF = KE + kK, VE = VF + kV, S = VE + kV, P = S + 2, O = P + 2, Q = O + 1, VZ = Q + 1,
+                         kBars = VZ + 1;
+    static constexpr int kTiles = (2 + kK + kV) * kTile;
+    static constexpr int kNotes = kTiles + (8 * kBars + 15) / 16 * 16;
+    static constexpr int kSlot = kNotes + 4 * kUnits;
+    static constexpr int kSmem = 1024 /*align*/ + kSlot + 16;
 };
 static_assert(Tc<128>::kSmem <= 232448, "shared memory of a CTA");
 
-// What the loaders say of a key tile: K's power of two as a factor, V's as an exponent, and which of its
-// eight groups of 16 keys are in pages (bits).
-struct TileNote {
-    float k_unit;
-    float v_exp;
-    uint32_t there;
-    uint32_t pad;
-};
-
 template <int kReq>
 struct TcLaunch {
+    CUtensorMap tm_k, tm_v;              // [n_pages][Hkv][page_size][d], boxes of a page's rows and 64 channels
     float* part_o;                       // [item][256][D] normalised
     float* part_lse;                     // [item][256] log2 domain
     uint32_t* tickets;                   // [unit], zero between launches
     PagedAttn<kReq> a;
 };
 
-// kind::f16 with A and B both f16 or both bf16, D fp32, A K-major, B K- or MN-major.
-__host__ __device__ constexpr uint32_t idesc16(bool half, int m, int n, bool b_mn_major) {
-    return (1u << 4) | (half ? 0u : 1u << 7 | 1u << 10) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
-           ((uint32_t)(m >> 4) << 24);
-}
-
-template <bool kHalf>
-__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
-    uint32_t r;
-    if constexpr (kHalf) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-
-// Two E4M3 codes times a scale, as f16.
-__device__ __forceinline__ uint32_t scaled2(uint32_t codes, uint32_t scale2) {
-    uint32_t h, r;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)codes));
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(h), "r"(scale2));
-    return r;
-}
-
-__device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src, bool there) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
-
 // The CTA's work: rows [row0, row0 + live) of request R's KV head hk, key tiles [j0, j0 + n).
 struct Item {
     PagedReq R;
     int hk, sp, row0, live, j0, n, unit;
-    int first, k_lo, k_hi;               // the first row's last key; keys that some row sees: [k_lo, k_hi)
+    int k_lo, k_hi;                      // keys that some row sees: [k_lo, k_hi)
 };
 
 template <int kReq>
@@ -125,9 +92,8 @@ __device__ __forceinline__ Item find_item(const PagedAttn<kReq>& P) {
     w.row0 = pr * kPair;
     w.live = min(kPair, n_rows - w.row0);
     const int before = w.R.n_keys - w.R.nq;
-    w.first = before + w.row0 / G;
     w.k_hi = before + (w.row0 + w.live - 1) / G + 1;
-    w.k_lo = P.window ? max(0, w.first - P.window + 1) : 0;
+    w.k_lo = P.window ? max(0, before + w.row0 / G - P.window + 1) : 0;
     const int t_lo = w.k_lo / BN, t_n = max(0, (w.k_hi + BN - 1) / BN - t_lo);
     w.j0 = t_lo + (int)((int64_t)t_n * w.sp / w.R.splits);
     w.n = t_lo + (int)((int64_t)t_n * (w.sp + 1) / w.R.splits) - w.j0;
@@ -136,160 +102,78 @@ __device__ __forceinline__ Item find_item(const PagedAttn<kReq>& P) {
 
 // ------------------------------------------------------------------ loaders
 
-// 128 threads bring K and V tiles, K one stage ahead: rows thread / kChunks + kStep * i, one 16-byte
-// chunk of each.
-template <int D, bool kCodes, int kReq>
-__device__ __forceinline__ void load_tiles(const PagedAttn<kReq>& P, const Item& w, int thread, uint32_t sK, uint32_t sV,
-                                           uint32_t bars, TileNote* notes, volatile uint32_t* abort) {
-    constexpr int EB = kCodes ? 1 : 2;
-    constexpr int kChunks = D * EB / 16, kStep = 128 / kChunks, kPasses = kChunks;
+// Which pages a tile's keys lie in, a tile ahead of its use: lane g (0..7) knows that of keys 16 g ...
+struct Pages {
+    const int32_t* table;
+    int shift, n_pages, k_lo, k_hi;
+    int asked;                           // page number read for the next tile; INT_MIN where it has no key in [k_lo, k_hi)
+    int page;                            // of the current tile, -1 for none
+    __device__ __forceinline__ void ask(int tile, int lane) {
+        const int key = tile * BN + (lane & 7) * 16;
+        // (pages that a window has left behind may be gone from the table)
+        asked = key < k_hi && ((key >> shift) + 1) << shift > k_lo ? __ldg(table + (key >> shift)) : INT_MIN;
+    }
+    __device__ __forceinline__ void take(int32_t* err, bool report) {
+        const bool ok = asked >= 0 && asked < n_pages;
+        if (!ok && asked != INT_MIN && report) atomicOr(err, 1);
+        page = ok ? asked : -1;
+    }
+    __device__ __forceinline__ uint32_t there() const { return __ballot_sync(0xffffffffu, page >= 0) & 0xffu; }
+};
+
+// One warp brings K and V tiles, a page a lane.
+template <int D, int kReq>
+__device__ __forceinline__ void load_tiles(const TcLaunch<kReq>& X, const Item& w, int lane, uint32_t sK, uint32_t sV, uint32_t bars,
+                                           uint32_t* notes, volatile uint32_t* abort) {
+    using C = Tc<D>;
+    const PagedAttn<kReq>& P = X.a;
     auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
-    const int lane = thread % 32, chunk = thread % kChunks, row_t = thread / kChunks;
-    const int ps = P.pg.page_shift;
-    const int32_t* const table = P.pg.table + (int64_t)w.R.row * P.pg.table_stride;
-    const int64_t head = ((int64_t)w.hk << ps);                  // rows of a page before the head's
-    // page of 16-key group `lane` (0..7) of a tile; -1 for none
-    auto look_up = [&](int j) {
-        const int key = (w.j0 + j) * BN + (lane & 7) * 16;
-        int page = -1;
-        if (j < w.n && key < w.k_hi) {
-            page = __ldg(table + (key >> ps));
-            if (page < 0 || page >= P.pg.n_pages) {
-                if (thread < 8) atomicOr(P.err, 1);
-                page = -1;
-            }
+    Pages pg{P.pg.table + (int64_t)w.R.row * P.pg.table_stride, P.pg.page_shift, P.pg.n_pages, w.k_lo, w.k_hi, INT_MIN, -1};
+    const int rows = 1 << pg.shift;                              // of a copy (a page holds at most a tile)
+    auto copy = [&](const CUtensorMap* tm, uint32_t tile, uint32_t full, uint32_t there) {
+        const int n = __popc(there) * 16;                        // rows that land; groups of a page come together
+        if (lane == 0) mbar_expect_tx(full, (uint32_t)n * D * 2);
+        __syncwarp();
+        if (lane < 8 && lane % (rows / 16) == 0 && pg.page >= 0) {         // a page a lane
+#pragma unroll
+            for (int b = 0; b < D / 64; ++b) tma_load_4d(tile + b * C::kHalf + lane * 16 * 128, tm, b * 64, 0, w.hk, pg.page, full);
         }
-        return page;
+        __syncwarp();
     };
-    // element offset of the thread's chunk of row `row` of a tile, and whether the row counts
-    auto row_at = [&](int j, int row, int pages, int64_t& at, int64_t& sat) {
-        const int page = __shfl_sync(0xffffffffu, pages, row >> 4);
-        const int key = (w.j0 + j) * BN + row;
-        const int64_t in_page = head + (key & ((1 << ps) - 1));
-        at = (int64_t)page * P.pg.page_stride + in_page * D + chunk * (16 / EB);
-        sat = (int64_t)page * P.pg.scale_stride + in_page;
-        return page >= 0 && key < w.k_hi && key >= w.k_lo;
-    };
-    // where 8 channels (16 bytes) from channel 8 * q on of row `row` lie in a tile
-    auto place = [](int row, int q) { return (uint32_t)((q >> 3) * (BN * 128) + row * 128 + (((q & 7) ^ (row & 7)) << 4)); };
-    auto note = [&](int j, int pages, float k_unit, float v_exp) {
-        const uint32_t there = __ballot_sync(0xffffffffu, pages >= 0) & 0xffu;
-        if (thread == 0) notes[j & (kUnits - 1)] = TileNote{k_unit, v_exp, there, 0u};
-    };
-    int pages = look_up(0);
-    if constexpr (kCodes) {
-        // a row's codes wait in registers while the other operand's tile is converted
-        uint4 rk[kPasses], rv[kPasses];
-        float sk = 0.f, sv = 0.f, sk4 = 0.f, sv4 = 0.f;          // the lane's row's scale; the largest of four others
-        const uint8_t* const pk = static_cast<const uint8_t*>(P.pg.k);
-        const uint8_t* const pv = static_cast<const uint8_t*>(P.pg.v);
-        constexpr int kRowsW = 32 / kChunks;                     // rows of a warp in a pass
-        auto fetch = [&](const uint8_t* base, const float* scales, int j, int pg, uint4 (&raw)[kPasses], float& mine, float& top) {
-#pragma unroll
-            for (int i = 0; i < kPasses; ++i) {
-                int64_t at, sat;
-                const bool ok = row_at(j, row_t + kStep * i, pg, at, sat);
-                raw[i] = ok ? __ldg(reinterpret_cast<const uint4*>(base + at)) : make_uint4(0u, 0u, 0u, 0u);
-            }
-            // scales: lane i * kRowsW + r has that of the warp's row r of pass i; the tile's largest comes
-            // from four rows a lane (32 lanes have all 128)
-            int64_t at, sat;
-            const int row = (thread / 32) * kRowsW + lane % kRowsW + kStep * (lane / kRowsW);
-            mine = row_at(j, row, pg, at, sat) ? __ldg(scales + sat) : 0.f;
-            uint32_t m = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (row_at(j, lane + 32 * i, pg, at, sat)) {
-                    const uint32_t b = __float_as_uint(__ldg(scales + sat)) & 0x7fffffffu;
-                    if (b < 0x7f800000u) m = max(m, b);
-                }
-            }
-            top = __uint_as_float(m);
-        };
-        auto unit_of = [&](float top) {                          // every scale of the tile is below 2^unit
-            const uint32_t m = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
-            return max(-100, min(100, (int)(m >> 23) - 126));
-        };
-        auto convert = [&](uint32_t tile, const uint4 (&raw)[kPasses], float mine, int unit) {
-            const float s = mine * exp2f((float)-unit);
-            const uint32_t s2 = pack16<true>(s, s);
-#pragma unroll
-            for (int i = 0; i < kPasses; ++i) {
-                const int row = row_t + kStep * i;
-                const uint32_t f = __shfl_sync(0xffffffffu, s2, i * kRowsW + lane / kChunks);
-                const uint32_t x[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-                uint32_t h[8];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    h[2 * e] = scaled2(x[e], f);
-                    h[2 * e + 1] = scaled2(x[e] >> 16, f);
-                }
-                sts128_(tile + place(row, 2 * chunk), make_uint4(h[0], h[1], h[2], h[3]));
-                sts128_(tile + place(row, 2 * chunk + 1), make_uint4(h[4], h[5], h[6], h[7]));
-            }
-        };
-        if (w.n > 0) {
-            fetch(pk, P.pg.k_scale, 0, pages, rk, sk, sk4);
-            fetch(pv, P.pg.v_scale, 0, pages, rv, sv, sv4);
+    uint32_t zeroed = 0;                 // tiles that went through VZ
+    pg.ask(w.j0, lane);
+    for (int j = 0; j < w.n; ++j) {
+        const int key0 = (w.j0 + j) * BN;
+        pg.take(P.err, lane < 8);
+        pg.ask(w.j0 + j + 1, lane);
+        // a page is copied whole if any of its groups has a key: so are the groups past the last key
+        uint32_t there = pg.there();
+        for (int g = 0; g < 8; g += rows / 16)
+            if (there >> g & 1u) there |= ((1u << (rows / 16)) - 1u) << g;
+        if (lane == 0) notes[j & (kUnits - 1)] = there;
+        const int ks = j % C::kK, vs = j % C::kV;
+        if (j >= C::kK) mbar_wait(bar(C::KE + ks), (uint32_t)(j / C::kK - 1) & 1u, P.err, abort);
+        copy(&X.tm_k, sK + ks * C::kTile, bar(C::KF + ks), there);
+        if (j >= C::kV) mbar_wait(bar(C::VE + vs), (uint32_t)(j / C::kV - 1) & 1u, P.err, abort);
+        const uint32_t tile = sV + vs * C::kTile;
+        if (there == 0xffu && key0 >= w.k_lo && key0 + BN <= w.k_hi) {
+            copy(&X.tm_v, tile, bar(C::VF + vs), there);
+            continue;
         }
-        for (int j = 0; j < w.n; ++j) {
-            const int next = look_up(j + 1);
-            const int uk = unit_of(sk4), uv = unit_of(sv4);
-            note(j, pages, exp2f((float)uk), (float)uv);
-            const int ks = j % kK, vs = j % kV;
-            if (j >= kK) mbar_wait(bar(kBarKE + ks), (uint32_t)(j / kK - 1) & 1u, P.err, abort);
-            convert(sK + ks * Tc<D>::kTile, rk, sk, uk);
-            fence_proxy_async();
-            mbar_arrive(bar(kBarKF + ks));
-            if (j + 1 < w.n) fetch(pk, P.pg.k_scale, j + 1, next, rk, sk, sk4);
-            if (j >= kV) mbar_wait(bar(kBarVE + vs), (uint32_t)(j / kV - 1) & 1u, P.err, abort);
-            convert(sV + vs * Tc<D>::kTile, rv, sv, uv);
-            fence_proxy_async();
-            mbar_arrive(bar(kBarVF + vs));
-            if (j + 1 < w.n) fetch(pv, P.pg.v_scale, j + 1, next, rv, sv, sv4);
-            pages = next;
-        }
-    } else {
-        using T = __nv_bfloat16;
-        auto fetch = [&](const void* base, uint32_t tile, int j, int pg) {
+        // some rows must be zero: the tile is handed over once they are (at most a CTA's first and last
+        // tiles, and those with a page that is none)
+        copy(&X.tm_v, tile, bar(C::VZ), there);
+        mbar_wait(bar(C::VZ), zeroed & 1u, P.err, abort);
+        ++zeroed;
+        for (int r = lane; r < BN; r += 32) {
+            const int key = key0 + r;
+            if (key >= w.k_lo && key < w.k_hi && (there >> (r >> 4) & 1u)) continue;
 #pragma unroll
-            for (int i = 0; i < kPasses; ++i) {
-                const int row = row_t + kStep * i;
-                int64_t at, sat;
-                const bool ok = row_at(j, row, pg, at, sat);
-                cp_async16_or_zero(tile + place(row, chunk), static_cast<const T*>(base) + (ok ? at : 0), ok);
-            }
-            cp_async_commit();
-        };
-        // three tiles on their way: K(j), V(j), K(j + 1); one is handed over when the next two are asked for
-        auto hand_over = [&](int f) {
-            fence_proxy_async();
-            mbar_arrive(bar(f));
-        };
-        for (int j = 0; j < w.n; ++j) {
-            const int next = look_up(j + 1);
-            note(j, pages, 1.f, 0.f);
-            const int ks = j % kK, vs = j % kV;
-            if (j >= kK) mbar_wait(bar(kBarKE + ks), (uint32_t)(j / kK - 1) & 1u, P.err, abort);
-            fetch(P.pg.k, sK + ks * Tc<D>::kTile, j, pages);
-            if (j > 0) {
-                cp_async_wait<2>();
-                hand_over(kBarKF + (j - 1) % kK);
-            }
-            if (j >= kV) mbar_wait(bar(kBarVE + vs), (uint32_t)(j / kV - 1) & 1u, P.err, abort);
-            fetch(P.pg.v, sV + vs * Tc<D>::kTile, j, pages);
-            if (j > 0) {
-                cp_async_wait<2>();
-                hand_over(kBarVF + (j - 1) % kV);
-            }
-            pages = next;
+            for (int q = 0; q < D / 8; ++q) sts128_(tile + (q >> 3) * C::kHalf + r * 128 + (q & 7) * 16, make_uint4(0u, 0u, 0u, 0u));
         }
-        if (w.n > 0) {
-            cp_async_wait<1>();
-            hand_over(kBarKF + (w.n - 1) % kK);
-            cp_async_wait<0>();
-            hand_over(kBarVF + (w.n - 1) % kV);
-        }
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::VF + vs));
     }
 }
 
@@ -297,22 +181,23 @@ __device__ __forceinline__ void load_tiles(const PagedAttn<kReq>& P, const Item&
 
 // Issue order per key tile: PV_A(j - 1), S_A(j), PV_B(j - 1), S_B(j): a tile's next scores follow the
 // product that read the weights they overwrite, and each tile's softmax runs beside the other's products.
-template <int D, bool kHalf>
+template <int D>
 __device__ __forceinline__ void issue_products(uint32_t tmem, uint32_t sQ, uint32_t sK, uint32_t sV, uint32_t bars, int n, bool has_b,
                                                int32_t* err, volatile uint32_t* abort) {
-    constexpr uint32_t idS = idesc16(kHalf, BM, BN, false), idO = idesc16(kHalf, BM, D, true);
-    constexpr uint64_t kTileDesc = (uint64_t)(Tc<D>::kTile >> 4);
+    constexpr uint32_t idS = idesc_bf16(BM, BN, false), idO = idesc_bf16(BM, D, true);
+    using C = Tc<D>;
+    constexpr uint64_t kTileDesc = (uint64_t)(C::kTile >> 4);
     auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
     auto wait = [&](int i, uint32_t parity) {
         mbar_wait(bar(i), parity, err, abort);
         tc_fence_after();
     };
-    const uint64_t dQa = sw128_desc(sQ, 16, 1024), dQb = sw128_desc(sQ + Tc<D>::kTile, 16, 1024);
-    const uint64_t dK0 = sw128_desc(sK, 16, 1024), dV0 = sw128_desc(sV, Tc<D>::kHalf, 1024);
+    const uint64_t dQa = sw128_desc(sQ, 16, 1024), dQb = sw128_desc(sQ + C::kTile, 16, 1024);
+    const uint64_t dK0 = sw128_desc(sK, 16, 1024), dV0 = sw128_desc(sV, C::kHalf, 1024);
     auto scores = [&](uint64_t dq, uint64_t dk, uint32_t d) {
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
-            const uint64_t off = (uint64_t)(((kk >> 2) * Tc<D>::kHalf + (kk & 3) * 32) >> 4);
+            const uint64_t off = (uint64_t)(((kk >> 2) * C::kHalf + (kk & 3) * 32) >> 4);
             mma_bf16(d, dq + off, dk + off, idS, kk > 0 ? 1u : 0u);
         }
     };
@@ -324,107 +209,90 @@ __device__ __forceinline__ void issue_products(uint32_t tmem, uint32_t sQ, uint3
     const uint32_t tSa = tmem, tSb = tmem + BN, tOa = tmem + kColO, tOb = tOa + D;
     int ks = 0, vs = 0;
     uint32_t kp = 0, vp = 0;
-    wait(kBarQ, 0);
-    wait(kBarKF, 0);
+    wait(C::Q, 0);
+    wait(C::KF, 0);
     scores(dQa, dK0, tSa);
-    mma_commit(bar(kBarS));
+    mma_commit(bar(C::S));
     if (has_b) {
         scores(dQb, dK0, tSb);
-        mma_commit(bar(kBarS + 1));
+        mma_commit(bar(C::S + 1));
     }
-    mma_commit(bar(kBarKE));
+    mma_commit(bar(C::KE));
     for (int j = 1; j <= n; ++j) {
         const bool more = j < n;
-        if (++ks == kK) {
+        if (++ks == C::kK) {
             ks = 0;
             kp ^= 1u;
         }
         const uint64_t dk = dK0 + (uint64_t)ks * kTileDesc, dv = dV0 + (uint64_t)vs * kTileDesc;
         const uint32_t acc = j > 1 ? 1u : 0u, pp = (uint32_t)(j - 1) & 1u;
-        wait(kBarP, pp);
-        wait(kBarVF + vs, vp);
+        wait(C::P, pp);
+        wait(C::VF + vs, vp);
         values(tSa, dv, tOa, acc);
         if (more) {
-            wait(kBarKF + ks, kp);
+            wait(C::KF + ks, kp);
             scores(dQa, dk, tSa);
-            mma_commit(bar(kBarS));
+            mma_commit(bar(C::S));
         }
         if (has_b) {
-            wait(kBarP + 1, pp);
+            wait(C::P + 1, pp);
             values(tSb, dv, tOb, acc);
         }
-        mma_commit(bar(kBarVE + vs));
+        mma_commit(bar(C::VE + vs));
         if (more) {
             if (has_b) {
                 scores(dQb, dk, tSb);
-                mma_commit(bar(kBarS + 1));
+                mma_commit(bar(C::S + 1));
             }
-            mma_commit(bar(kBarKE + ks));
+            mma_commit(bar(C::KE + ks));
         }
-        if (++vs == kV) {
+        if (++vs == C::kV) {
             vs = 0;
             vp ^= 1u;
         }
     }
-    mma_commit(bar(kBarO));
+    mma_commit(bar(C::O));
 }
 
 // ------------------------------------------------------------------ softmax
 
 // The pair's queries, turned, into their tiles (128-byte swizzle), by the eight softmax warps: a warp
 // takes a token, whose angles serve the heads of the group.
-template <int D, bool kHalf, int kReq>
-__device__ __forceinline__ void put_queries(const PagedAttn<kReq>& P, const Item& w, int warp, int lane, uint32_t sQ, float* s_rs) {
+template <int D, int kReq>
+__device__ __forceinline__ void put_queries(const PagedAttn<kReq>& P, const Item& w, int warp, int lane, uint32_t sQ) {
     using T = __nv_bfloat16;
+    using C = Tc<D>;
     const int G = P.hq / P.hkv;
-    constexpr int C = D / 64;                            // channels of each half a lane
-    const int c = lane * C;
+    constexpr int E = D / 64;                            // channels of each half a lane
+    const int c = lane * E;
     auto put = [&](int row, int ch, float a, float b) {  // channels ch and ch + 1
-        const uint32_t at = sQ + (row / BM) * Tc<D>::kTile + (ch >> 6) * Tc<D>::kHalf + (row % BM) * 128 +
+        const uint32_t at = sQ + (row / BM) * C::kTile + (ch >> 6) * C::kHalf + (row % BM) * 128 +
                             ((((ch >> 3) & 7) ^ (row & 7)) << 4) + (ch & 7) * 2;
-        asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(pack16<kHalf>(a, b)) : "memory");
+        asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(pack_bf16(a, b)) : "memory");
     };
     const int tok0 = w.row0 / G, tok1 = (w.row0 + w.live - 1) / G;
     for (int tk = tok0 + warp; tk <= tok1; tk += 8) {
-        float2 cs[C];
+        float2 cs[E];
         const int64_t t = w.R.q0 + tk;
         if (P.turn) {
             const int64_t pos = __ldg(P.turn + t);
 #pragma unroll
-            for (int e = 0; e < C; ++e) cs[e] = turn_cs(P.rope.turn[c + e], pos);
+            for (int e = 0; e < E; ++e) cs[e] = turn_cs(P.rope.turn[c + e], pos);
         }
         const int r0 = max(tk * G, w.row0), r1 = min((tk + 1) * G, w.row0 + w.live);
         const T* q = static_cast<const T*>(P.q) + t * P.q_stride + (int64_t)w.hk * G * D + c;
 #pragma unroll 4
         for (int rr = r0; rr < r1; ++rr) {
             const T* p = q + (rr - tk * G) * D;
-            float lo[C], hi[C];
+            float lo[E], hi[E];
 #pragma unroll
-            for (int e = 0; e < C; ++e) {
+            for (int e = 0; e < E; ++e) {
                 lo[e] = static_cast<float>(p[e]);
                 hi[e] = static_cast<float>(p[D / 2 + e]);
                 if (P.turn) rotate1(lo[e], hi[e], cs[e], lo[e], hi[e]);
             }
-            float back = 1.f;
-            if constexpr (kHalf) {       // the row's largest value to [2^14, 2^15); zero and non-finite rows as they are
-                uint32_t top = 0;
-#pragma unroll
-                for (int e = 0; e < C; ++e) top = max(top, max(__float_as_uint(lo[e]) & 0x7fffffffu, __float_as_uint(hi[e]) & 0x7fffffffu));
-                top = __reduce_max_sync(0xffffffffu, top);
-                const int ex = (int)(top >> 23) - 127;
-                if (top < 0x7f800000u && ex > -100) {
-                    const float f = exp2f((float)(14 - ex));
-                    back = exp2f((float)(ex - 14));
-#pragma unroll
-                    for (int e = 0; e < C; ++e) {
-                        lo[e] *= f;
-                        hi[e] *= f;
-                    }
-                }
-            }
             const int row = rr - w.row0;
-            if (lane == 0) s_rs[row] = back * P.scale_log2;
-            if constexpr (C == 2) {
+            if constexpr (E == 2) {
                 put(row, c, lo[0], lo[1]);
                 put(row, D / 2 + c, hi[0], hi[1]);
             } else {
@@ -437,17 +305,22 @@ __device__ __forceinline__ void put_queries(const PagedAttn<kReq>& P, const Item
         }
     }
     // rows of no query: zero, so that what they hold is a number
-    for (int row = w.live + warp; row < kPair; row += 8) {
-        if (lane == 0) s_rs[row] = P.scale_log2;
+    for (int row = w.live + warp; row < kPair; row += 8)
         for (int ch = 2 * lane; ch < D; ch += 64) put(row, ch, 0.f, 0.f);
-    }
 }
 
 // One softmax thread: row r of tile x over the CTA's key tiles, then its output.
-template <int D, bool kCodes, int kReq>
+//
+// Weights are 2^(score - ref) with the reference of the tiles before: bf16 holds any weight that fp32
+// does, so the tile's own maximum need not be known first, and is found after the weights are handed
+// over, beside the products.  O and the sum are scaled to a new reference, before the next tile, only
+// when the maximum has passed the old one by 8.  Where a sum shows weights of 2^40 and more (or the row
+// has no reference yet) the maximum comes first after all.
+template <int D, int kReq>
 __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item& w, uint32_t tmem, uint32_t bars, int x, int quad, int lane,
-                                             const TileNote* notes, const float* s_rs, volatile uint32_t* abort) {
+                                             const uint32_t* notes, volatile uint32_t* abort) {
     using T = __nv_bfloat16;
+    using C = Tc<D>;
     const PagedAttn<kReq>& P = X.a;
     auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
     const int G = P.hq / P.hkv;
@@ -458,79 +331,104 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
     const int my = min(row, w.live - 1);
     const int end = w.R.n_keys - w.R.nq + (w.row0 + my) / G;     // the last key the row sees
     const int start = P.window ? end - P.window : -1;            // and the last that it does not, before them
-    const float rs = s_rs[row];
-    float ref = -CUDART_INF_F, l = 0.f;
+    const float f = P.scale_log2;
+    float ref = -CUDART_INF_F, top = -CUDART_INF_F, l = 0.f;
+    auto scale_o = [&](float alpha) {
+#pragma unroll 1
+        for (int c = 0; c < D / 16; ++c) {
+            uint32_t ov[16];
+            tmem_ld16(colO + c * 16, ov);
+            tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * alpha);
+            tmem_st16(colO + c * 16, ov);
+        }
+    };
     for (int j = 0; j < w.n; ++j) {
-        mbar_wait(bar(kBarS + x), (uint32_t)j & 1u, P.err, abort);
+        mbar_wait(bar(C::S + x), (uint32_t)j & 1u, P.err, abort);
         tc_fence_after();
         uint32_t sv[4][32];
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld32(colS + c * 32, sv[c]);
-        const TileNote nt = notes[j & (kUnits - 1)];
-        const float f = kCodes ? rs * nt.k_unit : rs, ve = kCodes ? nt.v_exp : 0.f;
-        tmem_ld_wait();
+        // scores of tile j are complete, so is every product before them: O may be scaled
+        const bool moves = top > ref + 8.0f;
+        float alpha = 1.0f;
+        if (__any_sync(0xffffffffu, moves)) {
+            if (moves) {
+                alpha = ex2(ref - top);                          // (0 from no reference at all)
+                ref = top;
+            }
+            if (j > 0) scale_o(alpha);
+            l *= alpha;
+        }
+        const uint32_t groups = notes[j & (kUnits - 1)];
         const int key0 = (w.j0 + j) * BN;
-        if (key0 + BN - 1 > end || key0 <= start || nt.there != 0xffu) {
+        tmem_ld_wait();
+        if (key0 + BN - 1 > end || key0 <= start || groups != 0xffu) {
 #pragma unroll
             for (int c = 0; c < 4; ++c)
 #pragma unroll
                 for (int e = 0; e < 32; ++e) {
                     const int key = key0 + c * 32 + e;
-                    if (key > end || key <= start || !(nt.there >> (2 * c + e / 16) & 1u)) sv[c][e] = __float_as_uint(-CUDART_INF_F);
+                    if (key > end || key <= start || !(groups >> (2 * c + e / 16) & 1u)) sv[c][e] = __float_as_uint(-CUDART_INF_F);
                 }
         }
-        float top4[4];
+        auto find_top = [&]() {
+            float top4[4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            float m = fmaxf(__uint_as_float(sv[c][0]), __uint_as_float(sv[c][1]));
+            for (int c = 0; c < 4; ++c) {
+                float m = fmaxf(__uint_as_float(sv[c][0]), __uint_as_float(sv[c][1]));
 #pragma unroll
-            for (int e = 2; e < 32; e += 2) m = fmax3(m, __uint_as_float(sv[c][e]), __uint_as_float(sv[c][e + 1]));
-            top4[c] = m;
-        }
-        const float top = fmaf(fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])), f, ve);
-        // the reference moves only when weights would pass 2^8: a rescale of O reads and writes it all
-        const bool moves = top > ref + 8.0f;
-        const float now = moves ? top : ref;
-        const float alpha = moves ? ex2(ref - now) : 1.0f;
-        const float base = now == -CUDART_INF_F ? 0.f : now;     // nothing seen yet
-        if (j >= 1 && __any_sync(0xffffffffu, moves)) {
-            // scores of tile j are complete, so is every product before them: O may be scaled
-#pragma unroll 1
-            for (int c = 0; c < D / 16; ++c) {
-                uint32_t ov[16];
-                tmem_ld16(colO + c * 16, ov);
-                tmem_ld_wait();
-#pragma unroll
-                for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * alpha);
-                tmem_st16(colO + c * 16, ov);
+                for (int e = 2; e < 32; e += 2) m = fmax3(m, __uint_as_float(sv[c][e]), __uint_as_float(sv[c][e + 1]));
+                top4[c] = m;
             }
-        }
-        float ps[4] = {0.f, 0.f, 0.f, 0.f};
-        const float off = ve - base;
+            top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * f;
+        };
+        auto weigh = [&]() {
+            float ps[4] = {0.f, 0.f, 0.f, 0.f};
+            const float off = ref == -CUDART_INF_F ? 0.f : -ref;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            uint32_t pk[16];
+            for (int c = 0; c < 4; ++c) {
+                uint32_t pk[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float a0, a1;
-                ffma2(a0, a1, __uint_as_float(sv[c][2 * i]), __uint_as_float(sv[c][2 * i + 1]), f, off);
-                a0 = ex2(a0);
-                a1 = ex2(a1);
-                if (i & 1) fadd2(ps[2], ps[3], a0, a1);
-                else fadd2(ps[0], ps[1], a0, a1);
-                pk[i] = pack16<kCodes>(a0, a1);
+                for (int i = 0; i < 16; ++i) {
+                    float a0, a1;
+                    ffma2(a0, a1, __uint_as_float(sv[c][2 * i]), __uint_as_float(sv[c][2 * i + 1]), f, off);
+                    a0 = ex2(a0);
+                    a1 = ex2(a1);
+                    if (i & 1) fadd2(ps[2], ps[3], a0, a1);
+                    else fadd2(ps[0], ps[1], a0, a1);
+                    pk[i] = pack_bf16(a0, a1);
+                }
+                tmem_st16(colS + c * 16, pk);
             }
-            tmem_st16(colS + c * 16, pk);
+            return (ps[0] + ps[1]) + (ps[2] + ps[3]);
+        };
+        float sum = 0.f;
+        bool high = ref == -CUDART_INF_F;
+        if (!__all_sync(0xffffffffu, high)) {
+            sum = weigh();
+            high = high || !(sum < 1.0e12f);
+        }
+        if (__any_sync(0xffffffffu, high)) {
+            find_top();
+            alpha = 1.0f;
+            if (high && top > ref) {
+                alpha = ex2(ref - top);
+                ref = top;
+            }
+            if (j > 0) scale_o(alpha);
+            l *= alpha;
+            sum = weigh();
         }
         tmem_st_wait();
-        const float sum = (ps[0] + ps[1]) + (ps[2] + ps[3]);
-        l = l * alpha + (kCodes ? sum * ex2(-ve) : sum);
-        ref = now;
         tc_fence_before();
-        mbar_arrive(bar(kBarP + x));
+        mbar_arrive(bar(C::P + x));
+        l += sum;
+        find_top();
     }
     if (w.n > 0) {
-        mbar_wait(bar(kBarO), 0u, P.err, abort);
+        mbar_wait(bar(C::O), 0u, P.err, abort);
         tc_fence_after();
     }
     const float inv = l == 0.f ? 0.f : 1.0f / l;
@@ -563,7 +461,7 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
             for (int k = 0; k < 2; ++k) {
                 uint32_t o8[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o8[e] = pack16<false>(__uint_as_float(ov[16 * k + 2 * e]), __uint_as_float(ov[16 * k + 2 * e + 1]));
+                for (int e = 0; e < 8; ++e) o8[e] = pack_bf16(__uint_as_float(ov[16 * k + 2 * e]), __uint_as_float(ov[16 * k + 2 * e + 1]));
                 if (wide) {
                     stg256(orow + c * 32 + k * 16, o8);
                 } else {
@@ -592,7 +490,7 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
         const int hh = w.hk * G + rr % G;
         float q[D / 32], o[D / 32], m, sum;
         lane_query<T, D>(P, t, hh, lane, q);
-        row_attend<T, D, kCodes>(P, q, w.R.row, w.hk, lo, hi, 1, lane, m, sum, o);
+        row_attend<T, D, false>(P, q, w.R.row, w.hk, lo, hi, 1, lane, m, sum, o);
         const float iv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
         for (int e = 0; e < D / 32; ++e) {
@@ -606,43 +504,43 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
 
 // ------------------------------------------------------------------ kernel
 
-template <int D, bool kCodes, int kReq>
+template <int D, int kReq>
 __global__ void __launch_bounds__(kThreads, 1) paged_tc_kernel(const __grid_constant__ TcLaunch<kReq> X) {
     const PagedAttn<kReq>& P = X.a;
+    using C = Tc<D>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint32_t s_last;
     uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    const uint32_t sQ = smem_u32(smem), sK = sQ + 2 * Tc<D>::kTile, sV = sK + kK * Tc<D>::kTile;
-    const uint32_t bars = sV + kV * Tc<D>::kTile;
-    uint8_t* const tail = smem + (size_t)(2 + kK + kV) * Tc<D>::kTile + 8 * kBars;
-    uint32_t* const slot = reinterpret_cast<uint32_t*>(tail);
+    const uint32_t sQ = smem_u32(smem), sK = sQ + 2 * C::kTile, sV = sK + C::kK * C::kTile;
+    const uint32_t bars = sQ + C::kTiles;
+    uint32_t* const notes = reinterpret_cast<uint32_t*>(smem + C::kNotes);   // of a tile: which groups of 16 keys are there
+    uint32_t* const slot = reinterpret_cast<uint32_t*>(smem + C::kSlot);
     volatile uint32_t* const abort = slot + 1;
-    TileNote* const notes = reinterpret_cast<TileNote*>(tail + 16);
-    float* const s_rs = reinterpret_cast<float*>(tail + 16 + 16 * kUnits);
+    volatile uint32_t& s_last = slot[2];
     auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const Item w = find_item(P);
     const bool has_b = w.live > BM;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kK; ++s) {
-            mbar_init(bar(kBarKF + s), 128);
-            mbar_init(bar(kBarKE + s), 1);
+        for (int s = 0; s < C::kK; ++s) {
+            mbar_init(bar(C::KF + s), 1);
+            mbar_init(bar(C::KE + s), 1);
         }
-        for (int s = 0; s < kV; ++s) {
-            mbar_init(bar(kBarVF + s), 128);
-            mbar_init(bar(kBarVE + s), 1);
+        for (int s = 0; s < C::kV; ++s) {
+            mbar_init(bar(C::VF + s), 1);
+            mbar_init(bar(C::VE + s), 1);
         }
+        mbar_init(bar(C::VZ), 1);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(kBarS + i), 1);
-            mbar_init(bar(kBarP + i), 128);
+            mbar_init(bar(C::S + i), 1);
+            mbar_init(bar(C::P + i), 128);
         }
-        mbar_init(bar(kBarO), 1);
-        mbar_init(bar(kBarQ), 256);
+        mbar_init(bar(C::O), 1);
+        mbar_init(bar(C::Q), 256);
         *abort = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 12) {
+    if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -652,25 +550,22 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tc_kernel(const __grid_cons
     const uint32_t tmem = *slot;
 
     if (warp < 4) {
-        load_tiles<D, kCodes>(P, w, threadIdx.x, sK, sV, bars, notes, abort);
-    } else if (warp < 12) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
-        put_queries<D, kCodes>(P, w, warp - 4, lane, sQ, s_rs);
-        fence_proxy_async();
-        asm volatile("bar.sync 1, 256;" ::: "memory");           // (the row factors, too)
-        mbar_arrive(bar(kBarQ));
-        const int x = warp >= 8;
-        if (x == 0 || has_b) softmax_rows<D, kCodes>(X, w, tmem, bars, x, warp & 3, lane, notes, s_rs, abort);
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsLow));
+        if (warp == 1) load_tiles<D>(X, w, lane, sK, sV, bars, notes, abort);
+        else if (warp == 0 && lane == 0 && w.n > 0) issue_products<D>(tmem, sQ, sK, sV, bars, w.n, has_b, P.err, abort);
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
-        if (warp == 12 && lane == 0 && w.n > 0)
-            issue_products<D, kCodes>(tmem, sQ, sK, sV, bars, w.n, has_b, P.err, abort);
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+        put_queries<D>(P, w, warp - 4, lane, sQ);
+        fence_proxy_async();
+        mbar_arrive(bar(C::Q));
+        const int x = warp >= 8;
+        if (x == 0 || has_b) softmax_rows<D>(X, w, tmem, bars, x, warp & 3, lane, notes, abort);
     }
 
     tc_fence_before();
     if (w.R.splits > 1) __threadfence();                         // the partials, before the ticket
     __syncthreads();
-    if (warp == 12) {
+    if (warp == 0) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
     }
@@ -706,15 +601,15 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tc_kernel(const __grid_cons
         const int64_t tok = w.R.q0 + (w.row0 + row) / G;
         const int h = w.hk * G + (w.row0 + row) % G;
         *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(P.out) + (tok * P.hq + h) * D + 4 * f) =
-            make_uint2(pack16<false>(o.x * inv, o.y * inv), pack16<false>(o.z * inv, o.w * inv));
+            make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
         if (f == 0 && P.lse) P.lse[(int64_t)h * P.n_tokens + tok] = sum == 0.f ? -CUDART_INF_F : (top + log2f(sum)) * 0.69314718055994531f;
     }
 }
 
-template <int D, bool kCodes, int kReq>
+template <int D, int kReq>
 cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStream_t s) {
     static PerDevice<cudaError_t> smem_set;
-    const auto kernel = paged_tc_kernel<D, kCodes, kReq>;
+    const auto kernel = paged_tc_kernel<D, kReq>;
     cudaError_t e = opt_in_smem(smem_set, (const void*)kernel, Tc<D>::kSmem);
     if (e != cudaSuccess) return e;
     for (int b0 = 0; b0 < n; b0 += kReq) {
@@ -763,6 +658,10 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
             X.part_o = static_cast<float*>(p);
             X.part_lse = reinterpret_cast<float*>(static_cast<char*>(p) + o_bytes);
         }
+        const int rows = 1 << c.pg.page_shift;
+        if (!encode_page_map(&X.tm_k, c.pg.k, c.pg, c.hkv, D, false, 64, rows, CU_TENSOR_MAP_SWIZZLE_128B) ||
+            !encode_page_map(&X.tm_v, c.pg.v, c.pg, c.hkv, D, false, 64, rows, CU_TENSOR_MAP_SWIZZLE_128B))
+            return cudaErrorInvalidValue;
         kernel<<<(unsigned)items, kThreads, Tc<D>::kSmem, s>>>(X);
         e = cudaGetLastError();
         if (e != cudaSuccess) return e;
@@ -770,16 +669,15 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
     return cudaSuccess;
 }
 
-template <int D, bool kCodes>
+template <int D>
 cudaError_t by_count(const PagedAttnCall& c, const PagedReq* req, int n, cudaStream_t s) {
-    return n <= kPagedFew ? launch<D, kCodes, kPagedFew>(c, req, n, s) : launch<D, kCodes, kPagedMany>(c, req, n, s);
+    return n <= kPagedFew ? launch<D, kPagedFew>(c, req, n, s) : launch<D, kPagedMany>(c, req, n, s);
 }
 
 }  // namespace
 
-cudaError_t launch_paged_tc(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s) {
-    if (d == 128) return codes ? by_count<128, true>(c, req, n, s) : by_count<128, false>(c, req, n, s);
-    return codes ? by_count<64, true>(c, req, n, s) : by_count<64, false>(c, req, n, s);
+cudaError_t launch_paged_tc(const PagedAttnCall& c, const PagedReq* req, int n, int d, cudaStream_t s) {
+    return d == 128 ? by_count<128>(c, req, n, s) : by_count<64>(c, req, n, s);
 }
 
 }  // namespace c2kv

@@ -83,6 +83,16 @@ def test_window(shape, window):
     _check(_run(*shape, 32, [(1, 300), (40, 333), (4, 3), (150, 150)], window=window), shape[0])
 
 
+@pytest.mark.parametrize("nq", [3, 140])
+@pytest.mark.parametrize("size", [16, 64])
+@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[1], SHAPES[9]], ids=lambda s: "-".join(map(str, s)))
+def test_pages_that_a_window_left_behind(shape, size, nq):
+    """Pages whose rows no query sees any more may be gone from the table."""
+    def edit(pg):
+        pg.table[0, :(700 - nq - 37 + 1) // size] = -1
+    _check(_run(*shape, size, [(nq, 700)], window=37, edit=edit), shape[0])
+
+
 @pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[1], SHAPES[6], SHAPES[10]], ids=lambda s: "-".join(map(str, s)))
 def test_long_rows_are_split_and_joined(shape):
     _check(_run(*shape, 128, [(1, 9001), (3, 5000)], turn=False), shape[0])
