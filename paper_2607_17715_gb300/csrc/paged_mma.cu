@@ -230,6 +230,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2) paged_mma_kernel(const __grid_
     for (int i = 0; i < kStages; ++i) loaded[i] = i < n_it ? issue(i, i) : 0;
 
     // the tile's queries: turned, as fragments of A
+    uint64_t turn[D / 64] = {};
+    if (P.turn) {
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) turn[e] = lane_turn(P.rope.turn, lane * (D / 64) + e);
+    }
     for (int row = warp; row < kRows; row += kWarps) {
         float x[D / 32];                 // channels 2 lane (+ 1) of the lower half, and of the upper
         const bool there = row < live;
@@ -249,7 +254,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) paged_mma_kernel(const __grid_
 #pragma unroll
                 for (int e = 0; e < C; ++e) {
                     float a, b;
-                    rotate1(x[e], x[C + e], turn_cs(P.rope.turn[lane * C + e], pos), a, b);
+                    rotate1(x[e], x[C + e], turn_cs(turn[e], pos), a, b);
                     x[e] = a;
                     x[C + e] = b;
                 }

@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kMoveThreads) paged_move_kernel(const __grid_c
         }
         if (!angles) {
             for (int a = threadIdx.x; a < nt * (D / 2); a += kMoveThreads)
-                s_cs[a] = turn_cs(P.rope.turn[a % (D / 2)], __ldg(P.turn + t0 + a / (D / 2)));
+                s_cs[a] = turn_cs(lane_turn(P.rope.turn, a % (D / 2)), __ldg(P.turn + t0 + a / (D / 2)));
             __syncthreads();
             angles = true;
         }

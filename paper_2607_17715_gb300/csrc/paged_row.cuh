@@ -53,7 +53,7 @@ __device__ __forceinline__ void lane_query(const PagedAttn<kReq>& P, int64_t t, 
     for (int e = 0; e < C; ++e) {
         const float lo = static_cast<float>(q[c + e]), hi = static_cast<float>(q[c + D / 2 + e]);
         float a = lo, b = hi;
-        if (P.turn) rotate1(lo, hi, turn_cs(P.rope.turn[c + e], __ldg(P.turn + t)), a, b);
+        if (P.turn) rotate1(lo, hi, turn_cs(lane_turn(P.rope.turn, c + e), __ldg(P.turn + t)), a, b);
         x[e] = low ? a : b;
     }
 }

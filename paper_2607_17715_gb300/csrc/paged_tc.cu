@@ -270,36 +270,72 @@ __device__ __forceinline__ void put_queries(const PagedAttn<kReq>& P, const Item
                             ((((ch >> 3) & 7) ^ (row & 7)) << 4) + (ch & 7) * 2;
         asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(pack_bf16(a, b)) : "memory");
     };
-    const int tok0 = w.row0 / G, tok1 = (w.row0 + w.live - 1) / G;
-    for (int tk = tok0 + warp; tk <= tok1; tk += 8) {
-        float2 cs[E];
-        const int64_t t = w.R.q0 + tk;
-        if (P.turn) {
-            const int64_t pos = __ldg(P.turn + t);
+    // A warp's tokens are tok0 + warp, + 8, ..: their positions are read together, a token's rows while
+    // the angles of the one before are formed (one after the other, the loads' latencies made 9 us).
+    constexpr int kHeads = 4;                            // heads in flight
+    const int tok0 = w.row0 / G + warp, tok1 = (w.row0 + w.live - 1) / G;
+    const T* const base = static_cast<const T*>(P.q) + (int64_t)w.hk * G * D + c;
+    uint32_t next[kHeads][2];                            // both halves' channels, as they lie
+    auto fetch = [&](int tk, int g0, uint32_t (&x)[kHeads][2]) {
+        const T* const q = base + (w.R.q0 + tk) * P.q_stride;
 #pragma unroll
-            for (int e = 0; e < E; ++e) cs[e] = turn_cs(P.rope.turn[c + e], pos);
-        }
-        const int r0 = max(tk * G, w.row0), r1 = min((tk + 1) * G, w.row0 + w.live);
-        const T* q = static_cast<const T*>(P.q) + t * P.q_stride + (int64_t)w.hk * G * D + c;
-#pragma unroll 4
-        for (int rr = r0; rr < r1; ++rr) {
-            const T* p = q + (rr - tk * G) * D;
-            float lo[E], hi[E];
+        for (int g = 0; g < kHeads; ++g) {
+            if (tk > tok1 || g0 + g >= G) continue;
+            const T* const p = q + (int64_t)(g0 + g) * D;
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                lo[e] = static_cast<float>(p[e]);
-                hi[e] = static_cast<float>(p[D / 2 + e]);
-                if (P.turn) rotate1(lo[e], hi[e], cs[e], lo[e], hi[e]);
+            for (int half = 0; half < 2; ++half) {
+                if constexpr (E == 2) x[g][half] = __ldg(reinterpret_cast<const uint32_t*>(p + half * (D / 2)));
+                else x[g][half] = __ldg(reinterpret_cast<const uint16_t*>(p + half * (D / 2)));
             }
-            const int row = rr - w.row0;
-            if constexpr (E == 2) {
-                put(row, c, lo[0], lo[1]);
-                put(row, D / 2 + c, hi[0], hi[1]);
-            } else {
-                const float y0 = __shfl_down_sync(0xffffffffu, lo[0], 1), y1 = __shfl_down_sync(0xffffffffu, hi[0], 1);
-                if (!(lane & 1)) {
-                    put(row, c, lo[0], y0);
-                    put(row, D / 2 + c, hi[0], y1);
+        }
+    };
+    int pos32 = 0;
+    uint64_t turn[E] = {};
+    if (P.turn) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) turn[e] = lane_turn(P.rope.turn, c + e);
+    }
+    fetch(tok0, 0, next);
+    for (int tk = tok0, i = 0; tk <= tok1; tk += 8, ++i) {
+        if ((i & 31) == 0 && P.turn) pos32 = tk + 8 * lane <= tok1 ? __ldg(P.turn + w.R.q0 + tk + 8 * lane) : 0;
+        const int64_t pos = __shfl_sync(0xffffffffu, pos32, i & 31);
+        float2 cs[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) cs[e] = P.turn ? turn_cs(turn[e], pos) : make_float2(1.f, 0.f);
+        for (int g0 = 0; g0 < G; g0 += kHeads) {
+            uint32_t x[kHeads][2];
+#pragma unroll
+            for (int g = 0; g < kHeads; ++g) {
+                x[g][0] = next[g][0];
+                x[g][1] = next[g][1];
+            }
+            const bool last = g0 + kHeads >= G;
+            fetch(last ? tk + 8 : tk, last ? 0 : g0 + kHeads, next);
+#pragma unroll
+            for (int g = 0; g < kHeads; ++g) {
+                const int row = tk * G + g0 + g - w.row0;
+                if (g0 + g >= G || row < 0 || row >= w.live) continue;
+                float lo[E], hi[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    lo[e] = __uint_as_float(e == 0 ? x[g][0] << 16 : x[g][0] & 0xffff0000u);
+                    hi[e] = __uint_as_float(e == 0 ? x[g][1] << 16 : x[g][1] & 0xffff0000u);
+                    if (P.turn) {
+                        float a, b;
+                        rotate1(lo[e], hi[e], cs[e], a, b);
+                        lo[e] = a;
+                        hi[e] = b;
+                    }
+                }
+                if constexpr (E == 2) {
+                    put(row, c, lo[0], lo[1]);
+                    put(row, D / 2 + c, hi[0], hi[1]);
+                } else {
+                    const float y0 = __shfl_down_sync(0xffffffffu, lo[0], 1), y1 = __shfl_down_sync(0xffffffffu, hi[0], 1);
+                    if (!(lane & 1)) {
+                        put(row, c, lo[0], y0);
+                        put(row, D / 2 + c, hi[0], y1);
+                    }
                 }
             }
         }

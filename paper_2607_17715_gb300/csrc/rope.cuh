@@ -16,6 +16,15 @@ __device__ __forceinline__ float2 turn_cs(uint64_t turn, int64_t pos) {
     return make_float2(c, s);
 }
 
+// Frequency i of a table in a kernel's parameters, for an index that differs from lane to lane: an
+// ordinary load, since the constant cache serves one address of a warp at a time (a prologue that read
+// 64 frequencies a token took 9 us that way, 1 so).
+__device__ __forceinline__ uint64_t lane_turn(const uint64_t* turns, int i) {
+    uint64_t v;
+    asm volatile("ld.u64 %0, [%1];" : "=l"(v) : "l"(turns + i));
+    return v;
+}
+
 // (x, y) turned by the angle whose (cos, sin) is cs, with the rounding spelled out (one
 // product rounded, then a fused multiply-add) so that every kernel that turns a pair gets
 // the same bits.
