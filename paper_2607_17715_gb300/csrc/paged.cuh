@@ -73,6 +73,8 @@ struct PagedReq {
     int32_t item0;           // first work item of the request
     int32_t splits;          // stretches that its keys are cut into
     int32_t unit0;           // first unit (row tile of a KV head)
+    int32_t tile0;           // (paged_tc.cu) its row tiles of this entry: [tile0, tile0 + tiles)
+    int32_t tiles;
 };
 
 template <int kReq>

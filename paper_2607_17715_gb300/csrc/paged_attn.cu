@@ -137,7 +137,7 @@ cudaError_t launch_paged_attn(const PagedAttnCall& c, int dtype, int d, bool cod
     std::vector<PagedReq> req;
     req.reserve(c.batch);
     for (int r = 0; r < c.batch; ++r)
-        if (c.ptr[r + 1] > c.ptr[r]) req.push_back(PagedReq{c.ptr[r], c.ptr[r + 1] - c.ptr[r], c.n_keys[r], r, 0, 1, 0});
+        if (c.ptr[r + 1] > c.ptr[r]) req.push_back(PagedReq{c.ptr[r], c.ptr[r + 1] - c.ptr[r], c.n_keys[r], r, 0, 1, 0, 0, 0});
     const int n = (int)req.size();
     if (dtype == kDtypeF32)
         return d == 128 ? rows_of<float, 128>(c, req.data(), n, codes, s) : rows_of<float, 64>(c, req.data(), n, codes, s);

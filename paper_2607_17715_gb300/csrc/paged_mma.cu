@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) paged_mma_kernel(const __grid_
 #pragma unroll
                 for (int e = 0; e < C; ++e) {
                     float a, b;
-                    rotate1(x[e], x[C + e], turn_cs(turn[e], pos), a, b);
+                    rotate1(x[e], x[C + e], turn_cs_fast(turn[e], pos), a, b);
                     x[e] = a;
                     x[C + e] = b;
                 }

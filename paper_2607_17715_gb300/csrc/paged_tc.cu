@@ -22,6 +22,8 @@
 
 #include <algorithm>
 #include <climits>
+#include <utility>
+#include <vector>
 
 namespace c2kv {
 namespace {
@@ -60,14 +62,17 @@ struct TcLaunch {
     CUtensorMap tm_k, tm_v;              // [n_pages][Hkv][page_size][d], boxes of a page's rows and 64 channels
     float* part_o;                       // [item][256][D] normalised
     float* part_lse;                     // [item][256] log2 domain
-    uint32_t* tickets;                   // [unit], zero between launches
     PagedAttn<kReq> a;
 };
+
+__device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
 
 // The CTA's work: rows [row0, row0 + live) of request R's KV head hk, key tiles [j0, j0 + n).
 struct Item {
     PagedReq R;
-    int hk, sp, row0, live, j0, n, unit;
+    int hk, sp, row0, live, j0, n;
     int k_lo, k_hi;                      // keys that some row sees: [k_lo, k_hi)
 };
 
@@ -81,14 +86,13 @@ __device__ __forceinline__ Item find_item(const PagedAttn<kReq>& P) {
         else hi = mid;
     }
     w.R = P.req[r];
-    const int G = P.hq / P.hkv, n_rows = w.R.nq * G, pairs = (n_rows + kPair - 1) / kPair;
+    const int G = P.hq / P.hkv, n_rows = w.R.nq * G;
     int i = blockIdx.x - w.R.item0;
     // the last rows first: they see the most keys
     w.hk = i % P.hkv;
     i /= P.hkv;
     w.sp = i % w.R.splits;
-    const int pr = pairs - 1 - i / w.R.splits;
-    w.unit = w.R.unit0 + pr * P.hkv + w.hk;
+    const int pr = w.R.tile0 + w.R.tiles - 1 - i / w.R.splits;
     w.row0 = pr * kPair;
     w.live = min(kPair, n_rows - w.row0);
     const int before = w.R.n_keys - w.R.nq;
@@ -256,93 +260,91 @@ __device__ __forceinline__ void issue_products(uint32_t tmem, uint32_t sQ, uint3
 
 // ------------------------------------------------------------------ softmax
 
-// The pair's queries, turned, into their tiles (128-byte swizzle), by the eight softmax warps: a warp
-// takes a token, whose angles serve the heads of the group.
+// The pair's queries, turned, into their tiles (128-byte swizzle), by the eight softmax warps, 32 rows
+// each: copied as they are, all on their way at once, then turned in place, eight rows at a time (a row
+// after the other is a chain of dependent instructions, and took 9000 clocks in all).
 template <int D, int kReq>
 __device__ __forceinline__ void put_queries(const PagedAttn<kReq>& P, const Item& w, int warp, int lane, uint32_t sQ) {
     using T = __nv_bfloat16;
     using C = Tc<D>;
     const int G = P.hq / P.hkv;
-    constexpr int E = D / 64;                            // channels of each half a lane
-    const int c = lane * E;
-    auto put = [&](int row, int ch, float a, float b) {  // channels ch and ch + 1
-        const uint32_t at = sQ + (row / BM) * C::kTile + (ch >> 6) * C::kHalf + (row % BM) * 128 +
-                            ((((ch >> 3) & 7) ^ (row & 7)) << 4) + (ch & 7) * 2;
-        asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(pack_bf16(a, b)) : "memory");
-    };
-    // A warp's tokens are tok0 + warp, + 8, ..: their positions are read together, a token's rows while
-    // the angles of the one before are formed (one after the other, the loads' latencies made 9 us).
-    constexpr int kHeads = 4;                            // heads in flight
-    const int tok0 = w.row0 / G + warp, tok1 = (w.row0 + w.live - 1) / G;
-    const T* const base = static_cast<const T*>(P.q) + (int64_t)w.hk * G * D + c;
-    uint32_t next[kHeads][2];                            // both halves' channels, as they lie
-    auto fetch = [&](int tk, int g0, uint32_t (&x)[kHeads][2]) {
-        const T* const q = base + (w.R.q0 + tk) * P.q_stride;
+    const int r0 = warp * 32, n = max(0, min(32, w.live - r0));
+    const uint32_t tile = sQ + (r0 / BM) * C::kTile + (r0 % BM) * 128;
+    auto place = [&](int row, int q) { return tile + (uint32_t)((q >> 3) * C::kHalf + row * 128 + (((q & 7) ^ (row & 7)) << 4)); };
+    {
+        // lane i knows where row i lies; a copy takes whole rows, 16 bytes a lane
+        const int row = w.row0 + r0 + min(lane, max(0, n - 1)), tok = row / G;
+        const int64_t at = (w.R.q0 + tok) * P.q_stride + ((int64_t)w.hk * G + row - tok * G) * D;
+        constexpr int kChunks = D / 8, kStep = 32 / kChunks;
+        const int q = lane % kChunks;
+        const T* const base = static_cast<const T*>(P.q) + q * 8;
 #pragma unroll
-        for (int g = 0; g < kHeads; ++g) {
-            if (tk > tok1 || g0 + g >= G) continue;
-            const T* const p = q + (int64_t)(g0 + g) * D;
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                if constexpr (E == 2) x[g][half] = __ldg(reinterpret_cast<const uint32_t*>(p + half * (D / 2)));
-                else x[g][half] = __ldg(reinterpret_cast<const uint16_t*>(p + half * (D / 2)));
-            }
+        for (int i0 = 0; i0 < 32; i0 += kStep) {
+            const int i = i0 + lane / kChunks;
+            cp_async16_or_zero(place(i, q), base + __shfl_sync(0xffffffffu, at, i), i < n);   // zero past the rows: a number
         }
-    };
-    int pos32 = 0;
-    uint64_t turn[E] = {};
-    if (P.turn) {
+        cp_async_commit();
+    }
+    if (P.turn && n > 0) {
+        constexpr int E = D / 64, kBatch = 8;            // channels of each half a lane; rows in flight
+        const int c = lane * E, q0 = c >> 3, q1 = (D / 2 + c) >> 3;
+        uint64_t turn[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) turn[e] = lane_turn(P.rope.turn, c + e);
-    }
-    fetch(tok0, 0, next);
-    for (int tk = tok0, i = 0; tk <= tok1; tk += 8, ++i) {
-        if ((i & 31) == 0 && P.turn) pos32 = tk + 8 * lane <= tok1 ? __ldg(P.turn + w.R.q0 + tk + 8 * lane) : 0;
-        const int64_t pos = __shfl_sync(0xffffffffu, pos32, i & 31);
+        const int pos_row = __ldg(P.turn + w.R.q0 + (w.row0 + r0 + min(lane, n - 1)) / G);
+        int pos_cs = __shfl_sync(0xffffffffu, pos_row, 0);
         float2 cs[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) cs[e] = P.turn ? turn_cs(turn[e], pos) : make_float2(1.f, 0.f);
-        for (int g0 = 0; g0 < G; g0 += kHeads) {
-            uint32_t x[kHeads][2];
+        for (int e = 0; e < E; ++e) cs[e] = turn_cs_fast(turn[e], pos_cs);
+        cp_async_wait<0>();
+        __syncwarp();
+#pragma unroll 1
+        for (int i0 = 0; i0 < 32; i0 += kBatch) {
+            uint32_t x0[kBatch], x1[kBatch];
+            const uint32_t a0 = (c & 7) * 2 + (q0 >> 3) * C::kHalf + tile + i0 * 128, a1 = (c & 7) * 2 + (q1 >> 3) * C::kHalf + tile + i0 * 128;
 #pragma unroll
-            for (int g = 0; g < kHeads; ++g) {
-                x[g][0] = next[g][0];
-                x[g][1] = next[g][1];
-            }
-            const bool last = g0 + kHeads >= G;
-            fetch(last ? tk + 8 : tk, last ? 0 : g0 + kHeads, next);
-#pragma unroll
-            for (int g = 0; g < kHeads; ++g) {
-                const int row = tk * G + g0 + g - w.row0;
-                if (g0 + g >= G || row < 0 || row >= w.live) continue;
-                float lo[E], hi[E];
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    lo[e] = __uint_as_float(e == 0 ? x[g][0] << 16 : x[g][0] & 0xffff0000u);
-                    hi[e] = __uint_as_float(e == 0 ? x[g][1] << 16 : x[g][1] & 0xffff0000u);
-                    if (P.turn) {
-                        float a, b;
-                        rotate1(lo[e], hi[e], cs[e], a, b);
-                        lo[e] = a;
-                        hi[e] = b;
-                    }
-                }
+            for (int i = 0; i < kBatch; ++i) {           // (i0 is a multiple of 8: the rows swap as rows 0 .. 7 do)
+                const uint32_t s0 = a0 + i * 128 + (((q0 & 7) ^ i) << 4), s1 = a1 + i * 128 + (((q1 & 7) ^ i) << 4);
                 if constexpr (E == 2) {
-                    put(row, c, lo[0], lo[1]);
-                    put(row, D / 2 + c, hi[0], hi[1]);
+                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x0[i]) : "r"(s0));
+                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x1[i]) : "r"(s1));
                 } else {
-                    const float y0 = __shfl_down_sync(0xffffffffu, lo[0], 1), y1 = __shfl_down_sync(0xffffffffu, hi[0], 1);
-                    if (!(lane & 1)) {
-                        put(row, c, lo[0], y0);
-                        put(row, D / 2 + c, hi[0], y1);
-                    }
+                    uint16_t y0, y1;
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y0) : "r"(s0));
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y1) : "r"(s1));
+                    x0[i] = y0;
+                    x1[i] = y1;
+                }
+            }
+            float lo[kBatch][E], hi[kBatch][E];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const int pos = __shfl_sync(0xffffffffu, pos_row, i0 + i);
+                if (pos != pos_cs) {                     // the heads of a token share its angles
+#pragma unroll
+                    for (int e = 0; e < E; ++e) cs[e] = turn_cs_fast(turn[e], pos);
+                    pos_cs = pos;
+                }
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    rotate1(__uint_as_float(e == 0 ? x0[i] << 16 : x0[i] & 0xffff0000u),
+                            __uint_as_float(e == 0 ? x1[i] << 16 : x1[i] & 0xffff0000u), cs[e], lo[i][e], hi[i][e]);
+            }
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const uint32_t s0 = a0 + i * 128 + (((q0 & 7) ^ i) << 4), s1 = a1 + i * 128 + (((q1 & 7) ^ i) << 4);
+                if constexpr (E == 2) {
+                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(s0), "r"(pack_bf16(lo[i][0], lo[i][1])));
+                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(s1), "r"(pack_bf16(hi[i][0], hi[i][1])));
+                } else {
+                    asm volatile("st.shared.u16 [%0], %1;" ::"r"(s0), "h"(__bfloat16_as_ushort(__float2bfloat16_rn(lo[i][0]))));
+                    asm volatile("st.shared.u16 [%0], %1;" ::"r"(s1), "h"(__bfloat16_as_ushort(__float2bfloat16_rn(hi[i][0]))));
                 }
             }
         }
+    } else {
+        cp_async_wait<0>();
     }
-    // rows of no query: zero, so that what they hold is a number
-    for (int row = w.live + warp; row < kPair; row += 8)
-        for (int ch = 2 * lane; ch < D; ch += 64) put(row, ch, 0.f, 0.f);
 }
 
 // One softmax thread: row r of tile x over the CTA's key tiles, then its output.
@@ -507,8 +509,7 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                *reinterpret_cast<uint4*>(prow + c * 32 + k * 4) = make_uint4(ov[4 * k], ov[4 * k + 1], ov[4 * k + 2], ov[4 * k + 3]);
+            for (int k = 0; k < 4; ++k) stg256(prow + c * 32 + k * 8, ov + 8 * k);
         }
     }
     if (there) {
@@ -551,7 +552,6 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tc_kernel(const __grid_cons
     uint32_t* const notes = reinterpret_cast<uint32_t*>(smem + C::kNotes);   // of a tile: which groups of 16 keys are there
     uint32_t* const slot = reinterpret_cast<uint32_t*>(smem + C::kSlot);
     volatile uint32_t* const abort = slot + 1;
-    volatile uint32_t& s_last = slot[2];
     auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const Item w = find_item(P);
@@ -584,6 +584,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tc_kernel(const __grid_cons
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *slot;
+    // the kernel that joins cut keys may be set up from here on: it waits for this grid to end
+    if (threadIdx.x == 0) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsLow));
@@ -599,107 +601,246 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tc_kernel(const __grid_cons
     }
 
     tc_fence_before();
-    if (w.R.splits > 1) __threadfence();                         // the partials, before the ticket
     __syncthreads();
     if (warp == 0) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
     }
-    if (w.R.splits == 1) return;
-    if (threadIdx.x == 0) {
-        const uint32_t t = atomicAdd(X.tickets + w.unit, 1u);
-        s_last = t == (uint32_t)w.R.splits - 1;
-        if (s_last) X.tickets[w.unit] = 0;
+}
+
+// The stretches of cut keys joined: 32 rows of a unit a CTA, eight rows a thread on their way at once.
+// (Joined by the last stretch of a unit instead, 19 partials of 128 KB came through one SM: 72 us for 64
+// tokens over 30000 rows, where this takes 4 of them.)
+constexpr int kJoinThreads = 128, kJoinRows = 32;
+
+template <int D, int kReq>
+__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_constant__ TcLaunch<kReq> X) {
+    const PagedAttn<kReq>& P = X.a;
+    extern __shared__ float weight[];                            // [stretch][row]
+    constexpr int kSlices = kPair / kJoinRows;
+    const int u = blockIdx.x / kSlices, slice = blockIdx.x % kSlices;
+    int r = 0;
+    while (r + 1 < P.batch && P.req[r + 1].unit0 <= u) ++r;      // (entries that are not cut have no units)
+    asm volatile("griddepcontrol.wait;" ::: "memory");           // the partials are complete and visible
+    const PagedReq R = P.req[r];
+    const int G = P.hq / P.hkv, S = R.splits, k0 = u - R.unit0, hk = k0 % P.hkv, pr = R.tile0 + k0 / P.hkv;
+    const int first = slice * kJoinRows, live = min(kJoinRows, R.nq * G - pr * kPair - first);
+    if (live <= 0) return;
+    // items of the unit's stretch k: see find_item
+    const int64_t item0 = R.item0 + ((int64_t)(R.tile0 + R.tiles - 1 - pr) * S) * P.hkv + hk;
+    for (int row = threadIdx.x; row < live; row += kJoinThreads) {
+        float top = -CUDART_INF_F, sum = 0.f;
+        for (int k = 0; k < S; ++k) {
+            const float e = __ldcg(X.part_lse + (item0 + (int64_t)k * P.hkv) * kPair + first + row);
+            weight[k * kJoinRows + row] = e;
+            top = fmaxf(top, e);
+        }
+        const float base = top == -CUDART_INF_F ? 0.f : top;
+        for (int k = 0; k < S; ++k) sum += ex2(weight[k * kJoinRows + row] - base);
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        for (int k = 0; k < S; ++k) weight[k * kJoinRows + row] = ex2(weight[k * kJoinRows + row] - base) * inv;
+        if (P.lse) {
+            const int all = pr * kPair + first + row;
+            P.lse[(int64_t)(hk * G + all % G) * P.n_tokens + R.q0 + all / G] = sum == 0.f ? -CUDART_INF_F : (top + log2f(sum)) * 0.69314718055994531f;
+        }
     }
     __syncthreads();
-    if (!s_last) return;
-    __threadfence();
-    // the unit's stretches joined: items of stretch k are hkv apart
-    const int G = P.hq / P.hkv, S = w.R.splits;
-    const int64_t item0 = (int64_t)blockIdx.x - (int64_t)w.sp * P.hkv;
-    for (int i = threadIdx.x; i < w.live * (D / 4); i += kThreads) {
-        const int row = i / (D / 4), f = i % (D / 4);
-        float top = -CUDART_INF_F, sum = 0.f;
-        for (int k = 0; k < S; ++k) top = fmaxf(top, __ldcg(X.part_lse + (item0 + (int64_t)k * P.hkv) * kPair + row));
-        const float base = top == -CUDART_INF_F ? 0.f : top;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = 0; k < S; ++k) {
-            const int64_t at = (item0 + (int64_t)k * P.hkv) * kPair + row;
-            const float a = ex2(__ldcg(X.part_lse + at) - base);
-            const float4 y = __ldcg(reinterpret_cast<const float4*>(X.part_o + at * D + 4 * f));
-            sum += a;
-            o.x = fmaf(y.x, a, o.x);
-            o.y = fmaf(y.y, a, o.y);
-            o.z = fmaf(y.z, a, o.z);
-            o.w = fmaf(y.w, a, o.w);
+    constexpr int kLines = D / 4, kStep = kJoinThreads / kLines, kRows = kJoinRows / kStep;
+    const int f = threadIdx.x % kLines, row0 = threadIdx.x / kLines;
+    float4 o[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = 0; k < S; ++k) {
+        const float* const from = X.part_o + ((item0 + (int64_t)k * P.hkv) * kPair + first) * D + 4 * f;
+        float4 y[kRows];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) y[i] = __ldcg(reinterpret_cast<const float4*>(from + (int64_t)min(row0 + i * kStep, live - 1) * D));
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const float a = weight[k * kJoinRows + min(row0 + i * kStep, live - 1)];
+            o[i].x = fmaf(y[i].x, a, o[i].x);
+            o[i].y = fmaf(y[i].y, a, o[i].y);
+            o[i].z = fmaf(y[i].z, a, o[i].z);
+            o[i].w = fmaf(y[i].w, a, o[i].w);
         }
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        const int64_t tok = w.R.q0 + (w.row0 + row) / G;
-        const int h = w.hk * G + (w.row0 + row) % G;
-        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(P.out) + (tok * P.hq + h) * D + 4 * f) =
-            make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-        if (f == 0 && P.lse) P.lse[(int64_t)h * P.n_tokens + tok] = sum == 0.f ? -CUDART_INF_F : (top + log2f(sum)) * 0.69314718055994531f;
+    }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int row = row0 + i * kStep;
+        if (row >= live) continue;
+        const int all = pr * kPair + first + row;
+        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(P.out) + ((int64_t)(R.q0 + all / G) * P.hq + hk * G + all % G) * D + 4 * f) =
+            make_uint2(pack_bf16(o[i].x, o[i].y), pack_bf16(o[i].z, o[i].w));
     }
 }
 
+// ------------------------------------------------------------------ host side
+
+// Work items and their order.  A pair of row tiles over all its keys is one item, or its keys are cut
+// into stretches whose partials are joined: a stretch costs its own start and end (about as much as
+// kStart key tiles) and 128 KB written and read.  So keys are cut only where the schedule gets shorter:
+// where units are fewer than SMs, where one request's are much longer than the others', and in the last
+// round of many equal units.  The schedules compared are estimated by dealing items, longest first, to
+// the SMs that are free first, as the hardware does.
+constexpr double kStart = 6.0, kCutStart = 11.0;
+
+struct Deal {
+    // SMs by their load: (load, how many)
+    std::vector<std::pair<double, int>> sms;
+    explicit Deal(int n) { sms.push_back({0.0, n}); }
+    void items(double cost, int64_t count) {
+        while (count > 0) {
+            auto low = std::min_element(sms.begin(), sms.end());
+            // whole rounds over equally loaded SMs at once
+            if (sms.size() == 1 && count >= low->second) {
+                const int64_t rounds = count / low->second;
+                low->first += cost * rounds;
+                count -= rounds * low->second;
+                continue;
+            }
+            const int take = (int)std::min<int64_t>(low->second, count);
+            const double to = low->first + cost;
+            low->second -= take;
+            if (low->second == 0) sms.erase(low);
+            auto same = std::find_if(sms.begin(), sms.end(), [&](const auto& x) { return x.first == to; });
+            if (same != sms.end()) same->second += take;
+            else sms.push_back({to, take});
+            count -= take;
+        }
+    }
+    double longest() const { return std::max_element(sms.begin(), sms.end())->first; }
+};
+
+// Entries of the launch: requests, or parts of them that are cut alike; longest items first.
+std::vector<PagedReq> plan(const PagedAttnCall& c, const PagedReq* req, int n) {
+    const int slots = device_sms(), G = c.hq / c.hkv;
+    auto pairs_of = [&](const PagedReq& q) { return (int)(((int64_t)q.nq * G + kPair - 1) / kPair); };
+    auto keys_of = [&](const PagedReq& q, int pr) {      // key tiles of a pair
+        const int last = (int)std::min<int64_t>((int64_t)(pr + 1) * kPair, (int64_t)q.nq * G) - 1;
+        const int hi = q.n_keys - q.nq + last / G + 1, lo = c.window ? std::max(0, q.n_keys - q.nq + pr * kPair / G - c.window + 1) : 0;
+        return std::max(1, (hi + BN - 1) / BN - lo / BN);
+    };
+    auto piece = [](const PagedReq& e, int keys) { return (keys + e.splits - 1) / e.splits + (e.splits > 1 ? kCutStart : kStart); };
+    int64_t units = 0;
+    int longest = 1;
+    for (int i = 0; i < n; ++i) {
+        units += (int64_t)pairs_of(req[i]) * c.hkv;
+        longest = std::max(longest, keys_of(req[i], pairs_of(req[i]) - 1));
+    }
+    std::vector<PagedReq> best;
+    double best_cost = 0;
+    // at: stretches of at most this many key tiles; rest > 0: only the last round's units are cut, into rest
+    auto consider = [&](int at, int rest) {
+        std::vector<PagedReq> e;
+        const int64_t cut_units = rest ? units - units / slots * slots : 0;
+        int64_t left = (cut_units + c.hkv - 1) / c.hkv;   // pairs still to be cut
+        for (int i = n - 1; i >= 0; --i) {
+            PagedReq q = req[i];
+            const int pairs = pairs_of(q);
+            if (!rest) {
+                q.tile0 = 0;
+                q.tiles = pairs;
+                q.splits = (keys_of(q, pairs - 1) + at - 1) / at;
+                e.push_back(q);
+                continue;
+            }
+            const int cut = (int)std::min<int64_t>(left, pairs);          // the first pairs: those of fewest keys
+            left -= cut;
+            if (pairs > cut) {
+                q.tile0 = cut;
+                q.tiles = pairs - cut;
+                q.splits = 1;
+                e.push_back(q);
+            }
+            if (cut > 0) {
+                q.tile0 = 0;
+                q.tiles = cut;
+                q.splits = std::max(1, std::min(rest, keys_of(q, cut - 1)));
+                e.push_back(q);
+            }
+        }
+        std::stable_sort(e.begin(), e.end(), [&](const PagedReq& a, const PagedReq& b) {
+            return piece(a, keys_of(a, a.tile0 + a.tiles - 1)) > piece(b, keys_of(b, b.tile0 + b.tiles - 1));
+        });
+        Deal d(slots);
+        for (const PagedReq& q : e) {
+            // up to four groups of pairs, each as long as its longest
+            for (int g = std::min(4, q.tiles), hi = q.tile0 + q.tiles; g > 0; --g) {
+                const int lo = q.tile0 + q.tiles * (g - 1) / std::min(4, q.tiles);
+                d.items(piece(q, keys_of(q, hi - 1)), (int64_t)(hi - lo) * c.hkv * q.splits);
+                hi = lo;
+            }
+        }
+        if (best.empty() || d.longest() < best_cost * 0.97) {     // (ties go to fewer cuts)
+            best_cost = d.longest();
+            best = std::move(e);
+        }
+    };
+    consider(longest, 0);
+    if (units < 8 * (int64_t)slots) {
+        for (const int k : {2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+            const int at = (longest + k - 1) / k;
+            if (at < 2 || units * k > 16 * (int64_t)slots) break;
+            consider(at, 0);
+        }
+        if (units < slots) consider((int)std::max<int64_t>(2, (longest * units + slots - 1) / slots), 0);   // (one round of equal stretches)
+        if (units > slots && units % slots)
+            for (const int k : {2, 3, 4, 5, 6, 7, 8}) consider(longest, k);
+    }
+    return best;
+}
+
 template <int D, int kReq>
-cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStream_t s) {
+cudaError_t launch(const PagedAttnCall& c, const std::vector<PagedReq>& entries, cudaStream_t s) {
     static PerDevice<cudaError_t> smem_set;
     const auto kernel = paged_tc_kernel<D, kReq>;
     cudaError_t e = opt_in_smem(smem_set, (const void*)kernel, Tc<D>::kSmem);
     if (e != cudaSuccess) return e;
-    for (int b0 = 0; b0 < n; b0 += kReq) {
-        const int nb = std::min(n - b0, kReq);
+    const int rows = 1 << c.pg.page_shift;
+    for (size_t b0 = 0; b0 < entries.size(); b0 += kReq) {
+        const int nb = (int)std::min<size_t>(entries.size() - b0, kReq);
         TcLaunch<kReq> X;
-        fill_paged(X.a, c, D, req + b0, nb);
-        const int slots = device_sms(), G = c.hq / c.hkv;
-        auto pairs_of = [&](const PagedReq& q) { return (q.nq * G + kPair - 1) / kPair; };
-        auto tiles_of = [&](const PagedReq& q) {
-            const int keys = c.window ? std::min(q.n_keys, c.window + std::min(q.nq, kPair / G + 1) + BN) : q.n_keys;
-            return std::max(1, (keys + BN - 1) / BN);
-        };
-        // Keys are cut only where whole units would leave SMs without work, into stretches of eight
-        // tiles and more (a stretch's partial is written and read again, 128 KB).
-        int64_t units = 0, tiles = 0;
-        for (int i = 0; i < nb; ++i) {
-            units += (int64_t)pairs_of(X.a.req[i]) * c.hkv;
-            tiles += (int64_t)pairs_of(X.a.req[i]) * c.hkv * tiles_of(X.a.req[i]);
-        }
-        int per = units >= slots ? 1 << 30 : std::max(8, (int)((tiles + slots - 1) / slots));
-        auto count = [&](int p) {
-            int64_t items = 0;
-            for (int i = 0; i < nb; ++i) items += (int64_t)pairs_of(X.a.req[i]) * c.hkv * ((tiles_of(X.a.req[i]) + (int64_t)p - 1) / p);
-            return items;
-        };
-        while (per < (1 << 20) && count(per) > slots) per += std::max(1, per / 16);
-        int64_t items = 0;
-        units = 0;
-        bool split = false;
+        fill_paged(X.a, c, D, entries.data() + b0, nb);
+        int64_t items = 0, units = 0;
+        int32_t most = 1;
         for (int i = 0; i < nb; ++i) {
             PagedReq& q = X.a.req[i];
-            q.splits = (int32_t)((tiles_of(q) + (int64_t)per - 1) / per);
-            split = split || q.splits > 1;
             q.item0 = (int32_t)items;
             q.unit0 = (int32_t)units;
-            units += (int64_t)pairs_of(q) * c.hkv;
-            items += (int64_t)pairs_of(q) * c.hkv * q.splits;
+            if (q.splits > 1) {
+                units += (int64_t)q.tiles * c.hkv;
+                most = std::max(most, q.splits);
+            }
+            items += (int64_t)q.tiles * c.hkv * q.splits;
         }
         X.part_o = X.part_lse = nullptr;
-        X.tickets = nullptr;
-        if (split) {
+        if (units > 0) {
             void* p = nullptr;
+            uint32_t* none = nullptr;
             const size_t o_bytes = (size_t)items * kPair * D * 4;
-            e = context_workspace(c.ctx, o_bytes + (size_t)items * kPair * 4, (size_t)units, &p, &X.tickets);
+            e = context_workspace(c.ctx, o_bytes + (size_t)items * kPair * 4, 0, &p, &none);
             if (e != cudaSuccess) return e;
             X.part_o = static_cast<float*>(p);
             X.part_lse = reinterpret_cast<float*>(static_cast<char*>(p) + o_bytes);
         }
-        const int rows = 1 << c.pg.page_shift;
         if (!encode_page_map(&X.tm_k, c.pg.k, c.pg, c.hkv, D, false, 64, rows, CU_TENSOR_MAP_SWIZZLE_128B) ||
             !encode_page_map(&X.tm_v, c.pg.v, c.pg, c.hkv, D, false, 64, rows, CU_TENSOR_MAP_SWIZZLE_128B))
             return cudaErrorInvalidValue;
         kernel<<<(unsigned)items, kThreads, Tc<D>::kSmem, s>>>(X);
         e = cudaGetLastError();
+        if (e == cudaSuccess && units > 0) {
+            cudaLaunchConfig_t cfg{};
+            cudaLaunchAttribute at{};
+            at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            at.val.programmaticStreamSerializationAllowed = 1;
+            cfg.gridDim = dim3((unsigned)(units * (kPair / kJoinRows)));
+            cfg.blockDim = dim3(kJoinThreads);
+            cfg.dynamicSmemBytes = (size_t)most * kJoinRows * 4;
+            cfg.stream = s;
+            cfg.attrs = &at;
+            cfg.numAttrs = 1;
+            e = cudaLaunchKernelEx(&cfg, paged_join_kernel<D, kReq>, X);
+        }
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
@@ -707,7 +848,8 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
 
 template <int D>
 cudaError_t by_count(const PagedAttnCall& c, const PagedReq* req, int n, cudaStream_t s) {
-    return n <= kPagedFew ? launch<D, kPagedFew>(c, req, n, s) : launch<D, kPagedMany>(c, req, n, s);
+    const std::vector<PagedReq> entries = plan(c, req, n);
+    return (int)entries.size() <= kPagedFew ? launch<D, kPagedFew>(c, entries, s) : launch<D, kPagedMany>(c, entries, s);
 }
 
 }  // namespace
