@@ -97,10 +97,10 @@ _SIGS = {
     "c2kv_attend_noalloc": (_I32, [_VP, _VP, _I32, _VP, _VP, _VP, _I32, _VP, _VP]),
     "c2kv_decode": (_I32, [_VP, _VP, _I32, _VP, _VP, _VP, _P32, _VP, _VP]),
     "c2kv_extract_attention": (_I32, [_VP, _I32, _VP, _VP, _VP, _I32, _I32, _VP, _VP]),
-    "c2kv_paged_append": (_I32, [_VP, _VP, _I32, _VP, _I32, _I64, _P32, _P32, _VP, _VP, _I64, _VP]),
-    "c2kv_paged_gather": (_I32, [_VP, _VP, _I32, _VP, _I32, _I64, _P32, _P32, _VP, _VP, _I64, _VP]),
-    "c2kv_paged_attend": (_I32, [_VP, _VP, _I32, _VP, _I32, _I64, _P32, _P32, _I32, _VP, _I64, _VP, _VP, _VP]),
-    "c2kv_verify_drafts": (_I32, [_VP, _I32, _P32, _I32, _VP, _VP, _I64, _VP, _I64, _VP, _VP, _VP, _VP]),
+    "c2kv_paged_append": (_I32, [_VP, _VP, _I32, _VP, _I32, _I64, _VP, _VP, _VP, _VP, _I64, _VP]),
+    "c2kv_paged_gather": (_I32, [_VP, _VP, _I32, _VP, _I32, _I64, _VP, _VP, _VP, _VP, _I64, _VP]),
+    "c2kv_paged_attend": (_I32, [_VP, _VP, _I32, _VP, _I32, _I64, _VP, _VP, _I32, _VP, _I64, _VP, _VP, _VP]),
+    "c2kv_verify_drafts": (_I32, [_VP, _I32, _VP, _I32, _VP, _VP, _I64, _VP, _I64, _VP, _VP, _VP, _VP]),
     "c2kv_cache_release": (_I32, [_VP, _VP]),
     "c2kv_sync": (_I32, [_VP]),
     "c2kv_last_error": (ctypes.c_char_p, [_VP]),
@@ -154,6 +154,20 @@ def _i32(arr):
             return p, p
     a = np.ascontiguousarray(np.asarray(arr, dtype=np.int32))
     return a, a.ctypes.data_as(_P32)
+
+
+def _i32_at(arr):
+    """The values as int32 memory that the first result keeps, its address and how many there are: for
+    calls that a generation step makes by the dozen (an address costs half of what a pointer does)."""
+    if type(arr) is list:
+        try:
+            a = array.array("i", arr)
+        except TypeError:
+            pass
+        else:
+            return a, a.buffer_info()[0], len(a)
+    a = np.ascontiguousarray(np.asarray(arr, dtype=np.int32))
+    return a, a.ctypes.data, len(a)
 
 
 def _stream_handle(stream):
@@ -296,67 +310,72 @@ def _table(table, batch, rows):
     """Address, width and row stride of a table of page numbers (a torch int32 tensor [B, width]) for
     the requests that a call's host arrays describe."""
     b, w = table.shape
-    if b != batch or len(rows) != batch:
+    if b != batch or rows != batch:
         raise ValueError("the table, the ranges and the rows must describe one batch")
-    if table.element_size() != 4 or (w > 1 and table.stride(1) != 1):
-        raise ValueError("a table's rows must be dense int32")
+    if table.element_size() != 4:
+        raise ValueError("a table holds int32")
+    if table.is_contiguous():
+        return table.data_ptr(), w, w
+    if w > 1 and table.stride(1) != 1:
+        raise ValueError("a table's rows must be dense")
     return table.data_ptr(), w, table.stride(0) if b > 1 else w
+
+
+def _token_stride(x):
+    """Elements between tokens of a torch tensor [T, heads, d] whose heads are dense (0: dense too)."""
+    if x.is_contiguous():
+        return 0
+    t, h, d = x.shape
+    if (h > 1 and x.stride(1) != d) or x.stride(2) != 1:
+        raise ValueError("a token's heads must be one dense block")
+    return x.stride(0) if t > 1 else 0
+
+
+def _pair_stride(x, y):
+    """The token stride of two tensors of one shape."""
+    s, t = _token_stride(x), _token_stride(y)
+    if s != t and x.shape[0] > 1 and x.stride(0) != y.stride(0):
+        raise ValueError("k and v must have one token stride")
+    return s or t
+
+
+def _row_stride(x):
+    return 0 if x is None or x.is_contiguous() or x.shape[0] < 2 else x.stride(0)
 
 
 def c2kv_paged_append(ctx, pages, table, new_ptr, start, k, v, turn=None):
     """Write new tokens k, v [T, Hkv, d] into their requests' pages, K turned by turn [T]."""
-    ptr, ptr_p = _i32(new_ptr)
-    st, st_p = _i32(start)
-    batch = len(ptr) - 1
-    tb, w, ts = _table(table, batch, st)
-    _check(_lib.c2kv_paged_append(ctx, pages.address, batch, tb, w, ts, ptr_p, st_p, _ptr(k), _ptr(v),
-                                  _token_stride(k, v), _ptr(turn)), ctx)
+    ptr, ptr_p, n = _i32_at(new_ptr)
+    st, st_p, m = _i32_at(start)
+    tb, w, ts = _table(table, n - 1, m)
+    _check(_lib.c2kv_paged_append(ctx, pages.address, m, tb, w, ts, ptr_p, st_p, k.data_ptr(), v.data_ptr(), _pair_stride(k, v),
+                                  _ptr(turn)), ctx)
 
 
 def c2kv_paged_gather(ctx, pages, table, row_ptr, start, k_out, v_out, turn=None):
     """Read rows of the pages back into k_out, v_out [T, Hkv, d], K turned by turn [T]."""
-    ptr, ptr_p = _i32(row_ptr)
-    st, st_p = _i32(start)
-    batch = len(ptr) - 1
-    tb, w, ts = _table(table, batch, st)
-    _check(_lib.c2kv_paged_gather(ctx, pages.address, batch, tb, w, ts, ptr_p, st_p, _ptr(k_out), _ptr(v_out),
-                                  _token_stride(k_out, v_out), _ptr(turn)), ctx)
+    ptr, ptr_p, n = _i32_at(row_ptr)
+    st, st_p, m = _i32_at(start)
+    tb, w, ts = _table(table, n - 1, m)
+    _check(_lib.c2kv_paged_gather(ctx, pages.address, m, tb, w, ts, ptr_p, st_p, k_out.data_ptr(), v_out.data_ptr(),
+                                  _pair_stride(k_out, v_out), _ptr(turn)), ctx)
 
 
 def c2kv_paged_attend(ctx, pages, table, q_ptr, n_keys, q, out, lse=None, turn=None, window=0):
     """Attention of each request's newest tokens q [T, Hq, d] over its n_keys rows."""
-    ptr, ptr_p = _i32(q_ptr)
-    nk, nk_p = _i32(n_keys)
-    batch = len(ptr) - 1
-    tb, w, ts = _table(table, batch, nk)
-    _check(_lib.c2kv_paged_attend(ctx, pages.address, batch, tb, w, ts, ptr_p, nk_p, window, _ptr(q),
-                                  _token_stride(q), _ptr(turn), _ptr(out), _ptr(lse)), ctx)
+    ptr, ptr_p, n = _i32_at(q_ptr)
+    nk, nk_p, m = _i32_at(n_keys)
+    tb, w, ts = _table(table, n - 1, m)
+    _check(_lib.c2kv_paged_attend(ctx, pages.address, m, tb, w, ts, ptr_p, nk_p, window, q.data_ptr(), _token_stride(q), _ptr(turn),
+                                  _ptr(out), _ptr(lse)), ctx)
 
 
 def c2kv_verify_drafts(ctx, draft_ptr, tokens, p, q, u_accept, u_next, n_accepted, next_token):
     """Accept drafted tokens against the target's probabilities p [T + B, V] and the draft's q [T, V]
     (None: drafts without probabilities), and draw the token that follows them."""
-    ptr, ptr_p = _i32(draft_ptr)
-    _check(_lib.c2kv_verify_drafts(ctx, len(ptr) - 1, ptr_p, p.shape[1], _ptr(tokens), _ptr(p), _row_stride(p), _ptr(q),
-                                   _row_stride(q), _ptr(u_accept), _ptr(u_next), _ptr(n_accepted), _ptr(next_token)), ctx)
-
-
-def _token_stride(*tensors):
-    """Elements between tokens of torch tensors [T, heads, d] whose heads are dense (0: as they are)."""
-    s = 0
-    for x in tensors:
-        t, h, d = x.shape
-        if (h > 1 and x.stride(1) != d) or x.stride(2) != 1:
-            raise ValueError("a token's heads must be one dense block")
-        mine = x.stride(0) if t > 1 else 0
-        if s and mine and mine != s:
-            raise ValueError("tensors of one call must have one token stride")
-        s = mine or s
-    return s
-
-
-def _row_stride(x):
-    return 0 if x is None or x.shape[0] < 2 else x.stride(0)
+    ptr, ptr_p, n = _i32_at(draft_ptr)
+    _check(_lib.c2kv_verify_drafts(ctx, n - 1, ptr_p, p.shape[1], _ptr(tokens), p.data_ptr(), _row_stride(p), _ptr(q), _row_stride(q),
+                                   _ptr(u_accept), _ptr(u_next), _ptr(n_accepted), _ptr(next_token)), ctx)
 
 
 def c2kv_cache_release(ctx, cache):
