@@ -9,8 +9,10 @@
 // Two rows of the vocabulary are read once a request, which bounds the call at HBM's rate for a batch
 // and at the chain draft -> probabilities -> sum -> search for one request.  A cluster of CTAs shares a
 // request: each warp sums one contiguous stretch, the CTAs exchange their totals through distributed
-// shared memory, and the warp whose stretch holds the goal reads that stretch again (from L2).
+// shared memory, and the warp whose stretch holds the goal reads that stretch again (from L2).  Clusters
+// are as large as keeps them all on the GPU at once: 64 requests in clusters of 8 took two rounds.
 #include "paged.cuh"
+#include "per_device.cuh"
 
 #include <algorithm>
 
@@ -27,9 +29,21 @@ __device__ __forceinline__ uint64_t warp_sum(uint64_t x) {
     return x;
 }
 
-// A weight in [0, 1] as a multiple of 2^-44, cut off; NaN counts as 0 (fmaxf gives its other operand).
+// A weight in [0, 1] as a multiple of 2^-44, cut off, in two parts of 22 bits; NaN counts as 0 (fmaxf
+// gives its other operand).  Adding 2^23 rounded down leaves a whole number's bits in the fraction, and
+// every difference here is exact: five FP32 operations, where the conversion to 64 bits is slow.
+struct Parts {
+    uint32_t hi, lo;
+};
+__device__ __forceinline__ Parts parts(float w) {
+    const float x = fminf(fmaxf(w, 0.f), 1.f) * 0x1p22f;
+    const float a = __fadd_rd(x, 0x1p23f);
+    const float b = __fadd_rd((x - (a - 0x1p23f)) * 0x1p22f, 0x1p23f);
+    return {__float_as_uint(a) - 0x4b000000u, __float_as_uint(b) - 0x4b000000u};
+}
 __device__ __forceinline__ uint64_t whole(float w) {
-    return __float2ull_rz(fminf(fmaxf(w, 0.f), 1.f) * 0x1p44f);
+    const Parts p = parts(w);
+    return ((uint64_t)p.hi << 22) + p.lo;
 }
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -45,49 +59,116 @@ __device__ __forceinline__ uint32_t cluster_size() {
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
-// The 8 bytes at this CTA's shared address `local`, in the cluster's CTA `rank`.
-__device__ __forceinline__ uint64_t ld_peer(const uint64_t* local, uint32_t rank) {
+// 8 bytes to this CTA's shared address `local`, in the cluster's CTA `rank`.
+__device__ __forceinline__ void st_peer(const uint64_t* local, uint32_t rank, uint64_t v) {
     const uint32_t a = static_cast<uint32_t>(__cvta_generic_to_shared(local));
     uint32_t peer;
-    uint64_t v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(peer) : "r"(a), "r"(rank));
-    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(peer) : "memory");
-    return v;
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(peer), "l"(v) : "memory");
 }
 
-// Weight of token i: what p leaves over q (q may be null), or p without the refused token `drop`.
+// The row that a token is drawn from: what p leaves over q (q may be null), or p without the refused
+// token `drop`.
 struct Row {
     const float* p;
     const float* q;
     int drop;
-    __device__ __forceinline__ uint64_t at(int i) const {
-        const float w = q ? __ldg(p + i) - __ldg(q + i) : __ldg(p + i);
-        return i == drop ? 0 : whole(w);
-    }
 };
 
-// The sum of a warp's stretch [a, b), each lane's part summed over eight loads at a time.
+constexpr int kChunk = 512;              // elements a warp has on their way at once, 16 a lane
+
+// Weights of elements i + 128 u + 4 lane + e (v[4 u + e]) below b, 0 past it: by four 16-byte loads of
+// each row where both allow it (128 KB in flight an SM; at half of it the rows came at 2.4 TB/s).  Rows
+// that do not (an odd vocabulary) are read in the same order for a search; for a sum, whose order is
+// free, lanes take neighbours.
+template <bool kInOrder>
+__device__ __forceinline__ void load_chunk(const Row& w, int i, int b, int lane, float (&v)[16]) {
+    // (i is a multiple of 32 elements, so the rows' addresses decide)
+    const bool wide = ((reinterpret_cast<uintptr_t>(w.p) | reinterpret_cast<uintptr_t>(w.q)) & 15u) == 0 && i + kChunk <= b;
+    if (wide) {
+        float4 x[4], y[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = __ldg(reinterpret_cast<const float4*>(w.p + i + 128 * u) + lane);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            y[u] = w.q ? __ldg(reinterpret_cast<const float4*>(w.q + i + 128 * u) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            v[4 * u] = x[u].x - y[u].x;
+            v[4 * u + 1] = x[u].y - y[u].y;
+            v[4 * u + 2] = x[u].z - y[u].z;
+            v[4 * u + 3] = x[u].w - y[u].w;
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+            const int e = kInOrder ? i + 128 * (u / 4) + 4 * lane + u % 4 : i + 32 * u + lane;
+            v[u] = e < b && e != w.drop ? __ldg(w.p + e) - (w.q ? __ldg(w.q + e) : 0.f) : 0.f;
+        }
+        return;
+    }
+    const int drop = w.drop - i - 4 * lane;              // from the lane's first element
+#pragma unroll
+    for (int u = 0; u < 16; ++u)
+        if (drop == 128 * (u / 4) + u % 4) v[u] = 0.f;
+}
+
+// The sum of a warp's stretch [a, b).
 __device__ __forceinline__ uint64_t stretch_sum(const Row& w, int a, int b, int lane) {
     uint64_t sum = 0;
-    int i = a + lane;
-    for (; i + 7 * 32 < b; i += 8 * 32) {
-        float x[8], y[8];
+    for (int i = a; i < b; i += kChunk) {
+        float v[16];
+        load_chunk<false>(w, i, b, lane, v);
+        uint32_t hi = 0, lo = 0;         // (parts of at most 2^22, 16 of them)
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            x[u] = __ldg(w.p + i + 32 * u);
-            y[u] = w.q ? __ldg(w.q + i + 32 * u) : 0.f;
+        for (int u = 0; u < 16; ++u) {
+            const Parts x = parts(v[u]);
+            hi += x.hi;
+            lo += x.lo;
         }
-#pragma unroll
-        for (int u = 0; u < 8; ++u) sum += i + 32 * u == w.drop ? 0 : whole(x[u] - y[u]);
+        sum += ((uint64_t)hi << 22) + lo;
     }
-    for (; i < b; i += 32) sum += w.at(i);
     return warp_sum(sum);
 }
 
+// The first element of [a, b) whose running sum, from `before` on, passes goal (there is one).
+__device__ __forceinline__ int find(const Row& w, int a, int b, int lane, uint64_t before, uint64_t goal) {
+    for (int i = a; i < b; i += kChunk) {
+        float v[16];
+        load_chunk<true>(w, i, b, lane, v);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            uint64_t x[4], upto = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) upto += x[e] = whole(v[4 * u + e]);
+            const uint64_t mine = upto;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint64_t y = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += y;
+            }
+            const uint32_t past = __ballot_sync(0xffffffffu, before + upto > goal);
+            if (past) {
+                const int from = __ffs(past) - 1;
+                uint64_t run = before + upto - mine;
+                int e = 0;
+#pragma unroll
+                for (int k = 0; k < 3; ++k) {
+                    run += x[k];
+                    e += run <= goal;
+                }
+                return i + 128 * u + 4 * from + __shfl_sync(0xffffffffu, e, from);
+            }
+            before += __shfl_sync(0xffffffffu, upto, 31);
+        }
+    }
+    return b - 1;
+}
+
 template <int kReq>
-__global__ void __launch_bounds__(kVerThreads) verify_kernel(const __grid_constant__ VerifyParams<kReq> P) {
+__global__ void __launch_bounds__(kVerThreads, 2) verify_kernel(const __grid_constant__ VerifyParams<kReq> P) {
     __shared__ uint64_t s_warp[kVerWarps];
-    __shared__ uint64_t s_total;
+    __shared__ uint64_t s_total[2][kMaxCluster];          // of the cluster's CTAs, a pass
     __shared__ int s_accepted;
     const uint32_t rank = cluster_rank(), n_cta = cluster_size();
     const int r = blockIdx.x / n_cta, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -131,20 +212,20 @@ __global__ void __launch_bounds__(kVerThreads) verify_kernel(const __grid_consta
     uint64_t before = 0, total = 0;
     for (int pass = 0; pass < 2; ++pass) {
         const uint64_t mine = stretch_sum(w, a, b, lane);
+        if (pass) __syncthreads();         // (s_warp is summed above by others than its warps)
         if (lane == 0) s_warp[warp] = mine;
         __syncthreads();
         if (warp == 0) {
             const uint64_t t = warp_sum(lane < kVerWarps ? s_warp[lane] : 0);
-            if (lane == 0) s_total = t;
+            if (lane < n_cta) st_peer(&s_total[pass][rank], lane, t);
         }
-        cluster_sync();
+        cluster_sync();                    // (also of the warps' sums)
         before = total = 0;
         for (uint32_t c = 0; c < n_cta; ++c) {
-            const uint64_t t = ld_peer(&s_total, c);
+            const uint64_t t = s_total[pass][c];
             total += t;
             if (c < rank) before += t;
         }
-        cluster_sync();                    // read by all before anyone writes or leaves
         if (total != 0 || pass == 1) break;
         // nothing is left of p over q (a refusal that rounding made): p itself
         w.q = nullptr;
@@ -160,26 +241,14 @@ __global__ void __launch_bounds__(kVerThreads) verify_kernel(const __grid_consta
     const uint64_t goal = (total >> 24) * u + (((total & 0xffffff) * u) >> 24);
     for (int i = 0; i < warp; ++i) before += s_warp[i];
     if (goal < before || goal >= before + s_warp[warp]) return;
-    // the first token of the stretch whose running sum passes the goal
-    for (int i = a; i < b; i += 32) {
-        const uint64_t x = i + lane < b ? w.at(i + lane) : 0;
-        uint64_t upto = x;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint64_t y = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += y;
-        }
-        const uint32_t past = __ballot_sync(0xffffffffu, before + upto > goal);
-        if (past) {
-            if (lane == __ffs(past) - 1) P.next_token[P.b0 + r] = i + lane;
-            return;
-        }
-        before += __shfl_sync(0xffffffffu, upto, 31);
-    }
+    const int token = find(w, a, b, lane, before, goal);
+    if (lane == 0) P.next_token[P.b0 + r] = token;
 }
 
 template <int kReq>
 cudaError_t launch(const VerifyCall& c, cudaStream_t s) {
+    int size = kMaxCluster;
+    while (size > 1 && (int64_t)size * c.batch > 2 * (int64_t)device_sms()) size /= 2;
     for (int b0 = 0; b0 < c.batch; b0 += kReq) {
         const int nb = std::min(c.batch - b0, kReq);
         VerifyParams<kReq> P;
@@ -199,8 +268,8 @@ cudaError_t launch(const VerifyCall& c, cudaStream_t s) {
         cudaLaunchConfig_t cfg{};
         cudaLaunchAttribute at{};
         at.id = cudaLaunchAttributeClusterDimension;
-        at.val.clusterDim = {kMaxCluster, 1, 1};
-        cfg.gridDim = dim3(nb * kMaxCluster);
+        at.val.clusterDim = {(unsigned)size, 1, 1};
+        cfg.gridDim = dim3(nb * size);
         cfg.blockDim = dim3(kVerThreads);
         cfg.stream = s;
         cfg.attrs = &at;
