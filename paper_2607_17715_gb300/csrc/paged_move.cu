@@ -2,11 +2,12 @@
 // their positions) and V, quantised where the pages hold E4M3; c2kv_paged_gather reads rows back.
 //
 // A row of one KV head is worked on by d / 2 / N threads, N elements to 16 bytes of the dense type:
-// a thread holds N channels of the lower half and the N that they turn with, of K and of V, so four
-// 16-byte loads are in flight a thread and the turn needs no exchange.  A CTA takes as many tokens as
-// fill its threads with rows; their angles are formed once a token, in shared memory, while the rows
-// are on their way, and serve every head.
+// a thread holds N channels of the lower half and the N that they turn with, of K and of V, and works on
+// kU rows at once, so the turn needs no exchange and 64 kU bytes a thread are on their way.  A CTA takes
+// several tokens with all their heads: their pages are looked up and their angles formed once a token, in
+// shared memory, while the first rows are on their way.
 #include "paged.cuh"
+#include "per_device.cuh"
 #include "rope.cuh"
 #include "vec16.cuh"
 
@@ -16,8 +17,13 @@
 namespace c2kv {
 namespace {
 
-constexpr int kMoveThreads = 256;
+constexpr int kMoveThreads = 128;
 constexpr int kMaxTokens = 32;          // tokens of a CTA (angles: 32 x 64 x 8 bytes)
+// Rows of a thread on their way at once: two of what is read back; one of what is appended, whose maxima
+// and turns need the registers (16 requests' contexts read back: 76 us with two, 84 with one; prompts
+// appended: 44 and 35).
+__host__ __device__ constexpr int rows_at_once(bool append) { return append ? 1 : 2; }
+constexpr int kMovePasses = 2;          // passes of a CTA
 
 // Two fp32 -> two E4M3 codes (round to nearest even, clamped to +-448), lo in the low byte.
 __device__ __forceinline__ uint32_t to_codes2(float lo, float hi) {
@@ -59,32 +65,33 @@ __device__ __forceinline__ float2 row_scale(uint32_t top) {
     if (top >= 0x7f800000u) return make_float2(__uint_as_float(0x7fc00000u), 0.f);
     if (top < 0x0d800000u) return make_float2(0.f, 0.f);
     const float s = __fmul_rn(__uint_as_float(top), 1.0f / 448.0f);
-    return make_float2(s, __fdiv_rn(1.0f, s));
+    return make_float2(s, __frcp_rn(s));
 }
 
+// N codes of x * inv; inv = 0 (a row kept as zero, or not a number): codes 0.
 template <int N>
 __device__ __forceinline__ void store_codes(void* dst, const float* x, float inv) {
     uint32_t w[N / 4];
 #pragma unroll
     for (int i = 0; i < N / 4; ++i)
-        w[i] = to_codes2(x[4 * i] * inv, x[4 * i + 1] * inv) | to_codes2(x[4 * i + 2] * inv, x[4 * i + 3] * inv) << 16;
+        w[i] = inv == 0.f ? 0u
+                          : to_codes2(x[4 * i] * inv, x[4 * i + 1] * inv) | to_codes2(x[4 * i + 2] * inv, x[4 * i + 3] * inv) << 16;
     if constexpr (N == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
     else *reinterpret_cast<uint32_t*>(dst) = w[0];
 }
 
 template <int N>
-__device__ __forceinline__ void load_codes(const void* src, float* x, float scale) {
-    uint32_t w[N / 4];
-    if constexpr (N == 8) {
-        const uint2 t = __ldg(reinterpret_cast<const uint2*>(src));
-        w[0] = t.x;
-        w[1] = t.y;
-    } else {
-        w[0] = __ldg(reinterpret_cast<const uint32_t*>(src));
-    }
+__device__ __forceinline__ uint2 ld_codes(const void* src) {
+    if constexpr (N == 8) return __ldg(reinterpret_cast<const uint2*>(src));
+    else return make_uint2(__ldg(reinterpret_cast<const uint32_t*>(src)), 0u);
+}
+
+template <int N>
+__device__ __forceinline__ void from_codes(const uint2& w, float* x, float scale) {
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
-        const float2 a = from_codes2(w[i]), b = from_codes2(w[i] >> 16);
+        const uint32_t v = i ? w.y : w.x;
+        const float2 a = from_codes2(v), b = from_codes2(v >> 16);
         x[4 * i] = a.x * scale;
         x[4 * i + 1] = a.y * scale;
         x[4 * i + 2] = b.x * scale;
@@ -92,126 +99,169 @@ __device__ __forceinline__ void load_codes(const void* src, float* x, float scal
     }
 }
 
+// 2 N channels of a row, in two halves: c .. and D / 2 + c ..
+template <typename T>
+struct Halves {
+    uint4 lo, hi;
+    __device__ __forceinline__ void load(const T* p, int half) {
+        lo = ld16(p);
+        hi = ld16(p + half);
+    }
+    __device__ __forceinline__ void unpack(float* x) const {
+        Vec16<T>::unpack(lo, x);
+        Vec16<T>::unpack(hi, x + Vec16<T>::N);
+    }
+};
+
+// The largest magnitude of a thread's values as bits of fp32: two bf16 at once.
+__device__ __forceinline__ uint32_t top_of(const Halves<__nv_bfloat16>& r) {
+    const uint32_t w[8] = {r.lo.x, r.lo.y, r.lo.z, r.lo.w, r.hi.x, r.hi.y, r.hi.z, r.hi.w};
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+    return max(m & 0xffff0000u, m << 16);
+}
+__device__ __forceinline__ uint32_t top_of(const Halves<float>& r) {
+    const uint32_t w[8] = {r.lo.x, r.lo.y, r.lo.z, r.lo.w, r.hi.x, r.hi.y, r.hi.z, r.hi.w};
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7fffffffu);
+    return m;
+}
+// The same of turned values, which are numbers if those before the turn (`given`) are.
+template <int M>
+__device__ __forceinline__ uint32_t top_of_turned(const float* x, uint32_t given) {
+    float m = 0.f;
+#pragma unroll
+    for (int e = 0; e < M; ++e) m = fmaxf(m, fabsf(x[e]));
+    return given >= 0x7f800000u ? given : __float_as_uint(m);
+}
+
 template <typename T, int D, bool kCodes, bool kAppend, int kReq>
 __global__ void __launch_bounds__(kMoveThreads) paged_move_kernel(const __grid_constant__ PagedMove<kReq> P) {
-    constexpr int N = Vec16<T>::N;
+    constexpr int N = Vec16<T>::N, kU = rows_at_once(kAppend);
     constexpr int kLanes = D / 2 / N;                 // threads a row
-    constexpr int kRows = kMoveThreads / kLanes;      // rows a pass
+    constexpr int kRows = kMoveThreads / kLanes;      // rows a pass of one row a thread
     __shared__ float2 s_cs[kMaxTokens * (D / 2)];
+    __shared__ int64_t s_at[kMaxTokens], s_sat[kMaxTokens];   // where a token's row of head 0 is, in elements and scales
     const int t0 = P.t0 + blockIdx.x * P.tokens_per_cta;
     const int nt = min(P.tokens_per_cta, P.t1 - t0);
     const int lane = threadIdx.x % kLanes, c = lane * N;   // channels c .. and c + D / 2 ..
-    const int page_size = 1 << P.pg.page_shift;
-    const int n_rows = nt * P.hkv;
-    bool angles = P.turn == nullptr;
-    // every thread of the CTA makes the same passes (shuffles and the barrier below)
-    for (int i0 = 0; i0 < n_rows; i0 += kRows) {
-        const int i = i0 + threadIdx.x / kLanes;
-        const bool live = i < n_rows;
-        const int tl = live ? i / P.hkv : 0, h = live ? i - tl * P.hkv : 0, t = t0 + tl;
-        T* const dk = static_cast<T*>(P.k) + (int64_t)t * P.stride + (int64_t)h * D + c;
-        T* const dv = static_cast<T*>(P.v) + (int64_t)t * P.stride + (int64_t)h * D + c;
-        uint4 rk[2], rv[2];
-        if (kAppend && live) {
-            rk[0] = ld16(dk);
-            rk[1] = ld16(dk + D / 2);
-            rv[0] = ld16(dv);
-            rv[1] = ld16(dv + D / 2);
-        }
-        const int r = find_request(P, t);
-        const int row = P.start[r] + (t - P.ptr[r]);
-        const int page = live ? __ldg(P.pg.table + (int64_t)(P.b0 + r) * P.pg.table_stride + (row >> P.pg.page_shift)) : 0;
-        const bool ok = live && page >= 0 && page < P.pg.n_pages;
-        if (live && !ok && lane == 0) atomicOr(P.err, 1);
-        const int64_t in_page = (int64_t)h * page_size + (row & (page_size - 1));
-        const int64_t at = (int64_t)page * P.pg.page_stride + in_page * D + c;
-        const int64_t sat = (int64_t)page * P.pg.scale_stride + in_page;
-        float xk[2 * N], xv[2 * N];
-        if constexpr (kAppend) {
-            if (live) {
-                Vec16<T>::unpack(rk[0], xk);
-                Vec16<T>::unpack(rk[1], xk + N);
-                Vec16<T>::unpack(rv[0], xv);
-                Vec16<T>::unpack(rv[1], xv + N);
-            } else {
+    const int size = 1 << P.pg.page_shift, n_rows = nt * P.hkv;
+    T* const dense_k = static_cast<T*>(P.k) + (int64_t)t0 * P.stride + c;
+    T* const dense_v = static_cast<T*>(P.v) + (int64_t)t0 * P.stride + c;
+    Halves<T> rk[kU], rv[kU];
+    int tl[kU], h[kU];                                // token of the CTA and head of each row
+    bool live[kU];
+    int64_t dense[kU];
+    // (threads past the rows take the last one along, and store nothing)
+    auto rows_of = [&](int i0) {
 #pragma unroll
-                for (int e = 0; e < 2 * N; ++e) xk[e] = xv[e] = 0.f;
+        for (int u = 0; u < kU; ++u) {
+            const int want = i0 + u * kRows + threadIdx.x / kLanes, i = min(want, n_rows - 1);
+            live[u] = want < n_rows;
+            tl[u] = i / P.hkv;
+            h[u] = i - tl[u] * P.hkv;
+            dense[u] = (int64_t)tl[u] * P.stride + h[u] * D;
+            if (kAppend) {
+                rk[u].load(dense_k + dense[u], D / 2);
+                rv[u].load(dense_v + dense[u], D / 2);
             }
-        } else {
+        }
+    };
+    rows_of(0);
+    if (threadIdx.x < nt) {                           // one token a thread: its request, row and page
+        const int t = t0 + threadIdx.x, r = find_request(P, t), row = P.start[r] + (t - P.ptr[r]);
+        const int page = __ldg(P.pg.table + (int64_t)(P.b0 + r) * P.pg.table_stride + (row >> P.pg.page_shift));
+        const bool ok = page >= 0 && page < P.pg.n_pages;
+        if (!ok) atomicOr(P.err, 1);
+        s_at[threadIdx.x] = ok ? page * P.pg.page_stride + (int64_t)(row & (size - 1)) * D : -1;
+        s_sat[threadIdx.x] = page * P.pg.scale_stride + (row & (size - 1));
+    }
+    if (P.turn)
+        for (int a = threadIdx.x; a < nt * (D / 2); a += kMoveThreads) {
+            // (codes keep 4 bits: the special-function unit's angles are exact to them)
+            const uint64_t turn = lane_turn(P.rope.turn, a % (D / 2));
+            const int pos = __ldg(P.turn + t0 + a / (D / 2));
+            s_cs[a] = kAppend && kCodes ? turn_cs_fast(turn, pos) : turn_cs(turn, pos);
+        }
+    __syncthreads();
+    // every thread of the CTA makes the same passes (the rows' maxima are exchanged)
+    for (int i0 = 0; i0 < n_rows; i0 += kU * kRows) {
+        int64_t at[kU], sat[kU];
+        bool ok[kU];
+        float sk[kU], sv[kU];
+        uint2 ck[kU][2], cv[kU][2];                   // codes of both halves (gather)
 #pragma unroll
-            for (int e = 0; e < 2 * N; ++e) xk[e] = xv[e] = 0.f;
-            if (ok) {
+        for (int u = 0; u < kU; ++u) {
+            const int64_t base = s_at[tl[u]];
+            ok[u] = base >= 0;
+            at[u] = base + (int64_t)(h[u] * size) * D + c;
+            sat[u] = s_sat[tl[u]] + h[u] * size;
+            if constexpr (!kAppend) {
+                if (!ok[u]) continue;
                 if constexpr (kCodes) {
-                    const uint8_t* pk = static_cast<const uint8_t*>(P.pg.k) + at;
-                    const uint8_t* pv = static_cast<const uint8_t*>(P.pg.v) + at;
-                    const float sk = __ldg(P.pg.k_scale + sat), sv = __ldg(P.pg.v_scale + sat);
-                    load_codes<N>(pk, xk, sk);
-                    load_codes<N>(pk + D / 2, xk + N, sk);
-                    load_codes<N>(pv, xv, sv);
-                    load_codes<N>(pv + D / 2, xv + N, sv);
+                    const uint8_t* pk = static_cast<const uint8_t*>(P.pg.k) + at[u];
+                    const uint8_t* pv = static_cast<const uint8_t*>(P.pg.v) + at[u];
+                    ck[u][0] = ld_codes<N>(pk);
+                    ck[u][1] = ld_codes<N>(pk + D / 2);
+                    cv[u][0] = ld_codes<N>(pv);
+                    cv[u][1] = ld_codes<N>(pv + D / 2);
+                    sk[u] = __ldg(P.pg.k_scale + sat[u]);
+                    sv[u] = __ldg(P.pg.v_scale + sat[u]);
                 } else {
-                    const T* pk = static_cast<const T*>(P.pg.k) + at;
-                    const T* pv = static_cast<const T*>(P.pg.v) + at;
-                    rk[0] = ld16(pk);
-                    rk[1] = ld16(pk + D / 2);
-                    rv[0] = ld16(pv);
-                    rv[1] = ld16(pv + D / 2);
-                    Vec16<T>::unpack(rk[0], xk);
-                    Vec16<T>::unpack(rk[1], xk + N);
-                    Vec16<T>::unpack(rv[0], xv);
-                    Vec16<T>::unpack(rv[1], xv + N);
+                    rk[u].load(static_cast<const T*>(P.pg.k) + at[u], D / 2);
+                    rv[u].load(static_cast<const T*>(P.pg.v) + at[u], D / 2);
                 }
             }
         }
-        if (!angles) {
-            for (int a = threadIdx.x; a < nt * (D / 2); a += kMoveThreads)
-                s_cs[a] = turn_cs(lane_turn(P.rope.turn, a % (D / 2)), __ldg(P.turn + t0 + a / (D / 2)));
-            __syncthreads();
-            angles = true;
-        }
-        if (P.turn) {
-            float lo[N], hi[N];
-            rotate<N>(xk, xk + N, s_cs + tl * (D / 2) + c, lo, hi);
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                xk[e] = lo[e];
-                xk[N + e] = hi[e];
-            }
-        }
-        if constexpr (kAppend && kCodes) {
-            uint32_t mk = 0, mv = 0;
-#pragma unroll
-            for (int e = 0; e < 2 * N; ++e) {
-                mk = max(mk, __float_as_uint(xk[e]) & 0x7fffffffu);
-                mv = max(mv, __float_as_uint(xv[e]) & 0x7fffffffu);
-            }
-            const float2 sk = row_scale(row_top<kLanes>(mk)), sv = row_scale(row_top<kLanes>(mv));
-            if (ok) {
-                if (sk.y == 0.f)           // kept as zero, or NaN: codes 0
-#pragma unroll
-                    for (int e = 0; e < 2 * N; ++e) xk[e] = 0.f;
-                if (sv.y == 0.f)
-#pragma unroll
-                    for (int e = 0; e < 2 * N; ++e) xv[e] = 0.f;
-                uint8_t* pk = static_cast<uint8_t*>(P.pg.k) + at;
-                uint8_t* pv = static_cast<uint8_t*>(P.pg.v) + at;
-                store_codes<N>(pk, xk, sk.y);
-                store_codes<N>(pk + D / 2, xk + N, sk.y);
-                store_codes<N>(pv, xv, sv.y);
-                store_codes<N>(pv + D / 2, xv + N, sv.y);
-                if (lane == 0) {
-                    P.pg.k_scale[sat] = sk.x;
-                    P.pg.v_scale[sat] = sv.x;
+        for (int u = 0; u < kU; ++u) {
+            float x[2 * N];
+            auto row = [&](const Halves<T>& r, const uint2 (&codes)[2], float scale) {
+                if constexpr (!kAppend && kCodes) {
+                    from_codes<N>(codes[0], x, scale);
+                    from_codes<N>(codes[1], x + N, scale);
+                } else {
+                    r.unpack(x);
                 }
+                if (!kAppend && !ok[u])               // a page that is none reads as zero
+#pragma unroll
+                    for (int e = 0; e < 2 * N; ++e) x[e] = 0.f;
+            };
+            auto put = [&](void* pages, float* scales, T* out, uint32_t top) {
+                if constexpr (kAppend && kCodes) {
+                    const float2 s = row_scale(row_top<kLanes>(top));
+                    if (!live[u] || !ok[u]) return;
+                    uint8_t* const p = static_cast<uint8_t*>(pages) + at[u];
+                    store_codes<N>(p, x, s.y);
+                    store_codes<N>(p + D / 2, x + N, s.y);
+                    if (lane == 0) scales[sat[u]] = s.x;
+                } else {
+                    if (!live[u] || (kAppend && !ok[u])) return;
+                    T* const p = kAppend ? static_cast<T*>(pages) + at[u] : out + dense[u];
+                    st16(p, Vec16<T>::pack(x));
+                    st16(p + D / 2, Vec16<T>::pack(x + N));
+                }
+            };
+            uint32_t top = kAppend && kCodes ? top_of(rk[u]) : 0u;
+            row(rk[u], ck[u], sk[u]);
+            if (P.turn) {
+                float lo[N], hi[N];
+                rotate<N>(x, x + N, s_cs + tl[u] * (D / 2) + c, lo, hi);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    x[e] = lo[e];
+                    x[N + e] = hi[e];
+                }
+                if (kAppend && kCodes) top = top_of_turned<2 * N>(x, top);
             }
-        } else if (kAppend ? ok : live) {
-            T* const ok_ = kAppend ? static_cast<T*>(P.pg.k) + at : dk;
-            T* const ov_ = kAppend ? static_cast<T*>(P.pg.v) + at : dv;
-            st16(ok_, Vec16<T>::pack(xk));
-            st16(ok_ + D / 2, Vec16<T>::pack(xk + N));
-            st16(ov_, Vec16<T>::pack(xv));
-            st16(ov_ + D / 2, Vec16<T>::pack(xv + N));
+            put(P.pg.k, P.pg.k_scale, dense_k, top);
+            top = kAppend && kCodes ? top_of(rv[u]) : 0u;
+            row(rv[u], cv[u], sv[u]);
+            put(P.pg.v, P.pg.v_scale, dense_v, top);
         }
+        if (i0 + kU * kRows < n_rows) rows_of(i0 + kU * kRows);
     }
 }
 
@@ -230,14 +280,17 @@ cudaError_t launch_move(const PagedMoveCall& c, cudaStream_t s) {
         P.batch = nb;
         P.b0 = b0;
         P.hkv = c.hkv;
-        P.tokens_per_cta = std::max(1, std::min(kRows / c.hkv, kMaxTokens));
         P.t0 = c.ptr[b0];
         P.t1 = c.ptr[b0 + nb];
-        if (P.t1 == P.t0) continue;
+        const int tokens = P.t1 - P.t0;
+        if (tokens == 0) continue;
+        // a few passes a CTA where there are rows enough for every SM, one token where there are not
+        const int most = std::max(1, std::min(kMovePasses * rows_at_once(kAppend) * kRows / c.hkv, kMaxTokens));
+        P.tokens_per_cta = std::max(1, std::min(most, tokens / (4 * device_sms())));
         P.rope = *c.rope;
         for (int i = 0; i <= nb; ++i) P.ptr[i] = c.ptr[b0 + i];
         for (int i = 0; i < nb; ++i) P.start[i] = c.start[b0 + i];
-        const int ctas = (P.t1 - P.t0 + P.tokens_per_cta - 1) / P.tokens_per_cta;
+        const int ctas = (tokens + P.tokens_per_cta - 1) / P.tokens_per_cta;
         paged_move_kernel<T, D, kCodes, kAppend, kReq><<<ctas, kMoveThreads, 0, s>>>(P);
         const cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
