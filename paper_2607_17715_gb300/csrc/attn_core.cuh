@@ -186,6 +186,14 @@ __device__ __forceinline__ void core_score(const uint8_t* qb, const uint8_t* kb,
     }
 }
 
+// Whether a job copies its own key rows (pages, codes) and turns its queries in shared memory:
+// load_rows(keys, dst, pitch, rows, first) in place of core_copy over k, v, stride; turn_queries(q, pitch,
+// rows) once the query rows have landed.
+template <class Job>
+struct CoreOwnRows {
+    static constexpr bool value = false;
+};
+
 // Job: nrows (packed rows of the unit), nkeys (keys of this CTA's rows), k, v, stride (key rows),
 // scale_log2; q_row(r), out_row(r), lse_at(r) (null without lse); needed(k0, k1): some row of the
 // CTA may see a key of [k0, k1); whole(k0, k1): every row sees all of them; row(r): what
@@ -209,11 +217,15 @@ __device__ __forceinline__ void attention_core(const Job& job, int row0, int ns,
     // keys of tile t, and the rows of it that are copied (8 at a time; zeros past the last key)
     auto keys_in = [&](int t) { return min(kCoreKeys, job.nkeys - t * kCoreKeys); };
     auto load_k = [&](int t) {
-        core_copy<T, D>(sm + L::kK, L::kPitch, (keys_in(t) + 7) & ~7, CoreRows<T>{job.k, job.stride, t * kCoreKeys, job.nkeys});
+        const int rows = (keys_in(t) + 7) & ~7;
+        if constexpr (CoreOwnRows<Job>::value) job.load_rows(true, sm + L::kK, L::kPitch, rows, t * kCoreKeys);
+        else core_copy<T, D>(sm + L::kK, L::kPitch, rows, CoreRows<T>{job.k, job.stride, t * kCoreKeys, job.nkeys});
         core_commit();
     };
     auto load_v = [&](int t) {
-        core_copy<T, D>(sm + L::kV, D * 4, (keys_in(t) + 7) & ~7, CoreRows<T>{job.v, job.stride, t * kCoreKeys, job.nkeys});
+        const int rows = (keys_in(t) + 7) & ~7;
+        if constexpr (CoreOwnRows<Job>::value) job.load_rows(false, sm + L::kV, D * 4, rows, t * kCoreKeys);
+        else core_copy<T, D>(sm + L::kV, D * 4, rows, CoreRows<T>{job.v, job.stride, t * kCoreKeys, job.nkeys});
         core_commit();
     };
     const bool rows_here = KS || row0 + (tid >> 5) * 4 * RT < job.nrows;   // (a warp without rows only copies)
@@ -233,6 +245,12 @@ __device__ __forceinline__ void attention_core(const Job& job, int row0, int ns,
     else core_commit();
     if (t < t_end) load_v(t);
     else core_commit();
+
+    if constexpr (CoreOwnRows<Job>::value) {
+        core_wait<1>();
+        __syncthreads();                                   // the queries have landed
+        job.turn_queries(sm + L::kQ, L::kPitch, L::kRows);
+    }
 
     const uint8_t* qb = sm + L::kQ + r0 * L::kPitch;
     const uint8_t* kb = sm + L::kK + (key0 + tx) * L::kPitch;
@@ -398,7 +416,7 @@ __device__ __forceinline__ void attention_core(const Job& job, int row0, int ns,
         for (int i = 0; i < RT; ++i) {
             const int r = row0 + r0 + 4 * i;
             if (r >= job.nrows) continue;
-            const float inv = 1.f / l[i];
+            const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];      // (a row that sees nothing: zeros)
             T* out = job.out_row(r);
 #pragma unroll
             for (int h = 0; h < H; ++h)
@@ -434,11 +452,12 @@ __device__ __forceinline__ void attention_core(const Job& job, int row0, int ns,
         for (int q = 0; q < ns; ++q)
             for (int w = 0; w < W; ++w) mx = fmaxf(mx, part(sml, q)[4 * w + r].x);
         float ls = 0.f;
+        const float ms = mx == -CUDART_INF_F ? 0.f : mx;       // (a row that sees nothing)
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int q = 0; q < ns; ++q)
             for (int w = 0; w < W; ++w) {
                 const float2 ml = part(sml, q)[4 * w + r];
-                const float f = exp2f(ml.x - mx);          // 0 for a slot that saw nothing (some slot saw a key)
+                const float f = exp2f(ml.x - ms);          // 0 for a slot that saw nothing
                 const float4 v = reinterpret_cast<const float4*>(part(so, q) + (4 * w + r) * D)[c4];
                 acc.x = fmaf(f, v.x, acc.x);
                 acc.y = fmaf(f, v.y, acc.y);
@@ -446,7 +465,7 @@ __device__ __forceinline__ void attention_core(const Job& job, int row0, int ns,
                 acc.w = fmaf(f, v.w, acc.w);
                 ls = fmaf(f, ml.y, ls);
             }
-        const float inv = 1.f / ls;
+        const float inv = ls == 0.f ? 0.f : 1.f / ls;
         put(job.out_row(row0 + r) + 4 * c4, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
         float* lse = job.lse_at(row0 + r);
         if (lse != nullptr && c4 == 0) *lse = (mx + log2f(ls)) * 0.69314718055994531f;
