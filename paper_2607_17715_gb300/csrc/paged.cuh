@@ -73,7 +73,7 @@ struct PagedReq {
     int32_t item0;           // first work item of the request
     int32_t splits;          // stretches that its keys are cut into
     int32_t unit0;           // first unit (row tile of a KV head)
-    int32_t tile0;           // (paged_tc.cu) its row tiles of this entry: [tile0, tile0 + tiles)
+    int32_t tile0;           // its row tiles of this entry: [tile0, tile0 + tiles)
     int32_t tiles;
 };
 
@@ -90,6 +90,7 @@ struct PagedAttn {
     int32_t batch;
     int32_t hq;
     int32_t hkv;
+    int32_t group;           // hq / hkv
     int32_t window;          // a query sees at most the last `window` rows up to its own (0: all)
     float scale_log2;        // log2(e) / sqrt(d)
     RopeTurns rope;
@@ -151,6 +152,7 @@ void fill_paged(PagedAttn<kReq>& P, const PagedAttnCall& c, int d, const PagedRe
     P.batch = n;
     P.hq = c.hq;
     P.hkv = c.hkv;
+    P.group = c.hq / c.hkv;
     P.window = c.window;
     P.scale_log2 = (float)(1.4426950408889634 / __builtin_sqrt((double)d));
     P.rope = *c.rope;

@@ -1,20 +1,27 @@
 // Paged attention of few query rows: one to a few tokens of each request (c2kv_paged_attend).
 //
 // The rows of a (request, KV head) -- its tokens times the group's heads -- meet every key once, so
-// the call is bound by reading the pages.  One CTA takes 16 * MT rows and a stretch of keys, dealt to
-// its four warps in blocks of 32.  Each warp runs alone: a ring of TMA stages of its own, S = Q.K^T and
-// P.V on mma.sync (16 rows fill its M; a tcgen05 tile of 128 rows would be mostly empty, and would need
-// the 8-bit codes converted through shared memory instead of in registers), its own running maximum and
-// sum.  The warps' results join in shared memory, the stretches' in the CTA that ends last.
+// the call is bound by reading the pages.  One CTA takes 8 NT rows and a stretch of keys, dealt to its
+// four warps in blocks of 32.  Each warp runs alone: a ring of TMA stages of its own, its own running
+// maximum and sum.  The warps' results join in shared memory, the stretches' in the CTA that ends last.
 //
-// E4M3 codes become f16 in registers (exact); their scales stay in fp32: a key's K scale multiplies its
-// column of S, its V scale its column of P.  P must fit f16, so V scales are taken relative to a power
-// of two, the largest of them so far, that O is counted in; it moves like the running maximum does.
-// Queries are f16 too, each row scaled by a power of two so that its largest value is near 2^14: their
-// rounding is 2^-12 of a value.  Over 16-bit pages queries and weights are bf16.
+// The products are mma.sync (a tcgen05 tile of 128 rows would be mostly empty, and would need the 8-bit
+// codes converted through shared memory instead of in registers), turned over: S^T = K.Q^T and
+// O^T = V^T.P^T, keys and channels in the 16 rows of an operand, query rows in its columns of 8, so that
+// a token of four heads wastes half a tile and not three quarters.  P^T comes out of S^T's registers by
+// 8 x 8 transposes (movmatrix).
 //
-// Operand layouts.  The contraction over channels does not care for their order, so a lane of B takes
-// the channels that lie next to one another in its row: 16-byte shared loads, conflict-free under the
+// E4M3 codes become f16 in registers, exactly: half of them by the conversion instruction, which takes a
+// quarter of its lanes a clock and bound the kernel alone (a block 2350 clocks a warp), half by shifts
+// and masks, which leave 2^-8 of the value; the queries' channels, or O's, give that back.  Scales stay
+// in fp32: a key's K scale multiplies its row of S^T, its V scale its row of P^T.  P must fit f16, so V
+// scales are taken relative to a power of two, the largest of them so far, that O is counted in; it moves
+// like the running maximum does.  Queries are f16 too, each row scaled by a power of two so that its
+// largest value is near 2^6 (2^14 where codes are short of 2^8): their rounding is 2^-12 of a value.  Over
+// 16-bit pages queries and weights are bf16.
+//
+// Operand layouts.  The contraction over channels does not care for their order, so a lane takes the
+// channels that lie next to one another in its row: 16-byte shared loads, conflict-free under the
 // 128-byte swizzle, with no transpose of V (a lane loads the same channels of four keys and pairs them).
 #include "paged.cuh"
 #include "paged_row.cuh"
@@ -29,9 +36,13 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kBlk = 32;                 // keys of a warp's block
-constexpr int kStages = 3;               // blocks in flight a warp
 
-template <int D, bool kCodes>
+constexpr int kMostEights = 5;           // eights of query rows a CTA: what its registers hold
+
+// Blocks in flight a warp (kStages) and CTAs an SM (kCtas): three CTAs of two blocks where registers and
+// shared memory hold them (8-bit codes and eight rows), the warps' chains of dependent instructions being
+// what takes the time then; else two of three blocks, or one of heads of 128 channels in 16 bits.
+template <int D, bool kCodes, int NT>
 struct Lay {
     static constexpr int EB = kCodes ? 1 : 2;
     static constexpr int BC = kCodes ? D : 64;         // channels of a TMA box
@@ -42,14 +53,16 @@ struct Lay {
     static constexpr int CV = BC / 8;                  // channels of V a lane takes of a box row
     static constexpr int kBox = kBlk * RB;             // bytes of a box of a block
     static constexpr int kSide = NB * kBox;            // K (or V) of a block
+    static constexpr int kStages = kCodes && NT == 1 ? 2 : 3;
     static constexpr int kStage = 2 * kSide;
-    static constexpr int kScales = kCodes ? 2 * kBlk * 4 : 0;      // bytes of a block's scales
+    static constexpr int kScale = kCodes ? 2 * kBlk * 4 : 0;       // bytes of a block's scales
     static constexpr int kRing = kWarps * kStages * kStage;
-    static constexpr int kSmem = 1024 /*align*/ + kRing + kWarps * kStages * kScales;
-    static constexpr int kCtas = kSmem <= 108 * 1024 ? 2 : 1;      // an SM
+    static constexpr int kSmem = 1024 /*align*/ + kRing + kWarps * kStages * kScale;
+    static constexpr int kCtas = kCodes && NT == 1 ? 3 : kSmem <= 108 * 1024 ? 2 : 1;
     static constexpr int kPitch = D + 4;               // floats between rows of the joined results
 };
-static_assert(Lay<128, false>::kSmem + 12 * 1024 <= 227 * 1024, "shared memory of a CTA");
+static_assert(Lay<128, false, kMostEights>::kSmem + 14 * 1024 <= 227 * 1024 && 3 * (Lay<128, true, 1>::kSmem + 5 * 1024) <= 227 * 1024,
+              "shared memory of an SM");
 
 constexpr int kMaxStretches = 128;       // of one unit's keys: their weights join in shared memory
 
@@ -57,8 +70,8 @@ template <int kReq>
 struct MmaLaunch {
     CUtensorMap tm_k, tm_v;              // [n_pages][Hkv][page_size][d], boxes of min(page_size, 32) rows
     int32_t box_rows;
-    float* part_o;                       // [item][16 * MT][D] normalised
-    float* part_lse;                     // [item][16 * MT] log2 domain
+    float* part_o;                       // [item][8 * NT][D] normalised
+    float* part_lse;                     // [item][8 * NT] log2 domain
     uint32_t* tickets;                   // [unit], zero between launches
     PagedAttn<kReq> a;
 };
@@ -101,49 +114,62 @@ __device__ __forceinline__ uint32_t hi_half2(uint32_t w) { return half2_of((uint
 __device__ __forceinline__ void lds4(uint32_t a, uint32_t& x, uint32_t& y, uint32_t& z, uint32_t& w) {
     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x), "=r"(y), "=r"(z), "=r"(w) : "r"(a) : "memory");
 }
-__device__ __forceinline__ void lds2(uint32_t a, uint32_t& x, uint32_t& y) {
-    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(x), "=r"(y) : "r"(a) : "memory");
-}
-__device__ __forceinline__ float2 lds_f2(uint32_t a) {
-    float2 v;
-    asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
-    return v;
-}
 __device__ __forceinline__ float lds_f(uint32_t a) {
     float v;
     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
     return v;
 }
+__device__ __forceinline__ void lds2(uint32_t a, uint32_t& x, uint32_t& y) {
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(x), "=r"(y) : "r"(a) : "memory");
+}
+// The four codes of a word as two pairs of f16, 2^-8 of their values: bytes 0 and 2, bytes 1 and 3.
+__device__ __forceinline__ uint32_t masked_pair(uint32_t w) {
+    return (w & 0x80008000u) | ((w >> 1) & 0x3f803f80u);
+}
+__device__ __forceinline__ uint32_t odd_pair(uint32_t w) { return masked_pair(w); }
+__device__ __forceinline__ uint32_t even_pair(uint32_t w) { return masked_pair(w << 8); }
 
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-                 "l"(src), "r"(bytes), "r"(bar)
-                 : "memory");
+// An 8 x 8 matrix of 16-bit values, a row in four lanes, transposed.
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 
-// Where channel pair (ch, ch + 1) of tile row `row` lies in the fragments of Q: word of lane, register.
-template <int D, bool kCodes>
-__device__ __forceinline__ int q_word(int row, int ch) {
-    using L = Lay<D, kCodes>;
-    const int box = ch / L::BC, in = ch % L::BC, c = in / L::CQ, s = box * (L::CQ / 4) + in % L::CQ / 4;
-    const int reg = (in % 4 / 2) * 2 + (row % 16) / 8;
-    return ((row / 16 * L::KS + s) * 32 + (row % 8) * 4 + c) * 4 + reg;
+// K-step s of S (four channels a lane): by shifts and masks, or by the conversion instruction.
+__host__ __device__ constexpr bool by_masks(bool codes, int s) { return codes && (s & 1); }
+
+// Where channel ch of query row `row` lies in the fragments of Q^T: index of its 16 bits.
+template <int D, bool kCodes, int NT>
+__device__ __forceinline__ int q_place(int row, int ch) {
+    using L = Lay<D, kCodes, NT>;
+    const int box = ch / L::BC, in = ch % L::BC, c = in / L::CQ, s = box * (L::CQ / 4) + in % L::CQ / 4, e = in % 4;
+    const int reg = by_masks(kCodes, s) ? e & 1 : e >> 1, half = by_masks(kCodes, s) ? e >> 1 : e & 1;
+    return (((s * NT + row / 8) * 32 + (row % 8) * 4 + c) * 2 + reg) * 2 + half;
 }
 
-template <int D, bool kCodes, int MT, int kReq>
-__global__ void __launch_bounds__(kWarps * 32, 2) paged_mma_kernel(const __grid_constant__ MmaLaunch<kReq> X) {
-    using L = Lay<D, kCodes>;
+template <int D, bool kCodes, int NT, int kReq>
+__global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? Lay<D, kCodes, NT>::kCtas : 2) paged_mma_kernel(const __grid_constant__ MmaLaunch<kReq> X) {
+    using L = Lay<D, kCodes, NT>;
     using T = __nv_bfloat16;
-    constexpr int kRows = 16 * MT;
+    constexpr int kStages = L::kStages;
+    constexpr int kRows = 8 * NT, MT = D / 16;         // query rows; 16-channel tiles of O^T
+    constexpr bool kHeldQ = NT == 1;                   // Q^T in registers
     const PagedAttn<kReq>& P = X.a;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t s_full[kWarps][kStages];
-    __shared__ __align__(16) uint32_t s_q[MT * L::KS * 32 * 4];
+    __shared__ __align__(16) uint16_t s_q[L::KS * NT * 32 * 4];
     __shared__ float s_rs[kRows], s_m[kWarps][kRows], s_l[kWarps][kRows];
-    __shared__ uint32_t s_abort, s_bad, s_last;
+    __shared__ int s_end[kRows];
+    __shared__ uint32_t s_abort, s_last;
+    __shared__ uint64_t s_bad;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, c = lane % 4;
     uint8_t* const smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
 
+    if (threadIdx.x == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&X.tm_k)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&X.tm_v)) : "memory");
+    }
     // the work item: (request, stretch, KV head, row tile)
     int r = 0;
     for (int hi = P.batch; hi - r > 1;) {
@@ -152,29 +178,35 @@ __global__ void __launch_bounds__(kWarps * 32, 2) paged_mma_kernel(const __grid_
         else hi = mid;
     }
     const PagedReq R = P.req[r];
-    const int G = P.hq / P.hkv, n_rows = R.nq * G, n_tiles = (n_rows + kRows - 1) / kRows;
-    int it = blockIdx.x - R.item0;
-    const int rt = it % n_tiles;
-    it /= n_tiles;
-    const int hk = it % P.hkv, sp = it / P.hkv, n_split = R.splits;
-    const int row0 = rt * kRows, live = min(kRows, n_rows - row0);
+    const uint32_t G = P.group, n_tiles = R.tiles, n_split = R.splits;
+    uint32_t it = blockIdx.x - R.item0, rt = 0;
+    if (n_tiles > 1) {
+        rt = it % n_tiles;
+        it /= n_tiles;
+    }
+    const uint32_t sp = it / (uint32_t)P.hkv;
+    const int hk = (int)(it - sp * P.hkv);
+    const uint32_t row0 = rt * kRows;
+    const int live = min(kRows, (int)(R.nq * G - row0));
     // keys that any row of the tile sees: [k_lo, k_hi); the first row sees up to `first`
-    const int first = R.n_keys - R.nq + row0 / G, k_hi = R.n_keys - R.nq + (row0 + live - 1) / G + 1;
+    const int before = R.n_keys - R.nq, first = before + (int)(row0 / G), k_hi = before + (int)((row0 + live - 1) / G) + 1;
     const int k_lo = P.window ? max(0, first - P.window + 1) : 0;
     const int b_lo = k_lo / kBlk, b_n = max(0, (k_hi + kBlk - 1) / kBlk - b_lo);
-    const int b0 = b_lo + (int)((int64_t)b_n * sp / n_split), b1 = b_lo + (int)((int64_t)b_n * (sp + 1) / n_split);
+    const uint32_t each = (uint32_t)b_n / n_split, rest = (uint32_t)b_n - each * n_split;   // the first `rest` stretches: one more
+    const int b0 = b_lo + (int)(each * sp + min(sp, rest)), b1 = b0 + (int)(each + (sp < rest));
     const int n_it = b1 - b0 > warp ? (b1 - b0 - warp + kWarps - 1) / kWarps : 0;
 
+    // a warp's barriers are its own: a block is there when its tiles are, and each lane's scales
+    if (lane < kStages) mbar_init(smem_u32(&s_full[warp][lane]), kCodes ? 33 : 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    __syncwarp();
     if (threadIdx.x == 0) {
-        s_abort = s_bad = 0;
-        for (int w = 0; w < kWarps; ++w)
-            for (int s = 0; s < kStages; ++s) mbar_init(smem_u32(&s_full[w][s]), 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        s_abort = 0;
+        s_bad = 0;
     }
-    __syncthreads();
 
     const uint32_t ring = smem_u32(smem) + warp * kStages * L::kStage;
-    const uint32_t scales = smem_u32(smem) + L::kRing + warp * kStages * L::kScales;
+    const uint32_t scales = smem_u32(smem) + L::kRing + warp * kStages * L::kScale;
     const int32_t* const table = P.pg.table + (int64_t)R.row * P.pg.table_stride;
     const int box_rows = X.box_rows, boxes = kBlk / box_rows;      // pages a block spans: 1, or 2 of 16 rows
     // Pages of 32 of the warp's blocks, one a lane, looked up together; -1 for one that is none, or
@@ -200,11 +232,10 @@ __global__ void __launch_bounds__(kWarps * 32, 2) paged_mma_kernel(const __grid_
     // Block i of the warp into a stage; returns which halves of its keys are loaded (bits 0 and 1).
     auto issue = [&](int i, int stage) -> uint32_t {
         const int p0 = __shfl_sync(0xffffffffu, pages0, i & 31), p1 = __shfl_sync(0xffffffffu, pages1, i & 31);
+        const int off = ((b0 + warp + i * kWarps) * kBlk) & ((1 << P.pg.page_shift) - 1);
         if (lane == 0) {
-            const uint32_t bar = smem_u32(&s_full[warp][stage]), dst = ring + stage * L::kStage, ssc = scales + stage * L::kScales;
-            const int off = ((b0 + warp + i * kWarps) * kBlk) & ((1 << P.pg.page_shift) - 1);
-            const int n = (p0 >= 0) + (p1 >= 0);
-            mbar_expect_tx(bar, n * box_rows * (2 * D * L::EB + (kCodes ? 8 : 0)));
+            const uint32_t bar = smem_u32(&s_full[warp][stage]), dst = ring + stage * L::kStage;
+            mbar_expect_tx(bar, ((p0 >= 0) + (p1 >= 0)) * box_rows * 2 * D * L::EB);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const int page = k ? p1 : p0, at_row = k ? 0 : off;
@@ -215,170 +246,179 @@ __global__ void __launch_bounds__(kWarps * 32, 2) paged_mma_kernel(const __grid_
                     tma_load_4d(to, &X.tm_k, b * L::BC, at_row, hk, page, bar);
                     tma_load_4d(to + L::kSide, &X.tm_v, b * L::BC, at_row, hk, page, bar);
                 }
-                if constexpr (kCodes) {
-                    const int64_t at = (int64_t)page * P.pg.scale_stride + ((int64_t)hk << P.pg.page_shift) + at_row;
-                    bulk_load(ssc + k * 16 * 4, P.pg.k_scale + at, box_rows * 4, bar);
-                    bulk_load(ssc + (kBlk + k * 16) * 4, P.pg.v_scale + at, box_rows * 4, bar);
-                }
             }
+        }
+        if constexpr (kCodes) {          // a key's scales a lane (held in registers they were waited for at once)
+            const bool second = boxes == 2 && lane >= 16;
+            const int page = second ? p1 : p0;
+            const uint32_t to = scales + stage * L::kScale + lane * 4;
+            if (page >= 0) {
+                const int64_t at = (int64_t)page * P.pg.scale_stride + ((int64_t)hk << P.pg.page_shift) + (second ? lane - 16 : off + lane);
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(P.pg.k_scale + at) : "memory");
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + kBlk * 4), "l"(P.pg.v_scale + at) : "memory");
+            }
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(&s_full[warp][stage])) : "memory");
         }
         return boxes == 1 ? (p0 >= 0 ? 3u : 0u) : (p0 >= 0 ? 1u : 0u) | (p1 >= 0 ? 2u : 0u);
     };
     look_up(0);
     uint32_t loaded[kStages];            // of the blocks in flight, the next one to be used first
 #pragma unroll
-    for (int i = 0; i < kStages; ++i) loaded[i] = i < n_it ? issue(i, i) : 0;
+    for (int i = 0; i < kStages; ++i) loaded[i] = i < n_it ? issue(i, i) : 0u;
 
-    // the tile's queries: turned, as fragments of A
+    // the tile's queries: turned, as fragments of Q^T
     uint64_t turn[D / 64] = {};
     if (P.turn) {
 #pragma unroll
         for (int e = 0; e < D / 64; ++e) turn[e] = lane_turn(P.rope.turn, lane * (D / 64) + e);
     }
     for (int row = warp; row < kRows; row += kWarps) {
-        float x[D / 32];                 // channels 2 lane (+ 1) of the lower half, and of the upper
-        const bool there = row < live;
-        const int tok = R.q0 + (row0 + row) / G, h = hk * G + (row0 + row) % G;
-#pragma unroll
-        for (int e = 0; e < D / 32; ++e) x[e] = 0.f;
         constexpr int C = D / 64;        // channels of each half a lane
-        if (there) {
-            const T* q = static_cast<const T*>(P.q) + (int64_t)tok * P.q_stride + (int64_t)h * D + lane * C;
+        float x[2 * C];
+        const bool there = row < live;
+        const uint32_t rr = row0 + min(row, live - 1), tok = rr / G;
+        const T* q = static_cast<const T*>(P.q) + (int64_t)(R.q0 + tok) * P.q_stride + (int64_t)(hk * G + rr - tok * G) * D + lane * C;
+#pragma unroll
+        for (int e = 0; e < C; ++e) {
+            x[e] = there ? static_cast<float>(q[e]) : 0.f;
+            x[C + e] = there ? static_cast<float>(q[D / 2 + e]) : 0.f;
+        }
+        if (P.turn) {
+            const int64_t pos = __ldg(P.turn + R.q0 + tok);
 #pragma unroll
             for (int e = 0; e < C; ++e) {
-                x[e] = static_cast<float>(q[e]);
-                x[C + e] = static_cast<float>(q[D / 2 + e]);
-            }
-            if (P.turn) {
-                const int64_t pos = __ldg(P.turn + tok);
-#pragma unroll
-                for (int e = 0; e < C; ++e) {
-                    float a, b;
-                    rotate1(x[e], x[C + e], turn_cs_fast(turn[e], pos), a, b);
-                    x[e] = a;
-                    x[C + e] = b;
-                }
+                float a, b;
+                rotate1(x[e], x[C + e], turn_cs_fast(turn[e], pos), a, b);
+                x[e] = a;
+                x[C + e] = b;
             }
         }
-        float back = 1.f;
+        float back = 1.f, f = 1.f;
         if constexpr (kCodes) {
             uint32_t top = 0;
 #pragma unroll
-            for (int e = 0; e < D / 32; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+            for (int e = 0; e < 2 * C; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
             top = __reduce_max_sync(0xffffffffu, top);
-            // largest value to [2^14, 2^15); zero and non-finite rows as they are
+            // largest value to [2^6, 2^7); zero and non-finite rows as they are
             const int ex = (int)(top >> 23) - 127;
-            if (top != 0 && top < 0x7f800000u && ex > -100) {
-                const float f = exp2f((float)(14 - ex));
-                back = exp2f((float)(ex - 14));
-#pragma unroll
-                for (int e = 0; e < D / 32; ++e) x[e] *= f;
+            if (top < 0x7f800000u && ex > -100) {
+                f = exp2f((float)(6 - ex));
+                back = exp2f((float)(ex - 6));
             }
         }
-        if (lane == 0) s_rs[row] = back * P.scale_log2;
-        if constexpr (C == 2) {
-            s_q[q_word<D, kCodes>(row, 2 * lane)] = pack2<kCodes>(x[0], x[1]);
-            s_q[q_word<D, kCodes>(row, D / 2 + 2 * lane)] = pack2<kCodes>(x[2], x[3]);
-        } else {                         // one channel of each half a lane: pairs from even lanes
-            const float y0 = __shfl_down_sync(0xffffffffu, x[0], 1), y1 = __shfl_down_sync(0xffffffffu, x[1], 1);
-            if (!(lane & 1)) {
-                s_q[q_word<D, kCodes>(row, lane)] = pack2<kCodes>(x[0], y0);
-                s_q[q_word<D, kCodes>(row, D / 2 + lane)] = pack2<kCodes>(x[1], y1);
-            }
+        if (lane == 0) {
+            s_rs[row] = back * P.scale_log2;
+            s_end[row] = before + (int)tok;
+        }
+#pragma unroll
+        for (int e = 0; e < 2 * C; ++e) {
+            const int ch = (e / C) * (D / 2) + lane * C + e % C;
+            const bool masks = by_masks(kCodes, (ch % L::BC) % L::CQ / 4);
+            const uint32_t v = pack2<kCodes>(masks ? x[e] * f * 256.f : x[e] * f, 0.f);
+            s_q[q_place<D, kCodes, NT>(row, ch)] = (uint16_t)v;
         }
     }
     __syncthreads();
 
-    float o[MT][D / 8][4], m[MT][2], l[MT][2], rs[MT][2];
-    int last_key[MT][2];                 // the last key that rows g and g + 8 of each 16 see
+    // O^T: channel tile m of 16 (lane: channels g and g + 8 of it), rows 2c and 2c + 1 of each eight
+    float o[NT][MT][4], m[NT][2], l[NT][2];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
+    for (int t = 0; t < NT; ++t) {
 #pragma unroll
-        for (int n = 0; n < D / 8; ++n)
+        for (int n = 0; n < MT; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[t][n][e] = 0.f;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             m[t][e] = -INFINITY;
             l[t][e] = 0.f;
-            rs[t][e] = s_rs[t * 16 + e * 8 + g];
-            last_key[t][e] = R.n_keys - R.nq + (row0 + t * 16 + e * 8 + g) / G;
         }
     }
     int unit = -127;                     // O counts in 2^unit (E4M3)
-    uint32_t qf[MT == 1 ? L::KS : 1][4];
-    if constexpr (MT == 1) {
+    uint32_t qf[kHeldQ ? L::KS : 1][2];
+    const uint32_t q_at = smem_u32(s_q) + lane * 8;
+    if constexpr (kHeldQ) {
 #pragma unroll
-        for (int s = 0; s < L::KS; ++s) lds4(smem_u32(s_q) + (s * 32 + lane) * 16, qf[s][0], qf[s][1], qf[s][2], qf[s][3]);
+        for (int s = 0; s < L::KS; ++s) lds2(q_at + s * 256, qf[s][0], qf[s][1]);
     }
 
     int stage = 0, parity = 0;
     for (int i = 0; i < n_it; ++i) {
         const int key0 = (b0 + warp + i * kWarps) * kBlk;
-        const uint32_t sk = ring + stage * L::kStage, sv = sk + L::kSide, ssc = scales + stage * L::kScales;
-        const uint32_t has = loaded[0];
+        const uint32_t sk = ring + stage * L::kStage, sv = sk + L::kSide;
+        const uint32_t has = loaded[0], ssc = scales + stage * L::kScale;
         // some key is hidden from some row, or was not loaded: then every key is asked
         const bool edge = has != 3 || key0 + kBlk - 1 > first || (P.window && key0 <= k_hi - 1 - P.window);
         // key j of the block is there, and some row of the tile sees it
-        auto there = [&](int j) { return key0 + j < k_hi && key0 + j >= k_lo && (has >> (j >> 4) & 1); };
+        auto there = [&](int j) { return key0 + j < k_hi && key0 + j >= k_lo && (has >> (j >> 4) & 1u); };
         mbar_wait(smem_u32(&s_full[warp][stage]), parity, P.err, &s_abort);
 
-        float s[MT][4][4];
+        // S^T of keys 16 h + g (e = 0, 1) and + 8 (2, 3), rows 8 t + 2c and + 1
+        float s[NT][2][4];
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int n = 0; n < 4; ++n)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[t][n][e] = 0.f;
+                for (int e = 0; e < 4; ++e) s[t][h][e] = 0.f;
 #pragma unroll
         for (int b = 0; b < L::NB; ++b) {
             constexpr int KW = L::CQ * L::EB / 4;              // words of the lane's channels of a key
-            uint32_t w[4][KW];
+            uint32_t w[2][2][KW];
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
                 const uint32_t at = sk + b * L::kBox + (n * 8 + g) * L::RB;
+                uint32_t* const to = w[n >> 1][n & 1];
 #pragma unroll
                 for (int u = 0; u < KW / 4; ++u)
-                    lds4(at + (L::RB == 128 ? ((2 * c + u) ^ g) * 16 : c * 16), w[n][4 * u], w[n][4 * u + 1], w[n][4 * u + 2], w[n][4 * u + 3]);
+                    lds4(at + (L::RB == 128 ? ((2 * c + u) ^ g) * 16 : c * 16), to[4 * u], to[4 * u + 1], to[4 * u + 2], to[4 * u + 3]);
             }
 #pragma unroll
             for (int ks = 0; ks < L::CQ / 4; ++ks) {
-                uint32_t f[4][2];
+                uint32_t a[2][4];
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    f[n][0] = kCodes ? lo_half2(w[n][ks]) : w[n][(2 * ks) % KW];
-                    f[n][1] = kCodes ? hi_half2(w[n][ks]) : w[n][(2 * ks + 1) % KW];
-                }
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int t = 0; t < MT; ++t) {
-                    uint32_t a[4];
-                    if constexpr (MT == 1) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) a[e] = qf[b * (L::CQ / 4) + ks][e];
-                    } else {
-                        lds4(smem_u32(s_q) + ((t * L::KS + b * (L::CQ / 4) + ks) * 32 + lane) * 16, a[0], a[1], a[2], a[3]);
+                    for (int k = 0; k < 2; ++k) {              // rows g and g + 8 of the 16 keys
+                        const uint32_t x = w[h][k][kCodes ? ks : (2 * ks) % KW];
+                        if constexpr (kCodes) {
+                            a[h][k] = by_masks(true, ks) ? even_pair(x) : lo_half2(x);
+                            a[h][2 + k] = by_masks(true, ks) ? odd_pair(x) : hi_half2(x);
+                        } else {
+                            a[h][k] = x;
+                            a[h][2 + k] = w[h][k][(2 * ks + 1) % KW];
+                        }
                     }
 #pragma unroll
-                    for (int n = 0; n < 4; ++n) mma16816<kCodes>(s[t][n], a, f[n][0], f[n][1]);
+                for (int t = 0; t < NT; ++t) {
+                    const int s_i = b * (L::CQ / 4) + ks;
+                    uint32_t q0, q1;
+                    if constexpr (kHeldQ) {
+                        q0 = qf[s_i][0];
+                        q1 = qf[s_i][1];
+                    } else {
+                        lds2(q_at + (s_i * NT + t) * 256, q0, q1);
+                    }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) mma16816<kCodes>(s[t][h], a[h], q0, q1);
                 }
             }
         }
         // scales: K's on the scores; V's relative to the unit that O counts in
-        float vs[4][2], shift = 1.f;
+        float vs[2][2], shift = 1.f;
         if constexpr (kCodes) {
 #pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const float2 a = lds_f2(ssc + (n * 8 + 2 * c) * 4), b = lds_f2(ssc + (kBlk + n * 8 + 2 * c) * 4);
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int t = 0; t < MT; ++t) {
-                    s[t][n][0] *= a.x;
-                    s[t][n][1] *= a.y;
-                    s[t][n][2] *= a.x;
-                    s[t][n][3] *= a.y;
+                for (int k = 0; k < 2; ++k) {
+                    const float f = lds_f(ssc + (16 * h + 8 * k + g) * 4);
+                    vs[h][k] = lds_f(ssc + (kBlk + 16 * h + 8 * k + g) * 4);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        s[t][h][2 * k] *= f;
+                        s[t][h][2 * k + 1] *= f;
+                    }
                 }
-                vs[n][0] = b.x;
-                vs[n][1] = b.y;
-            }
             uint32_t top = __float_as_uint(lds_f(ssc + (kBlk + lane) * 4)) & 0x7fffffffu;
             if (top >= 0x7f800000u || (edge && !there(lane))) top = 0;
             top = __reduce_max_sync(0xffffffffu, top);
@@ -387,68 +427,67 @@ __global__ void __launch_bounds__(kWarps * 32, 2) paged_mma_kernel(const __grid_
             unit = u;
             const float inv = exp2f((float)-u);
 #pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                vs[n][0] *= inv;
-                vs[n][1] *= inv;
-            }
-        }
-        uint32_t pf[MT][2][4];           // P as fragments of A, 16 keys each
-        float grow[MT][2];
-        bool moved = shift != 1.f;
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
+                for (int k = 0; k < 2; ++k) vs[h][k] *= inv;
+        }
+        uint32_t pf[NT][2][2];           // P^T as fragments, 16 keys each
+        bool moved = shift != 1.f;
+        float grow[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            float2 rs;
+            asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(rs.x), "=f"(rs.y) : "r"(smem_u32(s_rs) + (t * 8 + 2 * c) * 4));
             if (edge) {
 #pragma unroll
-                for (int n = 0; n < 4; ++n)
+                for (int k = 0; k < 2; ++k) {
+                    const int end = s_end[t * 8 + 2 * c + k];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int j = n * 8 + 2 * c + (e & 1), key = key0 + j, end = last_key[t][e >> 1];
+                    for (int n = 0; n < 4; ++n) {
+                        const int j = n * 8 + g, key = key0 + j;
                         const bool seen = key <= end && (!P.window || key > end - P.window) && (has >> (j >> 4) & 1);
-                        if (!seen) s[t][n][e] = -INFINITY;
+                        if (!seen) s[t][n >> 1][(n & 1) * 2 + k] = -INFINITY;
                     }
+                }
             }
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float top = -INFINITY;
-#pragma unroll
-                for (int n = 0; n < 4; ++n) top = fmaxf(top, fmaxf(s[t][n][2 * e], s[t][n][2 * e + 1]));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                const float now = fmaxf(m[t][e], top * rs[t][e]);
-                const float base = now == -INFINITY ? 0.f : now;       // nothing seen yet: weights 2^-inf
-                const float f = ex2f(m[t][e] - base);
-                moved |= now != m[t][e];
-                m[t][e] = now;
-                grow[t][e] = f * shift;
+            for (int k = 0; k < 2; ++k) {
+                const float f = k ? rs.y : rs.x;
+                float top = fmaxf(fmaxf(s[t][0][k], s[t][0][2 + k]), fmaxf(s[t][1][k], s[t][1][2 + k]));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+                const float high = fmaxf(m[t][k], top * f);
+                const float base = high == -INFINITY ? 0.f : high;     // nothing seen yet: weights 2^-inf
+                const float a = ex2f(m[t][k] - base);
+                moved |= high != m[t][k];
+                m[t][k] = high;
+                grow[t][k] = a * shift;
                 float sum = 0.f;
 #pragma unroll
                 for (int n = 0; n < 4; ++n) {
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        float p = ex2f(fmaf(s[t][n][2 * e + k], rs[t][e], -base));
-                        sum += p;
-                        // a hidden key's scale may be anything
-                        if constexpr (kCodes) p = edge && s[t][n][2 * e + k] == -INFINITY ? 0.f : p * vs[n][k];
-                        s[t][n][2 * e + k] = p;
-                    }
+                    float& x = s[t][n >> 1][(n & 1) * 2 + k];
+                    float p = ex2f(fmaf(x, f, -base));
+                    sum += p;
+                    // a hidden key's scale may be anything
+                    if constexpr (kCodes) p = edge && x == -INFINITY ? 0.f : p * vs[n >> 1][n & 1];
+                    x = p;
                 }
-                l[t][e] = fmaf(l[t][e], f, sum);
+                l[t][k] = fmaf(l[t][k], a, sum);
             }
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    pf[t][h][e] = pack2<kCodes>(s[t][2 * h][2 * e], s[t][2 * h][2 * e + 1]);
-                    pf[t][h][2 + e] = pack2<kCodes>(s[t][2 * h + 1][2 * e], s[t][2 * h + 1][2 * e + 1]);
-                }
+            for (int h = 0; h < 2; ++h) {
+                pf[t][h][0] = transposed(pack2<kCodes>(s[t][h][0], s[t][h][1]));
+                pf[t][h][1] = transposed(pack2<kCodes>(s[t][h][2], s[t][h][3]));
+            }
         }
         if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
-            for (int t = 0; t < MT; ++t)
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int n = 0; n < D / 8; ++n)
+                for (int n = 0; n < MT; ++n)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[t][n][e] *= grow[t][e >> 1];
+                    for (int e = 0; e < 4; ++e) o[t][n][e] *= grow[t][e & 1];
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -466,25 +505,36 @@ __global__ void __launch_bounds__(kWarps * 32, 2) paged_mma_kernel(const __grid_
 #pragma unroll
                         for (int e = 0; e < VW; ++e) w[k][e] = 0;
                 }
+                // a[m]: channels 2m (rows g of the tile) and 2m + 1 (rows g + 8) of the lane's, four keys
 #pragma unroll
                 for (int e = 0; e < VW; ++e) {
-                    if constexpr (kCodes) {
-                        const uint32_t x0 = __byte_perm(w[0][e], w[1][e], 0x5140), x1 = __byte_perm(w[0][e], w[1][e], 0x7362);
-                        const uint32_t y0 = __byte_perm(w[2][e], w[3][e], 0x5140), y1 = __byte_perm(w[2][e], w[3][e], 0x7362);
-                        const uint32_t f[4] = {lo_half2(x0), hi_half2(x0), lo_half2(x1), hi_half2(x1)};
-                        const uint32_t h2[4] = {lo_half2(y0), hi_half2(y0), lo_half2(y1), hi_half2(y1)};
+                    constexpr int kTiles = kCodes ? 2 : 1;     // a word's channels in pairs
+                    uint32_t a[kTiles][4];
 #pragma unroll
-                        for (int t = 0; t < MT; ++t)
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) mma16816<kCodes>(o[t][4 * e + k], pf[t][h], f[k], h2[k]);
-                    } else {
-                        const uint32_t f[2] = {__byte_perm(w[0][e], w[1][e], 0x5410), __byte_perm(w[0][e], w[1][e], 0x7632)};
-                        const uint32_t h2[2] = {__byte_perm(w[2][e], w[3][e], 0x5410), __byte_perm(w[2][e], w[3][e], 0x7632)};
-#pragma unroll
-                        for (int t = 0; t < MT; ++t)
-#pragma unroll
-                            for (int k = 0; k < 2; ++k) mma16816<kCodes>(o[t][b * L::CV + 2 * e + k], pf[t][h], f[k], h2[k]);
+                    for (int k = 0; k < 2; ++k) {              // keys 2c, 2c + 1, then + 8
+                        const uint32_t x = w[2 * k][e], y = w[2 * k + 1][e];
+                        if constexpr (!kCodes) {
+                            a[0][2 * k] = __byte_perm(x, y, 0x5410);
+                            a[0][2 * k + 1] = __byte_perm(x, y, 0x7632);
+                        } else if (by_masks(true, e)) {
+                            const uint32_t ex = even_pair(x), ey = even_pair(y), ox = odd_pair(x), oy = odd_pair(y);
+                            a[0][2 * k] = __byte_perm(ex, ey, 0x5410);
+                            a[0][2 * k + 1] = __byte_perm(ox, oy, 0x5410);
+                            a[kTiles - 1][2 * k] = __byte_perm(ex, ey, 0x7632);
+                            a[kTiles - 1][2 * k + 1] = __byte_perm(ox, oy, 0x7632);
+                        } else {
+                            const uint32_t lo = __byte_perm(x, y, 0x5140), hi = __byte_perm(x, y, 0x7362);
+                            a[0][2 * k] = lo_half2(lo);
+                            a[0][2 * k + 1] = hi_half2(lo);
+                            a[kTiles - 1][2 * k] = lo_half2(hi);
+                            a[kTiles - 1][2 * k + 1] = hi_half2(hi);
+                        }
                     }
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int n = 0; n < kTiles; ++n)
+                            mma16816<kCodes>(o[t][b * (L::CV / 2) + kTiles * e + n], a[n], pf[t][h][0], pf[t][h][1]);
                 }
             }
         }
@@ -493,7 +543,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) paged_mma_kernel(const __grid_
         if (next < n_it && (next & 31) == 0) look_up(next);
 #pragma unroll
         for (int k = 0; k + 1 < kStages; ++k) loaded[k] = loaded[k + 1];
-        loaded[kStages - 1] = next < n_it ? issue(next, stage) : 0;
+        loaded[kStages - 1] = next < n_it ? issue(next, stage) : 0u;
         if (++stage == kStages) {
             stage = 0;
             parity ^= 1;
@@ -501,36 +551,34 @@ __global__ void __launch_bounds__(kWarps * 32, 2) paged_mma_kernel(const __grid_
     }
 
     // the warps' results join: O in units of one, rows [row][channel], lines of 16 bytes swapped within
-    // groups of eight so that the four lanes of a row meet different banks
+    // groups of eight so that lanes meet fewer banks
     __syncthreads();                     // every stage has been read
     float* const joined = reinterpret_cast<float*>(smem);
     auto line = [](int f) { return f ^ (2 * (f >> 3 & 3)); };
     const float one = kCodes ? exp2f((float)unit) : 1.f;
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            float sum = l[t][e];
-            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-            const int row = t * 16 + e * 8 + g;
-            if (c == 0) {
-                s_m[warp][row] = m[t][e];
+        for (int k = 0; k < 2; ++k) {
+            float sum = l[t][k];
+            sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+            const int row = t * 8 + 2 * c + k;
+            if (g == 0) {
+                s_m[warp][row] = m[t][k];
                 s_l[warp][row] = sum;
             }
             float* const to = joined + (warp * kRows + row) * L::kPitch;
 #pragma unroll
             for (int b = 0; b < L::NB; ++b)
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int q4 = 0; q4 < L::CV / 4; ++q4) {
-                        const int n = b * L::CV + 4 * q4;
-                        const int f = (b * L::BC + (2 * c + k) * L::CV) / 4 + q4;
-                        *reinterpret_cast<float4*>(to + line(f) * 4) =
-                            make_float4(o[t][n][2 * e + k] * one, o[t][n + 1][2 * e + k] * one, o[t][n + 2][2 * e + k] * one,
-                                        o[t][n + 3][2 * e + k] * one);
-                    }
+                for (int q4 = 0; q4 < L::CV / 4; ++q4) {       // the lane's channels 4 q4 .. + 3 of the box
+                    const int n = b * (L::CV / 2) + 2 * q4;
+                    const float f = by_masks(kCodes, q4) ? one * 256.f : one;
+                    *reinterpret_cast<float4*>(to + line((b * L::BC + g * L::CV) / 4 + q4) * 4) =
+                        make_float4(o[t][n][k] * f, o[t][n][2 + k] * f, o[t][n + 1][k] * f, o[t][n + 1][2 + k] * f);
+                }
         }
     __syncthreads();
     const bool whole = n_split == 1;
@@ -569,14 +617,14 @@ __global__ void __launch_bounds__(kWarps * 32, 2) paged_mma_kernel(const __grid_
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         if constexpr (!kCodes)           // infinity or NaN in V may belong to keys that this row does not see
             if (!(fabsf(x.x) <= 3.0e38f && fabsf(x.y) <= 3.0e38f && fabsf(x.z) <= 3.0e38f && fabsf(x.w) <= 3.0e38f))
-                atomicOr(&s_bad, 1u << row);
+                atomicOr(reinterpret_cast<unsigned long long*>(&s_bad), 1ull << row);
         put(row, f, sum == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv),
             sum == 0.f ? -INFINITY : top + log2f(sum));
     }
     if constexpr (!kCodes) {
         __syncthreads();
-        for (uint32_t bad = s_bad; bad; bad &= bad - 1) {      // those rows again, key by key
-            const int row = __ffs(bad) - 1;
+        for (uint64_t bad = s_bad; bad; bad &= bad - 1) {      // those rows again, key by key
+            const int row = __ffsll((long long)bad) - 1;
             if (row % kWarps != warp) continue;
             const int end = R.n_keys - R.nq + (row0 + row) / G;
             const int lo = max(b0 * kBlk, P.window ? end - P.window + 1 : 0), hi = min(b1 * kBlk, end + 1);
@@ -597,12 +645,12 @@ __global__ void __launch_bounds__(kWarps * 32, 2) paged_mma_kernel(const __grid_
     }
     if (whole) return;
     // the stretch that ends last joins them all: every partial is visible before its ticket is taken
-    const int unit_id = R.unit0 + hk * n_tiles + rt;
+    const int unit_id = R.unit0 + hk * (int)n_tiles + (int)rt;
     __threadfence();
     __syncthreads();
     if (threadIdx.x == 0) {
         const uint32_t t = atomicAdd(X.tickets + unit_id, 1u);
-        s_last = t == (uint32_t)n_split - 1;
+        s_last = t == n_split - 1;
         if (s_last) X.tickets[unit_id] = 0;
     }
     __syncthreads();
@@ -610,7 +658,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) paged_mma_kernel(const __grid_
     __threadfence();
     const int64_t step = (int64_t)P.hkv * n_tiles, item0 = R.item0 + (int64_t)hk * n_tiles + rt;   // items of this unit
     float* const weight = joined;        // [stretch][row]
-    for (int i = threadIdx.x; i < n_split * live; i += kWarps * 32) {
+    for (int i = threadIdx.x; i < (int)n_split * live; i += kWarps * 32) {
         const int k = i / live, row = i % live;
         weight[k * kRows + row] = __ldcg(X.part_lse + (item0 + k * step) * kRows + row);
     }
@@ -618,11 +666,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2) paged_mma_kernel(const __grid_
     if (threadIdx.x < live) {
         const int row = threadIdx.x;
         float top = -INFINITY, sum = 0.f;
-        for (int k = 0; k < n_split; ++k) top = fmaxf(top, weight[k * kRows + row]);
+        for (int k = 0; k < (int)n_split; ++k) top = fmaxf(top, weight[k * kRows + row]);
         const float base = top == -INFINITY ? 0.f : top;
-        for (int k = 0; k < n_split; ++k) sum += ex2f(weight[k * kRows + row] - base);
+        for (int k = 0; k < (int)n_split; ++k) sum += ex2f(weight[k * kRows + row] - base);
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        for (int k = 0; k < n_split; ++k) weight[k * kRows + row] = ex2f(weight[k * kRows + row] - base) * inv;
+        for (int k = 0; k < (int)n_split; ++k) weight[k * kRows + row] = ex2f(weight[k * kRows + row] - base) * inv;
         if (P.lse) {
             const int64_t tok = R.q0 + (row0 + row) / G;
             P.lse[(int64_t)(hk * G + (row0 + row) % G) * P.n_tokens + tok] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
@@ -634,7 +682,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) paged_mma_kernel(const __grid_
         const float* from = X.part_o + (item0 * kRows + row) * D + 4 * f;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-        for (int k = 0; k < n_split; ++k) {
+        for (int k = 0; k < (int)n_split; ++k) {
             const float a = weight[k * kRows + row];
             const float4 y = __ldcg(reinterpret_cast<const float4*>(from + k * step * kRows * D));
             x.x = fmaf(y.x, a, x.x);
@@ -650,12 +698,12 @@ __global__ void __launch_bounds__(kWarps * 32, 2) paged_mma_kernel(const __grid_
 
 // ------------------------------------------------------------------ host side
 
-template <int D, bool kCodes, int MT, int kReq>
+template <int D, bool kCodes, int NT, int kReq>
 cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStream_t s) {
-    using L = Lay<D, kCodes>;
-    constexpr int kRows = 16 * MT;
+    using L = Lay<D, kCodes, NT>;
+    constexpr int kRows = 8 * NT;
     static PerDevice<cudaError_t> smem_set;
-    const auto kernel = paged_mma_kernel<D, kCodes, MT, kReq>;
+    const auto kernel = paged_mma_kernel<D, kCodes, NT, kReq>;
     cudaError_t e = opt_in_smem(smem_set, (const void*)kernel, L::kSmem);
     if (e != cudaSuccess) return e;
     for (int b0 = 0; b0 < n; b0 += kReq) {
@@ -694,8 +742,9 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
             split = split || q.splits > 1;
             q.item0 = (int32_t)items;
             q.unit0 = (int32_t)units;
-            units += (int64_t)tiles_of(q) * c.hkv;
-            items += (int64_t)tiles_of(q) * c.hkv * q.splits;
+            q.tiles = tiles_of(q);
+            units += (int64_t)q.tiles * c.hkv;
+            items += (int64_t)q.tiles * c.hkv * q.splits;
         }
         X.box_rows = std::min(1 << c.pg.page_shift, kBlk);
         X.part_o = X.part_lse = nullptr;
@@ -719,13 +768,18 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
     return cudaSuccess;
 }
 
+// Row tiles of the largest request, and as few eights of rows a tile as hold them: conversions are done
+// once a tile, so one tile of 40 rows is better than two of 24.
 template <int D, bool kCodes>
 cudaError_t by_rows(const PagedAttnCall& c, const PagedReq* req, int n, cudaStream_t s) {
-    int rows = 0;
+    int rows = 1;
     for (int i = 0; i < n; ++i) rows = std::max(rows, req[i].nq * (c.hq / c.hkv));
-    if (rows <= 16)
-        return n <= kPagedFew ? launch<D, kCodes, 1, kPagedFew>(c, req, n, s) : launch<D, kCodes, 1, kPagedMany>(c, req, n, s);
-    return n <= kPagedFew ? launch<D, kCodes, 2, kPagedFew>(c, req, n, s) : launch<D, kCodes, 2, kPagedMany>(c, req, n, s);
+    const int eights = (rows + 7) / 8, tiles = (eights + kMostEights - 1) / kMostEights, nt = (eights + tiles - 1) / tiles;
+    if (nt == 1) return n <= kPagedFew ? launch<D, kCodes, 1, kPagedFew>(c, req, n, s) : launch<D, kCodes, 1, kPagedMany>(c, req, n, s);
+    if (nt == 2) return n <= kPagedFew ? launch<D, kCodes, 2, kPagedFew>(c, req, n, s) : launch<D, kCodes, 2, kPagedMany>(c, req, n, s);
+    if (nt == 3) return launch<D, kCodes, 3, kPagedFew>(c, req, n, s);
+    if (nt == 4) return launch<D, kCodes, 4, kPagedFew>(c, req, n, s);
+    return launch<D, kCodes, 5, kPagedFew>(c, req, n, s);
 }
 
 }  // namespace
