@@ -111,17 +111,21 @@ __device__ __forceinline__ uint32_t half2_of(uint16_t w) {
 __device__ __forceinline__ uint32_t lo_half2(uint32_t w) { return half2_of((uint16_t)w); }
 __device__ __forceinline__ uint32_t hi_half2(uint32_t w) { return half2_of((uint16_t)(w >> 16)); }
 
-__device__ __forceinline__ void lds4(uint32_t a, uint32_t& x, uint32_t& y, uint32_t& z, uint32_t& w) {
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x), "=r"(y), "=r"(z), "=r"(w) : "r"(a) : "memory");
+// Shared memory by ordinary loads, which the compiler may move between the barriers.
+__device__ __forceinline__ void lds4(const uint8_t* a, uint32_t& x, uint32_t& y, uint32_t& z, uint32_t& w) {
+    const uint4 v = *reinterpret_cast<const uint4*>(a);
+    x = v.x;
+    y = v.y;
+    z = v.z;
+    w = v.w;
 }
-__device__ __forceinline__ float lds_f(uint32_t a) {
-    float v;
-    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
-    return v;
+__device__ __forceinline__ void lds2(const uint8_t* a, uint32_t& x, uint32_t& y) {
+    const uint2 v = *reinterpret_cast<const uint2*>(a);
+    x = v.x;
+    y = v.y;
 }
-__device__ __forceinline__ void lds2(uint32_t a, uint32_t& x, uint32_t& y) {
-    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(x), "=r"(y) : "r"(a) : "memory");
-}
+__device__ __forceinline__ float lds_f(const uint8_t* a) { return *reinterpret_cast<const float*>(a); }
+
 // The four codes of a word as two pairs of f16, 2^-8 of their values: bytes 0 and 2, bytes 1 and 3.
 __device__ __forceinline__ uint32_t masked_pair(uint32_t w) {
     return (w & 0x80008000u) | ((w >> 1) & 0x3f803f80u);
@@ -132,7 +136,7 @@ __device__ __forceinline__ uint32_t even_pair(uint32_t w) { return masked_pair(w
 // An 8 x 8 matrix of 16-bit values, a row in four lanes, transposed.
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
     uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
 
@@ -159,7 +163,8 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t s_full[kWarps][kStages];
     __shared__ __align__(16) uint16_t s_q[L::KS * NT * 32 * 4];
-    __shared__ float s_rs[kRows], s_m[kWarps][kRows], s_l[kWarps][kRows];
+    __shared__ __align__(8) float s_rs[kRows];
+    __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
     __shared__ int s_end[kRows];
     __shared__ uint32_t s_abort, s_last;
     __shared__ uint64_t s_bad;
@@ -203,6 +208,27 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
     if (threadIdx.x == 0) {
         s_abort = 0;
         s_bad = 0;
+    }
+
+    // the warp's query rows, on their way before the keys are: behind a ring's worth of tiles they took 4 us
+    constexpr int C = D / 64, kMine = (kRows + kWarps - 1) / kWarps;   // channels of each half a lane; rows a warp
+    uint32_t q_raw[kMine][2];
+    int q_pos[kMine];
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        const uint32_t rr = row0 + min(warp + i * kWarps, live - 1), tok = rr / G;
+        const T* q = static_cast<const T*>(P.q) + (int64_t)(R.q0 + tok) * P.q_stride + (int64_t)(hk * G + rr - tok * G) * D + lane * C;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            if constexpr (C == 2) q_raw[i][half] = __ldg(reinterpret_cast<const uint32_t*>(q + half * (D / 2)));
+            else q_raw[i][half] = __ldg(reinterpret_cast<const uint16_t*>(q + half * (D / 2)));
+        }
+        q_pos[i] = P.turn ? __ldg(P.turn + R.q0 + tok) : 0;
+    }
+    uint64_t turn[C] = {};
+    if (P.turn) {
+#pragma unroll
+        for (int e = 0; e < C; ++e) turn[e] = lane_turn(P.rope.turn, lane * C + e);
     }
 
     const uint32_t ring = smem_u32(smem) + warp * kStages * L::kStage;
@@ -267,28 +293,23 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
     for (int i = 0; i < kStages; ++i) loaded[i] = i < n_it ? issue(i, i) : 0u;
 
     // the tile's queries: turned, as fragments of Q^T
-    uint64_t turn[D / 64] = {};
-    if (P.turn) {
 #pragma unroll
-        for (int e = 0; e < D / 64; ++e) turn[e] = lane_turn(P.rope.turn, lane * (D / 64) + e);
-    }
-    for (int row = warp; row < kRows; row += kWarps) {
-        constexpr int C = D / 64;        // channels of each half a lane
+    for (int i = 0; i < kMine; ++i) {
+        const int row = warp + i * kWarps;
+        if (row >= kRows) break;
         float x[2 * C];
         const bool there = row < live;
-        const uint32_t rr = row0 + min(row, live - 1), tok = rr / G;
-        const T* q = static_cast<const T*>(P.q) + (int64_t)(R.q0 + tok) * P.q_stride + (int64_t)(hk * G + rr - tok * G) * D + lane * C;
+        const uint32_t tok = (row0 + min(row, live - 1)) / G;
 #pragma unroll
         for (int e = 0; e < C; ++e) {
-            x[e] = there ? static_cast<float>(q[e]) : 0.f;
-            x[C + e] = there ? static_cast<float>(q[D / 2 + e]) : 0.f;
+            x[e] = there ? __uint_as_float(e == 0 ? q_raw[i][0] << 16 : q_raw[i][0] & 0xffff0000u) : 0.f;
+            x[C + e] = there ? __uint_as_float(e == 0 ? q_raw[i][1] << 16 : q_raw[i][1] & 0xffff0000u) : 0.f;
         }
         if (P.turn) {
-            const int64_t pos = __ldg(P.turn + R.q0 + tok);
 #pragma unroll
             for (int e = 0; e < C; ++e) {
                 float a, b;
-                rotate1(x[e], x[C + e], turn_cs_fast(turn[e], pos), a, b);
+                rotate1(x[e], x[C + e], turn_cs_fast(turn[e], q_pos[i]), a, b);
                 x[e] = a;
                 x[C + e] = b;
             }
@@ -336,7 +357,7 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
     }
     int unit = -127;                     // O counts in 2^unit (E4M3)
     uint32_t qf[kHeldQ ? L::KS : 1][2];
-    const uint32_t q_at = smem_u32(s_q) + lane * 8;
+    const uint8_t* const q_at = reinterpret_cast<const uint8_t*>(s_q) + lane * 8;
     if constexpr (kHeldQ) {
 #pragma unroll
         for (int s = 0; s < L::KS; ++s) lds2(q_at + s * 256, qf[s][0], qf[s][1]);
@@ -345,8 +366,10 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
     int stage = 0, parity = 0;
     for (int i = 0; i < n_it; ++i) {
         const int key0 = (b0 + warp + i * kWarps) * kBlk;
-        const uint32_t sk = ring + stage * L::kStage, sv = sk + L::kSide;
-        const uint32_t has = loaded[0], ssc = scales + stage * L::kScale;
+        const uint8_t* const sk = smem + (warp * kStages + stage) * L::kStage;
+        const uint8_t* const sv = sk + L::kSide;
+        const uint8_t* const ssc = smem + L::kRing + (warp * kStages + stage) * L::kScale;
+        const uint32_t has = loaded[0];
         // some key is hidden from some row, or was not loaded: then every key is asked
         const bool edge = has != 3 || key0 + kBlk - 1 > first || (P.window && key0 <= k_hi - 1 - P.window);
         // key j of the block is there, and some row of the tile sees it
@@ -367,7 +390,7 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
             uint32_t w[2][2][KW];
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
-                const uint32_t at = sk + b * L::kBox + (n * 8 + g) * L::RB;
+                const uint8_t* const at = sk + b * L::kBox + (n * 8 + g) * L::RB;
                 uint32_t* const to = w[n >> 1][n & 1];
 #pragma unroll
                 for (int u = 0; u < KW / 4; ++u)
@@ -436,8 +459,7 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
         float grow[NT][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            float2 rs;
-            asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(rs.x), "=f"(rs.y) : "r"(smem_u32(s_rs) + (t * 8 + 2 * c) * 4));
+            const float2 rs = *reinterpret_cast<const float2*>(s_rs + t * 8 + 2 * c);
             if (edge) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
@@ -498,7 +520,7 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {                  // keys 2c, 2c + 1, 2c + 8, 2c + 9
                     const int row = h * 16 + 2 * c + (k & 1) + (k >> 1) * 8;
-                    const uint32_t at = sv + b * L::kBox + row * L::RB;
+                    const uint8_t* const at = sv + b * L::kBox + row * L::RB;
                     if constexpr (VW == 4) lds4(at + (g ^ (row & 7)) * 16, w[k][0], w[k][1], w[k][2], w[k][3]);
                     else lds2(at + g * 8, w[k][0], w[k][1]);
                     if (edge && !there(row))       // whatever lies there: 0 times it must be 0
@@ -646,53 +668,60 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
     if (whole) return;
     // the stretch that ends last joins them all: every partial is visible before its ticket is taken
     const int unit_id = R.unit0 + hk * (int)n_tiles + (int)rt;
-    __threadfence();
     __syncthreads();
     if (threadIdx.x == 0) {
+        __threadfence();                 // (cumulative: of what the CTA's threads wrote before the barrier)
         const uint32_t t = atomicAdd(X.tickets + unit_id, 1u);
         s_last = t == n_split - 1;
         if (s_last) X.tickets[unit_id] = 0;
+        __threadfence();
     }
     __syncthreads();
     if (!s_last) return;
-    __threadfence();
-    const int64_t step = (int64_t)P.hkv * n_tiles, item0 = R.item0 + (int64_t)hk * n_tiles + rt;   // items of this unit
-    float* const weight = joined;        // [stretch][row]
-    for (int i = threadIdx.x; i < (int)n_split * live; i += kWarps * 32) {
-        const int k = i / live, row = i % live;
-        weight[k * kRows + row] = __ldcg(X.part_lse + (item0 + k * step) * kRows + row);
-    }
-    __syncthreads();
-    if (threadIdx.x < live) {
-        const int row = threadIdx.x;
-        float top = -INFINITY, sum = 0.f;
-        for (int k = 0; k < (int)n_split; ++k) top = fmaxf(top, weight[k * kRows + row]);
-        const float base = top == -INFINITY ? 0.f : top;
-        for (int k = 0; k < (int)n_split; ++k) sum += ex2f(weight[k * kRows + row] - base);
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        for (int k = 0; k < (int)n_split; ++k) weight[k * kRows + row] = ex2f(weight[k * kRows + row] - base) * inv;
-        if (P.lse) {
-            const int64_t tok = R.q0 + (row0 + row) / G;
-            P.lse[(int64_t)(hk * G + (row0 + row) % G) * P.n_tokens + tok] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
-        }
-    }
-    __syncthreads();
+    // items of this unit's stretches, `step` apart; a thread's sixteen at a time on their way at once
+    const int64_t step = (int64_t)P.hkv * n_tiles, item0 = R.item0 + (int64_t)hk * n_tiles + rt;
     for (int i = threadIdx.x; i < live * (D / 4); i += kWarps * 32) {
         const int row = i / (D / 4), f = i % (D / 4);
-        const float* from = X.part_o + (item0 * kRows + row) * D + 4 * f;
+        const float* const from = X.part_o + (item0 * kRows + row) * D + 4 * f;
+        const float* const from_lse = X.part_lse + item0 * kRows + row;
+        float top = -INFINITY, sum = 0.f;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int k = 0; k < (int)n_split; ++k) {
-            const float a = weight[k * kRows + row];
-            const float4 y = __ldcg(reinterpret_cast<const float4*>(from + k * step * kRows * D));
-            x.x = fmaf(y.x, a, x.x);
-            x.y = fmaf(y.y, a, x.y);
-            x.z = fmaf(y.z, a, x.z);
-            x.w = fmaf(y.w, a, x.w);
+        constexpr int kBatch = 16;
+        for (int k0 = 0; k0 < (int)n_split; k0 += kBatch) {
+            float e[kBatch];
+            float4 y[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                if (k0 + k >= (int)n_split) {
+                    e[k] = -INFINITY;
+                    y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    continue;
+                }
+                e[k] = __ldcg(from_lse + (k0 + k) * step * kRows);
+                y[k] = __ldcg(reinterpret_cast<const float4*>(from + (k0 + k) * step * kRows * D));
+            }
+            float now = top;
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) now = fmaxf(now, e[k]);
+            const float base = now == -INFINITY ? 0.f : now, a = ex2f(top - base);
+            top = now;
+            sum *= a;
+            x = make_float4(x.x * a, x.y * a, x.z * a, x.w * a);
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const float w = ex2f(e[k] - base);
+                sum += w;
+                x.x = fmaf(y[k].x, w, x.x);
+                x.y = fmaf(y[k].y, w, x.y);
+                x.z = fmaf(y[k].z, w, x.z);
+                x.w = fmaf(y[k].w, w, x.w);
+            }
         }
-        const int64_t tok = R.q0 + (row0 + row) / G;
-        *reinterpret_cast<uint2*>(out + (tok * P.hq + hk * G + (row0 + row) % G) * D + 4 * f) =
-            make_uint2(pack2<false>(x.x, x.y), pack2<false>(x.z, x.w));
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const uint32_t tok = (row0 + row) / G, h = hk * G + row0 + row - tok * G;
+        *reinterpret_cast<uint2*>(out + ((int64_t)(R.q0 + tok) * P.hq + h) * D + 4 * f) =
+            make_uint2(pack2<false>(x.x * inv, x.y * inv), pack2<false>(x.z * inv, x.w * inv));
+        if (f == 0 && P.lse) P.lse[(int64_t)h * P.n_tokens + R.q0 + tok] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
     }
 }
 
