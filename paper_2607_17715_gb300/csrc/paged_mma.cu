@@ -37,7 +37,8 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kBlk = 32;                 // keys of a warp's block
 
-constexpr int kMostEights = 5;           // eights of query rows a CTA: what its registers hold
+constexpr int kMostEights = 4;           // eights of query rows a CTA: what its registers hold (40 rows: two tiles of
+                                         // three eights 33 us, one of five, which spills, 44)
 
 // Blocks in flight a warp (kStages) and CTAs an SM (kCtas): three CTAs of two blocks where registers and
 // shared memory hold them (8-bit codes and eight rows), the warps' chains of dependent instructions being
@@ -797,8 +798,8 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
     return cudaSuccess;
 }
 
-// Row tiles of the largest request, and as few eights of rows a tile as hold them: conversions are done
-// once a tile, so one tile of 40 rows is better than two of 24.
+// As few row tiles as hold the largest request's rows, and as few eights of rows a tile as make them up:
+// a tile's keys are loaded and converted once for all its rows.
 template <int D, bool kCodes>
 cudaError_t by_rows(const PagedAttnCall& c, const PagedReq* req, int n, cudaStream_t s) {
     int rows = 1;
@@ -807,8 +808,7 @@ cudaError_t by_rows(const PagedAttnCall& c, const PagedReq* req, int n, cudaStre
     if (nt == 1) return n <= kPagedFew ? launch<D, kCodes, 1, kPagedFew>(c, req, n, s) : launch<D, kCodes, 1, kPagedMany>(c, req, n, s);
     if (nt == 2) return n <= kPagedFew ? launch<D, kCodes, 2, kPagedFew>(c, req, n, s) : launch<D, kCodes, 2, kPagedMany>(c, req, n, s);
     if (nt == 3) return launch<D, kCodes, 3, kPagedFew>(c, req, n, s);
-    if (nt == 4) return launch<D, kCodes, 4, kPagedFew>(c, req, n, s);
-    return launch<D, kCodes, 5, kPagedFew>(c, req, n, s);
+    return launch<D, kCodes, 4, kPagedFew>(c, req, n, s);
 }
 
 }  // namespace
