@@ -73,6 +73,7 @@ struct PagedReq {
     int32_t item0;           // first work item of the request
     int32_t splits;          // stretches that its keys are cut into
     int32_t unit0;           // first unit (row tile of a KV head)
+    int32_t scratch;         // (paged_tc.cu) its key tile 0 among the launch's key tiles
     int32_t tile0;           // its row tiles of this entry: [tile0, tile0 + tiles)
     int32_t tiles;
 };
@@ -123,21 +124,30 @@ cudaError_t launch_paged_mma(const PagedAttnCall& c, const PagedReq* req, int n,
 // Tensor map of pages [n_pages][Hkv][page_size][d], elements of 16 bits or codes of 8.
 bool encode_page_map(CUtensorMap* tm, const void* base, const PageView& pg, int hkv, int d, bool codes, int box_channels,
                      int box_rows, CUtensorMapSwizzle swizzle);
-// bf16 queries of n requests over 16-bit pages on tcgen05 (paged_tc.cu).
-cudaError_t launch_paged_tc(const PagedAttnCall& c, const PagedReq* req, int n, int d, cudaStream_t s);
-// E4M3 pages of n requests as 16-bit ones (paged_move.cu): request i's pages become pages first[i] .. of
-// `to`, of one size with them, and row i of to.table names them (-1 for a page that is none).
+// Key tiles: what requests see of their pages, 128 keys of a KV head at a time, as f16 relative to a power
+// of two of the tile's own (paged_expand.cu).  Key tile t of a request is tile `scratch` + t.
+constexpr int kTileKeys = 128;
+struct KeyTiles {
+    void* k;                 // [n][Hkv][128][d] f16; rows that no query sees, or of no page, are zero
+    void* v;
+    float2* unit;            // [n][Hkv]: the factor that K's values lack, and the exponent of V's
+    uint32_t* there;         // [n]: which groups of 16 keys lie in pages (bits 0 .. 7)
+    int32_t n;
+};
 struct PagedExpandCall {
-    PageView from, to;
+    PageView pg;
+    KeyTiles to;
     int32_t* err;
     int32_t hkv;
     int32_t n;
     const PagedReq* req;
-    const int32_t* page0;    // first page of each request that any query sees ...
-    const int32_t* pages;    // ... how many from there on
-    const int32_t* first;    // ... and the page of `to` that it becomes
+    const int32_t* tile0;    // first key tile of each request that any query sees ...
+    const int32_t* tiles;    // ... how many from there on; they follow one another in `to`
+    const int32_t* key0;     // ... and the first key
 };
-cudaError_t launch_paged_expand(const PagedExpandCall& c, int d, cudaStream_t s);
+cudaError_t launch_paged_expand(const PagedExpandCall& c, int d, bool codes, cudaStream_t s);
+// bf16 queries of n requests over their key tiles on tcgen05 (paged_tc.cu).
+cudaError_t launch_paged_tc(const PagedAttnCall& c, const KeyTiles& tiles, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
 
 template <int kReq>
 void fill_paged(PagedAttn<kReq>& P, const PagedAttnCall& c, int d, const PagedReq* req, int n) {

@@ -14,58 +14,53 @@ namespace {
 // 80 rows 60 / 36; 8-bit pages of 128 channels 48 rows 52 / 83, 80 rows 97 / 82.
 int mma_rows(int d, bool codes) { return codes ? 64 : d == 128 ? 40 : 56; }
 
-// Requests of many rows on tcgen05.  Their 8-bit pages are expanded to 16 bits first, in scratch that the
-// stream hands back; requests go in groups so that the scratch stays small beside the cache.
-constexpr int64_t kExpandBytes = (int64_t)512 << 20;
+// Requests of many rows on tcgen05: what they see of their pages becomes key tiles first, in scratch that
+// the stream hands back; requests go in groups so that the scratch stays small beside the cache.
+constexpr int64_t kTileBytes = (int64_t)512 << 20;
 
 cudaError_t launch_many(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s) {
-    if (!codes) return launch_paged_tc(c, req, n, d, s);
-    const int shift = c.pg.page_shift;
-    const int64_t page_bytes = ((int64_t)c.hkv << shift) * d * 2;
+    const int64_t tile_bytes = (int64_t)c.hkv * kTileKeys * d * 2;
     for (int b0 = 0; b0 < n;) {
         std::vector<PagedReq> part;
-        std::vector<int32_t> page0, pages, first;
-        int64_t total = 0, width = 1;
+        std::vector<int32_t> tile0, tiles, key0;
+        int64_t total = 0;
         for (; b0 < n; ++b0) {
-            const PagedReq& q = req[b0];
-            const int64_t seen = c.window ? std::max<int64_t>(0, (int64_t)q.n_keys - q.nq + 1 - c.window) : 0;   // the first row that a query sees
-            const int32_t lo = (int32_t)(seen >> shift), hi = (int32_t)(((int64_t)q.n_keys + (1 << shift) - 1) >> shift);
-            if (!part.empty() && (total + hi - lo) * page_bytes * 2 > kExpandBytes) break;
-            page0.push_back(lo);
-            pages.push_back(std::max(0, hi - lo));
-            first.push_back((int32_t)total);
-            total += pages.back();
-            width = std::max<int64_t>(width, hi);
+            PagedReq q = req[b0];
+            const int64_t first = c.window ? std::max<int64_t>(0, (int64_t)q.n_keys - q.nq + 1 - c.window) : 0;   // the first row that a query sees
+            const int32_t lo = (int32_t)(first / kTileKeys), hi = (int32_t)(((int64_t)q.n_keys + kTileKeys - 1) / kTileKeys);
+            if (!part.empty() && (total + hi - lo) * tile_bytes * 2 > kTileBytes) break;
+            tile0.push_back(lo);
+            tiles.push_back(std::max(0, hi - lo));
+            key0.push_back((int32_t)first);
+            q.scratch = (int32_t)(total - lo);
+            total += tiles.back();
             part.push_back(q);
         }
         const int m = (int)part.size();
-        const size_t half = (size_t)std::max<int64_t>(1, total) * page_bytes;
+        const size_t half = (size_t)std::max<int64_t>(1, total) * tile_bytes, units = (size_t)std::max<int64_t>(1, total) * c.hkv * 8;
         void* p = nullptr;
-        cudaError_t e = context_alloc(c.ctx, &p, 2 * half + (size_t)m * width * 4);
-        if (e == cudaErrorMemoryAllocation) {           // no room: code by code, slower
+        cudaError_t e = context_alloc(c.ctx, &p, 2 * half + units + (size_t)std::max<int64_t>(1, total) * 4);
+        if (e == cudaErrorMemoryAllocation) {           // no room: key by key, slower
             (void)cudaGetLastError();
-            e = launch_paged_mma(c, part.data(), m, d, true, s);
+            e = launch_paged_mma(c, part.data(), m, d, codes, s);
             if (e != cudaSuccess) return e;
             continue;
         }
         if (e != cudaSuccess) return e;
+        char* const base = static_cast<char*>(p);
         PagedExpandCall x{};
-        x.from = c.pg;
-        x.to = PageView{p, static_cast<char*>(p) + half, nullptr, nullptr,
-                        reinterpret_cast<const int32_t*>(static_cast<char*>(p) + 2 * half), page_bytes / 2, 0, width,
-                        (int32_t)std::max<int64_t>(1, total), shift};
+        x.pg = c.pg;
+        x.to = KeyTiles{base, base + half, reinterpret_cast<float2*>(base + 2 * half), reinterpret_cast<uint32_t*>(base + 2 * half + units),
+                        (int32_t)std::max<int64_t>(1, total)};
         x.err = c.err;
         x.hkv = c.hkv;
         x.n = m;
         x.req = part.data();
-        x.page0 = page0.data();
-        x.pages = pages.data();
-        x.first = first.data();
-        e = launch_paged_expand(x, d, s);
-        PagedAttnCall a = c;
-        a.pg = x.to;
-        for (int i = 0; i < m; ++i) part[i].row = i;
-        if (e == cudaSuccess) e = launch_paged_tc(a, part.data(), m, d, s);
+        x.tile0 = tile0.data();
+        x.tiles = tiles.data();
+        x.key0 = key0.data();
+        e = launch_paged_expand(x, d, codes, s);
+        if (e == cudaSuccess) e = launch_paged_tc(c, x.to, part.data(), m, d, codes, s);
         context_free(c.ctx, p);
         if (e != cudaSuccess) return e;
     }
@@ -78,7 +73,7 @@ cudaError_t launch_paged_attn(const PagedAttnCall& c, int dtype, int d, bool cod
     std::vector<PagedReq> req;
     req.reserve(c.batch);
     for (int r = 0; r < c.batch; ++r)
-        if (c.ptr[r + 1] > c.ptr[r]) req.push_back(PagedReq{c.ptr[r], c.ptr[r + 1] - c.ptr[r], c.n_keys[r], r, 0, 1, 0, 0, 0});
+        if (c.ptr[r + 1] > c.ptr[r]) req.push_back(PagedReq{c.ptr[r], c.ptr[r + 1] - c.ptr[r], c.n_keys[r], r, 0, 1, 0, 0, 0, 0});
     if (dtype == kDtypeF32) return launch_paged_simt(c, req.data(), (int)req.size(), d, codes, s);
     // requests of many rows on tcgen05, those of few on mma.sync
     std::vector<PagedReq> few, many;

@@ -313,102 +313,7 @@ cudaError_t move_rows(const PagedMoveCall& c, int dtype, int d, bool codes, cuda
     return d == 128 ? move_of<__nv_bfloat16, 128, kAppend>(c, codes, s) : move_of<__nv_bfloat16, 64, kAppend>(c, codes, s);
 }
 
-// ------------------------------------------------------------------ 8-bit pages as 16-bit ones
-
-constexpr int kExpandThreads = 256;
-
-template <int kReq>
-struct PagedExpand {
-    PageView from, to;
-    int32_t* err;
-    int32_t hkv;
-    int32_t n;
-    int32_t item0[kReq + 1];     // pages of the launch before request i's
-    int32_t row[kReq];           // its row of from.table
-    int32_t page0[kReq];         // its first page there
-    int32_t first[kReq];         // the page of `to` that this becomes
-};
-
-// One page of one KV head a CTA: K and V, 16 codes a thread and pass.  A code times its scale is rounded
-// to bf16 (2^-9 of it), as the rows of 16-bit pages are: the products that read it are of bf16.  Bytes
-// bound it: one read, two written for each code.
-template <int D, int kReq>
-__global__ void __launch_bounds__(kExpandThreads) paged_expand_kernel(const __grid_constant__ PagedExpand<kReq> P) {
-    using T = __nv_bfloat16;
-    int r = 0;
-    for (int hi = P.n; hi - r > 1;) {
-        const int mid = (r + hi) >> 1;
-        if (P.item0[mid] <= (int)blockIdx.x) r = mid;
-        else hi = mid;
-    }
-    const int i = blockIdx.x - P.item0[r], h = blockIdx.y, size = 1 << P.from.page_shift;
-    const int page = __ldg(P.from.table + (int64_t)P.row[r] * P.from.table_stride + P.page0[r] + i);
-    const bool ok = page >= 0 && page < P.from.n_pages;
-    if (threadIdx.x == 0 && h == 0) {
-        const_cast<int32_t*>(P.to.table)[(int64_t)r * P.to.table_stride + P.page0[r] + i] = ok ? P.first[r] + i : -1;
-        if (!ok) atomicOr(P.err, 1);
-    }
-    if (!ok) return;
-    constexpr int kChunks = D / 16;
-    const int64_t from = (int64_t)page * P.from.page_stride + (int64_t)h * size * D;
-    const int64_t sfrom = (int64_t)page * P.from.scale_stride + (int64_t)h * size;
-    const int64_t to = (int64_t)(P.first[r] + i) * P.to.page_stride + (int64_t)h * size * D;
-    for (int e = threadIdx.x; e < 2 * size * kChunks; e += kExpandThreads) {
-        const bool v = e >= size * kChunks;
-        const int c = v ? e - size * kChunks : e;
-        const uint8_t* src = static_cast<const uint8_t*>(v ? P.from.v : P.from.k) + from + (int64_t)c * 16;
-        const float s = __ldg((v ? P.from.v_scale : P.from.k_scale) + sfrom + c / kChunks);
-        const uint4 w = ld16(src);
-        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-        float f[16];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float2 a = from_codes2(x[k]), b = from_codes2(x[k] >> 16);
-            f[4 * k] = a.x * s;
-            f[4 * k + 1] = a.y * s;
-            f[4 * k + 2] = b.x * s;
-            f[4 * k + 3] = b.y * s;
-        }
-        T* dst = static_cast<T*>(v ? P.to.v : P.to.k) + to + (int64_t)c * 16;
-        st16(dst, Vec16<T>::pack(f));
-        st16(dst + 8, Vec16<T>::pack(f + 8));
-    }
-}
-
-template <int D, int kReq>
-cudaError_t launch_expand(const PagedExpandCall& c, cudaStream_t s) {
-    for (int b0 = 0; b0 < c.n; b0 += kReq) {
-        const int nb = std::min(c.n - b0, kReq);
-        PagedExpand<kReq> P;
-        P.from = c.from;
-        P.to = c.to;
-        P.to.table += (int64_t)b0 * c.to.table_stride;
-        P.err = c.err;
-        P.hkv = c.hkv;
-        P.n = nb;
-        int items = 0;
-        for (int i = 0; i < nb; ++i) {
-            P.item0[i] = items;
-            P.row[i] = c.req[b0 + i].row;
-            P.page0[i] = c.page0[b0 + i];
-            P.first[i] = c.first[b0 + i];
-            items += c.pages[b0 + i];
-        }
-        P.item0[nb] = items;
-        if (items == 0) continue;
-        paged_expand_kernel<D, kReq><<<dim3(items, c.hkv), kExpandThreads, 0, s>>>(P);
-        const cudaError_t e = cudaGetLastError();
-        if (e != cudaSuccess) return e;
-    }
-    return cudaSuccess;
-}
-
 }  // namespace
-
-cudaError_t launch_paged_expand(const PagedExpandCall& c, int d, cudaStream_t s) {
-    if (c.n <= kPagedFew) return d == 128 ? launch_expand<128, kPagedFew>(c, s) : launch_expand<64, kPagedFew>(c, s);
-    return d == 128 ? launch_expand<128, kPagedMany>(c, s) : launch_expand<64, kPagedMany>(c, s);
-}
 
 cudaError_t launch_paged_append(const PagedMoveCall& c, int dtype, int d, bool codes, cudaStream_t s) {
     return move_rows<true>(c, dtype, d, codes, s);

@@ -5,12 +5,10 @@
 // tensor memory, and each tile's softmax (a warpgroup, a row a thread) runs beside the other tile's
 // products.  The tensor cores bound it, four products of 2 M multiply-adds a key tile and CTA.
 //
-// A tile of 128 keys is gathered from up to eight pages by TMA, swizzled, straight into the operands'
-// tiles; rows of V that no query may feel (past the last key, or of a page that is none) are zeroed
-// there, whatever memory holds.  E4M3 pages are expanded to 16 bits first, once a call (see expand): to
-// turn codes in this kernel takes every CTA of a head the same work again, and its three idle warps
-// needed twice the time of the products (the conversion instruction is slow): 249 us against 124 for
-// 1216 tokens over 8384 rows.
+// The keys come by TMA from key tiles, f16 relative to a power of two of their own (paged_expand.cu).  The
+// tiles' powers of two come back in the softmax: K's as a factor of the scores, V's as an offset of the
+// exponent (the running reference is of score + offset, so that weights of every tile fit f16; the sum of
+// weights takes the offset back).  Queries are f16 too, each row scaled by a power of two.
 #include "paged.cuh"
 #include "paged_row.cuh"
 #include "per_device.cuh"
@@ -21,7 +19,6 @@
 #include <math_constants.h>
 
 #include <algorithm>
-#include <climits>
 #include <utility>
 #include <vector>
 
@@ -47,23 +44,45 @@ struct Tc {
     static constexpr int kK = 3, kV = 2;                   // stages of K and of V tiles
     static constexpr int kTile = BN * D * 2;               // bytes of a tile
     static constexpr int kHalf = BN * 128;                 // of its 64-channel block
-    // barriers: tile landed / free (K, V), scores, weights, O, queries, and a V tile before its zeros
-    static constexpr int KF = 0, KE = KF + kK, VF = KE + kK, VE = VF + kV, S = VE + kV, P = S + 2, O = P + 2, Q = O + 1, VZ = Q + 1,
-                         kBars = VZ + 1;
+    // barriers: tile landed / free (K, V), scores, weights, O, queries
+    static constexpr int KF = 0, KE = KF + kK, VF = KE + kK, VE = VF + kV, S = VE + kV, P = S + 2, O = P + 2, Q = O + 1, kBars = Q + 1;
     static constexpr int kTiles = (2 + kK + kV) * kTile;
     static constexpr int kNotes = kTiles + (8 * kBars + 15) / 16 * 16;
-    static constexpr int kSlot = kNotes + 4 * kUnits;
+    static constexpr int kBack = kNotes + 16 * kUnits;     // powers of two of the queries' rows: a byte each
+    static constexpr int kSlot = kBack + kPair;
     static constexpr int kSmem = 1024 /*align*/ + kSlot + 16;
 };
 static_assert(Tc<128>::kSmem <= 232448, "shared memory of a CTA");
 
+// What the softmax needs to know of a key tile: K's power of two, V's exponent, and which of its eight
+// groups of 16 keys lie in pages (bits).
+struct TileNote {
+    float k_unit;
+    float v_exp;
+    uint32_t there;
+    uint32_t pad;
+};
+
 template <int kReq>
 struct TcLaunch {
-    CUtensorMap tm_k, tm_v;              // [n_pages][Hkv][page_size][d], boxes of a page's rows and 64 channels
+    CUtensorMap tm_k, tm_v;              // key tiles [n * Hkv][128][d], boxes of 64 channels
+    const float2* unit;                  // [n][Hkv]
+    const uint32_t* there;               // [n]
     float* part_o;                       // [item][256][D] normalised
     float* part_lse;                     // [item][256] log2 domain
     PagedAttn<kReq> a;
 };
+
+// kind::f16 with f16 operands, D fp32, A K-major, B K- or MN-major.
+__host__ __device__ constexpr uint32_t idesc_f16(int m, int n, bool b_mn_major) {
+    return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
 
 __device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src, bool there) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
@@ -106,78 +125,32 @@ __device__ __forceinline__ Item find_item(const PagedAttn<kReq>& P) {
 
 // ------------------------------------------------------------------ loaders
 
-// Which pages a tile's keys lie in, a tile ahead of its use: lane g (0..7) knows that of keys 16 g ...
-struct Pages {
-    const int32_t* table;
-    int shift, n_pages, k_lo, k_hi;
-    int asked;                           // page number read for the next tile; INT_MIN where it has no key in [k_lo, k_hi)
-    int page;                            // of the current tile, -1 for none
-    __device__ __forceinline__ void ask(int tile, int lane) {
-        const int key = tile * BN + (lane & 7) * 16;
-        // (pages that a window has left behind may be gone from the table)
-        asked = key < k_hi && ((key >> shift) + 1) << shift > k_lo ? __ldg(table + (key >> shift)) : INT_MIN;
-    }
-    __device__ __forceinline__ void take(int32_t* err, bool report) {
-        const bool ok = asked >= 0 && asked < n_pages;
-        if (!ok && asked != INT_MIN && report) atomicOr(err, 1);
-        page = ok ? asked : -1;
-    }
-    __device__ __forceinline__ uint32_t there() const { return __ballot_sync(0xffffffffu, page >= 0) & 0xffu; }
-};
-
-// One warp brings K and V tiles, a page a lane.
+// One thread brings K and V tiles, and the softmax's notes of them.
 template <int D, int kReq>
-__device__ __forceinline__ void load_tiles(const TcLaunch<kReq>& X, const Item& w, int lane, uint32_t sK, uint32_t sV, uint32_t bars,
-                                           uint32_t* notes, volatile uint32_t* abort) {
+__device__ __forceinline__ void load_tiles(const TcLaunch<kReq>& X, const Item& w, uint32_t sK, uint32_t sV, uint32_t bars,
+                                           TileNote* notes, volatile uint32_t* abort) {
     using C = Tc<D>;
     const PagedAttn<kReq>& P = X.a;
     auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
-    Pages pg{P.pg.table + (int64_t)w.R.row * P.pg.table_stride, P.pg.page_shift, P.pg.n_pages, w.k_lo, w.k_hi, INT_MIN, -1};
-    const int rows = 1 << pg.shift;                              // of a copy (a page holds at most a tile)
-    auto copy = [&](const CUtensorMap* tm, uint32_t tile, uint32_t full, uint32_t there) {
-        const int n = __popc(there) * 16;                        // rows that land; groups of a page come together
-        if (lane == 0) mbar_expect_tx(full, (uint32_t)n * D * 2);
-        __syncwarp();
-        if (lane < 8 && lane % (rows / 16) == 0 && pg.page >= 0) {         // a page a lane
-#pragma unroll
-            for (int b = 0; b < D / 64; ++b) tma_load_4d(tile + b * C::kHalf + lane * 16 * 128, tm, b * 64, 0, w.hk, pg.page, full);
-        }
-        __syncwarp();
-    };
-    uint32_t zeroed = 0;                 // tiles that went through VZ
-    pg.ask(w.j0, lane);
+    const int t0 = w.R.scratch + w.j0;
+    float2 unit = __ldg(X.unit + (int64_t)t0 * P.hkv + w.hk);
+    uint32_t there = __ldg(X.there + t0);
     for (int j = 0; j < w.n; ++j) {
-        const int key0 = (w.j0 + j) * BN;
-        pg.take(P.err, lane < 8);
-        pg.ask(w.j0 + j + 1, lane);
-        // a page is copied whole if any of its groups has a key: so are the groups past the last key
-        uint32_t there = pg.there();
-        for (int g = 0; g < 8; g += rows / 16)
-            if (there >> g & 1u) there |= ((1u << (rows / 16)) - 1u) << g;
-        if (lane == 0) notes[j & (kUnits - 1)] = there;
+        const int at = (t0 + j) * P.hkv + w.hk;
+        notes[j & (kUnits - 1)] = TileNote{unit.x, unit.y, there, 0u};
+        if (j + 1 < w.n) {               // (the next tile's: on their way while this one's are)
+            unit = __ldg(X.unit + (int64_t)at + P.hkv);
+            there = __ldg(X.there + t0 + j + 1);
+        }
         const int ks = j % C::kK, vs = j % C::kV;
         if (j >= C::kK) mbar_wait(bar(C::KE + ks), (uint32_t)(j / C::kK - 1) & 1u, P.err, abort);
-        copy(&X.tm_k, sK + ks * C::kTile, bar(C::KF + ks), there);
-        if (j >= C::kV) mbar_wait(bar(C::VE + vs), (uint32_t)(j / C::kV - 1) & 1u, P.err, abort);
-        const uint32_t tile = sV + vs * C::kTile;
-        if (there == 0xffu && key0 >= w.k_lo && key0 + BN <= w.k_hi) {
-            copy(&X.tm_v, tile, bar(C::VF + vs), there);
-            continue;
-        }
-        // some rows must be zero: the tile is handed over once they are (at most a CTA's first and last
-        // tiles, and those with a page that is none)
-        copy(&X.tm_v, tile, bar(C::VZ), there);
-        mbar_wait(bar(C::VZ), zeroed & 1u, P.err, abort);
-        ++zeroed;
-        for (int r = lane; r < BN; r += 32) {
-            const int key = key0 + r;
-            if (key >= w.k_lo && key < w.k_hi && (there >> (r >> 4) & 1u)) continue;
+        mbar_expect_tx(bar(C::KF + ks), C::kTile);
 #pragma unroll
-            for (int q = 0; q < D / 8; ++q) sts128_(tile + (q >> 3) * C::kHalf + r * 128 + (q & 7) * 16, make_uint4(0u, 0u, 0u, 0u));
-        }
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::VF + vs));
+        for (int b = 0; b < D / 64; ++b) tma_load_3d(sK + ks * C::kTile + b * C::kHalf, &X.tm_k, b * 64, 0, at, bar(C::KF + ks));
+        if (j >= C::kV) mbar_wait(bar(C::VE + vs), (uint32_t)(j / C::kV - 1) & 1u, P.err, abort);
+        mbar_expect_tx(bar(C::VF + vs), C::kTile);
+#pragma unroll
+        for (int b = 0; b < D / 64; ++b) tma_load_3d(sV + vs * C::kTile + b * C::kHalf, &X.tm_v, b * 64, 0, at, bar(C::VF + vs));
     }
 }
 
@@ -188,7 +161,7 @@ __device__ __forceinline__ void load_tiles(const TcLaunch<kReq>& X, const Item& 
 template <int D>
 __device__ __forceinline__ void issue_products(uint32_t tmem, uint32_t sQ, uint32_t sK, uint32_t sV, uint32_t bars, int n, bool has_b,
                                                int32_t* err, volatile uint32_t* abort) {
-    constexpr uint32_t idS = idesc_bf16(BM, BN, false), idO = idesc_bf16(BM, D, true);
+    constexpr uint32_t idS = idesc_f16(BM, BN, false), idO = idesc_f16(BM, D, true);
     using C = Tc<D>;
     constexpr uint64_t kTileDesc = (uint64_t)(C::kTile >> 4);
     auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
@@ -261,10 +234,11 @@ __device__ __forceinline__ void issue_products(uint32_t tmem, uint32_t sQ, uint3
 // ------------------------------------------------------------------ softmax
 
 // The pair's queries, turned, into their tiles (128-byte swizzle), by the eight softmax warps, 32 rows
-// each: copied as they are, all on their way at once, then turned in place, eight rows at a time (a row
-// after the other is a chain of dependent instructions, and took 9000 clocks in all).
+// each: copied as they are, all on their way at once, then turned and made f16 in place, eight rows at a
+// time (a row after the other is a chain of dependent instructions, and took 9000 clocks in all).  A
+// row's largest value goes to [2^14, 2^15): its scores come back by 2^back.
 template <int D, int kReq>
-__device__ __forceinline__ void put_queries(const PagedAttn<kReq>& P, const Item& w, int warp, int lane, uint32_t sQ) {
+__device__ __forceinline__ void put_queries(const PagedAttn<kReq>& P, const Item& w, int warp, int lane, uint32_t sQ, int8_t* s_back) {
     using T = __nv_bfloat16;
     using C = Tc<D>;
     const int G = P.hq / P.hkv;
@@ -285,78 +259,98 @@ __device__ __forceinline__ void put_queries(const PagedAttn<kReq>& P, const Item
         }
         cp_async_commit();
     }
+    constexpr int E = D / 64, kBatch = 8;                // channels of each half a lane; rows in flight
+    const int c = lane * E, q0 = c >> 3, q1 = (D / 2 + c) >> 3;
+    uint64_t turn[E] = {};
+    int pos_row = 0;
+    float2 cs[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) cs[e] = make_float2(1.f, 0.f);
     if (P.turn && n > 0) {
-        constexpr int E = D / 64, kBatch = 8;            // channels of each half a lane; rows in flight
-        const int c = lane * E, q0 = c >> 3, q1 = (D / 2 + c) >> 3;
-        uint64_t turn[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) turn[e] = lane_turn(P.rope.turn, c + e);
-        const int pos_row = __ldg(P.turn + w.R.q0 + (w.row0 + r0 + min(lane, n - 1)) / G);
-        int pos_cs = __shfl_sync(0xffffffffu, pos_row, 0);
-        float2 cs[E];
+        pos_row = __ldg(P.turn + w.R.q0 + (w.row0 + r0 + min(lane, n - 1)) / G);
+    }
+    int pos_cs = __shfl_sync(0xffffffffu, pos_row, 0);
+    if (P.turn)
 #pragma unroll
         for (int e = 0; e < E; ++e) cs[e] = turn_cs_fast(turn[e], pos_cs);
-        cp_async_wait<0>();
-        __syncwarp();
+    cp_async_wait<0>();
+    __syncwarp();
 #pragma unroll 1
-        for (int i0 = 0; i0 < 32; i0 += kBatch) {
-            uint32_t x0[kBatch], x1[kBatch];
-            const uint32_t a0 = (c & 7) * 2 + (q0 >> 3) * C::kHalf + tile + i0 * 128, a1 = (c & 7) * 2 + (q1 >> 3) * C::kHalf + tile + i0 * 128;
+    for (int i0 = 0; i0 < 32; i0 += kBatch) {
+        uint32_t x0[kBatch], x1[kBatch];
+        const uint32_t a0 = (c & 7) * 2 + (q0 >> 3) * C::kHalf + tile + i0 * 128, a1 = (c & 7) * 2 + (q1 >> 3) * C::kHalf + tile + i0 * 128;
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) {           // (i0 is a multiple of 8: the rows swap as rows 0 .. 7 do)
-                const uint32_t s0 = a0 + i * 128 + (((q0 & 7) ^ i) << 4), s1 = a1 + i * 128 + (((q1 & 7) ^ i) << 4);
-                if constexpr (E == 2) {
-                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x0[i]) : "r"(s0));
-                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x1[i]) : "r"(s1));
-                } else {
-                    uint16_t y0, y1;
-                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y0) : "r"(s0));
-                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y1) : "r"(s1));
-                    x0[i] = y0;
-                    x1[i] = y1;
-                }
-            }
-            float lo[kBatch][E], hi[kBatch][E];
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                const int pos = __shfl_sync(0xffffffffu, pos_row, i0 + i);
-                if (pos != pos_cs) {                     // the heads of a token share its angles
-#pragma unroll
-                    for (int e = 0; e < E; ++e) cs[e] = turn_cs_fast(turn[e], pos);
-                    pos_cs = pos;
-                }
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    rotate1(__uint_as_float(e == 0 ? x0[i] << 16 : x0[i] & 0xffff0000u),
-                            __uint_as_float(e == 0 ? x1[i] << 16 : x1[i] & 0xffff0000u), cs[e], lo[i][e], hi[i][e]);
-            }
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                const uint32_t s0 = a0 + i * 128 + (((q0 & 7) ^ i) << 4), s1 = a1 + i * 128 + (((q1 & 7) ^ i) << 4);
-                if constexpr (E == 2) {
-                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(s0), "r"(pack_bf16(lo[i][0], lo[i][1])));
-                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(s1), "r"(pack_bf16(hi[i][0], hi[i][1])));
-                } else {
-                    asm volatile("st.shared.u16 [%0], %1;" ::"r"(s0), "h"(__bfloat16_as_ushort(__float2bfloat16_rn(lo[i][0]))));
-                    asm volatile("st.shared.u16 [%0], %1;" ::"r"(s1), "h"(__bfloat16_as_ushort(__float2bfloat16_rn(hi[i][0]))));
-                }
+        for (int i = 0; i < kBatch; ++i) {               // (i0 is a multiple of 8: the rows swap as rows 0 .. 7 do)
+            const uint32_t s0 = a0 + i * 128 + (((q0 & 7) ^ i) << 4), s1 = a1 + i * 128 + (((q1 & 7) ^ i) << 4);
+            if constexpr (E == 2) {
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x0[i]) : "r"(s0));
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x1[i]) : "r"(s1));
+            } else {
+                uint16_t y0, y1;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y0) : "r"(s0));
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y1) : "r"(s1));
+                x0[i] = y0;
+                x1[i] = y1;
             }
         }
-    } else {
-        cp_async_wait<0>();
+        float lo[kBatch][E], hi[kBatch][E];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int pos = __shfl_sync(0xffffffffu, pos_row, i0 + i);
+            if (pos != pos_cs) {                         // the heads of a token share its angles
+#pragma unroll
+                for (int e = 0; e < E; ++e) cs[e] = turn_cs_fast(turn[e], pos);
+                pos_cs = pos;
+            }
+            uint32_t top = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float x = __uint_as_float(e == 0 ? x0[i] << 16 : x0[i] & 0xffff0000u);
+                const float y = __uint_as_float(e == 0 ? x1[i] << 16 : x1[i] & 0xffff0000u);
+                rotate1(x, y, cs[e], lo[i][e], hi[i][e]);
+                if (!P.turn) {
+                    lo[i][e] = x;
+                    hi[i][e] = y;
+                }
+                top = max(top, max(__float_as_uint(lo[i][e]) & 0x7fffffffu, __float_as_uint(hi[i][e]) & 0x7fffffffu));
+            }
+            top = __reduce_max_sync(0xffffffffu, top);
+            const int ex = (int)(top >> 23) - 127;       // zero and non-finite rows stay as they are
+            const bool scaled = top < 0x7f800000u && ex > -100;
+            const float f = scaled ? exp2f((float)(14 - ex)) : 1.f;
+            if (lane == 0) s_back[r0 + i0 + i] = (int8_t)(scaled ? ex - 14 : 0);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                lo[i][e] *= f;
+                hi[i][e] *= f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const uint32_t s0 = a0 + i * 128 + (((q0 & 7) ^ i) << 4), s1 = a1 + i * 128 + (((q1 & 7) ^ i) << 4);
+            if constexpr (E == 2) {
+                asm volatile("st.shared.u32 [%0], %1;" ::"r"(s0), "r"(pack_f16(lo[i][0], lo[i][1])));
+                asm volatile("st.shared.u32 [%0], %1;" ::"r"(s1), "r"(pack_f16(hi[i][0], hi[i][1])));
+            } else {
+                asm volatile("st.shared.u16 [%0], %1;" ::"r"(s0), "h"((uint16_t)pack_f16(lo[i][0], 0.f)));
+                asm volatile("st.shared.u16 [%0], %1;" ::"r"(s1), "h"((uint16_t)pack_f16(hi[i][0], 0.f)));
+            }
+        }
     }
 }
 
 // One softmax thread: row r of tile x over the CTA's key tiles, then its output.
 //
-// Weights are 2^(score - ref) with the reference of the tiles before: bf16 holds any weight that fp32
-// does, so the tile's own maximum need not be known first, and is found after the weights are handed
-// over, beside the products.  O and the sum are scaled to a new reference, before the next tile, only
-// when the maximum has passed the old one by 8.  Where a sum shows weights of 2^40 and more (or the row
-// has no reference yet) the maximum comes first after all.
-template <int D, int kReq>
+// Weights are 2^(score + offset - ref) with the reference of the tiles before: the tile's own maximum need
+// not be known first, and is found after the weights are handed over, beside the products.  O and the sum
+// are scaled to a new reference, before the next tile, only when the maximum has passed the old one by 8.
+// Where a sum shows weights near f16's largest (or the row has no reference yet) the maximum comes first
+// after all.
+template <int D, bool kCodes, int kReq>
 __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item& w, uint32_t tmem, uint32_t bars, int x, int quad, int lane,
-                                             const uint32_t* notes, volatile uint32_t* abort) {
+                                             const TileNote* notes, const int8_t* s_back, volatile uint32_t* abort) {
     using T = __nv_bfloat16;
     using C = Tc<D>;
     const PagedAttn<kReq>& P = X.a;
@@ -369,7 +363,7 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
     const int my = min(row, w.live - 1);
     const int end = w.R.n_keys - w.R.nq + (w.row0 + my) / G;     // the last key the row sees
     const int start = P.window ? end - P.window : -1;            // and the last that it does not, before them
-    const float f = P.scale_log2;
+    const float rs = P.scale_log2 * exp2f((float)s_back[row]);
     float ref = -CUDART_INF_F, top = -CUDART_INF_F, l = 0.f;
     auto scale_o = [&](float alpha) {
 #pragma unroll 1
@@ -399,7 +393,9 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
             if (j > 0) scale_o(alpha);
             l *= alpha;
         }
-        const uint32_t groups = notes[j & (kUnits - 1)];
+        const TileNote nt = notes[j & (kUnits - 1)];
+        const uint32_t groups = nt.there;
+        const float f = rs * nt.k_unit, ve = nt.v_exp;
         const int key0 = (w.j0 + j) * BN;
         tmem_ld_wait();
         if (key0 + BN - 1 > end || key0 <= start || groups != 0xffu) {
@@ -420,11 +416,11 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
                 for (int e = 2; e < 32; e += 2) m = fmax3(m, __uint_as_float(sv[c][e]), __uint_as_float(sv[c][e + 1]));
                 top4[c] = m;
             }
-            top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * f;
+            top = fmaf(fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])), f, ve);
         };
         auto weigh = [&]() {
             float ps[4] = {0.f, 0.f, 0.f, 0.f};
-            const float off = ref == -CUDART_INF_F ? 0.f : -ref;
+            const float off = ref == -CUDART_INF_F ? ve : ve - ref;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 uint32_t pk[16];
@@ -436,7 +432,7 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
                     a1 = ex2(a1);
                     if (i & 1) fadd2(ps[2], ps[3], a0, a1);
                     else fadd2(ps[0], ps[1], a0, a1);
-                    pk[i] = pack_bf16(a0, a1);
+                    pk[i] = pack_f16(a0, a1);
                 }
                 tmem_st16(colS + c * 16, pk);
             }
@@ -446,7 +442,7 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
         bool high = ref == -CUDART_INF_F;
         if (!__all_sync(0xffffffffu, high)) {
             sum = weigh();
-            high = high || !(sum < 1.0e12f);
+            high = high || !(sum < 32768.f);
         }
         if (__any_sync(0xffffffffu, high)) {
             find_top();
@@ -462,7 +458,7 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
         tmem_st_wait();
         tc_fence_before();
         mbar_arrive(bar(C::P + x));
-        l += sum;
+        l = fmaf(sum, ex2(-ve), l);
         find_top();
     }
     if (w.n > 0) {
@@ -527,7 +523,7 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
         const int hh = w.hk * G + rr % G;
         float q[D / 32], o[D / 32], m, sum;
         lane_query<T, D>(P, t, hh, lane, q);
-        row_attend<T, D, false>(P, q, w.R.row, w.hk, lo, hi, 1, lane, m, sum, o);
+        row_attend<T, D, kCodes>(P, q, w.R.row, w.hk, lo, hi, 1, lane, m, sum, o);
         const float iv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
         for (int e = 0; e < D / 32; ++e) {
@@ -541,7 +537,7 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
 
 // ------------------------------------------------------------------ kernel
 
-template <int D, int kReq>
+template <int D, bool kCodes, int kReq>
 __global__ void __launch_bounds__(kThreads, 1) paged_tc_kernel(const __grid_constant__ TcLaunch<kReq> X) {
     const PagedAttn<kReq>& P = X.a;
     using C = Tc<D>;
@@ -549,7 +545,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tc_kernel(const __grid_cons
     uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t sQ = smem_u32(smem), sK = sQ + 2 * C::kTile, sV = sK + C::kK * C::kTile;
     const uint32_t bars = sQ + C::kTiles;
-    uint32_t* const notes = reinterpret_cast<uint32_t*>(smem + C::kNotes);   // of a tile: which groups of 16 keys are there
+    TileNote* const notes = reinterpret_cast<TileNote*>(smem + C::kNotes);
+    int8_t* const s_back = reinterpret_cast<int8_t*>(smem + C::kBack);
     uint32_t* const slot = reinterpret_cast<uint32_t*>(smem + C::kSlot);
     volatile uint32_t* const abort = slot + 1;
     auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
@@ -566,7 +563,6 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tc_kernel(const __grid_cons
             mbar_init(bar(C::VF + s), 1);
             mbar_init(bar(C::VE + s), 1);
         }
-        mbar_init(bar(C::VZ), 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(C::S + i), 1);
             mbar_init(bar(C::P + i), 128);
@@ -589,15 +585,16 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tc_kernel(const __grid_cons
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsLow));
-        if (warp == 1) load_tiles<D>(X, w, lane, sK, sV, bars, notes, abort);
+        if (warp == 1 && lane == 0 && w.n > 0) load_tiles<D>(X, w, sK, sV, bars, notes, abort);
         else if (warp == 0 && lane == 0 && w.n > 0) issue_products<D>(tmem, sQ, sK, sV, bars, w.n, has_b, P.err, abort);
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
-        put_queries<D>(P, w, warp - 4, lane, sQ);
+        put_queries<D>(P, w, warp - 4, lane, sQ, s_back);
         fence_proxy_async();
+        asm volatile("bar.sync 1, 256;" ::: "memory");           // (the rows' powers of two)
         mbar_arrive(bar(C::Q));
         const int x = warp >= 8;
-        if (x == 0 || has_b) softmax_rows<D>(X, w, tmem, bars, x, warp & 3, lane, notes, abort);
+        if (x == 0 || has_b) softmax_rows<D, kCodes>(X, w, tmem, bars, x, warp & 3, lane, notes, s_back, abort);
     }
 
     tc_fence_before();
@@ -790,13 +787,12 @@ std::vector<PagedReq> plan(const PagedAttnCall& c, const PagedReq* req, int n) {
     return best;
 }
 
-template <int D, int kReq>
-cudaError_t launch(const PagedAttnCall& c, const std::vector<PagedReq>& entries, cudaStream_t s) {
+template <int D, bool kCodes, int kReq>
+cudaError_t launch(const PagedAttnCall& c, const KeyTiles& tiles, const std::vector<PagedReq>& entries, cudaStream_t s) {
     static PerDevice<cudaError_t> smem_set;
-    const auto kernel = paged_tc_kernel<D, kReq>;
+    const auto kernel = paged_tc_kernel<D, kCodes, kReq>;
     cudaError_t e = opt_in_smem(smem_set, (const void*)kernel, Tc<D>::kSmem);
     if (e != cudaSuccess) return e;
-    const int rows = 1 << c.pg.page_shift;
     for (size_t b0 = 0; b0 < entries.size(); b0 += kReq) {
         const int nb = (int)std::min<size_t>(entries.size() - b0, kReq);
         TcLaunch<kReq> X;
@@ -823,9 +819,13 @@ cudaError_t launch(const PagedAttnCall& c, const std::vector<PagedReq>& entries,
             X.part_o = static_cast<float*>(p);
             X.part_lse = reinterpret_cast<float*>(static_cast<char*>(p) + o_bytes);
         }
-        if (!encode_page_map(&X.tm_k, c.pg.k, c.pg, c.hkv, D, false, 64, rows, CU_TENSOR_MAP_SWIZZLE_128B) ||
-            !encode_page_map(&X.tm_v, c.pg.v, c.pg, c.hkv, D, false, 64, rows, CU_TENSOR_MAP_SWIZZLE_128B))
+        const cuuint64_t dims[3] = {D, kTileKeys, (cuuint64_t)tiles.n * c.hkv}, strides[2] = {D * 2, kTileKeys * D * 2};
+        const cuuint32_t box[3] = {64, kTileKeys, 1};
+        if (!encode_tensor_map(&X.tm_k, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, tiles.k, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B) ||
+            !encode_tensor_map(&X.tm_v, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, tiles.v, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B))
             return cudaErrorInvalidValue;
+        X.unit = tiles.unit;
+        X.there = tiles.there;
         kernel<<<(unsigned)items, kThreads, Tc<D>::kSmem, s>>>(X);
         e = cudaGetLastError();
         if (e == cudaSuccess && units > 0) {
@@ -846,16 +846,17 @@ cudaError_t launch(const PagedAttnCall& c, const std::vector<PagedReq>& entries,
     return cudaSuccess;
 }
 
-template <int D>
-cudaError_t by_count(const PagedAttnCall& c, const PagedReq* req, int n, cudaStream_t s) {
+template <int D, bool kCodes>
+cudaError_t by_count(const PagedAttnCall& c, const KeyTiles& tiles, const PagedReq* req, int n, cudaStream_t s) {
     const std::vector<PagedReq> entries = plan(c, req, n);
-    return (int)entries.size() <= kPagedFew ? launch<D, kPagedFew>(c, entries, s) : launch<D, kPagedMany>(c, entries, s);
+    return (int)entries.size() <= kPagedFew ? launch<D, kCodes, kPagedFew>(c, tiles, entries, s) : launch<D, kCodes, kPagedMany>(c, tiles, entries, s);
 }
 
 }  // namespace
 
-cudaError_t launch_paged_tc(const PagedAttnCall& c, const PagedReq* req, int n, int d, cudaStream_t s) {
-    return d == 128 ? by_count<128>(c, req, n, s) : by_count<64>(c, req, n, s);
+cudaError_t launch_paged_tc(const PagedAttnCall& c, const KeyTiles& tiles, const PagedReq* req, int n, int d, bool codes, cudaStream_t s) {
+    if (d == 128) return codes ? by_count<128, true>(c, tiles, req, n, s) : by_count<128, false>(c, tiles, req, n, s);
+    return codes ? by_count<64, true>(c, tiles, req, n, s) : by_count<64, false>(c, tiles, req, n, s);
 }
 
 }  // namespace c2kv

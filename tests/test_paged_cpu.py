@@ -44,3 +44,12 @@ def test_verify_by_hand():
     assert run([1, 1], [0.4, 0.0], 0.49) == (0, 0)           # 0.4 * 0.75 >= 0.25: left over q are 0.25, 0, 0.25
     assert run([1, 1], [0.4, 0.0], 0.51) == (0, 2)
     assert run([0, 0], [0.9, 0.0], 0.0) == (1, 1)            # p of the second draft is 0, its product 0: refused
+
+
+def test_no_context_is_refused():
+    import __graft_entry__ as g
+    g.build()
+    from paper_2607_17715_gb300 import c2kv
+    for name in ("c2kv_paged_append", "c2kv_paged_gather", "c2kv_paged_attend", "c2kv_verify_drafts"):
+        fn = getattr(c2kv._lib, name)
+        assert fn(*[None if t is c2kv._VP else 0 for t in fn.argtypes]) == c2kv.ERR_ARG
