@@ -10,6 +10,7 @@
 //
 // Bytes bound it: a page's read once, two written for each value.
 #include "paged.cuh"
+#include "ptx.cuh"
 #include "vec16.cuh"
 
 #include <algorithm>
@@ -49,6 +50,8 @@ template <int D, bool kCodes, int kReq>
 __global__ void __launch_bounds__(kExpandThreads) paged_expand_kernel(const __grid_constant__ PagedExpand<kReq> P) {
     constexpr int kChunks = D / 16, kStep = kExpandThreads / kChunks, kPasses = kTileKeys / kStep;   // rows a pass
     __shared__ uint32_t s_top[kExpandThreads / 32], s_there;
+    // the attention may be set up and turn its queries meanwhile: it waits for this grid before it reads tiles
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     int r = 0;
     for (int hi = P.n; hi - r > 1;) {
         const int mid = (r + hi) >> 1;
@@ -125,10 +128,10 @@ __global__ void __launch_bounds__(kExpandThreads) paged_expand_kernel(const __gr
     for (int w = 0; w < kExpandThreads / 32; ++w) top = max(top, s_top[w]);
     // 16-bit values to below 2^9, as codes times their relative scales are
     const int unit = kCodes ? above(top) : max(-100, above(top) - 9);
-    const float inv = exp2f((float)-unit);
+    const float inv = pow2i(-unit);
     if (threadIdx.x == 0) {
         float* const u = reinterpret_cast<float*>(P.to.unit + tile * P.hkv + h);
-        u[v] = v ? (float)unit : exp2f((float)unit);
+        u[v] = v ? (float)unit : pow2i(unit);
         if (h == 0 && !v) P.to.there[tile] = s_there;
     }
     __half* const out = static_cast<__half*>(v ? P.to.v : P.to.k) + (tile * P.hkv + h) * kTileKeys * D + chunk * 16;

@@ -326,8 +326,8 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
             // largest value to [2^6, 2^7); zero and non-finite rows as they are
             const int ex = (int)(top >> 23) - 127;
             if (top < 0x7f800000u && ex > -100) {
-                f = exp2f((float)(6 - ex));
-                back = exp2f((float)(ex - 6));
+                f = pow2i(6 - ex);
+                back = pow2i(ex - 6);
             }
         }
         if (lane == 0) {
@@ -460,9 +460,9 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
             if (top >= 0x7f800000u || (edge && !there(lane))) top = 0;
             top = __reduce_max_sync(0xffffffffu, top);
             const int u = max(unit, min((int)(top >> 23) - 126, 126));     // every scale below 2^u
-            shift = unit == u ? 1.f : exp2f((float)max(unit - u, -250));
+            shift = pow2i(unit - u);
             unit = u;
-            const float inv = exp2f((float)-u);
+            const float inv = pow2i(-u);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -591,7 +591,7 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
     __syncthreads();                     // every stage has been read
     float* const joined = reinterpret_cast<float*>(smem);
     auto line = [](int f) { return f ^ (2 * (f >> 3 & 3)); };
-    const float one = kCodes ? exp2f((float)unit) : 1.f;
+    const float one = kCodes ? pow2i(unit) : 1.f;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll

@@ -133,6 +133,7 @@ __device__ __forceinline__ void load_tiles(const TcLaunch<kReq>& X, const Item& 
     const PagedAttn<kReq>& P = X.a;
     auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
     const int t0 = w.R.scratch + w.j0;
+    asm volatile("griddepcontrol.wait;" ::: "memory");           // the key tiles are complete and visible
     float2 unit = __ldg(X.unit + (int64_t)t0 * P.hkv + w.hk);
     uint32_t there = __ldg(X.there + t0);
     for (int j = 0; j < w.n; ++j) {
@@ -319,7 +320,7 @@ __device__ __forceinline__ void put_queries(const PagedAttn<kReq>& P, const Item
             top = __reduce_max_sync(0xffffffffu, top);
             const int ex = (int)(top >> 23) - 127;       // zero and non-finite rows stay as they are
             const bool scaled = top < 0x7f800000u && ex > -100;
-            const float f = scaled ? exp2f((float)(14 - ex)) : 1.f;
+            const float f = scaled ? pow2i(14 - ex) : 1.f;
             if (lane == 0) s_back[r0 + i0 + i] = (int8_t)(scaled ? ex - 14 : 0);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
@@ -363,7 +364,7 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
     const int my = min(row, w.live - 1);
     const int end = w.R.n_keys - w.R.nq + (w.row0 + my) / G;     // the last key the row sees
     const int start = P.window ? end - P.window : -1;            // and the last that it does not, before them
-    const float rs = P.scale_log2 * exp2f((float)s_back[row]);
+    const float rs = P.scale_log2 * pow2i(s_back[row]);
     float ref = -CUDART_INF_F, top = -CUDART_INF_F, l = 0.f;
     auto scale_o = [&](float alpha) {
 #pragma unroll 1
@@ -826,18 +827,22 @@ cudaError_t launch(const PagedAttnCall& c, const KeyTiles& tiles, const std::vec
             return cudaErrorInvalidValue;
         X.unit = tiles.unit;
         X.there = tiles.there;
-        kernel<<<(unsigned)items, kThreads, Tc<D>::kSmem, s>>>(X);
-        e = cudaGetLastError();
+        // each starts while the kernel before it ends, and waits for it where it reads what that wrote
+        cudaLaunchConfig_t cfg{};
+        cudaLaunchAttribute at{};
+        at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at.val.programmaticStreamSerializationAllowed = 1;
+        cfg.gridDim = dim3((unsigned)items);
+        cfg.blockDim = dim3(kThreads);
+        cfg.dynamicSmemBytes = Tc<D>::kSmem;
+        cfg.stream = s;
+        cfg.attrs = &at;
+        cfg.numAttrs = b0 == 0;          // (a later part follows other kernels of the call)
+        e = cudaLaunchKernelEx(&cfg, kernel, X);
         if (e == cudaSuccess && units > 0) {
-            cudaLaunchConfig_t cfg{};
-            cudaLaunchAttribute at{};
-            at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-            at.val.programmaticStreamSerializationAllowed = 1;
             cfg.gridDim = dim3((unsigned)(units * (kPair / kJoinRows)));
             cfg.blockDim = dim3(kJoinThreads);
             cfg.dynamicSmemBytes = (size_t)most * kJoinRows * 4;
-            cfg.stream = s;
-            cfg.attrs = &at;
             cfg.numAttrs = 1;
             e = cudaLaunchKernelEx(&cfg, paged_join_kernel<D, kReq>, X);
         }

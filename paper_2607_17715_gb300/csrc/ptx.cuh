@@ -16,6 +16,9 @@ __device__ __forceinline__ uint32_t smem_u32(const void* p) {
     return static_cast<uint32_t>(__cvta_generic_to_shared(p));
 }
 
+// 2^e for -127 < e < 128, from its bits; 0 for smaller e.
+__device__ __forceinline__ float pow2i(int e) { return e > -127 ? __uint_as_float((uint32_t)(e + 127) << 23) : 0.f; }
+
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
