@@ -8,11 +8,12 @@ namespace c2kv {
 namespace {
 
 // Query rows of a KV head up to which mma.sync takes a request.  tcgen05 works on 128 rows whatever they
-// are, and over 8-bit pages pays for their expansion first; mma.sync reads and converts the keys again for
-// every 32 rows.  Measured (us, mma.sync / tcgen05; 8 requests of 4000 rows, 32 / 8 heads): 16-bit pages of
-// 128 channels 48 rows 61 / 43, and 40 rows (64 heads, 6000 rows) 43 / 54; of 64 channels 48 rows 33 / 36,
-// 80 rows 60 / 36; 8-bit pages of 128 channels 48 rows 52 / 83, 80 rows 97 / 82.
-int mma_rows(int d, bool codes) { return codes ? 64 : d == 128 ? 40 : 56; }
+// are and pays for its key tiles first; mma.sync reads and converts the keys again for every 32 rows.
+// Measured (us, mma.sync / tcgen05; 32 / 8 heads, 64 and 80 rows; 1 request of 30000 rows, 8 of 4000, 16 of
+// 500): 8-bit pages of 128 channels 60 / 92 and 74 / 92, 62 / 78 and 96 / 78, 23 / 34 and 39 / 33; 16-bit
+// ones 91 / 100 and 126 / 100, 97 / 90 and 185 / 90, 44 / 37 and 62 / 38; 16-bit of 64 channels 44 / 65 and
+// 56 / 66, 47 / 60 and 75 / 61, 19 / 27 and 30 / 27.
+constexpr int kMmaRows = 64;
 
 // Requests of many rows on tcgen05: what they see of their pages becomes key tiles first, in scratch that
 // the stream hands back; requests go in groups so that the scratch stays small beside the cache.
@@ -77,7 +78,7 @@ cudaError_t launch_paged_attn(const PagedAttnCall& c, int dtype, int d, bool cod
     if (dtype == kDtypeF32) return launch_paged_simt(c, req.data(), (int)req.size(), d, codes, s);
     // requests of many rows on tcgen05, those of few on mma.sync
     std::vector<PagedReq> few, many;
-    for (const PagedReq& q : req) ((int64_t)q.nq * (c.hq / c.hkv) > mma_rows(d, codes) ? many : few).push_back(q);
+    for (const PagedReq& q : req) ((int64_t)q.nq * (c.hq / c.hkv) > kMmaRows ? many : few).push_back(q);
     cudaError_t e = cudaSuccess;
     if (!many.empty()) e = launch_many(c, many.data(), (int)many.size(), d, codes, s);
     if (e == cudaSuccess && !few.empty()) e = launch_paged_mma(c, few.data(), (int)few.size(), d, codes, s);
