@@ -444,7 +444,7 @@ typedef struct c2kv_pages {
  *   batch        : requests B >= 1.
  *   table        : device int32 [B] rows of table_width page numbers, table_stride apart.
  *   new_ptr      : host int32 [B + 1], non-decreasing from 0; a request may have no new token.
- *   start        : host int32 [B].
+ *   start        : host int32 [B]; rows end at 2^30.
  *   k, v         : device [T][Hkv][d] in the context's type, tokens kv_stride elements apart
  *                  (0 = Hkv * d; rows of a fused projection are further apart).
  *   turn         : device int32 [T], or NULL.
@@ -482,7 +482,7 @@ c2kv_status c2kv_paged_gather(c2kv_ctx* ctx, const c2kv_pages* pages, int32_t ba
  *
  *   batch, table, table_width, table_stride : as c2kv_paged_append.
  *   q_ptr        : host int32 [B + 1], non-decreasing from 0; a request may have no query.
- *   n_keys       : host int32 [B] rows of each request, >= 0.
+ *   n_keys       : host int32 [B] rows of each request, 0 .. 2^30.
  *   q            : device [T][Hq][d], tokens q_stride elements apart (0 = Hq * d).
  *   turn         : device int32 [T] positions of the queries, or NULL (turned already).
  *   out          : device [T][Hq][d] (context dtype).

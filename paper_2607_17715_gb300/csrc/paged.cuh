@@ -132,7 +132,7 @@ struct KeyTiles {
     void* v;
     float2* unit;            // [n][Hkv]: the factor that K's values lack, and the exponent of V's
     uint32_t* there;         // [n]: which groups of 16 keys lie in pages (bits 0 .. 7)
-    int32_t n;
+    int32_t n;               // may be 0: no query sees a row
 };
 struct PagedExpandCall {
     PageView pg;

@@ -3,9 +3,10 @@
 #include "c2kv.h"
 #include "paged.cuh"
 
+#include <algorithm>
 #include <cstdarg>
 #include <cstdio>
-#include <new>
+#include <exception>
 
 namespace {
 
@@ -68,9 +69,12 @@ c2kv_status check_device(c2kv_ctx* c, const char* what, std::initializer_list<co
     return C2KV_OK;
 }
 
-// Rows [0, rows) of every request must be named by its table.
+// Rows [0, rows) of every request must be named by its table.  The kernels count rows in 32 bits and
+// round them up to whole tiles: 2^30 leave room.
+constexpr int64_t kMostRows = (int64_t)1 << 30;
+
 bool in_table(int64_t rows, int32_t table_width, const c2kv::PageView& pg) {
-    return rows <= (int64_t)table_width << pg.page_shift;
+    return rows <= std::min((int64_t)table_width << pg.page_shift, kMostRows);
 }
 
 c2kv_status move(c2kv_ctx* c, const char* what, bool append, const c2kv_pages* pages, int32_t batch, const int32_t* table,
@@ -124,8 +128,8 @@ c2kv_status c2kv_paged_append(c2kv_ctx* ctx, const c2kv_pages* pages, int32_t ba
     try {
         return move(ctx, "paged_append", true, pages, batch, table, table_width, table_stride, new_ptr, start,
                     const_cast<void*>(k), const_cast<void*>(v), kv_stride, turn);
-    } catch (...) {
-        return C2KV_ERR_NOMEM;
+    } catch (const std::exception&) {
+        return refuse(ctx, C2KV_ERR_NOMEM, "paged_append: host allocation failed");
     }
 }
 
@@ -136,8 +140,8 @@ c2kv_status c2kv_paged_gather(c2kv_ctx* ctx, const c2kv_pages* pages, int32_t ba
     try {
         return move(ctx, "paged_gather", false, pages, batch, table, table_width, table_stride, row_ptr, start, k_out, v_out,
                     out_stride, turn);
-    } catch (...) {
-        return C2KV_ERR_NOMEM;
+    } catch (const std::exception&) {
+        return refuse(ctx, C2KV_ERR_NOMEM, "paged_gather: host allocation failed");
     }
 }
 
@@ -154,9 +158,12 @@ c2kv_status c2kv_paged_attend(c2kv_ctx* ctx, const c2kv_pages* pages, int32_t ba
         if (st != C2KV_OK) return st;
         if (!n_keys) return refuse(ctx, C2KV_ERR_ARG, "%s: null n_keys", what);
         if (window < 0) return refuse(ctx, C2KV_ERR_ARG, "%s: window < 0", what);
-        for (int32_t r = 0; r < batch; ++r)
+        int32_t most = 0;
+        for (int32_t r = 0; r < batch; ++r) {
             if (n_keys[r] < 0 || !in_table(n_keys[r], table_width, a.pg))
                 return refuse(ctx, C2KV_ERR_ARG, "%s: rows of request %d are outside its table", what, r);
+            most = std::max(most, n_keys[r]);
+        }
         if (q_ptr[batch] == 0) return c2kv::set_last_error(ctx, C2KV_OK, "");
         if (!q || !out) return refuse(ctx, C2KV_ERR_ARG, "%s: null q or out", what);
         const int64_t row = (int64_t)x.n_q_heads * x.head_dim;
@@ -178,7 +185,7 @@ c2kv_status c2kv_paged_attend(c2kv_ctx* ctx, const c2kv_pages* pages, int32_t ba
         a.err = x.err;
         a.hq = x.n_q_heads;
         a.hkv = x.n_kv_heads;
-        a.window = window;
+        a.window = window < most ? window : 0;   // (one that leaves nothing out is none)
         a.batch = batch;
         a.ptr = q_ptr;
         a.n_keys = n_keys;
@@ -187,8 +194,8 @@ c2kv_status c2kv_paged_attend(c2kv_ctx* ctx, const c2kv_pages* pages, int32_t ba
         const cudaError_t e = c2kv::launch_paged_attn(a, x.dtype, x.head_dim, pages->format == C2KV_PAGES_E4M3, x.stream);
         if (e != cudaSuccess) return launched(ctx, e, what);
         return c2kv::set_last_error(ctx, C2KV_OK, "");
-    } catch (...) {
-        return C2KV_ERR_NOMEM;
+    } catch (const std::exception&) {
+        return refuse(ctx, C2KV_ERR_NOMEM, "paged_attend: host allocation failed");
     }
 }
 
@@ -233,8 +240,8 @@ c2kv_status c2kv_verify_drafts(c2kv_ctx* ctx, int32_t batch, const int32_t* draf
         const cudaError_t e = c2kv::launch_verify(v, x.stream);
         if (e != cudaSuccess) return launched(ctx, e, what);
         return c2kv::set_last_error(ctx, C2KV_OK, "");
-    } catch (...) {
-        return C2KV_ERR_NOMEM;
+    } catch (const std::exception&) {
+        return refuse(ctx, C2KV_ERR_NOMEM, "verify_drafts: host allocation failed");
     }
 }
 

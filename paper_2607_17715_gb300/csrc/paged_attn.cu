@@ -52,7 +52,7 @@ cudaError_t launch_many(const PagedAttnCall& c, const PagedReq* req, int n, int 
         PagedExpandCall x{};
         x.pg = c.pg;
         x.to = KeyTiles{base, base + half, reinterpret_cast<float2*>(base + 2 * half), reinterpret_cast<uint32_t*>(base + 2 * half + units),
-                        (int32_t)std::max<int64_t>(1, total)};
+                        (int32_t)total};
         x.err = c.err;
         x.hkv = c.hkv;
         x.n = m;

@@ -179,7 +179,7 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
             const int64_t r = (int64_t)P.req[i].nq * (c.hq / c.hkv);
             rows += r;
             most = std::max(most, r);
-            keys = std::max<int64_t>(keys, c.window ? std::min(P.req[i].n_keys, c.window + P.req[i].nq) : P.req[i].n_keys);
+            keys = std::max<int64_t>(keys, c.window ? std::min<int64_t>(P.req[i].n_keys, (int64_t)c.window + P.req[i].nq) : P.req[i].n_keys);
         }
         const CorePlan plan = core_plan(most, c.hkv * std::max<int64_t>(1, (rows + most / 2) / most), keys, D, false,
                                         [&](int form, int ns, bool alone) {

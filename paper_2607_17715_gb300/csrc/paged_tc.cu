@@ -820,7 +820,7 @@ cudaError_t launch(const PagedAttnCall& c, const KeyTiles& tiles, const std::vec
             X.part_o = static_cast<float*>(p);
             X.part_lse = reinterpret_cast<float*>(static_cast<char*>(p) + o_bytes);
         }
-        const cuuint64_t dims[3] = {D, kTileKeys, (cuuint64_t)tiles.n * c.hkv}, strides[2] = {D * 2, kTileKeys * D * 2};
+        const cuuint64_t dims[3] = {D, kTileKeys, (cuuint64_t)std::max(1, tiles.n) * c.hkv}, strides[2] = {D * 2, kTileKeys * D * 2};
         const cuuint32_t box[3] = {64, kTileKeys, 1};
         if (!encode_tensor_map(&X.tm_k, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, tiles.k, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B) ||
             !encode_tensor_map(&X.tm_v, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, tiles.v, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B))
@@ -837,7 +837,7 @@ cudaError_t launch(const PagedAttnCall& c, const KeyTiles& tiles, const std::vec
         cfg.dynamicSmemBytes = Tc<D>::kSmem;
         cfg.stream = s;
         cfg.attrs = &at;
-        cfg.numAttrs = b0 == 0;          // (a later part follows other kernels of the call)
+        cfg.numAttrs = b0 == 0 && tiles.n > 0;   // (after another kernel than the tiles' it waits for all of that)
         e = cudaLaunchKernelEx(&cfg, kernel, X);
         if (e == cudaSuccess && units > 0) {
             cfg.gridDim = dim3((unsigned)(units * (kPair / kJoinRows)));

@@ -231,3 +231,32 @@ def test_same_result_twice():
             assert torch.equal(out, first)
     finally:
         c2kv.c2kv_destroy(ctx)
+
+
+@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[1], SHAPES[9]], ids=lambda s: "-".join(map(str, s)))
+def test_window_that_leaves_nothing_out(shape):
+    """Any window from the longest request's rows on, to the largest number, is none."""
+    lens = [(1, 300), (40, 333), (150, 150), (3, 0)]
+    none = _run(*shape, 32, lens)
+    for window in (333, 2 ** 31 - 1):
+        got = _run(*shape, 32, lens, window=window)
+        assert np.array_equal(got[0], none[0]) and np.array_equal(got[1], none[1])
+
+
+@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[1]], ids=lambda s: "-".join(map(str, s)))
+def test_chunk_over_no_rows_after_other_calls(shape):
+    """A chunk whose request has no row: zeros, in its place among the stream's other work."""
+    dtype, fmt, hq, hkv, d = shape
+    rng = np.random.default_rng(5)
+    c2kv, ctx = P.lib(), P.context(dtype, hq, hkv, d)
+    try:
+        pg = P.Paged(rng, dtype, fmt, hkv, d, 16, [400])
+        pg.fill_rows(rng)
+        q = torch.randn((200, hq, d), device="cuda", dtype=torch.bfloat16)
+        out, lse = torch.empty_like(q), torch.empty((hq, 200), device="cuda")
+        for keys in (400, 0, 400, 0):
+            c2kv.c2kv_paged_attend(ctx, pg.pages(), pg.table, [0, 200], [keys], q, out, lse=lse)
+        c2kv.c2kv_sync(ctx)
+        assert not out.any() and torch.isneginf(lse).all()
+    finally:
+        c2kv.c2kv_destroy(ctx)

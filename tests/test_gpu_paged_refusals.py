@@ -149,3 +149,13 @@ def test_binding_refuses_what_it_cannot_describe(setup):
         c2kv.make_pages(pg.k.transpose(2, 3), pg.v.transpose(2, 3), pg.ks, pg.vs)
     with pytest.raises(ValueError):
         c2kv.make_pages(pg.k, pg.v[:2], pg.ks, pg.vs)
+
+
+def test_rows_end_at_2_30(setup):
+    """The kernels count rows in 32 bits: a request past 2^30 is refused, whatever its table names."""
+    c2kv, ctx, pg = setup
+    keep, calls = _calls(c2kv, ctx, pg)
+    wide, far = dict(width=1 << 27, stride=1 << 27), np.array([(1 << 30) + 1, 20], np.int32)
+    for name in CALLS[:2]:
+        assert _status(c2kv, ctx, name, *dict(calls[name], start=far.ctypes.data, **wide).values()) == c2kv.ERR_ARG
+    assert _status(c2kv, ctx, CALLS[2], *dict(calls[CALLS[2]], n_keys=far.ctypes.data, **wide).values()) == c2kv.ERR_ARG
