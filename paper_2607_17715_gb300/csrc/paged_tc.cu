@@ -235,47 +235,60 @@ __device__ __forceinline__ void issue_products(uint32_t tmem, uint32_t sQ, uint3
 // ------------------------------------------------------------------ softmax
 
 // The pair's queries, turned, into their tiles (128-byte swizzle), by the eight softmax warps, 32 rows
-// each: copied as they are, all on their way at once, then turned and made f16 in place, eight rows at a
-// time (a row after the other is a chain of dependent instructions, and took 9000 clocks in all).  A
-// row's largest value goes to [2^14, 2^15): its scores come back by 2^back.
+// each: copied as they are, all on their way at once and before the CTA is set up (fetch), then turned and
+// made f16 in place, eight rows at a time (a row after the other is a chain of dependent instructions).  A
+// row's largest value goes to [2^14, 2^15) before it turns, which keeps it below 2^15.5: its scores come
+// back by 2^back.
+template <int D>
+struct QueryRows {
+    static constexpr int E = D / 64;                     // channels of each half a lane
+    uint64_t turn[E];
+    int pos;                                             // of row `lane`
+};
+
 template <int D, int kReq>
-__device__ __forceinline__ void put_queries(const PagedAttn<kReq>& P, const Item& w, int warp, int lane, uint32_t sQ, int8_t* s_back) {
+__device__ __forceinline__ QueryRows<D> fetch_queries(const PagedAttn<kReq>& P, const Item& w, int warp, int lane, uint32_t sQ) {
     using T = __nv_bfloat16;
     using C = Tc<D>;
     const int G = P.hq / P.hkv;
     const int r0 = warp * 32, n = max(0, min(32, w.live - r0));
     const uint32_t tile = sQ + (r0 / BM) * C::kTile + (r0 % BM) * 128;
-    auto place = [&](int row, int q) { return tile + (uint32_t)((q >> 3) * C::kHalf + row * 128 + (((q & 7) ^ (row & 7)) << 4)); };
-    {
-        // lane i knows where row i lies; a copy takes whole rows, 16 bytes a lane
-        const int row = w.row0 + r0 + min(lane, max(0, n - 1)), tok = row / G;
-        const int64_t at = (w.R.q0 + tok) * P.q_stride + ((int64_t)w.hk * G + row - tok * G) * D;
-        constexpr int kChunks = D / 8, kStep = 32 / kChunks;
-        const int q = lane % kChunks;
-        const T* const base = static_cast<const T*>(P.q) + q * 8;
+    // lane i knows where row i lies; a copy takes whole rows, 16 bytes a lane
+    const int row = w.row0 + r0 + min(lane, max(0, n - 1)), tok = row / G;
+    const int64_t at = (w.R.q0 + tok) * P.q_stride + ((int64_t)w.hk * G + row - tok * G) * D;
+    constexpr int kChunks = D / 8, kStep = 32 / kChunks;
+    const int q = lane % kChunks;
+    const T* const base = static_cast<const T*>(P.q) + q * 8;
 #pragma unroll
-        for (int i0 = 0; i0 < 32; i0 += kStep) {
-            const int i = i0 + lane / kChunks;
-            cp_async16_or_zero(place(i, q), base + __shfl_sync(0xffffffffu, at, i), i < n);   // zero past the rows: a number
-        }
-        cp_async_commit();
+    for (int i0 = 0; i0 < 32; i0 += kStep) {
+        const int i = i0 + lane / kChunks;
+        const uint32_t to = tile + (uint32_t)((q >> 3) * C::kHalf + i * 128 + (((q & 7) ^ (i & 7)) << 4));
+        cp_async16_or_zero(to, base + __shfl_sync(0xffffffffu, at, i), i < n);   // zero past the rows: a number
     }
-    constexpr int E = D / 64, kBatch = 8;                // channels of each half a lane; rows in flight
-    const int c = lane * E, q0 = c >> 3, q1 = (D / 2 + c) >> 3;
-    uint64_t turn[E] = {};
-    int pos_row = 0;
-    float2 cs[E];
+    cp_async_commit();
+    QueryRows<D> k;
+    k.pos = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) cs[e] = make_float2(1.f, 0.f);
+    for (int e = 0; e < k.E; ++e) k.turn[e] = 0;
     if (P.turn && n > 0) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) turn[e] = lane_turn(P.rope.turn, c + e);
-        pos_row = __ldg(P.turn + w.R.q0 + (w.row0 + r0 + min(lane, n - 1)) / G);
+        for (int e = 0; e < k.E; ++e) k.turn[e] = lane_turn(P.rope.turn, lane * k.E + e);
+        k.pos = __ldg(P.turn + w.R.q0 + tok);
     }
-    int pos_cs = __shfl_sync(0xffffffffu, pos_row, 0);
-    if (P.turn)
+    return k;
+}
+
+template <int D, int kReq>
+__device__ __forceinline__ void turn_queries(const PagedAttn<kReq>& P, const QueryRows<D>& k, int warp, int lane, uint32_t sQ, int8_t* s_back) {
+    using C = Tc<D>;
+    constexpr int E = QueryRows<D>::E, kBatch = 8;       // rows in flight
+    const int r0 = warp * 32;
+    const int c = lane * E, q0 = c >> 3, q1 = (D / 2 + c) >> 3;
+    const uint32_t tile = sQ + (r0 / BM) * C::kTile + (r0 % BM) * 128;
+    float2 cs[E];
+    int pos_cs = __shfl_sync(0xffffffffu, k.pos, 0);
 #pragma unroll
-        for (int e = 0; e < E; ++e) cs[e] = turn_cs_fast(turn[e], pos_cs);
+    for (int e = 0; e < E; ++e) cs[e] = turn_cs_fast(k.turn[e], pos_cs);
     cp_async_wait<0>();
     __syncwarp();
 #pragma unroll 1
@@ -296,47 +309,47 @@ __device__ __forceinline__ void put_queries(const PagedAttn<kReq>& P, const Item
                 x1[i] = y1;
             }
         }
-        float lo[kBatch][E], hi[kBatch][E];
+        float f[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
-            const int pos = __shfl_sync(0xffffffffu, pos_row, i0 + i);
-            if (pos != pos_cs) {                         // the heads of a token share its angles
-#pragma unroll
-                for (int e = 0; e < E; ++e) cs[e] = turn_cs_fast(turn[e], pos);
-                pos_cs = pos;
-            }
-            uint32_t top = 0;
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float x = __uint_as_float(e == 0 ? x0[i] << 16 : x0[i] & 0xffff0000u);
-                const float y = __uint_as_float(e == 0 ? x1[i] << 16 : x1[i] & 0xffff0000u);
-                rotate1(x, y, cs[e], lo[i][e], hi[i][e]);
-                if (!P.turn) {
-                    lo[i][e] = x;
-                    hi[i][e] = y;
-                }
-                top = max(top, max(__float_as_uint(lo[i][e]) & 0x7fffffffu, __float_as_uint(hi[i][e]) & 0x7fffffffu));
-            }
-            top = __reduce_max_sync(0xffffffffu, top);
+            const uint32_t m = __vmaxu2(x0[i] & 0x7fff7fffu, x1[i] & 0x7fff7fffu);
+            const uint32_t top = __reduce_max_sync(0xffffffffu, max(m & 0xffff0000u, m << 16));
             const int ex = (int)(top >> 23) - 127;       // zero and non-finite rows stay as they are
             const bool scaled = top < 0x7f800000u && ex > -100;
-            const float f = scaled ? pow2i(14 - ex) : 1.f;
-            if (lane == 0) s_back[r0 + i0 + i] = (int8_t)(scaled ? ex - 14 : 0);
+            f[i] = scaled ? pow2i(14 - ex) : 1.f;
+            if (lane == i) s_back[r0 + i0 + i] = (int8_t)(scaled ? ex - 14 : 0);
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            float x[E], y[E], lo[E], hi[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                lo[i][e] *= f;
-                hi[i][e] *= f;
+                x[e] = __uint_as_float(e == 0 ? x0[i] << 16 : x0[i] & 0xffff0000u) * f[i];
+                y[e] = __uint_as_float(e == 0 ? x1[i] << 16 : x1[i] & 0xffff0000u) * f[i];
+                lo[e] = x[e];
+                hi[e] = y[e];
             }
+            if (P.turn) {
+                const int pos = __shfl_sync(0xffffffffu, k.pos, i0 + i);
+                if (pos != pos_cs) {                     // the heads of a token share its angles
+#pragma unroll
+                    for (int e = 0; e < E; ++e) cs[e] = turn_cs_fast(k.turn[e], pos);
+                    pos_cs = pos;
+                }
+                rotate<E>(x, y, cs, lo, hi);
+            }
+            x0[i] = pack_f16(lo[0], E == 2 ? lo[E - 1] : 0.f);
+            x1[i] = pack_f16(hi[0], E == 2 ? hi[E - 1] : 0.f);
         }
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
             const uint32_t s0 = a0 + i * 128 + (((q0 & 7) ^ i) << 4), s1 = a1 + i * 128 + (((q1 & 7) ^ i) << 4);
             if constexpr (E == 2) {
-                asm volatile("st.shared.u32 [%0], %1;" ::"r"(s0), "r"(pack_f16(lo[i][0], lo[i][1])));
-                asm volatile("st.shared.u32 [%0], %1;" ::"r"(s1), "r"(pack_f16(hi[i][0], hi[i][1])));
+                asm volatile("st.shared.u32 [%0], %1;" ::"r"(s0), "r"(x0[i]));
+                asm volatile("st.shared.u32 [%0], %1;" ::"r"(s1), "r"(x1[i]));
             } else {
-                asm volatile("st.shared.u16 [%0], %1;" ::"r"(s0), "h"((uint16_t)pack_f16(lo[i][0], 0.f)));
-                asm volatile("st.shared.u16 [%0], %1;" ::"r"(s1), "h"((uint16_t)pack_f16(hi[i][0], 0.f)));
+                asm volatile("st.shared.u16 [%0], %1;" ::"r"(s0), "h"((uint16_t)x0[i]));
+                asm volatile("st.shared.u16 [%0], %1;" ::"r"(s1), "h"((uint16_t)x1[i]));
             }
         }
     }
@@ -554,6 +567,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tc_kernel(const __grid_cons
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const Item w = find_item(P);
     const bool has_b = w.live > BM;
+    QueryRows<D> rows;
+    if (warp >= 4) rows = fetch_queries<D>(P, w, warp - 4, lane, sQ);
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::kK; ++s) {
@@ -590,7 +605,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tc_kernel(const __grid_cons
         else if (warp == 0 && lane == 0 && w.n > 0) issue_products<D>(tmem, sQ, sK, sV, bars, w.n, has_b, P.err, abort);
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
-        put_queries<D>(P, w, warp - 4, lane, sQ, s_back);
+        turn_queries<D>(P, rows, warp - 4, lane, sQ, s_back);
         fence_proxy_async();
         asm volatile("bar.sync 1, 256;" ::: "memory");           // (the rows' powers of two)
         mbar_arrive(bar(C::Q));
