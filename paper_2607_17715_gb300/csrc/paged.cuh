@@ -39,6 +39,7 @@ struct PagedMove {
     int32_t batch;
     int32_t b0;              // table row of the launch's first request
     int32_t hkv;
+    float per_hkv;           // 1 / hkv
     int32_t tokens_per_cta;
     int32_t t0;              // first token of this launch
     int32_t t1;              // one past its last

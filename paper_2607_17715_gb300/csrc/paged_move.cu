@@ -71,11 +71,11 @@ __device__ __forceinline__ float2 row_scale(uint32_t top) {
 // N codes of x * inv; inv = 0 (a row kept as zero, or not a number): codes 0.
 template <int N>
 __device__ __forceinline__ void store_codes(void* dst, const float* x, float inv) {
-    uint32_t w[N / 4];
+    uint32_t w[N / 4] = {};
+    if (inv != 0.f)
 #pragma unroll
-    for (int i = 0; i < N / 4; ++i)
-        w[i] = inv == 0.f ? 0u
-                          : to_codes2(x[4 * i] * inv, x[4 * i + 1] * inv) | to_codes2(x[4 * i + 2] * inv, x[4 * i + 3] * inv) << 16;
+        for (int i = 0; i < N / 4; ++i)
+            w[i] = to_codes2(x[4 * i] * inv, x[4 * i + 1] * inv) | to_codes2(x[4 * i + 2] * inv, x[4 * i + 3] * inv) << 16;
     if constexpr (N == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
     else *reinterpret_cast<uint32_t*>(dst) = w[0];
 }
@@ -113,28 +113,14 @@ struct Halves {
     }
 };
 
-// The largest magnitude of a thread's values as bits of fp32: two bf16 at once.
-__device__ __forceinline__ uint32_t top_of(const Halves<__nv_bfloat16>& r) {
-    const uint32_t w[8] = {r.lo.x, r.lo.y, r.lo.z, r.lo.w, r.hi.x, r.hi.y, r.hi.z, r.hi.w};
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
-    return max(m & 0xffff0000u, m << 16);
-}
-__device__ __forceinline__ uint32_t top_of(const Halves<float>& r) {
-    const uint32_t w[8] = {r.lo.x, r.lo.y, r.lo.z, r.lo.w, r.hi.x, r.hi.y, r.hi.z, r.hi.w};
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7fffffffu);
-    return m;
-}
-// The same of turned values, which are numbers if those before the turn (`given`) are.
+// The largest magnitude of a thread's values as bits: NaN if any is (an infinity and a NaN alike make the
+// row's scale one).
 template <int M>
-__device__ __forceinline__ uint32_t top_of_turned(const float* x, uint32_t given) {
+__device__ __forceinline__ uint32_t top_of(const float* x) {
     float m = 0.f;
 #pragma unroll
-    for (int e = 0; e < M; ++e) m = fmaxf(m, fabsf(x[e]));
-    return given >= 0x7f800000u ? given : __float_as_uint(m);
+    for (int e = 0; e < M; e += 2) asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(x[e]), "f"(x[e + 1]));
+    return __float_as_uint(m);
 }
 
 template <typename T, int D, bool kCodes, bool kAppend, int kReq>
@@ -160,7 +146,7 @@ __global__ void __launch_bounds__(kMoveThreads) paged_move_kernel(const __grid_c
         for (int u = 0; u < kU; ++u) {
             const int want = i0 + u * kRows + threadIdx.x / kLanes, i = min(want, n_rows - 1);
             live[u] = want < n_rows;
-            tl[u] = i / P.hkv;
+            tl[u] = (int)(((float)i + 0.5f) * P.per_hkv);      // i / hkv: i is far below 2^20
             h[u] = i - tl[u] * P.hkv;
             dense[u] = (int64_t)tl[u] * P.stride + h[u] * D;
             if (kAppend) {
@@ -229,9 +215,9 @@ __global__ void __launch_bounds__(kMoveThreads) paged_move_kernel(const __grid_c
 #pragma unroll
                     for (int e = 0; e < 2 * N; ++e) x[e] = 0.f;
             };
-            auto put = [&](void* pages, float* scales, T* out, uint32_t top) {
+            auto put = [&](void* pages, float* scales, T* out) {
                 if constexpr (kAppend && kCodes) {
-                    const float2 s = row_scale(row_top<kLanes>(top));
+                    const float2 s = row_scale(row_top<kLanes>(top_of<2 * N>(x)));
                     if (!live[u] || !ok[u]) return;
                     uint8_t* const p = static_cast<uint8_t*>(pages) + at[u];
                     store_codes<N>(p, x, s.y);
@@ -244,7 +230,6 @@ __global__ void __launch_bounds__(kMoveThreads) paged_move_kernel(const __grid_c
                     st16(p + D / 2, Vec16<T>::pack(x + N));
                 }
             };
-            uint32_t top = kAppend && kCodes ? top_of(rk[u]) : 0u;
             row(rk[u], ck[u], sk[u]);
             if (P.turn) {
                 float lo[N], hi[N];
@@ -254,12 +239,10 @@ __global__ void __launch_bounds__(kMoveThreads) paged_move_kernel(const __grid_c
                     x[e] = lo[e];
                     x[N + e] = hi[e];
                 }
-                if (kAppend && kCodes) top = top_of_turned<2 * N>(x, top);
             }
-            put(P.pg.k, P.pg.k_scale, dense_k, top);
-            top = kAppend && kCodes ? top_of(rv[u]) : 0u;
+            put(P.pg.k, P.pg.k_scale, dense_k);
             row(rv[u], cv[u], sv[u]);
-            put(P.pg.v, P.pg.v_scale, dense_v, top);
+            put(P.pg.v, P.pg.v_scale, dense_v);
         }
         if (i0 + kU * kRows < n_rows) rows_of(i0 + kU * kRows);
     }
@@ -280,6 +263,7 @@ cudaError_t launch_move(const PagedMoveCall& c, cudaStream_t s) {
         P.batch = nb;
         P.b0 = b0;
         P.hkv = c.hkv;
+        P.per_hkv = 1.0f / (float)c.hkv;
         P.t0 = c.ptr[b0];
         P.t1 = c.ptr[b0 + nb];
         const int tokens = P.t1 - P.t0;
