@@ -8,7 +8,8 @@
 // weights and E4M3 rows, and all 8 of bf16 values down to 2^-25 of their tile's largest.  What f16 lacks
 // in range the powers of two hold.
 //
-// Bytes bound it: a page's read once, two written for each value.
+// Bytes bound it: a page's read once, two written for each value.  Measured: 32768 rows of codes of 8 heads,
+// 67 MB to 134 MB, in 38 us (5.3 TB/s).
 #include "paged.cuh"
 #include "ptx.cuh"
 #include "vec16.cuh"

@@ -6,6 +6,12 @@
 // kU rows at once, so the turn needs no exchange and 64 kU bytes a thread are on their way.  A CTA takes
 // several tokens with all their heads: their pages are looked up and their angles formed once a token, in
 // shared memory, while the first rows are on their way.
+//
+// Bytes bound it, and for a token or two the launch.  Measured: 16 requests' contexts read back, 480 MB in
+// 76 us (6.3 TB/s); prompts of eight requests appended as codes, 138 MB in 31 us (4.4 TB/s: the CTAs are
+// short, and their chain position -> angle -> turn -> largest value is a fifth of it; without a turn 27,
+// with 16-bit pages, half as many bytes more, 32).  Angles formed by each thread for itself, with no shared
+// memory between, took 38; more passes a CTA 34; more CTAs an SM with fewer registers 36.
 #include "paged.cuh"
 #include "per_device.cuh"
 #include "rope.cuh"
@@ -21,7 +27,7 @@ constexpr int kMoveThreads = 128;
 constexpr int kMaxTokens = 32;          // tokens of a CTA (angles: 32 x 64 x 8 bytes)
 // Rows of a thread on their way at once: two of what is read back; one of what is appended, whose maxima
 // and turns need the registers (16 requests' contexts read back: 76 us with two, 84 with one; prompts
-// appended: 44 and 35).
+// appended: 34 and 32).
 __host__ __device__ constexpr int rows_at_once(bool append) { return append ? 1 : 2; }
 constexpr int kMovePasses = 2;          // passes of a CTA
 
