@@ -8,10 +8,12 @@
 // shared memory, while the first rows are on their way.
 //
 // Bytes bound it, and for a token or two the launch.  Measured: 16 requests' contexts read back, 480 MB in
-// 76 us (6.3 TB/s); prompts of eight requests appended as codes, 138 MB in 31 us (4.4 TB/s: the CTAs are
+// 76 us (6.3 TB/s); prompts of eight requests appended as codes, 138 MB in 32 us (4.3 TB/s: the CTAs are
 // short, and their chain position -> angle -> turn -> largest value is a fifth of it; without a turn 27,
-// with 16-bit pages, half as many bytes more, 32).  Angles formed by each thread for itself, with no shared
-// memory between, took 38; more passes a CTA 34; more CTAs an SM with fewer registers 36.
+// with 16-bit pages, a third more bytes, 32).  Angles formed by each thread for itself, with no shared
+// memory between, took 38; more passes a CTA 34; more CTAs an SM with fewer registers 36.  The
+// special-function unit's sine and cosine save half a microsecond and move codes that lie near the middle
+// between two: angles are fp32's.
 #include "paged.cuh"
 #include "per_device.cuh"
 #include "rope.cuh"
@@ -172,10 +174,8 @@ __global__ void __launch_bounds__(kMoveThreads) paged_move_kernel(const __grid_c
     }
     if (P.turn)
         for (int a = threadIdx.x; a < nt * (D / 2); a += kMoveThreads) {
-            // (codes keep 4 bits: the special-function unit's angles are exact to them)
             const uint64_t turn = lane_turn(P.rope.turn, a % (D / 2));
-            const int pos = __ldg(P.turn + t0 + a / (D / 2));
-            s_cs[a] = kAppend && kCodes ? turn_cs_fast(turn, pos) : turn_cs(turn, pos);
+            s_cs[a] = turn_cs(turn, __ldg(P.turn + t0 + a / (D / 2)));
         }
     __syncthreads();
     // every thread of the CTA makes the same passes (the rows' maxima are exchanged)

@@ -233,3 +233,27 @@ def test_a_stream_of_ones_own():
         assert torch.equal(ko, x) and torch.equal(vo, x)
     finally:
         c2kv.c2kv_destroy(ctx)
+
+
+def test_turned_codes_are_those_of_fp32_angles():
+    """A code differs from the nearest one only where the turned value is within fp32's error of the middle
+    between two: the angle's argument is rounded to fp32 (pi 2^-24), its sine and cosine to 2 units, and the
+    two products and their sum once each, together below 2^-21 of the pair; the scale's inverse and its
+    product below 2^-22 of the value."""
+    rng = np.random.default_rng(12)
+    c2kv, ctx = P.lib(), P.context("bf16", 8, 8, 128, THETA)
+    try:
+        n = 1000
+        pg = P.Paged(rng, "bf16", "e4m3", 8, 128, 64, [n])
+        k, k64 = _rows(rng, "bf16", n, 8, 128)
+        pos = rng.integers(0, 100000, n).astype(np.int32)
+        c2kv.c2kv_paged_append(ctx, pg.pages(), pg.table, [0, n], [0], k, k, turn=torch.from_numpy(pos).cuda())
+        c2kv.c2kv_sync(ctx)
+        x = orc.turned(k64, pos, THETA)
+        codes = orc.rows_of(pg.k.float().cpu().numpy().astype(np.float64), pg.table_np, 0, 0, n, 64)
+        scale = np.stack([pg.ks.cpu().numpy().astype(np.float64)[pg.table_np[0, j // 64], :, j % 64] for j in range(n)])[..., None]
+        y = x / scale
+        step = 2.0 ** (np.floor(np.log2(np.maximum(np.abs(codes), 2.0 ** -6))) - 3)
+        assert np.all(np.abs(codes - y) <= 0.5 * step + 2.0 ** -21 * _pair(k64) / scale + 2.0 ** -22 * np.abs(y))
+    finally:
+        c2kv.c2kv_destroy(ctx)
