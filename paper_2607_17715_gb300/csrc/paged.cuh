@@ -119,6 +119,8 @@ struct PagedAttnCall {
 cudaError_t launch_paged_attn(const PagedAttnCall& c, int dtype, int d, bool codes, cudaStream_t s);
 // fp32 queries of n requests on the CUDA cores (paged_simt.cu).
 cudaError_t launch_paged_simt(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
+// The same of few rows a request (paged_lane.cu).
+cudaError_t launch_paged_lane(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
 // bf16 queries of n requests on mma.sync (paged_mma.cu).
 cudaError_t launch_paged_mma(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
 

@@ -15,6 +15,16 @@ namespace {
 // 56 / 66, 47 / 60 and 75 / 61, 19 / 27 and 30 / 27.
 constexpr int kMmaRows = 64;
 
+// The same of fp32 contexts, and the keys that some request has to see for it: the lanes' kernel reads keys
+// again for every 4 rows, the register-tiled loop works on 16 rows or, below that, leaves most of its lanes
+// to wait.  Measured (us, lanes / tiles; 16-bit pages as good as 8-bit ones).  32 / 8 heads of 128 channels, 4
+// and 16 rows: 27 requests of 1381 keys 66 / 94 and 186 / 241, one of 30000 49 / 247 and 145 / 368, 16 of 9000
+// 191 / 403 and 703 / 909; 24 rows of 8 requests of 700 keys 75 / 63.  8 / 8 heads of 64, 4 and 8 rows: 42 / 54
+// and 67 / 77, 38 / 151 and 59 / 191, 135 / 182 and 295 / 277.  One request of 200 keys, any: 13 / 12, and four
+// of 300: 14 / 15.
+constexpr int lane_rows(int d) { return d == 128 ? 16 : 4; }
+constexpr int kLaneKeys = 256;
+
 // Requests of many rows on tcgen05: what they see of their pages becomes key tiles first, in scratch that
 // the stream hands back; requests go in groups so that the scratch stays small beside the cache.
 constexpr int64_t kTileBytes = (int64_t)512 << 20;
@@ -75,11 +85,26 @@ cudaError_t launch_paged_attn(const PagedAttnCall& c, int dtype, int d, bool cod
     req.reserve(c.batch);
     for (int r = 0; r < c.batch; ++r)
         if (c.ptr[r + 1] > c.ptr[r]) req.push_back(PagedReq{c.ptr[r], c.ptr[r + 1] - c.ptr[r], c.n_keys[r], r, 0, 1, 0, 0, 0, 0});
-    if (dtype == kDtypeF32) return launch_paged_simt(c, req.data(), (int)req.size(), d, codes, s);
-    // requests of many rows on tcgen05, those of few on mma.sync
     std::vector<PagedReq> few, many;
-    for (const PagedReq& q : req) ((int64_t)q.nq * (c.hq / c.hkv) > kMmaRows ? many : few).push_back(q);
+    auto part = [&](int64_t rows) {
+        for (const PagedReq& q : req) ((int64_t)q.nq * (c.hq / c.hkv) > rows ? many : few).push_back(q);
+    };
     cudaError_t e = cudaSuccess;
+    if (dtype == kDtypeF32) {    // CUDA cores: a register-tiled loop, or lanes that share a key
+        part(lane_rows(d));
+        const bool seen = std::any_of(few.begin(), few.end(), [&](const PagedReq& q) {
+            return q.n_keys > kLaneKeys && (!c.window || (int64_t)c.window + q.nq > kLaneKeys);
+        });
+        if (!seen) {
+            many = req;
+            few.clear();
+        }
+        if (!many.empty()) e = launch_paged_simt(c, many.data(), (int)many.size(), d, codes, s);
+        if (e == cudaSuccess && !few.empty()) e = launch_paged_lane(c, few.data(), (int)few.size(), d, codes, s);
+        return e;
+    }
+    part(kMmaRows);
+    // requests of many rows on tcgen05, those of few on mma.sync
     if (!many.empty()) e = launch_many(c, many.data(), (int)many.size(), d, codes, s);
     if (e == cudaSuccess && !few.empty()) e = launch_paged_mma(c, few.data(), (int)few.size(), d, codes, s);
     return e;

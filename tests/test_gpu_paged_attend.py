@@ -260,3 +260,33 @@ def test_chunk_over_no_rows_after_other_calls(shape):
         assert not out.any() and torch.isneginf(lse).all()
     finally:
         c2kv.c2kv_destroy(ctx)
+
+
+FEW_F32 = [("f32", "native", 16, 4, 64), ("f32", "e4m3", 8, 8, 64), ("f32", "native", 4, 4, 128), ("f32", "e4m3", 16, 4, 128),
+           ("f32", "native", 6, 2, 128)]
+
+
+@pytest.mark.parametrize("window", [0, 1, 270, 400])
+@pytest.mark.parametrize("lens", [[(1, 300)], [(1, 1200), (0, 400), (1, 0), (1, 1), (2, 40), (3, 257), (1, 32), (1, 999)], [(4, 5003), (1, 700)],
+                                  [(1, 260 + 9 * i) for i in range(70)]], ids=["one", "ragged", "long", "many"])
+@pytest.mark.parametrize("shape", FEW_F32, ids=lambda s: "-".join(map(str, s)))
+def test_few_rows_of_fp32(shape, lens, window):
+    """Tokens over more keys than the register-tiled loop is for, next to short and empty requests."""
+    _check(_run(*shape, 16, lens, window=window), shape[0])
+
+
+@pytest.mark.parametrize("shape", FEW_F32, ids=lambda s: "-".join(map(str, s)))
+def test_few_rows_of_fp32_beside_values_that_are_not_finite(shape):
+    """The last two of 700 rows: the first two of four queries see neither, the last sees both."""
+    def edit(pg):
+        for key, bad in ((699, float("nan")), (698, float("inf"))):
+            page, at = int(pg.table_np[0, key // 32]), key % 32
+            if pg.ks is None:
+                pg.k[page, :, at, 3] = bad
+                pg.v[page, :, at, 5] = bad
+            else:
+                pg.ks[page, :, at] = float("nan")
+                pg.vs[page, :, at] = float("nan")
+    out, lse, want, want_l = _run(*shape, 32, [(4, 700)], edit=edit)
+    assert np.isfinite(out[:2]).all() and np.isnan(out[3]).all()
+    _check((out[:2], lse[:, :2], want[:2], want_l[:, :2]), shape[0])
