@@ -11,7 +11,7 @@
 // Issue bounds it (a key takes 2 D / 8 multiply-adds a row and lane, and half as much around them), at half
 // of its rate with the two warps a scheduler that registers leave.  Measured, 32 / 8 heads of 128 channels,
 // E4M3 pages: one token over 30000 rows 49 us, 16 requests' over 9000 rows 191 (the bytes alone: 45), 27
-// requests' over 1381 66.  A key at a time (and one row after the other) took 223 of the 191.
+// requests' over 1381 66.  With one group of keys at a time, rows one after the other, the 191 were 223.
 #include "paged.cuh"
 #include "per_device.cuh"
 #include "ptx.cuh"
