@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(kLaneThreads, lane_ctas(D)) paged_lane_kernel(
         const int key = b * kLaneBlk + lane;
         int page = -1;
         if (b < b1 && key >= k_lo && key < k_hi) {
-            page = __ldg(table + (key >> P.pg.page_shift));
+            page = ld_after(table + (key >> P.pg.page_shift));
             if (page < 0 || page >= P.pg.n_pages) {
                 atomicOr(P.err, 1);
                 page = -1;
@@ -141,6 +141,7 @@ __global__ void __launch_bounds__(kLaneThreads, lane_ctas(D)) paged_lane_kernel(
         }
         return page;
     };
+    after_kernels_before();
     uint8_t* const ring = ring_bytes + warp * kDepth * Ring::kGroup;
     const int mine = b0 + warp < b1 ? (b1 - b0 - warp + kLaneWarps - 1) / kLaneWarps * kGroups : 0;   // the warp's groups of four keys
     int pages = pages_of(b0 + warp), pages_next = pages_of(b0 + warp + kLaneWarps);
@@ -181,7 +182,7 @@ __global__ void __launch_bounds__(kLaneThreads, lane_ctas(D)) paged_lane_kernel(
         float lo = q[0], hi = q[D / 2];
         if (P.turn) {
             const float x = lo, y = hi;
-            rotate1(x, y, turn_cs(lane_turn(P.rope.turn, c), __ldg(P.turn + tok)), lo, hi);
+            rotate1(x, y, turn_cs(lane_turn(P.rope.turn, c), ld_after(P.turn + tok)), lo, hi);
         }
         s_q[k / (D / 2)][c] = lo;
         s_q[k / (D / 2)][c + D / 2] = hi;
@@ -426,8 +427,7 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
             X.part_o = static_cast<float*>(p);
             X.part_lse = reinterpret_cast<float*>(static_cast<char*>(p) + o_bytes);
         }
-        kernel<<<(unsigned)items, kLaneThreads, kSmem, s>>>(X);
-        e = cudaGetLastError();
+        e = launch_overlapped(kernel, (unsigned)items, kLaneThreads, kSmem, s, X);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;

@@ -218,6 +218,7 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
         s_bad = 0;
     }
 
+    after_kernels_before();
     // the warp's query rows, on their way before the keys are: behind a ring's worth of tiles they took 4 us
     constexpr int C = D / 64, kMine = (kRows + kWarps - 1) / kWarps;   // channels of each half a lane; rows a warp
     uint32_t q_raw[kMine][2];
@@ -228,10 +229,10 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
         const T* q = static_cast<const T*>(P.q) + (int64_t)(R.q0 + tok) * P.q_stride + (int64_t)(hk * G + rr - tok * G) * D + lane * C;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            if constexpr (C == 2) q_raw[i][half] = __ldg(reinterpret_cast<const uint32_t*>(q + half * (D / 2)));
-            else q_raw[i][half] = __ldg(reinterpret_cast<const uint16_t*>(q + half * (D / 2)));
+            if constexpr (C == 2) q_raw[i][half] = ld_after(reinterpret_cast<const uint32_t*>(q + half * (D / 2)));
+            else q_raw[i][half] = ld_after(reinterpret_cast<const uint16_t*>(q + half * (D / 2)));
         }
-        q_pos[i] = P.turn ? __ldg(P.turn + R.q0 + tok) : 0;
+        q_pos[i] = P.turn ? ld_after(P.turn + R.q0 + tok) : 0;
     }
     uint64_t turn[C] = {};
     if (P.turn) {
@@ -252,8 +253,8 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
         const int key = (b0 + warp + (i0 + lane) * kWarps) * kBlk;
         // (a page that a window has left behind may be gone from the table)
         const bool one = boxes == 1 || key + 16 > k_lo, two = boxes == 2 && key + 16 < k_hi;
-        if (one) pages0 = __ldg(table + (key >> P.pg.page_shift));
-        if (two) pages1 = __ldg(table + ((key + 16) >> P.pg.page_shift));
+        if (one) pages0 = ld_after(table + (key >> P.pg.page_shift));
+        if (two) pages1 = ld_after(table + ((key + 16) >> P.pg.page_shift));
         if (one && (pages0 < 0 || pages0 >= P.pg.n_pages)) {
             atomicOr(P.err, 1);
             pages0 = -1;
@@ -809,8 +810,7 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
         if (!encode_page_map(&X.tm_k, c.pg.k, c.pg, c.hkv, D, kCodes, L::BC, X.box_rows, swizzle) ||
             !encode_page_map(&X.tm_v, c.pg.v, c.pg, c.hkv, D, kCodes, L::BC, X.box_rows, swizzle))
             return cudaErrorInvalidValue;
-        kernel<<<(unsigned)items, kWarps * 32, L::kSmem, s>>>(X);
-        e = cudaGetLastError();
+        e = launch_overlapped(kernel, (unsigned)items, kWarps * 32, L::kSmem, s, X);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;

@@ -90,8 +90,8 @@ __device__ __forceinline__ void store_codes(void* dst, const float* x, float inv
 
 template <int N>
 __device__ __forceinline__ uint2 ld_codes(const void* src) {
-    if constexpr (N == 8) return __ldg(reinterpret_cast<const uint2*>(src));
-    else return make_uint2(__ldg(reinterpret_cast<const uint32_t*>(src)), 0u);
+    if constexpr (N == 8) return ld_after(reinterpret_cast<const uint2*>(src));
+    else return make_uint2(ld_after(reinterpret_cast<const uint32_t*>(src)), 0u);
 }
 
 template <int N>
@@ -112,8 +112,8 @@ template <typename T>
 struct Halves {
     uint4 lo, hi;
     __device__ __forceinline__ void load(const T* p, int half) {
-        lo = ld16(p);
-        hi = ld16(p + half);
+        lo = ld_after(reinterpret_cast<const uint4*>(p));
+        hi = ld_after(reinterpret_cast<const uint4*>(p + half));
     }
     __device__ __forceinline__ void unpack(float* x) const {
         Vec16<T>::unpack(lo, x);
@@ -163,10 +163,11 @@ __global__ void __launch_bounds__(kMoveThreads) paged_move_kernel(const __grid_c
             }
         }
     };
+    after_kernels_before();
     rows_of(0);
     if (threadIdx.x < nt) {                           // one token a thread: its request, row and page
         const int t = t0 + threadIdx.x, r = find_request(P, t), row = P.start[r] + (t - P.ptr[r]);
-        const int page = __ldg(P.pg.table + (int64_t)(P.b0 + r) * P.pg.table_stride + (row >> P.pg.page_shift));
+        const int page = ld_after(P.pg.table + (int64_t)(P.b0 + r) * P.pg.table_stride + (row >> P.pg.page_shift));
         const bool ok = page >= 0 && page < P.pg.n_pages;
         if (!ok) atomicOr(P.err, 1);
         s_at[threadIdx.x] = ok ? page * P.pg.page_stride + (int64_t)(row & (size - 1)) * D : -1;
@@ -175,7 +176,7 @@ __global__ void __launch_bounds__(kMoveThreads) paged_move_kernel(const __grid_c
     if (P.turn)
         for (int a = threadIdx.x; a < nt * (D / 2); a += kMoveThreads) {
             const uint64_t turn = lane_turn(P.rope.turn, a % (D / 2));
-            s_cs[a] = turn_cs(turn, __ldg(P.turn + t0 + a / (D / 2)));
+            s_cs[a] = turn_cs(turn, ld_after(P.turn + t0 + a / (D / 2)));
         }
     __syncthreads();
     // every thread of the CTA makes the same passes (the rows' maxima are exchanged)
@@ -199,8 +200,8 @@ __global__ void __launch_bounds__(kMoveThreads) paged_move_kernel(const __grid_c
                     ck[u][1] = ld_codes<N>(pk + D / 2);
                     cv[u][0] = ld_codes<N>(pv);
                     cv[u][1] = ld_codes<N>(pv + D / 2);
-                    sk[u] = __ldg(P.pg.k_scale + sat[u]);
-                    sv[u] = __ldg(P.pg.v_scale + sat[u]);
+                    sk[u] = ld_after(P.pg.k_scale + sat[u]);
+                    sv[u] = ld_after(P.pg.v_scale + sat[u]);
                 } else {
                     rk[u].load(static_cast<const T*>(P.pg.k) + at[u], D / 2);
                     rv[u].load(static_cast<const T*>(P.pg.v) + at[u], D / 2);
@@ -281,8 +282,8 @@ cudaError_t launch_move(const PagedMoveCall& c, cudaStream_t s) {
         for (int i = 0; i <= nb; ++i) P.ptr[i] = c.ptr[b0 + i];
         for (int i = 0; i < nb; ++i) P.start[i] = c.start[b0 + i];
         const int ctas = (tokens + P.tokens_per_cta - 1) / P.tokens_per_cta;
-        paged_move_kernel<T, D, kCodes, kAppend, kReq><<<ctas, kMoveThreads, 0, s>>>(P);
-        const cudaError_t e = cudaGetLastError();
+        // (a few tokens: the host takes longer to launch it than the device to run it)
+        const cudaError_t e = launch_overlapped(paged_move_kernel<T, D, kCodes, kAppend, kReq>, ctas, kMoveThreads, 0, s, P, P.tokens_per_cta > 1);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;

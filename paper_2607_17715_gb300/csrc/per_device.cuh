@@ -52,5 +52,31 @@ inline cudaError_t opt_in_smem(PerDevice<cudaError_t>& kept, const void* kernel,
     return kept.get([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); });
 }
 
+// Launches `kernel` so that its CTAs may be set up while the kernel before it in the stream ends: it has to
+// wait (after_kernels_before) ahead of its first access to memory that others write or read.  That saves the
+// device 1.5 to 2.5 us a launch and costs the host 0.5; `overlap` false: a launch like any other.
+template <class Params>
+inline cudaError_t launch_overlapped(void (*kernel)(Params), dim3 grid, unsigned threads, size_t smem, cudaStream_t s, const Params& params, bool overlap = true) {
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = &at;
+    cfg.numAttrs = overlap ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, params);
+}
+
+// The kernels before this one in the stream have ended and what they wrote is visible.
+__device__ __forceinline__ void after_kernels_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// An ordinary load: one that says that its memory never changes (__ldg) may be moved ahead of that wait.
+template <class T>
+__device__ __forceinline__ T ld_after(const T* p) {
+    return *p;
+}
+
 }  // namespace
 }  // namespace c2kv

@@ -91,10 +91,10 @@ __device__ __forceinline__ void load_chunk(const Row& w, int i, int b, int lane,
     if (wide) {
         float4 x[4], y[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) x[u] = __ldg(reinterpret_cast<const float4*>(w.p + i + 128 * u) + lane);
+        for (int u = 0; u < 4; ++u) x[u] = ld_after(reinterpret_cast<const float4*>(w.p + i + 128 * u) + lane);
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-            y[u] = w.q ? __ldg(reinterpret_cast<const float4*>(w.q + i + 128 * u) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+            y[u] = w.q ? ld_after(reinterpret_cast<const float4*>(w.q + i + 128 * u) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             v[4 * u] = x[u].x - y[u].x;
@@ -106,7 +106,7 @@ __device__ __forceinline__ void load_chunk(const Row& w, int i, int b, int lane,
 #pragma unroll
         for (int u = 0; u < 16; ++u) {
             const int e = kInOrder ? i + 128 * (u / 4) + 4 * lane + u % 4 : i + 32 * u + lane;
-            v[u] = e < b && e != w.drop ? __ldg(w.p + e) - (w.q ? __ldg(w.q + e) : 0.f) : 0.f;
+            v[u] = e < b && e != w.drop ? ld_after(w.p + e) - (w.q ? ld_after(w.q + e) : 0.f) : 0.f;
         }
         return;
     }
@@ -177,19 +177,20 @@ __global__ void __launch_bounds__(kVerThreads, 2) verify_kernel(const __grid_con
     const int r = blockIdx.x / n_cta, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int lo = P.ptr[r], n = P.ptr[r + 1] - lo, V = P.vocab;
     const int64_t p_row = (int64_t)lo + P.b0 + r;         // the request's first row of p
+    after_kernels_before();
     if (warp == 0) {
         int a = 0;
         for (; a < n; a += 32) {
             bool yes = true;
             if (a + lane < n) {
-                const int x = __ldg(P.tokens + lo + a + lane);
+                const int x = ld_after(P.tokens + lo + a + lane);
                 yes = x >= 0 && x < V;
                 if (!yes) {
                     if (rank == 0) atomicOr(P.err, 1);
                 } else {
-                    const float px = __ldg(P.p + (p_row + a + lane) * P.p_stride + x);
-                    const float qx = P.q ? __ldg(P.q + (int64_t)(lo + a + lane) * P.q_stride + x) : 1.f;
-                    yes = __fmul_rn(__ldg(P.u_accept + lo + a + lane), qx) < px;
+                    const float px = ld_after(P.p + (p_row + a + lane) * P.p_stride + x);
+                    const float qx = P.q ? ld_after(P.q + (int64_t)(lo + a + lane) * P.q_stride + x) : 1.f;
+                    yes = __fmul_rn(ld_after(P.u_accept + lo + a + lane), qx) < px;
                 }
             }
             const uint32_t no = __ballot_sync(0xffffffffu, !yes);
@@ -205,7 +206,7 @@ __global__ void __launch_bounds__(kVerThreads, 2) verify_kernel(const __grid_con
     Row w{P.p + (p_row + acc) * P.p_stride, nullptr, -1};
     if (acc < n) {
         if (P.q) w.q = P.q + (int64_t)(lo + acc) * P.q_stride;
-        else w.drop = __ldg(P.tokens + lo + acc);
+        else w.drop = ld_after(P.tokens + lo + acc);
     }
     // warps of the cluster take stretches of whole 32-element lines, in order
     const int warps = kVerWarps * (int)n_cta;
@@ -239,7 +240,7 @@ __global__ void __launch_bounds__(kVerThreads, 2) verify_kernel(const __grid_con
         if (total == 0) P.next_token[P.b0 + r] = -1;
     }
     if (total == 0) return;
-    const float uf = __ldg(P.u_next + P.b0 + r) * 0x1p24f;
+    const float uf = ld_after(P.u_next + P.b0 + r) * 0x1p24f;
     const uint64_t u = min((uint64_t)__float2ull_rz(fmaxf(uf, 0.f)), (uint64_t)0xffffff);
     const uint64_t goal = (total >> 24) * u + (((total & 0xffffff) * u) >> 24);
     for (int i = 0; i < warp; ++i) before += s_warp[i];
@@ -269,14 +270,16 @@ cudaError_t launch(const VerifyCall& c, cudaStream_t s) {
         P.b0 = b0;
         for (int i = 0; i <= nb; ++i) P.ptr[i] = c.ptr[b0 + i];
         cudaLaunchConfig_t cfg{};
-        cudaLaunchAttribute at{};
-        at.id = cudaLaunchAttributeClusterDimension;
-        at.val.clusterDim = {(unsigned)size, 1, 1};
+        cudaLaunchAttribute at[2] = {};
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim = {(unsigned)size, 1, 1};
+        at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[1].val.programmaticStreamSerializationAllowed = 1;
         cfg.gridDim = dim3(nb * size);
         cfg.blockDim = dim3(kVerThreads);
         cfg.stream = s;
-        cfg.attrs = &at;
-        cfg.numAttrs = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 2;
         const cudaError_t e = cudaLaunchKernelEx(&cfg, verify_kernel<kReq>, P);
         if (e != cudaSuccess) return e;
     }
