@@ -8,10 +8,10 @@
 // shared memory, while the first rows are on their way.
 //
 // Bytes bound it, and for a token or two the launch.  Measured: 16 requests' contexts read back, 480 MB in
-// 76 us (6.3 TB/s); prompts of eight requests appended as codes, 138 MB in 32 us (4.3 TB/s: the CTAs are
-// short, and their chain position -> angle -> turn -> largest value is a fifth of it; without a turn 27,
-// with 16-bit pages, a third more bytes, 32).  Angles formed by each thread for itself, with no shared
-// memory between, took 38; more passes a CTA 34; more CTAs an SM with fewer registers 36.  The
+// 73 us (6.6 TB/s); prompts of eight requests appended as codes, 138 MB in 29 us (4.7 TB/s: the CTAs are
+// short, and their chain position -> angle -> turn -> largest value is a fifth of it; launched
+// with no overlap 32, without a turn 27, with 16-bit pages, a third more bytes, 32).  Angles formed by each thread for itself, with no shared
+// memory between, took 38 of the 32; more passes a CTA 34; more CTAs an SM with fewer registers 36.  The
 // special-function unit's sine and cosine save half a microsecond and move codes that lie near the middle
 // between two: angles are fp32's.
 #include "paged.cuh"
