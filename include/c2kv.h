@@ -450,7 +450,7 @@ typedef struct c2kv_pages {
  *   turn         : device int32 [T], or NULL.
  * A page number outside [0, n_pages) is refused by the kernel: the row is not written, and
  * c2kv_sync returns ERR_DEVICE_BOUNDS.  Recorded by the trace as C2KV_PROF_SUFFIX.
- * Errors: ERR_ARG, ERR_DTYPE (page format), ERR_CUDA.
+ * Errors: ERR_ARG, ERR_DTYPE (page format), ERR_NOMEM, ERR_CUDA.
  */
 c2kv_status c2kv_paged_append(c2kv_ctx* ctx, const c2kv_pages* pages, int32_t batch, const int32_t* table,
                               int32_t table_width, int64_t table_stride, const int32_t* new_ptr,
@@ -516,7 +516,7 @@ c2kv_status c2kv_paged_attend(c2kv_ctx* ctx, const c2kv_pages* pages, int32_t ba
  *                  probabilities (q = 1 at the token, 0 elsewhere).
  *   u_accept     : device fp32 [T] in [0, 1);  u_next : device fp32 [B] in [0, 1).
  *   n_accepted, next_token : device int32 [B].
- * Not recorded by the trace.  Errors: ERR_ARG, ERR_CUDA.
+ * Not recorded by the trace.  Errors: ERR_ARG, ERR_NOMEM, ERR_CUDA.
  */
 c2kv_status c2kv_verify_drafts(c2kv_ctx* ctx, int32_t batch, const int32_t* draft_ptr, int32_t vocab,
                                const int32_t* tokens, const float* p, int64_t p_stride, const float* q,

@@ -650,7 +650,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
     for (int row = threadIdx.x; row < live; row += kJoinThreads) {
         float top = -CUDART_INF_F, sum = 0.f;
         for (int k = 0; k < S; ++k) {
-            const float e = __ldcg(X.part_lse + (item0 + (int64_t)k * P.hkv) * kPair + first + row);
+            const float e = ld_after_l2(X.part_lse + (item0 + (int64_t)k * P.hkv) * kPair + first + row);
             weight[k * kJoinRows + row] = e;
             top = fmaxf(top, e);
         }
@@ -673,7 +673,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
         const float* const from = X.part_o + ((item0 + (int64_t)k * P.hkv) * kPair + first) * D + 4 * f;
         float4 y[kRows];
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) y[i] = __ldcg(reinterpret_cast<const float4*>(from + (int64_t)min(row0 + i * kStep, live - 1) * D));
+        for (int i = 0; i < kRows; ++i) y[i] = ld_after_l2(reinterpret_cast<const float4*>(from + (int64_t)min(row0 + i * kStep, live - 1) * D));
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
             const float a = weight[k * kJoinRows + min(row0 + i * kStep, live - 1)];

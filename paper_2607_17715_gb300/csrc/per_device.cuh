@@ -77,6 +77,17 @@ template <class T>
 __device__ __forceinline__ T ld_after(const T* p) {
     return *p;
 }
+// The same from L2, for what other SMs wrote.
+__device__ __forceinline__ float ld_after_l2(const float* p) {
+    float v;
+    asm volatile("ld.global.cg.f32 %0, [%1];" : "=f"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 ld_after_l2(const float4* p) {
+    float4 v;
+    asm volatile("ld.global.cg.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p) : "memory");
+    return v;
+}
 
 }  // namespace
 }  // namespace c2kv
