@@ -418,6 +418,10 @@ c2kv_status c2kv_extract_attention(c2kv_ctx* ctx, int32_t n_layers, const void* 
  *
  * The pages and their scales are laid out head by head, so that one head's rows of a page are one
  * run; a page may lie anywhere (page_stride), in an allocation that holds other layers' pages too.
+ *
+ * The paged calls may be captured in a CUDA graph.  Their host arrays are read when the call is made,
+ * so a graph holds one step; its scratch is the graph's own, which later calls leave alone and which
+ * other streams may run beside.  The graph must not outlive the context.
  */
 #define C2KV_PAGES_NATIVE 0
 #define C2KV_PAGES_E4M3   1

@@ -73,7 +73,8 @@ struct c2kv_ctx {
     // launches (each unit's last split sets its counter back), cleared again after a device error
     uint32_t* tickets = nullptr;
     size_t tickets_cap = 0;
-    // scratch of the paged calls, one for each stream that they ran on (grown rarely)
+    // scratch of the paged calls, one for each stream that they ran on (grown rarely; a call that a
+    // graph captures takes its own instead)
     struct Workspace {
         cudaStream_t stream = nullptr;
         void* p = nullptr;
@@ -1832,7 +1833,9 @@ bool context_view(const c2kv_ctx* c, ContextView* v) {
 cudaError_t context_alloc(c2kv_ctx* c, void** p, size_t bytes) { return pool_alloc(c, p, bytes); }
 void context_free(c2kv_ctx* c, void* p) { pool_free(c, p); }
 
-cudaError_t context_workspace(c2kv_ctx* c, size_t bytes, size_t counters, void** p, uint32_t** cnt) {
+namespace {
+
+cudaError_t kept_workspace(c2kv_ctx* c, size_t bytes, size_t counters, void** p, uint32_t** cnt) {
     auto w = std::find_if(c->workspaces.begin(), c->workspaces.end(),
                           [&](const c2kv_ctx::Workspace& x) { return x.stream == c->stream; });
     if (w == c->workspaces.end()) {
@@ -1870,6 +1873,28 @@ cudaError_t context_workspace(c2kv_ctx* c, size_t bytes, size_t counters, void**
     *cnt = w->counters;
     return e;
 }
+
+}  // namespace
+
+// A captured launch keeps its pointers for as long as its graph lives, and may run on any stream: what it
+// works in is allocated, cleared and freed by the graph itself.
+Workspace::Workspace(c2kv_ctx* c, size_t bytes, size_t n) : ctx_(c) {
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    err = cudaStreamIsCapturing(c->stream, &capture);
+    if (err != cudaSuccess) return;
+    if (capture == cudaStreamCaptureStatusNone) {
+        err = kept_workspace(c, bytes, n, &p, &counters);
+        return;
+    }
+    bytes = (bytes + 15) / 16 * 16;
+    err = pool_alloc(c, &own_, bytes + n * sizeof(uint32_t));
+    if (err != cudaSuccess) return;
+    p = own_;
+    counters = reinterpret_cast<uint32_t*>(static_cast<char*>(own_) + bytes);
+    if (n > 0) err = cudaMemsetAsync(counters, 0, n * sizeof(uint32_t), c->stream);
+}
+
+Workspace::~Workspace() { pool_free(ctx_, own_); }
 
 TraceScope::TraceScope(c2kv_ctx* c, int kind) : ctx_(c), kind_(kind), begin_(nullptr) {
     if (!c->prof) return;

@@ -388,9 +388,24 @@ struct ContextView {
 bool context_view(const c2kv_ctx* ctx, ContextView* v);
 cudaError_t context_alloc(c2kv_ctx* ctx, void** p, size_t bytes);    // stream-ordered, from the context's memory pool
 void context_free(c2kv_ctx* ctx, void* p);
-// At least `bytes` of device memory and `counters` counters, zero between launches, for work on the
-// context's current stream: kept for the stream, so that calls on different streams do not share them.
-cudaError_t context_workspace(c2kv_ctx* ctx, size_t bytes, size_t counters, void** p, uint32_t** c);
+// At least `bytes` of device memory and `n` counters, zero between launches, for what is enqueued on the
+// context's current stream during its lifetime.  It is kept for the stream, so that calls on different
+// streams do not share it; while the stream is being captured it is the graph's own.
+class Workspace {
+public:
+    Workspace(c2kv_ctx* ctx, size_t bytes, size_t n);
+    ~Workspace();
+    Workspace(const Workspace&) = delete;
+    Workspace& operator=(const Workspace&) = delete;
+
+    cudaError_t err = cudaSuccess;
+    void* p = nullptr;
+    uint32_t* counters = nullptr;
+
+private:
+    c2kv_ctx* ctx_;
+    void* own_ = nullptr;    // the graph's
+};
 // Brackets the launches made in its lifetime with the trace's events, when a trace is on.
 class TraceScope {
 public:

@@ -19,6 +19,7 @@
 
 #include <algorithm>
 #include <cuda_fp16.h>
+#include <optional>
 
 namespace c2kv {
 namespace {
@@ -419,13 +420,14 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
         }
         X.part_o = X.part_lse = nullptr;
         X.tickets = nullptr;
+        std::optional<Workspace> work;
         if (split) {
-            void* p = nullptr;
             const size_t o_bytes = (size_t)items * NR * D * 4;
-            e = context_workspace(c.ctx, o_bytes + (size_t)items * NR * 4, (size_t)units, &p, &X.tickets);
-            if (e != cudaSuccess) return e;
-            X.part_o = static_cast<float*>(p);
-            X.part_lse = reinterpret_cast<float*>(static_cast<char*>(p) + o_bytes);
+            work.emplace(c.ctx, o_bytes + (size_t)items * NR * 4, (size_t)units);
+            if (work->err != cudaSuccess) return work->err;
+            X.part_o = static_cast<float*>(work->p);
+            X.part_lse = reinterpret_cast<float*>(static_cast<char*>(work->p) + o_bytes);
+            X.tickets = work->counters;
         }
         e = launch_overlapped(kernel, (unsigned)items, kLaneThreads, kSmem, s, X);
         if (e != cudaSuccess) return e;

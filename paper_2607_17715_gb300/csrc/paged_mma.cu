@@ -36,6 +36,7 @@
 
 #include <algorithm>
 #include <cuda_fp16.h>
+#include <optional>
 
 namespace c2kv {
 namespace {
@@ -798,13 +799,14 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
         X.box_rows = std::min(1 << c.pg.page_shift, kBlk);
         X.part_o = X.part_lse = nullptr;
         X.tickets = nullptr;
+        std::optional<Workspace> work;
         if (split) {
-            void* p = nullptr;
             const size_t o_bytes = (size_t)items * kRows * D * 4;
-            e = context_workspace(c.ctx, o_bytes + (size_t)items * kRows * 4, (size_t)units, &p, &X.tickets);
-            if (e != cudaSuccess) return e;
-            X.part_o = static_cast<float*>(p);
-            X.part_lse = reinterpret_cast<float*>(static_cast<char*>(p) + o_bytes);
+            work.emplace(c.ctx, o_bytes + (size_t)items * kRows * 4, (size_t)units);
+            if (work->err != cudaSuccess) return work->err;
+            X.part_o = static_cast<float*>(work->p);
+            X.part_lse = reinterpret_cast<float*>(static_cast<char*>(work->p) + o_bytes);
+            X.tickets = work->counters;
         }
         const auto swizzle = L::RB == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE;
         if (!encode_page_map(&X.tm_k, c.pg.k, c.pg, c.hkv, D, kCodes, L::BC, X.box_rows, swizzle) ||

@@ -25,6 +25,7 @@
 #include <math_constants.h>
 
 #include <algorithm>
+#include <optional>
 #include <utility>
 #include <vector>
 
@@ -832,14 +833,13 @@ cudaError_t launch(const PagedAttnCall& c, const KeyTiles& tiles, const std::vec
             items += (int64_t)q.tiles * c.hkv * q.splits;
         }
         X.part_o = X.part_lse = nullptr;
+        std::optional<Workspace> work;
         if (units > 0) {
-            void* p = nullptr;
-            uint32_t* none = nullptr;
             const size_t o_bytes = (size_t)items * kPair * D * 4;
-            e = context_workspace(c.ctx, o_bytes + (size_t)items * kPair * 4, 0, &p, &none);
-            if (e != cudaSuccess) return e;
-            X.part_o = static_cast<float*>(p);
-            X.part_lse = reinterpret_cast<float*>(static_cast<char*>(p) + o_bytes);
+            work.emplace(c.ctx, o_bytes + (size_t)items * kPair * 4, 0);
+            if (work->err != cudaSuccess) return work->err;
+            X.part_o = static_cast<float*>(work->p);
+            X.part_lse = reinterpret_cast<float*>(static_cast<char*>(work->p) + o_bytes);
         }
         const cuuint64_t dims[3] = {D, kTileKeys, (cuuint64_t)std::max(1, tiles.n) * c.hkv}, strides[2] = {D * 2, kTileKeys * D * 2};
         const cuuint32_t box[3] = {64, kTileKeys, 1};

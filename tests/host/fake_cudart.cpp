@@ -17,6 +17,8 @@ std::vector<Launch> launches;
 std::function<bool(size_t)> alloc_fails = [](size_t) { return false; };
 std::function<int(const std::string&)> registers = [](const std::string&) { return 168; };
 std::function<int(int)> sms = [](int) { return 152; };
+bool capturing = false;
+std::vector<size_t> pool_allocations;
 
 namespace {
 std::map<const void*, std::string>& kernels() {
@@ -163,13 +165,20 @@ cudaError_t cudaPointerGetAttributes(cudaPointerAttributes* a, const void* p) {
     a->devicePointer = const_cast<void*>(p);
     return cudaSuccess;
 }
-cudaError_t cudaMalloc(void** p, size_t bytes) { return allocate(p, bytes); }
+cudaError_t cudaMalloc(void** p, size_t bytes) { return capturing ? answer(cudaErrorStreamCaptureUnsupported) : allocate(p, bytes); }
 cudaError_t cudaFree(void* p) {
+    if (capturing) return answer(cudaErrorStreamCaptureUnsupported);
     std::free(p);
     return cudaSuccess;
 }
-cudaError_t cudaMallocFromPoolAsync(void** p, size_t bytes, cudaMemPool_t, cudaStream_t) { return allocate(p, bytes); }
-cudaError_t cudaFreeAsync(void* p, cudaStream_t) { return cudaFree(p); }
+cudaError_t cudaMallocFromPoolAsync(void** p, size_t bytes, cudaMemPool_t, cudaStream_t) {
+    pool_allocations.push_back(bytes);
+    return allocate(p, bytes);
+}
+cudaError_t cudaFreeAsync(void* p, cudaStream_t) {
+    std::free(p);
+    return cudaSuccess;
+}
 cudaError_t cudaMemPoolCreate(cudaMemPool_t* p, const cudaMemPoolProps*) { return handle(p); }
 cudaError_t cudaMemPoolDestroy(cudaMemPool_t) { return cudaSuccess; }
 cudaError_t cudaMemPoolSetAttribute(cudaMemPool_t, cudaMemPoolAttr, void*) { return cudaSuccess; }
@@ -182,7 +191,11 @@ cudaError_t cudaMemset(void*, int, size_t) { return cudaSuccess; }
 cudaError_t cudaMemsetAsync(void*, int, size_t, cudaStream_t) { return cudaSuccess; }
 cudaError_t cudaStreamCreateWithFlags(cudaStream_t* s, unsigned) { return handle(s); }
 cudaError_t cudaStreamDestroy(cudaStream_t) { return cudaSuccess; }
-cudaError_t cudaStreamSynchronize(cudaStream_t) { return cudaSuccess; }
+cudaError_t cudaStreamSynchronize(cudaStream_t) { return capturing ? answer(cudaErrorStreamCaptureUnsupported) : cudaSuccess; }
+cudaError_t cudaStreamIsCapturing(cudaStream_t, cudaStreamCaptureStatus* s) {
+    *s = capturing ? cudaStreamCaptureStatusActive : cudaStreamCaptureStatusNone;
+    return cudaSuccess;
+}
 cudaError_t cudaStreamWaitEvent(cudaStream_t, cudaEvent_t, unsigned) { return cudaSuccess; }
 cudaError_t cudaEventCreate(cudaEvent_t* e) { return handle(e); }
 cudaError_t cudaEventCreateWithFlags(cudaEvent_t* e, unsigned) { return handle(e); }

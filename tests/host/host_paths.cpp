@@ -70,6 +70,20 @@ struct Context {
     c2kv_status extract(int tokens, int ratio) {
         return c2kv_extract_attention(ctx, 1, buffer, buffer, buffer, tokens, ratio, buffer, nullptr);
     }
+    // each of `batch` requests' newest `tokens` over `rows` rows of pages
+    c2kv_status paged(int batch, int tokens, int rows, bool codes) {
+        c2kv_pages pages{};
+        pages.k = pages.v = buffer;
+        pages.k_scale = pages.v_scale = reinterpret_cast<float*>(buffer);
+        pages.n_pages = 1 << 20;
+        pages.page_size = 64;
+        pages.format = codes ? C2KV_PAGES_E4M3 : C2KV_PAGES_NATIVE;
+        std::vector<int32_t> ptr(batch + 1), keys(batch, rows);
+        for (int r = 0; r <= batch; ++r) ptr[r] = r * tokens;
+        const int32_t width = (rows + 63) / 64;
+        return c2kv_paged_attend(ctx, &pages, batch, reinterpret_cast<int32_t*>(buffer), width, width, ptr.data(), keys.data(), 0,
+                                 buffer, 0, nullptr, buffer, nullptr);
+    }
     c2kv_status step(int chunks, int slots, int suffix, c2kv_cache** cache) {
         std::vector<int32_t> ids;
         for (int i = 0; i < chunks; ++i) ids.push_back(chunk(slots));
@@ -218,6 +232,34 @@ void short64() {
     }
 }
 
+// What a captured call of cut keys works in belongs to its graph: the call takes memory of its own, whether
+// the stream's kept block would do or not, and no call frees a block that a graph may still use.
+void paged_capture() {
+    const struct {
+        Shape s;
+        int tokens;
+        const char* kernel;
+    } kinds[] = {{{kBf16, 32, 8, 128}, 1, "paged_mma_kernel"}, {{kBf16, 32, 8, 64}, 1, "paged_mma_kernel"},
+                 {{kBf16, 32, 8, 128}, 64, "paged_tc_kernel"}, {{kF32, 32, 8, 128}, 1, "paged_lane_kernel"}};
+    for (const auto& k : kinds) {
+        for (int warm = 0; warm < 2; ++warm) {
+            Context one(k.s);
+            if (warm) CHECK(one.paged(1, k.tokens, 9000, true) == C2KV_OK, "%s: %s", k.kernel, c2kv_last_error(one.ctx));
+            fake::launches.clear();
+            fake::pool_allocations.clear();
+            fake::capturing = true;
+            const c2kv_status st = one.paged(1, k.tokens, 9000, true);
+            fake::capturing = false;
+            CHECK(st == C2KV_OK, "%s, captured, warm %d: %s", k.kernel, warm, c2kv_last_error(one.ctx));
+            CHECK(fake::launched(k.kernel), "%s", k.kernel);
+            // its partials, and the key tiles of a chunk
+            CHECK(fake::pool_allocations.size() == (k.tokens > 1 ? 2u : 1u), "%s, warm %d: %zu allocations", k.kernel, warm,
+                  fake::pool_allocations.size());
+            CHECK(one.paged(8, k.tokens, 60000, true) == C2KV_OK, "%s: %s", k.kernel, c2kv_last_error(one.ctx));
+        }
+    }
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
@@ -232,6 +274,7 @@ int main(int argc, char** argv) {
     else if (name == "short64") short64();
     else if (name == "no_partials") no_partials();
     else if (name == "no_queries") no_queries();
+    else if (name == "paged_capture") paged_capture();
     else CHECK(false, "unknown scenario '%s'", name.c_str());
     std::printf("ok\n");
 }
