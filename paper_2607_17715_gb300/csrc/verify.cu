@@ -59,6 +59,14 @@ __device__ __forceinline__ uint32_t cluster_size() {
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
     return r;
 }
+// Every CTA of the cluster has started: only then does its shared memory take stores.  Said when the kernel
+// starts, and waited for ahead of the first store.
+__device__ __forceinline__ void cluster_started() {
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_started_wait() {
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+}
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
@@ -177,6 +185,7 @@ __global__ void __launch_bounds__(kVerThreads, 2) verify_kernel(const __grid_con
     const int r = blockIdx.x / n_cta, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int lo = P.ptr[r], n = P.ptr[r + 1] - lo, V = P.vocab;
     const int64_t p_row = (int64_t)lo + P.b0 + r;         // the request's first row of p
+    cluster_started();
     after_kernels_before();
     if (warp == 0) {
         int a = 0;
@@ -219,9 +228,11 @@ __global__ void __launch_bounds__(kVerThreads, 2) verify_kernel(const __grid_con
         if (pass) __syncthreads();         // (s_warp is summed above by others than its warps)
         if (lane == 0) s_warp[warp] = mine;
         __syncthreads();
+        if (pass == 0) cluster_started_wait();
         if (warp == 0) {
             const uint64_t t = warp_sum(lane < kVerWarps ? s_warp[lane] : 0);
             if (lane < n_cta) st_peer(&s_total[pass][rank], lane, t);
+            __syncwarp();
         }
         cluster_sync();                    // (also of the warps' sums)
         before = total = 0;
