@@ -3,6 +3,7 @@
 #pragma once
 
 #include "paged.cuh"
+#include "per_device.cuh"
 #include "rope.cuh"
 
 #include <cuda_fp16.h>
@@ -24,14 +25,14 @@ __device__ __forceinline__ void lane_row(const void* base, int64_t at, float sca
     if constexpr (kCodes) {
         const uint8_t* p = static_cast<const uint8_t*>(base) + at + lane * C;
         if constexpr (C == 4) {
-            const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(p));
+            const uint32_t w = ld_after(reinterpret_cast<const uint32_t*>(p));
             const float2 a = codes2(w), b = codes2(w >> 16);
             x[0] = a.x * scale;
             x[1] = a.y * scale;
             x[2] = b.x * scale;
             x[3] = b.y * scale;
         } else {
-            const float2 a = codes2(__ldg(reinterpret_cast<const uint16_t*>(p)));
+            const float2 a = codes2(ld_after(reinterpret_cast<const uint16_t*>(p)));
             x[0] = a.x * scale;
             x[1] = a.y * scale;
         }
@@ -53,7 +54,7 @@ __device__ __forceinline__ void lane_query(const PagedAttn<kReq>& P, int64_t t, 
     for (int e = 0; e < C; ++e) {
         const float lo = static_cast<float>(q[c + e]), hi = static_cast<float>(q[c + D / 2 + e]);
         float a = lo, b = hi;
-        if (P.turn) rotate1(lo, hi, turn_cs(lane_turn(P.rope.turn, c + e), __ldg(P.turn + t)), a, b);
+        if (P.turn) rotate1(lo, hi, turn_cs(lane_turn(P.rope.turn, c + e), ld_after(P.turn + t)), a, b);
         x[e] = low ? a : b;
     }
 }
@@ -70,7 +71,7 @@ __device__ __forceinline__ void row_attend(const PagedAttn<kReq>& P, const float
 #pragma unroll
     for (int e = 0; e < C; ++e) o[e] = 0.f;
     for (int j = lo; j < hi; j += step) {
-        const int page = __ldg(P.pg.table + (int64_t)r * P.pg.table_stride + (j >> P.pg.page_shift));
+        const int page = ld_after(P.pg.table + (int64_t)r * P.pg.table_stride + (j >> P.pg.page_shift));
         if (page < 0 || page >= P.pg.n_pages) {
             if (lane == 0) atomicOr(P.err, 1);
             continue;
@@ -78,8 +79,8 @@ __device__ __forceinline__ void row_attend(const PagedAttn<kReq>& P, const float
         const int64_t in_page = (int64_t)hk * page_size + (j & (page_size - 1));
         const int64_t at = (int64_t)page * P.pg.page_stride + in_page * D, sat = (int64_t)page * P.pg.scale_stride + in_page;
         float k[C], v[C];
-        lane_row<T, D, kCodes>(P.pg.k, at, kCodes ? __ldg(P.pg.k_scale + sat) : 1.f, lane, k);
-        lane_row<T, D, kCodes>(P.pg.v, at, kCodes ? __ldg(P.pg.v_scale + sat) : 1.f, lane, v);
+        lane_row<T, D, kCodes>(P.pg.k, at, kCodes ? ld_after(P.pg.k_scale + sat) : 1.f, lane, k);
+        lane_row<T, D, kCodes>(P.pg.v, at, kCodes ? ld_after(P.pg.v_scale + sat) : 1.f, lane, v);
         float s = 0.f;
 #pragma unroll
         for (int e = 0; e < C; ++e) s = fmaf(q[e], k[e], s);

@@ -141,14 +141,14 @@ __device__ __forceinline__ void load_tiles(const TcLaunch<kReq>& X, const Item& 
     auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
     const int t0 = w.R.scratch + w.j0;
     asm volatile("griddepcontrol.wait;" ::: "memory");           // the key tiles are complete and visible
-    float2 unit = __ldg(X.unit + (int64_t)t0 * P.hkv + w.hk);
-    uint32_t there = __ldg(X.there + t0);
+    float2 unit = ld_after(X.unit + (int64_t)t0 * P.hkv + w.hk);
+    uint32_t there = ld_after(X.there + t0);
     for (int j = 0; j < w.n; ++j) {
         const int at = (t0 + j) * P.hkv + w.hk;
         notes[j & (kUnits - 1)] = TileNote{unit.x, unit.y, there, 0u};
         if (j + 1 < w.n) {               // (the next tile's: on their way while this one's are)
-            unit = __ldg(X.unit + (int64_t)at + P.hkv);
-            there = __ldg(X.there + t0 + j + 1);
+            unit = ld_after(X.unit + (int64_t)at + P.hkv);
+            there = ld_after(X.there + t0 + j + 1);
         }
         const int ks = j % C::kK, vs = j % C::kV;
         if (j >= C::kK) mbar_wait(bar(C::KE + ks), (uint32_t)(j / C::kK - 1) & 1u, P.err, abort);
@@ -280,7 +280,7 @@ __device__ __forceinline__ QueryRows<D> fetch_queries(const PagedAttn<kReq>& P, 
     if (P.turn && n > 0) {
 #pragma unroll
         for (int e = 0; e < k.E; ++e) k.turn[e] = lane_turn(P.rope.turn, lane * k.E + e);
-        k.pos = __ldg(P.turn + w.R.q0 + tok);
+        k.pos = ld_after(P.turn + w.R.q0 + tok);
     }
     return k;
 }

@@ -27,3 +27,16 @@ def test_peers_are_written_after_they_have_started(repo_root):
     arrive, wait, store = (body.find(x) for x in ("cluster_started()", "cluster_started_wait()", "st_peer("))
     assert 0 <= arrive < wait < store
     assert "return" not in body[:wait]
+
+
+OVERLAPPED = ["paged_mma.cu", "paged_lane.cu", "paged_move.cu", "paged_tc.cu", "paged_row.cuh", "verify.cu"]
+
+
+@pytest.mark.parametrize("name", OVERLAPPED)
+def test_overlapped_kernels_load_no_read_only_memory(repo_root, name):
+    """A kernel that is set up while the one before it runs waits for it (griddepcontrol.wait) and then loads
+    what that wrote: by ordinary loads, since one of memory that never changes may be moved ahead of the wait."""
+    text = _source(repo_root, name)
+    assert not re.search(r"__ldg\(|\bld16\(|ld\.global(\.\w+)*\.nc", text)
+    if name.endswith(".cu"):
+        assert "launch_overlapped" in text or "ProgrammaticStreamSerialization" in text
