@@ -178,6 +178,10 @@ def _stream_handle(stream):
     return stream.cuda_stream
 
 
+# Query heads, KV heads and channels of each context made here: what the paged calls' tensors must have.
+_heads = {}
+
+
 # ---------------------------------------------------------------------------- calls
 
 def c2kv_abi_version() -> int:
@@ -196,11 +200,13 @@ def c2kv_create(layers, n_q_heads, n_kv_heads, head_dim, rope_theta, dtype, pool
                       pool_slots, int(fixed_pos), attn_impl, attn_split, fuse, storage, attn_pairs)
     out = _VP()
     _check(_lib.c2kv_create(ctypes.byref(cfg), _stream_handle(stream), ctypes.byref(out)))
+    _heads[out.value] = (n_q_heads, n_kv_heads, head_dim)
     return out.value
 
 
 def c2kv_destroy(ctx):
     _check(_lib.c2kv_destroy(ctx), None)
+    _heads.pop(ctx, None)
 
 
 def c2kv_set_stream(ctx, stream):
@@ -291,7 +297,7 @@ def make_pages(k, v, k_scale=None, v_scale=None):
     n, _, rows, d = k.shape
     eight = k.element_size() == 1
     for x, inner in ((k, (rows * d, d, 1)), (v, (rows * d, d, 1)), (k_scale, (rows, 1)), (v_scale, (rows, 1))):
-        if x is not None and x.stride()[1:] != inner:
+        if x is not None and (x.stride()[1:] != inner or (n > 1 and x.stride(0) == 0)):
             raise ValueError("a page must be one dense block of its heads' rows")
     if v.shape != k.shape or v.dtype != k.dtype or (n > 1 and v.stride(0) != k.stride(0)):
         raise ValueError("k and v pages must have one shape, type and stride")
@@ -302,6 +308,7 @@ def make_pages(k, v, k_scale=None, v_scale=None):
     p = c2kv_pages(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), k.stride(0) if n > 1 else 0,
                    k_scale.stride(0) if eight and n > 1 else 0, n, rows, PAGES_E4M3 if eight else PAGES_NATIVE)
     p.keep = (k, v, k_scale, v_scale)
+    p.heads = (k.shape[1], d)
     p.address = ctypes.addressof(p)
     return p
 
@@ -321,26 +328,58 @@ def _table(table, batch, rows):
     return table.data_ptr(), w, table.stride(0) if b > 1 else w
 
 
-def _token_stride(x):
-    """Elements between tokens of a torch tensor [T, heads, d] whose heads are dense (0: dense too)."""
-    if x.is_contiguous():
+def _token_stride(x, tokens, heads):
+    """Elements between tokens of a torch tensor [at least `tokens`, *heads] whose heads are dense (0: dense too).
+    A dense tensor may have its heads in one dimension, or be one run."""
+    dense, shape = x.is_contiguous(), x.shape
+    t, *inner = shape
+    if t < tokens or (shape[1:] != heads and not (dense and inner == [heads[0] * heads[1]])):
+        if len(shape) != 1 or not dense or t < tokens * heads[0] * heads[1]:
+            raise ValueError(f"{tokens} tokens of {heads[0]} heads of {heads[1]} channels are needed, not {tuple(shape)}")
+    if dense:
         return 0
-    t, h, d = x.shape
+    h, d = inner
     if (h > 1 and x.stride(1) != d) or x.stride(2) != 1:
         raise ValueError("a token's heads must be one dense block")
+    if t > 1 and x.stride(0) == 0:
+        raise ValueError("tokens must not share their memory")
     return x.stride(0) if t > 1 else 0
 
 
-def _pair_stride(x, y):
+def _pair_stride(x, y, tokens, heads):
     """The token stride of two tensors of one shape."""
-    s, t = _token_stride(x), _token_stride(y)
-    if s != t and x.shape[0] > 1 and x.stride(0) != y.stride(0):
+    s, t = _token_stride(x, tokens, heads), _token_stride(y, tokens, heads)
+    if s != t and tokens > 1 and x.stride(0) != y.stride(0):
         raise ValueError("k and v must have one token stride")
     return s or t
 
 
-def _row_stride(x):
-    return 0 if x is None or x.is_contiguous() or x.shape[0] < 2 else x.stride(0)
+def _kv_heads(ctx, pages):
+    """KV heads and channels of the pages, which must be the context's."""
+    known = _heads.get(ctx)
+    if known is not None and known[1:] != pages.heads:
+        raise ValueError(f"pages hold {pages.heads[0]} heads of {pages.heads[1]} channels, the context has {known[1]} of {known[2]}")
+    return pages.heads
+
+
+def _vector(x, n, what):
+    """Address of a dense tensor of at least n entries (or of what has an address only)."""
+    if hasattr(x, "stride") and (x.dim() != 1 or x.shape[0] < n or (n > 1 and x.stride(0) != 1)):
+        raise ValueError(f"{what} must be one dense run of {n} entries")
+    return _ptr(x)
+
+
+def _rows(x, rows, vocab, what):
+    """Address and row stride of probabilities [at least `rows`, vocab] (0: dense)."""
+    if x is None:
+        return None, 0
+    if x.dim() != 2 or x.shape[0] < rows or x.shape[1] != vocab or (vocab > 1 and x.stride(1) != 1):
+        raise ValueError(f"{what} must be {rows} rows of {vocab} probabilities, each dense")
+    if x.shape[0] < 2 or x.is_contiguous():
+        return x.data_ptr(), 0
+    if x.stride(0) == 0:
+        raise ValueError(f"{what}: rows must not share their memory")
+    return x.data_ptr(), x.stride(0)
 
 
 def c2kv_paged_append(ctx, pages, table, new_ptr, start, k, v, turn=None):
@@ -348,8 +387,9 @@ def c2kv_paged_append(ctx, pages, table, new_ptr, start, k, v, turn=None):
     ptr, ptr_p, n = _i32_at(new_ptr)
     st, st_p, m = _i32_at(start)
     tb, w, ts = _table(table, n - 1, m)
-    _check(_lib.c2kv_paged_append(ctx, pages.address, m, tb, w, ts, ptr_p, st_p, k.data_ptr(), v.data_ptr(), _pair_stride(k, v),
-                                  _ptr(turn)), ctx)
+    t = ptr[m]
+    _check(_lib.c2kv_paged_append(ctx, pages.address, m, tb, w, ts, ptr_p, st_p, k.data_ptr(), v.data_ptr(),
+                                  _pair_stride(k, v, t, _kv_heads(ctx, pages)), _vector(turn, t, "turn")), ctx)
 
 
 def c2kv_paged_gather(ctx, pages, table, row_ptr, start, k_out, v_out, turn=None):
@@ -357,8 +397,9 @@ def c2kv_paged_gather(ctx, pages, table, row_ptr, start, k_out, v_out, turn=None
     ptr, ptr_p, n = _i32_at(row_ptr)
     st, st_p, m = _i32_at(start)
     tb, w, ts = _table(table, n - 1, m)
+    t = ptr[m]
     _check(_lib.c2kv_paged_gather(ctx, pages.address, m, tb, w, ts, ptr_p, st_p, k_out.data_ptr(), v_out.data_ptr(),
-                                  _pair_stride(k_out, v_out), _ptr(turn)), ctx)
+                                  _pair_stride(k_out, v_out, t, _kv_heads(ctx, pages)), _vector(turn, t, "turn")), ctx)
 
 
 def c2kv_paged_attend(ctx, pages, table, q_ptr, n_keys, q, out, lse=None, turn=None, window=0):
@@ -366,16 +407,26 @@ def c2kv_paged_attend(ctx, pages, table, q_ptr, n_keys, q, out, lse=None, turn=N
     ptr, ptr_p, n = _i32_at(q_ptr)
     nk, nk_p, m = _i32_at(n_keys)
     tb, w, ts = _table(table, n - 1, m)
-    _check(_lib.c2kv_paged_attend(ctx, pages.address, m, tb, w, ts, ptr_p, nk_p, window, q.data_ptr(), _token_stride(q), _ptr(turn),
-                                  _ptr(out), _ptr(lse)), ctx)
+    t, known, d = ptr[m], _heads.get(ctx), _kv_heads(ctx, pages)[1]
+    heads = (known[0], d) if known is not None else (q.shape[1] if q.dim() == 3 else q.shape[-1] // d, d)
+    if hasattr(out, "stride") and _token_stride(out, t, heads):
+        raise ValueError("out must be dense")
+    if hasattr(lse, "stride") and not (lse.is_contiguous() and (lse.shape == (heads[0], t) or lse.dim() == 1 and lse.shape[0] >= heads[0] * t)):
+        raise ValueError(f"lse must be dense, [{heads[0]}, {t}]")
+    _check(_lib.c2kv_paged_attend(ctx, pages.address, m, tb, w, ts, ptr_p, nk_p, window, q.data_ptr(), _token_stride(q, t, heads),
+                                  _vector(turn, t, "turn"), _ptr(out), _ptr(lse)), ctx)
 
 
 def c2kv_verify_drafts(ctx, draft_ptr, tokens, p, q, u_accept, u_next, n_accepted, next_token):
     """Accept drafted tokens against the target's probabilities p [T + B, V] and the draft's q [T, V]
     (None: drafts without probabilities), and draw the token that follows them."""
     ptr, ptr_p, n = _i32_at(draft_ptr)
-    _check(_lib.c2kv_verify_drafts(ctx, n - 1, ptr_p, p.shape[1], _ptr(tokens), p.data_ptr(), _row_stride(p), _ptr(q), _row_stride(q),
-                                   _ptr(u_accept), _ptr(u_next), _ptr(n_accepted), _ptr(next_token)), ctx)
+    b, vocab = n - 1, p.shape[1]
+    t = ptr[b] if n > 0 else 0
+    (pp, ps), (qp, qs) = _rows(p, t + b, vocab, "p"), _rows(q, t, vocab, "q")
+    _check(_lib.c2kv_verify_drafts(ctx, b, ptr_p, vocab, _vector(tokens, t, "tokens"), pp, ps, qp, qs, _vector(u_accept, t, "u_accept"),
+                                   _vector(u_next, b, "u_next"), _vector(n_accepted, b, "n_accepted"),
+                                   _vector(next_token, b, "next_token")), ctx)
 
 
 def c2kv_cache_release(ctx, cache):
