@@ -10,6 +10,7 @@ from __future__ import annotations
 import array
 import ctypes
 import os
+import sys
 
 import numpy as np
 
@@ -178,8 +179,19 @@ def _stream_handle(stream):
     return stream.cuda_stream
 
 
-# Query heads, KV heads and channels of each context made here: what the paged calls' tensors must have.
-_heads = {}
+# Query heads, KV heads and channels of each context made here, and its type: what the paged calls' tensors
+# must have.
+_heads, _types = {}, {}
+
+
+def _torch():
+    """torch, which whoever passes a tensor has imported (the binding does not)."""
+    return sys.modules["torch"]
+
+
+def _of_type(x, dtype, what):
+    if x.dtype is not dtype:
+        raise ValueError(f"{what} must hold {dtype}, not {x.dtype}")
 
 
 # ---------------------------------------------------------------------------- calls
@@ -201,12 +213,14 @@ def c2kv_create(layers, n_q_heads, n_kv_heads, head_dim, rope_theta, dtype, pool
     out = _VP()
     _check(_lib.c2kv_create(ctypes.byref(cfg), _stream_handle(stream), ctypes.byref(out)))
     _heads[out.value] = (n_q_heads, n_kv_heads, head_dim)
+    _types[out.value] = dtype
     return out.value
 
 
 def c2kv_destroy(ctx):
     _check(_lib.c2kv_destroy(ctx), None)
     _heads.pop(ctx, None)
+    _types.pop(ctx, None)
 
 
 def c2kv_set_stream(ctx, stream):
@@ -295,20 +309,24 @@ def make_pages(k, v, k_scale=None, v_scale=None):
     8-bit (torch.float8_e4m3fn or uint8 codes) with fp32 scales [n_pages, Hkv, page_size].  The
     description keeps the tensors."""
     n, _, rows, d = k.shape
-    eight = k.element_size() == 1
+    t = _torch()
+    eight = k.dtype in (t.float8_e4m3fn, t.uint8)
+    if not eight and k.dtype not in (t.bfloat16, t.float32):
+        raise ValueError(f"pages hold bfloat16, float32, float8_e4m3fn or its codes as uint8, not {k.dtype}")
     for x, inner in ((k, (rows * d, d, 1)), (v, (rows * d, d, 1)), (k_scale, (rows, 1)), (v_scale, (rows, 1))):
         if x is not None and (x.stride()[1:] != inner or (n > 1 and x.stride(0) == 0)):
             raise ValueError("a page must be one dense block of its heads' rows")
     if v.shape != k.shape or v.dtype != k.dtype or (n > 1 and v.stride(0) != k.stride(0)):
         raise ValueError("k and v pages must have one shape, type and stride")
     if eight and (k_scale is None or v_scale is None or k_scale.shape != k.shape[:3] or v_scale.shape != k.shape[:3] or
-                  k_scale.element_size() != 4 or v_scale.element_size() != 4 or
+                  k_scale.dtype is not t.float32 or v_scale.dtype is not t.float32 or
                   (n > 1 and v_scale.stride(0) != k_scale.stride(0))):
         raise ValueError("8-bit pages need fp32 scales [n_pages, Hkv, page_size], of one stride")
     p = c2kv_pages(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), k.stride(0) if n > 1 else 0,
                    k_scale.stride(0) if eight and n > 1 else 0, n, rows, PAGES_E4M3 if eight else PAGES_NATIVE)
     p.keep = (k, v, k_scale, v_scale)
     p.heads = (k.shape[1], d)
+    p.dtype = None if eight else k.dtype
     p.address = ctypes.addressof(p)
     return p
 
@@ -319,8 +337,7 @@ def _table(table, batch, rows):
     b, w = table.shape
     if b != batch or rows != batch:
         raise ValueError("the table, the ranges and the rows must describe one batch")
-    if table.element_size() != 4:
-        raise ValueError("a table holds int32")
+    _of_type(table, _torch().int32, "a table")
     if table.is_contiguous():
         return table.data_ptr(), w, w
     if w > 1 and table.stride(1) != 1:
@@ -362,10 +379,22 @@ def _kv_heads(ctx, pages):
     return pages.heads
 
 
-def _vector(x, n, what):
+def _rows_of_type(ctx, pages, x, y):
+    """Two tensors of rows must hold the context's type, and so must native pages."""
+    t, known = _torch(), _types.get(ctx)
+    dtype = x.dtype if known is None else t.float32 if known == DTYPE_F32 else t.bfloat16
+    if dtype is not t.bfloat16 and dtype is not t.float32:
+        raise ValueError(f"rows hold bfloat16 or float32, not {dtype}")
+    if x.dtype is not dtype or y.dtype is not dtype or (pages.dtype is not None and pages.dtype is not dtype):
+        raise ValueError(f"the context's type is {dtype}, not {x.dtype}, {y.dtype} or pages of {pages.dtype}")
+
+
+def _vector(x, n, what, dtype="int32"):
     """Address of a dense tensor of at least n entries (or of what has an address only)."""
-    if hasattr(x, "stride") and (x.dim() != 1 or x.shape[0] < n or (n > 1 and x.stride(0) != 1)):
-        raise ValueError(f"{what} must be one dense run of {n} entries")
+    if hasattr(x, "stride"):
+        _of_type(x, getattr(_torch(), dtype), what)
+        if x.numel() < n or not x.is_contiguous():
+            raise ValueError(f"{what} must be one dense run of {n} entries")
     return _ptr(x)
 
 
@@ -375,6 +404,7 @@ def _rows(x, rows, vocab, what):
         return None, 0
     if x.dim() != 2 or x.shape[0] < rows or x.shape[1] != vocab or (vocab > 1 and x.stride(1) != 1):
         raise ValueError(f"{what} must be {rows} rows of {vocab} probabilities, each dense")
+    _of_type(x, _torch().float32, what)
     if x.shape[0] < 2 or x.is_contiguous():
         return x.data_ptr(), 0
     if x.stride(0) == 0:
@@ -388,6 +418,7 @@ def c2kv_paged_append(ctx, pages, table, new_ptr, start, k, v, turn=None):
     st, st_p, m = _i32_at(start)
     tb, w, ts = _table(table, n - 1, m)
     t = ptr[m]
+    _rows_of_type(ctx, pages, k, v)
     _check(_lib.c2kv_paged_append(ctx, pages.address, m, tb, w, ts, ptr_p, st_p, k.data_ptr(), v.data_ptr(),
                                   _pair_stride(k, v, t, _kv_heads(ctx, pages)), _vector(turn, t, "turn")), ctx)
 
@@ -398,6 +429,7 @@ def c2kv_paged_gather(ctx, pages, table, row_ptr, start, k_out, v_out, turn=None
     st, st_p, m = _i32_at(start)
     tb, w, ts = _table(table, n - 1, m)
     t = ptr[m]
+    _rows_of_type(ctx, pages, k_out, v_out)
     _check(_lib.c2kv_paged_gather(ctx, pages.address, m, tb, w, ts, ptr_p, st_p, k_out.data_ptr(), v_out.data_ptr(),
                                   _pair_stride(k_out, v_out, t, _kv_heads(ctx, pages)), _vector(turn, t, "turn")), ctx)
 
@@ -409,8 +441,11 @@ def c2kv_paged_attend(ctx, pages, table, q_ptr, n_keys, q, out, lse=None, turn=N
     tb, w, ts = _table(table, n - 1, m)
     t, known, d = ptr[m], _heads.get(ctx), _kv_heads(ctx, pages)[1]
     heads = (known[0], d) if known is not None else (q.shape[1] if q.dim() == 3 else q.shape[-1] // d, d)
+    _rows_of_type(ctx, pages, q, out if hasattr(out, "stride") else q)
     if hasattr(out, "stride") and _token_stride(out, t, heads):
         raise ValueError("out must be dense")
+    if hasattr(lse, "stride"):
+        _of_type(lse, _torch().float32, "lse")
     if hasattr(lse, "stride") and not (lse.is_contiguous() and (lse.shape == (heads[0], t) or lse.dim() == 1 and lse.shape[0] >= heads[0] * t)):
         raise ValueError(f"lse must be dense, [{heads[0]}, {t}]")
     _check(_lib.c2kv_paged_attend(ctx, pages.address, m, tb, w, ts, ptr_p, nk_p, window, q.data_ptr(), _token_stride(q, t, heads),
@@ -424,9 +459,9 @@ def c2kv_verify_drafts(ctx, draft_ptr, tokens, p, q, u_accept, u_next, n_accepte
     b, vocab = n - 1, p.shape[1]
     t = ptr[b] if n > 0 else 0
     (pp, ps), (qp, qs) = _rows(p, t + b, vocab, "p"), _rows(q, t, vocab, "q")
-    _check(_lib.c2kv_verify_drafts(ctx, b, ptr_p, vocab, _vector(tokens, t, "tokens"), pp, ps, qp, qs, _vector(u_accept, t, "u_accept"),
-                                   _vector(u_next, b, "u_next"), _vector(n_accepted, b, "n_accepted"),
-                                   _vector(next_token, b, "next_token")), ctx)
+    _check(_lib.c2kv_verify_drafts(ctx, b, ptr_p, vocab, _vector(tokens, t, "tokens"), pp, ps, qp, qs,
+                                   _vector(u_accept, t, "u_accept", "float32"), _vector(u_next, b, "u_next", "float32"),
+                                   _vector(n_accepted, b, "n_accepted"), _vector(next_token, b, "next_token")), ctx)
 
 
 def c2kv_cache_release(ctx, cache):

@@ -132,3 +132,47 @@ def test_other_layouts_of_the_same_are_taken(args):
     flat = torch.zeros((T, HQ * D), dtype=torch.bfloat16)
     _taken("attend", dict(args["attend"], q=flat, out=flat.view(-1), lse=torch.zeros(HQ * T)))
     _taken("append", dict(args["append"], ptr=np.array([0, 3, 4]), rows=np.array([7, 1]), turn=None))
+
+
+TYPES = [("append", "turn", "int64"), ("gather", "turn", "int64"), ("attend", "turn", "int64"), ("attend", "turn", "float32"),
+         ("append", "table", "float32"), ("append", "k", "float16"), ("append", "v", "float32"), ("gather", "v", "float16"),
+         ("attend", "q", "float32"), ("attend", "out", "float32"), ("attend", "lse", "float64"), ("attend", "lse", "bfloat16"),
+         ("verify", "tokens", "int64"), ("verify", "p", "bfloat16"), ("verify", "q", "float64"), ("verify", "u_accept", "float64"),
+         ("verify", "u_next", "bfloat16"), ("verify", "n_accepted", "int64"), ("verify", "next_token", "float32")]
+
+
+@pytest.mark.parametrize("name,key,dtype", TYPES)
+def test_types_that_the_call_would_misread(args, name, key, dtype):
+    a = args[name]
+    with pytest.raises(ValueError):
+        _call(name, dict(a, **{key: a[key].to(getattr(torch, dtype))}))
+
+
+@pytest.mark.parametrize("dtype", ["float16", "float64", "float8_e5m2", "int16", "bool"])
+def test_pages_of_types_that_are_none(dtype):
+    k = torch.zeros((6, HKV, 16, D)).to(getattr(torch, dtype))
+    s = torch.zeros((6, HKV, 16))
+    with pytest.raises(ValueError):
+        c2kv.make_pages(k, k.clone(), s, s.clone())
+
+
+def test_scales_of_another_type():
+    k = torch.zeros((6, HKV, 16, D), dtype=torch.uint8)
+    s = torch.zeros((6, HKV, 16), dtype=torch.int32)
+    with pytest.raises(ValueError):
+        c2kv.make_pages(k, k.clone(), s, s.clone())
+
+
+def test_pages_of_another_type_than_the_rows(args):
+    """fp32 rows over 16-bit pages; over 8-bit pages both types of row are some context's."""
+    f32 = torch.zeros((T, HKV, D))
+    with pytest.raises(ValueError):
+        _call("append", dict(args["append"], k=f32, v=f32))
+    codes, scale = torch.zeros((6, HKV, 16, D)).to(torch.float8_e4m3fn), torch.zeros((6, HKV, 16))
+    _taken("append", dict(args["append"], pages=c2kv.make_pages(codes, codes.clone(), scale, scale.clone()), k=f32, v=f32))
+
+
+def test_entries_in_any_shape(args):
+    """A dense tensor of the entries, whatever its dimensions."""
+    a = args["verify"]
+    _taken("verify", dict(a, n_accepted=a["n_accepted"][:, None], u_next=a["u_next"].view(1, 2)))
