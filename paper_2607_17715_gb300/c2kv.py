@@ -314,7 +314,8 @@ def make_pages(k, v, k_scale=None, v_scale=None):
     if not eight and k.dtype not in (t.bfloat16, t.float32):
         raise ValueError(f"pages hold bfloat16, float32, float8_e4m3fn or its codes as uint8, not {k.dtype}")
     for x, inner in ((k, (rows * d, d, 1)), (v, (rows * d, d, 1)), (k_scale, (rows, 1)), (v_scale, (rows, 1))):
-        if x is not None and (x.stride()[1:] != inner or (n > 1 and x.stride(0) == 0)):
+        # (the stride of a single head says nothing)
+        if x is not None and (x.stride()[2:] != inner[1:] or (k.shape[1] > 1 and x.stride(1) != inner[0]) or (n > 1 and x.stride(0) == 0)):
             raise ValueError("a page must be one dense block of its heads' rows")
     if v.shape != k.shape or v.dtype != k.dtype or (n > 1 and v.stride(0) != k.stride(0)):
         raise ValueError("k and v pages must have one shape, type and stride")

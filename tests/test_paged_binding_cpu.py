@@ -176,3 +176,13 @@ def test_entries_in_any_shape(args):
     """A dense tensor of the entries, whatever its dimensions."""
     a = args["verify"]
     _taken("verify", dict(a, n_accepted=a["n_accepted"][:, None], u_next=a["u_next"].view(1, 2)))
+
+
+def test_pages_of_one_head_among_others():
+    """One head's pages as a slice of several heads': each is one run, wherever the next head would lie."""
+    k = torch.zeros((6, 3, 16, D), dtype=torch.bfloat16)[:, 1:2]
+    p = c2kv.make_pages(k, k)
+    assert p.page_stride == 3 * 16 * D and p.heads == (1, D)
+    codes, scale = torch.zeros((6, 3, 16, D), dtype=torch.uint8)[:, 2:], torch.zeros((6, 3, 16))[:, :1]
+    p = c2kv.make_pages(codes, codes, scale, scale)
+    assert (p.page_stride, p.scale_stride) == (3 * 16 * D, 3 * 16)
