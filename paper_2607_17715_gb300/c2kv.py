@@ -179,9 +179,15 @@ def _stream_handle(stream):
     return stream.cuda_stream
 
 
-# Query heads, KV heads and channels of each context made here, and its type: what the paged calls' tensors
-# must have.
-_heads, _types = {}, {}
+class _Known:
+    """What the paged calls' tensors must be like: heads and channels, and the rows' type (torch's)."""
+    __slots__ = ("q", "kv", "f32", "dtype")
+
+    def __init__(self, hq, hkv, d, f32):
+        self.q, self.kv, self.f32, self.dtype = (hq, d), (hkv, d), f32, None
+
+
+_contexts = {}                                       # of each context made here
 
 
 def _torch():
@@ -212,15 +218,13 @@ def c2kv_create(layers, n_q_heads, n_kv_heads, head_dim, rope_theta, dtype, pool
                       pool_slots, int(fixed_pos), attn_impl, attn_split, fuse, storage, attn_pairs)
     out = _VP()
     _check(_lib.c2kv_create(ctypes.byref(cfg), _stream_handle(stream), ctypes.byref(out)))
-    _heads[out.value] = (n_q_heads, n_kv_heads, head_dim)
-    _types[out.value] = dtype
+    _contexts[out.value] = _Known(n_q_heads, n_kv_heads, head_dim, dtype == DTYPE_F32)
     return out.value
 
 
 def c2kv_destroy(ctx):
     _check(_lib.c2kv_destroy(ctx), None)
-    _heads.pop(ctx, None)
-    _types.pop(ctx, None)
+    _contexts.pop(ctx, None)
 
 
 def c2kv_set_stream(ctx, stream):
@@ -328,6 +332,7 @@ def make_pages(k, v, k_scale=None, v_scale=None):
     p.keep = (k, v, k_scale, v_scale)
     p.heads = (k.shape[1], d)
     p.dtype = None if eight else k.dtype
+    p.fits = None                                    # the context that they were last found to fit
     p.address = ctypes.addressof(p)
     return p
 
@@ -346,10 +351,30 @@ def _table(table, batch, rows):
     return table.data_ptr(), w, table.stride(0) if b > 1 else w
 
 
-def _token_stride(x, tokens, heads):
+def _known(ctx, pages, x, heads):
+    """What the tensors of a call must be like, by its context (one that was not made here: by the pages and by
+    x, whose heads are `heads`).  The pages must be the context's."""
+    known = _contexts.get(ctx)
+    if known is not None and pages.fits is known:
+        return known
+    t = _torch()
+    if known is None:
+        if x.dtype is not t.bfloat16 and x.dtype is not t.float32:
+            raise ValueError(f"rows hold bfloat16 or float32, not {x.dtype}")
+        known = _Known(heads, *pages.heads, x.dtype is t.float32)
+    known.dtype = t.float32 if known.f32 else t.bfloat16
+    if pages.heads != known.kv or pages.dtype not in (None, known.dtype):
+        raise ValueError(f"pages hold heads {pages.heads} of {pages.dtype}, the context has {known.kv} of {known.dtype}")
+    pages.fits = known
+    return known
+
+
+def _token_stride(x, tokens, heads, dtype):
     """Elements between tokens of a torch tensor [at least `tokens`, *heads] whose heads are dense (0: dense too).
     A dense tensor may have its heads in one dimension, or be one run."""
     dense, shape = x.is_contiguous(), x.shape
+    if x.dtype is not dtype:
+        raise ValueError(f"rows must hold {dtype}, as the context does, not {x.dtype}")
     t, *inner = shape
     if t < tokens or (shape[1:] != heads and not (dense and inner == [heads[0] * heads[1]])):
         if len(shape) != 1 or not dense or t < tokens * heads[0] * heads[1]:
@@ -364,49 +389,38 @@ def _token_stride(x, tokens, heads):
     return x.stride(0) if t > 1 else 0
 
 
-def _pair_stride(x, y, tokens, heads):
-    """The token stride of two tensors of one shape."""
-    s, t = _token_stride(x, tokens, heads), _token_stride(y, tokens, heads)
+def _pair_stride(ctx, pages, x, y, tokens):
+    """The token stride of two tensors of the pages' heads."""
+    known = _known(ctx, pages, x, 0)
+    dtype, (h, d) = known.dtype, known.kv
+    want = (tokens, h, d)
+    if x.dtype is dtype and y.dtype is dtype and x.shape == want and y.shape == want and x.is_contiguous() and y.is_contiguous():
+        return 0
+    s, t = _token_stride(x, tokens, known.kv, dtype), _token_stride(y, tokens, known.kv, dtype)
     if s != t and tokens > 1 and x.stride(0) != y.stride(0):
         raise ValueError("k and v must have one token stride")
     return s or t
 
 
-def _kv_heads(ctx, pages):
-    """KV heads and channels of the pages, which must be the context's."""
-    known = _heads.get(ctx)
-    if known is not None and known[1:] != pages.heads:
-        raise ValueError(f"pages hold {pages.heads[0]} heads of {pages.heads[1]} channels, the context has {known[1]} of {known[2]}")
-    return pages.heads
-
-
-def _rows_of_type(ctx, pages, x, y):
-    """Two tensors of rows must hold the context's type, and so must native pages."""
-    t, known = _torch(), _types.get(ctx)
-    dtype = x.dtype if known is None else t.float32 if known == DTYPE_F32 else t.bfloat16
-    if dtype is not t.bfloat16 and dtype is not t.float32:
-        raise ValueError(f"rows hold bfloat16 or float32, not {dtype}")
-    if x.dtype is not dtype or y.dtype is not dtype or (pages.dtype is not None and pages.dtype is not dtype):
-        raise ValueError(f"the context's type is {dtype}, not {x.dtype}, {y.dtype} or pages of {pages.dtype}")
-
-
-def _vector(x, n, what, dtype="int32"):
+def _vector(x, n, what, dtype):
     """Address of a dense tensor of at least n entries (or of what has an address only)."""
-    if hasattr(x, "stride"):
-        _of_type(x, getattr(_torch(), dtype), what)
-        if x.numel() < n or not x.is_contiguous():
-            raise ValueError(f"{what} must be one dense run of {n} entries")
-    return _ptr(x)
-
-
-def _rows(x, rows, vocab, what):
-    """Address and row stride of probabilities [at least `rows`, vocab] (0: dense)."""
     if x is None:
-        return None, 0
-    if x.dim() != 2 or x.shape[0] < rows or x.shape[1] != vocab or (vocab > 1 and x.stride(1) != 1):
-        raise ValueError(f"{what} must be {rows} rows of {vocab} probabilities, each dense")
-    _of_type(x, _torch().float32, what)
-    if x.shape[0] < 2 or x.is_contiguous():
+        return None
+    if not hasattr(x, "data_ptr"):
+        return _ptr(x)
+    if x.dtype is not dtype or x.numel() < n or not x.is_contiguous():
+        raise ValueError(f"{what} must be one dense run of {n} entries of {dtype}, not {tuple(x.shape)} of {x.dtype}")
+    return x.data_ptr()
+
+
+def _rows(x, rows, vocab, what, dtype):
+    """Address and row stride of probabilities [at least `rows`, vocab] (0: dense)."""
+    shape, dense = x.shape, x.is_contiguous()
+    if x.dtype is dtype and dense and shape == (rows, vocab):
+        return x.data_ptr(), 0
+    if x.dtype is not dtype or len(shape) != 2 or shape[0] < rows or shape[1] != vocab or (vocab > 1 and x.stride(1) != 1):
+        raise ValueError(f"{what} must be {rows} rows of {vocab} probabilities, each dense, of {dtype}, not {tuple(shape)} of {x.dtype}")
+    if shape[0] < 2 or dense:
         return x.data_ptr(), 0
     if x.stride(0) == 0:
         raise ValueError(f"{what}: rows must not share their memory")
@@ -419,9 +433,8 @@ def c2kv_paged_append(ctx, pages, table, new_ptr, start, k, v, turn=None):
     st, st_p, m = _i32_at(start)
     tb, w, ts = _table(table, n - 1, m)
     t = ptr[m]
-    _rows_of_type(ctx, pages, k, v)
     _check(_lib.c2kv_paged_append(ctx, pages.address, m, tb, w, ts, ptr_p, st_p, k.data_ptr(), v.data_ptr(),
-                                  _pair_stride(k, v, t, _kv_heads(ctx, pages)), _vector(turn, t, "turn")), ctx)
+                                  _pair_stride(ctx, pages, k, v, t), _vector(turn, t, "turn", _torch().int32)), ctx)
 
 
 def c2kv_paged_gather(ctx, pages, table, row_ptr, start, k_out, v_out, turn=None):
@@ -430,9 +443,8 @@ def c2kv_paged_gather(ctx, pages, table, row_ptr, start, k_out, v_out, turn=None
     st, st_p, m = _i32_at(start)
     tb, w, ts = _table(table, n - 1, m)
     t = ptr[m]
-    _rows_of_type(ctx, pages, k_out, v_out)
     _check(_lib.c2kv_paged_gather(ctx, pages.address, m, tb, w, ts, ptr_p, st_p, k_out.data_ptr(), v_out.data_ptr(),
-                                  _pair_stride(k_out, v_out, t, _kv_heads(ctx, pages)), _vector(turn, t, "turn")), ctx)
+                                  _pair_stride(ctx, pages, k_out, v_out, t), _vector(turn, t, "turn", _torch().int32)), ctx)
 
 
 def c2kv_paged_attend(ctx, pages, table, q_ptr, n_keys, q, out, lse=None, turn=None, window=0):
@@ -440,29 +452,35 @@ def c2kv_paged_attend(ctx, pages, table, q_ptr, n_keys, q, out, lse=None, turn=N
     ptr, ptr_p, n = _i32_at(q_ptr)
     nk, nk_p, m = _i32_at(n_keys)
     tb, w, ts = _table(table, n - 1, m)
-    t, known, d = ptr[m], _heads.get(ctx), _kv_heads(ctx, pages)[1]
-    heads = (known[0], d) if known is not None else (q.shape[1] if q.dim() == 3 else q.shape[-1] // d, d)
-    _rows_of_type(ctx, pages, q, out if hasattr(out, "stride") else q)
-    if hasattr(out, "stride") and _token_stride(out, t, heads):
+    t, d = ptr[m], pages.heads[1]
+    known = _contexts.get(ctx)
+    if known is None or pages.fits is not known:
+        known = _known(ctx, pages, q, q.shape[1] if q.dim() == 3 else q.shape[-1] // d)
+    dtype, hq, tensor, stride = known.dtype, known.q[0], hasattr(out, "data_ptr"), 0
+    want = (t, hq, d)
+    if not (q.dtype is dtype and q.shape == want and q.is_contiguous()):
+        stride = _token_stride(q, t, known.q, dtype)
+    if tensor and not (out.dtype is dtype and out.shape == want and out.is_contiguous()) and _token_stride(out, t, known.q, dtype):
         raise ValueError("out must be dense")
-    if hasattr(lse, "stride"):
+    if lse is not None and hasattr(lse, "data_ptr"):
         _of_type(lse, _torch().float32, "lse")
-    if hasattr(lse, "stride") and not (lse.is_contiguous() and (lse.shape == (heads[0], t) or lse.dim() == 1 and lse.shape[0] >= heads[0] * t)):
-        raise ValueError(f"lse must be dense, [{heads[0]}, {t}]")
-    _check(_lib.c2kv_paged_attend(ctx, pages.address, m, tb, w, ts, ptr_p, nk_p, window, q.data_ptr(), _token_stride(q, t, heads),
-                                  _vector(turn, t, "turn"), _ptr(out), _ptr(lse)), ctx)
+        if not (lse.is_contiguous() and (lse.shape == (hq, t) or lse.dim() == 1 and lse.shape[0] >= hq * t)):
+            raise ValueError(f"lse must be dense, [{hq}, {t}]")
+    _check(_lib.c2kv_paged_attend(ctx, pages.address, m, tb, w, ts, ptr_p, nk_p, window, q.data_ptr(), stride,
+                                  _vector(turn, t, "turn", _torch().int32), out.data_ptr() if tensor else _ptr(out), _ptr(lse)), ctx)
 
 
 def c2kv_verify_drafts(ctx, draft_ptr, tokens, p, q, u_accept, u_next, n_accepted, next_token):
     """Accept drafted tokens against the target's probabilities p [T + B, V] and the draft's q [T, V]
     (None: drafts without probabilities), and draw the token that follows them."""
     ptr, ptr_p, n = _i32_at(draft_ptr)
-    b, vocab = n - 1, p.shape[1]
+    b, vocab, i32, f32 = n - 1, p.shape[1], _torch().int32, _torch().float32
     t = ptr[b] if n > 0 else 0
-    (pp, ps), (qp, qs) = _rows(p, t + b, vocab, "p"), _rows(q, t, vocab, "q")
-    _check(_lib.c2kv_verify_drafts(ctx, b, ptr_p, vocab, _vector(tokens, t, "tokens"), pp, ps, qp, qs,
-                                   _vector(u_accept, t, "u_accept", "float32"), _vector(u_next, b, "u_next", "float32"),
-                                   _vector(n_accepted, b, "n_accepted"), _vector(next_token, b, "next_token")), ctx)
+    pp, ps = _rows(p, t + b, vocab, "p", f32)
+    qp, qs = (None, 0) if q is None else _rows(q, t, vocab, "q", f32)
+    _check(_lib.c2kv_verify_drafts(ctx, b, ptr_p, vocab, _vector(tokens, t, "tokens", i32), pp, ps, qp, qs,
+                                   _vector(u_accept, t, "u_accept", f32), _vector(u_next, b, "u_next", f32),
+                                   _vector(n_accepted, b, "n_accepted", i32), _vector(next_token, b, "next_token", i32)), ctx)
 
 
 def c2kv_cache_release(ctx, cache):
