@@ -188,7 +188,8 @@ __device__ __forceinline__ void core_score(const uint8_t* qb, const uint8_t* kb,
 
 // Whether a job copies its own key rows (pages, codes) and turns its queries in shared memory:
 // load_rows(keys, dst, pitch, rows, first) in place of core_copy over k, v, stride; turn_queries(q, pitch,
-// rows) once the query rows have landed.
+// rows) once the query rows have landed.  Its rows may see nothing (sees_nothing(r)): zeros, where a row whose
+// every score is -inf is not a number.
 template <class Job>
 struct CoreOwnRows {
     static constexpr bool value = false;
@@ -416,7 +417,9 @@ __device__ __forceinline__ void attention_core(const Job& job, int row0, int ns,
         for (int i = 0; i < RT; ++i) {
             const int r = row0 + r0 + 4 * i;
             if (r >= job.nrows) continue;
-            const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];      // (a row that sees nothing: zeros)
+            float inv = 1.f / l[i];
+            if constexpr (CoreOwnRows<Job>::value)
+                if (l[i] == 0.f && job.sees_nothing(r)) inv = 0.f;
             T* out = job.out_row(r);
 #pragma unroll
             for (int h = 0; h < H; ++h)
@@ -452,12 +455,12 @@ __device__ __forceinline__ void attention_core(const Job& job, int row0, int ns,
         for (int q = 0; q < ns; ++q)
             for (int w = 0; w < W; ++w) mx = fmaxf(mx, part(sml, q)[4 * w + r].x);
         float ls = 0.f;
-        const float ms = mx == -CUDART_INF_F ? 0.f : mx;       // (a row that sees nothing)
+        const float ms = CoreOwnRows<Job>::value && mx == -CUDART_INF_F ? 0.f : mx;   // (maybe a row that sees nothing)
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int q = 0; q < ns; ++q)
             for (int w = 0; w < W; ++w) {
                 const float2 ml = part(sml, q)[4 * w + r];
-                const float f = exp2f(ml.x - ms);          // 0 for a slot that saw nothing
+                const float f = exp2f(ml.x - ms);          // 0 for a slot that saw nothing (some slot saw a key)
                 const float4 v = reinterpret_cast<const float4*>(part(so, q) + (4 * w + r) * D)[c4];
                 acc.x = fmaf(f, v.x, acc.x);
                 acc.y = fmaf(f, v.y, acc.y);
@@ -465,7 +468,9 @@ __device__ __forceinline__ void attention_core(const Job& job, int row0, int ns,
                 acc.w = fmaf(f, v.w, acc.w);
                 ls = fmaf(f, ml.y, ls);
             }
-        const float inv = ls == 0.f ? 0.f : 1.f / ls;
+        float inv = 1.f / ls;
+        if constexpr (CoreOwnRows<Job>::value)
+            if (ls == 0.f && job.sees_nothing(row0 + r)) inv = 0.f;
         put(job.out_row(row0 + r) + 4 * c4, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
         float* lse = job.lse_at(row0 + r);
         if (lse != nullptr && c4 == 0) *lse = (mx + log2f(ls)) * 0.69314718055994531f;

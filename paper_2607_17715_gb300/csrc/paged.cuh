@@ -172,6 +172,22 @@ void fill_paged(PagedAttn<kReq>& P, const PagedAttnCall& c, int d, const PagedRe
     for (int i = 0; i < n; ++i) P.req[i] = req[i];
 }
 
+// Whether any row lo .. hi - 1 of the request at row `r` of the table lies in a page.
+__device__ __forceinline__ bool any_page(const PageView& pg, int r, int lo, int hi) {
+    if (hi <= lo) return false;
+    for (int j = lo >> pg.page_shift; j <= (hi - 1) >> pg.page_shift; ++j) {
+        const int page = pg.table[(int64_t)r * pg.table_stride + j];
+        if (page >= 0 && page < pg.n_pages) return true;
+    }
+    return false;
+}
+// The output of a row whose weights' sum is zero, its last key being `end`: zero where it sees no key, and no
+// number where every score that it sees is -inf.
+template <int kReq>
+__device__ __forceinline__ float of_no_weight(const PagedAttn<kReq>& P, int r, int end) {
+    return any_page(P.pg, r, P.window ? max(0, end - P.window + 1) : 0, end + 1) ? __uint_as_float(0x7fc00000u) : 0.f;
+}
+
 // Drafted tokens against the target's probabilities (verify.cu).
 template <int kReq>
 struct VerifyParams {

@@ -42,6 +42,10 @@ struct PagedJob {
         const int page = __ldg(table + (key >> P.pg.page_shift));
         return page >= 0 && page < P.pg.n_pages ? page : -1;
     }
+    __device__ bool sees_nothing(int r) const {
+        const int end = row(r);
+        return !any_page(P.pg, R.row, P.window ? max(0, end - P.window + 1) : 0, end + 1);
+    }
     __device__ bool sees(int end, int key) const {
         return key <= end && (!P.window || key > end - P.window) &&
                (*reinterpret_cast<volatile uint32_t*>(gap) == 0u || page_of(key) >= 0);
