@@ -481,8 +481,9 @@ c2kv_status c2kv_paged_gather(c2kv_ctx* ctx, const c2kv_pages* pages, int32_t ba
  * at row i = n_keys[r] - (q_ptr[r + 1] - t) and
  *     O[t, h] = softmax_j( R(turn_t) Q_t,h . K_j,h/G / sqrt(d) ) V_j,h/G    over rows j <= i,
  *                                                    j > i - window where window > 0
- * (G = Hq / Hkv, any).  A query that sees no row (i < 0) gives zeros, and lse -inf.  Rows that no
- * query sees are never read into a result, whatever they hold.
+ * (G = Hq / Hkv, any).  A query that sees no row (i < 0) gives zeros, and lse -inf; one whose every
+ * score is -inf gives NaN, and lse -inf.  Rows that no query sees are never read into a result,
+ * whatever they hold.
  *
  *   batch, table, table_width, table_stride : as c2kv_paged_append.
  *   q_ptr        : host int32 [B + 1], non-decreasing from 0; a request may have no query.

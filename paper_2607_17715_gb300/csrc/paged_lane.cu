@@ -329,11 +329,14 @@ __global__ void __launch_bounds__(kLaneThreads, lane_ctas(D)) paged_lane_kernel(
             sum = fmaf(l, w, sum * a);
             x = make_float4(fmaf(y.x, w, x.x * a), fmaf(y.y, w, x.y * a), fmaf(y.z, w, x.z * a), fmaf(y.w, w, x.w * a));
         }
-        __device__ float4 value() const {
+        __device__ float4 value(float none) const {                  // (none: of no weight)
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            return sum == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+            return sum == 0.f ? make_float4(none, none, none, none) : make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
         }
         __device__ float lse2() const { return sum == 0.f ? -INFINITY : top + log2f(sum); }
+    };
+    auto none = [&](const Joined& j, int row) {
+        return j.sum == 0.f ? of_no_weight(P, R.row, R.n_keys - R.nq + (row0 + row) / G) : 0.f;
     };
     for (int k = threadIdx.x; k < live * (D / 4); k += kLaneThreads) {
         const int row = k / (D / 4), f = k % (D / 4);
@@ -341,9 +344,9 @@ __global__ void __launch_bounds__(kLaneThreads, lane_ctas(D)) paged_lane_kernel(
 #pragma unroll
         for (int w = 0; w < kLaneWarps; ++w) j.add(s_m[w][row], s_l[w][row], *reinterpret_cast<const float4*>(&s_o[w][row][4 * f]));
         if (whole) {
-            put(row, f, j.value(), j.lse2());
+            put(row, f, j.value(none(j, row)), j.lse2());
         } else {
-            *reinterpret_cast<float4*>(X.part_o + ((int64_t)blockIdx.x * NR + row) * D + 4 * f) = j.value();
+            *reinterpret_cast<float4*>(X.part_o + ((int64_t)blockIdx.x * NR + row) * D + 4 * f) = j.value(0.f);
             if (f == 0) X.part_lse[(int64_t)blockIdx.x * NR + row] = j.lse2();
         }
     }
@@ -370,7 +373,7 @@ __global__ void __launch_bounds__(kLaneThreads, lane_ctas(D)) paged_lane_kernel(
             const float4 y = __ldcg(reinterpret_cast<const float4*>(X.part_o + (item * NR + row) * D + 4 * f));
             j.add(e, e == -INFINITY ? 0.f : 1.f, y);
         }
-        put(row, f, j.value(), j.lse2());
+        put(row, f, j.value(none(j, row)), j.lse2());
     }
 }
 

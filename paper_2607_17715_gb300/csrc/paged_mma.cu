@@ -640,6 +640,8 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
             if (f == 0) part_lse[row] = lse2;
         }
     };
+    // of a row of no weight; a stretch's is zero, and the others' decide
+    auto none = [&](int row) { return whole ? of_no_weight(P, R.row, before + (int)((row0 + row) / G)) : 0.f; };
     for (int i = threadIdx.x; i < live * (D / 4); i += kWarps * 32) {
         const int row = i / (D / 4), f = i % (D / 4);
         float top = -INFINITY, sum = 0.f;
@@ -661,8 +663,9 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
         if constexpr (!kCodes)           // infinity or NaN in V may belong to keys that this row does not see
             if (!(fabsf(x.x) <= 3.0e38f && fabsf(x.y) <= 3.0e38f && fabsf(x.z) <= 3.0e38f && fabsf(x.w) <= 3.0e38f))
                 atomicOr(reinterpret_cast<unsigned long long*>(&s_bad), 1ull << row);
-        put(row, f, sum == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv),
-            sum == 0.f ? -INFINITY : top + log2f(sum));
+        if (sum == 0.f) x.x = x.y = x.z = x.w = none(row);
+        else x = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+        put(row, f, x, sum == 0.f ? -INFINITY : top + log2f(sum));
     }
     if constexpr (!kCodes) {
         __syncthreads();
@@ -675,6 +678,9 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
             lane_query<T, D>(P, R.q0 + (row0 + row) / G, hk * G + (row0 + row) % G, lane, q);
             row_attend<T, D, kCodes>(P, q, R.row, hk, lo, hi, 1, lane, rm, rl, x);
             const float inv = rl == 0.f ? 0.f : 1.f / rl;
+            if (rl == 0.f)
+#pragma unroll
+                for (float& e : x) e += none(row);
             float4 y = make_float4(x[0] * inv, x[1] * inv, 0.f, 0.f);
             if constexpr (D == 128) {
                 y.z = x[2] * inv;
@@ -739,6 +745,7 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
             }
         }
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        if (sum == 0.f) x.x = of_no_weight(P, R.row, before + (int)((row0 + row) / G)), x.y = x.z = x.w = x.x;
         const uint32_t tok = (row0 + row) / G, h = hk * G + row0 + row - tok * G;
         *reinterpret_cast<uint2*>(out + ((int64_t)(R.q0 + tok) * P.hq + h) * D + 4 * f) =
             make_uint2(pack2<false>(x.x * inv, x.y * inv), pack2<false>(x.z * inv, x.w * inv));

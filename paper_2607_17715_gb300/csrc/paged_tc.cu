@@ -494,6 +494,7 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
     T* const orow = static_cast<T*>(P.out) + (tok * P.hq + h) * D;
     float* const prow = X.part_o + ((int64_t)blockIdx.x * kPair + row) * D;
     const bool wide = (reinterpret_cast<uintptr_t>(P.out) & 31u) == 0;
+    const float none = there && whole && l == 0.f ? of_no_weight(P, w.R.row, end) : 0.f;
     float fin = 0.f;                     // zero, or NaN where O is not finite
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
@@ -508,7 +509,7 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
 #pragma unroll
         for (int e = 0; e < 32; ++e) {
             fin = fmaf(__uint_as_float(ov[e]), 0.f, fin);
-            ov[e] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(ov[e]) * inv);
+            ov[e] = l == 0.f ? __float_as_uint(none) : __float_as_uint(__uint_as_float(ov[e]) * inv);
         }
         if (!there) continue;
         if (whole) {
@@ -546,6 +547,9 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
         lane_query<T, D>(P, t, hh, lane, q);
         row_attend<T, D, kCodes>(P, q, w.R.row, w.hk, lo, hi, 1, lane, m, sum, o);
         const float iv = sum == 0.f ? 0.f : 1.f / sum;
+        if (whole && sum == 0.f)
+#pragma unroll
+            for (float& e : o) e += of_no_weight(P, w.R.row, last);
 #pragma unroll
         for (int e = 0; e < D / 32; ++e) {
             const int ch = lane * (D / 32) + e;
@@ -658,7 +662,8 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
         const float base = top == -CUDART_INF_F ? 0.f : top;
         for (int k = 0; k < S; ++k) sum += ex2(weight[k * kJoinRows + row] - base);
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        for (int k = 0; k < S; ++k) weight[k * kJoinRows + row] = ex2(weight[k * kJoinRows + row] - base) * inv;
+        const float none = sum == 0.f ? of_no_weight(P, R.row, R.n_keys - R.nq + (pr * kPair + first + row) / G) : 0.f;
+        for (int k = 0; k < S; ++k) weight[k * kJoinRows + row] = ex2(weight[k * kJoinRows + row] - base) * inv + none;
         if (P.lse) {
             const int all = pr * kPair + first + row;
             P.lse[(int64_t)(hk * G + all % G) * P.n_tokens + R.q0 + all / G] = sum == 0.f ? -CUDART_INF_F : (top + log2f(sum)) * 0.69314718055994531f;
