@@ -16,7 +16,9 @@
 // and masks, which leave 2^-8 of the value; the queries' channels, or O's, give that back.  Scales stay
 // in fp32: a key's K scale multiplies its row of S^T, its V scale its row of P^T.  P must fit f16, so V
 // scales are taken relative to a power of two, the largest of them so far, that O is counted in; it moves
-// like the running maximum does.  Queries are f16 too, each row scaled by a power of two so that its
+// like the running maximum does.  The largest weight is 2^15, so that f16 keeps 11 bits of weight times scale
+// down to 2^-29 of the largest of both (with a largest weight of one a row whose value is 2^10 times the others',
+// whatever its own weight, left nothing of weights of 2^-15).  Queries are f16 too, each row scaled by a power of two so that its
 // largest value is near 2^6 (2^14 where codes are short of 2^8): their rounding is 2^-12 of a value.  Over
 // 16-bit pages operands are bf16, and the queries two terms of it each: one alone, 8 bits of a value that
 // RoPE turned, made two thirds of the output's error over long contexts (5.6e-3 of it, against 2e-3).
@@ -71,6 +73,12 @@ struct Lay {
 };
 static_assert(Lay<128, false, kMostEights>::kSmem + 20 * 1024 <= 227 * 1024 && 3 * (Lay<128, true, 1>::kSmem + 5 * 1024) <= 227 * 1024,
               "shared memory of an SM");
+
+// log2 of the largest weight: what the reference lies below a row's largest score so far (P: f16 or bf16).
+template <bool kCodes>
+__host__ __device__ constexpr float top_weight() {
+    return kCodes ? 15.f : 0.f;
+}
 
 constexpr int kMaxStretches = 128;       // of one unit's keys: their weights join in shared memory
 
@@ -500,7 +508,7 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-                const float high = fmaxf(m[t][k], top * f);
+                const float high = fmaxf(m[t][k], fmaf(top, f, -top_weight<kCodes>()));
                 const float base = high == -INFINITY ? 0.f : high;     // nothing seen yet: weights 2^-inf
                 const float a = ex2f(m[t][k] - base);
                 moved |= high != m[t][k];
