@@ -8,6 +8,11 @@
 // weights and E4M3 rows, and all 8 of bf16 values down to 2^-25 of their tile's largest.  What f16 lacks
 // in range the powers of two hold.
 //
+// V's power of two is one for most tiles of a request's head, since a tile's weights lie that much lower in
+// f16 where its own is smaller than others': with one row 2^10 times the others' the others' weights lost 10
+// of their bits.  It leaves room for rows 2^12 above the largest of a sample of 32 rows; tiles of larger values,
+// or of values too small for it, have their own.
+//
 // Bytes bound it: a page's read once, two written for each value.  Measured: 32768 rows of codes of 8 heads,
 // 67 MB to 134 MB, in 38 us (5.3 TB/s).
 #include "paged.cuh"
@@ -46,11 +51,15 @@ __device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
     return r;
 }
 
+// Binades above the sample's largest value that the common power of two of V leaves room for, and how far
+// below it a tile's own may be: its largest value is then 2^-9, 16 bits above what f16 cuts off.
+constexpr int kSampleRoom = 12, kSampleDepth = 24;
+
 // K (z = 0) or V (1) of one tile and KV head a CTA, 16 values a thread and pass.
 template <int D, bool kCodes, int kReq>
 __global__ void __launch_bounds__(kExpandThreads) paged_expand_kernel(const __grid_constant__ PagedExpand<kReq> P) {
     constexpr int kChunks = D / 16, kStep = kExpandThreads / kChunks, kPasses = kTileKeys / kStep;   // rows a pass
-    __shared__ uint32_t s_top[kExpandThreads / 32], s_there;
+    __shared__ uint32_t s_top[kExpandThreads / 32], s_there, s_sample;
     // the attention may be set up and turn its queries meanwhile: it waits for this grid before it reads tiles
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     int r = 0;
@@ -101,6 +110,27 @@ __global__ void __launch_bounds__(kExpandThreads) paged_expand_kernel(const __gr
             raw[i][1] = ok ? ld16(p + 8) : make_uint4(0u, 0u, 0u, 0u);
         }
     }
+    // (V) magnitude bits of row `lane` of 32 spread over what is seen, the same for every tile of the request's head
+    uint32_t sample = 0;
+    if (v && warp == 0) {
+        const int key = P.key0[r] + (int)((int64_t)(P.n_keys[r] - P.key0[r]) * lane / 32);
+        const int pg = __ldg(P.pg.table + (int64_t)P.row[r] * P.pg.table_stride + (key >> shift));
+        if (pg >= 0 && pg < P.pg.n_pages) {
+            const int64_t in_page = (int64_t)h * size + (key & (size - 1));
+            if constexpr (kCodes) {
+                const uint32_t b = __float_as_uint(__ldg(scales + (int64_t)pg * P.pg.scale_stride + in_page)) & 0x7fffffffu;
+                if (b < 0x7f800000u) sample = b;
+            } else {                     // eight of its channels
+                const uint4 x = ld16(static_cast<const __nv_bfloat16*>(base) + (int64_t)pg * P.pg.page_stride + in_page * D + lane * 8 % D);
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t lo = w[e] << 16 & 0x7fff0000u, hi = w[e] & 0x7fff0000u;
+                    sample = max(sample, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
+                }
+            }
+        }
+    }
     if constexpr (kCodes) {              // a row's values are at most 448 of its scale: the scales decide
 #pragma unroll
         for (int i = 0; i < kPasses; ++i) {
@@ -122,13 +152,23 @@ __global__ void __launch_bounds__(kExpandThreads) paged_expand_kernel(const __gr
     }
     top = __reduce_max_sync(0xffffffffu, top);
     if (lane == 0) s_top[warp] = top;
+    if (v && warp == 0) {
+        const uint32_t m = __reduce_max_sync(0xffffffffu, sample);
+        if (lane == 0) s_sample = m;
+    }
     if (threadIdx.x == 0) s_there = there;
     __syncthreads();
     top = 0;
 #pragma unroll
     for (int w = 0; w < kExpandThreads / 32; ++w) top = max(top, s_top[w]);
-    // 16-bit values to below 2^9, as codes times their relative scales are
-    const int unit = kCodes ? above(top) : max(-100, above(top) - 9);
+    // 16-bit values to below 2^9, as codes times their relative scales are; V to below 2^15
+    constexpr int kBits = kCodes ? 0 : 9;
+    int unit = max(-100, above(top) - kBits);
+    if (v) {                             // (from -90 on: the sum of weights takes 2^-unit, 2^16 of them a tile)
+        unit = max(-90, above(top) - kBits - 6);
+        const int common = s_sample == 0u ? 0 : max(-90, min(120, above(s_sample) - kBits - 6 + kSampleRoom));
+        if (top == 0u || (s_sample != 0u && unit <= common && unit >= common - kSampleDepth)) unit = common;
+    }
     const float inv = pow2i(-unit);
     if (threadIdx.x == 0) {
         float* const u = reinterpret_cast<float*>(P.to.unit + tile * P.hkv + h);

@@ -365,10 +365,13 @@ __device__ __forceinline__ void turn_queries(const PagedAttn<kReq>& P, const Que
 // One softmax thread: row r of tile x over the CTA's key tiles, then its output.
 //
 // Weights are 2^(score + offset - ref) with the reference of the tiles before: the tile's own maximum need
-// not be known first, and is found after the weights are handed over, beside the products.  O and the sum
-// are scaled to a new reference, before the next tile, only when the maximum has passed the old one by 8.
-// Where a sum shows weights near f16's largest (or the row has no reference yet) the maximum comes first
-// after all.
+// not be known first, and is found after the weights are handed over, beside the products.  A reference is
+// set 2^8 below the maximum, so that a long tail of small weights keeps f16's 11 bits down to 2^-22 of the
+// largest (and a tile of equal weights, 2^15 together, passes for what the guard lets through).  O and the sum
+// are scaled to a new one, before the next tile, only when weights have passed 2^14.  Where a sum shows
+// weights near f16's largest (or the row has no reference yet) the maximum comes first after all.
+constexpr float kBelow = 8.f, kRoom = 14.f, kMostSum = 61440.f;
+
 template <int D, bool kCodes, int kReq>
 __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item& w, uint32_t tmem, uint32_t bars, int x, int quad, int lane,
                                              const TileNote* notes, const int8_t* s_back, volatile uint32_t* abort) {
@@ -404,12 +407,12 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld32(colS + c * 32, sv[c]);
         // scores of tile j are complete, so is every product before them: O may be scaled
-        const bool moves = top > ref + 8.0f;
+        const bool moves = top > ref + kRoom;
         float alpha = 1.0f;
         if (__any_sync(0xffffffffu, moves)) {
             if (moves) {
-                alpha = ex2(ref - top);                          // (0 from no reference at all)
-                ref = top;
+                alpha = ex2(ref - (top - kBelow));               // (0 from no reference at all)
+                ref = top - kBelow;
             }
             if (j > 0) scale_o(alpha);
             l *= alpha;
@@ -463,14 +466,14 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
         bool high = ref == -CUDART_INF_F;
         if (!__all_sync(0xffffffffu, high)) {
             sum = weigh();
-            high = high || !(sum < 32768.f);
+            high = high || !(sum < kMostSum);
         }
         if (__any_sync(0xffffffffu, high)) {
             find_top();
             alpha = 1.0f;
-            if (high && top > ref) {
-                alpha = ex2(ref - top);
-                ref = top;
+            if (high && top - kBelow > ref) {
+                alpha = ex2(ref - (top - kBelow));
+                ref = top - kBelow;
             }
             if (j > 0) scale_o(alpha);
             l *= alpha;

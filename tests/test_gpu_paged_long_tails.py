@@ -61,3 +61,13 @@ def _case(fmt, hq, hkv, d, batch, nq, keys, tail, apart, big):
     ("native", 32, 8, 128, 64, 1, 16384, 13), ("e4m3", 32, 8, 128, 1, 1, 131072, 16)])
 def test_few_rows(fmt, hq, hkv, d, batch, nq, keys, tail, apart):
     assert _case(fmt, hq, hkv, d, batch, nq, keys, tail, apart, 5) <= 5e-3
+
+
+# chunks: the large weight and the large value in one key tile, or tiles apart, and the tail in all the others
+@pytest.mark.parametrize("big", [5, 5000])
+@pytest.mark.parametrize("apart", [0, 6, 10, 13])
+@pytest.mark.parametrize("fmt,hq,hkv,d,batch,nq,keys,tail", [
+    ("e4m3", 32, 8, 128, 1, 1024, 32768, 14), ("native", 32, 8, 128, 1, 1024, 32768, 14), ("e4m3", 8, 8, 64, 4, 200, 16384, 13),
+    ("native", 8, 2, 64, 40, 64, 16384, 13), ("e4m3", 32, 8, 128, 1, 64, 131072, 16), ("native", 8, 2, 128, 1, 500, 131072, 16)])
+def test_chunks(fmt, hq, hkv, d, batch, nq, keys, tail, apart, big):
+    assert _case(fmt, hq, hkv, d, batch, nq, keys, tail, apart, big) <= 5e-3
