@@ -419,7 +419,9 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
         }
         const TileNote nt = notes[j & (kUnits - 1)];
         const uint32_t groups = nt.there;
-        const float f = rs * nt.k_unit, ve = nt.v_exp;
+        // (kept within fp32's normal range: hidden scores of -inf times zero, or scores of zero times infinity,
+        // would be no number)
+        const float f = fminf(fmaxf(rs * nt.k_unit, 0x1p-126f), 0x1.fffffep127f), ve = nt.v_exp;
         const int key0 = (w.j0 + j) * BN;
         tmem_ld_wait();
         if (key0 + BN - 1 > end || key0 <= start || groups != 0xffu) {
