@@ -411,26 +411,37 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
         }
         int64_t items = 0, units = 0;
         bool split = false;
-        for (int i = 0; i < nb; ++i) {
-            PagedReq& q = X.a.req[i];
-            q.splits = (int32_t)splits_of(q);
-            split = split || q.splits > 1;
-            q.item0 = (int32_t)items;
-            q.unit0 = (int32_t)units;
-            q.tiles = (int32_t)(units_of(q) / c.hkv);
-            units += units_of(q);
-            items += units_of(q) * q.splits;
-        }
+        auto lay_out = [&](bool cut) {
+            items = units = 0;
+            split = false;
+            for (int i = 0; i < nb; ++i) {
+                PagedReq& q = X.a.req[i];
+                q.splits = cut ? (int32_t)splits_of(q) : 1;
+                split = split || q.splits > 1;
+                q.item0 = (int32_t)items;
+                q.unit0 = (int32_t)units;
+                q.tiles = (int32_t)(units_of(q) / c.hkv);
+                units += units_of(q);
+                items += units_of(q) * q.splits;
+            }
+        };
+        lay_out(true);
         X.part_o = X.part_lse = nullptr;
         X.tickets = nullptr;
         std::optional<Workspace> work;
         if (split) {
             const size_t o_bytes = (size_t)items * NR * D * 4;
             work.emplace(c.ctx, o_bytes + (size_t)items * NR * 4, (size_t)units);
-            if (work->err != cudaSuccess) return work->err;
-            X.part_o = static_cast<float*>(work->p);
-            X.part_lse = reinterpret_cast<float*>(static_cast<char*>(work->p) + o_bytes);
-            X.tickets = work->counters;
+            if (work->err == cudaErrorMemoryAllocation) {        // no room for partials: keys are not cut, slower
+                (void)cudaGetLastError();
+                lay_out(false);
+            } else if (work->err != cudaSuccess) {
+                return work->err;
+            } else {
+                X.part_o = static_cast<float*>(work->p);
+                X.part_lse = reinterpret_cast<float*>(static_cast<char*>(work->p) + o_bytes);
+                X.tickets = work->counters;
+            }
         }
         e = launch_overlapped(kernel, (unsigned)items, kLaneThreads, kSmem, s, X);
         if (e != cudaSuccess) return e;

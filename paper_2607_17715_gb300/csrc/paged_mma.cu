@@ -801,16 +801,21 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
         }
         int64_t items = 0, units = 0;
         bool split = false;
-        for (int i = 0; i < nb; ++i) {
-            PagedReq& q = X.a.req[i];
-            q.splits = splits_of(q, per);
-            split = split || q.splits > 1;
-            q.item0 = (int32_t)items;
-            q.unit0 = (int32_t)units;
-            q.tiles = tiles_of(q);
-            units += (int64_t)q.tiles * c.hkv;
-            items += (int64_t)q.tiles * c.hkv * q.splits;
-        }
+        auto lay_out = [&](bool cut) {
+            items = units = 0;
+            split = false;
+            for (int i = 0; i < nb; ++i) {
+                PagedReq& q = X.a.req[i];
+                q.splits = cut ? splits_of(q, per) : 1;
+                split = split || q.splits > 1;
+                q.item0 = (int32_t)items;
+                q.unit0 = (int32_t)units;
+                q.tiles = tiles_of(q);
+                units += (int64_t)q.tiles * c.hkv;
+                items += (int64_t)q.tiles * c.hkv * q.splits;
+            }
+        };
+        lay_out(true);
         X.box_rows = std::min(1 << c.pg.page_shift, kBlk);
         X.part_o = X.part_lse = nullptr;
         X.tickets = nullptr;
@@ -818,10 +823,16 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
         if (split) {
             const size_t o_bytes = (size_t)items * kRows * D * 4;
             work.emplace(c.ctx, o_bytes + (size_t)items * kRows * 4, (size_t)units);
-            if (work->err != cudaSuccess) return work->err;
-            X.part_o = static_cast<float*>(work->p);
-            X.part_lse = reinterpret_cast<float*>(static_cast<char*>(work->p) + o_bytes);
-            X.tickets = work->counters;
+            if (work->err == cudaErrorMemoryAllocation) {        // no room for partials: keys are not cut, slower
+                (void)cudaGetLastError();
+                lay_out(false);
+            } else if (work->err != cudaSuccess) {
+                return work->err;
+            } else {
+                X.part_o = static_cast<float*>(work->p);
+                X.part_lse = reinterpret_cast<float*>(static_cast<char*>(work->p) + o_bytes);
+                X.tickets = work->counters;
+            }
         }
         const auto swizzle = L::RB == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE;
         if (!encode_page_map(&X.tm_k, c.pg.k, c.pg, c.hkv, D, kCodes, L::BC, X.box_rows, swizzle) ||

@@ -832,24 +832,36 @@ cudaError_t launch(const PagedAttnCall& c, const KeyTiles& tiles, const std::vec
         fill_paged(X.a, c, D, entries.data() + b0, nb);
         int64_t items = 0, units = 0;
         int32_t most = 1;
-        for (int i = 0; i < nb; ++i) {
-            PagedReq& q = X.a.req[i];
-            q.item0 = (int32_t)items;
-            q.unit0 = (int32_t)units;
-            if (q.splits > 1) {
-                units += (int64_t)q.tiles * c.hkv;
-                most = std::max(most, q.splits);
+        auto lay_out = [&](bool cut) {
+            items = units = 0;
+            most = 1;
+            for (int i = 0; i < nb; ++i) {
+                PagedReq& q = X.a.req[i];
+                if (!cut) q.splits = 1;
+                q.item0 = (int32_t)items;
+                q.unit0 = (int32_t)units;
+                if (q.splits > 1) {
+                    units += (int64_t)q.tiles * c.hkv;
+                    most = std::max(most, q.splits);
+                }
+                items += (int64_t)q.tiles * c.hkv * q.splits;
             }
-            items += (int64_t)q.tiles * c.hkv * q.splits;
-        }
+        };
+        lay_out(true);
         X.part_o = X.part_lse = nullptr;
         std::optional<Workspace> work;
         if (units > 0) {
             const size_t o_bytes = (size_t)items * kPair * D * 4;
             work.emplace(c.ctx, o_bytes + (size_t)items * kPair * 4, 0);
-            if (work->err != cudaSuccess) return work->err;
-            X.part_o = static_cast<float*>(work->p);
-            X.part_lse = reinterpret_cast<float*>(static_cast<char*>(work->p) + o_bytes);
+            if (work->err == cudaErrorMemoryAllocation) {        // no room for partials: keys are not cut, slower
+                (void)cudaGetLastError();
+                lay_out(false);
+            } else if (work->err != cudaSuccess) {
+                return work->err;
+            } else {
+                X.part_o = static_cast<float*>(work->p);
+                X.part_lse = reinterpret_cast<float*>(static_cast<char*>(work->p) + o_bytes);
+            }
         }
         const cuuint64_t dims[3] = {D, kTileKeys, (cuuint64_t)std::max(1, tiles.n) * c.hkv}, strides[2] = {D * 2, kTileKeys * D * 2};
         const cuuint32_t box[3] = {64, kTileKeys, 1};

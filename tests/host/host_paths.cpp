@@ -260,6 +260,46 @@ void paged_capture() {
     }
 }
 
+// Partials of cut keys, and a chunk's key tiles, only make a call faster: it is made without them.
+void paged_no_memory() {
+    auto grid = [](const char* kernel) {
+        for (const fake::Launch& l : fake::launches)
+            if (l.kernel.find(kernel) != std::string::npos) return (int)l.grid.x;
+        return 0;
+    };
+    const size_t mb = 1 << 20, partials = 30 * mb;               // (the key tiles of 9000 rows: 37 MB)
+    struct {
+        Shape s;
+        int tokens;
+        const char* kernel;
+        int uncut;                                               // CTAs, keys not cut
+    } const kinds[] = {{{kBf16, 32, 8, 128}, 1, "paged_mma_kernel", 8}, {{kBf16, 8, 2, 64}, 3, "paged_mma_kernel", 2},
+                       {{kBf16, 32, 8, 128}, 64, "paged_tc_kernel", 8}, {{kF32, 32, 8, 128}, 1, "paged_lane_kernel", 8}};
+    for (const auto& k : kinds) {
+        fake::alloc_fails = [](size_t) { return false; };
+        Context one(k.s), none(k.s);
+        fake::launches.clear();
+        CHECK(one.paged(1, k.tokens, 9000, true) == C2KV_OK, "%s: %s", k.kernel, c2kv_last_error(one.ctx));
+        CHECK(grid(k.kernel) > k.uncut, "%s: keys are cut when there is memory", k.kernel);
+        fake::launches.clear();
+        fake::alloc_fails = [=](size_t bytes) { return bytes >= mb && bytes < partials; };
+        CHECK(none.paged(1, k.tokens, 9000, true) == C2KV_OK, "%s without partials: %s", k.kernel, c2kv_last_error(none.ctx));
+        CHECK(grid(k.kernel) == k.uncut && !fake::launched("paged_join_kernel"), "%s: %d CTAs", k.kernel, grid(k.kernel));
+        CHECK(cudaGetLastError() == cudaSuccess, "%s: the refusal of memory stays behind", k.kernel);
+    }
+    // no key tiles: a chunk goes key by key, its keys cut or not
+    const Shape s{kBf16, 32, 8, 128};
+    for (const size_t from : {partials, (size_t)1}) {
+        fake::alloc_fails = [](size_t) { return false; };
+        Context chunk(s);
+        fake::launches.clear();
+        fake::alloc_fails = [=](size_t bytes) { return bytes >= from; };
+        CHECK(chunk.paged(1, 64, 9000, true) == C2KV_OK, "chunk without key tiles: %s", c2kv_last_error(chunk.ctx));
+        CHECK(fake::launched("paged_mma_kernel") && !fake::launched("paged_tc_kernel") && !fake::launched("paged_expand_kernel"), "chunk");
+    }
+    fake::alloc_fails = [](size_t) { return false; };
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
@@ -275,6 +315,7 @@ int main(int argc, char** argv) {
     else if (name == "no_partials") no_partials();
     else if (name == "no_queries") no_queries();
     else if (name == "paged_capture") paged_capture();
+    else if (name == "paged_no_memory") paged_no_memory();
     else CHECK(false, "unknown scenario '%s'", name.c_str());
     std::printf("ok\n");
 }
