@@ -132,7 +132,8 @@ bool encode_page_map(CUtensorMap* tm, const void* base, const PageView& pg, int 
 constexpr int kTileKeys = 128;
 struct KeyTiles {
     void* k;                 // [n][Hkv][128][d] f16; rows that no query sees, or of no page, are zero
-    void* v;
+    void* v;                 // (and values of V that are not finite)
+    uint4* odd;              // [n][Hkv]: rows of V with values that are not finite (128 bits)
     float2* unit;            // [n][Hkv]: the factor that K's values lack, and the exponent of V's
     uint32_t* there;         // [n]: which groups of 16 keys lie in pages (bits 0 .. 7)
     int32_t n;               // may be 0: no query sees a row

@@ -48,9 +48,9 @@ cudaError_t launch_many(const PagedAttnCall& c, const PagedReq* req, int n, int 
             part.push_back(q);
         }
         const int m = (int)part.size();
-        const size_t half = (size_t)std::max<int64_t>(1, total) * tile_bytes, units = (size_t)std::max<int64_t>(1, total) * c.hkv * 8;
+        const size_t most = (size_t)std::max<int64_t>(1, total), half = most * tile_bytes, odd = most * c.hkv * 16, units = most * c.hkv * 8;
         void* p = nullptr;
-        cudaError_t e = context_alloc(c.ctx, &p, 2 * half + units + (size_t)std::max<int64_t>(1, total) * 4);
+        cudaError_t e = context_alloc(c.ctx, &p, 2 * half + odd + units + most * 4);
         if (e == cudaErrorMemoryAllocation) {           // no room: key by key, slower
             (void)cudaGetLastError();
             e = launch_paged_mma(c, part.data(), m, d, codes, s);
@@ -61,8 +61,8 @@ cudaError_t launch_many(const PagedAttnCall& c, const PagedReq* req, int n, int 
         char* const base = static_cast<char*>(p);
         PagedExpandCall x{};
         x.pg = c.pg;
-        x.to = KeyTiles{base, base + half, reinterpret_cast<float2*>(base + 2 * half), reinterpret_cast<uint32_t*>(base + 2 * half + units),
-                        (int32_t)total};
+        x.to = KeyTiles{base, base + half, reinterpret_cast<uint4*>(base + 2 * half), reinterpret_cast<float2*>(base + 2 * half + odd),
+                        reinterpret_cast<uint32_t*>(base + 2 * half + odd + units), (int32_t)total};
         x.err = c.err;
         x.hkv = c.hkv;
         x.n = m;

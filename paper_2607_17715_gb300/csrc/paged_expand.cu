@@ -13,6 +13,9 @@
 // of their bits.  It leaves room for rows 2^12 above the largest of a sample of 32 rows; tiles of larger values,
 // or of values too small for it, have their own.
 //
+// Values of V that are not finite become zero here, and their rows are noted: a query that does not see such a
+// row is not touched by it (0 times it is NaN), and one that does takes them in at the end (paged_tc.cu).
+//
 // Bytes bound it: a page's read once, two written for each value.  Measured: 32768 rows of codes of 8 heads,
 // 67 MB to 134 MB, in 38 us (5.3 TB/s).
 #include "paged.cuh"
@@ -60,6 +63,7 @@ template <int D, bool kCodes, int kReq>
 __global__ void __launch_bounds__(kExpandThreads) paged_expand_kernel(const __grid_constant__ PagedExpand<kReq> P) {
     constexpr int kChunks = D / 16, kStep = kExpandThreads / kChunks, kPasses = kTileKeys / kStep;   // rows a pass
     __shared__ uint32_t s_top[kExpandThreads / 32], s_there, s_sample;
+    __shared__ uint8_t s_odd[kTileKeys];
     // the attention may be set up and turn its queries meanwhile: it waits for this grid before it reads tiles
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     int r = 0;
@@ -112,6 +116,38 @@ __global__ void __launch_bounds__(kExpandThreads) paged_expand_kernel(const __gr
     }
     // (V) magnitude bits of row `lane` of 32 spread over what is seen, the same for every tile of the request's head
     uint32_t sample = 0;
+    if (v) {
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+            bool odd = false;
+            if constexpr (kCodes) {
+                uint32_t* const w = reinterpret_cast<uint32_t*>(&raw[i][0]);
+                if (!(fabsf(scale[i]) < INFINITY)) {
+                    odd = true;
+                    scale[i] = 0.f;
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {            // codes 0x7f and 0xff are NaN
+                    const uint32_t nan = ((w[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                    odd = odd || nan != 0u;
+                    w[e] &= ~((nan >> 7) * 0xffu);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    uint32_t* const w = reinterpret_cast<uint32_t*>(&raw[i][k]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {        // (an exponent of ones carries into the bit above it)
+                        const uint32_t out = ((w[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+                        odd = odd || out != 0u;
+                        w[e] &= ~((out >> 15) * 0xffffu);
+                    }
+                }
+            }
+            const uint32_t all = __ballot_sync(0xffffffffu, odd);      // a row's threads lie next to one another
+            if (chunk == 0) s_odd[threadIdx.x / kChunks + kStep * i] = (all >> (lane & ~(kChunks - 1)) & ((1u << kChunks) - 1u)) != 0u;
+        }
+    }
     if (v && warp == 0) {
         const int key = P.key0[r] + (int)((int64_t)(P.n_keys[r] - P.key0[r]) * lane / 32);
         const int pg = __ldg(P.pg.table + (int64_t)P.row[r] * P.pg.table_stride + (key >> shift));
@@ -174,6 +210,12 @@ __global__ void __launch_bounds__(kExpandThreads) paged_expand_kernel(const __gr
         float* const u = reinterpret_cast<float*>(P.to.unit + tile * P.hkv + h);
         u[v] = v ? (float)unit : pow2i(unit);
         if (h == 0 && !v) P.to.there[tile] = s_there;
+    }
+    if (v && warp == 0) {
+        uint32_t odd[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) odd[k] = __ballot_sync(0xffffffffu, s_odd[32 * k + lane] != 0);
+        if (lane == 0) P.to.odd[tile * P.hkv + h] = make_uint4(odd[0], odd[1], odd[2], odd[3]);
     }
     __half* const out = static_cast<__half*>(v ? P.to.v : P.to.k) + (tile * P.hkv + h) * kTileKeys * D + chunk * 16;
 #pragma unroll

@@ -684,7 +684,7 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
             const int lo = max(b0 * kBlk, P.window ? end - P.window + 1 : 0), hi = min(b1 * kBlk, end + 1);
             float q[D / 32], x[D / 32], rm, rl;
             lane_query<T, D>(P, R.q0 + (row0 + row) / G, hk * G + (row0 + row) % G, lane, q);
-            row_attend<T, D, kCodes>(P, q, R.row, hk, lo, hi, 1, lane, rm, rl, x);
+            row_attend<T, D, kCodes>(P, q, R.row, hk, lo, hi, lane, rm, rl, x);
             const float inv = rl == 0.f ? 0.f : 1.f / rl;
             if (rl == 0.f)
 #pragma unroll

@@ -59,18 +59,18 @@ __device__ __forceinline__ void lane_query(const PagedAttn<kReq>& P, int64_t t, 
     }
 }
 
-// Rows lo, lo + step, .. below hi of the request at row `r` of the table: the largest score m (log2 domain),
+// Rows lo .. hi - 1 of the request at row `r` of the table: the largest score m (log2 domain),
 // the sum l of 2^(score - m), and the lane's channels of the sum of 2^(score - m) v.
 template <typename T, int D, bool kCodes, int kReq>
 __device__ __forceinline__ void row_attend(const PagedAttn<kReq>& P, const float (&q)[D / 32], int r, int hk, int lo, int hi,
-                                           int step, int lane, float& m, float& l, float (&o)[D / 32]) {
+                                           int lane, float& m, float& l, float (&o)[D / 32]) {
     constexpr int C = D / 32;
     const int page_size = 1 << P.pg.page_shift;
     m = -INFINITY;
     l = 0.f;
 #pragma unroll
     for (int e = 0; e < C; ++e) o[e] = 0.f;
-    for (int j = lo; j < hi; j += step) {
+    for (int j = lo; j < hi; ++j) {
         const int page = ld_after(P.pg.table + (int64_t)r * P.pg.table_stride + (j >> P.pg.page_shift));
         if (page < 0 || page >= P.pg.n_pages) {
             if (lane == 0) atomicOr(P.err, 1);

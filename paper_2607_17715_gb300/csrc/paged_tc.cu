@@ -26,6 +26,7 @@
 
 #include <algorithm>
 #include <optional>
+#include <type_traits>
 #include <utility>
 #include <vector>
 
@@ -55,19 +56,20 @@ struct Tc {
     static constexpr int KF = 0, KE = KF + kK, VF = KE + kK, VE = VF + kV, S = VE + kV, P = S + 2, O = P + 2, Q = O + 1, kBars = Q + 1;
     static constexpr int kTiles = (2 + kK + kV) * kTile;
     static constexpr int kNotes = kTiles + (8 * kBars + 15) / 16 * 16;
-    static constexpr int kBack = kNotes + 16 * kUnits;     // powers of two of the queries' rows: a byte each
+    static constexpr int kBack = kNotes + 32 * kUnits;     // powers of two of the queries' rows: a byte each
     static constexpr int kSlot = kBack + kPair;
     static constexpr int kSmem = 1024 /*align*/ + kSlot + 16;
 };
 static_assert(Tc<128>::kSmem <= 232448, "shared memory of a CTA");
 
-// What the softmax needs to know of a key tile: K's power of two, V's exponent, and which of its eight
-// groups of 16 keys lie in pages (bits).
-struct TileNote {
+// What the softmax needs to know of a key tile: K's power of two, V's exponent, which of its eight groups of
+// 16 keys lie in pages (bits), and which rows of V have values that are not finite (zero in the tile).
+struct __align__(16) TileNote {
     float k_unit;
     float v_exp;
     uint32_t there;
     uint32_t pad;
+    uint4 odd;
 };
 
 template <int kReq>
@@ -75,6 +77,7 @@ struct TcLaunch {
     CUtensorMap tm_k, tm_v;              // key tiles [n * Hkv][128][d], boxes of 64 channels
     const float2* unit;                  // [n][Hkv]
     const uint32_t* there;               // [n]
+    const uint4* odd;                    // [n][Hkv]
     float* part_o;                       // [item][256][D] normalised
     float* part_lse;                     // [item][256] log2 domain
     PagedAttn<kReq> a;
@@ -143,12 +146,14 @@ __device__ __forceinline__ void load_tiles(const TcLaunch<kReq>& X, const Item& 
     asm volatile("griddepcontrol.wait;" ::: "memory");           // the key tiles are complete and visible
     float2 unit = ld_after(X.unit + (int64_t)t0 * P.hkv + w.hk);
     uint32_t there = ld_after(X.there + t0);
+    uint4 odd = ld_after(X.odd + (int64_t)t0 * P.hkv + w.hk);
     for (int j = 0; j < w.n; ++j) {
         const int at = (t0 + j) * P.hkv + w.hk;
-        notes[j & (kUnits - 1)] = TileNote{unit.x, unit.y, there, 0u};
+        notes[j & (kUnits - 1)] = TileNote{unit.x, unit.y, there, 0u, odd};
         if (j + 1 < w.n) {               // (the next tile's: on their way while this one's are)
             unit = ld_after(X.unit + (int64_t)at + P.hkv);
             there = ld_after(X.there + t0 + j + 1);
+            odd = ld_after(X.odd + (int64_t)at + P.hkv);
         }
         const int ks = j % C::kK, vs = j % C::kV;
         if (j >= C::kK) mbar_wait(bar(C::KE + ks), (uint32_t)(j / C::kK - 1) & 1u, P.err, abort);
@@ -362,6 +367,77 @@ __device__ __forceinline__ void turn_queries(const PagedAttn<kReq>& P, const Que
     }
 }
 
+// Of 32 keys key0 .. whose bits are `keys`, those in (start, end].
+__device__ __forceinline__ uint32_t within(uint32_t keys, int key0, int start, int end) {
+    const int lo = max(0, start + 1 - key0), hi = min(31, end - key0);
+    return lo > hi ? 0u : keys & (0xffffffffu << lo) & (0xffffffffu >> (31 - hi));
+}
+
+// Rows that see values of V which are not finite (bits of `bad`, a lane a row from row0 on): of a channel's
+// infinities and NaN nothing is left but which there are, and nothing else matters there.  The warp looks the
+// noted keys up once for all its rows.  (Computed again key by key, a chunk of 256 tokens over one such row
+// of 8192 took 28 ms for 70 us.)
+template <int D, bool kCodes, int kReq>
+__device__ __forceinline__ void take_in(const TcLaunch<kReq>& X, const Item& w, uint32_t bad, int start, int end, int row0, int lane, uint8_t* q_tiles) {
+    using T = __nv_bfloat16;
+    constexpr int E = D / 32;                                    // channels a lane, a byte each: 1 infinity, 2 minus it, 4 NaN
+    constexpr uint32_t kNan = E == 4 ? 0x04040404u : 0x0404u;
+    using Word = typename std::conditional<E == 4, uint32_t, uint16_t>::type;
+    const PagedAttn<kReq>& P = X.a;
+    const int G = P.hq / P.hkv, size = 1 << P.pg.page_shift;
+    const int32_t* const table = P.pg.table + (int64_t)w.R.row * P.pg.table_stride;
+    Word* const of_row = reinterpret_cast<Word*>(q_tiles + row0 * D) + lane;      // (the products have read the queries)
+    for (int i = 0; i < 32; ++i) of_row[i * 32] = 0;
+    after_kernels_before();                                      // (the notes in memory: this thread has not waited)
+    uint32_t common = 0;                                         // of keys that all of the rows see
+    bool rest = true;
+    for (int j0 = 0; j0 < w.n && rest; j0 += 32) {
+        uint4 odd = make_uint4(0u, 0u, 0u, 0u);
+        if (j0 + lane < w.n) odd = ld_after(X.odd + (int64_t)(w.R.scratch + w.j0 + j0 + lane) * P.hkv + w.hk);
+        for (uint32_t tiles = __ballot_sync(0xffffffffu, (odd.x | odd.y | odd.z | odd.w) != 0u); tiles && rest; tiles &= tiles - 1) {
+            const int j = __ffs(tiles) - 1;
+#pragma unroll 1
+            for (int k = 0; k < 4 && rest; ++k) {
+                uint32_t keys = __shfl_sync(0xffffffffu, k == 0 ? odd.x : k == 1 ? odd.y : k == 2 ? odd.z : odd.w, j);
+                for (; keys && rest; keys &= keys - 1) {
+                    const int key = (w.j0 + j0 + j) * BN + 32 * k + __ffs(keys) - 1;
+                    uint32_t rows = __ballot_sync(0xffffffffu, key > start && key <= end) & bad;
+                    if (rows == 0u) continue;
+                    const int64_t page = ld_after(table + (key >> P.pg.page_shift)), in_page = (int64_t)w.hk * size + (key & (size - 1));
+                    float v[E];
+                    lane_row<T, D, kCodes>(P.pg.v, page * P.pg.page_stride + in_page * D,
+                                           kCodes ? ld_after(P.pg.v_scale + page * P.pg.scale_stride + in_page) : 1.f, lane, v);
+                    uint32_t is = 0;
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        is |= (v[e] == CUDART_INF_F ? 1u : v[e] == -CUDART_INF_F ? 2u : isnan(v[e]) ? 4u : 0u) << (8 * e);
+                    if (rows == bad) {
+                        common |= is;
+                        rest = __any_sync(0xffffffffu, (common & kNan) != kNan);
+                    } else {
+                        for (; rows; rows &= rows - 1) of_row[(__ffs(rows) - 1) * 32] |= (Word)is;
+                    }
+                }
+            }
+        }
+    }
+    const bool whole = w.R.splits == 1;
+    __syncwarp();                                                // (after the rows' own stores)
+    for (; bad; bad &= bad - 1) {
+        const int i = __ffs(bad) - 1, rr = w.row0 + row0 + i;
+        const uint32_t is = common | of_row[i * 32];
+        const int64_t at = whole ? ((w.R.q0 + rr / G) * (int64_t)P.hq + w.hk * G + rr % G) * D : ((int64_t)blockIdx.x * kPair + row0 + i) * D;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const uint32_t f = is >> (8 * e) & 7u;
+            if (f == 0u) continue;
+            const float y = f == 1u ? CUDART_INF_F : f == 2u ? -CUDART_INF_F : CUDART_NAN_F;
+            if (whole) static_cast<T*>(P.out)[at + lane * E + e] = static_cast<T>(y);
+            else X.part_o[at + lane * E + e] = y;
+        }
+    }
+}
+
 // One softmax thread: row r of tile x over the CTA's key tiles, then its output.
 //
 // Weights are 2^(score + offset - ref) with the reference of the tiles before: the tile's own maximum need
@@ -374,7 +450,7 @@ constexpr float kBelow = 8.f, kRoom = 14.f, kMostSum = 61440.f;
 
 template <int D, bool kCodes, int kReq>
 __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item& w, uint32_t tmem, uint32_t bars, int x, int quad, int lane,
-                                             const TileNote* notes, const int8_t* s_back, volatile uint32_t* abort) {
+                                             const TileNote* notes, const int8_t* s_back, volatile uint32_t* abort, uint8_t* q_tiles) {
     using T = __nv_bfloat16;
     using C = Tc<D>;
     const PagedAttn<kReq>& P = X.a;
@@ -389,6 +465,7 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
     const int start = P.window ? end - P.window : -1;            // and the last that it does not, before them
     const float rs = P.scale_log2 * pow2i(s_back[row]);
     float ref = -CUDART_INF_F, top = -CUDART_INF_F, l = 0.f;
+    bool touched = false;                // by values that are not finite
     auto scale_o = [&](float alpha) {
 #pragma unroll 1
         for (int c = 0; c < D / 16; ++c) {
@@ -423,6 +500,9 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
         // would be no number)
         const float f = fminf(fmaxf(rs * nt.k_unit, 0x1p-126f), 0x1.fffffep127f), ve = nt.v_exp;
         const int key0 = (w.j0 + j) * BN;
+        if (nt.odd.x | nt.odd.y | nt.odd.z | nt.odd.w)
+            touched = touched || within(nt.odd.x, key0, start, end) || within(nt.odd.y, key0 + 32, start, end) ||
+                      within(nt.odd.z, key0 + 64, start, end) || within(nt.odd.w, key0 + 96, start, end);
         tmem_ld_wait();
         if (key0 + BN - 1 > end || key0 <= start || groups != 0xffu) {
 #pragma unroll
@@ -500,7 +580,6 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
     float* const prow = X.part_o + ((int64_t)blockIdx.x * kPair + row) * D;
     const bool wide = (reinterpret_cast<uintptr_t>(P.out) & 31u) == 0;
     const float none = there && whole && l == 0.f ? of_no_weight(P, w.R.row, end) : 0.f;
-    float fin = 0.f;                     // zero, or NaN where O is not finite
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
         uint32_t ov[32];
@@ -513,7 +592,6 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
         }
 #pragma unroll
         for (int e = 0; e < 32; ++e) {
-            fin = fmaf(__uint_as_float(ov[e]), 0.f, fin);
             ov[e] = l == 0.f ? __float_as_uint(none) : __float_as_uint(__uint_as_float(ov[e]) * inv);
         }
         if (!there) continue;
@@ -539,30 +617,8 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
         if (!whole) X.part_lse[(int64_t)blockIdx.x * kPair + row] = lse2;
         else if (P.lse) P.lse[(int64_t)h * P.n_tokens + tok] = lse2 * 0.69314718055994531f;
     }
-    // Rows whose O is not finite though their weights' sum is: a value that is not finite may belong to
-    // keys that the row does not see (0 times it is NaN).  Those rows again, key by key, in fp32.
-    uint32_t bad = __ballot_sync(0xffffffffu, there && fin != 0.f && l < CUDART_INF_F);
-    for (; bad; bad &= bad - 1) {
-        const int i = __ffs(bad) - 1, rr = w.row0 + x * BM + quad * 32 + i;
-        const int last = w.R.n_keys - w.R.nq + rr / G;
-        const int lo = max(w.j0 * BN, P.window ? last - P.window + 1 : 0), hi = min((w.j0 + w.n) * BN, last + 1);
-        const int64_t t = w.R.q0 + rr / G;
-        const int hh = w.hk * G + rr % G;
-        float q[D / 32], o[D / 32], m, sum;
-        lane_query<T, D>(P, t, hh, lane, q);
-        row_attend<T, D, kCodes>(P, q, w.R.row, w.hk, lo, hi, 1, lane, m, sum, o);
-        const float iv = sum == 0.f ? 0.f : 1.f / sum;
-        if (whole && sum == 0.f)
-#pragma unroll
-            for (float& e : o) e += of_no_weight(P, w.R.row, last);
-#pragma unroll
-        for (int e = 0; e < D / 32; ++e) {
-            const int ch = lane * (D / 32) + e;
-            if (whole) static_cast<T*>(P.out)[(t * P.hq + hh) * D + ch] = static_cast<T>(o[e] * iv);
-            else X.part_o[((int64_t)blockIdx.x * kPair + rr - w.row0) * D + ch] = o[e] * iv;
-        }
-        if (!whole && lane == 0) X.part_lse[(int64_t)blockIdx.x * kPair + rr - w.row0] = sum == 0.f ? -CUDART_INF_F : m + log2f(sum);
-    }
+    const uint32_t bad = __ballot_sync(0xffffffffu, there && touched && l > 0.f && l < CUDART_INF_F);
+    if (bad) take_in<D, kCodes>(X, w, bad, start, end, x * BM + quad * 32, lane, q_tiles);
 }
 
 // ------------------------------------------------------------------ kernel
@@ -626,7 +682,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tc_kernel(const __grid_cons
         asm volatile("bar.sync 1, 256;" ::: "memory");           // (the rows' powers of two)
         mbar_arrive(bar(C::Q));
         const int x = warp >= 8;
-        if (x == 0 || has_b) softmax_rows<D, kCodes>(X, w, tmem, bars, x, warp & 3, lane, notes, s_back, abort);
+        if (x == 0 || has_b) softmax_rows<D, kCodes>(X, w, tmem, bars, x, warp & 3, lane, notes, s_back, abort, smem);
     }
 
     tc_fence_before();
@@ -870,6 +926,7 @@ cudaError_t launch(const PagedAttnCall& c, const KeyTiles& tiles, const std::vec
             return cudaErrorInvalidValue;
         X.unit = tiles.unit;
         X.there = tiles.there;
+        X.odd = tiles.odd;
         // each starts while the kernel before it ends, and waits for it where it reads what that wrote
         cudaLaunchConfig_t cfg{};
         cudaLaunchAttribute at{};
