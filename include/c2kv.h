@@ -414,7 +414,8 @@ c2kv_status c2kv_extract_attention(c2kv_ctx* ctx, int32_t n_layers, const void* 
  * the rounded 1 / s), and stands for code * s.  A scale of its own for every row lets rows be
  * appended without touching earlier ones.  A row of magnitudes below 2^-100 is kept as zero.  A
  * row with an infinity or a NaN is kept with scale NaN and codes 0: queries that see it give NaN,
- * the others are not touched by it.  The library writes no NaN code (0x7f, 0xff).
+ * the others are not touched by it.  The library writes no NaN code (0x7f, 0xff), and pages must not
+ * hold any: the attention takes them for numbers in places.
  *
  * The pages and their scales are laid out head by head, so that one head's rows of a page are one
  * run; a page may lie anywhere (page_stride), in an allocation that holds other layers' pages too.

@@ -23,6 +23,14 @@
 // 16-bit pages operands are bf16, and the queries two terms of it each: one alone, 8 bits of a value that
 // RoPE turned, made two thirds of the output's error over long contexts (5.6e-3 of it, against 2e-3).
 //
+// Values that are not finite (16-bit pages): 0 times one of V would be NaN for rows that do not see it, and a
+// query's second term makes NaN of an infinity of K.  A warp looks at its sums every eight blocks, and where
+// they show one it begins again with care: such values of V become zero, which rows see them is noted, and
+// they are taken in when the warps join; keys of infinities meet the first terms alone.  That is about twice
+// the time at most, where rows computed again key by key took 14 ms for 0.3 (64 requests over 8192 rows).
+// Over 8-bit pages a row that is no number has scale NaN, and a hidden key's weight is set to zero after it
+// meets that.
+//
 // Operand layouts.  The contraction over channels does not care for their order, so a lane takes the
 // channels that lie next to one another in its row: 16-byte shared loads, conflict-free under the
 // 128-byte swizzle, with no transpose of V (a lane loads the same channels of four keys and pairs them).
@@ -32,13 +40,14 @@
 // are half; five tokens of eight requests with groups of eight (40 rows), 46 MB in 30 us, bound by the issue of
 // the warps' chains: each of two tiles of 24 rows converts the codes for itself.
 #include "paged.cuh"
-#include "paged_row.cuh"
 #include "per_device.cuh"
 #include "ptx.cuh"
+#include "rope.cuh"
 
 #include <algorithm>
 #include <cuda_fp16.h>
 #include <optional>
+#include <type_traits>
 
 namespace c2kv {
 namespace {
@@ -71,7 +80,7 @@ struct Lay {
     static constexpr int kCtas = kCodes && NT == 1 ? 3 : kSmem <= 108 * 1024 ? 2 : 1;
     static constexpr int kPitch = D + 4;               // floats between rows of the joined results
 };
-static_assert(Lay<128, false, kMostEights>::kSmem + 20 * 1024 <= 227 * 1024 && 3 * (Lay<128, true, 1>::kSmem + 5 * 1024) <= 227 * 1024,
+static_assert(Lay<128, false, kMostEights>::kSmem + 24 * 1024 <= 227 * 1024 && 3 * (Lay<128, true, 1>::kSmem + 5 * 1024) <= 227 * 1024,
               "shared memory of an SM");
 
 // log2 of the largest weight: what the reference lies below a row's largest score so far (P: f16 or bf16).
@@ -168,6 +177,88 @@ __device__ __forceinline__ int q_place(int row, int ch) {
     return (((s * NT + row / 8) * 32 + (row % 8) * 4 + c) * 2 + reg) * 2 + half;
 }
 
+// 16-bit values that are not finite become zero: an exponent of ones carries into the bit above it.
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+__device__ __forceinline__ uint32_t finite(uint32_t w) { return w & ~((not_finite(w) >> 15) * 0xffffu); }
+
+// The scores of a block of 16-bit keys among which some value is not finite, the queries' second terms taken
+// times the finite ones alone: of an infinity times a query, its first term says all.
+template <int NT>
+struct Scores {
+    float x[NT][2][4];
+};
+template <int D, int NT>
+__device__ __noinline__ Scores<NT> scores_of_infinities(const uint8_t* sk, const uint8_t* q_at, int g, int c) {
+    using L = Lay<D, false, NT>;
+    Scores<NT> r;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r.x[t][h][e] = 0.f;
+#pragma unroll 1
+    for (int s = 0; s < L::KS; ++s) {                          // (words 2 s, 2 s + 1 of the lane's channels of a key)
+        const int b = s / (L::CQ / 4), u = s % (L::CQ / 4);
+        uint32_t a[2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                lds2(sk + b * L::kBox + (16 * h + 8 * k + g) * L::RB + ((2 * c + u / 2) ^ g) * 16 + u % 2 * 8, a[h][k], a[h][2 + k]);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int x = 1; x >= 0; --x) {
+                uint32_t q0, q1;
+                lds2(q_at + x * (L::KS * NT * 256) + (s * NT + t) * 256, q0, q1);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t y[4] = {x ? finite(a[h][0]) : a[h][0], x ? finite(a[h][1]) : a[h][1], x ? finite(a[h][2]) : a[h][2],
+                                           x ? finite(a[h][3]) : a[h][3]};
+                    mma16816<false>(r.x[t][h], y, q0, q1);
+                }
+            }
+    }
+    return r;
+}
+
+// Values of a block's V (16 bits) that are not finite become zero in shared memory, and are noted for the rows
+// that see them: a byte a channel in odd[row][D / 4], 1 infinity, 2 minus it, 4 NaN.  `end`: the rows' last keys.
+template <int D>
+__device__ __noinline__ void set_aside(uint8_t* sv, int key0, uint32_t has, int k_lo, int k_hi, const int* end, int window, int live, uint32_t* odd,
+                                       int lane) {
+    using L = Lay<D, false, 1>;
+    constexpr int kLanes = D / 4, kStep = 32 / kLanes;         // 8 bytes a lane: four channels
+    const int b = lane % kLanes / 16, u = lane % 16;
+    uint32_t any = 0;
+#pragma unroll
+    for (int j = 0; j < kBlk; j += kStep) {
+        const uint2 w = *(reinterpret_cast<const uint2*>(sv + b * L::kBox + (j + lane / kLanes) * L::RB) + u);
+        any |= not_finite(w.x) | not_finite(w.y);
+    }
+    if (!__any_sync(0xffffffffu, any != 0u)) return;
+    for (int j = lane / kLanes; j < kBlk; j += kStep) {
+        const int key = key0 + j;
+        if (key < k_lo || key >= k_hi || !(has >> (j >> 4) & 1u)) continue;
+        uint2* const at = reinterpret_cast<uint2*>(sv + b * L::kBox + j * L::RB) + u;
+        const uint2 w = *at;
+        if ((not_finite(w.x) | not_finite(w.y)) == 0u) continue;
+        uint32_t is = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t x = (e < 2 ? w.x : w.y) >> (16 * (e & 1)) & 0xffffu;
+            if ((x & 0x7f80u) == 0x7f80u) is |= ((x & 0x7fu) ? 4u : (x & 0x8000u) ? 2u : 1u) << (8 * e);
+        }
+        const int word = b * 16 + ((u / 2) ^ (j & 7)) * 2 + u % 2;       // (16-byte lines of a row are swapped)
+        for (int row = 0; row < live; ++row)
+            if (key <= end[row] && (!window || key > end[row] - window)) atomicOr(odd + row * (D / 4) + word, is);
+        *at = make_uint2(finite(w.x), finite(w.y));
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");         // (TMA writes there next)
+    __syncwarp();
+}
+
 template <int D, bool kCodes, int NT, int kReq>
 __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? Lay<D, kCodes, NT>::kCtas : 2) paged_mma_kernel(const __grid_constant__ MmaLaunch<kReq> X) {
     using L = Lay<D, kCodes, NT>;
@@ -184,7 +275,9 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
     __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
     __shared__ int s_end[kRows];
     __shared__ uint32_t s_abort, s_last;
-    __shared__ uint64_t s_bad;
+    // (16-bit pages) values that are not finite, of keys that a row sees: a byte a channel, 1 infinity, 2 minus
+    // it, 4 NaN
+    __shared__ uint32_t s_odd[kCodes ? 1 : kRows * (D / 4)];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, c = lane % 4;
     uint8_t* const smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
 
@@ -222,10 +315,9 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
     if (lane < kStages) mbar_init(smem_u32(&s_full[warp][lane]), kCodes ? 33 : 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncwarp();
-    if (threadIdx.x == 0) {
-        s_abort = 0;
-        s_bad = 0;
-    }
+    if (threadIdx.x == 0) s_abort = 0;
+    if constexpr (!kCodes)
+        for (int i = threadIdx.x; i < kRows * (D / 4); i += kWarps * 32) s_odd[i] = 0;
 
     after_kernels_before();
     // the warp's query rows, on their way before the keys are: behind a ring's worth of tiles they took 4 us
@@ -366,18 +458,21 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
 
     // O^T: channel tile m of 16 (lane: channels g and g + 8 of it), rows 2c and 2c + 1 of each eight
     float o[NT][MT][4], m[NT][2], l[NT][2];
+    auto start = [&] {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
+        for (int t = 0; t < NT; ++t) {
 #pragma unroll
-        for (int n = 0; n < MT; ++n)
+            for (int n = 0; n < MT; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[t][n][e] = 0.f;
+                for (int e = 0; e < 4; ++e) o[t][n][e] = 0.f;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            m[t][e] = -INFINITY;
-            l[t][e] = 0.f;
+            for (int e = 0; e < 2; ++e) {
+                m[t][e] = -INFINITY;
+                l[t][e] = 0.f;
+            }
         }
-    }
+    };
+    start();
     int unit = -127;                     // O counts in 2^unit (E4M3)
     uint32_t qf[kTerms][kHeldQ ? L::KS : 1][2];
     const uint8_t* const q_at = reinterpret_cast<const uint8_t*>(s_q) + lane * 8;
@@ -390,216 +485,272 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
     }
 
     int stage = 0, parity = 0;
-    for (int i = 0; i < n_it; ++i) {
-        const int key0 = (b0 + warp + i * kWarps) * kBlk;
-        const uint8_t* const sk = smem + (warp * kStages + stage) * L::kStage;
-        const uint8_t* const sv = sk + L::kSide;
-        const uint8_t* const ssc = smem + L::kRing + (warp * kStages + stage) * L::kScale;
-        const uint32_t has = loaded[0];
-        // some key is hidden from some row, or was not loaded: then every key is asked
-        const bool edge = has != 3 || key0 + kBlk - 1 > first || (P.window && key0 <= k_hi - 1 - P.window);
-        // key j of the block is there, and some row of the tile sees it
-        auto there = [&](int j) { return key0 + j < k_hi && key0 + j >= k_lo && (has >> (j >> 4) & 1u); };
-        mbar_wait(smem_u32(&s_full[warp][stage]), parity, P.err, &s_abort);
-
-        // S^T of keys 16 h + g (e = 0, 1) and + 8 (2, 3), rows 8 t + 2c and + 1
-        float s[NT][2][4];
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[t][h][e] = 0.f;
-#pragma unroll
-        for (int b = 0; b < L::NB; ++b) {
-            constexpr int KW = L::CQ * L::EB / 4;              // words of the lane's channels of a key
-            uint32_t w[2][2][KW];
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const uint8_t* const at = sk + b * L::kBox + (n * 8 + g) * L::RB;
-                uint32_t* const to = w[n >> 1][n & 1];
-#pragma unroll
-                for (int u = 0; u < KW / 4; ++u)
-                    lds4(at + (L::RB == 128 ? ((2 * c + u) ^ g) * 16 : c * 16), to[4 * u], to[4 * u + 1], to[4 * u + 2], to[4 * u + 3]);
-            }
-#pragma unroll
-            for (int ks = 0; ks < L::CQ / 4; ++ks) {
-                uint32_t a[2][4];
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {              // rows g and g + 8 of the 16 keys
-                        const uint32_t x = w[h][k][kCodes ? ks : (2 * ks) % KW];
-                        if constexpr (kCodes) {
-                            a[h][k] = by_masks(true, ks) ? even_pair(x) : lo_half2(x);
-                            a[h][2 + k] = by_masks(true, ks) ? odd_pair(x) : hi_half2(x);
-                        } else {
-                            a[h][k] = x;
-                            a[h][2 + k] = w[h][k][(2 * ks + 1) % KW];
-                        }
-                    }
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const int s_i = b * (L::CQ / 4) + ks;
-#pragma unroll
-                    for (int x = kTerms - 1; x >= 0; --x) {
-                        uint32_t q0, q1;
-                        if constexpr (kHeldQ) {
-                            q0 = qf[x][s_i][0];
-                            q1 = qf[x][s_i][1];
-                        } else {
-                            lds2(q_at + x * kTermBytes + (s_i * NT + t) * 256, q0, q1);
-                        }
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) mma16816<kCodes>(s[t][h], a[h], q0, q1);
-                    }
-                }
-            }
-        }
-        // scales: K's on the scores; V's relative to the unit that O counts in
-        float vs[2][2], shift = 1.f;
-        if constexpr (kCodes) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const float f = lds_f(ssc + (16 * h + 8 * k + g) * 4);
-                    vs[h][k] = lds_f(ssc + (kBlk + 16 * h + 8 * k + g) * 4);
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        s[t][h][2 * k] *= f;
-                        s[t][h][2 * k + 1] *= f;
-                    }
-                }
-            uint32_t top = __float_as_uint(lds_f(ssc + (kBlk + lane) * 4)) & 0x7fffffffu;
-            if (top >= 0x7f800000u || (edge && !there(lane))) top = 0;
-            top = __reduce_max_sync(0xffffffffu, top);
-            const int u = max(unit, min((int)(top >> 23) - 126, 126));     // every scale below 2^u
-            shift = pow2i(unit - u);
-            unit = u;
-            const float inv = pow2i(-u);
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) vs[h][k] *= inv;
-        }
-        uint32_t pf[NT][2][2];           // P^T as fragments, 16 keys each
-        bool moved = shift != 1.f;
-        float grow[NT][2];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const float2 rs = *reinterpret_cast<const float2*>(s_rs + t * 8 + 2 * c);
-            if (edge) {
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int end = s_end[t * 8 + 2 * c + k];
-#pragma unroll
-                    for (int n = 0; n < 4; ++n) {
-                        const int j = n * 8 + g, key = key0 + j;
-                        const bool seen = key <= end && (!P.window || key > end - P.window) && (has >> (j >> 4) & 1);
-                        if (!seen) s[t][n >> 1][(n & 1) * 2 + k] = -INFINITY;
-                    }
-                }
-            }
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const float f = k ? rs.y : rs.x;
-                float top = fmaxf(fmaxf(s[t][0][k], s[t][0][2 + k]), fmaxf(s[t][1][k], s[t][1][2 + k]));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-                const float high = fmaxf(m[t][k], fmaf(top, f, -top_weight<kCodes>()));
-                const float base = high == -INFINITY ? 0.f : high;     // nothing seen yet: weights 2^-inf
-                const float a = ex2f(m[t][k] - base);
-                moved |= high != m[t][k];
-                m[t][k] = high;
-                grow[t][k] = a * shift;
-                float sum = 0.f;
-#pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    float& x = s[t][n >> 1][(n & 1) * 2 + k];
-                    float p = ex2f(fmaf(x, f, -base));
-                    sum += p;
-                    // a hidden key's scale may be anything
-                    if constexpr (kCodes) p = edge && x == -INFINITY ? 0.f : p * vs[n >> 1][n & 1];
-                    x = p;
-                }
-                l[t][k] = fmaf(l[t][k], a, sum);
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                pf[t][h][0] = transposed(pack2<kCodes>(s[t][h][0], s[t][h][1]));
-                pf[t][h][1] = transposed(pack2<kCodes>(s[t][h][2], s[t][h][3]));
-            }
-        }
-        if (__any_sync(0xffffffffu, moved)) {
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int n = 0; n < MT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[t][n][e] *= grow[t][e & 1];
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int b = 0; b < L::NB; ++b) {
-                constexpr int VW = L::CV * L::EB / 4;          // words of the lane's V of a key: 4 or 2
-                uint32_t w[4][VW];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {                  // keys 2c, 2c + 1, 2c + 8, 2c + 9
-                    const int row = h * 16 + 2 * c + (k & 1) + (k >> 1) * 8;
-                    const uint8_t* const at = sv + b * L::kBox + row * L::RB;
-                    if constexpr (VW == 4) lds4(at + (g ^ (row & 7)) * 16, w[k][0], w[k][1], w[k][2], w[k][3]);
-                    else lds2(at + g * 8, w[k][0], w[k][1]);
-                    if (edge && !there(row))       // whatever lies there: 0 times it must be 0
-#pragma unroll
-                        for (int e = 0; e < VW; ++e) w[k][e] = 0;
-                }
-                // a[m]: channels 2m (rows g of the tile) and 2m + 1 (rows g + 8) of the lane's, four keys
-#pragma unroll
-                for (int e = 0; e < VW; ++e) {
-                    constexpr int kTiles = kCodes ? 2 : 1;     // a word's channels in pairs
-                    uint32_t a[kTiles][4];
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {              // keys 2c, 2c + 1, then + 8
-                        const uint32_t x = w[2 * k][e], y = w[2 * k + 1][e];
-                        if constexpr (!kCodes) {
-                            a[0][2 * k] = __byte_perm(x, y, 0x5410);
-                            a[0][2 * k + 1] = __byte_perm(x, y, 0x7632);
-                        } else if (by_masks(true, e)) {
-                            const uint32_t ex = even_pair(x), ey = even_pair(y), ox = odd_pair(x), oy = odd_pair(y);
-                            a[0][2 * k] = __byte_perm(ex, ey, 0x5410);
-                            a[0][2 * k + 1] = __byte_perm(ox, oy, 0x5410);
-                            a[kTiles - 1][2 * k] = __byte_perm(ex, ey, 0x7632);
-                            a[kTiles - 1][2 * k + 1] = __byte_perm(ox, oy, 0x7632);
-                        } else {
-                            const uint32_t lo = __byte_perm(x, y, 0x5140), hi = __byte_perm(x, y, 0x7362);
-                            a[0][2 * k] = lo_half2(lo);
-                            a[0][2 * k + 1] = hi_half2(lo);
-                            a[kTiles - 1][2 * k] = lo_half2(hi);
-                            a[kTiles - 1][2 * k + 1] = hi_half2(hi);
-                        }
-                    }
-#pragma unroll
-                    for (int t = 0; t < NT; ++t)
-#pragma unroll
-                        for (int n = 0; n < kTiles; ++n)
-                            mma16816<kCodes>(o[t][b * (L::CV / 2) + kTiles * e + n], a[n], pf[t][h][0], pf[t][h][1]);
-                }
-            }
-        }
-        __syncwarp();                    // every lane has read the stage
-        const int next = i + kStages;
-        if (next < n_it && (next & 31) == 0) look_up(next);
-#pragma unroll
-        for (int k = 0; k + 1 < kStages; ++k) loaded[k] = loaded[k + 1];
-        loaded[kStages - 1] = next < n_it ? issue(next, stage) : 0u;
+    auto advance = [&] {
         if (++stage == kStages) {
             stage = 0;
             parity ^= 1;
         }
-    }
+    };
+    // The warp's blocks.  Without care it may stop early, and returns how many it has done, where a sum is not
+    // finite (16-bit pages); else -1.
+    auto blocks = [&](auto care) -> int {
+        constexpr bool kCare = decltype(care)::value;
+        for (int i = 0; i < n_it; ++i) {
+            const int key0 = (b0 + warp + i * kWarps) * kBlk;
+            const uint8_t* const sk = smem + (warp * kStages + stage) * L::kStage;
+            const uint8_t* const sv = sk + L::kSide;
+            const uint8_t* const ssc = smem + L::kRing + (warp * kStages + stage) * L::kScale;
+            const uint32_t has = loaded[0];
+            // some key is hidden from some row, or was not loaded: then every key is asked
+            const bool edge = has != 3 || key0 + kBlk - 1 > first || (P.window && key0 <= k_hi - 1 - P.window);
+            // key j of the block is there, and some row of the tile sees it
+            auto there = [&](int j) { return key0 + j < k_hi && key0 + j >= k_lo && (has >> (j >> 4) & 1u); };
+            mbar_wait(smem_u32(&s_full[warp][stage]), parity, P.err, &s_abort);
+
+            // S^T of keys 16 h + g (e = 0, 1) and + 8 (2, 3), rows 8 t + 2c and + 1
+            float s[NT][2][4];
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[t][h][e] = 0.f;
+#pragma unroll
+            for (int b = 0; b < L::NB; ++b) {
+                constexpr int KW = L::CQ * L::EB / 4;              // words of the lane's channels of a key
+                uint32_t w[2][2][KW];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    const uint8_t* const at = sk + b * L::kBox + (n * 8 + g) * L::RB;
+                    uint32_t* const to = w[n >> 1][n & 1];
+#pragma unroll
+                    for (int u = 0; u < KW / 4; ++u)
+                        lds4(at + (L::RB == 128 ? ((2 * c + u) ^ g) * 16 : c * 16), to[4 * u], to[4 * u + 1], to[4 * u + 2], to[4 * u + 3]);
+                }
+#pragma unroll
+                for (int ks = 0; ks < L::CQ / 4; ++ks) {
+                    uint32_t a[2][4];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {              // rows g and g + 8 of the 16 keys
+                            const uint32_t x = w[h][k][kCodes ? ks : (2 * ks) % KW];
+                            if constexpr (kCodes) {
+                                a[h][k] = by_masks(true, ks) ? even_pair(x) : lo_half2(x);
+                                a[h][2 + k] = by_masks(true, ks) ? odd_pair(x) : hi_half2(x);
+                            } else {
+                                a[h][k] = x;
+                                a[h][2 + k] = w[h][k][(2 * ks + 1) % KW];
+                            }
+                        }
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const int s_i = b * (L::CQ / 4) + ks;
+#pragma unroll
+                        for (int x = kTerms - 1; x >= 0; --x) {
+                            uint32_t q0, q1;
+                            if constexpr (kHeldQ) {
+                                q0 = qf[x][s_i][0];
+                                q1 = qf[x][s_i][1];
+                            } else {
+                                lds2(q_at + x * kTermBytes + (s_i * NT + t) * 256, q0, q1);
+                            }
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) mma16816<kCodes>(s[t][h], a[h], q0, q1);
+                        }
+                    }
+                }
+            }
+            if constexpr (kCare) {
+                float z = 0.f;
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) z += s[t][h][e];
+                if (__any_sync(0xffffffffu, isnan(z))) {
+                    const Scores<NT> r = scores_of_infinities<D, NT>(sk, q_at, g, c);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) s[t][h][e] = r.x[t][h][e];
+                }
+            }
+            // scales: K's on the scores; V's relative to the unit that O counts in
+            float vs[2][2], shift = 1.f;
+            if constexpr (kCodes) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const float f = lds_f(ssc + (16 * h + 8 * k + g) * 4);
+                        vs[h][k] = lds_f(ssc + (kBlk + 16 * h + 8 * k + g) * 4);
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            s[t][h][2 * k] *= f;
+                            s[t][h][2 * k + 1] *= f;
+                        }
+                    }
+                uint32_t top = __float_as_uint(lds_f(ssc + (kBlk + lane) * 4)) & 0x7fffffffu;
+                if (top >= 0x7f800000u || (edge && !there(lane))) top = 0;
+                top = __reduce_max_sync(0xffffffffu, top);
+                const int u = max(unit, min((int)(top >> 23) - 126, 126));     // every scale below 2^u
+                shift = pow2i(unit - u);
+                unit = u;
+                const float inv = pow2i(-u);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) vs[h][k] *= inv;
+            }
+            uint32_t pf[NT][2][2];           // P^T as fragments, 16 keys each
+            bool moved = shift != 1.f;
+            float grow[NT][2];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const float2 rs = *reinterpret_cast<const float2*>(s_rs + t * 8 + 2 * c);
+                if (edge) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int end = s_end[t * 8 + 2 * c + k];
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) {
+                            const int j = n * 8 + g, key = key0 + j;
+                            const bool seen = key <= end && (!P.window || key > end - P.window) && (has >> (j >> 4) & 1);
+                            if (!seen) s[t][n >> 1][(n & 1) * 2 + k] = -INFINITY;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const float f = k ? rs.y : rs.x;
+                    float top = fmaxf(fmaxf(s[t][0][k], s[t][0][2 + k]), fmaxf(s[t][1][k], s[t][1][2 + k]));
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+                    const float high = fmaxf(m[t][k], fmaf(top, f, -top_weight<kCodes>()));
+                    const float base = high == -INFINITY ? 0.f : high;     // nothing seen yet: weights 2^-inf
+                    const float a = ex2f(m[t][k] - base);
+                    moved |= high != m[t][k];
+                    m[t][k] = high;
+                    grow[t][k] = a * shift;
+                    float sum = 0.f;
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) {
+                        float& x = s[t][n >> 1][(n & 1) * 2 + k];
+                        float p = ex2f(fmaf(x, f, -base));
+                        sum += p;
+                        // a hidden key's scale may be anything
+                        if constexpr (kCodes) p = edge && x == -INFINITY ? 0.f : p * vs[n >> 1][n & 1];
+                        x = p;
+                    }
+                    l[t][k] = fmaf(l[t][k], a, sum);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    pf[t][h][0] = transposed(pack2<kCodes>(s[t][h][0], s[t][h][1]));
+                    pf[t][h][1] = transposed(pack2<kCodes>(s[t][h][2], s[t][h][3]));
+                }
+            }
+            if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int n = 0; n < MT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[t][n][e] *= grow[t][e & 1];
+            }
+            if constexpr (kCare) set_aside<D>(const_cast<uint8_t*>(sv), key0, has, k_lo, k_hi, s_end, P.window, live, s_odd, lane);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int b = 0; b < L::NB; ++b) {
+                    constexpr int VW = L::CV * L::EB / 4;          // words of the lane's V of a key: 4 or 2
+                    uint32_t w[4][VW];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {                  // keys 2c, 2c + 1, 2c + 8, 2c + 9
+                        const int row = h * 16 + 2 * c + (k & 1) + (k >> 1) * 8;
+                        const uint8_t* const at = sv + b * L::kBox + row * L::RB;
+                        if constexpr (VW == 4) lds4(at + (g ^ (row & 7)) * 16, w[k][0], w[k][1], w[k][2], w[k][3]);
+                        else lds2(at + g * 8, w[k][0], w[k][1]);
+                        if (edge && !there(row))       // whatever lies there: 0 times it must be 0
+#pragma unroll
+                            for (int e = 0; e < VW; ++e) w[k][e] = 0;
+                    }
+                    // a[m]: channels 2m (rows g of the tile) and 2m + 1 (rows g + 8) of the lane's, four keys
+#pragma unroll
+                    for (int e = 0; e < VW; ++e) {
+                        constexpr int kTiles = kCodes ? 2 : 1;     // a word's channels in pairs
+                        uint32_t a[kTiles][4];
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {              // keys 2c, 2c + 1, then + 8
+                            const uint32_t x = w[2 * k][e], y = w[2 * k + 1][e];
+                            if constexpr (!kCodes) {
+                                a[0][2 * k] = __byte_perm(x, y, 0x5410);
+                                a[0][2 * k + 1] = __byte_perm(x, y, 0x7632);
+                            } else if (by_masks(true, e)) {
+                                const uint32_t ex = even_pair(x), ey = even_pair(y), ox = odd_pair(x), oy = odd_pair(y);
+                                a[0][2 * k] = __byte_perm(ex, ey, 0x5410);
+                                a[0][2 * k + 1] = __byte_perm(ox, oy, 0x5410);
+                                a[kTiles - 1][2 * k] = __byte_perm(ex, ey, 0x7632);
+                                a[kTiles - 1][2 * k + 1] = __byte_perm(ox, oy, 0x7632);
+                            } else {
+                                const uint32_t lo = __byte_perm(x, y, 0x5140), hi = __byte_perm(x, y, 0x7362);
+                                a[0][2 * k] = lo_half2(lo);
+                                a[0][2 * k + 1] = hi_half2(lo);
+                                a[kTiles - 1][2 * k] = lo_half2(hi);
+                                a[kTiles - 1][2 * k + 1] = hi_half2(hi);
+                            }
+                        }
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int n = 0; n < kTiles; ++n)
+                                mma16816<kCodes>(o[t][b * (L::CV / 2) + kTiles * e + n], a[n], pf[t][h][0], pf[t][h][1]);
+                    }
+                }
+            }
+            __syncwarp();                    // every lane has read the stage
+            const int next = i + kStages;
+            if (next < n_it && (next & 31) == 0) look_up(next);
+#pragma unroll
+            for (int k = 0; k + 1 < kStages; ++k) loaded[k] = loaded[k + 1];
+            loaded[kStages - 1] = next < n_it ? issue(next, stage) : 0u;
+            advance();
+            if constexpr (!kCodes && !kCare) {
+                if ((i & 7) == 7 || i + 1 == n_it) {
+                    float z[4] = {};         // zero, or NaN where a sum is not finite
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                        for (int n = 0; n < MT; ++n)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) z[e] = fmaf(o[t][n][e], 0.f, z[e]);
+                        z[t & 3] = fmaf(l[t][0] + l[t][1], 0.f, z[t & 3]);
+                    }
+                    if (__any_sync(0xffffffffu, (z[0] + z[1]) + (z[2] + z[3]) != 0.f)) return i + 1;
+                }
+            }
+        }
+        return -1;
+    };
+    const int stopped = blocks(std::false_type{});
+    if constexpr (!kCodes)
+        if (stopped >= 0) {
+            for (int k = min(kStages, n_it - stopped); k > 0; --k) {         // what is on its way lands first
+                mbar_wait(smem_u32(&s_full[warp][stage]), parity, P.err, &s_abort);
+                advance();
+            }
+            __syncwarp();
+            start();
+            look_up(0);
+#pragma unroll
+            for (int k = 0; k < kStages; ++k) loaded[k] = k < n_it ? issue(k, (stage + k) % kStages) : 0u;
+            blocks(std::true_type{});
+        }
 
     // the warps' results join: O in units of one, rows [row][channel], lines of 16 bytes swapped within
     // groups of eight so that lanes meet fewer banks
@@ -668,37 +819,21 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
             x.w = fmaf(y.w, a, x.w);
         }
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        if constexpr (!kCodes)           // infinity or NaN in V may belong to keys that this row does not see
-            if (!(fabsf(x.x) <= 3.0e38f && fabsf(x.y) <= 3.0e38f && fabsf(x.z) <= 3.0e38f && fabsf(x.w) <= 3.0e38f))
-                atomicOr(reinterpret_cast<unsigned long long*>(&s_bad), 1ull << row);
         if (sum == 0.f) x.x = x.y = x.z = x.w = none(row);
         else x = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
-        put(row, f, x, sum == 0.f ? -INFINITY : top + log2f(sum));
-    }
-    if constexpr (!kCodes) {
-        __syncthreads();
-        for (uint64_t bad = s_bad; bad; bad &= bad - 1) {      // those rows again, key by key
-            const int row = __ffsll((long long)bad) - 1;
-            if (row % kWarps != warp) continue;
-            const int end = R.n_keys - R.nq + (row0 + row) / G;
-            const int lo = max(b0 * kBlk, P.window ? end - P.window + 1 : 0), hi = min(b1 * kBlk, end + 1);
-            float q[D / 32], x[D / 32], rm, rl;
-            lane_query<T, D>(P, R.q0 + (row0 + row) / G, hk * G + (row0 + row) % G, lane, q);
-            row_attend<T, D, kCodes>(P, q, R.row, hk, lo, hi, lane, rm, rl, x);
-            const float inv = rl == 0.f ? 0.f : 1.f / rl;
-            if (rl == 0.f)
-#pragma unroll
-                for (float& e : x) e += none(row);
-            float4 y = make_float4(x[0] * inv, x[1] * inv, 0.f, 0.f);
-            if constexpr (D == 128) {
-                y.z = x[2] * inv;
-                y.w = x[3] * inv;
-                put(row, lane, y, rl == 0.f ? -INFINITY : rm + log2f(rl));
-            } else {
-                const float z = __shfl_down_sync(0xffffffffu, y.x, 1), w = __shfl_down_sync(0xffffffffu, y.y, 1);
-                if (!(lane & 1)) put(row, lane / 2, make_float4(y.x, y.y, z, w), rl == 0.f ? -INFINITY : rm + log2f(rl));
+        if constexpr (!kCodes) {         // values that are not finite, of keys that the row sees
+            const uint32_t odd = s_odd[row * (D / 4) + f];
+            if (odd != 0u && sum > 0.f && sum < INFINITY) {
+                auto take_in = [&](float& y, uint32_t is) {
+                    if (is != 0u) y = is == 1u ? INFINITY : is == 2u ? -INFINITY : __uint_as_float(0x7fc00000u);
+                };
+                take_in(x.x, odd & 7u);
+                take_in(x.y, odd >> 8 & 7u);
+                take_in(x.z, odd >> 16 & 7u);
+                take_in(x.w, odd >> 24 & 7u);
             }
         }
+        put(row, f, x, sum == 0.f ? -INFINITY : top + log2f(sum));
     }
     if (whole) return;
     // the stretch that ends last joins them all: every partial is visible before its ticket is taken

@@ -88,3 +88,40 @@ def test_a_chunk_over_one_bad_row_takes_its_usual_time(shape, key):
         assert out[..., 3].isnan().any()
     finally:
         c2kv.c2kv_destroy(ctx)
+
+
+@pytest.mark.parametrize("window", [0, 90])
+@pytest.mark.parametrize("nq,keys", [(1, 300), (3, 300), (10, 2000), (5, 9000)])
+@pytest.mark.parametrize("shape", [*SHAPES[:2], ("bf16", "native", 28, 4, 128), ("bf16", "native", 4, 4, 64)], ids=lambda s: "-".join(map(str, s)))
+def test_every_channel_is_its_own_of_few_rows(shape, nq, keys, window):
+    test_every_channel_is_its_own(shape, nq, keys, window)
+
+
+@pytest.mark.parametrize("nq,batch", [(1, 64), (4, 64), (1, 1)])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "-".join(map(str, s)))
+def test_few_rows_over_one_bad_row_take_their_usual_time(shape, nq, batch):
+    """Requests over the same 8192 rows; a row that is not finite may make them twice as long."""
+    dtype, fmt, hq, hkv, d = shape
+    rng = np.random.default_rng(7)
+    c2kv, ctx = P.lib(), P.context(dtype, hq, hkv, d)
+    try:
+        pg = P.Paged(rng, dtype, fmt, hkv, d, 32, [8192], fill=0.5)
+        q = torch.randn((nq * batch, hq, d), device="cuda").to(P.TDT[dtype])
+        out, table, pages = torch.empty_like(q), pg.table.repeat(batch, 1), pg.pages()
+
+        def time():
+            took = []
+            for _ in range(8):
+                a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+                a.record()
+                c2kv.c2kv_paged_attend(ctx, pages, table, [nq * i for i in range(batch + 1)], [8192] * batch, q, out)
+                b.record()
+                torch.cuda.synchronize()
+                took.append(a.elapsed_time(b))
+            return min(took)
+        usual = time()
+        _set(pg, 5000, 3 if fmt == "native" else None, NAN)
+        assert time() <= 2 * usual
+        assert out[..., 3].isnan().all()
+    finally:
+        c2kv.c2kv_destroy(ctx)
