@@ -12,7 +12,9 @@ namespace {
 // Measured (us, mma.sync / tcgen05; 32 / 8 heads, 64 and 80 rows; 1 request of 30000 rows, 8 of 4000, 16 of
 // 500): 8-bit pages of 128 channels 60 / 92 and 74 / 92, 62 / 78 and 96 / 78, 23 / 34 and 39 / 33; 16-bit
 // ones 91 / 100 and 126 / 100, 97 / 90 and 185 / 90, 44 / 37 and 62 / 38; 16-bit of 64 channels 44 / 65 and
-// 56 / 66, 47 / 60 and 75 / 61, 19 / 27 and 30 / 27.
+// 56 / 66, 47 / 60 and 75 / 61, 19 / 27 and 30 / 27.  One limit for all of them: it is right for 8-bit pages and
+// for heads of 64 channels, and late for 16-bit pages of 128 channels, where 64 rows of eight and of sixteen
+// requests take 8 and 19 % longer than on tcgen05.
 constexpr int kMmaRows = 64;
 
 // The same of fp32 contexts, and the keys that some request has to see for it: the lanes' kernel reads keys
@@ -21,7 +23,8 @@ constexpr int kMmaRows = 64;
 // and 16 rows: 27 requests of 1381 keys 66 / 94 and 186 / 241, one of 30000 49 / 247 and 145 / 368, 16 of 9000
 // 191 / 403 and 703 / 909; 24 rows of 8 requests of 700 keys 75 / 63.  8 / 8 heads of 64, 4 and 8 rows: 42 / 54
 // and 67 / 77, 38 / 151 and 59 / 191, 135 / 182 and 295 / 277.  One request of 200 keys, any: 13 / 12, and four
-// of 300: 14 / 15.
+// of 300: 14 / 15.  The limits go by a request's rows alone, so as to lose nowhere; heads of 64 channels with
+// eight rows over one long context would gain most from another (59 where the tiles take 191).
 constexpr int lane_rows(int d) { return d == 128 ? 16 : 4; }
 constexpr int kLaneKeys = 256;
 

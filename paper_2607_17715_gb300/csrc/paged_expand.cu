@@ -17,7 +17,7 @@
 // row is not touched by it (0 times it is NaN), and one that does takes them in at the end (paged_tc.cu).
 //
 // Bytes bound it: a page's read once, two written for each value.  Measured: 32768 rows of codes of 8 heads,
-// 67 MB to 134 MB, in 38 us (5.3 TB/s).
+// 67 MB to 134 MB, in 39 us (5.2 TB/s).
 #include "paged.cuh"
 #include "ptx.cuh"
 #include "vec16.cuh"

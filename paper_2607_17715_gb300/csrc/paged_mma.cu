@@ -35,7 +35,7 @@
 // channels that lie next to one another in its row: 16-byte shared loads, conflict-free under the
 // 128-byte swizzle, with no transpose of V (a lane loads the same channels of four keys and pairs them).
 //
-// Measured (32 / 8 heads): one token over 131000 rows of 16 bits, 537 MB in 86 us (6.2 TB/s); one token of
+// Measured (32 / 8 heads): one token over 131000 rows of 16 bits, 537 MB in 87 us (6.2 TB/s); one token of
 // 16 requests over 500 to 2000 rows of codes, 37 MB in 12 us, of which first loads and the two joins
 // are half; five tokens of eight requests with groups of eight (40 rows), 46 MB in 30 us, bound by the issue of
 // the warps' chains: each of two tiles of 24 rows converts the codes for itself.

@@ -10,11 +10,11 @@
 // exponent (the running reference is of score + offset, so that weights of every tile fit f16; the sum of
 // weights takes the offset back).  Queries are f16 too, each row scaled by a power of two.
 //
-// Measured: 2048 tokens over 30720 rows (32 / 8 heads) 846 us with the tiles' making and the join, 1.26
+// Measured: 2048 tokens over 30720 rows (32 / 8 heads) 866 us with the tiles' making and the join, 1.23
 // PFLOP/s; a key tile takes a CTA 1.7 us where its products alone would take 1.33 (the weights of a tile
 // lie where its next scores go, so a tile's softmax and its own products follow one another, and only the
 // other tile's run beside them).  A CTA's start and end are 8 us: chunks of four prompts, 64 equal units on
-// 152 SMs, 84 us.
+// 152 SMs, 86 us.
 #include "paged.cuh"
 #include "paged_row.cuh"
 #include "per_device.cuh"

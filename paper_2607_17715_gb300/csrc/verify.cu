@@ -12,8 +12,8 @@
 // shared memory, and the warp whose stretch holds the goal reads that stretch again (from L2).  Clusters
 // are as large as keeps them all on the GPU at once: 64 requests in clusters of 8 took two rounds.
 //
-// Measured: 64 requests over 131072 tokens, 67 MB in 15 us (4.5 TB/s); one over 32000, 6 us, nearly all of it
-// the chain, and the host's launch.
+// Measured: 64 requests over 131072 tokens, 67 MB in 15 us (4.5 TB/s); one over 32000, 7.5 us, nearly all of it
+// the chain, and the host's checks and launch.
 #include "paged.cuh"
 #include "per_device.cuh"
 
