@@ -225,6 +225,7 @@ __device__ __noinline__ Scores<NT> scores_of_infinities(const uint8_t* sk, const
 
 // Values of a block's V (16 bits) that are not finite become zero in shared memory, and are noted for the rows
 // that see them: a byte a channel in odd[row][D / 4], 1 infinity, 2 minus it, 4 NaN.  `end`: the rows' last keys.
+// A key with an infinity of K too scores -inf where the row's sum is a number: 0 times its infinities is NaN.
 template <int D>
 __device__ __noinline__ void set_aside(uint8_t* sv, int key0, uint32_t has, int k_lo, int k_hi, const int* end, int window, int live, uint32_t* odd,
                                        int lane) {
@@ -238,17 +239,20 @@ __device__ __noinline__ void set_aside(uint8_t* sv, int key0, uint32_t has, int 
         any |= not_finite(w.x) | not_finite(w.y);
     }
     if (!__any_sync(0xffffffffu, any != 0u)) return;
+#pragma unroll 1
     for (int j = lane / kLanes; j < kBlk; j += kStep) {
         const int key = key0 + j;
-        if (key < k_lo || key >= k_hi || !(has >> (j >> 4) & 1u)) continue;
         uint2* const at = reinterpret_cast<uint2*>(sv + b * L::kBox + j * L::RB) + u;
-        const uint2 w = *at;
+        const uint2 w = *at, y = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(at) - L::kSide);   // (K's)
+        const uint32_t of_k = __ballot_sync(0xffffffffu, (not_finite(y.x) | not_finite(y.y)) != 0u) >> (lane & ~(kLanes - 1));
+        if (key < k_lo || key >= k_hi || !(has >> (j >> 4) & 1u)) continue;
         if ((not_finite(w.x) | not_finite(w.y)) == 0u) continue;
+        const bool no_weight = (of_k & (0xffffffffu >> (32 - kLanes))) != 0u;
         uint32_t is = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const uint32_t x = (e < 2 ? w.x : w.y) >> (16 * (e & 1)) & 0xffffu;
-            if ((x & 0x7f80u) == 0x7f80u) is |= ((x & 0x7fu) ? 4u : (x & 0x8000u) ? 2u : 1u) << (8 * e);
+            if ((x & 0x7f80u) == 0x7f80u) is |= ((x & 0x7fu) || no_weight ? 4u : (x & 0x8000u) ? 2u : 1u) << (8 * e);
         }
         const int word = b * 16 + ((u / 2) ^ (j & 7)) * 2 + u % 2;       // (16-byte lines of a row are swapped)
         for (int row = 0; row < live; ++row)
@@ -823,7 +827,7 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
         else x = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
         if constexpr (!kCodes) {         // values that are not finite, of keys that the row sees
             const uint32_t odd = s_odd[row * (D / 4) + f];
-            if (odd != 0u && sum > 0.f && sum < INFINITY) {
+            if (odd != 0u && sum < INFINITY) {
                 auto take_in = [&](float& y, uint32_t is) {
                     if (is != 0u) y = is == 1u ? INFINITY : is == 2u ? -INFINITY : __uint_as_float(0x7fc00000u);
                 };

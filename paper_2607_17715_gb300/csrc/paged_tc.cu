@@ -407,10 +407,19 @@ __device__ __forceinline__ void take_in(const TcLaunch<kReq>& X, const Item& w, 
                     float v[E];
                     lane_row<T, D, kCodes>(P.pg.v, page * P.pg.page_stride + in_page * D,
                                            kCodes ? ld_after(P.pg.v_scale + page * P.pg.scale_stride + in_page) : 1.f, lane, v);
+                    // a key with an infinity of K too scores -inf, the row's sum being a number: 0 times it is NaN
+                    float y[E];
+                    lane_row<T, D, kCodes>(P.pg.k, page * P.pg.page_stride + in_page * D,
+                                           kCodes ? ld_after(P.pg.k_scale + page * P.pg.scale_stride + in_page) : 1.f, lane, y);
+                    bool odd_k = false;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) odd_k = odd_k || !(fabsf(y[e]) < CUDART_INF_F);
+                    const bool no_weight = __any_sync(0xffffffffu, odd_k);
                     uint32_t is = 0;
 #pragma unroll
                     for (int e = 0; e < E; ++e)
-                        is |= (v[e] == CUDART_INF_F ? 1u : v[e] == -CUDART_INF_F ? 2u : isnan(v[e]) ? 4u : 0u) << (8 * e);
+                        if (!(fabsf(v[e]) < CUDART_INF_F))
+                            is |= (isnan(v[e]) || no_weight ? 4u : v[e] > 0.f ? 1u : 2u) << (8 * e);
                     if (rows == bad) {
                         common |= is;
                         rest = __any_sync(0xffffffffu, (common & kNan) != kNan);
@@ -617,7 +626,7 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
         if (!whole) X.part_lse[(int64_t)blockIdx.x * kPair + row] = lse2;
         else if (P.lse) P.lse[(int64_t)h * P.n_tokens + tok] = lse2 * 0.69314718055994531f;
     }
-    const uint32_t bad = __ballot_sync(0xffffffffu, there && touched && l > 0.f && l < CUDART_INF_F);
+    const uint32_t bad = __ballot_sync(0xffffffffu, there && touched && l < CUDART_INF_F);
     if (bad) take_in<D, kCodes>(X, w, bad, start, end, x * BM + quad * 32, lane, q_tiles);
 }
 

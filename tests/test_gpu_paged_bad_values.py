@@ -125,3 +125,36 @@ def test_few_rows_over_one_bad_row_take_their_usual_time(shape, nq, batch):
         assert out[..., 3].isnan().all()
     finally:
         c2kv.c2kv_destroy(ctx)
+
+
+@pytest.mark.parametrize("nq,keys", [(1, 300), (3, 300), (5, 9000), (140, 200), (140, 9000)])
+@pytest.mark.parametrize("shape", [*SHAPES[:2], ("f32", "native", 16, 4, 64), ("f32", "native", 4, 4, 128)], ids=lambda s: "-".join(map(str, s)))
+def test_infinite_values_of_keys_of_no_weight(shape, nq, keys):
+    """A key that scores -inf has weight 0, and 0 times an infinity is NaN: for the rows that see it, in the
+    channels where its value is one."""
+    dtype, fmt, hq, hkv, d = shape
+    rng = np.random.default_rng(6)
+    c2kv, ctx = P.lib(), P.context(dtype, hq, hkv, d)
+    try:
+        pg = P.Paged(rng, dtype, fmt, hkv, d, 32, [keys])
+        pg.fill_rows(rng)
+        for key, channel, value in ((4, 5, INF), (keys // 2, 6, -INF), (keys - 1, 7, INF), (keys - 1, 8, NAN)):
+            _set(pg, key, channel, value)
+            pg.k[int(pg.table_np[0, key // 32]), :, key % 32, 3] = -INF
+        _set(pg, 40, 9, INF)                                  # and one of a key that has its weight
+        q = torch.from_numpy(rng.standard_normal((nq, hq, d)).astype(np.float32))
+        q[..., 3] = q[..., 3].abs() + 0.1
+        q = q.to(P.TDT[dtype]).cuda()
+        out = torch.full_like(q, 7.0)
+        c2kv.c2kv_paged_attend(ctx, pg.pages(), pg.table, [0, nq], [keys], q, out)
+        c2kv.c2kv_sync(ctx)
+        k, v = (orc.rows_of(x, pg.table_np, 0, 0, keys, 32) for x in pg.host())
+        with np.errstate(invalid="ignore"):
+            want, _ = orc.attend(q.double().cpu().numpy(), k, v, keys)
+        got = out.float().cpu().numpy()
+        assert np.isnan(want[-1][..., [5, 6, 7, 8]]).all() and np.isposinf(want[..., 9]).all()
+        assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isposinf(got), np.isposinf(want))
+        fine = np.isfinite(want)
+        assert np.all(np.abs(got - want)[fine] <= TOL[dtype] + TOL[dtype] * np.abs(want[fine]))
+    finally:
+        c2kv.c2kv_destroy(ctx)
