@@ -503,6 +503,31 @@ c2kv_status c2kv_paged_attend(c2kv_ctx* ctx, const c2kv_pages* pages, int32_t ba
                               const int32_t* turn, void* out, float* lse);
 
 /*
+ * c2kv_paged_attend_tree -- the same attention for drafted tokens that branch.  Tokens [tree_ptr[r],
+ * tree_ptr[r + 1]) are the nodes of request r's tree, its newest rows in that order (append first): node i
+ * is row n_keys[r] - n + i of its n.  parent[t] is the place of token t's parent among its request's nodes,
+ * before its own, or -1 for a root; node 0 is commonly the last token kept, and the drafts descend from it.
+ * A node sees the rows before the tree, the nodes on its way to its root, and itself; with a window, the
+ * last `window` of that path:
+ *     O[t, h] = softmax_j( R(turn_t) Q_t,h . K_j,h/G / sqrt(d) ) V_j,h/G
+ *               over rows j < x with j > x + depth_t - window, and rows x + a of the first `window` nodes a
+ *               from t up                                     (x = n_keys - n, roots have depth 0)
+ * Siblings have one position: turn says it, x + depth_t where rows stand for one position each.  A chain
+ * (parent = node before) gives what c2kv_paged_attend gives.
+ *   tree_ptr     : host int32 [B + 1], non-decreasing from 0; at most 512 nodes a request, and at most its
+ *                  rows; a request may have none.
+ *   n_keys, window, q, q_stride, turn, out, lse : as c2kv_paged_attend.
+ *   parent       : device int32 [T].
+ * A parent outside [-1, its child) is refused by the kernel: the node is taken for a root, and c2kv_sync
+ * returns ERR_DEVICE_BOUNDS, as for a page number outside [0, n_pages).  Recorded by the trace as
+ * C2KV_PROF_ATTN.  Errors: as c2kv_paged_attend, and ERR_UNSUPPORTED (more than 512 nodes).
+ */
+c2kv_status c2kv_paged_attend_tree(c2kv_ctx* ctx, const c2kv_pages* pages, int32_t batch, const int32_t* table,
+                                   int32_t table_width, int64_t table_stride, const int32_t* tree_ptr, const int32_t* n_keys,
+                                   const int32_t* parent, int32_t window, const void* q, int64_t q_stride, const int32_t* turn,
+                                   void* out, float* lse);
+
+/*
  * c2kv_verify_drafts -- how many of each request's drafted tokens the target's probabilities
  * accept, and the token that follows them, so that the tokens kept are distributed as the target's
  * own.  Draft t (token x, row t of q) is accepted while u_accept[t] * q[t][x] < p[row][x] (the

@@ -8,6 +8,7 @@ from __future__ import annotations
 import concurrent.futures
 import glob
 import os
+import re
 import shutil
 import subprocess
 import sys
@@ -37,6 +38,13 @@ def _newest_header() -> float:
     return max((os.path.getmtime(h) for h in hdrs), default=0.0)
 
 
+def _newest_source(src: str) -> float:
+    """The source, and the sources that it includes (one compiled again for another case)."""
+    with open(src) as f:
+        more = re.findall(r'#include "(\w+\.cu)"', f.read())
+    return max(os.path.getmtime(p) for p in [src] + [os.path.join(CSRC, m) for m in more])
+
+
 def _compile(nvcc: str, src: str, obj: str) -> str:
     cmd = [nvcc, *NVCC_FLAGS, "-c", src, "-o", obj]
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -56,11 +64,11 @@ def build(verbose: bool = False) -> str:
     for src in srcs:
         obj = os.path.join(BUILD_DIR, os.path.basename(src)[:-3] + ".o")
         objs.append(obj)
-        if (not os.path.exists(obj) or os.path.getmtime(obj) < os.path.getmtime(src)
+        if (not os.path.exists(obj) or os.path.getmtime(obj) < _newest_source(src)
                 or os.path.getmtime(obj) < hdr_time):
             jobs.append((src, obj))
     if jobs:
-        with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, len(jobs))) as ex:
+        with concurrent.futures.ThreadPoolExecutor(max_workers=min(max(8, os.cpu_count() or 1), len(jobs))) as ex:
             futs = {ex.submit(_compile, nvcc, s, o): s for s, o in jobs}
             for fut in concurrent.futures.as_completed(futs):
                 log = fut.result()

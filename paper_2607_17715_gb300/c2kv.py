@@ -101,6 +101,7 @@ _SIGS = {
     "c2kv_paged_append": (_I32, [_VP, _VP, _I32, _VP, _I32, _I64, _VP, _VP, _VP, _VP, _I64, _VP]),
     "c2kv_paged_gather": (_I32, [_VP, _VP, _I32, _VP, _I32, _I64, _VP, _VP, _VP, _VP, _I64, _VP]),
     "c2kv_paged_attend": (_I32, [_VP, _VP, _I32, _VP, _I32, _I64, _VP, _VP, _I32, _VP, _I64, _VP, _VP, _VP]),
+    "c2kv_paged_attend_tree": (_I32, [_VP, _VP, _I32, _VP, _I32, _I64, _VP, _VP, _VP, _I32, _VP, _I64, _VP, _VP, _VP]),
     "c2kv_verify_drafts": (_I32, [_VP, _I32, _VP, _I32, _VP, _VP, _I64, _VP, _I64, _VP, _VP, _VP, _VP]),
     "c2kv_cache_release": (_I32, [_VP, _VP]),
     "c2kv_sync": (_I32, [_VP]),
@@ -447,8 +448,9 @@ def c2kv_paged_gather(ctx, pages, table, row_ptr, start, k_out, v_out, turn=None
                                   _pair_stride(ctx, pages, k_out, v_out, t), _vector(turn, t, "turn", _torch().int32)), ctx)
 
 
-def c2kv_paged_attend(ctx, pages, table, q_ptr, n_keys, q, out, lse=None, turn=None, window=0):
-    """Attention of each request's newest tokens q [T, Hq, d] over its n_keys rows."""
+def _attend_args(ctx, pages, table, q_ptr, n_keys, q, out, lse):
+    """What the two attentions have in common: the host arrays (kept by the first result), the table, and where
+    the rows lie; T last."""
     ptr, ptr_p, n = _i32_at(q_ptr)
     nk, nk_p, m = _i32_at(n_keys)
     tb, w, ts = _table(table, n - 1, m)
@@ -466,8 +468,23 @@ def c2kv_paged_attend(ctx, pages, table, q_ptr, n_keys, q, out, lse=None, turn=N
         _of_type(lse, _torch().float32, "lse")
         if not (lse.is_contiguous() and (lse.shape == (hq, t) or lse.dim() == 1 and lse.shape[0] >= hq * t)):
             raise ValueError(f"lse must be dense, [{hq}, {t}]")
-    _check(_lib.c2kv_paged_attend(ctx, pages.address, m, tb, w, ts, ptr_p, nk_p, window, q.data_ptr(), stride,
-                                  _vector(turn, t, "turn", _torch().int32), out.data_ptr() if tensor else _ptr(out), _ptr(lse)), ctx)
+    return (ptr, nk), (m, tb, w, ts, ptr_p, nk_p), q.data_ptr(), stride, out.data_ptr() if tensor else _ptr(out), _ptr(lse), t
+
+
+def c2kv_paged_attend(ctx, pages, table, q_ptr, n_keys, q, out, lse=None, turn=None, window=0):
+    """Attention of each request's newest tokens q [T, Hq, d] over its n_keys rows."""
+    keep, host, q_at, stride, out_at, lse_at, t = _attend_args(ctx, pages, table, q_ptr, n_keys, q, out, lse)
+    _check(_lib.c2kv_paged_attend(ctx, pages.address, *host, window, q_at, stride, _vector(turn, t, "turn", _torch().int32), out_at,
+                                  lse_at), ctx)
+
+
+def c2kv_paged_attend_tree(ctx, pages, table, tree_ptr, n_keys, parent, q, out, lse=None, turn=None, window=0):
+    """Attention of each request's newest tokens q [T, Hq, d], the nodes of trees, over its n_keys rows: parent [T]
+    among a request's nodes, -1 for a root."""
+    keep, host, q_at, stride, out_at, lse_at, t = _attend_args(ctx, pages, table, tree_ptr, n_keys, q, out, lse)
+    i32 = _torch().int32
+    _check(_lib.c2kv_paged_attend_tree(ctx, pages.address, *host, _vector(parent, t, "parent", i32), window, q_at, stride,
+                                       _vector(turn, t, "turn", i32), out_at, lse_at), ctx)
 
 
 def c2kv_verify_drafts(ctx, draft_ptr, tokens, p, q, u_accept, u_next, n_accepted, next_token):

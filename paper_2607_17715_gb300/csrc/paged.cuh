@@ -86,6 +86,7 @@ struct PagedAttn {
     void* out;               // [T][Hq][d]
     float* lse;              // [Hq][T] natural log, or null
     const int32_t* turn;     // [T] positions that the queries turn by, or null
+    const int32_t* parent;   // [T] (trees) the queries' parents among their request's, -1 for a root
     int32_t* err;
     int64_t q_stride;
     int64_t n_tokens;        // T
@@ -106,6 +107,7 @@ struct PagedAttnCall {
     void* out;
     float* lse;
     const int32_t* turn;
+    const int32_t* parent;   // null: each request's queries follow one another
     int32_t* err;
     int64_t q_stride;
     int32_t hq;
@@ -123,6 +125,10 @@ cudaError_t launch_paged_simt(const PagedAttnCall& c, const PagedReq* req, int n
 cudaError_t launch_paged_lane(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
 // bf16 queries of n requests on mma.sync (paged_mma.cu).
 cudaError_t launch_paged_mma(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
+// The same of trees (paged_*_tree.cu): what the three launchers call where there are parents.
+cudaError_t launch_paged_simt_tree(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
+cudaError_t launch_paged_lane_tree(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
+cudaError_t launch_paged_mma_tree(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
 
 // Tensor map of pages [n_pages][Hkv][page_size][d], elements of 16 bits or codes of 8.
 bool encode_page_map(CUtensorMap* tm, const void* base, const PageView& pg, int hkv, int d, bool codes, int box_channels,
@@ -152,6 +158,7 @@ struct PagedExpandCall {
 cudaError_t launch_paged_expand(const PagedExpandCall& c, int d, bool codes, cudaStream_t s);
 // bf16 queries of n requests over their key tiles on tcgen05 (paged_tc.cu).
 cudaError_t launch_paged_tc(const PagedAttnCall& c, const KeyTiles& tiles, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
+cudaError_t launch_paged_tc_tree(const PagedAttnCall& c, const KeyTiles& tiles, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
 
 template <int kReq>
 void fill_paged(PagedAttn<kReq>& P, const PagedAttnCall& c, int d, const PagedReq* req, int n) {
@@ -160,6 +167,7 @@ void fill_paged(PagedAttn<kReq>& P, const PagedAttnCall& c, int d, const PagedRe
     P.out = c.out;
     P.lse = c.lse;
     P.turn = c.turn;
+    P.parent = c.parent;
     P.err = c.err;
     P.q_stride = c.q_stride;
     P.n_tokens = c.ptr[c.batch];
@@ -182,11 +190,50 @@ __device__ __forceinline__ bool any_page(const PageView& pg, int r, int lo, int 
     }
     return false;
 }
-// The output of a row whose weights' sum is zero, its last key being `end`: zero where it sees no key, and no
+// Trees (c2kv_paged_attend_tree): the queries of a request are the nodes of trees, parents before children, and
+// node i's key is row `before` + i.  A node sees the rows before the tree, the nodes on its way to its root and
+// itself; with a window, the last `window` rows of that path.
+constexpr int kTreeMost = 512;           // nodes of a request: a bit a node in shared memory for every query row
+constexpr int kTreeWords = kTreeMost / 32;
+
+// f(node) for node i and those above it that it sees, by the parents of its request; returns i's depth.  A parent
+// that is none of the nodes before its child is refused, and the child a root: the way always ends.
+template <class F>
+__device__ __forceinline__ int tree_way(const int32_t* parent, int i, int window, int32_t* err, const F& f) {
+    int depth = 0;
+    for (;; ++depth) {
+        if (!window || depth < window) f(i);
+        const int p = parent[i];
+        if (p < -1 || p >= i) atomicOr(err, 1);
+        if (p < 0 || p >= i) return depth;
+        i = p;
+    }
+}
+// What a node sees as a bit a node (bits[kTreeWords], zero before), and the last row before the tree that it does
+// not see (-1: it sees all of them).
+__device__ __forceinline__ int tree_bits(const int32_t* parent, int i, int before, int window, int32_t* err, uint32_t* bits) {
+    const int depth = tree_way(parent, i, window, err, [&](int j) { bits[j >> 5] |= 1u << (j & 31); });
+    return window ? max(-1, min(before + depth - window, before - 1)) : -1;
+}
+__device__ __forceinline__ bool tree_sees(int key, int before, int start, const uint32_t* bits) {
+    if (key < before) return key > start;
+    const int j = key - before;
+    return j < kTreeMost && (bits[j >> 5] >> (j & 31) & 1u);
+}
+
+// The output of a row whose weights' sum is zero, of query `tok` of the request: zero where it sees no key, and no
 // number where every score that it sees is -inf.
-template <int kReq>
-__device__ __forceinline__ float of_no_weight(const PagedAttn<kReq>& P, int r, int end) {
-    return any_page(P.pg, r, P.window ? max(0, end - P.window + 1) : 0, end + 1) ? __uint_as_float(0x7fc00000u) : 0.f;
+template <bool kTree, int kReq>
+__device__ __forceinline__ float of_no_weight(const PagedAttn<kReq>& P, const PagedReq& R, int tok) {
+    const int before = R.n_keys - R.nq, end = before + tok;
+    bool any = false;
+    if constexpr (kTree) {
+        const int depth = tree_way(P.parent + R.q0, tok, P.window, P.err, [&](int j) { any = any || any_page(P.pg, R.row, before + j, before + j + 1); });
+        any = any || any_page(P.pg, R.row, P.window ? max(0, before + depth - P.window + 1) : 0, before);
+    } else {
+        any = any_page(P.pg, R.row, P.window ? max(0, end - P.window + 1) : 0, end + 1);
+    }
+    return any ? __uint_as_float(0x7fc00000u) : 0.f;
 }
 
 // Drafted tokens against the target's probabilities (verify.cu).

@@ -95,7 +95,7 @@ struct LaneRing {
     }
 };
 
-template <int D, bool kCodes, int NR>
+template <int D, bool kCodes, int NR, bool kTree>
 __global__ void __launch_bounds__(kLaneThreads, lane_ctas(D)) paged_lane_kernel(const __grid_constant__ LaneLaunch X) {
     using Ring = LaneRing<D, kCodes>;
     constexpr int C = Ring::C, kDepth = Ring::kDepth, kGroups = kLaneBlk / 4;
@@ -105,6 +105,8 @@ __global__ void __launch_bounds__(kLaneThreads, lane_ctas(D)) paged_lane_kernel(
     __shared__ __align__(16) float s_o[kLaneWarps][NR][D];
     __shared__ float s_m[kLaneWarps][NR], s_l[kLaneWarps][NR];
     __shared__ bool s_last;
+    __shared__ uint32_t s_bits[kTree ? NR * kTreeWords : 1];
+    __shared__ int s_start[NR];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, sub = lane / 8, i8 = lane % 8;
     int r = 0;
     for (int hi = P.batch; hi - r > 1;) {
@@ -123,7 +125,8 @@ __global__ void __launch_bounds__(kLaneThreads, lane_ctas(D)) paged_lane_kernel(
     int end[NR];
 #pragma unroll
     for (int k = 0; k < NR; ++k) end[k] = R.n_keys - R.nq + (row0 + min(k, live - 1)) / G;
-    const int k_hi = max(0, end[NR - 1] + 1), k_lo = P.window ? max(0, end[0] - P.window + 1) : 0;
+    const int before = R.n_keys - R.nq;
+    const int k_hi = max(0, end[NR - 1] + 1), k_lo = P.window ? max(0, (kTree ? before : end[0]) - P.window + 1) : 0;
     const int blk_lo = k_lo / kLaneBlk, blocks = max(0, (k_hi + kLaneBlk - 1) / kLaneBlk - blk_lo);
     const int b0 = blk_lo + (int)((int64_t)blocks * split / R.splits), b1 = blk_lo + (int)((int64_t)blocks * (split + 1) / R.splits);
     const int size = 1 << P.pg.page_shift;
@@ -175,6 +178,14 @@ __global__ void __launch_bounds__(kLaneThreads, lane_ctas(D)) paged_lane_kernel(
 #pragma unroll 1
     for (int n = 0; n < kDepth - kPair; ++n) ask(n);
 
+    if constexpr (kTree) {
+        if (threadIdx.x < NR) {          // the rows' ways through the tree
+            const int row = threadIdx.x;
+#pragma unroll
+            for (int i = 0; i < kTreeWords; ++i) s_bits[row * kTreeWords + i] = 0u;
+            s_start[row] = tree_bits(P.parent + R.q0, (row0 + min(row, live - 1)) / G, before, P.window, P.err, s_bits + row * kTreeWords);
+        }
+    }
     // the queries, turned, while the first keys are on their way
     for (int k = threadIdx.x; k < NR * (D / 2); k += kLaneThreads) {
         const int row = min(k / (D / 2), live - 1), c = k % (D / 2);
@@ -189,6 +200,14 @@ __global__ void __launch_bounds__(kLaneThreads, lane_ctas(D)) paged_lane_kernel(
         s_q[k / (D / 2)][c + D / 2] = hi;
     }
     __syncthreads();
+    if constexpr (kTree) {               // (`end`: the last row before the tree that a row does not see)
+#pragma unroll
+        for (int k = 0; k < NR; ++k) end[k] = s_start[k];
+    }
+    auto sees_key = [&](int k, int key) {
+        if constexpr (kTree) return tree_sees(key, before, end[k], s_bits + k * kTreeWords);
+        else return key <= end[k] && (!P.window || key > end[k] - P.window);
+    };
     float q[NR][C], o[NR][C], m[NR], l[NR];
 #pragma unroll
     for (int k = 0; k < NR; ++k) {
@@ -220,7 +239,7 @@ __global__ void __launch_bounds__(kLaneThreads, lane_ctas(D)) paged_lane_kernel(
                 s[u][k] = 0.f;
 #pragma unroll
                 for (int e = 0; e < C; ++e) s[u][k] = fmaf(q[k][e], x[e], s[u][k]);
-                if ((there >> (kDepth - 1 - u) & 1u) && key <= end[k] && (!P.window || key > end[k] - P.window)) sees |= 1u << (u * NR + k);
+                if ((there >> (kDepth - 1 - u) & 1u) && sees_key(k, key)) sees |= 1u << (u * NR + k);
             }
         }
 #pragma unroll
@@ -336,7 +355,7 @@ __global__ void __launch_bounds__(kLaneThreads, lane_ctas(D)) paged_lane_kernel(
         __device__ float lse2() const { return sum == 0.f ? -INFINITY : top + log2f(sum); }
     };
     auto none = [&](const Joined& j, int row) {
-        return j.sum == 0.f ? of_no_weight(P, R.row, R.n_keys - R.nq + (row0 + row) / G) : 0.f;
+        return j.sum == 0.f ? of_no_weight<kTree>(P, R, (row0 + row) / G) : 0.f;
     };
     for (int k = threadIdx.x; k < live * (D / 4); k += kLaneThreads) {
         const int row = k / (D / 4), f = k % (D / 4);
@@ -377,10 +396,10 @@ __global__ void __launch_bounds__(kLaneThreads, lane_ctas(D)) paged_lane_kernel(
     }
 }
 
-template <int D, bool kCodes, int NR>
+template <int D, bool kCodes, int NR, bool kTree>
 cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStream_t s) {
     static PerDevice<cudaError_t> smem_set;
-    const auto kernel = paged_lane_kernel<D, kCodes, NR>;
+    const auto kernel = paged_lane_kernel<D, kCodes, NR, kTree>;
     constexpr int kSmem = LaneRing<D, kCodes>::kBytes;
     cudaError_t e = opt_in_smem(smem_set, (const void*)kernel, kSmem);
     if (e != cudaSuccess) return e;
@@ -449,18 +468,34 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
     return cudaSuccess;
 }
 
-template <int D, bool kCodes>
+template <int D, bool kCodes, bool kTree>
 cudaError_t by_rows(const PagedAttnCall& c, const PagedReq* req, int n, cudaStream_t s) {
     bool one = true;
     for (int i = 0; i < n; ++i) one = one && (int64_t)req[i].nq * (c.hq / c.hkv) == 1;
-    return one ? launch<D, kCodes, 1>(c, req, n, s) : launch<D, kCodes, 4>(c, req, n, s);
+    return one ? launch<D, kCodes, 1, kTree>(c, req, n, s) : launch<D, kCodes, 4, kTree>(c, req, n, s);
+}
+
+template <bool kTree>
+cudaError_t by_kind(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s) {
+    if (d == 128) return codes ? by_rows<128, true, kTree>(c, req, n, s) : by_rows<128, false, kTree>(c, req, n, s);
+    return codes ? by_rows<64, true, kTree>(c, req, n, s) : by_rows<64, false, kTree>(c, req, n, s);
 }
 
 }  // namespace
 
+// This file is compiled twice: trees of tokens are paged_lane_tree.cu's.
+#ifndef C2KV_TREES
+
 cudaError_t launch_paged_lane(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s) {
-    if (d == 128) return codes ? by_rows<128, true>(c, req, n, s) : by_rows<128, false>(c, req, n, s);
-    return codes ? by_rows<64, true>(c, req, n, s) : by_rows<64, false>(c, req, n, s);
+    return c.parent ? launch_paged_lane_tree(c, req, n, d, codes, s) : by_kind<false>(c, req, n, d, codes, s);
 }
+
+#else
+
+cudaError_t launch_paged_lane_tree(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s) {
+    return by_kind<true>(c, req, n, d, codes, s);
+}
+
+#endif
 
 }  // namespace c2kv

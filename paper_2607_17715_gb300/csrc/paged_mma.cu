@@ -224,10 +224,10 @@ __device__ __noinline__ Scores<NT> scores_of_infinities(const uint8_t* sk, const
 }
 
 // Values of a block's V (16 bits) that are not finite become zero in shared memory, and are noted for the rows
-// that see them: a byte a channel in odd[row][D / 4], 1 infinity, 2 minus it, 4 NaN.  `end`: the rows' last keys.
+// that see them: a byte a channel in odd[row][D / 4], 1 infinity, 2 minus it, 4 NaN.
 // A key with an infinity of K too scores -inf where the row's sum is a number: 0 times its infinities is NaN.
-template <int D>
-__device__ __noinline__ void set_aside(uint8_t* sv, int key0, uint32_t has, int k_lo, int k_hi, const int* end, int window, int live, uint32_t* odd,
+template <int D, class Sees>
+__device__ __noinline__ void set_aside(uint8_t* sv, int key0, uint32_t has, int k_lo, int k_hi, const Sees sees, int live, uint32_t* odd,
                                        int lane) {
     using L = Lay<D, false, 1>;
     constexpr int kLanes = D / 4, kStep = 32 / kLanes;         // 8 bytes a lane: four channels
@@ -256,14 +256,27 @@ __device__ __noinline__ void set_aside(uint8_t* sv, int key0, uint32_t has, int 
         }
         const int word = b * 16 + ((u / 2) ^ (j & 7)) * 2 + u % 2;       // (16-byte lines of a row are swapped)
         for (int row = 0; row < live; ++row)
-            if (key <= end[row] && (!window || key > end[row] - window)) atomicOr(odd + row * (D / 4) + word, is);
+            if (sees(row, key)) atomicOr(odd + row * (D / 4) + word, is);
         *at = make_uint2(finite(w.x), finite(w.y));
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");         // (TMA writes there next)
     __syncwarp();
 }
 
-template <int D, bool kCodes, int NT, int kReq>
+// Whether a query row sees a key that is there: rows up to its own, or its way to the root of its tree.
+struct RowsBefore {
+    const int* end;          // [row]: the last key it sees
+    int window;
+    __device__ __forceinline__ bool operator()(int row, int key) const { return key <= end[row] && (!window || key > end[row] - window); }
+};
+struct RowsOfTree {
+    const int* start;        // [row]: the last key before the tree that it does not see
+    const uint32_t* bits;    // [row][kTreeWords]
+    int before;
+    __device__ __forceinline__ bool operator()(int row, int key) const { return tree_sees(key, before, start[row], bits + row * kTreeWords); }
+};
+
+template <int D, bool kCodes, int NT, int kReq, bool kTree>
 __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? Lay<D, kCodes, NT>::kCtas : 2) paged_mma_kernel(const __grid_constant__ MmaLaunch<kReq> X) {
     using L = Lay<D, kCodes, NT>;
     using T = __nv_bfloat16;
@@ -277,7 +290,8 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
     __shared__ __align__(16) uint16_t s_q[kTerms][L::KS * NT * 32 * 4];
     __shared__ __align__(8) float s_rs[kRows];
     __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
-    __shared__ int s_end[kRows];
+    __shared__ int s_end[kRows];         // (trees: the last key before the tree that a row does not see)
+    __shared__ uint32_t s_bits[kTree ? kRows * kTreeWords : 1];
     __shared__ uint32_t s_abort, s_last;
     // (16-bit pages) values that are not finite, of keys that a row sees: a byte a channel, 1 infinity, 2 minus
     // it, 4 NaN
@@ -307,9 +321,9 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
     const int hk = (int)(it - sp * P.hkv);
     const uint32_t row0 = rt * kRows;
     const int live = min(kRows, (int)(R.nq * G - row0));
-    // keys that any row of the tile sees: [k_lo, k_hi); the first row sees up to `first`
-    const int before = R.n_keys - R.nq, first = before + (int)(row0 / G), k_hi = before + (int)((row0 + live - 1) / G) + 1;
-    const int k_lo = P.window ? max(0, first - P.window + 1) : 0;
+    // keys that any row of the tile sees: [k_lo, k_hi); every row sees up to `first` (from its window on)
+    const int before = R.n_keys - R.nq, first = kTree ? before - 1 : before + (int)(row0 / G), k_hi = before + (int)((row0 + live - 1) / G) + 1;
+    const int k_lo = P.window ? max(0, (kTree ? before : first) - P.window + 1) : 0;      // (a tree's root has the least depth)
     const int b_lo = k_lo / kBlk, b_n = max(0, (k_hi + kBlk - 1) / kBlk - b_lo);
     const uint32_t each = (uint32_t)b_n / n_split, rest = (uint32_t)b_n - each * n_split;   // the first `rest` stretches: one more
     const int b0 = b_lo + (int)(each * sp + min(sp, rest)), b1 = b0 + (int)(each + (sp < rest));
@@ -405,6 +419,16 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
     uint32_t loaded[kStages];            // of the blocks in flight, the next one to be used first
 #pragma unroll
     for (int i = 0; i < kStages; ++i) loaded[i] = i < n_it ? issue(i, i) : 0u;
+    if constexpr (kTree) {               // the rows' ways through the tree, where the stretch meets it or a window
+        if (threadIdx.x < kRows) {
+            const int row = threadIdx.x;
+#pragma unroll
+            for (int i = 0; i < kTreeWords; ++i) s_bits[row * kTreeWords + i] = 0u;
+            s_end[row] = -1;
+            if (b1 * kBlk > before || P.window)
+                s_end[row] = tree_bits(P.parent + R.q0, (int)((row0 + min(row, live - 1)) / G), before, P.window, P.err, s_bits + row * kTreeWords);
+        }
+    }
 
     // the tile's queries: turned, as fragments of Q^T
 #pragma unroll
@@ -443,7 +467,7 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
         }
         if (lane == 0) {
             s_rs[row] = back * P.scale_log2;
-            s_end[row] = before + (int)tok;
+            if constexpr (!kTree) s_end[row] = before + (int)tok;
         }
 #pragma unroll
         for (int e = 0; e < 2 * C; ++e) {
@@ -488,6 +512,10 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
             for (int s = 0; s < L::KS; ++s) lds2(q_at + x * kTermBytes + s * 256, qf[x][s][0], qf[x][s][1]);
     }
 
+    const auto sees = [&] {
+        if constexpr (kTree) return RowsOfTree{s_end, s_bits, before};
+        else return RowsBefore{s_end, P.window};
+    }();
     int stage = 0, parity = 0;
     auto advance = [&] {
         if (++stage == kStages) {
@@ -619,11 +647,11 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
                 if (edge) {
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        const int end = s_end[t * 8 + 2 * c + k];
+                        const int row = t * 8 + 2 * c + k;
 #pragma unroll
                         for (int n = 0; n < 4; ++n) {
                             const int j = n * 8 + g, key = key0 + j;
-                            const bool seen = key <= end && (!P.window || key > end - P.window) && (has >> (j >> 4) & 1);
+                            const bool seen = sees(row, key) && (has >> (j >> 4) & 1);
                             if (!seen) s[t][n >> 1][(n & 1) * 2 + k] = -INFINITY;
                         }
                     }
@@ -667,7 +695,7 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[t][n][e] *= grow[t][e & 1];
             }
-            if constexpr (kCare) set_aside<D>(const_cast<uint8_t*>(sv), key0, has, k_lo, k_hi, s_end, P.window, live, s_odd, lane);
+            if constexpr (kCare) set_aside<D>(const_cast<uint8_t*>(sv), key0, has, k_lo, k_hi, sees, live, s_odd, lane);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -804,7 +832,7 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
         }
     };
     // of a row of no weight; a stretch's is zero, and the others' decide
-    auto none = [&](int row) { return whole ? of_no_weight(P, R.row, before + (int)((row0 + row) / G)) : 0.f; };
+    auto none = [&](int row) { return whole ? of_no_weight<kTree>(P, R, (int)((row0 + row) / G)) : 0.f; };
     for (int i = threadIdx.x; i < live * (D / 4); i += kWarps * 32) {
         const int row = i / (D / 4), f = i % (D / 4);
         float top = -INFINITY, sum = 0.f;
@@ -892,7 +920,7 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
             }
         }
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        if (sum == 0.f) x.x = of_no_weight(P, R.row, before + (int)((row0 + row) / G)), x.y = x.z = x.w = x.x;
+        if (sum == 0.f) x.x = of_no_weight<kTree>(P, R, (int)((row0 + row) / G)), x.y = x.z = x.w = x.x;
         const uint32_t tok = (row0 + row) / G, h = hk * G + row0 + row - tok * G;
         *reinterpret_cast<uint2*>(out + ((int64_t)(R.q0 + tok) * P.hq + h) * D + 4 * f) =
             make_uint2(pack2<false>(x.x * inv, x.y * inv), pack2<false>(x.z * inv, x.w * inv));
@@ -902,12 +930,12 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
 
 // ------------------------------------------------------------------ host side
 
-template <int D, bool kCodes, int NT, int kReq>
+template <int D, bool kCodes, int NT, int kReq, bool kTree>
 cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStream_t s) {
     using L = Lay<D, kCodes, NT>;
     constexpr int kRows = 8 * NT;
     static PerDevice<cudaError_t> smem_set;
-    const auto kernel = paged_mma_kernel<D, kCodes, NT, kReq>;
+    const auto kernel = paged_mma_kernel<D, kCodes, NT, kReq, kTree>;
     cudaError_t e = opt_in_smem(smem_set, (const void*)kernel, L::kSmem);
     if (e != cudaSuccess) return e;
     for (int b0 = 0; b0 < n; b0 += kReq) {
@@ -985,18 +1013,30 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
 
 // As few row tiles as hold the largest request's rows, and as few eights of rows a tile as make them up:
 // a tile's keys are loaded and converted once for all its rows.
-template <int D, bool kCodes>
+template <int D, bool kCodes, bool kTree>
 cudaError_t by_rows(const PagedAttnCall& c, const PagedReq* req, int n, cudaStream_t s) {
     int rows = 1;
     for (int i = 0; i < n; ++i) rows = std::max(rows, req[i].nq * (c.hq / c.hkv));
     const int eights = (rows + 7) / 8, tiles = (eights + kMostEights - 1) / kMostEights, nt = (eights + tiles - 1) / tiles;
-    if (nt == 1) return n <= kPagedFew ? launch<D, kCodes, 1, kPagedFew>(c, req, n, s) : launch<D, kCodes, 1, kPagedMany>(c, req, n, s);
-    if (nt == 2) return n <= kPagedFew ? launch<D, kCodes, 2, kPagedFew>(c, req, n, s) : launch<D, kCodes, 2, kPagedMany>(c, req, n, s);
-    if (nt == 3) return launch<D, kCodes, 3, kPagedFew>(c, req, n, s);
-    return launch<D, kCodes, 4, kPagedFew>(c, req, n, s);
+    // (few requests have trees as small as this: their launches take the small block whatever their number)
+    const bool small = kTree || n <= kPagedFew;
+    constexpr int kLarge = kTree ? kPagedFew : kPagedMany;
+    if (nt == 1) return small ? launch<D, kCodes, 1, kPagedFew, kTree>(c, req, n, s) : launch<D, kCodes, 1, kLarge, kTree>(c, req, n, s);
+    if (nt == 2) return small ? launch<D, kCodes, 2, kPagedFew, kTree>(c, req, n, s) : launch<D, kCodes, 2, kLarge, kTree>(c, req, n, s);
+    if (nt == 3) return launch<D, kCodes, 3, kPagedFew, kTree>(c, req, n, s);
+    return launch<D, kCodes, 4, kPagedFew, kTree>(c, req, n, s);
+}
+
+template <bool kTree>
+cudaError_t by_kind(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s) {
+    if (d == 128) return codes ? by_rows<128, true, kTree>(c, req, n, s) : by_rows<128, false, kTree>(c, req, n, s);
+    return codes ? by_rows<64, true, kTree>(c, req, n, s) : by_rows<64, false, kTree>(c, req, n, s);
 }
 
 }  // namespace
+
+// This file is compiled twice: trees of tokens are paged_mma_tree.cu's.
+#ifndef C2KV_TREES
 
 bool encode_page_map(CUtensorMap* tm, const void* base, const PageView& pg, int hkv, int d, bool codes, int box_channels, int box_rows,
               CUtensorMapSwizzle swizzle) {
@@ -1009,8 +1049,15 @@ bool encode_page_map(CUtensorMap* tm, const void* base, const PageView& pg, int 
 }
 
 cudaError_t launch_paged_mma(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s) {
-    if (d == 128) return codes ? by_rows<128, true>(c, req, n, s) : by_rows<128, false>(c, req, n, s);
-    return codes ? by_rows<64, true>(c, req, n, s) : by_rows<64, false>(c, req, n, s);
+    return c.parent ? launch_paged_mma_tree(c, req, n, d, codes, s) : by_kind<false>(c, req, n, d, codes, s);
 }
+
+#else
+
+cudaError_t launch_paged_mma_tree(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s) {
+    return by_kind<true>(c, req, n, d, codes, s);
+}
+
+#endif
 
 }  // namespace c2kv

@@ -19,7 +19,13 @@ namespace {
 
 constexpr int kSimtReq = 64;             // requests of a launch
 
-template <int D, bool kCodes>
+// What a row sees (sees(row, key) of attention_core): up to its last key, or through its tree.
+struct TreeRow {
+    int start;               // the last key before the tree that it does not see
+    const uint32_t* bits;    // [kTreeWords]
+};
+
+template <int D, bool kCodes, bool kTree>
 struct PagedJob {
     const PagedAttn<kSimtReq>& P;
     const PagedReq& R;
@@ -27,32 +33,39 @@ struct PagedJob {
     uint32_t* gap;                       // shared: some page was none, so its keys are hidden
     int hk, g_heads, row0, nrows, nkeys;
     int first, last;                     // last keys that the CTA's first and last rows see
+    const uint32_t* bits;                // shared (trees): [query from that of row0 on][kTreeWords] ...
+    const int* start;                    // ... and [query]
     float scale_log2;
     __device__ int64_t token(int r) const { return R.q0 + r / g_heads; }
     __device__ int head(int r) const { return hk * g_heads + r % g_heads; }
     __device__ const float* q_row(int r) const { return static_cast<const float*>(P.q) + token(r) * P.q_stride + (int64_t)head(r) * D; }
     __device__ float* out_row(int r) const { return static_cast<float*>(P.out) + (token(r) * P.hq + head(r)) * D; }
     __device__ float* lse_at(int r) const { return P.lse ? P.lse + (int64_t)head(r) * P.n_tokens + token(r) : nullptr; }
-    __device__ bool needed(int, int k1) const { return !P.window || k1 > first - P.window + 1; }
+    __device__ int before() const { return R.n_keys - R.nq; }
+    __device__ int lowest() const { return (kTree ? before() : first) - P.window; }  // the last key that a window hides from all (a tree's root has the least depth)
+    __device__ bool needed(int, int k1) const { return !P.window || k1 > lowest() + 1; }
     __device__ bool whole(int k0, int k1) const {
-        return k1 - 1 <= first && (!P.window || k0 > last - P.window) && *reinterpret_cast<volatile uint32_t*>(gap) == 0u;
+        return k1 - 1 <= (kTree ? before() - 1 : first) && (!P.window || k0 > last - P.window) && *reinterpret_cast<volatile uint32_t*>(gap) == 0u;
     }
-    __device__ int row(int r) const { return R.n_keys - R.nq + r / g_heads; }      // its last key
+    __device__ auto row(int r) const {
+        if constexpr (kTree) {
+            const int i = (r < nrows ? r : nrows - 1) / g_heads - row0 / g_heads;
+            return TreeRow{start[i], bits + i * kTreeWords};
+        } else {
+            return before() + r / g_heads;                         // its last key
+        }
+    }
     __device__ int page_of(int key) const {
         const int page = __ldg(table + (key >> P.pg.page_shift));
         return page >= 0 && page < P.pg.n_pages ? page : -1;
     }
-    __device__ bool sees_nothing(int r) const {
-        const int end = row(r);
-        return !any_page(P.pg, R.row, P.window ? max(0, end - P.window + 1) : 0, end + 1);
-    }
-    __device__ bool sees(int end, int key) const {
-        return key <= end && (!P.window || key > end - P.window) &&
-               (*reinterpret_cast<volatile uint32_t*>(gap) == 0u || page_of(key) >= 0);
-    }
+    __device__ bool sees_nothing(int r) const { return of_no_weight<kTree>(P, R, r / g_heads) == 0.f; }
+    __device__ bool sees(int end, int key) const { return key <= end && (!P.window || key > end - P.window) && in_page(key); }
+    __device__ bool sees(TreeRow w, int key) const { return tree_sees(key, before(), w.start, w.bits) && in_page(key); }
+    __device__ bool in_page(int key) const { return *reinterpret_cast<volatile uint32_t*>(gap) == 0u || page_of(key) >= 0; }
     // page of a key that some row may see; -1 for one that none does, and for a page that is none
     __device__ int page_at(int key) const {
-        if (key >= nkeys || (P.window && key <= first - P.window)) return -1;
+        if (key >= nkeys || (P.window && key <= lowest())) return -1;
         const int page = page_of(key);
         if (page < 0) {
             atomicOr(P.err, 1);
@@ -120,22 +133,24 @@ struct PagedJob {
     }
 };
 
-template <int D, bool kCodes>
-struct CoreOwnRows<PagedJob<D, kCodes>> {
+template <int D, bool kCodes, bool kTree>
+struct CoreOwnRows<PagedJob<D, kCodes, kTree>> {
     static constexpr bool value = true;
 };
 
 // Item: a row tile of a request (over `ns` CTAs of a cluster), times KV heads along y.
-template <int D, bool kCodes, int RT>
+template <int D, bool kCodes, int RT, bool kTree>
 __global__ void __launch_bounds__(kCoreThreads, core_ctas(D, RT)) paged_simt_kernel(const __grid_constant__ PagedAttn<kSimtReq> P, int ns) {
     extern __shared__ __align__(16) uint8_t core_smem[];
     __shared__ uint32_t s_gap;
+    __shared__ uint32_t s_bits[kTree ? Core<D, RT>::kRows * kTreeWords : 1];
+    __shared__ int s_start[kTree ? Core<D, RT>::kRows : 1];
     if (threadIdx.x == 0) s_gap = 0u;
     __syncthreads();
     const int item = (int)(blockIdx.x / (unsigned)ns), rank = (int)(blockIdx.x % (unsigned)ns);
     int r = 0;
     while (r + 1 < P.batch && P.req[r + 1].item0 <= item) ++r;
-    PagedJob<D, kCodes> j{P, P.req[r]};
+    PagedJob<D, kCodes, kTree> j{P, P.req[r]};
     j.table = P.pg.table + (int64_t)j.R.row * P.pg.table_stride;
     j.gap = &s_gap;
     j.hk = blockIdx.y;
@@ -147,16 +162,27 @@ __global__ void __launch_bounds__(kCoreThreads, core_ctas(D, RT)) paged_simt_ker
     j.last = before + (j.row0 + rows - 1) / j.g_heads;
     j.nkeys = max(0, j.last + 1);
     j.scale_log2 = P.scale_log2;
+    if constexpr (kTree) {               // the queries' ways through the tree
+        j.bits = s_bits;
+        j.start = s_start;
+        const int q0 = j.row0 / j.g_heads, n = (j.row0 + rows - 1) / j.g_heads - q0 + 1;
+        if ((int)threadIdx.x < n) {
+#pragma unroll
+            for (int i = 0; i < kTreeWords; ++i) s_bits[threadIdx.x * kTreeWords + i] = 0u;
+            s_start[threadIdx.x] = tree_bits(P.parent + j.R.q0, q0 + (int)threadIdx.x, before, P.window, P.err, s_bits + threadIdx.x * kTreeWords);
+        }
+        __syncthreads();
+    }
     attention_core<float, D, RT>(j, j.row0, ns, rank, core_smem);
 }
 
-template <int D, bool kCodes, int RT>
+template <int D, bool kCodes, int RT, bool kTree>
 CoreKernel<D, RT> ready() {
     static PerDevice<CoreKernel<D, RT>> kept;
-    return kept.get([] { return CoreKernel<D, RT>(reinterpret_cast<const void*>(&paged_simt_kernel<D, kCodes, RT>), device_sms()); });
+    return kept.get([] { return CoreKernel<D, RT>(reinterpret_cast<const void*>(&paged_simt_kernel<D, kCodes, RT, kTree>), device_sms()); });
 }
 
-template <int D, bool kCodes, int RT>
+template <int D, bool kCodes, int RT, bool kTree>
 cudaError_t launch_form(PagedAttn<kSimtReq>& P, CorePlan plan, cudaStream_t s) {
     constexpr int kRows = Core<D, RT>::kRows;
     int64_t items = 0;
@@ -166,15 +192,15 @@ cudaError_t launch_form(PagedAttn<kSimtReq>& P, CorePlan plan, cudaStream_t s) {
     }
     if (items * plan.ns > 0x7fffffffLL || P.hkv > 65535) return cudaErrorInvalidValue;
     void* args[2] = {&P, &plan.ns};
-    return core_launch(reinterpret_cast<const void*>(&paged_simt_kernel<D, kCodes, RT>), dim3((unsigned)(items * plan.ns), P.hkv),
+    return core_launch(reinterpret_cast<const void*>(&paged_simt_kernel<D, kCodes, RT, kTree>), dim3((unsigned)(items * plan.ns), P.hkv),
                        Core<D, RT>::kSmem, plan, false, args, s);
 }
 
-template <int D, bool kCodes>
+template <int D, bool kCodes, bool kTree>
 cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStream_t s) {
-    const CoreKernel<D, 4> large = ready<D, kCodes, 4>();
-    const CoreKernel<D, 1> small = ready<D, kCodes, 1>();
-    const CoreKernel<D, 0> four = ready<D, kCodes, 0>();
+    const CoreKernel<D, 4> large = ready<D, kCodes, 4, kTree>();
+    const CoreKernel<D, 1> small = ready<D, kCodes, 1, kTree>();
+    const CoreKernel<D, 0> four = ready<D, kCodes, 0, kTree>();
     if (large.err != cudaSuccess) return large.err;
     if (small.err != cudaSuccess || four.err != cudaSuccess) return small.err != cudaSuccess ? small.err : four.err;
     for (int b0 = 0; b0 < n; b0 += kSimtReq) {
@@ -193,19 +219,35 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
                                         [&](int form, int ns, bool alone) {
                                             return form == 4 ? large.slots[alone][ns] : form == 1 ? small.slots[alone][ns] : four.slots[alone][ns];
                                         });
-        const cudaError_t e = plan.form == 4   ? launch_form<D, kCodes, 4>(P, plan, s)
-                              : plan.form == 1 ? launch_form<D, kCodes, 1>(P, plan, s)
-                                               : launch_form<D, kCodes, 0>(P, plan, s);
+        const cudaError_t e = plan.form == 4   ? launch_form<D, kCodes, 4, kTree>(P, plan, s)
+                              : plan.form == 1 ? launch_form<D, kCodes, 1, kTree>(P, plan, s)
+                                               : launch_form<D, kCodes, 0, kTree>(P, plan, s);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
 }
 
+template <bool kTree>
+cudaError_t by_kind(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s) {
+    if (d == 128) return codes ? launch<128, true, kTree>(c, req, n, s) : launch<128, false, kTree>(c, req, n, s);
+    return codes ? launch<64, true, kTree>(c, req, n, s) : launch<64, false, kTree>(c, req, n, s);
+}
+
 }  // namespace
 
+// This file is compiled twice: trees of tokens are paged_simt_tree.cu's.
+#ifndef C2KV_TREES
+
 cudaError_t launch_paged_simt(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s) {
-    if (d == 128) return codes ? launch<128, true>(c, req, n, s) : launch<128, false>(c, req, n, s);
-    return codes ? launch<64, true>(c, req, n, s) : launch<64, false>(c, req, n, s);
+    return c.parent ? launch_paged_simt_tree(c, req, n, d, codes, s) : by_kind<false>(c, req, n, d, codes, s);
 }
+
+#else
+
+cudaError_t launch_paged_simt_tree(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s) {
+    return by_kind<true>(c, req, n, d, codes, s);
+}
+
+#endif
 
 }  // namespace c2kv

@@ -105,7 +105,7 @@ struct Item {
     int k_lo, k_hi;                      // keys that some row sees: [k_lo, k_hi)
 };
 
-template <int kReq>
+template <bool kTree, int kReq>
 __device__ __forceinline__ Item find_item(const PagedAttn<kReq>& P) {
     Item w;
     int r = 0;
@@ -126,7 +126,7 @@ __device__ __forceinline__ Item find_item(const PagedAttn<kReq>& P) {
     w.live = min(kPair, n_rows - w.row0);
     const int before = w.R.n_keys - w.R.nq;
     w.k_hi = before + (w.row0 + w.live - 1) / G + 1;
-    w.k_lo = P.window ? max(0, before + w.row0 / G - P.window + 1) : 0;
+    w.k_lo = P.window ? max(0, before + (kTree ? 0 : w.row0 / G) - P.window + 1) : 0;    // (a tree's root has the least depth)
     const int t_lo = w.k_lo / BN, t_n = max(0, (w.k_hi + BN - 1) / BN - t_lo);
     w.j0 = t_lo + (int)((int64_t)t_n * w.sp / w.R.splits);
     w.n = t_lo + (int)((int64_t)t_n * (w.sp + 1) / w.R.splits) - w.j0;
@@ -373,12 +373,52 @@ __device__ __forceinline__ uint32_t within(uint32_t keys, int key0, int start, i
     return lo > hi ? 0u : keys & (0xffffffffu << lo) & (0xffffffffu >> (31 - hi));
 }
 
+// The keys that a row sees: up to its last one, in its window.
+struct Before {
+    int start, end;                      // (start, end]
+    template <int kReq>
+    __device__ __forceinline__ Before(const PagedAttn<kReq>& P, const Item& w, int tok) {
+        end = w.R.n_keys - w.R.nq + tok;
+        start = P.window ? end - P.window : -1;
+    }
+    __device__ __forceinline__ bool sees(int key) const { return key > start && key <= end; }
+    // all of 128 keys from key0 on
+    __device__ __forceinline__ bool sees_tile(int key0) const { return key0 + BN - 1 <= end && key0 > start; }
+    // of 32 keys from key0 on, a bit each
+    __device__ __forceinline__ uint32_t of32(int key0) const { return within(0xffffffffu, key0, start, end); }
+};
+// The same of a tree's node: the rows before the tree, and its way to the root, a bit a node (in local memory:
+// few of a CTA's key tiles meet the tree).
+struct Through {
+    int start, before;
+    uint32_t bits[kTreeWords];
+    template <int kReq>
+    __device__ __forceinline__ Through(const PagedAttn<kReq>& P, const Item& w, int tok) {
+        before = w.R.n_keys - w.R.nq;
+        start = -1;
+#pragma unroll
+        for (int i = 0; i < kTreeWords; ++i) bits[i] = 0u;
+        if ((w.j0 + w.n) * BN > before || P.window) start = tree_bits(P.parent + w.R.q0, tok, before, P.window, P.err, bits);
+    }
+    __device__ __forceinline__ bool sees(int key) const { return tree_sees(key, before, start, bits); }
+    __device__ __forceinline__ bool sees_tile(int key0) const { return key0 + BN <= before && key0 > start; }
+    __device__ __forceinline__ uint32_t of32(int key0) const {
+        uint32_t seen = key0 < before ? within(0xffffffffu, key0, start, before - 1) : 0u;
+        const int j = key0 - before;                     // the node of the first key
+        if (j > -32 && j < 0) seen |= bits[0] << -j;
+        else if (j >= 0 && j < kTreeMost) seen |= __funnelshift_r(bits[j >> 5], j + 32 < kTreeMost ? bits[(j >> 5) + 1] : 0u, j & 31);
+        return seen;
+    }
+};
+template <bool kTree>
+using Sight = typename std::conditional<kTree, Through, Before>::type;
+
 // Rows that see values of V which are not finite (bits of `bad`, a lane a row from row0 on): of a channel's
 // infinities and NaN nothing is left but which there are, and nothing else matters there.  The warp looks the
 // noted keys up once for all its rows.  (Computed again key by key, a chunk of 256 tokens over one such row
 // of 8192 took 28 ms for 70 us.)
-template <int D, bool kCodes, int kReq>
-__device__ __forceinline__ void take_in(const TcLaunch<kReq>& X, const Item& w, uint32_t bad, int start, int end, int row0, int lane, uint8_t* q_tiles) {
+template <int D, bool kCodes, class S, int kReq>
+__device__ __forceinline__ void take_in(const TcLaunch<kReq>& X, const Item& w, uint32_t bad, const S& sight, int row0, int lane, uint8_t* q_tiles) {
     using T = __nv_bfloat16;
     constexpr int E = D / 32;                                    // channels a lane, a byte each: 1 infinity, 2 minus it, 4 NaN
     constexpr uint32_t kNan = E == 4 ? 0x04040404u : 0x0404u;
@@ -401,7 +441,7 @@ __device__ __forceinline__ void take_in(const TcLaunch<kReq>& X, const Item& w, 
                 uint32_t keys = __shfl_sync(0xffffffffu, k == 0 ? odd.x : k == 1 ? odd.y : k == 2 ? odd.z : odd.w, j);
                 for (; keys && rest; keys &= keys - 1) {
                     const int key = (w.j0 + j0 + j) * BN + 32 * k + __ffs(keys) - 1;
-                    uint32_t rows = __ballot_sync(0xffffffffu, key > start && key <= end) & bad;
+                    uint32_t rows = __ballot_sync(0xffffffffu, sight.sees(key)) & bad;
                     if (rows == 0u) continue;
                     const int64_t page = ld_after(table + (key >> P.pg.page_shift)), in_page = (int64_t)w.hk * size + (key & (size - 1));
                     float v[E];
@@ -457,7 +497,7 @@ __device__ __forceinline__ void take_in(const TcLaunch<kReq>& X, const Item& w, 
 // weights near f16's largest (or the row has no reference yet) the maximum comes first after all.
 constexpr float kBelow = 8.f, kRoom = 14.f, kMostSum = 61440.f;
 
-template <int D, bool kCodes, int kReq>
+template <int D, bool kCodes, bool kTree, int kReq>
 __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item& w, uint32_t tmem, uint32_t bars, int x, int quad, int lane,
                                              const TileNote* notes, const int8_t* s_back, volatile uint32_t* abort, uint8_t* q_tiles) {
     using T = __nv_bfloat16;
@@ -470,8 +510,7 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
     const uint32_t colS = tmem + lane_addr + (uint32_t)(x * BN), colO = tmem + lane_addr + kColO + (uint32_t)(x * D);
     const bool there = row < w.live;
     const int my = min(row, w.live - 1);
-    const int end = w.R.n_keys - w.R.nq + (w.row0 + my) / G;     // the last key the row sees
-    const int start = P.window ? end - P.window : -1;            // and the last that it does not, before them
+    const Sight<kTree> sight(P, w, (w.row0 + my) / G);
     const float rs = P.scale_log2 * pow2i(s_back[row]);
     float ref = -CUDART_INF_F, top = -CUDART_INF_F, l = 0.f;
     bool touched = false;                // by values that are not finite
@@ -510,17 +549,17 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
         const float f = fminf(fmaxf(rs * nt.k_unit, 0x1p-126f), 0x1.fffffep127f), ve = nt.v_exp;
         const int key0 = (w.j0 + j) * BN;
         if (nt.odd.x | nt.odd.y | nt.odd.z | nt.odd.w)
-            touched = touched || within(nt.odd.x, key0, start, end) || within(nt.odd.y, key0 + 32, start, end) ||
-                      within(nt.odd.z, key0 + 64, start, end) || within(nt.odd.w, key0 + 96, start, end);
+            touched = touched || (nt.odd.x & sight.of32(key0)) || (nt.odd.y & sight.of32(key0 + 32)) || (nt.odd.z & sight.of32(key0 + 64)) ||
+                      (nt.odd.w & sight.of32(key0 + 96));
         tmem_ld_wait();
-        if (key0 + BN - 1 > end || key0 <= start || groups != 0xffu) {
+        if (!sight.sees_tile(key0) || groups != 0xffu) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+            for (int c = 0; c < 4; ++c) {
+                const uint32_t seen = sight.of32(key0 + c * 32) & ((groups >> (2 * c) & 1u ? 0xffffu : 0u) | (groups >> (2 * c + 1) & 1u ? 0xffff0000u : 0u));
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const int key = key0 + c * 32 + e;
-                    if (key > end || key <= start || !(groups >> (2 * c + e / 16) & 1u)) sv[c][e] = __float_as_uint(-CUDART_INF_F);
-                }
+                for (int e = 0; e < 32; ++e)
+                    if (!(seen >> e & 1u)) sv[c][e] = __float_as_uint(-CUDART_INF_F);
+            }
         }
         auto find_top = [&]() {
             float top4[4];
@@ -588,7 +627,7 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
     T* const orow = static_cast<T*>(P.out) + (tok * P.hq + h) * D;
     float* const prow = X.part_o + ((int64_t)blockIdx.x * kPair + row) * D;
     const bool wide = (reinterpret_cast<uintptr_t>(P.out) & 31u) == 0;
-    const float none = there && whole && l == 0.f ? of_no_weight(P, w.R.row, end) : 0.f;
+    const float none = there && whole && l == 0.f ? of_no_weight<kTree>(P, w.R, (w.row0 + my) / G) : 0.f;
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
         uint32_t ov[32];
@@ -627,12 +666,12 @@ __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item
         else if (P.lse) P.lse[(int64_t)h * P.n_tokens + tok] = lse2 * 0.69314718055994531f;
     }
     const uint32_t bad = __ballot_sync(0xffffffffu, there && touched && l < CUDART_INF_F);
-    if (bad) take_in<D, kCodes>(X, w, bad, start, end, x * BM + quad * 32, lane, q_tiles);
+    if (bad) take_in<D, kCodes>(X, w, bad, sight, x * BM + quad * 32, lane, q_tiles);
 }
 
 // ------------------------------------------------------------------ kernel
 
-template <int D, bool kCodes, int kReq>
+template <int D, bool kCodes, int kReq, bool kTree>
 __global__ void __launch_bounds__(kThreads, 1) paged_tc_kernel(const __grid_constant__ TcLaunch<kReq> X) {
     const PagedAttn<kReq>& P = X.a;
     using C = Tc<D>;
@@ -646,7 +685,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tc_kernel(const __grid_cons
     volatile uint32_t* const abort = slot + 1;
     auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const Item w = find_item(P);
+    const Item w = find_item<kTree>(P);
     const bool has_b = w.live > BM;
     QueryRows<D> rows;
     if (warp >= 4) rows = fetch_queries<D>(P, w, warp - 4, lane, sQ);
@@ -691,7 +730,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tc_kernel(const __grid_cons
         asm volatile("bar.sync 1, 256;" ::: "memory");           // (the rows' powers of two)
         mbar_arrive(bar(C::Q));
         const int x = warp >= 8;
-        if (x == 0 || has_b) softmax_rows<D, kCodes>(X, w, tmem, bars, x, warp & 3, lane, notes, s_back, abort, smem);
+        if (x == 0 || has_b) softmax_rows<D, kCodes, kTree>(X, w, tmem, bars, x, warp & 3, lane, notes, s_back, abort, smem);
     }
 
     tc_fence_before();
@@ -707,7 +746,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tc_kernel(const __grid_cons
 // tokens over 30000 rows, where this takes 4 of them.)
 constexpr int kJoinThreads = 128, kJoinRows = 32;
 
-template <int D, int kReq>
+template <int D, int kReq, bool kTree>
 __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_constant__ TcLaunch<kReq> X) {
     const PagedAttn<kReq>& P = X.a;
     extern __shared__ float weight[];                            // [stretch][row]
@@ -732,7 +771,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
         const float base = top == -CUDART_INF_F ? 0.f : top;
         for (int k = 0; k < S; ++k) sum += ex2(weight[k * kJoinRows + row] - base);
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        const float none = sum == 0.f ? of_no_weight(P, R.row, R.n_keys - R.nq + (pr * kPair + first + row) / G) : 0.f;
+        const float none = sum == 0.f ? of_no_weight<kTree>(P, R, (pr * kPair + first + row) / G) : 0.f;
         for (int k = 0; k < S; ++k) weight[k * kJoinRows + row] = ex2(weight[k * kJoinRows + row] - base) * inv + none;
         if (P.lse) {
             const int all = pr * kPair + first + row;
@@ -812,7 +851,7 @@ std::vector<PagedReq> plan(const PagedAttnCall& c, const PagedReq* req, int n) {
     auto pairs_of = [&](const PagedReq& q) { return (int)(((int64_t)q.nq * G + kPair - 1) / kPair); };
     auto keys_of = [&](const PagedReq& q, int pr) {      // key tiles of a pair
         const int last = (int)std::min<int64_t>((int64_t)(pr + 1) * kPair, (int64_t)q.nq * G) - 1;
-        const int hi = q.n_keys - q.nq + last / G + 1, lo = c.window ? std::max(0, q.n_keys - q.nq + pr * kPair / G - c.window + 1) : 0;
+        const int hi = q.n_keys - q.nq + last / G + 1, lo = c.window ? std::max(0, q.n_keys - q.nq + (c.parent ? 0 : pr * kPair / G) - c.window + 1) : 0;
         return std::max(1, (hi + BN - 1) / BN - lo / BN);
     };
     auto piece = [](const PagedReq& e, int keys) { return (keys + e.splits - 1) / e.splits + (e.splits > 1 ? kCutStart : kStart); };
@@ -885,10 +924,10 @@ std::vector<PagedReq> plan(const PagedAttnCall& c, const PagedReq* req, int n) {
     return best;
 }
 
-template <int D, bool kCodes, int kReq>
+template <int D, bool kCodes, int kReq, bool kTree>
 cudaError_t launch(const PagedAttnCall& c, const KeyTiles& tiles, const std::vector<PagedReq>& entries, cudaStream_t s) {
     static PerDevice<cudaError_t> smem_set;
-    const auto kernel = paged_tc_kernel<D, kCodes, kReq>;
+    const auto kernel = paged_tc_kernel<D, kCodes, kReq, kTree>;
     cudaError_t e = opt_in_smem(smem_set, (const void*)kernel, Tc<D>::kSmem);
     if (e != cudaSuccess) return e;
     for (size_t b0 = 0; b0 < entries.size(); b0 += kReq) {
@@ -953,24 +992,42 @@ cudaError_t launch(const PagedAttnCall& c, const KeyTiles& tiles, const std::vec
             cfg.blockDim = dim3(kJoinThreads);
             cfg.dynamicSmemBytes = (size_t)most * kJoinRows * 4;
             cfg.numAttrs = 1;
-            e = cudaLaunchKernelEx(&cfg, paged_join_kernel<D, kReq>, X);
+            e = cudaLaunchKernelEx(&cfg, paged_join_kernel<D, kReq, kTree>, X);
         }
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
 }
 
-template <int D, bool kCodes>
+template <int D, bool kCodes, bool kTree>
 cudaError_t by_count(const PagedAttnCall& c, const KeyTiles& tiles, const PagedReq* req, int n, cudaStream_t s) {
     const std::vector<PagedReq> entries = plan(c, req, n);
-    return (int)entries.size() <= kPagedFew ? launch<D, kCodes, kPagedFew>(c, tiles, entries, s) : launch<D, kCodes, kPagedMany>(c, tiles, entries, s);
+    constexpr int kLarge = kTree ? kPagedFew : kPagedMany;       // (few requests have trees)
+    return (int)entries.size() <= kPagedFew ? launch<D, kCodes, kPagedFew, kTree>(c, tiles, entries, s)
+                                            : launch<D, kCodes, kLarge, kTree>(c, tiles, entries, s);
+}
+
+template <bool kTree>
+cudaError_t by_kind(const PagedAttnCall& c, const KeyTiles& tiles, const PagedReq* req, int n, int d, bool codes, cudaStream_t s) {
+    if (d == 128) return codes ? by_count<128, true, kTree>(c, tiles, req, n, s) : by_count<128, false, kTree>(c, tiles, req, n, s);
+    return codes ? by_count<64, true, kTree>(c, tiles, req, n, s) : by_count<64, false, kTree>(c, tiles, req, n, s);
 }
 
 }  // namespace
 
+// This file is compiled twice: trees of tokens are paged_tc_tree.cu's.
+#ifndef C2KV_TREES
+
 cudaError_t launch_paged_tc(const PagedAttnCall& c, const KeyTiles& tiles, const PagedReq* req, int n, int d, bool codes, cudaStream_t s) {
-    if (d == 128) return codes ? by_count<128, true>(c, tiles, req, n, s) : by_count<128, false>(c, tiles, req, n, s);
-    return codes ? by_count<64, true>(c, tiles, req, n, s) : by_count<64, false>(c, tiles, req, n, s);
+    return c.parent ? launch_paged_tc_tree(c, tiles, req, n, d, codes, s) : by_kind<false>(c, tiles, req, n, d, codes, s);
 }
+
+#else
+
+cudaError_t launch_paged_tc_tree(const PagedAttnCall& c, const KeyTiles& tiles, const PagedReq* req, int n, int d, bool codes, cudaStream_t s) {
+    return by_kind<true>(c, tiles, req, n, d, codes, s);
+}
+
+#endif
 
 }  // namespace c2kv
