@@ -554,6 +554,98 @@ c2kv_status c2kv_verify_drafts(c2kv_ctx* ctx, int32_t batch, const int32_t* draf
                                int64_t q_stride, const float* u_accept, const float* u_next,
                                int32_t* n_accepted, int32_t* next_token);
 
+/*
+ * c2kv_verify_tree -- which of each request's drafted tokens, a tree as c2kv_paged_attend_tree takes it, the
+ * target's probabilities keep, and the token that follows them.  Node 0 is the last token kept; from there on,
+ * at each node t a token is drawn from row t of p by u[t], exactly as c2kv_verify_drafts draws (weights are
+ * whole multiples of 2^-44, the token the lowest index whose running sum passes floor(sum * k / 2^24)); where
+ * children of the node hold it, the walk goes on at the first of them, else it ends and the token is the next
+ * one.  So every token is the target's own draw, and kept and next ones are distributed as without drafts,
+ * however those were made.  Only the rows of nodes that the walk meets are read.
+ *
+ *   tree_ptr     : host int32 [B + 1], non-decreasing from 0; at most 512 nodes a request; a request may have
+ *                  none (nothing accepted, no next token).
+ *   vocab        : 1 <= V <= 2^19.
+ *   tokens       : device int32 [T]; the root's is not read, one outside [0, V) is never drawn.
+ *   parent       : device int32 [T].  One outside [-1, its child) is refused: the node is no child, and
+ *                  c2kv_sync returns ERR_DEVICE_BOUNDS.
+ *   p            : device fp32 [T][V], rows p_stride apart (0 = V): the target's probabilities after each node.
+ *   u            : device fp32 [T] in [0, 1).
+ *   n_accepted   : device int32 [B]: drafts kept (the root is not one).
+ *   path         : device int32 [T]: request r's nodes from tree_ptr[r] on, 0 and those kept, then -1.
+ *   next_token   : device int32 [B]; -1 where the last row has no weight.
+ * Not recorded by the trace.  Errors: ERR_ARG, ERR_UNSUPPORTED (more than 512 nodes), ERR_NOMEM, ERR_CUDA.
+ */
+c2kv_status c2kv_verify_tree(c2kv_ctx* ctx, int32_t batch, const int32_t* tree_ptr, int32_t vocab, const int32_t* tokens,
+                             const int32_t* parent, const float* p, int64_t p_stride, const float* u, int32_t* n_accepted, int32_t* path,
+                             int32_t* next_token);
+
+/*
+ * c2kv_paged_keep -- the rows of the tokens that a walk kept moved together, in every layer: row start[r] +
+ * path[i] of request r becomes row start[r] + i, i <= n_accepted[r], K, V and scales as they are (a token's
+ * position was its depth's, so its key is turned as it has to be).  The request then has start[r] +
+ * n_accepted[r] + 1 rows; those behind hold what they held.
+ *
+ *   pages        : host array of n_layers descriptions, of one format, page size, page count and strides; the
+ *                  layers' pages must not lie over one another.
+ *   table, ..    : as c2kv_paged_append, for all layers.
+ *   tree_ptr     : host int32 [B + 1] as c2kv_verify_tree.
+ *   start        : host int32 [B]: the row of each tree's node 0.
+ *   path, n_accepted : device, as c2kv_verify_tree writes them: path rises, from at least 0.
+ * n_accepted outside [0, nodes) is refused by the kernel (the request's rows stay), so are entries of path that
+ * do not rise or are no node (they and those behind stay) and page numbers outside [0, n_pages) (the row stays);
+ * c2kv_sync returns ERR_DEVICE_BOUNDS.  Recorded by the trace as C2KV_PROF_SUFFIX.
+ * Errors: ERR_ARG, ERR_DTYPE (page format), ERR_UNSUPPORTED (more than 512 nodes), ERR_NOMEM, ERR_CUDA.
+ */
+c2kv_status c2kv_paged_keep(c2kv_ctx* ctx, const c2kv_pages* pages, int32_t n_layers, int32_t batch, const int32_t* table,
+                            int32_t table_width, int64_t table_stride, const int32_t* tree_ptr, const int32_t* start, const int32_t* path,
+                            const int32_t* n_accepted);
+
+/*
+ * c2kv_beam_select -- the n_best continuations of each request's beams.  Beam w of request r and token v make
+ * the candidate of score s[w] + (x[w][v] - norm[w]) (s[w] + x[w][v] without norm), each operation rounded to
+ * fp32; the largest are kept, in order, of equal ones those of lower w V + v.  A beam that has ended (done not
+ * 0) has one candidate, end_token at its own score.  Scores of -inf and NaN are no candidates (a first step's
+ * beams but one have the score -inf).
+ *
+ *   batch, width, vocab, n_best : B >= 1, 1 <= W <= 64, 1 <= V <= 2^19, 1 <= n_best <= 64; B W <= 2^22.
+ *   dtype, x     : C2KV_DTYPE_*; device [B W][V] of it, rows x_stride elements apart (0 = V): log-probabilities,
+ *                  or logits with
+ *   norm         : device fp32 [B W], their log-sum-exp; or NULL.
+ *   score, done  : device fp32 [B W], int32 [B W] or NULL.
+ *   end_token    : in [0, V), or -1 (none: done must be NULL).
+ *   parent, token, score_out : device int32, int32, fp32 [B][n_best]: the beam of each (0 .. W - 1), its token and
+ *                  score; -1, -1, -inf past the last candidate.
+ *   done_out     : device int32 [B][n_best], 1 where the continuation has ended; or NULL.
+ * Outputs must not lie over inputs.  May be captured, as the paged calls.  Not recorded by the trace.
+ * Errors: ERR_ARG, ERR_DTYPE, ERR_NOMEM, ERR_CUDA.
+ */
+c2kv_status c2kv_beam_select(c2kv_ctx* ctx, int32_t batch, int32_t width, int32_t vocab, int32_t n_best, int32_t dtype, const void* x,
+                             int64_t x_stride, const float* norm, const float* score, const int32_t* done, int32_t end_token,
+                             int32_t* parent, int32_t* token, float* score_out, int32_t* done_out);
+
+/*
+ * c2kv_paged_reorder -- the beams' pages after a choice: beam w of request r goes on from beam parent[r][w] (-1:
+ * from itself).  Tables are by beam, rows r W + w; a request's beams have n_rows[r] rows each.  Whole pages are
+ * shared: table_out names the parent's.  The page after them, which the next rows go to, must be every beam's
+ * own: where it holds rows already, the first beam that goes on from a parent takes the parent's page, and the
+ * others copy its rows, in every layer, into the pages of beams from which none goes on, in order of both (there
+ * are as many).  All other entries are the beam's own, so pages reserved ahead stay with their place.
+ *   pages, n_layers : as c2kv_paged_keep.
+ *   batch, width : B >= 1, 1 <= W <= 64.
+ *   table        : device int32 [B W] rows of table_width page numbers, table_stride apart.  A request's beams must
+ *                  have different pages after the whole ones.
+ *   n_rows       : host int32 [B].
+ *   parent       : device int32 [B][W].  One outside [-1, W) is refused: taken for -1, and c2kv_sync returns
+ *                  ERR_DEVICE_BOUNDS.
+ *   table_out    : device int32 [B W], rows table_out_stride apart; not over `table`.
+ * A page number to copy from or to outside [0, n_pages) is refused by the kernel, and its copy not made.
+ * Recorded by the trace as C2KV_PROF_COMPOSE.  Errors: ERR_ARG, ERR_DTYPE (page format), ERR_NOMEM, ERR_CUDA.
+ */
+c2kv_status c2kv_paged_reorder(c2kv_ctx* ctx, const c2kv_pages* pages, int32_t n_layers, int32_t batch, int32_t width, const int32_t* table,
+                               int32_t table_width, int64_t table_stride, const int32_t* n_rows, const int32_t* parent, int32_t* table_out,
+                               int64_t table_out_stride);
+
 /* c2kv_cache_release -- free a composed cache (stream-ordered). */
 c2kv_status c2kv_cache_release(c2kv_ctx* ctx, c2kv_cache* cache);
 

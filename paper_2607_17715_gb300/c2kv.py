@@ -103,6 +103,10 @@ _SIGS = {
     "c2kv_paged_attend": (_I32, [_VP, _VP, _I32, _VP, _I32, _I64, _VP, _VP, _I32, _VP, _I64, _VP, _VP, _VP]),
     "c2kv_paged_attend_tree": (_I32, [_VP, _VP, _I32, _VP, _I32, _I64, _VP, _VP, _VP, _I32, _VP, _I64, _VP, _VP, _VP]),
     "c2kv_verify_drafts": (_I32, [_VP, _I32, _VP, _I32, _VP, _VP, _I64, _VP, _I64, _VP, _VP, _VP, _VP]),
+    "c2kv_verify_tree": (_I32, [_VP, _I32, _VP, _I32, _VP, _VP, _VP, _I64, _VP, _VP, _VP, _VP]),
+    "c2kv_paged_keep": (_I32, [_VP, _VP, _I32, _I32, _VP, _I32, _I64, _VP, _VP, _VP, _VP]),
+    "c2kv_beam_select": (_I32, [_VP, _I32, _I32, _I32, _I32, _I32, _VP, _I64, _VP, _VP, _VP, _I32, _VP, _VP, _VP, _VP]),
+    "c2kv_paged_reorder": (_I32, [_VP, _VP, _I32, _I32, _I32, _VP, _I32, _I64, _VP, _VP, _VP, _I64]),
     "c2kv_cache_release": (_I32, [_VP, _VP]),
     "c2kv_sync": (_I32, [_VP]),
     "c2kv_last_error": (ctypes.c_char_p, [_VP]),
@@ -338,6 +342,46 @@ def make_pages(k, v, k_scale=None, v_scale=None):
     return p
 
 
+class _Layers:
+    """Pages of several layers in one array of descriptions, which a call takes by its address."""
+
+    def __init__(self, pages):
+        pages = list(pages)
+        if not pages:
+            raise ValueError("at least one layer's pages are needed")
+        first = pages[0]
+        for p in pages:
+            if p.heads != first.heads or p.dtype != first.dtype:
+                raise ValueError("the layers' pages must have one type and the same heads")
+        self.keep, self.n, self.heads, self.dtype = pages, len(pages), first.heads, first.dtype
+        self.array = (c2kv_pages * len(pages))(*pages)
+        self.address = ctypes.addressof(self.array)
+        self.fits = None                             # the context that they were last found to fit
+
+
+def make_layers(k, v=None, k_scale=None, v_scale=None):
+    """Describe the pages of a model's layers: tensors as make_pages takes them, with a first dimension of layers;
+    or (k alone) a list of what make_pages returned."""
+    if v is None:
+        return _Layers(k)
+    return _Layers(make_pages(k[i], v[i], None if k_scale is None else k_scale[i], None if v_scale is None else v_scale[i])
+                   for i in range(k.shape[0]))
+
+
+def _fitting(ctx, layers):
+    """The layers of a call (a single layer's pages are taken too), of the heads and type of its context."""
+    if isinstance(layers, c2kv_pages):
+        layers = _Layers([layers])
+    known = _contexts.get(ctx)
+    if known is not None and layers.fits is not known:
+        t = _torch()
+        dtype = t.float32 if known.f32 else t.bfloat16
+        if layers.heads != known.kv or layers.dtype not in (None, dtype):
+            raise ValueError(f"pages hold heads {layers.heads} of {layers.dtype}, the context has {known.kv} of {dtype}")
+        layers.fits = known
+    return layers
+
+
 def _table(table, batch, rows):
     """Address, width and row stride of a table of page numbers (a torch int32 tensor [B, width]) for
     the requests that a call's host arrays describe."""
@@ -498,6 +542,60 @@ def c2kv_verify_drafts(ctx, draft_ptr, tokens, p, q, u_accept, u_next, n_accepte
     _check(_lib.c2kv_verify_drafts(ctx, b, ptr_p, vocab, _vector(tokens, t, "tokens", i32), pp, ps, qp, qs,
                                    _vector(u_accept, t, "u_accept", f32), _vector(u_next, b, "u_next", f32),
                                    _vector(n_accepted, b, "n_accepted", i32), _vector(next_token, b, "next_token", i32)), ctx)
+
+
+def c2kv_verify_tree(ctx, tree_ptr, tokens, parent, p, u, n_accepted, path, next_token):
+    """Walk down trees of drafted tokens by draws from the target's probabilities p [T, V], a row after each node."""
+    ptr, ptr_p, n = _i32_at(tree_ptr)
+    b, vocab, i32, f32 = n - 1, p.shape[1], _torch().int32, _torch().float32
+    t = ptr[b] if n > 0 else 0
+    pp, ps = _rows(p, t, vocab, "p", f32)
+    _check(_lib.c2kv_verify_tree(ctx, b, ptr_p, vocab, _vector(tokens, t, "tokens", i32), _vector(parent, t, "parent", i32), pp, ps,
+                                 _vector(u, t, "u", f32), _vector(n_accepted, b, "n_accepted", i32), _vector(path, t, "path", i32),
+                                 _vector(next_token, b, "next_token", i32)), ctx)
+
+
+def c2kv_paged_keep(ctx, layers, table, tree_ptr, start, path, n_accepted):
+    """Move the rows that a walk kept together, in the pages of every layer (make_layers, or one layer's make_pages)."""
+    layers, (ptr, ptr_p, n), (st, st_p, m) = _fitting(ctx, layers), _i32_at(tree_ptr), _i32_at(start)
+    tb, w, ts = _table(table, n - 1, m)
+    i32 = _torch().int32
+    _check(_lib.c2kv_paged_keep(ctx, layers.address, layers.n, m, tb, w, ts, ptr_p, st_p, _vector(path, ptr[m], "path", i32),
+                                _vector(n_accepted, m, "n_accepted", i32)), ctx)
+
+
+def c2kv_beam_select(ctx, x, score, parent, token, score_out, norm=None, done=None, end_token=-1, done_out=None):
+    """The best continuations of beams: x [B * W, V] log-probabilities (or logits, with norm [B * W]), score [B, W];
+    parent, token, score_out (and done_out) [B, n] receive the n best."""
+    t = _torch()
+    if x.dtype is not t.float32 and x.dtype is not t.bfloat16:
+        raise ValueError(f"x must hold bfloat16 or float32, not {x.dtype}")
+    (b, w), (b2, best), (rows, vocab), i32, f32 = score.shape, parent.shape, x.shape, t.int32, t.float32
+    if b2 != b:
+        raise ValueError("score and parent must describe one batch")
+    at, stride = _rows(x, b * w, vocab, "x", x.dtype)
+    out = b * best
+    _check(_lib.c2kv_beam_select(ctx, b, w, vocab, best, DTYPE_F32 if x.dtype is f32 else DTYPE_BF16, at, stride,
+                                 _vector(norm, b * w, "norm", f32), _vector(score, b * w, "score", f32), _vector(done, b * w, "done", i32),
+                                 end_token, _vector(parent, out, "parent", i32), _vector(token, out, "token", i32),
+                                 _vector(score_out, out, "score_out", f32), _vector(done_out, out, "done_out", i32)), ctx)
+
+
+def c2kv_paged_reorder(ctx, layers, table, n_rows, parent, table_out):
+    """The beams' tables and pages after a choice: table [B * W, pages] by beam, n_rows [B], parent [B, W]; table_out
+    receives the new one."""
+    layers, (nr, nr_p, b) = _fitting(ctx, layers), _i32_at(n_rows)
+    if parent.dim() != 2 or parent.shape[0] != b:
+        raise ValueError("parent must be [B, W], as n_rows says")
+    width = parent.shape[1]
+    tb, w, ts = _table(table, b * width, b * width)
+    to, w2, to_s = _table(table_out, b * width, b * width)
+    if w2 != w:
+        raise ValueError("the new table must have the old one's width")
+    if b * width > 1 and to_s < w:
+        raise ValueError("rows of the new table must not share their memory")
+    _check(_lib.c2kv_paged_reorder(ctx, layers.address, layers.n, b, width, tb, w, ts, nr_p, _vector(parent, b * width, "parent", _torch().int32),
+                                   to, to_s), ctx)
 
 
 def c2kv_cache_release(ctx, cache):

@@ -1824,6 +1824,24 @@ MemKind mem_kind(const void* p) {
     return MemKind::kUnknown;
 }
 
+bool DeviceMemory::holds(const void* p) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    for (int i = 0; i < n_; ++i)
+        if (at >= known_[i].begin && at < known_[i].end) return true;
+    if (mem_kind(p) != MemKind::kDevice) return false;
+    using Fn = int (*)(unsigned long long*, size_t*, unsigned long long);    // (cuMemGetAddressRange: base, bytes, pointer)
+    static const Fn range_of = [] {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult q{};
+        if (cudaGetDriverEntryPointByVersion("cuMemGetAddressRange", &fn, 12000, cudaEnableDefault, &q) != cudaSuccess) (void)cudaGetLastError();
+        return q == cudaDriverEntryPointSuccess ? reinterpret_cast<Fn>(fn) : nullptr;
+    }();
+    unsigned long long base = 0;
+    size_t bytes = 0;
+    if (p && range_of && n_ < (int)(sizeof(known_) / sizeof(known_[0])) && range_of(&base, &bytes, at) == 0) known_[n_++] = {(uintptr_t)base, (uintptr_t)(base + bytes)};
+    return true;
+}
+
 bool context_view(const c2kv_ctx* c, ContextView* v) {
     if (!c || !v) return false;
     *v = ContextView{c->cfg.n_q_heads, c->cfg.n_kv_heads, c->cfg.head_dim, c->cfg.dtype, c->sms, c->stream, c->d_err, &c->turns};

@@ -270,4 +270,92 @@ struct VerifyCall {
 };
 cudaError_t launch_verify(const VerifyCall& c, cudaStream_t s);
 
+// The walk down a tree of drafted tokens (verify_tree.cu).
+template <int kReq>
+struct VerifyTreeParams {
+    const int32_t* tokens;   // [T] drafted tokens (the root's is not read)
+    const int32_t* parent;   // [T] among the request's nodes, -1 for a root
+    const float* p;          // [T] target's probabilities after each node, p_stride apart
+    const float* u;          // [T]
+    int32_t* n_accepted;     // [B]
+    int32_t* path;           // [T]
+    int32_t* next_token;     // [B]
+    int32_t* err;
+    int64_t p_stride;
+    int32_t vocab;
+    int32_t b0;
+    int32_t ptr[kReq + 1];
+};
+struct VerifyTreeCall {
+    const int32_t* tokens;
+    const int32_t* parent;
+    const float* p;
+    const float* u;
+    int32_t* n_accepted;
+    int32_t* path;
+    int32_t* next_token;
+    int32_t* err;
+    int64_t p_stride;
+    int32_t vocab;
+    int32_t batch;
+    const int32_t* ptr;      // host [batch + 1]
+};
+cudaError_t launch_verify_tree(const VerifyTreeCall& c, cudaStream_t s);
+
+// Rows moved within the pages of several layers, which share a table and their pages' geometry (paged_rows.cu).
+struct LayerPages {
+    void* k;
+    void* v;
+    float* k_scale;
+    float* v_scale;
+};
+struct PagedRowsCall {
+    PageView pg;             // geometry and table; its pages are layer 0's
+    const LayerPages* layers;     // host [n_layers]
+    int32_t n_layers;
+    int32_t hkv;
+    int32_t row_bytes;       // of one KV head's row of K or V
+    int32_t* err;
+    int32_t batch;
+    // rows of the tokens that a walk kept
+    const int32_t* ptr;      // host [batch + 1]
+    const int32_t* start;    // host [batch]
+    const int32_t* path;     // [T]
+    const int32_t* n_accepted;    // [batch]
+    // beams
+    const int32_t* n_rows;   // host [batch]
+    const int32_t* parent;   // [batch][width]
+    int32_t* table_out;      // [batch * width], table_out_stride apart
+    int64_t table_out_stride;
+    int32_t table_width;
+    int32_t width;
+};
+cudaError_t launch_paged_keep(const PagedRowsCall& c, cudaStream_t s);
+cudaError_t launch_paged_reorder(const PagedRowsCall& c, cudaStream_t s);
+constexpr int kBeamsMost = 64;           // beams of a request, and candidates that a choice leaves
+
+// The best continuations of beams over the vocabulary (beam_select.cu).
+struct BeamParams {
+    const void* x;           // [batch * width][vocab], x_stride elements apart
+    const float* norm;       // [batch * width] or null
+    const float* score;      // [batch * width]
+    const int32_t* done;     // [batch * width] or null
+    int32_t* parent;         // [batch][best]
+    int32_t* token;
+    float* score_out;
+    int32_t* done_out;       // or null
+    int64_t x_stride;
+    uint2* part;             // [batch][parts][best]: keys and places of each part's best
+    uint32_t* tickets;       // [batch], zero between launches
+    int32_t batch, width, vocab, best, end_token;
+    int32_t parts;           // CTAs of a request: `width` times those of a beam
+    int32_t per;             // values of a beam that one of them takes
+};
+struct BeamCall {
+    c2kv_ctx* ctx;
+    BeamParams p;            // (all but the partials)
+    bool bf16;
+};
+cudaError_t launch_beam_select(const BeamCall& c, cudaStream_t s);
+
 }  // namespace c2kv
