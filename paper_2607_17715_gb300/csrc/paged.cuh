@@ -348,8 +348,8 @@ struct BeamParams {
     uint2* part;             // [batch][parts][best]: keys and places of each part's best
     uint32_t* tickets;       // [batch], zero between launches
     int32_t batch, width, vocab, best, end_token;
-    int32_t parts;           // CTAs of a request: `width` times those of a beam
-    int32_t per;             // values of a beam that one of them takes
+    int32_t b0;              // the launch's first request
+    int32_t parts;           // CTAs (stretches) of a request
 };
 struct BeamCall {
     c2kv_ctx* ctx;

@@ -192,3 +192,25 @@ def test_a_loop_of_steps_without_the_host(ctx):
     P.lib().c2kv_sync(ctx)
     c.check()
     d.check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("batch,width", [(1, 2), (16, 12)])
+def test_masks_of_the_lowest_value(ctx, batch, width, dtype):
+    """Most of the vocabulary at the type's lowest value, here all of a stretch, there all but a few: the scores
+    round to one another's, and the first places win."""
+    rng = np.random.default_rng(4)
+    lowest = float(torch.finfo(P.TDT[dtype]).min)
+    x = np.full((batch * width, 40000), lowest)
+    for row in x[::2]:
+        at = rng.integers(0, 40000, 9)
+        row[at] = rng.standard_normal(9)
+    _run(ctx, batch, width, 40000, 8, dtype, x=x)
+    _run(ctx, batch, width, 40000, 16, dtype, x=np.where(x == lowest, -1e9, x), norm=True)
+
+
+def test_values_beside_large_scores(ctx):
+    """Scores so large that hundreds of values round to one score: places decide."""
+    x = np.random.default_rng(5).standard_normal((40, 50000))
+    _run(ctx, 1, 1, 50000, 16, x=x[:1], score=[[-3.0e6]])
+    _run(ctx, 20, 2, 50000, 16, x=x, score=-1.0e5 * np.arange(1, 41).reshape(20, 2))
