@@ -513,7 +513,7 @@ c2kv_status c2kv_paged_attend(c2kv_ctx* ctx, const c2kv_pages* pages, int32_t ba
  *               over rows j < x with j > x + depth_t - window, and rows x + a of the first `window` nodes a
  *               from t up                                     (x = n_keys - n, roots have depth 0)
  * Siblings have one position: turn says it, x + depth_t where rows stand for one position each.  A chain
- * (parent = node before) gives what c2kv_paged_attend gives.
+ * (parent = node before) is the attention of c2kv_paged_attend, to rounding.
  *   tree_ptr     : host int32 [B + 1], non-decreasing from 0; at most 512 nodes a request, and at most its
  *                  rows; a request may have none.
  *   n_keys, window, q, q_stride, turn, out, lse : as c2kv_paged_attend.

@@ -130,6 +130,9 @@ cudaError_t launch_paged_simt_tree(const PagedAttnCall& c, const PagedReq* req, 
 cudaError_t launch_paged_lane_tree(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
 cudaError_t launch_paged_mma_tree(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
 
+// bf16 trees of n requests on tcgen05, straight from the pages (paged_direct.cu).
+cudaError_t launch_paged_direct(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
+
 // Tensor map of pages [n_pages][Hkv][page_size][d], elements of 16 bits or codes of 8.
 bool encode_page_map(CUtensorMap* tm, const void* base, const PageView& pg, int hkv, int d, bool codes, int box_channels,
                      int box_rows, CUtensorMapSwizzle swizzle);

@@ -17,6 +17,9 @@ namespace {
 // requests take 8 and 19 % longer than on tcgen05.
 constexpr int kMmaRows = 64;
 
+// The same of trees, and the rows up to which tcgen05 takes them straight from the pages.
+constexpr int kTreeMmaRows = 32, kDirectRows = 512;
+
 // The same of fp32 contexts, and the keys that some request has to see for it: the lanes' kernel reads keys
 // again for every 4 rows, the register-tiled loop works on 16 rows or, below that, leaves most of its lanes
 // to wait.  Measured (us, lanes / tiles; 16-bit pages as good as 8-bit ones).  32 / 8 heads of 128 channels, 4
@@ -106,7 +109,17 @@ cudaError_t launch_paged_attn(const PagedAttnCall& c, int dtype, int d, bool cod
         if (e == cudaSuccess && !few.empty()) e = launch_paged_lane(c, few.data(), (int)few.size(), d, codes, s);
         return e;
     }
-    part(kMmaRows);
+    if (c.parent) {              // trees: those of middling size straight from the pages
+        std::vector<PagedReq> middling, rest;
+        for (const PagedReq& q : req) {
+            const int64_t rows = (int64_t)q.nq * (c.hq / c.hkv);
+            (rows > kTreeMmaRows && rows <= kDirectRows ? middling : rest).push_back(q);
+        }
+        if (!middling.empty()) e = launch_paged_direct(c, middling.data(), (int)middling.size(), d, codes, s);
+        if (e != cudaSuccess || rest.empty()) return e;
+        req.swap(rest);
+    }
+    part(c.parent ? kTreeMmaRows : kMmaRows);
     // requests of many rows on tcgen05, those of few on mma.sync
     if (!many.empty()) e = launch_many(c, many.data(), (int)many.size(), d, codes, s);
     if (e == cudaSuccess && !few.empty()) e = launch_paged_mma(c, few.data(), (int)few.size(), d, codes, s);

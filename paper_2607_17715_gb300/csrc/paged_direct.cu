@@ -1,0 +1,831 @@
+// Paged attention of trees of tokens whose rows fill a tile or two (c2kv_paged_attend_tree): tcgen05 straight from
+// the pages.
+//
+// Key tiles made ahead (paged_expand.cu) pay where many row tiles meet them.  Here a (request, KV head) has one or
+// two, of 128 rows each, and reading the pages bounds the call: TMA brings them into shared memory, and nothing but
+// partials goes back.  8-bit codes become f16 there, as they are; a key's K scale multiplies its scores and its V scale
+// its weights, in fp32 (a scale that is NaN makes NaN of the rows that see it).  16-bit pages are operands as they lie,
+// the queries two bf16 terms of them and the weights one, as in paged_mma.cu.
+//
+// A CTA has an SM to itself, in two groups of eight warps that take the tiles of 128 keys in turn, each with its own
+// scores and output in tensor memory: one's products and loads run beside the other's conversions and softmax (a row is
+// two threads' of a group, 64 keys each).  A ninth warp of each group issues its products and copies: where one of the
+// eight did, it waited for the tensor cores' queue, and they for it (7300 clocks a tile).  The groups' results join in
+// shared memory, the stretches' in a kernel of their own.
+//
+// Values of V that are not finite (16-bit pages): 0 times one is NaN for rows that do not see it, and a query's second
+// term makes NaN of an infinity of K.  A CTA whose results show either begins again with care: such values become zero in
+// the tile and are noted, and the rows that see them take them in at the end; keys of a tile with an infinity meet the
+// first terms alone.
+#include "paged_tile.cuh"
+
+#include <algorithm>
+#include <cuda_fp16.h>
+#include <optional>
+#include <vector>
+
+namespace c2kv {
+namespace {
+
+constexpr int kDirGroup = 256, kDirThreads = 2 * kDirGroup + 128;         // (the last warpgroup's first two warps issue)
+// Registers: 96 a thread at launch, of which the last warpgroup gives up what the others take.
+constexpr int kDirRegs = 96, kDirRegsIssue = 64, kDirRegsOthers = 104;
+static_assert(2 * kDirGroup * kDirRegsOthers + 128 * kDirRegsIssue <= kDirThreads * kDirRegs, "register split");
+constexpr uint32_t kDirTmem = 512;       // a group: S (P over the first half of each half of it), O
+constexpr int kLeastTiles = 2;           // of a stretch: one a group
+constexpr int kMostCuts = 256;           // stretches of one unit's keys: their weights join in shared memory
+
+template <int kReq>
+struct DirectLaunch {
+    CUtensorMap tm_k, tm_v;              // [n_pages][Hkv][page_size][d], boxes of a page's rows (at most 128)
+    uint4* odd;                          // [key tile][Hkv]: rows of V with values that are not finite (16-bit pages)
+    float* part_o;                       // [item][128][D] normalised
+    float* part_lse;                     // [item][128] log2 domain
+    PagedAttn<kReq> a;
+};
+
+// Shared memory: queries, then each group's tiles and what is small.
+template <int D, bool kCodes>
+struct Dir : TileOf<D> {
+    using TileOf<D>::kTile;
+    static constexpr int kRaw = kCodes ? BN * D : 0;       // bytes of a tile of codes
+    static constexpr int kQ = (kCodes ? 1 : 2) * kTile;
+    static constexpr int kGroupBytes = 2 * kTile + 2 * kRaw;                  // K, V, and as they come
+    static constexpr int kSmall = kQ + 2 * kGroupBytes;    // [group] (codes) scales of K and V, (else) a row's two values
+    static constexpr int kBack = kSmall + 2 * 1024;        // powers of two of the queries' rows: a byte each
+    static constexpr int kBars = kBack + BM;               // [group] scores, output, K, V, tiles of K and of V ready, weights, scales
+    static constexpr int kWords = kBars + 2 * 8 * 8;       // tensor memory, abort, [group] K not finite, rows touched (four), [group][2] pages
+    static constexpr int kSmem = kWords + 64;
+};
+static_assert(Dir<128, true>::kSmem <= 232448 && Dir<128, false>::kSmem <= 232448, "shared memory of a CTA");
+
+// Two products, rounded as one each.
+__device__ __forceinline__ void fmul2(float& d0, float& d1, float a0, float a1, float b0, float b1) {
+    asm("{\n\t.reg .b64 pa, pb, pd;\n\t"
+        "mov.b64 pa, {%2, %3};\n\t"
+        "mov.b64 pb, {%4, %5};\n\t"
+        "mul.rn.f32x2 pd, pa, pb;\n\t"
+        "mov.b64 {%0, %1}, pd;\n\t}"
+        : "=f"(d0), "=f"(d1)
+        : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+
+__device__ __forceinline__ void group_sync(int g) { asm volatile("bar.sync %0, 256;" ::"r"(1 + g) : "memory"); }
+__device__ __forceinline__ bool group_or(int g, bool x) {
+    uint32_t any;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(any)
+                 : "r"((uint32_t)x), "r"(1 + g)
+                 : "memory");
+    return any != 0u;
+}
+
+// The queries' rows of a warp (32), turned, as two bf16 terms: the first in place, what it lacks a tile behind.
+template <int D, int kReq>
+__device__ __forceinline__ void turn_queries_twice(const PagedAttn<kReq>& P, const QueryRows<D>& k, int warp, int lane, uint32_t sQ) {
+    using C = TileOf<D>;
+    constexpr int E = QueryRows<D>::E;
+    const int r0 = warp * 32, c = lane * E, q0 = c >> 3, q1 = (D / 2 + c) >> 3;
+    cp_async_wait<0>();
+    __syncwarp();
+    float2 cs[E];
+    int pos_cs = __shfl_sync(0xffffffffu, k.pos, 0);
+#pragma unroll
+    for (int e = 0; e < E; ++e) cs[e] = turn_cs_fast(k.turn[e], pos_cs);
+#pragma unroll 4
+    for (int i = 0; i < 32; ++i) {
+        const uint32_t at = sQ + (r0 + i) * 128 + (c & 7) * 2;
+        const uint32_t a0 = at + (q0 >> 3) * C::kHalf + (((q0 & 7) ^ (i & 7)) << 4), a1 = at + (q1 >> 3) * C::kHalf + (((q1 & 7) ^ (i & 7)) << 4);
+        uint32_t x0, x1;
+        if constexpr (E == 2) {
+            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x0) : "r"(a0));
+            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x1) : "r"(a1));
+        } else {
+            uint16_t y0, y1;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y0) : "r"(a0));
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y1) : "r"(a1));
+            x0 = y0;
+            x1 = y1;
+        }
+        float x[E], y[E], lo[E], hi[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            lo[e] = x[e] = __uint_as_float(e == 0 ? x0 << 16 : x0 & 0xffff0000u);
+            hi[e] = y[e] = __uint_as_float(e == 0 ? x1 << 16 : x1 & 0xffff0000u);
+        }
+        if (P.turn) {
+            const int pos = __shfl_sync(0xffffffffu, k.pos, i);
+            if (pos != pos_cs) {                             // the heads of a token share its angles
+#pragma unroll
+                for (int e = 0; e < E; ++e) cs[e] = turn_cs_fast(k.turn[e], pos);
+                pos_cs = pos;
+            }
+            rotate<E>(x, y, cs, lo, hi);
+        }
+        // (what is left of an infinity is nothing)
+        auto left = [](float v, uint32_t first) {
+            const float d = v - __uint_as_float(first << 16);
+            return fabsf(d) < 3.0e38f ? d : 0.f;
+        };
+        const uint32_t f0 = pack_bf16(lo[0], E == 2 ? lo[E - 1] : 0.f), f1 = pack_bf16(hi[0], E == 2 ? hi[E - 1] : 0.f);
+        const uint32_t s0 = pack_bf16(left(lo[0], f0 & 0xffffu), E == 2 ? left(lo[E - 1], f0 >> 16) : 0.f);
+        const uint32_t s1 = pack_bf16(left(hi[0], f1 & 0xffffu), E == 2 ? left(hi[E - 1], f1 >> 16) : 0.f);
+        if constexpr (E == 2) {
+            asm volatile("st.shared.u32 [%0], %1;" ::"r"(a0), "r"(f0));
+            asm volatile("st.shared.u32 [%0], %1;" ::"r"(a1), "r"(f1));
+            asm volatile("st.shared.u32 [%0], %1;" ::"r"(a0 + C::kTile), "r"(s0));
+            asm volatile("st.shared.u32 [%0], %1;" ::"r"(a1 + C::kTile), "r"(s1));
+        } else {
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(a0), "h"((uint16_t)f0));
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(a1), "h"((uint16_t)f1));
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(a0 + C::kTile), "h"((uint16_t)s0));
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(a1 + C::kTile), "h"((uint16_t)s1));
+        }
+    }
+}
+
+// Which rows of a key tile are there: of 16-key groups that lie in pages (bits), from lo to below hi.
+struct Rows {
+    uint32_t groups;
+    int lo, hi;
+    __device__ __forceinline__ bool all() const { return groups == 0xffu && lo <= 0 && hi >= BN; }
+    __device__ __forceinline__ bool has(int row) const { return (groups >> (row >> 4) & 1u) != 0u && row >= lo && row < hi; }
+    // of 32 rows from 32 k on, a bit each
+    __device__ __forceinline__ uint32_t of32(int k) const {
+        return within((groups >> (2 * k) & 1u ? 0xffffu : 0u) | (groups >> (2 * k + 1) & 1u ? 0xffff0000u : 0u), 32 * k, lo - 1, hi - 1);
+    }
+};
+
+// A tile of codes [128][D] as f16 in 64-channel blocks under the 128-byte swizzle, by a group's threads; (not `all`) rows
+// that are not there become zero.
+template <int D>
+__device__ __forceinline__ void codes_to_f16(uint32_t raw, uint32_t tile, int t, bool all, const Rows& rows) {
+    constexpr int kChunks = D / 16, kStep = kDirGroup / kChunks, kPasses = BN / kStep;
+    const int chunk = t % kChunks, block = chunk / 4, q = chunk % 4 * 2, first = block & 1;
+    uint4 w[kPasses];
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) w[i] = lds128(raw + (t / kChunks + kStep * i) * D + chunk * 16);
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+        const int row = t / kChunks + kStep * i;
+        if (!all && !rows.has(row)) w[i] = make_uint4(0u, 0u, 0u, 0u);
+        const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+        uint32_t y[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e]) : "h"((uint16_t)x[e]));
+            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e + 1]) : "h"((uint16_t)(x[e] >> 16)));
+        }
+        const uint32_t at = tile + block * TileOf<D>::kHalf + row * 128;
+        // (the blocks' threads begin with different halves, so that a row's eight meet all banks)
+        const uint4 a = make_uint4(y[0], y[1], y[2], y[3]), b = make_uint4(y[4], y[5], y[6], y[7]);
+        sts128_(at + (((q + first) ^ (row & 7)) << 4), first ? b : a);
+        sts128_(at + (((q + 1 - first) ^ (row & 7)) << 4), first ? a : b);
+    }
+}
+
+// (16-bit pages) whether a tile has values that are not finite in the thread's row; and V's tile put right: rows that are
+// not there become zero, with care values that are not finite too, and whether there were any.  Two threads a row.
+template <int D>
+__device__ __forceinline__ bool tile_odd(uint32_t tile, int t, const Rows& rows) {
+    const int row = t / 2;
+    bool odd = false;
+    if (!rows.has(row)) return false;
+#pragma unroll 4
+    for (int i = 0; i < D / 16; ++i) {
+        const int line = (t & 1) * (D / 16) + i;
+        const uint4 w = lds128(tile + line / 8 * TileOf<D>::kHalf + row * 128 + line % 8 * 16);
+        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) odd = odd || (((x[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0u;
+    }
+    return odd;
+}
+template <int D>
+__device__ __forceinline__ bool put_right(uint32_t tile, int t, const Rows& rows, bool care) {
+    const int row = t / 2;
+    const bool there = rows.has(row);
+    bool odd = false;
+    if (there && !care) return false;
+#pragma unroll 1
+    for (int i = 0; i < D / 16; ++i) {
+        const int line = (t & 1) * (D / 16) + i;
+        const uint32_t at = tile + line / 8 * TileOf<D>::kHalf + row * 128 + line % 8 * 16;
+        uint4 w = make_uint4(0u, 0u, 0u, 0u);
+        if (there) {
+            w = lds128(at);
+            uint32_t* const x = reinterpret_cast<uint32_t*>(&w);
+            uint32_t any = 0u;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {                    // (an exponent of ones carries into the bit above it)
+                const uint32_t out = ((x[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+                any |= out;
+                x[e] &= ~((out >> 15) * 0xffffu);
+            }
+            if (any == 0u) continue;
+            odd = true;
+        }
+        sts128_(at, w);
+    }
+    return odd;
+}
+
+template <int D, bool kCodes, int kReq>
+__global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __grid_constant__ DirectLaunch<kReq> X) {
+    using T = __nv_bfloat16;
+    using C = Dir<D, kCodes>;
+    constexpr uint32_t idS = kCodes ? idesc_f16(BM, BN, false) : idesc_bf16(BM, BN, false);
+    constexpr uint32_t idO = kCodes ? idesc_f16(BM, D, true) : idesc_bf16(BM, D, true);
+    constexpr int EB = kCodes ? 1 : 2, kBox = kCodes ? D : 64;       // channels of a TMA box
+    const PagedAttn<kReq>& P = X.a;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const bool issues = threadIdx.x >= 2 * kDirGroup;        // (its group's ninth warp; the two behind it have nothing to do)
+    const int g = issues ? threadIdx.x / 32 & 1 : threadIdx.x / kDirGroup, t = threadIdx.x % kDirGroup;
+    const int warp = issues ? 8 : t / 32, lane = threadIdx.x % 32;            // of the group
+    const uint32_t sQ = smem_u32(smem), sK = sQ + C::kQ + g * C::kGroupBytes, sV = sK + C::kTile;
+    const uint32_t inK = kCodes ? sV + C::kTile : sK, inV = kCodes ? inK + C::kRaw : sV;      // where the pages go
+    float* const scales = reinterpret_cast<float*>(smem + C::kSmall) + g * BN * 2;            // (codes) [K, V][key]
+    // a row's two values; with codes over the K tile, which the scores have been formed of by then
+    float* const two = kCodes ? reinterpret_cast<float*>(smem + C::kQ + g * C::kGroupBytes) : scales;
+    int8_t* const s_back = reinterpret_cast<int8_t*>(smem + C::kBack);
+    const uint32_t bars = sQ + C::kBars + g * 64, barS = bars, barO = bars + 8, barK = bars + 16, barV = bars + 24;
+    const uint32_t readyK = bars + 32, readyV = bars + 40, readyP = bars + 48, readyC = bars + 56;     // (an arrival a warp)
+    uint32_t* const words = reinterpret_cast<uint32_t*>(smem + C::kWords);
+    volatile uint32_t* const abort = words + 1;
+    volatile uint32_t* const s_alone = words + 2 + g;         // the queries' first terms alone: K's tile has values that are not finite
+    uint32_t* const s_touched = words + 4;                    // [4]: a bit a row
+    volatile uint32_t* const s_groups = words + 8 + 2 * g;    // [2]: which 16-key groups of a tile lie in pages, every other tile's
+    if ((sQ & 1023u) != 0u) {                                 // (tiles lie on their swizzle's pattern: it always does)
+        if (threadIdx.x == 0) atomicOr(P.err, 2);
+        return;
+    }
+    const Item w = find_item<true, BM>(P, (int)blockIdx.x);
+    const int hi = w.R.n_keys, head = w.hk << P.pg.page_shift;        // the head's first row in a page
+    const int32_t* const table = P.pg.table + (int64_t)w.R.row * P.pg.table_stride;
+    const int box_rows = min(BN, 1 << P.pg.page_shift), boxes = BN / box_rows;
+    const int n = threadIdx.x >= 2 * kDirGroup + 64 ? 0 : (w.n + 1 - g) / 2;         // the group's tiles: g, g + 2, ..
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 16; ++i) mbar_init(sQ + C::kBars + 8 * i, i % 8 < 4 || i % 8 == 7 ? 1 : 8);
+        *abort = 0u;
+        for (int i = 0; i < 4; ++i) s_touched[i] = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&X.tm_k)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&X.tm_v)) : "memory");
+    }
+    if (threadIdx.x / 32 == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(words)), "r"(kDirTmem) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    after_kernels_before();
+    // the page of box `lane` (and, codes, of 16-key group lane % 8) of the group's tile i, -1 for none or without a key that
+    // any query sees
+    auto key_of = [&](int i) { return (w.j0 + 2 * i + g) * BN; };
+    auto page_at = [&](int i, int key) {
+        // (pages that a window has left behind may be gone from the table)
+        if (i >= n || key >= hi || ((key >> P.pg.page_shift) + 1) << P.pg.page_shift <= w.k_lo) return -1;
+        const int page = ld_after(table + (key >> P.pg.page_shift));
+        if (page >= 0 && page < P.pg.n_pages) return page;
+        atomicOr(P.err, 1);
+        return -1;
+    };
+    auto pages_of = [&](int i) { return page_at(i, key_of(i) + (lane & 7) * 16); };
+    // tile of `pages` (of 16-key groups) into shared memory, by a whole warp
+    auto bring = [&](const CUtensorMap* tm, uint32_t to, uint32_t bar, int pages) {
+        const int p = __shfl_sync(0xffffffffu, pages, lane * (box_rows / 16) & 7);
+        const bool mine = lane < boxes && p >= 0;
+        const uint32_t count = __popc(__ballot_sync(0xffffffffu, mine));
+        if (lane == 0) mbar_expect_tx(bar, count * (uint32_t)(box_rows * D * EB));
+        __syncwarp();
+        if (mine) {
+#pragma unroll
+            for (int b = 0; b < D / kBox; ++b)
+                tma_load_4d(to + b * TileOf<D>::kHalf + lane * box_rows * (kBox * EB), tm, b * kBox, 0, w.hk, p, bar);
+        }
+    };
+    // (codes) K's and V's scales of keys 32 e + lane of the group's tile i, by the ninth warp
+    auto ask_scales = [&](int i, int pages, float (&x)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int key = (e & 3) * 32 + lane, p = __shfl_sync(0xffffffffu, pages, key >> 4), at = key_of(i) + key;
+            const bool ok = p >= 0 && at >= w.k_lo && at < hi;
+            x[e] = 0.f;
+            if (ok) x[e] = ld_after((e < 4 ? P.pg.k_scale : P.pg.v_scale) + (int64_t)p * P.pg.scale_stride + head + (key & ((1 << P.pg.page_shift) - 1)));
+        }
+    };
+    int pages = -1, pages1 = -1;                              // (the ninth warp) of 16-key groups of this tile and the next
+    QueryRows<D> rows;
+    if (g == 0 && warp < 4) rows = fetch_queries<D>(P, w, warp, lane, sQ);
+    tc_fence_before();
+    __syncthreads();                                          // (barriers, tensor memory)
+    tc_fence_after();
+    const uint32_t tmem = words[0] + (uint32_t)(g * 256), tmemO = tmem + BN;
+    // the kernel that joins cut keys may be set up from here on: it waits for this grid to end
+    if (threadIdx.x == 0) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    const int G = P.hq / P.hkv, half = warp / 4, row = warp % 4 * 32 + lane;        // (half 2: issues, for no row)
+    const uint32_t lane_addr = (uint32_t)(warp % 4 * 32) << 16;
+    const uint32_t colS = tmem + lane_addr + (uint32_t)(half * 64), colO = tmemO + lane_addr + (uint32_t)(half * (D / 2));
+    const Climb<PagedAttn<kReq>> sight(P, w, (w.row0 + min(row, w.live - 1)) / G);
+    float ref = -CUDART_INF_F, l = 0.f;
+    bool touched = false;                                     // by values that are not finite
+    uint32_t uses = 0;                                        // of the barriers, parity of their next phase: a tile each
+    bool ready = false;                                       // the queries are
+
+    auto arrive = [&](uint32_t bar) {                         // the warp has written what the products read
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar);
+    };
+    // The ninth warp.
+    auto issue = [&](auto with_care) {
+        [[maybe_unused]] constexpr bool kCare = decltype(with_care)::value;
+        [[maybe_unused]] float x[8];
+        // K of tile i, V of tile i, and what the others need to know of it
+        auto bring_k = [&](int i, int pages) {
+            const uint32_t there = __ballot_sync(0xffffffffu, pages >= 0) & 0xffu;
+            if (lane == 0) s_groups[i & 1] = there;
+            bring(&X.tm_k, inK, barK, pages);
+        };
+        auto put_scales = [&] {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) scales[e * 32 + lane] = x[e];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(readyC);
+        };
+        pages = pages_of(0);
+        pages1 = pages_of(1);
+        if (n > 0) {
+            bring_k(0, pages);
+            bring(&X.tm_v, inV, barV, pages);
+            if constexpr (kCodes) {
+                ask_scales(0, pages, x);
+                put_scales();
+            }
+        }
+        if (!ready) __syncthreads();
+        ready = true;
+        const uint64_t dq = sw128_desc(sQ, 16, 1024), dk = sw128_desc(sK, 16, 1024), dv = sw128_desc(sV, C::kHalf, 1024);
+        auto scores = [&](int i, uint32_t phase) {
+            if constexpr (!kCodes) mbar_wait(barK, phase, P.err, abort);
+            if constexpr (kCodes) mbar_wait(readyK, phase, P.err, abort);
+            else if constexpr (kCare) mbar_wait(readyK, (uint32_t)i & 1u, P.err, abort);      // (this way round alone)
+            if (lane == 0) {
+                tc_fence_after();
+                const bool alone = kCare && *s_alone != 0u;
+#pragma unroll
+                for (int y = kCodes ? 0 : 1; y >= 0; --y) {
+                    if (y == 1 && alone) continue;
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const uint64_t off = (uint64_t)(((kk >> 2) * C::kHalf + (kk & 3) * 32) >> 4);
+                        mma_bf16(tmem, dq + (uint64_t)(y * C::kTile >> 4) + off, dk + off, idS, kk > 0 || (!kCodes && y == 0 && !alone) ? 1u : 0u);
+                    }
+                }
+                mma_commit(barS);
+            }
+            __syncwarp();
+        };
+        if (n > 0) scores(0, uses);
+        for (int i = 0; i < n; ++i, uses ^= 1u) {
+            const int pages2 = pages_of(i + 2);
+            const bool more = i + 1 < n;
+            // K's next tile where this one's has been read: by the conversion, or by the products
+            if constexpr (!kCodes) mbar_wait(barS, uses, P.err, abort);
+            if (more) bring_k(i + 1, pages1);
+            if constexpr (kCodes) {
+                if (more) ask_scales(i + 1, pages1, x);
+                mbar_wait(readyV, uses, P.err, abort);
+                if (more) bring(&X.tm_v, inV, barV, pages1);
+            }
+            mbar_wait(readyP, uses, P.err, abort);
+            if constexpr (!kCodes) mbar_wait(barV, uses, P.err, abort);
+            if (lane == 0) {
+                tc_fence_after();
+#pragma unroll
+                for (int kk = 0; kk < BN / 16; ++kk)
+                    mma_bf16_ts(tmemO, tmem + (uint32_t)kk * 8u, dv + (uint64_t)((kk * 16 * 128) >> 4), idO, kk > 0 || i > 0 ? 1u : 0u);
+                mma_commit(barO);
+            }
+            __syncwarp();
+            if constexpr (kCodes) {
+                if (more) put_scales();                       // (the weights have taken the ones before)
+            }
+            if (more) scores(i + 1, uses ^ 1u);
+            if constexpr (!kCodes) {
+                mbar_wait(barO, uses, P.err, abort);
+                if (more) bring(&X.tm_v, inV, barV, pages1);
+            }
+            pages = pages1;
+            pages1 = pages2;
+        }
+    };
+    // The others.
+    auto tiles = [&](auto with_care) {
+        [[maybe_unused]] constexpr bool kCare = decltype(with_care)::value;
+        ref = -CUDART_INF_F;
+        l = 0.f;
+        if (!ready) {                                         // the first tiles are on their way meanwhile
+            if (g == 0 && warp < 4) {
+                if constexpr (kCodes) turn_queries<D>(P, rows, warp, lane, sQ, s_back);
+                else turn_queries_twice<D>(P, rows, warp, lane, sQ);
+                fence_proxy_async();
+            }
+            __syncthreads();
+            ready = true;
+        }
+        const float f = kCodes ? P.scale_log2 * pow2i(s_back[row]) : P.scale_log2;
+        for (int i = 0; i < n; ++i, uses ^= 1u) {
+            const int key0 = key_of(i);
+            if constexpr (kCodes) {
+                group_sync(g);                                // (`two` has been read: K's tile lies there)
+                mbar_wait(barK, uses, P.err, abort);
+                codes_to_f16<D>(inK, sK, t, true, Rows{});     // (hidden keys' scores are replaced)
+                fence_proxy_async();
+                arrive(readyK);
+            } else if constexpr (kCare) {
+                mbar_wait(barK, uses, P.err, abort);
+            } else {
+                mbar_wait(barS, uses, P.err, abort);
+            }
+            // (written ahead of what has been waited for)
+            const Rows rows{s_groups[i & 1], w.k_lo - key0, hi - key0};
+            const bool whole_tile = rows.all();
+            if constexpr (kCodes) {
+                if (i > 0) mbar_wait(barO, uses ^ 1u, P.err, abort);                 // the products before have read V
+                mbar_wait(barV, uses, P.err, abort);
+                codes_to_f16<D>(inV, sV, t, whole_tile, rows);
+                fence_proxy_async();
+                arrive(readyV);
+                mbar_wait(readyC, uses, P.err, abort);
+            } else if constexpr (kCare) {
+                const bool odd = group_or(g, tile_odd<D>(sK, t, rows));
+                if (t == 0) *s_alone = odd;
+                arrive(readyK);
+            }
+            if (!kCodes && (kCare || !whole_tile)) {
+                mbar_wait(barV, uses, P.err, abort);
+                const bool odd = put_right<D>(sV, t, rows, kCare);
+                fence_proxy_async();
+                if constexpr (kCare) {                        // a row's two threads, then its bit
+                    const uint32_t two_bits = __ballot_sync(0xffffffffu, odd);
+                    if (lane == 0) {
+                        const uint32_t m = two_bits | two_bits >> 1;
+                        uint32_t bits = 0;
+                        for (int k = 0; k < 16; ++k) bits |= (m >> (2 * k) & 1u) << k;
+                        reinterpret_cast<uint16_t*>(two)[warp] = (uint16_t)bits;     // (16 rows a warp; group_or is behind `two`'s readers)
+                    }
+                    group_sync(g);
+                    const uint4 note = *reinterpret_cast<const uint4*>(two);
+                    uint32_t lo, up;                          // (the row's other thread looks at the other half)
+                    sight.of64(key0 + half * 64, lo, up);
+                    touched = touched || ((half ? note.z : note.x) & lo) || ((half ? note.w : note.y) & up);
+                    if (t == 0) X.odd[(int64_t)(w.R.scratch + w.j0 + 2 * i + g) * P.hkv + w.hk] = note;
+                    group_sync(g);                            // (`two` is written again below)
+                }
+            }
+
+            // the softmax of the thread's 64 keys
+            mbar_wait(barS, uses, P.err, abort);
+            tc_fence_after();
+            uint32_t sv[2][32];
+            tmem_ld32(colS, sv[0]);
+            tmem_ld32(colS + 32, sv[1]);
+            tmem_ld_wait();
+            int v_unit = 0;
+            if constexpr (kCodes) {                           // the power of two above the largest of V's scales
+                const float4 x = reinterpret_cast<const float4*>(scales + BN)[lane];
+                uint32_t top = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t y = __float_as_uint(e == 0 ? x.x : e == 1 ? x.y : e == 2 ? x.z : x.w) & 0x7fffffffu;
+                    top = max(top, y < 0x7f800000u ? y : 0u);
+                }
+                top = __reduce_max_sync(0xffffffffu, top);
+                v_unit = top == 0u ? 0 : max(-90, min(126, (int)(top >> 23) - 126));
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) {
+                        const float4 ks = *reinterpret_cast<const float4*>(scales + half * 64 + c * 32 + e);
+                        float y[4];
+                        fmul2(y[0], y[1], __uint_as_float(sv[c][e]), __uint_as_float(sv[c][e + 1]), f, f);
+                        fmul2(y[2], y[3], __uint_as_float(sv[c][e + 2]), __uint_as_float(sv[c][e + 3]), f, f);
+                        fmul2(y[0], y[1], y[0], y[1], ks.x, ks.y);
+                        fmul2(y[2], y[3], y[2], y[3], ks.z, ks.w);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) sv[c][e + k] = __float_as_uint(y[k]);
+                    }
+            }
+            const bool edge = !whole_tile || !sight.sees_tile(key0);
+            uint32_t seen[2] = {0xffffffffu, 0xffffffffu};
+            if (edge) {
+                sight.of64(key0 + half * 64, seen[0], seen[1]);
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    seen[c] &= rows.of32(half * 2 + c);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if (!(seen[c] >> e & 1u)) sv[c][e] = __float_as_uint(-CUDART_INF_F);
+                }
+            }
+            float m = -CUDART_INF_F;
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) m = fmax3(m, __uint_as_float(sv[c][e]), __uint_as_float(sv[c][e + 1]));
+            two[half * BM + row] = m;
+            tc_fence_before();
+            group_sync(g);                                    // (and every score is in registers: weights may lie over them)
+            tc_fence_after();
+            m = fmaxf(two[row], two[BM + row]);
+            const float most = kCodes ? m + (float)v_unit : m * f;
+            const bool moves = most > ref + kRoom;            // (from -inf: any number)
+            if (__any_sync(0xffffffffu, moves)) {
+                float alpha = 1.f;
+                if (moves) {
+                    alpha = ex2(ref - (most - kBelow));
+                    ref = most - kBelow;
+                }
+                l *= alpha;
+                if (i > 0) {
+#pragma unroll 1
+                    for (int c = 0; c < D / 32; ++c) {
+                        uint32_t ov[16];
+                        tmem_ld16(colO + c * 16, ov);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * alpha);
+                        tmem_st16(colO + c * 16, ov);
+                    }
+                }
+            }
+            auto weigh = [&](auto hides) {
+                float ps[4] = {0.f, 0.f, 0.f, 0.f};
+                const float off = ref == -CUDART_INF_F ? 0.f : -ref;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {                 // sixteen keys at a time
+                    uint32_t pk[8];
+                    [[maybe_unused]] float4 vs;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int e = (c % 2) * 16 + 2 * k;
+                        float a0 = __uint_as_float(sv[c / 2][e]), a1 = __uint_as_float(sv[c / 2][e + 1]);
+                        if constexpr (kCodes) fadd2(a0, a1, off, off);
+                        else ffma2(a0, a1, a0, a1, f, off);
+                        a0 = ex2(a0);
+                        a1 = ex2(a1);
+                        if (k & 1) fadd2(ps[2], ps[3], a0, a1);
+                        else fadd2(ps[0], ps[1], a0, a1);
+                        if constexpr (kCodes) {
+                            if (k % 2 == 0) vs = *reinterpret_cast<const float4*>(scales + BN + half * 64 + (c / 2) * 32 + e);
+                            fmul2(a0, a1, a0, a1, k % 2 ? vs.z : vs.x, k % 2 ? vs.w : vs.y);
+                            if constexpr (decltype(hides)::value) {          // a hidden key's scale may be anything
+                                if (!(seen[c / 2] >> e & 1u)) a0 = 0.f;
+                                if (!(seen[c / 2] >> (e + 1) & 1u)) a1 = 0.f;
+                            }
+                            pk[k] = pack_f16(a0, a1);
+                        } else {
+                            pk[k] = pack_bf16(a0, a1);
+                        }
+                    }
+                    tmem_st8(tmem + lane_addr + (uint32_t)(half * 32 + c * 8), pk);
+                }
+                l += (ps[0] + ps[1]) + (ps[2] + ps[3]);
+            };
+            // (edges differ from row to row: the warp's)
+            if (kCodes && __any_sync(0xffffffffu, edge)) weigh(std::true_type{});
+            else weigh(std::false_type{});
+            tmem_st_wait();
+            tc_fence_before();
+            arrive(readyP);
+        }
+        if (n > 0) {
+            mbar_wait(barO, uses ^ 1u, P.err, abort);
+            tc_fence_after();
+        }
+    };
+    // (the same barriers of all warps on both ways)
+    if (issues) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDirRegsIssue));
+        issue(std::false_type{});
+        if constexpr (!kCodes)
+            if (__syncthreads_or(0)) issue(std::true_type{});
+        for (int i = 0; i < 4; ++i) __syncthreads();
+        return;
+    }
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kDirRegsOthers));
+    tiles(std::false_type{});
+    if constexpr (!kCodes) {
+        // values that are not finite: of a sum, or (where weights of zero met them) of the output
+        float z = l * 0.f;
+        if (n > 0) {
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t ov[16];
+                tmem_ld16(colO + c * 16, ov);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) z = fmaf(__uint_as_float(ov[e]), 0.f, z);
+            }
+        }
+        tc_fence_before();
+        if (__syncthreads_or(z != 0.f)) {
+            tc_fence_after();
+            tiles(std::true_type{});
+        }
+    }
+
+    // (found again: kept over the tiles it would take registers of theirs)
+    int item;
+    asm volatile("mov.u32 %0, %%ctaid.x;" : "=r"(item));
+    const Item v = find_item<true, BM>(P, item);
+    const bool there = row < v.live;
+    const int my = min(row, v.live - 1), tok = (v.row0 + my) / G;
+
+    // the groups join: the second's output, in units of the common reference, through its tiles, a column a row of them
+    float* const joined = reinterpret_cast<float*>(smem + C::kQ + C::kGroupBytes);            // [D][128]
+    float* const of_second = reinterpret_cast<float*>(smem + C::kSmall);                      // [reference, sum, of the first][128]
+    group_sync(g);                                            // (they have been read)
+    two[half * BM + row] = l;
+    group_sync(g);
+    l = two[row] + two[BM + row];
+    tc_fence_before();
+    __syncthreads();                                          // (what lay there has been read)
+    tc_fence_after();
+    if (half == 0) (of_second + 2 * BM * g)[row] = ref, (of_second + 2 * BM * g)[BM + row] = l;
+    if (touched) atomicOr(s_touched + row / 32, 1u << (row & 31));
+    __syncthreads();
+    const float ref0 = of_second[row], l0 = of_second[BM + row], ref1 = of_second[2 * BM + row], l1 = of_second[3 * BM + row];
+    const float top = fmaxf(ref0, ref1), base = top == -CUDART_INF_F ? 0.f : top;
+    const float a0 = ex2(ref0 - base), a1 = ex2(ref1 - base);
+    if (g == 1) {
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+            uint32_t ov[16];
+            if (n > 0) {
+                tmem_ld16(colO + c * 16, ov);
+                tmem_ld_wait();
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) joined[(half * (D / 2) + c * 16 + e) * BM + row] = n > 0 ? __uint_as_float(ov[e]) * a1 : 0.f;
+        }
+    }
+    __syncthreads();
+    l = fmaf(l0, a0, l1 * a1);
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    const float lse2 = l == 0.f ? -CUDART_INF_F : top + log2f(l);
+    const bool whole = v.R.splits == 1;
+    if (g == 0) {
+        const int64_t out_tok = v.R.q0 + tok;
+        const int h = v.hk * G + (v.row0 + my) % G;
+        T* const orow = static_cast<T*>(P.out) + (out_tok * P.hq + h) * D + half * (D / 2);
+        float* const prow = X.part_o + ((int64_t)item * BM + row) * D + half * (D / 2);
+        const bool wide = (reinterpret_cast<uintptr_t>(P.out) & 31u) == 0;
+        const float none = there && whole && l == 0.f ? of_no_weight<true>(P, v.R, tok) : 0.f;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+            uint32_t ov[16];
+            if (n > 0) {
+                tmem_ld16(colO + c * 16, ov);
+                tmem_ld_wait();
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float y = fmaf(n > 0 ? __uint_as_float(ov[e]) : 0.f, a0, joined[(half * (D / 2) + c * 16 + e) * BM + row]);
+                ov[e] = __float_as_uint(l == 0.f ? none : y * inv);
+            }
+            if (!there) continue;
+            if (whole) {
+                uint32_t o8[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o8[e] = pack_bf16(__uint_as_float(ov[2 * e]), __uint_as_float(ov[2 * e + 1]));
+                if (wide) {
+                    stg256(orow + c * 16, o8);
+                } else {
+                    *reinterpret_cast<uint4*>(orow + c * 16) = make_uint4(o8[0], o8[1], o8[2], o8[3]);
+                    *reinterpret_cast<uint4*>(orow + c * 16 + 8) = make_uint4(o8[4], o8[5], o8[6], o8[7]);
+                }
+            } else {
+                stg256(prow + c * 16, ov);
+                stg256(prow + c * 16 + 8, ov + 8);
+            }
+        }
+        if (there && half == 0) {
+            if (!whole) X.part_lse[(int64_t)item * BM + row] = lse2;
+            else if (P.lse) P.lse[(int64_t)h * P.n_tokens + out_tok] = lse2 * 0.69314718055994531f;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();                                          // (a row's other half is written, too)
+    if (!kCodes && g == 0 && half == 0) {
+        const uint32_t bad = __ballot_sync(0xffffffffu, there && (s_touched[row / 32] >> (row & 31) & 1u) && l < CUDART_INF_F);
+        if (bad) take_in<D, kCodes, BM>(X, v, bad, sight, warp * 32, lane, smem);
+    }
+    if (threadIdx.x / 32 == 0) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(words[0]), "r"(kDirTmem) : "memory");
+    }
+}
+
+// ------------------------------------------------------------------ host side
+
+template <int D, bool kCodes, int kReq>
+cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStream_t s) {
+    static PerDevice<cudaError_t> smem_set;
+    const auto kernel = paged_direct_kernel<D, kCodes, kReq>;
+    constexpr int kSmem = Dir<D, kCodes>::kSmem;
+    cudaError_t e = opt_in_smem(smem_set, (const void*)kernel, kSmem);
+    if (e != cudaSuccess) return e;
+    const int G = c.hq / c.hkv;
+    for (int b0 = 0; b0 < n; b0 += kReq) {
+        const int nb = std::min(n - b0, kReq);
+        DirectLaunch<kReq> X;
+        fill_paged(X.a, c, D, req + b0, nb);
+        // key tiles of each request, and the stretches that make one wave of CTAs of them
+        std::vector<int> tiles(nb);
+        int64_t notes = 0, work = 0;
+        for (int i = 0; i < nb; ++i) {
+            PagedReq& q = X.a.req[i];
+            const int64_t first = c.window ? std::max<int64_t>(0, (int64_t)q.n_keys - q.nq + 1 - c.window) : 0;
+            const int lo = (int)(first / BN), hi = (int)(((int64_t)q.n_keys + BN - 1) / BN);
+            tiles[i] = std::max(1, hi - lo);
+            q.tile0 = 0;
+            q.tiles = (int32_t)(((int64_t)q.nq * G + BM - 1) / BM);
+            q.scratch = (int32_t)(notes - lo);
+            notes += tiles[i];
+            work += (int64_t)tiles[i] * q.tiles * c.hkv;
+        }
+        const int slots = device_sms();
+        int per = (int)std::max<int64_t>(kLeastTiles, (work + slots - 1) / slots);
+        auto splits_of = [&](int i) { return std::min((tiles[i] + per - 1) / per, kMostCuts); };
+        for (int tries = 0; tries < 64; ++tries) {
+            int64_t items = 0;
+            bool any = false;
+            for (int i = 0; i < nb; ++i) {
+                items += (int64_t)splits_of(i) * X.a.req[i].tiles * c.hkv;
+                any = any || splits_of(i) > 1;
+            }
+            if (items <= slots || !any) break;
+            per = std::max(per + 1, per * 33 / 32);
+        }
+        int64_t items = 0, units = 0;
+        int most = 1;
+        auto lay_out = [&](bool cut) {
+            items = units = 0;
+            most = 1;
+            for (int i = 0; i < nb; ++i) {
+                PagedReq& q = X.a.req[i];
+                q.splits = cut ? splits_of(i) : 1;
+                q.item0 = (int32_t)items;
+                q.unit0 = (int32_t)units;
+                if (q.splits > 1) {
+                    units += (int64_t)q.tiles * c.hkv;
+                    most = std::max(most, q.splits);
+                }
+                items += (int64_t)q.tiles * c.hkv * q.splits;
+            }
+        };
+        lay_out(true);
+        // (partials are stored 32 bytes at a time)
+        const size_t odd_bytes = ((size_t)notes * c.hkv * sizeof(uint4) + 255) / 256 * 256;
+        std::optional<Workspace> scratch;
+        size_t o_bytes = units > 0 ? (size_t)items * BM * D * 4 : 0;
+        scratch.emplace(c.ctx, odd_bytes + o_bytes + (units > 0 ? (size_t)items * BM * 4 : 0), 0);
+        if (scratch->err == cudaErrorMemoryAllocation && units > 0) {     // no room for partials: keys are not cut, slower
+            (void)cudaGetLastError();
+            lay_out(false);
+            o_bytes = 0;
+            scratch.emplace(c.ctx, odd_bytes, 0);
+        }
+        if (scratch->err == cudaErrorMemoryAllocation) {                  // nor for a note a key tile
+            (void)cudaGetLastError();
+            e = launch_paged_mma(c, req + b0, nb, D, kCodes, s);
+            if (e != cudaSuccess) return e;
+            continue;
+        }
+        if (scratch->err != cudaSuccess) return scratch->err;
+        char* const base = static_cast<char*>(scratch->p);
+        X.odd = reinterpret_cast<uint4*>(base);
+        X.part_o = reinterpret_cast<float*>(base + odd_bytes);
+        X.part_lse = reinterpret_cast<float*>(base + odd_bytes + o_bytes);
+        const int box_rows = std::min(BN, 1 << c.pg.page_shift), box = kCodes ? D : 64;
+        const auto swizzle = kCodes ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B;
+        if (!encode_page_map(&X.tm_k, c.pg.k, c.pg, c.hkv, D, kCodes, box, box_rows, swizzle) ||
+            !encode_page_map(&X.tm_v, c.pg.v, c.pg, c.hkv, D, kCodes, box, box_rows, swizzle))
+            return cudaErrorInvalidValue;
+        e = launch_overlapped(kernel, (unsigned)items, kDirThreads, kSmem, s, X);
+        if (e == cudaSuccess && units > 0)
+            e = launch_overlapped(paged_join_kernel<D, BM, true, DirectLaunch<kReq>>, (unsigned)(units * (BM / kJoinRows)), kJoinThreads,
+                                  (size_t)most * kJoinRows * 4, s, X);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace
+
+cudaError_t launch_paged_direct(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s) {
+    if (d == 128) return codes ? launch<128, true, kPagedFew>(c, req, n, s) : launch<128, false, kPagedFew>(c, req, n, s);
+    return codes ? launch<64, true, kPagedFew>(c, req, n, s) : launch<64, false, kPagedFew>(c, req, n, s);
+}
+
+}  // namespace c2kv
