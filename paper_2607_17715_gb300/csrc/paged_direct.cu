@@ -27,11 +27,9 @@
 namespace c2kv {
 namespace {
 
-constexpr int kDirGroup = 256, kDirThreads = 2 * kDirGroup + 128;         // (the last warpgroup's first two warps issue)
-// Registers: 96 a thread at launch, of which the last warpgroup gives up what the others take.
-constexpr int kDirRegs = 96, kDirRegsIssue = 64, kDirRegsOthers = 104;
-static_assert(2 * kDirGroup * kDirRegsOthers + 128 * kDirRegsIssue <= kDirThreads * kDirRegs, "register split");
-constexpr uint32_t kDirTmem = 512;       // a group: S (P over the first half of each half of it), O
+constexpr int kDirGroup = 256, kDirThreads = 2 * kDirGroup + 64;          // (and two warps that issue)
+constexpr uint32_t kDirTmem = 512;       // a group: S (P over the first half of each half of it: a thread's own), O
+constexpr bool kLateV = false;
 constexpr int kLeastTiles = 2;           // of a stretch: one a group
 constexpr int kMostCuts = 256;           // stretches of one unit's keys: their weights join in shared memory
 
@@ -53,8 +51,8 @@ struct Dir : TileOf<D> {
     static constexpr int kGroupBytes = 2 * kTile + 2 * kRaw;                  // K, V, and as they come
     static constexpr int kSmall = kQ + 2 * kGroupBytes;    // [group] (codes) scales of K and V, (else) a row's two values
     static constexpr int kBack = kSmall + 2 * 1024;        // powers of two of the queries' rows: a byte each
-    static constexpr int kBars = kBack + BM;               // [group] scores, output, K, V, tiles of K and of V ready, weights, scales
-    static constexpr int kWords = kBars + 2 * 8 * 8;       // tensor memory, abort, [group] K not finite, rows touched (four), [group][2] pages
+    static constexpr int kBars = kBack + BM;               // [group] scores, output, K, V, K's tile ready, -, weights and V's, scales
+    static constexpr int kWords = kBars + 2 * 8 * 8;       // tensor memory, abort, [group] K not finite, rows touched (four), [group][2] pages, units
     static constexpr int kSmem = kWords + 64;
 };
 static_assert(Dir<128, true>::kSmem <= 232448 && Dir<128, false>::kSmem <= 232448, "shared memory of a CTA");
@@ -239,7 +237,7 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
     constexpr int EB = kCodes ? 1 : 2, kBox = kCodes ? D : 64;       // channels of a TMA box
     const PagedAttn<kReq>& P = X.a;
     extern __shared__ __align__(1024) uint8_t smem[];
-    const bool issues = threadIdx.x >= 2 * kDirGroup;        // (its group's ninth warp; the two behind it have nothing to do)
+    const bool issues = threadIdx.x >= 2 * kDirGroup;        // (its group's ninth warp)
     const int g = issues ? threadIdx.x / 32 & 1 : threadIdx.x / kDirGroup, t = threadIdx.x % kDirGroup;
     const int warp = issues ? 8 : t / 32, lane = threadIdx.x % 32;            // of the group
     const uint32_t sQ = smem_u32(smem), sK = sQ + C::kQ + g * C::kGroupBytes, sV = sK + C::kTile;
@@ -249,11 +247,12 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
     float* const two = kCodes ? reinterpret_cast<float*>(smem + C::kQ + g * C::kGroupBytes) : scales;
     int8_t* const s_back = reinterpret_cast<int8_t*>(smem + C::kBack);
     const uint32_t bars = sQ + C::kBars + g * 64, barS = bars, barO = bars + 8, barK = bars + 16, barV = bars + 24;
-    const uint32_t readyK = bars + 32, readyV = bars + 40, readyP = bars + 48, readyC = bars + 56;     // (an arrival a warp)
+    const uint32_t readyK = bars + 32, readyP = bars + 48, readyC = bars + 56;     // (an arrival a warp)
     uint32_t* const words = reinterpret_cast<uint32_t*>(smem + C::kWords);
     volatile uint32_t* const abort = words + 1;
     volatile uint32_t* const s_alone = words + 2 + g;         // the queries' first terms alone: K's tile has values that are not finite
     uint32_t* const s_touched = words + 4;                    // [4]: a bit a row
+    volatile int32_t* const s_units = reinterpret_cast<int32_t*>(words) + 12 + 2 * g;        // (codes) exponents of the tile's scales
     volatile uint32_t* const s_groups = words + 8 + 2 * g;    // [2]: which 16-key groups of a tile lie in pages, every other tile's
     if ((sQ & 1023u) != 0u) {                                 // (tiles lie on their swizzle's pattern: it always does)
         if (threadIdx.x == 0) atomicOr(P.err, 2);
@@ -263,7 +262,7 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
     const int hi = w.R.n_keys, head = w.hk << P.pg.page_shift;        // the head's first row in a page
     const int32_t* const table = P.pg.table + (int64_t)w.R.row * P.pg.table_stride;
     const int box_rows = min(BN, 1 << P.pg.page_shift), boxes = BN / box_rows;
-    const int n = threadIdx.x >= 2 * kDirGroup + 64 ? 0 : (w.n + 1 - g) / 2;         // the group's tiles: g, g + 2, ..
+    const int n = (w.n + 1 - g) / 2;                          // the group's tiles: g, g + 2, ..
     if (threadIdx.x == 0) {
         for (int i = 0; i < 16; ++i) mbar_init(sQ + C::kBars + 8 * i, i % 8 < 4 || i % 8 == 7 ? 1 : 8);
         *abort = 0u;
@@ -345,9 +344,22 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
             if (lane == 0) s_groups[i & 1] = there;
             bring(&X.tm_k, inK, barK, pages);
         };
-        auto put_scales = [&] {
+        auto put_scales = [&] {                               // each side's relative to the power of two above its largest
 #pragma unroll
-            for (int e = 0; e < 8; ++e) scales[e * 32 + lane] = x[e];
+            for (int v = 0; v < 2; ++v) {
+                uint32_t top = 0;
+#pragma unroll
+                for (int e = 4 * v; e < 4 * v + 4; ++e) {
+                    const uint32_t y = __float_as_uint(x[e]) & 0x7fffffffu;
+                    top = max(top, y < 0x7f800000u ? y : 0u);
+                }
+                top = __reduce_max_sync(0xffffffffu, top);
+                const int unit = top == 0u ? 0 : max(-90, min(126, (int)(top >> 23) - 126));
+                const float inv = pow2i(-unit);
+#pragma unroll
+                for (int e = 4 * v; e < 4 * v + 4; ++e) scales[e * 32 + lane] = x[e] * inv;
+                if (lane == 0) s_units[v] = unit;
+            }
             __syncwarp();
             if (lane == 0) mbar_arrive(readyC);
         };
@@ -393,8 +405,6 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
             if (more) bring_k(i + 1, pages1);
             if constexpr (kCodes) {
                 if (more) ask_scales(i + 1, pages1, x);
-                mbar_wait(readyV, uses, P.err, abort);
-                if (more) bring(&X.tm_v, inV, barV, pages1);
             }
             mbar_wait(readyP, uses, P.err, abort);
             if constexpr (!kCodes) mbar_wait(barV, uses, P.err, abort);
@@ -402,12 +412,15 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
                 tc_fence_after();
 #pragma unroll
                 for (int kk = 0; kk < BN / 16; ++kk)
-                    mma_bf16_ts(tmemO, tmem + (uint32_t)kk * 8u, dv + (uint64_t)((kk * 16 * 128) >> 4), idO, kk > 0 || i > 0 ? 1u : 0u);
+                    mma_bf16_ts(tmemO, tmem + (uint32_t)(kk / 4 * 64 + kk % 4 * 8), dv + (uint64_t)((kk * 16 * 128) >> 4), idO, kk > 0 || i > 0 ? 1u : 0u);
                 mma_commit(barO);
             }
             __syncwarp();
             if constexpr (kCodes) {
-                if (more) put_scales();                       // (the weights have taken the ones before)
+                if (more) {
+                    put_scales();                             // (the weights have taken the ones before)
+                    bring(&X.tm_v, inV, barV, pages1);        // (and V has been converted)
+                }
             }
             if (more) scores(i + 1, uses ^ 1u);
             if constexpr (!kCodes) {
@@ -432,7 +445,7 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
             __syncthreads();
             ready = true;
         }
-        const float f = kCodes ? P.scale_log2 * pow2i(s_back[row]) : P.scale_log2;
+        const float row_f = kCodes ? P.scale_log2 * pow2i(s_back[row]) : P.scale_log2;
         for (int i = 0; i < n; ++i, uses ^= 1u) {
             const int key0 = key_of(i);
             if constexpr (kCodes) {
@@ -450,11 +463,12 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
             const Rows rows{s_groups[i & 1], w.k_lo - key0, hi - key0};
             const bool whole_tile = rows.all();
             if constexpr (kCodes) {
-                if (i > 0) mbar_wait(barO, uses ^ 1u, P.err, abort);                 // the products before have read V
-                mbar_wait(barV, uses, P.err, abort);
-                codes_to_f16<D>(inV, sV, t, whole_tile, rows);
-                fence_proxy_async();
-                arrive(readyV);
+                if constexpr (!kLateV) {
+                    if (i > 0) mbar_wait(barO, uses ^ 1u, P.err, abort);             // the products before have read V
+                    mbar_wait(barV, uses, P.err, abort);
+                    codes_to_f16<D>(inV, sV, t, whole_tile, rows);
+                    fence_proxy_async();
+                }
                 mbar_wait(readyC, uses, P.err, abort);
             } else if constexpr (kCare) {
                 const bool odd = group_or(g, tile_odd<D>(sK, t, rows));
@@ -486,58 +500,50 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
             // the softmax of the thread's 64 keys
             mbar_wait(barS, uses, P.err, abort);
             tc_fence_after();
-            uint32_t sv[2][32];
-            tmem_ld32(colS, sv[0]);
-            tmem_ld32(colS + 32, sv[1]);
-            tmem_ld_wait();
-            int v_unit = 0;
-            if constexpr (kCodes) {                           // the power of two above the largest of V's scales
-                const float4 x = reinterpret_cast<const float4*>(scales + BN)[lane];
-                uint32_t top = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t y = __float_as_uint(e == 0 ? x.x : e == 1 ? x.y : e == 2 ? x.z : x.w) & 0x7fffffffu;
-                    top = max(top, y < 0x7f800000u ? y : 0u);
-                }
-                top = __reduce_max_sync(0xffffffffu, top);
-                v_unit = top == 0u ? 0 : max(-90, min(126, (int)(top >> 23) - 126));
-#pragma unroll
-                for (int c = 0; c < 2; ++c)
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
-                        const float4 ks = *reinterpret_cast<const float4*>(scales + half * 64 + c * 32 + e);
-                        float y[4];
-                        fmul2(y[0], y[1], __uint_as_float(sv[c][e]), __uint_as_float(sv[c][e + 1]), f, f);
-                        fmul2(y[2], y[3], __uint_as_float(sv[c][e + 2]), __uint_as_float(sv[c][e + 3]), f, f);
-                        fmul2(y[0], y[1], y[0], y[1], ks.x, ks.y);
-                        fmul2(y[2], y[3], y[2], y[3], ks.z, ks.w);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) sv[c][e + k] = __float_as_uint(y[k]);
-                    }
-            }
+            // (codes) scores in units of 2^[K's exponent], weights of V's
+            // (within fp32's normal range: hidden scores of -inf times zero would be no number)
+            const float f = kCodes ? fminf(fmaxf(row_f * pow2i(s_units[0]), 0x1p-126f), 0x1.fffffep127f) : row_f, ve = kCodes ? (float)s_units[1] : 0.f;
             const bool edge = !whole_tile || !sight.sees_tile(key0);
             uint32_t seen[2] = {0xffffffffu, 0xffffffffu};
             if (edge) {
                 sight.of64(key0 + half * 64, seen[0], seen[1]);
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    seen[c] &= rows.of32(half * 2 + c);
+                for (int c = 0; c < 2; ++c) seen[c] &= rows.of32(half * 2 + c);
+            }
+            // Scores of 32 of the thread's keys.  They are taken twice, for the largest and for the weights: 64 at once do not
+            // fit the registers, and what does not goes through an L1 that shared memory leaves next to nothing of.
+            auto take = [&](int c, uint32_t (&sv)[32]) {
+                tmem_ld32(colS + c * 32, sv);
+                tmem_ld_wait();
+                if constexpr (kCodes) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) {
+                        const float4 ks = *reinterpret_cast<const float4*>(scales + half * 64 + c * 32 + e);
+                        float y[4];
+                        fmul2(y[0], y[1], __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]), ks.x, ks.y);
+                        fmul2(y[2], y[3], __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]), ks.z, ks.w);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) sv[e + k] = __float_as_uint(y[k]);
+                    }
+                }
+                if (edge) {
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
-                        if (!(seen[c] >> e & 1u)) sv[c][e] = __float_as_uint(-CUDART_INF_F);
+                        if (!(seen[c] >> e & 1u)) sv[e] = __float_as_uint(-CUDART_INF_F);
                 }
-            }
+            };
             float m = -CUDART_INF_F;
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
+            for (int c = 0; c < 2; ++c) {
+                uint32_t sv[32];
+                take(c, sv);
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) m = fmax3(m, __uint_as_float(sv[c][e]), __uint_as_float(sv[c][e + 1]));
+                for (int e = 0; e < 32; e += 2) m = fmax3(m, __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
+            }
             two[half * BM + row] = m;
-            tc_fence_before();
-            group_sync(g);                                    // (and every score is in registers: weights may lie over them)
-            tc_fence_after();
+            group_sync(g);
             m = fmaxf(two[row], two[BM + row]);
-            const float most = kCodes ? m + (float)v_unit : m * f;
+            const float most = fmaf(m, f, ve);
             const bool moves = most > ref + kRoom;            // (from -inf: any number)
             if (__any_sync(0xffffffffu, moves)) {
                 float alpha = 1.f;
@@ -560,42 +566,51 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
             }
             auto weigh = [&](auto hides) {
                 float ps[4] = {0.f, 0.f, 0.f, 0.f};
-                const float off = ref == -CUDART_INF_F ? 0.f : -ref;
+                const float off = ve - (ref == -CUDART_INF_F ? 0.f : ref);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {                 // sixteen keys at a time
-                    uint32_t pk[8];
-                    [[maybe_unused]] float4 vs;
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t sv[32];
+                    take(c, sv);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const int e = (c % 2) * 16 + 2 * k;
-                        float a0 = __uint_as_float(sv[c / 2][e]), a1 = __uint_as_float(sv[c / 2][e + 1]);
-                        if constexpr (kCodes) fadd2(a0, a1, off, off);
-                        else ffma2(a0, a1, a0, a1, f, off);
-                        a0 = ex2(a0);
-                        a1 = ex2(a1);
-                        if (k & 1) fadd2(ps[2], ps[3], a0, a1);
-                        else fadd2(ps[0], ps[1], a0, a1);
-                        if constexpr (kCodes) {
-                            if (k % 2 == 0) vs = *reinterpret_cast<const float4*>(scales + BN + half * 64 + (c / 2) * 32 + e);
-                            fmul2(a0, a1, a0, a1, k % 2 ? vs.z : vs.x, k % 2 ? vs.w : vs.y);
-                            if constexpr (decltype(hides)::value) {          // a hidden key's scale may be anything
-                                if (!(seen[c / 2] >> e & 1u)) a0 = 0.f;
-                                if (!(seen[c / 2] >> (e + 1) & 1u)) a1 = 0.f;
+                    for (int q = 0; q < 2; ++q) {             // (over the scores of the same thread that are taken)
+                        uint32_t pk[8];
+                        [[maybe_unused]] float4 vs;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const int e = q * 16 + 2 * k;
+                            float a0 = __uint_as_float(sv[e]), a1 = __uint_as_float(sv[e + 1]);
+                            ffma2(a0, a1, a0, a1, f, off);
+                            a0 = ex2(a0);
+                            a1 = ex2(a1);
+                            if (k & 1) fadd2(ps[2], ps[3], a0, a1);
+                            else fadd2(ps[0], ps[1], a0, a1);
+                            if constexpr (kCodes) {
+                                if (k % 2 == 0) vs = *reinterpret_cast<const float4*>(scales + BN + half * 64 + c * 32 + e);
+                                fmul2(a0, a1, a0, a1, k % 2 ? vs.z : vs.x, k % 2 ? vs.w : vs.y);
+                                if constexpr (decltype(hides)::value) {          // a hidden key's scale may be anything
+                                    if (!(seen[c] >> e & 1u)) a0 = 0.f;
+                                    if (!(seen[c] >> (e + 1) & 1u)) a1 = 0.f;
+                                }
+                                pk[k] = pack_f16(a0, a1);
+                            } else {
+                                pk[k] = pack_bf16(a0, a1);
                             }
-                            pk[k] = pack_f16(a0, a1);
-                        } else {
-                            pk[k] = pack_bf16(a0, a1);
                         }
+                        tmem_st8(colS + c * 16 + q * 8, pk);
                     }
-                    tmem_st8(tmem + lane_addr + (uint32_t)(half * 32 + c * 8), pk);
                 }
-                l += (ps[0] + ps[1]) + (ps[2] + ps[3]);
+                l = fmaf((ps[0] + ps[1]) + (ps[2] + ps[3]), ex2(-ve), l);
             };
             // (edges differ from row to row: the warp's)
             if (kCodes && __any_sync(0xffffffffu, edge)) weigh(std::true_type{});
             else weigh(std::false_type{});
             tmem_st_wait();
             tc_fence_before();
+            if constexpr (kCodes && kLateV) {                 // (the scores are behind the products that read V's tile)
+                mbar_wait(barV, uses, P.err, abort);
+                codes_to_f16<D>(inV, sV, t, whole_tile, rows);
+                fence_proxy_async();
+            }
             arrive(readyP);
         }
         if (n > 0) {
@@ -605,14 +620,12 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
     };
     // (the same barriers of all warps on both ways)
     if (issues) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDirRegsIssue));
         issue(std::false_type{});
         if constexpr (!kCodes)
             if (__syncthreads_or(0)) issue(std::true_type{});
         for (int i = 0; i < 4; ++i) __syncthreads();
         return;
     }
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kDirRegsOthers));
     tiles(std::false_type{});
     if constexpr (!kCodes) {
         // values that are not finite: of a sum, or (where weights of zero met them) of the output
