@@ -3,15 +3,15 @@
 //
 // Key tiles made ahead (paged_expand.cu) pay where many row tiles meet them.  Here a (request, KV head) has one or
 // two, of 128 rows each, and reading the pages bounds the call: TMA brings them into shared memory, and nothing but
-// partials goes back.  8-bit codes become f16 there, as they are; a key's K scale multiplies its scores and its V scale
-// its weights, in fp32 (a scale that is NaN makes NaN of the rows that see it).  16-bit pages are operands as they lie,
+// partials goes back.  8-bit codes become f16 there, relative to a power of two for every
+// 32 keys (a V scale that is NaN makes NaN of the rows that see it, and zero of the row itself).  16-bit pages are operands as they lie,
 // the queries two bf16 terms of them and the weights one, as in paged_mma.cu.
 //
-// A CTA has an SM to itself, in two groups of eight warps that take the tiles of 128 keys in turn, each with its own
-// scores and output in tensor memory: one's products and loads run beside the other's conversions and softmax (a row is
-// two threads' of a group, 64 keys each).  A ninth warp of each group issues its products and copies: where one of the
-// eight did, it waited for the tensor cores' queue, and they for it (7300 clocks a tile).  The groups' results join in
-// shared memory, the stretches' in a kernel of their own.
+// A CTA has an SM to itself, in two groups that take the tiles of 128 keys in turn, each with its own scores and output in
+// tensor memory, and its own warps: four for the softmax (a row a thread), four that convert (8-bit codes) or look after
+// tiles that are not whole, one that issues products and copies.  So a tile's conversions run beside the softmax of the
+// one before, and one group's products beside the other's softmax.  The groups' results join in shared memory, the
+// stretches' in a kernel of their own.
 //
 // Values of V that are not finite (16-bit pages): 0 times one is NaN for rows that do not see it, and a query's second
 // term makes NaN of an infinity of K.  A CTA whose results show either begins again with care: such values become zero in
@@ -27,9 +27,9 @@
 namespace c2kv {
 namespace {
 
-constexpr int kDirGroup = 256, kDirThreads = 2 * kDirGroup + 64;          // (and two warps that issue)
-constexpr uint32_t kDirTmem = 512;       // a group: S (P over the first half of each half of it: a thread's own), O
-constexpr bool kLateV = false;
+constexpr int kDirGroup = 128;           // threads of a group's softmax, and of its conversions
+constexpr int kDirThreads = 4 * kDirGroup + 64;
+constexpr uint32_t kDirTmem = 512;       // a group: S (P over its first half), O
 constexpr int kLeastTiles = 2;           // of a stretch: one a group
 constexpr int kMostCuts = 256;           // stretches of one unit's keys: their weights join in shared memory
 
@@ -49,29 +49,19 @@ struct Dir : TileOf<D> {
     static constexpr int kRaw = kCodes ? BN * D : 0;       // bytes of a tile of codes
     static constexpr int kQ = (kCodes ? 1 : 2) * kTile;
     static constexpr int kGroupBytes = 2 * kTile + 2 * kRaw;                  // K, V, and as they come
-    static constexpr int kSmall = kQ + 2 * kGroupBytes;    // [group] (codes) scales of K and V, (else) a row's two values
+    static constexpr int kSmall = kQ + 2 * kGroupBytes;    // [group] (codes) scales of K and V; the join's sums
     static constexpr int kBack = kSmall + 2 * 1024;        // powers of two of the queries' rows: a byte each
-    static constexpr int kBars = kBack + BM;               // [group] scores, output, K, V, K's tile ready, -, weights and V's, scales
-    static constexpr int kWords = kBars + 2 * 8 * 8;       // tensor memory, abort, [group] K not finite, rows touched (four), [group][2] pages, units
-    static constexpr int kSmem = kWords + 64;
+    static constexpr int kBars = kBack + BM;               // [group] scores, output, K, V, K's and V's tiles ready, weights, scales
+    static constexpr int kWords = kBars + 2 * 8 * 8;       // tensor memory, abort, [group] K not finite, rows touched (four), [group][2] pages, [group][12] units, [group][4] notes
+    static constexpr int kSmem = kWords + 192;
 };
 static_assert(Dir<128, true>::kSmem <= 232448 && Dir<128, false>::kSmem <= 232448, "shared memory of a CTA");
 
-// Two products, rounded as one each.
-__device__ __forceinline__ void fmul2(float& d0, float& d1, float a0, float a1, float b0, float b1) {
-    asm("{\n\t.reg .b64 pa, pb, pd;\n\t"
-        "mov.b64 pa, {%2, %3};\n\t"
-        "mov.b64 pb, {%4, %5};\n\t"
-        "mul.rn.f32x2 pd, pa, pb;\n\t"
-        "mov.b64 {%0, %1}, pd;\n\t}"
-        : "=f"(d0), "=f"(d1)
-        : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
-}
-
-__device__ __forceinline__ void group_sync(int g) { asm volatile("bar.sync %0, 256;" ::"r"(1 + g) : "memory"); }
-__device__ __forceinline__ bool group_or(int g, bool x) {
+// A barrier of a group's conversions, and whether x holds in any thread of them.
+__device__ __forceinline__ void convert_sync(int g) { asm volatile("bar.sync %0, 128;" ::"r"(1 + g) : "memory"); }
+__device__ __forceinline__ bool convert_or(int g, bool x) {
     uint32_t any;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
                  : "=r"(any)
                  : "r"((uint32_t)x), "r"(1 + g)
                  : "memory");
@@ -154,15 +144,21 @@ struct Rows {
     }
 };
 
-// A tile of codes [128][D] as f16 in 64-channel blocks under the 128-byte swizzle, by a group's threads; (not `all`) rows
-// that are not there become zero.
+// A tile of codes [128][D] times their rows' scales (f16, twice in a word) as f16 in 64-channel blocks under the 128-byte
+// swizzle, by a group's threads; (not `all`) rows that are not there become zero.  The scale's rounding and the product's
+// are 2^-12 of a value each; the output's own is 2^-9.  (Scales in fp32 on the scores and the weights instead, whose rows
+// every thread reads from shared memory, took the softmax twice the time: 3400 clocks a tile for 1600.)
 template <int D>
-__device__ __forceinline__ void codes_to_f16(uint32_t raw, uint32_t tile, int t, bool all, const Rows& rows) {
+__device__ __forceinline__ void codes_to_f16(uint32_t raw, uint32_t tile, const uint32_t* scale, int t, bool all, const Rows& rows) {
     constexpr int kChunks = D / 16, kStep = kDirGroup / kChunks, kPasses = BN / kStep;
     const int chunk = t % kChunks, block = chunk / 4, q = chunk % 4 * 2, first = block & 1;
     uint4 w[kPasses];
+    uint32_t f[kPasses];
 #pragma unroll
-    for (int i = 0; i < kPasses; ++i) w[i] = lds128(raw + (t / kChunks + kStep * i) * D + chunk * 16);
+    for (int i = 0; i < kPasses; ++i) {
+        w[i] = lds128(raw + (t / kChunks + kStep * i) * D + chunk * 16);
+        f[i] = scale[t / kChunks + kStep * i];
+    }
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
         const int row = t / kChunks + kStep * i;
@@ -170,9 +166,11 @@ __device__ __forceinline__ void codes_to_f16(uint32_t raw, uint32_t tile, int t,
         const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
         uint32_t y[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e]) : "h"((uint16_t)x[e]));
-            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * e + 1]) : "h"((uint16_t)(x[e] >> 16)));
+        for (int e = 0; e < 8; ++e) {
+            uint32_t h;
+            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)(x[e / 2] >> (16 * (e & 1)))));
+            const __half2 z = __hmul2(*reinterpret_cast<const __half2*>(&h), *reinterpret_cast<const __half2*>(&f[i]));
+            y[e] = *reinterpret_cast<const uint32_t*>(&z);
         }
         const uint32_t at = tile + block * TileOf<D>::kHalf + row * 128;
         // (the blocks' threads begin with different halves, so that a row's eight meet all banks)
@@ -183,15 +181,14 @@ __device__ __forceinline__ void codes_to_f16(uint32_t raw, uint32_t tile, int t,
 }
 
 // (16-bit pages) whether a tile has values that are not finite in the thread's row; and V's tile put right: rows that are
-// not there become zero, with care values that are not finite too, and whether there were any.  Two threads a row.
+// not there become zero, with care values that are not finite too, and whether there were any.  A thread a row.
 template <int D>
 __device__ __forceinline__ bool tile_odd(uint32_t tile, int t, const Rows& rows) {
-    const int row = t / 2;
+    const int row = t;
     bool odd = false;
     if (!rows.has(row)) return false;
 #pragma unroll 4
-    for (int i = 0; i < D / 16; ++i) {
-        const int line = (t & 1) * (D / 16) + i;
+    for (int line = 0; line < D / 8; ++line) {
         const uint4 w = lds128(tile + line / 8 * TileOf<D>::kHalf + row * 128 + line % 8 * 16);
         const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -201,13 +198,12 @@ __device__ __forceinline__ bool tile_odd(uint32_t tile, int t, const Rows& rows)
 }
 template <int D>
 __device__ __forceinline__ bool put_right(uint32_t tile, int t, const Rows& rows, bool care) {
-    const int row = t / 2;
+    const int row = t;
     const bool there = rows.has(row);
     bool odd = false;
     if (there && !care) return false;
 #pragma unroll 1
-    for (int i = 0; i < D / 16; ++i) {
-        const int line = (t & 1) * (D / 16) + i;
+    for (int line = 0; line < D / 8; ++line) {
         const uint32_t at = tile + line / 8 * TileOf<D>::kHalf + row * 128 + line % 8 * 16;
         uint4 w = make_uint4(0u, 0u, 0u, 0u);
         if (there) {
@@ -237,34 +233,32 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
     constexpr int EB = kCodes ? 1 : 2, kBox = kCodes ? D : 64;       // channels of a TMA box
     const PagedAttn<kReq>& P = X.a;
     extern __shared__ __align__(1024) uint8_t smem[];
-    const bool issues = threadIdx.x >= 2 * kDirGroup;        // (its group's ninth warp)
-    const int g = issues ? threadIdx.x / 32 & 1 : threadIdx.x / kDirGroup, t = threadIdx.x % kDirGroup;
-    const int warp = issues ? 8 : t / 32, lane = threadIdx.x % 32;            // of the group
+    enum { kSoftmax, kConvert, kIssue };
+    const int role = threadIdx.x / (2 * kDirGroup), t = threadIdx.x % kDirGroup, lane = threadIdx.x % 32;
+    const int g = role == kIssue ? threadIdx.x / 32 & 1 : threadIdx.x / kDirGroup & 1;
     const uint32_t sQ = smem_u32(smem), sK = sQ + C::kQ + g * C::kGroupBytes, sV = sK + C::kTile;
     const uint32_t inK = kCodes ? sV + C::kTile : sK, inV = kCodes ? inK + C::kRaw : sV;      // where the pages go
-    float* const scales = reinterpret_cast<float*>(smem + C::kSmall) + g * BN * 2;            // (codes) [K, V][key]
-    // a row's two values; with codes over the K tile, which the scores have been formed of by then
-    float* const two = kCodes ? reinterpret_cast<float*>(smem + C::kQ + g * C::kGroupBytes) : scales;
+    uint32_t* const scales = reinterpret_cast<uint32_t*>(smem + C::kSmall) + g * BN * 2;      // (codes) [K, V][key], f16 twice
     int8_t* const s_back = reinterpret_cast<int8_t*>(smem + C::kBack);
     const uint32_t bars = sQ + C::kBars + g * 64, barS = bars, barO = bars + 8, barK = bars + 16, barV = bars + 24;
-    const uint32_t readyK = bars + 32, readyP = bars + 48, readyC = bars + 56;     // (an arrival a warp)
+    const uint32_t readyK = bars + 32, readyV = bars + 40, readyP = bars + 48, readyC = bars + 56;     // (an arrival a warp)
     uint32_t* const words = reinterpret_cast<uint32_t*>(smem + C::kWords);
     volatile uint32_t* const abort = words + 1;
     volatile uint32_t* const s_alone = words + 2 + g;         // the queries' first terms alone: K's tile has values that are not finite
     uint32_t* const s_touched = words + 4;                    // [4]: a bit a row
-    volatile int32_t* const s_units = reinterpret_cast<int32_t*>(words) + 12 + 2 * g;        // (codes) exponents of the tile's scales
     volatile uint32_t* const s_groups = words + 8 + 2 * g;    // [2]: which 16-key groups of a tile lie in pages, every other tile's
+    // (codes) exponents that 32 keys lack: K's of every other tile, V's; and rows of V's tile that are not finite, a bit each
+    volatile int32_t* const s_units = reinterpret_cast<int32_t*>(words) + 12 + 12 * g;
+    volatile uint32_t* const s_note = words + 36 + 4 * g;
     if ((sQ & 1023u) != 0u) {                                 // (tiles lie on their swizzle's pattern: it always does)
         if (threadIdx.x == 0) atomicOr(P.err, 2);
         return;
     }
     const Item w = find_item<true, BM>(P, (int)blockIdx.x);
-    const int hi = w.R.n_keys, head = w.hk << P.pg.page_shift;        // the head's first row in a page
-    const int32_t* const table = P.pg.table + (int64_t)w.R.row * P.pg.table_stride;
-    const int box_rows = min(BN, 1 << P.pg.page_shift), boxes = BN / box_rows;
+    const int hi = w.R.n_keys;
     const int n = (w.n + 1 - g) / 2;                          // the group's tiles: g, g + 2, ..
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 16; ++i) mbar_init(sQ + C::kBars + 8 * i, i % 8 < 4 || i % 8 == 7 ? 1 : 8);
+        for (int i = 0; i < 16; ++i) mbar_init(sQ + C::kBars + 8 * i, i % 8 < 4 ? 1 : 4);
         *abort = 0u;
         for (int i = 0; i < 4; ++i) s_touched[i] = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -276,113 +270,64 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     after_kernels_before();
-    // the page of box `lane` (and, codes, of 16-key group lane % 8) of the group's tile i, -1 for none or without a key that
-    // any query sees
-    auto key_of = [&](int i) { return (w.j0 + 2 * i + g) * BN; };
-    auto page_at = [&](int i, int key) {
-        // (pages that a window has left behind may be gone from the table)
-        if (i >= n || key >= hi || ((key >> P.pg.page_shift) + 1) << P.pg.page_shift <= w.k_lo) return -1;
-        const int page = ld_after(table + (key >> P.pg.page_shift));
-        if (page >= 0 && page < P.pg.n_pages) return page;
-        atomicOr(P.err, 1);
-        return -1;
-    };
-    auto pages_of = [&](int i) { return page_at(i, key_of(i) + (lane & 7) * 16); };
-    // tile of `pages` (of 16-key groups) into shared memory, by a whole warp
-    auto bring = [&](const CUtensorMap* tm, uint32_t to, uint32_t bar, int pages) {
-        const int p = __shfl_sync(0xffffffffu, pages, lane * (box_rows / 16) & 7);
-        const bool mine = lane < boxes && p >= 0;
-        const uint32_t count = __popc(__ballot_sync(0xffffffffu, mine));
-        if (lane == 0) mbar_expect_tx(bar, count * (uint32_t)(box_rows * D * EB));
-        __syncwarp();
-        if (mine) {
-#pragma unroll
-            for (int b = 0; b < D / kBox; ++b)
-                tma_load_4d(to + b * TileOf<D>::kHalf + lane * box_rows * (kBox * EB), tm, b * kBox, 0, w.hk, p, bar);
-        }
-    };
-    // (codes) K's and V's scales of keys 32 e + lane of the group's tile i, by the ninth warp
-    auto ask_scales = [&](int i, int pages, float (&x)[8]) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int key = (e & 3) * 32 + lane, p = __shfl_sync(0xffffffffu, pages, key >> 4), at = key_of(i) + key;
-            const bool ok = p >= 0 && at >= w.k_lo && at < hi;
-            x[e] = 0.f;
-            if (ok) x[e] = ld_after((e < 4 ? P.pg.k_scale : P.pg.v_scale) + (int64_t)p * P.pg.scale_stride + head + (key & ((1 << P.pg.page_shift) - 1)));
-        }
-    };
-    int pages = -1, pages1 = -1;                              // (the ninth warp) of 16-key groups of this tile and the next
     QueryRows<D> rows;
-    if (g == 0 && warp < 4) rows = fetch_queries<D>(P, w, warp, lane, sQ);
+    if (threadIdx.x < BM) rows = fetch_queries<D>(P, w, t / 32, lane, sQ);
     tc_fence_before();
     __syncthreads();                                          // (barriers, tensor memory)
     tc_fence_after();
     const uint32_t tmem = words[0] + (uint32_t)(g * 256), tmemO = tmem + BN;
     // the kernel that joins cut keys may be set up from here on: it waits for this grid to end
     if (threadIdx.x == 0) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-
-    const int G = P.hq / P.hkv, half = warp / 4, row = warp % 4 * 32 + lane;        // (half 2: issues, for no row)
-    const uint32_t lane_addr = (uint32_t)(warp % 4 * 32) << 16;
-    const uint32_t colS = tmem + lane_addr + (uint32_t)(half * 64), colO = tmemO + lane_addr + (uint32_t)(half * (D / 2));
-    const Climb<PagedAttn<kReq>> sight(P, w, (w.row0 + min(row, w.live - 1)) / G);
-    float ref = -CUDART_INF_F, l = 0.f;
-    bool touched = false;                                     // by values that are not finite
-    uint32_t uses = 0;                                        // of the barriers, parity of their next phase: a tile each
-    bool ready = false;                                       // the queries are
-
+    auto key_of = [&](int i) { return (w.j0 + 2 * i + g) * BN; };
+    auto rows_of = [&](int i) { return Rows{s_groups[i & 1], w.k_lo - key_of(i), hi - key_of(i)}; };
     auto arrive = [&](uint32_t bar) {                         // the warp has written what the products read
         __syncwarp();
         if (lane == 0) mbar_arrive(bar);
     };
-    // The ninth warp.
-    auto issue = [&](auto with_care) {
-        [[maybe_unused]] constexpr bool kCare = decltype(with_care)::value;
-        [[maybe_unused]] float x[8];
-        // K of tile i, V of tile i, and what the others need to know of it
-        auto bring_k = [&](int i, int pages) {
+    uint32_t uses = 0;                                        // of the barriers, parity of their next phase: a tile each
+
+    // the page of 16-key group lane % 8 of the group's tile i, -1 for none or without a key that any query sees
+    auto pages_of = [&](int i) {
+        const int key = key_of(i) + (lane & 7) * 16;
+        // (pages that a window has left behind may be gone from the table)
+        if (i >= n || key >= hi || ((key >> P.pg.page_shift) + 1) << P.pg.page_shift <= w.k_lo) return -1;
+        const int page = ld_after(P.pg.table + (int64_t)w.R.row * P.pg.table_stride + (key >> P.pg.page_shift));
+        if (page >= 0 && page < P.pg.n_pages) return page;
+        atomicOr(P.err, 1);
+        return -1;
+    };
+
+    if (role == kIssue) {
+        const int box_rows = min(BN, 1 << P.pg.page_shift), boxes = BN / box_rows;
+        // a tile of `pages` into shared memory
+        auto bring = [&](const CUtensorMap* tm, uint32_t to, uint32_t bar, int pages) {
+            const int p = __shfl_sync(0xffffffffu, pages, lane * (box_rows / 16) & 7);
+            const bool mine = lane < boxes && p >= 0;
+            const uint32_t count = __popc(__ballot_sync(0xffffffffu, mine));
+            if (lane == 0) mbar_expect_tx(bar, count * (uint32_t)(box_rows * D * EB));
+            __syncwarp();
+            if (mine) {
+#pragma unroll
+                for (int b = 0; b < D / kBox; ++b)
+                    tma_load_4d(to + b * TileOf<D>::kHalf + lane * box_rows * (kBox * EB), tm, b * kBox, 0, w.hk, p, bar);
+            }
+        };
+        auto bring_k = [&](int i, int pages) {                // K of tile i, and which rows the others find there
             const uint32_t there = __ballot_sync(0xffffffffu, pages >= 0) & 0xffu;
             if (lane == 0) s_groups[i & 1] = there;
             bring(&X.tm_k, inK, barK, pages);
         };
-        auto put_scales = [&] {                               // each side's relative to the power of two above its largest
-#pragma unroll
-            for (int v = 0; v < 2; ++v) {
-                uint32_t top = 0;
-#pragma unroll
-                for (int e = 4 * v; e < 4 * v + 4; ++e) {
-                    const uint32_t y = __float_as_uint(x[e]) & 0x7fffffffu;
-                    top = max(top, y < 0x7f800000u ? y : 0u);
-                }
-                top = __reduce_max_sync(0xffffffffu, top);
-                const int unit = top == 0u ? 0 : max(-90, min(126, (int)(top >> 23) - 126));
-                const float inv = pow2i(-unit);
-#pragma unroll
-                for (int e = 4 * v; e < 4 * v + 4; ++e) scales[e * 32 + lane] = x[e] * inv;
-                if (lane == 0) s_units[v] = unit;
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(readyC);
-        };
-        pages = pages_of(0);
-        pages1 = pages_of(1);
-        if (n > 0) {
-            bring_k(0, pages);
-            bring(&X.tm_v, inV, barV, pages);
-            if constexpr (kCodes) {
-                ask_scales(0, pages, x);
-                put_scales();
-            }
-        }
-        if (!ready) __syncthreads();
-        ready = true;
         const uint64_t dq = sw128_desc(sQ, 16, 1024), dk = sw128_desc(sK, 16, 1024), dv = sw128_desc(sV, C::kHalf, 1024);
-        auto scores = [&](int i, uint32_t phase) {
-            if constexpr (!kCodes) mbar_wait(barK, phase, P.err, abort);
-            if constexpr (kCodes) mbar_wait(readyK, phase, P.err, abort);
-            else if constexpr (kCare) mbar_wait(readyK, (uint32_t)i & 1u, P.err, abort);      // (this way round alone)
+        auto scores = [&](int i, uint32_t phase, bool care) {
+            if constexpr (kCodes) {
+                mbar_wait(readyK, phase, P.err, abort);
+            } else {
+                mbar_wait(barK, phase, P.err, abort);
+                if (care) mbar_wait(readyK, (uint32_t)i & 1u, P.err, abort);          // (this way round alone)
+            }
             if (lane == 0) {
                 tc_fence_after();
-                const bool alone = kCare && *s_alone != 0u;
+                const bool alone = !kCodes && care && *s_alone != 0u;
 #pragma unroll
                 for (int y = kCodes ? 0 : 1; y >= 0; --y) {
                     if (y == 1 && alone) continue;
@@ -396,154 +341,197 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
             }
             __syncwarp();
         };
-        if (n > 0) scores(0, uses);
-        for (int i = 0; i < n; ++i, uses ^= 1u) {
-            const int pages2 = pages_of(i + 2);
-            const bool more = i + 1 < n;
-            // K's next tile where this one's has been read: by the conversion, or by the products
-            if constexpr (!kCodes) mbar_wait(barS, uses, P.err, abort);
-            if (more) bring_k(i + 1, pages1);
-            if constexpr (kCodes) {
-                if (more) ask_scales(i + 1, pages1, x);
+        auto all = [&](bool care) {
+            int pages = pages_of(0), pages1 = pages_of(1);    // of this tile and the next
+            if (n > 0) {
+                bring_k(0, pages);
+                bring(&X.tm_v, inV, barV, pages);
             }
-            mbar_wait(readyP, uses, P.err, abort);
-            if constexpr (!kCodes) mbar_wait(barV, uses, P.err, abort);
-            if (lane == 0) {
-                tc_fence_after();
+            if (!care) __syncthreads();                       // (the queries)
+            if (n > 0) scores(0, uses, care);
+            for (int i = 0; i < n; ++i, uses ^= 1u) {
+                const int pages2 = pages_of(i + 2);
+                const bool more = i + 1 < n;
+                // a next tile where this one's has been read: by the conversion, or by the products
+                if constexpr (!kCodes) mbar_wait(barS, uses, P.err, abort);
+                if (more) bring_k(i + 1, pages1);
+                mbar_wait(readyV, uses, P.err, abort);
+                if (kCodes && more) bring(&X.tm_v, inV, barV, pages1);
+                mbar_wait(readyP, uses, P.err, abort);
+                if (lane == 0) {
+                    tc_fence_after();
 #pragma unroll
-                for (int kk = 0; kk < BN / 16; ++kk)
-                    mma_bf16_ts(tmemO, tmem + (uint32_t)(kk / 4 * 64 + kk % 4 * 8), dv + (uint64_t)((kk * 16 * 128) >> 4), idO, kk > 0 || i > 0 ? 1u : 0u);
-                mma_commit(barO);
-            }
-            __syncwarp();
-            if constexpr (kCodes) {
-                if (more) {
-                    put_scales();                             // (the weights have taken the ones before)
-                    bring(&X.tm_v, inV, barV, pages1);        // (and V has been converted)
+                    for (int kk = 0; kk < BN / 16; ++kk)
+                        mma_bf16_ts(tmemO, tmem + (uint32_t)kk * 8u, dv + (uint64_t)((kk * 16 * 128) >> 4), idO, kk > 0 || i > 0 ? 1u : 0u);
+                    mma_commit(barO);
                 }
+                __syncwarp();
+                if (more) scores(i + 1, uses ^ 1u, care);
+                if constexpr (!kCodes) {
+                    mbar_wait(barO, uses, P.err, abort);
+                    if (more) bring(&X.tm_v, inV, barV, pages1);
+                }
+                pages = pages1;
+                pages1 = pages2;
             }
-            if (more) scores(i + 1, uses ^ 1u);
-            if constexpr (!kCodes) {
-                mbar_wait(barO, uses, P.err, abort);
-                if (more) bring(&X.tm_v, inV, barV, pages1);
+        };
+        all(false);
+        if constexpr (!kCodes)
+            if (__syncthreads_or(0)) all(true);
+        for (int i = 0; i < 4; ++i) __syncthreads();          // (of the join below)
+        return;
+    }
+    if (role == kConvert) {
+        // (codes) K's and V's scale of key t of tile i
+        [[maybe_unused]] int pages1 = -1;                     // of the next tile
+        [[maybe_unused]] float k_scale = 0.f, v_scale = 0.f;
+        auto ask_scales = [&](int i, int pages) {
+            const int p = __shfl_sync(0xffffffffu, pages, t >> 4), at = key_of(i) + t;
+            const bool ok = p >= 0 && at >= w.k_lo && at < hi;
+            const int64_t from = (int64_t)p * P.pg.scale_stride + (w.hk << P.pg.page_shift) + (t & ((1 << P.pg.page_shift) - 1));
+            k_scale = v_scale = 0.f;
+            if (ok) {
+                k_scale = ld_after(P.pg.k_scale + from);
+                v_scale = ld_after(P.pg.v_scale + from);
             }
-            pages = pages1;
-            pages1 = pages2;
-        }
-    };
-    // The others.
-    auto tiles = [&](auto with_care) {
-        [[maybe_unused]] constexpr bool kCare = decltype(with_care)::value;
+        };
+        // ... relative to a power of two for 32 keys, the largest to [2^6, 2^7): a code's product is below 2^16
+        auto put_scale = [&](float x, uint32_t* to, int least) {
+            const uint32_t y = __float_as_uint(x) & 0x7fffffffu, top = __reduce_max_sync(0xffffffffu, y < 0x7f800000u ? y : 0u);
+            const int unit = top == 0u ? 0 : max(least, min(119, (int)(top >> 23) - 126 - 7));
+            const __half2 h = __float2half2_rn(x * pow2i(-unit));
+            to[t] = *reinterpret_cast<const uint32_t*>(&h);
+            return unit;
+        };
+        auto all = [&](bool care) {
+            if constexpr (kCodes) {
+                ask_scales(0, pages_of(0));
+                pages1 = pages_of(1);
+            }
+            if (!care) __syncthreads();
+            for (int i = 0; i < n; ++i, uses ^= 1u) {
+                if constexpr (kCodes) {
+                    mbar_wait(barK, uses, P.err, abort);
+                    if (i > 0) mbar_wait(barS, uses ^ 1u, P.err, abort);             // the products before have read K's tile, and V's
+                    const bool odd = !(fabsf(v_scale) < CUDART_INF_F);       // (V's row becomes zero, and NaN of the rows that see it)
+                    // (V's from -90 on: the sum of weights takes 2^-unit)
+                    const int k_unit = put_scale(k_scale, scales, -120), v_unit = put_scale(odd ? 0.f : v_scale, scales + BN, -90);
+                    if (lane == 0) s_units[(i & 1) * 4 + t / 32] = k_unit;
+                    convert_sync(g);
+                    ask_scales(i + 1, pages1);
+                    pages1 = pages_of(i + 2);
+                    codes_to_f16<D>(inK, sK, scales, t, true, Rows{});               // (hidden keys' scores are replaced)
+                    fence_proxy_async();
+                    arrive(readyK);
+                    mbar_wait(barV, uses, P.err, abort);
+                    const Rows there = rows_of(i);
+                    if (i > 0) mbar_wait(barO, uses ^ 1u, P.err, abort);
+                    const uint32_t note = __ballot_sync(0xffffffffu, odd);
+                    if (lane == 0) {                          // (the tile before has been taken)
+                        s_units[8 + t / 32] = v_unit;
+                        s_note[t / 32] = note;
+                    }
+                    arrive(readyC);
+                    codes_to_f16<D>(inV, sV, scales + BN, t, there.all(), there);
+                    fence_proxy_async();
+                    convert_sync(g);                          // (the scales have been read)
+                } else {
+                    if (care) {
+                        mbar_wait(barK, uses, P.err, abort);
+                        const bool odd = convert_or(g, tile_odd<D>(sK, t, rows_of(i)));
+                        if (t == 0) *s_alone = odd;
+                        arrive(readyK);
+                    }
+                    mbar_wait(barV, uses, P.err, abort);
+                    const Rows there = rows_of(i);
+                    if (care || !there.all()) {
+                        const uint32_t odd = __ballot_sync(0xffffffffu, put_right<D>(sV, t, there, care));
+                        fence_proxy_async();
+                        if (care && lane == 0) {
+                            s_note[t / 32] = odd;
+                            reinterpret_cast<uint32_t*>(X.odd + (int64_t)(w.R.scratch + w.j0 + 2 * i + g) * P.hkv + w.hk)[t / 32] = odd;
+                        }
+                    }
+                }
+                arrive(readyV);
+            }
+        };
+        all(false);
+        if constexpr (!kCodes)
+            if (__syncthreads_or(0)) all(true);
+        for (int i = 0; i < 4; ++i) __syncthreads();
+        return;
+    }
+
+    const int G = P.hq / P.hkv, row = t;
+    const uint32_t lane_addr = (uint32_t)(t & ~31) << 16;
+    const uint32_t colS = tmem + lane_addr, colO = tmemO + lane_addr;
+    const Climb<PagedAttn<kReq>> sight(P, w, (w.row0 + min(row, w.live - 1)) / G);
+    float ref = -CUDART_INF_F, l = 0.f;
+    bool touched = false;                                     // by values that are not finite
+    auto softmax = [&](bool care) {
         ref = -CUDART_INF_F;
         l = 0.f;
-        if (!ready) {                                         // the first tiles are on their way meanwhile
-            if (g == 0 && warp < 4) {
-                if constexpr (kCodes) turn_queries<D>(P, rows, warp, lane, sQ, s_back);
-                else turn_queries_twice<D>(P, rows, warp, lane, sQ);
+        if (!care) {                                          // the first tiles are on their way meanwhile
+            if (g == 0) {
+                if constexpr (kCodes) turn_queries<D>(P, rows, t / 32, lane, sQ, s_back);
+                else turn_queries_twice<D>(P, rows, t / 32, lane, sQ);
                 fence_proxy_async();
             }
             __syncthreads();
-            ready = true;
         }
         const float row_f = kCodes ? P.scale_log2 * pow2i(s_back[row]) : P.scale_log2;
         for (int i = 0; i < n; ++i, uses ^= 1u) {
             const int key0 = key_of(i);
-            if constexpr (kCodes) {
-                group_sync(g);                                // (`two` has been read: K's tile lies there)
-                mbar_wait(barK, uses, P.err, abort);
-                codes_to_f16<D>(inK, sK, t, true, Rows{});     // (hidden keys' scores are replaced)
-                fence_proxy_async();
-                arrive(readyK);
-            } else if constexpr (kCare) {
-                mbar_wait(barK, uses, P.err, abort);
-            } else {
-                mbar_wait(barS, uses, P.err, abort);
-            }
-            // (written ahead of what has been waited for)
-            const Rows rows{s_groups[i & 1], w.k_lo - key0, hi - key0};
-            const bool whole_tile = rows.all();
-            if constexpr (kCodes) {
-                if constexpr (!kLateV) {
-                    if (i > 0) mbar_wait(barO, uses ^ 1u, P.err, abort);             // the products before have read V
-                    mbar_wait(barV, uses, P.err, abort);
-                    codes_to_f16<D>(inV, sV, t, whole_tile, rows);
-                    fence_proxy_async();
-                }
-                mbar_wait(readyC, uses, P.err, abort);
-            } else if constexpr (kCare) {
-                const bool odd = group_or(g, tile_odd<D>(sK, t, rows));
-                if (t == 0) *s_alone = odd;
-                arrive(readyK);
-            }
-            if (!kCodes && (kCare || !whole_tile)) {
-                mbar_wait(barV, uses, P.err, abort);
-                const bool odd = put_right<D>(sV, t, rows, kCare);
-                fence_proxy_async();
-                if constexpr (kCare) {                        // a row's two threads, then its bit
-                    const uint32_t two_bits = __ballot_sync(0xffffffffu, odd);
-                    if (lane == 0) {
-                        const uint32_t m = two_bits | two_bits >> 1;
-                        uint32_t bits = 0;
-                        for (int k = 0; k < 16; ++k) bits |= (m >> (2 * k) & 1u) << k;
-                        reinterpret_cast<uint16_t*>(two)[warp] = (uint16_t)bits;     // (16 rows a warp; group_or is behind `two`'s readers)
-                    }
-                    group_sync(g);
-                    const uint4 note = *reinterpret_cast<const uint4*>(two);
-                    uint32_t lo, up;                          // (the row's other thread looks at the other half)
-                    sight.of64(key0 + half * 64, lo, up);
-                    touched = touched || ((half ? note.z : note.x) & lo) || ((half ? note.w : note.y) & up);
-                    if (t == 0) X.odd[(int64_t)(w.R.scratch + w.j0 + 2 * i + g) * P.hkv + w.hk] = note;
-                    group_sync(g);                            // (`two` is written again below)
-                }
-            }
-
-            // the softmax of the thread's 64 keys
+            if constexpr (kCodes) mbar_wait(readyC, uses, P.err, abort);
             mbar_wait(barS, uses, P.err, abort);
             tc_fence_after();
-            // (codes) scores in units of 2^[K's exponent], weights of V's
+            const Rows there = rows_of(i);                    // (written ahead of the copies that the scores are behind)
+            // of 32 keys (codes): scores in units of 2^[K's exponent], weights of V's
             // (within fp32's normal range: hidden scores of -inf times zero would be no number)
-            const float f = kCodes ? fminf(fmaxf(row_f * pow2i(s_units[0]), 0x1p-126f), 0x1.fffffep127f) : row_f, ve = kCodes ? (float)s_units[1] : 0.f;
-            const bool edge = !whole_tile || !sight.sees_tile(key0);
-            uint32_t seen[2] = {0xffffffffu, 0xffffffffu};
+            auto factor = [&](int c) { return kCodes ? fminf(fmaxf(row_f * pow2i(s_units[(i & 1) * 4 + c]), 0x1p-126f), 0x1.fffffep127f) : row_f; };
+            auto exponent = [&](int c) { return kCodes ? (float)s_units[8 + c] : 0.f; };
+            const bool edge = !there.all() || !sight.sees_tile(key0);
+            uint32_t seen[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
             if (edge) {
-                sight.of64(key0 + half * 64, seen[0], seen[1]);
+                sight.of64(key0, seen[0], seen[1]);
+                sight.of64(key0 + 64, seen[2], seen[3]);
 #pragma unroll
-                for (int c = 0; c < 2; ++c) seen[c] &= rows.of32(half * 2 + c);
+                for (int c = 0; c < 4; ++c) seen[c] &= there.of32(c);
             }
-            // Scores of 32 of the thread's keys.  They are taken twice, for the largest and for the weights: 64 at once do not
-            // fit the registers, and what does not goes through an L1 that shared memory leaves next to nothing of.
+            if (kCodes ? (s_note[0] | s_note[1] | s_note[2] | s_note[3]) != 0u : care) {       // rows of V that are not finite
+                if (!kCodes) mbar_wait(readyV, uses, P.err, abort);
+                uint32_t of[4];
+                sight.of64(key0, of[0], of[1]);
+                sight.of64(key0 + 64, of[2], of[3]);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) touched = touched || (s_note[c] & of[c]) != 0u;
+            }
+            // Scores of 32 keys.  They are taken twice, for the largest and for the weights: 128 at once do not fit the
+            // registers, and what does not goes through an L1 that shared memory leaves next to nothing of.
             auto take = [&](int c, uint32_t (&sv)[32]) {
                 tmem_ld32(colS + c * 32, sv);
                 tmem_ld_wait();
-                if constexpr (kCodes) {
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
-                        const float4 ks = *reinterpret_cast<const float4*>(scales + half * 64 + c * 32 + e);
-                        float y[4];
-                        fmul2(y[0], y[1], __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]), ks.x, ks.y);
-                        fmul2(y[2], y[3], __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]), ks.z, ks.w);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) sv[e + k] = __float_as_uint(y[k]);
-                    }
-                }
                 if (edge) {
+                    const uint32_t bits = c < 2 ? c == 0 ? seen[0] : seen[1] : c == 2 ? seen[2] : seen[3];
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
-                        if (!(seen[c] >> e & 1u)) sv[e] = __float_as_uint(-CUDART_INF_F);
+                        if (!(bits >> e & 1u)) sv[e] = __float_as_uint(-CUDART_INF_F);
                 }
             };
-            float m = -CUDART_INF_F;
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
+            float most = -CUDART_INF_F;
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
                 uint32_t sv[32];
                 take(c, sv);
+                float m = -CUDART_INF_F, m2 = -CUDART_INF_F;
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) m = fmax3(m, __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
+                for (int e = 0; e < 32; e += 4) {
+                    m = fmax3(m, __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
+                    m2 = fmax3(m2, __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
+                }
+                most = fmaxf(most, fmaf(fmaxf(m, m2), factor(c), exponent(c)));
             }
-            two[half * BM + row] = m;
-            group_sync(g);
-            m = fmaxf(two[row], two[BM + row]);
-            const float most = fmaf(m, f, ve);
             const bool moves = most > ref + kRoom;            // (from -inf: any number)
             if (__any_sync(0xffffffffu, moves)) {
                 float alpha = 1.f;
@@ -554,7 +542,7 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
                 l *= alpha;
                 if (i > 0) {
 #pragma unroll 1
-                    for (int c = 0; c < D / 32; ++c) {
+                    for (int c = 0; c < D / 16; ++c) {
                         uint32_t ov[16];
                         tmem_ld16(colO + c * 16, ov);
                         tmem_ld_wait();
@@ -564,53 +552,31 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
                     }
                 }
             }
-            auto weigh = [&](auto hides) {
+            const float base = ref == -CUDART_INF_F ? 0.f : ref;
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+                uint32_t sv[32];
+                take(c, sv);
+                const float f = factor(c), ve = exponent(c), off = ve - base;
                 float ps[4] = {0.f, 0.f, 0.f, 0.f};
-                const float off = ve - (ref == -CUDART_INF_F ? 0.f : ref);
+                uint32_t pk[16];
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t sv[32];
-                    take(c, sv);
+                for (int e = 0; e < 32; e += 4) {
+                    float a[4];
+                    ffma2(a[0], a[1], __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]), f, off);
+                    ffma2(a[2], a[3], __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]), f, off);
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {             // (over the scores of the same thread that are taken)
-                        uint32_t pk[8];
-                        [[maybe_unused]] float4 vs;
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const int e = q * 16 + 2 * k;
-                            float a0 = __uint_as_float(sv[e]), a1 = __uint_as_float(sv[e + 1]);
-                            ffma2(a0, a1, a0, a1, f, off);
-                            a0 = ex2(a0);
-                            a1 = ex2(a1);
-                            if (k & 1) fadd2(ps[2], ps[3], a0, a1);
-                            else fadd2(ps[0], ps[1], a0, a1);
-                            if constexpr (kCodes) {
-                                if (k % 2 == 0) vs = *reinterpret_cast<const float4*>(scales + BN + half * 64 + c * 32 + e);
-                                fmul2(a0, a1, a0, a1, k % 2 ? vs.z : vs.x, k % 2 ? vs.w : vs.y);
-                                if constexpr (decltype(hides)::value) {          // a hidden key's scale may be anything
-                                    if (!(seen[c] >> e & 1u)) a0 = 0.f;
-                                    if (!(seen[c] >> (e + 1) & 1u)) a1 = 0.f;
-                                }
-                                pk[k] = pack_f16(a0, a1);
-                            } else {
-                                pk[k] = pack_bf16(a0, a1);
-                            }
-                        }
-                        tmem_st8(colS + c * 16 + q * 8, pk);
-                    }
+                    for (int k = 0; k < 4; ++k) a[k] = ex2(a[k]);
+                    fadd2(ps[0], ps[1], a[0], a[1]);
+                    fadd2(ps[2], ps[3], a[2], a[3]);
+                    pk[e / 2] = kCodes ? pack_f16(a[0], a[1]) : pack_bf16(a[0], a[1]);
+                    pk[e / 2 + 1] = kCodes ? pack_f16(a[2], a[3]) : pack_bf16(a[2], a[3]);
                 }
+                tmem_st16(colS + c * 16, pk);                 // (over scores that are taken: the thread's own)
                 l = fmaf((ps[0] + ps[1]) + (ps[2] + ps[3]), ex2(-ve), l);
-            };
-            // (edges differ from row to row: the warp's)
-            if (kCodes && __any_sync(0xffffffffu, edge)) weigh(std::true_type{});
-            else weigh(std::false_type{});
+            }
             tmem_st_wait();
             tc_fence_before();
-            if constexpr (kCodes && kLateV) {                 // (the scores are behind the products that read V's tile)
-                mbar_wait(barV, uses, P.err, abort);
-                codes_to_f16<D>(inV, sV, t, whole_tile, rows);
-                fence_proxy_async();
-            }
             arrive(readyP);
         }
         if (n > 0) {
@@ -618,21 +584,13 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
             tc_fence_after();
         }
     };
-    // (the same barriers of all warps on both ways)
-    if (issues) {
-        issue(std::false_type{});
-        if constexpr (!kCodes)
-            if (__syncthreads_or(0)) issue(std::true_type{});
-        for (int i = 0; i < 4; ++i) __syncthreads();
-        return;
-    }
-    tiles(std::false_type{});
+    softmax(false);
     if constexpr (!kCodes) {
         // values that are not finite: of a sum, or (where weights of zero met them) of the output
         float z = l * 0.f;
         if (n > 0) {
 #pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
+            for (int c = 0; c < D / 16; ++c) {
                 uint32_t ov[16];
                 tmem_ld16(colO + c * 16, ov);
                 tmem_ld_wait();
@@ -643,7 +601,7 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
         tc_fence_before();
         if (__syncthreads_or(z != 0.f)) {
             tc_fence_after();
-            tiles(std::true_type{});
+            softmax(true);
         }
     }
 
@@ -656,46 +614,46 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
 
     // the groups join: the second's output, in units of the common reference, through its tiles, a column a row of them
     float* const joined = reinterpret_cast<float*>(smem + C::kQ + C::kGroupBytes);            // [D][128]
-    float* const of_second = reinterpret_cast<float*>(smem + C::kSmall);                      // [reference, sum, of the first][128]
-    group_sync(g);                                            // (they have been read)
-    two[half * BM + row] = l;
-    group_sync(g);
-    l = two[row] + two[BM + row];
+    float* const of_group = reinterpret_cast<float*>(smem + C::kSmall);                       // [reference, sum, of the first][128]
     tc_fence_before();
     __syncthreads();                                          // (what lay there has been read)
     tc_fence_after();
-    if (half == 0) (of_second + 2 * BM * g)[row] = ref, (of_second + 2 * BM * g)[BM + row] = l;
+    of_group[2 * BM * g + row] = ref;
+    of_group[2 * BM * g + BM + row] = l;
     if (touched) atomicOr(s_touched + row / 32, 1u << (row & 31));
     __syncthreads();
-    const float ref0 = of_second[row], l0 = of_second[BM + row], ref1 = of_second[2 * BM + row], l1 = of_second[3 * BM + row];
+    const float ref0 = of_group[row], l0 = of_group[BM + row], ref1 = of_group[2 * BM + row], l1 = of_group[3 * BM + row];
     const float top = fmaxf(ref0, ref1), base = top == -CUDART_INF_F ? 0.f : top;
     const float a0 = ex2(ref0 - base), a1 = ex2(ref1 - base);
     if (g == 1) {
 #pragma unroll 1
-        for (int c = 0; c < D / 32; ++c) {
+        for (int c = 0; c < D / 16; ++c) {
             uint32_t ov[16];
             if (n > 0) {
                 tmem_ld16(colO + c * 16, ov);
                 tmem_ld_wait();
             }
 #pragma unroll
-            for (int e = 0; e < 16; ++e) joined[(half * (D / 2) + c * 16 + e) * BM + row] = n > 0 ? __uint_as_float(ov[e]) * a1 : 0.f;
+            for (int e = 0; e < 16; ++e) joined[(c * 16 + e) * BM + row] = n > 0 ? __uint_as_float(ov[e]) * a1 : 0.f;
         }
     }
+    tc_fence_before();
     __syncthreads();
+    tc_fence_after();
     l = fmaf(l0, a0, l1 * a1);
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    const bool poisoned = s_touched[row / 32] >> (row & 31) & 1u;            // (codes) by a row of V whose scale is no number
+    const float inv = l == 0.f ? 0.f : kCodes && poisoned ? CUDART_NAN_F : 1.0f / l;
     const float lse2 = l == 0.f ? -CUDART_INF_F : top + log2f(l);
     const bool whole = v.R.splits == 1;
     if (g == 0) {
         const int64_t out_tok = v.R.q0 + tok;
         const int h = v.hk * G + (v.row0 + my) % G;
-        T* const orow = static_cast<T*>(P.out) + (out_tok * P.hq + h) * D + half * (D / 2);
-        float* const prow = X.part_o + ((int64_t)item * BM + row) * D + half * (D / 2);
+        T* const orow = static_cast<T*>(P.out) + (out_tok * P.hq + h) * D;
+        float* const prow = X.part_o + ((int64_t)item * BM + row) * D;
         const bool wide = (reinterpret_cast<uintptr_t>(P.out) & 31u) == 0;
         const float none = there && whole && l == 0.f ? of_no_weight<true>(P, v.R, tok) : 0.f;
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
+#pragma unroll 2
+        for (int c = 0; c < D / 16; ++c) {
             uint32_t ov[16];
             if (n > 0) {
                 tmem_ld16(colO + c * 16, ov);
@@ -703,7 +661,7 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
             }
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const float y = fmaf(n > 0 ? __uint_as_float(ov[e]) : 0.f, a0, joined[(half * (D / 2) + c * 16 + e) * BM + row]);
+                const float y = fmaf(n > 0 ? __uint_as_float(ov[e]) : 0.f, a0, joined[(c * 16 + e) * BM + row]);
                 ov[e] = __float_as_uint(l == 0.f ? none : y * inv);
             }
             if (!there) continue;
@@ -722,16 +680,16 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
                 stg256(prow + c * 16 + 8, ov + 8);
             }
         }
-        if (there && half == 0) {
+        if (there) {
             if (!whole) X.part_lse[(int64_t)item * BM + row] = lse2;
             else if (P.lse) P.lse[(int64_t)h * P.n_tokens + out_tok] = lse2 * 0.69314718055994531f;
         }
     }
     tc_fence_before();
-    __syncthreads();                                          // (a row's other half is written, too)
-    if (!kCodes && g == 0 && half == 0) {
-        const uint32_t bad = __ballot_sync(0xffffffffu, there && (s_touched[row / 32] >> (row & 31) & 1u) && l < CUDART_INF_F);
-        if (bad) take_in<D, kCodes, BM>(X, v, bad, sight, warp * 32, lane, smem);
+    __syncthreads();
+    if (!kCodes && g == 0) {
+        const uint32_t bad = __ballot_sync(0xffffffffu, there && poisoned && l < CUDART_INF_F);
+        if (bad) take_in<D, kCodes, BM>(X, v, bad, sight, row & ~31, lane, smem);
     }
     if (threadIdx.x / 32 == 0) {
         tc_fence_after();
