@@ -117,6 +117,7 @@ struct PagedAttnCall {
     const int32_t* ptr;      // host [batch + 1]
     const int32_t* n_keys;   // host [batch]
     const RopeTurns* rope;
+    int32_t eights;          // most eights of query rows a CTA of paged_mma.cu, 0: as many as it holds
 };
 cudaError_t launch_paged_attn(const PagedAttnCall& c, int dtype, int d, bool codes, cudaStream_t s);
 // fp32 queries of n requests on the CUDA cores (paged_simt.cu).
@@ -129,6 +130,8 @@ cudaError_t launch_paged_mma(const PagedAttnCall& c, const PagedReq* req, int n,
 cudaError_t launch_paged_simt_tree(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
 cudaError_t launch_paged_lane_tree(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
 cudaError_t launch_paged_mma_tree(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);
+// CTAs of that many eights of query rows which an SM holds.
+int paged_mma_tree_ctas(int d, bool codes, int eights);
 
 // bf16 trees of n requests on tcgen05, straight from the pages (paged_direct.cu).
 cudaError_t launch_paged_direct(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s);

@@ -1,5 +1,6 @@
 // Attention of each request's new tokens over its paged cache (c2kv_paged_attend).
 #include "paged.cuh"
+#include "per_device.cuh"
 
 #include <algorithm>
 #include <vector>
@@ -17,8 +18,23 @@ namespace {
 // requests take 8 and 19 % longer than on tcgen05.
 constexpr int kMmaRows = 64;
 
-// The same of trees, and the rows up to which tcgen05 takes them straight from the pages.
-constexpr int kTreeMmaRows = 32, kDirectRows = 512;
+// The same of trees, and the rows up to which tcgen05 takes them straight from the pages instead of making key
+// tiles first.  Measured (us, mma.sync / straight from the pages; one request of 30000 rows, 8 of 4000, 16 of 500): 8-bit
+// pages of 128 channels, 16 rows 32 / 42, 30 / 41, 16 / 18, 32 rows 53 / 42, 44 / 41, 26 / 19; 16-bit ones, 16 rows 39 / 43, 40 / 42,
+// 14 / 18, 32 rows 64 / 43, 66 / 42, 24 / 19; 8-bit ones of 64 channels, 32 rows 32 / 35, 30 / 34, 19 / 15.  24 rows of eight requests
+// of 4000: 35 / 41 from 8-bit pages, 49 / 42 from 16-bit ones.  Straight from the pages / with key tiles: 256 rows 68 / 91, 66 / 89,
+// 40 / 38; 384 rows 87 / 109, 119 / 107, 62 / 56, 12 requests of 3000 rows 105 / 130, 32 of 2000 221 / 263, of up to 2000
+// 117 / 130; 512 rows 120 / 112, 133 / 113, 82 / 59.
+constexpr int tree_mma_rows(int d, bool codes) { return d * (codes ? 1 : 2) == 64 ? 32 : d * (codes ? 1 : 2) == 128 ? 24 : 16; }
+constexpr int kDirectRows = 384;
+
+// ... and trees over few keys, which many rows a CTA would leave SMs idle for: mma.sync takes them eight rows a CTA,
+// or 16, where that is one wave of CTAs that read at most so many values of K, counted for eight rows.  Measured (us, eight /
+// 16 / the routes above; 8-bit pages of 128 channels): one request of 1500 rows, 64 rows of queries 13.1 / 16.4 / 18.6, 128 rows (26
+// million values) 17.4 / 18.4 / 18.8; of 6000, 48 rows (38 million) 19.6 / 20.5 / 28, 64 rows (49) 22.7 / 22.2 / 28; four of 500, 64
+// rows 13.2 / 16.6 / 18; 16-bit pages, 64 rows over 1500 15.5 / 16.9 / 19.3, 48 over 6000 26.8 / 24.6 / 28; 64 channels, 256
+// rows over 1500 20 / 18.4 / 18.
+constexpr int64_t kShortValues[2] = {26000000, 38000000};
 
 // The same of fp32 contexts, and the keys that some request has to see for it: the lanes' kernel reads keys
 // again for every 4 rows, the register-tiled loop works on 16 rows or, below that, leaves most of its lanes
@@ -84,6 +100,21 @@ cudaError_t launch_many(const PagedAttnCall& c, const PagedReq* req, int n, int 
     return cudaSuccess;
 }
 
+// Eights of query rows a CTA for trees that short rows of keys leave SMs free for, 0 for others.
+int short_eights(const PagedAttnCall& c, const std::vector<PagedReq>& req, int d, bool codes) {
+    const int64_t G = c.hq / c.hkv;
+    for (int eights = 1; eights <= 2; ++eights) {
+        int64_t units = 0, values = 0;
+        for (const PagedReq& q : req) {
+            const int64_t keys = c.window ? std::min<int64_t>(q.n_keys, (int64_t)c.window + q.nq) : q.n_keys;
+            units += (q.nq * G + 8 * eights - 1) / (8 * eights) * c.hkv;
+            values += (q.nq * G + 7) / 8 * c.hkv * keys * d;
+        }
+        if (values <= kShortValues[eights - 1] && units <= (int64_t)device_sms() * paged_mma_tree_ctas(d, codes, eights)) return eights;
+    }
+    return 0;
+}
+
 }  // namespace
 
 cudaError_t launch_paged_attn(const PagedAttnCall& c, int dtype, int d, bool codes, cudaStream_t s) {
@@ -109,17 +140,23 @@ cudaError_t launch_paged_attn(const PagedAttnCall& c, int dtype, int d, bool cod
         if (e == cudaSuccess && !few.empty()) e = launch_paged_lane(c, few.data(), (int)few.size(), d, codes, s);
         return e;
     }
-    if (c.parent) {              // trees: those of middling size straight from the pages
+    if (c.parent) {
+        if (const int eights = short_eights(c, req, d, codes)) {
+            PagedAttnCall by_eights = c;
+            by_eights.eights = eights;
+            return launch_paged_mma(by_eights, req.data(), (int)req.size(), d, codes, s);
+        }
+        // those of middling size straight from the pages
         std::vector<PagedReq> middling, rest;
         for (const PagedReq& q : req) {
             const int64_t rows = (int64_t)q.nq * (c.hq / c.hkv);
-            (rows > kTreeMmaRows && rows <= kDirectRows ? middling : rest).push_back(q);
+            (rows > tree_mma_rows(d, codes) && rows <= kDirectRows ? middling : rest).push_back(q);
         }
         if (!middling.empty()) e = launch_paged_direct(c, middling.data(), (int)middling.size(), d, codes, s);
         if (e != cudaSuccess || rest.empty()) return e;
         req.swap(rest);
     }
-    part(c.parent ? kTreeMmaRows : kMmaRows);
+    part(c.parent ? tree_mma_rows(d, codes) : kMmaRows);
     // requests of many rows on tcgen05, those of few on mma.sync
     if (!many.empty()) e = launch_many(c, many.data(), (int)many.size(), d, codes, s);
     if (e == cudaSuccess && !few.empty()) e = launch_paged_mma(c, few.data(), (int)few.size(), d, codes, s);

@@ -11,7 +11,14 @@
 // tensor memory, and its own warps: four for the softmax (a row a thread), four that convert (8-bit codes) or look after
 // tiles that are not whole, one that issues products and copies.  So a tile's conversions run beside the softmax of the
 // one before, and one group's products beside the other's softmax.  The groups' results join in shared memory, the
-// stretches' in a kernel of their own.
+// stretches' in a kernel of their own.  Stretches go out longest first, as long as lets the last SM end first.
+//
+// A tile of 128 keys takes a CTA 1.4 us: tensor cores are busy for 0.8 us of it (16-bit pages, two terms of the queries) or 0.6,
+// shared memory for 0.9 (products of 128 x 128 read both operands from it at its full rate), the exponentials 0.5.  A stretch
+// takes 5 us before its first scores and after its last.  Eight trees of up to 64 nodes over up to 6000 rows of 16-bit pages
+// take 54 us (2.0 TB/s of pages, which two row tiles read), 32 nodes over 120000 rows of 8-bit pages 108 us (2.3).
+// Tried and slower: scores 64 keys at a time in two pieces of tensor memory (62 -> 68 us), the next piece of scores
+// asked for while one is worked on (61 -> 63), all 128 scores of a row held (spills).
 //
 // Values of V that are not finite (16-bit pages): 0 times one is NaN for rows that do not see it, and a query's second
 // term makes NaN of an infinity of K.  A CTA whose results show either begins again with care: such values become zero in
@@ -20,6 +27,7 @@
 #include "paged_tile.cuh"
 
 #include <algorithm>
+#include <array>
 #include <cuda_fp16.h>
 #include <optional>
 #include <vector>
@@ -29,8 +37,11 @@ namespace {
 
 constexpr int kDirGroup = 128;           // threads of a group's softmax, and of its conversions
 constexpr int kDirThreads = 4 * kDirGroup + 64;
+constexpr int kTurned = 16;              // rows of queries that a warp of the softmax turns (32 by half the warps took 4 us)
 constexpr uint32_t kDirTmem = 512;       // a group: S (P over its first half), O
 constexpr int kLeastTiles = 2;           // of a stretch: one a group
+constexpr int kJoinRows = 8;             // rows of a unit that a CTA joins
+constexpr int kItemTiles = 6, kJoinTiles = 3;   // what a stretch takes beside its tiles, and the kernel that joins them, in tiles
 constexpr int kMostCuts = 256;           // stretches of one unit's keys: their weights join in shared memory
 
 template <int kReq>
@@ -73,15 +84,15 @@ template <int D, int kReq>
 __device__ __forceinline__ void turn_queries_twice(const PagedAttn<kReq>& P, const QueryRows<D>& k, int warp, int lane, uint32_t sQ) {
     using C = TileOf<D>;
     constexpr int E = QueryRows<D>::E;
-    const int r0 = warp * 32, c = lane * E, q0 = c >> 3, q1 = (D / 2 + c) >> 3;
+    const int r0 = warp * kTurned, c = lane * E, q0 = c >> 3, q1 = (D / 2 + c) >> 3;
     cp_async_wait<0>();
     __syncwarp();
     float2 cs[E];
     int pos_cs = __shfl_sync(0xffffffffu, k.pos, 0);
 #pragma unroll
     for (int e = 0; e < E; ++e) cs[e] = turn_cs_fast(k.turn[e], pos_cs);
-#pragma unroll 4
-    for (int i = 0; i < 32; ++i) {
+#pragma unroll 8
+    for (int i = 0; i < kTurned; ++i) {
         const uint32_t at = sQ + (r0 + i) * 128 + (c & 7) * 2;
         const uint32_t a0 = at + (q0 >> 3) * C::kHalf + (((q0 & 7) ^ (i & 7)) << 4), a1 = at + (q1 >> 3) * C::kHalf + (((q1 & 7) ^ (i & 7)) << 4);
         uint32_t x0, x1;
@@ -271,7 +282,7 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
     }
     after_kernels_before();
     QueryRows<D> rows;
-    if (threadIdx.x < BM) rows = fetch_queries<D>(P, w, t / 32, lane, sQ);
+    if (role == kSoftmax) rows = fetch_queries<D, kTurned>(P, w, (int)threadIdx.x / 32, lane, sQ);
     tc_fence_before();
     __syncthreads();                                          // (barriers, tensor memory)
     tc_fence_after();
@@ -473,11 +484,9 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
         ref = -CUDART_INF_F;
         l = 0.f;
         if (!care) {                                          // the first tiles are on their way meanwhile
-            if (g == 0) {
-                if constexpr (kCodes) turn_queries<D>(P, rows, t / 32, lane, sQ, s_back);
-                else turn_queries_twice<D>(P, rows, t / 32, lane, sQ);
-                fence_proxy_async();
-            }
+            if constexpr (kCodes) turn_queries<D, kTurned>(P, rows, (int)threadIdx.x / 32, lane, sQ, s_back);
+            else turn_queries_twice<D>(P, rows, (int)threadIdx.x / 32, lane, sQ);
+            fence_proxy_async();
             __syncthreads();
         }
         const float row_f = kCodes ? P.scale_log2 * pow2i(s_back[row]) : P.scale_log2;
@@ -711,9 +720,10 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
         const int nb = std::min(n - b0, kReq);
         DirectLaunch<kReq> X;
         fill_paged(X.a, c, D, req + b0, nb);
-        // key tiles of each request, and the stretches that make one wave of CTAs of them
-        std::vector<int> tiles(nb);
+        // key tiles of each request, and the stretches of them that are done first
+        std::array<int, kReq> tiles{};
         int64_t notes = 0, work = 0;
+        int longest = 0;
         for (int i = 0; i < nb; ++i) {
             PagedReq& q = X.a.req[i];
             const int64_t first = c.window ? std::max<int64_t>(0, (int64_t)q.n_keys - q.nq + 1 - c.window) : 0;
@@ -724,19 +734,54 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
             q.scratch = (int32_t)(notes - lo);
             notes += tiles[i];
             work += (int64_t)tiles[i] * q.tiles * c.hkv;
+            longest = std::max(longest, tiles[i]);
         }
         const int slots = device_sms();
-        int per = (int)std::max<int64_t>(kLeastTiles, (work + slots - 1) / slots);
-        auto splits_of = [&](int i) { return std::min((tiles[i] + per - 1) / per, kMostCuts); };
-        for (int tries = 0; tries < 64; ++tries) {
-            int64_t items = 0;
-            bool any = false;
-            for (int i = 0; i < nb; ++i) {
-                items += (int64_t)splits_of(i) * X.a.req[i].tiles * c.hkv;
-                any = any || splits_of(i) > 1;
+        auto splits_at = [&](int i, int per) { return std::min((tiles[i] + per - 1) / per, kMostCuts); };
+        auto length_at = [&](int i, int per) { return (tiles[i] + splits_at(i, per) - 1) / splits_at(i, per); };
+        std::array<int, kReq> order{};
+        auto sort_at = [&](int per) {
+            for (int i = 0; i < nb; ++i) order[i] = i;
+            std::stable_sort(order.begin(), order.begin() + nb, [&](int x, int y) { return length_at(x, per) > length_at(y, per); });
+        };
+        // the tiles that the last SM has done when stretches of `per` go out, longest first, to SMs as these get free
+        auto end_at = [&](int per) {
+            struct Free {
+                int64_t at, sms;
+            };
+            std::vector<Free> free{{0, slots}};               // (the last is the first to be free)
+            bool cut = false;
+            sort_at(per);
+            for (int k = 0; k < nb; ++k) {
+                const int i = order[k], s = splits_at(i, per);
+                cut = cut || s > 1;
+                for (int64_t n = (int64_t)s * X.a.req[i].tiles * c.hkv; n > 0;) {
+                    const Free f = free.back();
+                    const int64_t m = std::min(n, f.sms);
+                    free.back().sms -= m;
+                    if (free.back().sms == 0) free.pop_back();
+                    const Free then{f.at + kItemTiles + length_at(i, per), m};
+                    free.insert(std::find_if(free.begin(), free.end(), [&](const Free& x) { return x.at <= then.at; }), then);
+                    n -= m;
+                }
             }
-            if (items <= slots || !any) break;
-            per = std::max(per + 1, per * 33 / 32);
+            return free.front().at + (cut ? kJoinTiles : 0);
+        };
+        int per = longest;
+        int64_t end = end_at(per);
+        for (int p = (int)std::max<int64_t>(kLeastTiles, work / slots / 3); p < longest; p = std::max(p + 1, p * 6 / 5)) {
+            const int64_t e = end_at(p);
+            if (e < end) end = e, per = p;
+        }
+        auto splits_of = [&](int i) { return splits_at(i, per); };
+        sort_at(per);
+        {
+            const std::array<int, kReq> was = tiles;
+            std::vector<PagedReq> reqs(X.a.req, X.a.req + nb);
+            for (int k = 0; k < nb; ++k) {
+                tiles[k] = was[order[k]];
+                X.a.req[k] = reqs[order[k]];
+            }
         }
         int64_t items = 0, units = 0;
         int most = 1;
@@ -785,7 +830,7 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
             return cudaErrorInvalidValue;
         e = launch_overlapped(kernel, (unsigned)items, kDirThreads, kSmem, s, X);
         if (e == cudaSuccess && units > 0)
-            e = launch_overlapped(paged_join_kernel<D, BM, true, DirectLaunch<kReq>>, (unsigned)(units * (BM / kJoinRows)), kJoinThreads,
+            e = launch_overlapped(paged_join_kernel<D, BM, kJoinRows, true, DirectLaunch<kReq>>, (unsigned)(units * (BM / kJoinRows)), kJoinThreads,
                                   (size_t)most * kJoinRows * 4, s, X);
         if (e != cudaSuccess) return e;
     }

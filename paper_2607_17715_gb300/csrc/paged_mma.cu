@@ -1017,7 +1017,8 @@ template <int D, bool kCodes, bool kTree>
 cudaError_t by_rows(const PagedAttnCall& c, const PagedReq* req, int n, cudaStream_t s) {
     int rows = 1;
     for (int i = 0; i < n; ++i) rows = std::max(rows, req[i].nq * (c.hq / c.hkv));
-    const int eights = (rows + 7) / 8, tiles = (eights + kMostEights - 1) / kMostEights, nt = (eights + tiles - 1) / tiles;
+    const int hold = c.eights ? c.eights : kMostEights;
+    const int eights = (rows + 7) / 8, tiles = (eights + hold - 1) / hold, nt = (eights + tiles - 1) / tiles;
     // (few requests have trees as small as this: their launches take the small block whatever their number)
     const bool small = kTree || n <= kPagedFew;
     constexpr int kLarge = kTree ? kPagedFew : kPagedMany;
@@ -1056,6 +1057,16 @@ cudaError_t launch_paged_mma(const PagedAttnCall& c, const PagedReq* req, int n,
 
 cudaError_t launch_paged_mma_tree(const PagedAttnCall& c, const PagedReq* req, int n, int d, bool codes, cudaStream_t s) {
     return by_kind<true>(c, req, n, d, codes, s);
+}
+
+template <int D, bool kCodes>
+int ctas_of(int eights) {
+    return eights == 1 ? Lay<D, kCodes, 1>::kCtas : eights == 2 ? Lay<D, kCodes, 2>::kCtas : Lay<D, kCodes, kMostEights>::kCtas;
+}
+
+int paged_mma_tree_ctas(int d, bool codes, int eights) {
+    if (d == 128) return codes ? ctas_of<128, true>(eights) : ctas_of<128, false>(eights);
+    return codes ? ctas_of<64, true>(eights) : ctas_of<64, false>(eights);
 }
 
 #endif

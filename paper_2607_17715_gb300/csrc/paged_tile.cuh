@@ -90,12 +90,12 @@ struct QueryRows {
     int pos;                                             // of row `lane`
 };
 
-template <int D, int kReq>
+template <int D, int kRows = 32, int kReq>
 __device__ __forceinline__ QueryRows<D> fetch_queries(const PagedAttn<kReq>& P, const Item& w, int warp, int lane, uint32_t sQ) {
     using T = __nv_bfloat16;
     using C = TileOf<D>;
     const int G = P.hq / P.hkv;
-    const int r0 = warp * 32, n = max(0, min(32, w.live - r0));
+    const int r0 = warp * kRows, n = max(0, min(kRows, w.live - r0));
     const uint32_t tile = sQ + (r0 / BM) * C::kTile + (r0 % BM) * 128;
     // lane i knows where row i lies; a copy takes whole rows, 16 bytes a lane
     const int row = w.row0 + r0 + min(lane, max(0, n - 1)), tok = row / G;
@@ -104,7 +104,7 @@ __device__ __forceinline__ QueryRows<D> fetch_queries(const PagedAttn<kReq>& P, 
     const int q = lane % kChunks;
     const T* const base = static_cast<const T*>(P.q) + q * 8;
 #pragma unroll
-    for (int i0 = 0; i0 < 32; i0 += kStep) {
+    for (int i0 = 0; i0 < kRows; i0 += kStep) {
         const int i = i0 + lane / kChunks;
         const uint32_t to = tile + (uint32_t)((q >> 3) * C::kHalf + i * 128 + (((q & 7) ^ (i & 7)) << 4));
         cp_async16_or_zero(to, base + __shfl_sync(0xffffffffu, at, i), i < n);   // zero past the rows: a number
@@ -122,11 +122,11 @@ __device__ __forceinline__ QueryRows<D> fetch_queries(const PagedAttn<kReq>& P, 
     return k;
 }
 
-template <int D, int kReq>
+template <int D, int kRows = 32, int kReq>
 __device__ __forceinline__ void turn_queries(const PagedAttn<kReq>& P, const QueryRows<D>& k, int warp, int lane, uint32_t sQ, int8_t* s_back) {
     using C = TileOf<D>;
     constexpr int E = QueryRows<D>::E, kBatch = 8;       // rows in flight
-    const int r0 = warp * 32;
+    const int r0 = warp * kRows;
     const int c = lane * E, q0 = c >> 3, q1 = (D / 2 + c) >> 3;
     const uint32_t tile = sQ + (r0 / BM) * C::kTile + (r0 % BM) * 128;
     float2 cs[E];
@@ -136,7 +136,7 @@ __device__ __forceinline__ void turn_queries(const PagedAttn<kReq>& P, const Que
     cp_async_wait<0>();
     __syncwarp();
 #pragma unroll 1
-    for (int i0 = 0; i0 < 32; i0 += kBatch) {
+    for (int i0 = 0; i0 < kRows; i0 += kBatch) {
         uint32_t x0[kBatch], x1[kBatch];
         const uint32_t a0 = (c & 7) * 2 + (q0 >> 3) * C::kHalf + tile + i0 * 128, a1 = (c & 7) * 2 + (q1 >> 3) * C::kHalf + tile + i0 * 128;
 #pragma unroll
@@ -347,12 +347,14 @@ __device__ __forceinline__ void take_in(const Launch& X, const Item& w, uint32_t
     }
 }
 
-// The stretches of cut keys joined: 32 rows of a unit a CTA, eight rows a thread on their way at once.
+// The stretches of cut keys joined: kJoinRows rows of a unit a CTA, eight loads a thread on their way at once,
+// of several stretches where a thread has less than eight rows (one request of 8 KV heads has few units: 64 rows over 30000
+// took 44 us with 8 rows a CTA, 54 with 32, which are 32 CTAs of eight rows a thread).
 // (Joined by the last stretch of a unit instead, 19 partials of 128 KB came through one SM: 72 us for 64
 // tokens over 30000 rows, where this takes 4 of them.)
-constexpr int kJoinThreads = 128, kJoinRows = 32;
+constexpr int kJoinThreads = 128;
 
-template <int D, int kUnit, bool kTree, class Launch>
+template <int D, int kUnit, int kJoinRows, bool kTree, class Launch>
 __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_constant__ Launch X) {
     const auto& P = X.a;
     extern __shared__ float weight[];                            // [stretch][row]
@@ -367,13 +369,13 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
     if (live <= 0) return;
     // items of the unit's stretch k: see find_item
     const int64_t item0 = R.item0 + ((int64_t)(R.tile0 + R.tiles - 1 - pr) * S) * P.hkv + hk;
+    for (int i = threadIdx.x; i < S * kJoinRows; i += kJoinThreads) {
+        if (i % kJoinRows < live) weight[i] = ld_after_l2(X.part_lse + (item0 + (int64_t)(i / kJoinRows) * P.hkv) * kUnit + first + i % kJoinRows);
+    }
+    __syncthreads();
     for (int row = threadIdx.x; row < live; row += kJoinThreads) {
         float top = -CUDART_INF_F, sum = 0.f;
-        for (int k = 0; k < S; ++k) {
-            const float e = ld_after_l2(X.part_lse + (item0 + (int64_t)k * P.hkv) * kUnit + first + row);
-            weight[k * kJoinRows + row] = e;
-            top = fmaxf(top, e);
-        }
+        for (int k = 0; k < S; ++k) top = fmaxf(top, weight[k * kJoinRows + row]);
         const float base = top == -CUDART_INF_F ? 0.f : top;
         for (int k = 0; k < S; ++k) sum += ex2(weight[k * kJoinRows + row] - base);
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -385,23 +387,31 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
         }
     }
     __syncthreads();
-    constexpr int kLines = D / 4, kStep = kJoinThreads / kLines, kRows = kJoinRows / kStep;
+    constexpr int kLines = D / 4, kStep = kJoinThreads / kLines, kRows = kJoinRows / kStep, kBatch = 8 / kRows;
+    static_assert(kRows >= 1 && kRows * kBatch == 8, "eight loads on their way at once");
     const int f = threadIdx.x % kLines, row0 = threadIdx.x / kLines;
     float4 o[kRows];
 #pragma unroll
     for (int i = 0; i < kRows; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k = 0; k < S; ++k) {
-        const float* const from = X.part_o + ((item0 + (int64_t)k * P.hkv) * kUnit + first) * D + 4 * f;
-        float4 y[kRows];
+    for (int k0 = 0; k0 < S; k0 += kBatch) {
+        float4 y[kBatch][kRows];
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) y[i] = ld_after_l2(reinterpret_cast<const float4*>(from + (int64_t)min(row0 + i * kStep, live - 1) * D));
+        for (int b = 0; b < kBatch; ++b) {
+            const float* const from = X.part_o + ((item0 + (int64_t)min(k0 + b, S - 1) * P.hkv) * kUnit + first) * D + 4 * f;
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const float a = weight[k * kJoinRows + min(row0 + i * kStep, live - 1)];
-            o[i].x = fmaf(y[i].x, a, o[i].x);
-            o[i].y = fmaf(y[i].y, a, o[i].y);
-            o[i].z = fmaf(y[i].z, a, o[i].z);
-            o[i].w = fmaf(y[i].w, a, o[i].w);
+            for (int i = 0; i < kRows; ++i) y[b][i] = ld_after_l2(reinterpret_cast<const float4*>(from + (int64_t)min(row0 + i * kStep, live - 1) * D));
+        }
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            if (k0 + b >= S) break;
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                const float a = weight[(k0 + b) * kJoinRows + min(row0 + i * kStep, live - 1)];
+                o[i].x = fmaf(y[b][i].x, a, o[i].x);
+                o[i].y = fmaf(y[b][i].y, a, o[i].y);
+                o[i].z = fmaf(y[b][i].z, a, o[i].z);
+                o[i].w = fmaf(y[b][i].w, a, o[i].w);
+            }
         }
     }
 #pragma unroll
