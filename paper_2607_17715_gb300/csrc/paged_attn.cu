@@ -47,6 +47,16 @@ constexpr int64_t kShortValues[2] = {26000000, 38000000};
 constexpr int lane_rows(int d) { return d == 128 ? 16 : 4; }
 constexpr int kLaneKeys = 256;
 
+// Trees whose (four rows, KV head, key)s are no more than this go to the lanes' kernel, whatever their rows: a CTA a stretch for
+// every four rows fills the SMs where tiles leave most of them without one.  Measured (us, lanes / tiles): 16 / 4 heads of 64
+// channels, one request of 700 keys, 104 rows (75 thousand) 18.7 / 20.7, 256 rows (196) 34 / 27, one of 3000, 64 rows (193) 31 / 37,
+// three of 700, 64 rows (137) 25 / 27, eight of 1500, 16 rows (193) 31 / 35, 32 rows (386) 61 / 40; 32 / 8 heads of 128, one of 700,
+// 64 rows (92) 25 / 37, 256 rows (391) 78 / 61, three of 700, 32 rows (136) 40 / 50, 64 rows (275) 76 / 56, one of 3000, 32 rows (193) 42 / 70.
+constexpr int64_t kLaneTrees = 190000;
+
+// The keys that any of a request's queries sees, at most.
+int64_t keys_of(const PagedAttnCall& c, const PagedReq& q) { return c.window ? std::min<int64_t>(q.n_keys, (int64_t)c.window + q.nq) : q.n_keys; }
+
 // Requests of many rows on tcgen05: what they see of their pages becomes key tiles first, in scratch that
 // the stream hands back; requests go in groups so that the scratch stays small beside the cache.
 constexpr int64_t kTileBytes = (int64_t)512 << 20;
@@ -106,9 +116,8 @@ int short_eights(const PagedAttnCall& c, const std::vector<PagedReq>& req, int d
     for (int eights = 1; eights <= 2; ++eights) {
         int64_t units = 0, values = 0;
         for (const PagedReq& q : req) {
-            const int64_t keys = c.window ? std::min<int64_t>(q.n_keys, (int64_t)c.window + q.nq) : q.n_keys;
             units += (q.nq * G + 8 * eights - 1) / (8 * eights) * c.hkv;
-            values += (q.nq * G + 7) / 8 * c.hkv * keys * d;
+            values += (q.nq * G + 7) / 8 * c.hkv * keys_of(c, q) * d;
         }
         if (values <= kShortValues[eights - 1] && units <= (int64_t)device_sms() * paged_mma_tree_ctas(d, codes, eights)) return eights;
     }
@@ -128,6 +137,9 @@ cudaError_t launch_paged_attn(const PagedAttnCall& c, int dtype, int d, bool cod
     };
     cudaError_t e = cudaSuccess;
     if (dtype == kDtypeF32) {    // CUDA cores: a register-tiled loop, or lanes that share a key
+        int64_t met = 0;
+        for (const PagedReq& q : req) met += ((int64_t)q.nq * (c.hq / c.hkv) + 3) / 4 * c.hkv * keys_of(c, q);
+        if (c.parent && met <= kLaneTrees) return launch_paged_lane(c, req.data(), (int)req.size(), d, codes, s);
         part(lane_rows(d));
         const bool seen = std::any_of(few.begin(), few.end(), [&](const PagedReq& q) {
             return q.n_keys > kLaneKeys && (!c.window || (int64_t)c.window + q.nq > kLaneKeys);

@@ -25,12 +25,9 @@ _beside = False
 
 @pytest.fixture(autouse=True, params=["alone", "beside_others"])
 def _work_beside(request):
-    """Calls of little work go another way than those of much: each test runs as it is, and (bf16) with a large tree
-    as one more request, of more rows and keys than the first way takes."""
+    """Calls of little work go another way than those of much: each test runs as it is, and with a large tree as one
+    more request, of more rows and keys than the first way takes."""
     global _beside
-    shape = getattr(request.node, "callspec").params.get("shape", ("bf16",))
-    if request.param != "alone" and shape[0] == "f32":
-        pytest.skip("fp32 contexts have one way")
     _beside = request.param != "alone"
     yield
     _beside = False
