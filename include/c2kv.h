@@ -574,7 +574,7 @@ c2kv_status c2kv_verify_drafts(c2kv_ctx* ctx, int32_t batch, const int32_t* draf
  *   n_accepted   : device int32 [B]: drafts kept (the root is not one).
  *   path         : device int32 [T]: request r's nodes from tree_ptr[r] on, 0 and those kept, then -1.
  *   next_token   : device int32 [B]; -1 where the last row has no weight.
- * Not recorded by the trace.  Errors: ERR_ARG, ERR_UNSUPPORTED (more than 512 nodes), ERR_NOMEM, ERR_CUDA.
+ * Outputs must not lie over inputs.  Not recorded by the trace.  Errors: ERR_ARG, ERR_UNSUPPORTED (more than 512 nodes), ERR_NOMEM, ERR_CUDA.
  */
 c2kv_status c2kv_verify_tree(c2kv_ctx* ctx, int32_t batch, const int32_t* tree_ptr, int32_t vocab, const int32_t* tokens,
                              const int32_t* parent, const float* p, int64_t p_stride, const float* u, int32_t* n_accepted, int32_t* path,

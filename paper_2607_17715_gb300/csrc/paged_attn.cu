@@ -116,6 +116,7 @@ int short_eights(const PagedAttnCall& c, const std::vector<PagedReq>& req, int d
     for (int eights = 1; eights <= 2; ++eights) {
         int64_t units = 0, values = 0;
         for (const PagedReq& q : req) {
+            if (values > kShortValues[1]) return 0;
             units += (q.nq * G + 8 * eights - 1) / (8 * eights) * c.hkv;
             values += (q.nq * G + 7) / 8 * c.hkv * keys_of(c, q) * d;
         }
@@ -138,7 +139,8 @@ cudaError_t launch_paged_attn(const PagedAttnCall& c, int dtype, int d, bool cod
     cudaError_t e = cudaSuccess;
     if (dtype == kDtypeF32) {    // CUDA cores: a register-tiled loop, or lanes that share a key
         int64_t met = 0;
-        for (const PagedReq& q : req) met += ((int64_t)q.nq * (c.hq / c.hkv) + 3) / 4 * c.hkv * keys_of(c, q);
+        for (const PagedReq& q : req)
+            if (met <= kLaneTrees) met += ((int64_t)q.nq * (c.hq / c.hkv) + 3) / 4 * c.hkv * keys_of(c, q);
         if (c.parent && met <= kLaneTrees) return launch_paged_lane(c, req.data(), (int)req.size(), d, codes, s);
         part(lane_rows(d));
         const bool seen = std::any_of(few.begin(), few.end(), [&](const PagedReq& q) {
