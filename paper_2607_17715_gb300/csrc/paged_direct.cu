@@ -16,9 +16,10 @@
 // A tile of 128 keys takes a CTA 1.4 us: tensor cores are busy for 0.8 us of it (16-bit pages, two terms of the queries) or 0.6,
 // shared memory for 0.9 (products of 128 x 128 read both operands from it at its full rate), the exponentials 0.5.  A stretch
 // takes 5 us before its first scores and after its last.  Eight trees of up to 64 nodes over up to 6000 rows of 16-bit pages
-// take 54 us (2.0 TB/s of pages, which two row tiles read), 32 nodes over 120000 rows of 8-bit pages 108 us (2.3).
+// take 52 us (2.1 TB/s of pages, which two row tiles read), 32 nodes over 120000 rows of 8-bit pages 103 us (2.5).
 // Tried and slower: scores 64 keys at a time in two pieces of tensor memory (62 -> 68 us), the next piece of scores
-// asked for while one is worked on (61 -> 63), all 128 scores of a row held (spills).
+// asked for while one is worked on (61 -> 63), all 128 scores of a row held (spills); the largest of a tile first, then its weights
+// (52 -> 54, 103 -> 107).
 //
 // Values of V that are not finite (16-bit pages): 0 times one is NaN for rows that do not see it, and a query's second
 // term makes NaN of an infinity of K.  A CTA whose results show either begins again with care: such values become zero in
@@ -480,6 +481,35 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
     const Climb<PagedAttn<kReq>> sight(P, w, (w.row0 + min(row, w.live - 1)) / G);
     float ref = -CUDART_INF_F, l = 0.f;
     bool touched = false;                                     // by values that are not finite
+    // (an output of products that came before these scores, and are done)
+    auto scale_output = [&](float alpha) {
+#pragma unroll 1
+        for (int c = 0; c < D / 16; ++c) {
+            uint32_t ov[16];
+            tmem_ld16(colO + c * 16, ov);
+            tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * alpha);
+            tmem_st16(colO + c * 16, ov);
+        }
+    };
+    // weights of the first n times 32 keys, by a power of two
+    auto scale_weights = [&](int n, float alpha) {
+        tmem_st_wait();
+#pragma unroll 1
+        for (int c = 0; c < n; ++c) {
+            uint32_t pv[16];
+            tmem_ld16(colS + c * 16, pv);
+            tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float2 w = kCodes ? __half22float2(*reinterpret_cast<const __half2*>(&pv[e]))
+                                        : make_float2(__uint_as_float(pv[e] << 16), __uint_as_float(pv[e] & 0xffff0000u));
+                pv[e] = kCodes ? pack_f16(w.x * alpha, w.y * alpha) : pack_bf16(w.x * alpha, w.y * alpha);
+            }
+            tmem_st16(colS + c * 16, pv);
+        }
+    };
     auto softmax = [&](bool care) {
         ref = -CUDART_INF_F;
         l = 0.f;
@@ -516,9 +546,12 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
 #pragma unroll
                 for (int c = 0; c < 4; ++c) touched = touched || (s_note[c] & of[c]) != 0u;
             }
-            // Scores of 32 keys.  They are taken twice, for the largest and for the weights: 128 at once do not fit the
-            // registers, and what does not goes through an L1 that shared memory leaves next to nothing of.
-            auto take = [&](int c, uint32_t (&sv)[32]) {
+            // 32 keys at a time: 128 scores do not fit the registers, and what does not goes through an L1 that shared memory
+            // leaves next to nothing of.  The reference is a whole number: where a later piece moves it, weights that are written
+            // already take the difference in their exponents.
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+                uint32_t sv[32];
                 tmem_ld32(colS + c * 32, sv);
                 tmem_ld_wait();
                 if (edge) {
@@ -527,46 +560,27 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
                     for (int e = 0; e < 32; ++e)
                         if (!(bits >> e & 1u)) sv[e] = __float_as_uint(-CUDART_INF_F);
                 }
-            };
-            float most = -CUDART_INF_F;
-#pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-                uint32_t sv[32];
-                take(c, sv);
+                const float f = factor(c), ve = exponent(c);
                 float m = -CUDART_INF_F, m2 = -CUDART_INF_F;
 #pragma unroll
                 for (int e = 0; e < 32; e += 4) {
                     m = fmax3(m, __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
                     m2 = fmax3(m2, __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
                 }
-                most = fmaxf(most, fmaf(fmaxf(m, m2), factor(c), exponent(c)));
-            }
-            const bool moves = most > ref + kRoom;            // (from -inf: any number)
-            if (__any_sync(0xffffffffu, moves)) {
-                float alpha = 1.f;
-                if (moves) {
-                    alpha = ex2(ref - (most - kBelow));
-                    ref = most - kBelow;
-                }
-                l *= alpha;
-                if (i > 0) {
-#pragma unroll 1
-                    for (int c = 0; c < D / 16; ++c) {
-                        uint32_t ov[16];
-                        tmem_ld16(colO + c * 16, ov);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * alpha);
-                        tmem_st16(colO + c * 16, ov);
+                const float most = fmaf(fmaxf(m, m2), f, ve);
+                const bool moves = most > ref + kRoom;        // (from -inf: any number)
+                if (__any_sync(0xffffffffu, moves)) {
+                    float alpha = 1.f;
+                    if (moves) {
+                        const float to = ceilf(most - kBelow);
+                        alpha = ex2(ref - to);
+                        ref = to;
                     }
+                    l *= alpha;
+                    if (i > 0) scale_output(alpha);
+                    if (c > 0) scale_weights(c, alpha);
                 }
-            }
-            const float base = ref == -CUDART_INF_F ? 0.f : ref;
-#pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-                uint32_t sv[32];
-                take(c, sv);
-                const float f = factor(c), ve = exponent(c), off = ve - base;
+                const float off = ve - (ref == -CUDART_INF_F ? 0.f : ref);
                 float ps[4] = {0.f, 0.f, 0.f, 0.f};
                 uint32_t pk[16];
 #pragma unroll
