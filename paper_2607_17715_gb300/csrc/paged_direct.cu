@@ -10,16 +10,17 @@
 // A CTA has an SM to itself, in two groups that take the tiles of 128 keys in turn, each with its own scores and output in
 // tensor memory, and its own warps: four for the softmax (a row a thread), four that convert (8-bit codes) or look after
 // tiles that are not whole, one that issues products and copies.  So a tile's conversions run beside the softmax of the
-// one before, and one group's products beside the other's softmax.  The groups' results join in shared memory, the
+// one before, one group's products beside the other's softmax, and the products of a tile's first 64 weights beside the
+// forming of its others.  The groups' results join in shared memory, the
 // stretches' in a kernel of their own.  Stretches go out longest first, as long as lets the last SM end first.
 //
 // A tile of 128 keys takes a CTA 1.4 us: tensor cores are busy for 0.8 us of it (16-bit pages, two terms of the queries) or 0.6,
 // shared memory for 0.9 (products of 128 x 128 read both operands from it at its full rate), the exponentials 0.5.  A stretch
 // takes 5 us before its first scores and after its last.  Eight trees of up to 64 nodes over up to 6000 rows of 16-bit pages
-// take 52 us (2.1 TB/s of pages, which two row tiles read), 32 nodes over 120000 rows of 8-bit pages 103 us (2.5).
+// take 52 us (2.1 TB/s of pages, which two row tiles read), 32 nodes over 120000 rows of 8-bit pages 100 us (2.5).
 // Tried and slower: scores 64 keys at a time in two pieces of tensor memory (62 -> 68 us), the next piece of scores
 // asked for while one is worked on (61 -> 63), all 128 scores of a row held (spills); the largest of a tile first, then its weights
-// (52 -> 54, 103 -> 107).
+// (52 -> 54, 103 -> 107).  Nothing is full: the chain scores, weights, products takes most of a group's time for a tile.
 //
 // Values of V that are not finite (16-bit pages): 0 times one is NaN for rows that do not see it, and a query's second
 // term makes NaN of an infinity of K.  A CTA whose results show either begins again with care: such values become zero in
@@ -63,8 +64,8 @@ struct Dir : TileOf<D> {
     static constexpr int kGroupBytes = 2 * kTile + 2 * kRaw;                  // K, V, and as they come
     static constexpr int kSmall = kQ + 2 * kGroupBytes;    // [group] (codes) scales of K and V; the join's sums
     static constexpr int kBack = kSmall + 2 * 1024;        // powers of two of the queries' rows: a byte each
-    static constexpr int kBars = kBack + BM;               // [group] scores, output, K, V, K's and V's tiles ready, weights, scales
-    static constexpr int kWords = kBars + 2 * 8 * 8;       // tensor memory, abort, [group] K not finite, rows touched (four), [group][2] pages, [group][12] units, [group][4] notes
+    static constexpr int kBars = kBack + BM;               // [group] scores, output, K, V, K's and V's tiles ready, last 64 weights, scales, first 64 weights, their products
+    static constexpr int kWords = kBars + 2 * 10 * 8;       // tensor memory, abort, [group] K not finite, rows touched (four), [group][2] pages, [group][12] units, [group][4] notes
     static constexpr int kSmem = kWords + 192;
 };
 static_assert(Dir<128, true>::kSmem <= 232448 && Dir<128, false>::kSmem <= 232448, "shared memory of a CTA");
@@ -252,8 +253,8 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
     const uint32_t inK = kCodes ? sV + C::kTile : sK, inV = kCodes ? inK + C::kRaw : sV;      // where the pages go
     uint32_t* const scales = reinterpret_cast<uint32_t*>(smem + C::kSmall) + g * BN * 2;      // (codes) [K, V][key], f16 twice
     int8_t* const s_back = reinterpret_cast<int8_t*>(smem + C::kBack);
-    const uint32_t bars = sQ + C::kBars + g * 64, barS = bars, barO = bars + 8, barK = bars + 16, barV = bars + 24;
-    const uint32_t readyK = bars + 32, readyV = bars + 40, readyP = bars + 48, readyC = bars + 56;     // (an arrival a warp)
+    const uint32_t bars = sQ + C::kBars + g * 80, barS = bars, barO = bars + 8, barK = bars + 16, barV = bars + 24;
+    const uint32_t readyK = bars + 32, readyV = bars + 40, readyP = bars + 48, readyC = bars + 56, readyW = bars + 64, barW = bars + 72;     // (an arrival a warp)
     uint32_t* const words = reinterpret_cast<uint32_t*>(smem + C::kWords);
     volatile uint32_t* const abort = words + 1;
     volatile uint32_t* const s_alone = words + 2 + g;         // the queries' first terms alone: K's tile has values that are not finite
@@ -270,7 +271,7 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
     const int hi = w.R.n_keys;
     const int n = (w.n + 1 - g) / 2;                          // the group's tiles: g, g + 2, ..
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 16; ++i) mbar_init(sQ + C::kBars + 8 * i, i % 8 < 4 ? 1 : 4);
+        for (int i = 0; i < 20; ++i) mbar_init(sQ + C::kBars + 8 * i, i % 10 < 4 || i % 10 == 9 ? 1 : 4);
         *abort = 0u;
         for (int i = 0; i < 4; ++i) s_touched[i] = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -369,15 +370,19 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
                 if (more) bring_k(i + 1, pages1);
                 mbar_wait(readyV, uses, P.err, abort);
                 if (kCodes && more) bring(&X.tm_v, inV, barV, pages1);
-                mbar_wait(readyP, uses, P.err, abort);
-                if (lane == 0) {
-                    tc_fence_after();
+                for (int half = 0; half < 2; ++half) {
+                    mbar_wait(half ? readyP : readyW, uses, P.err, abort);
+                    if (lane == 0) {
+                        tc_fence_after();
 #pragma unroll
-                    for (int kk = 0; kk < BN / 16; ++kk)
-                        mma_bf16_ts(tmemO, tmem + (uint32_t)kk * 8u, dv + (uint64_t)((kk * 16 * 128) >> 4), idO, kk > 0 || i > 0 ? 1u : 0u);
-                    mma_commit(barO);
+                        for (int kk = 0; kk < BN / 32; ++kk) {
+                            const int k = half * (BN / 32) + kk;
+                            mma_bf16_ts(tmemO, tmem + (uint32_t)k * 8u, dv + (uint64_t)((k * 16 * 128) >> 4), idO, k > 0 || i > 0 ? 1u : 0u);
+                        }
+                        mma_commit(half ? barO : barW);
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
                 if (more) scores(i + 1, uses ^ 1u, care);
                 if constexpr (!kCodes) {
                     mbar_wait(barO, uses, P.err, abort);
@@ -493,22 +498,19 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
             tmem_st16(colO + c * 16, ov);
         }
     };
-    // weights of the first n times 32 keys, by a power of two
-    auto scale_weights = [&](int n, float alpha) {
+    // weights of 32 keys, by a power of two
+    auto scale_weights = [&](int c, float alpha) {
+        uint32_t pv[16];
         tmem_st_wait();
-#pragma unroll 1
-        for (int c = 0; c < n; ++c) {
-            uint32_t pv[16];
-            tmem_ld16(colS + c * 16, pv);
-            tmem_ld_wait();
+        tmem_ld16(colS + c * 16, pv);
+        tmem_ld_wait();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const float2 w = kCodes ? __half22float2(*reinterpret_cast<const __half2*>(&pv[e]))
-                                        : make_float2(__uint_as_float(pv[e] << 16), __uint_as_float(pv[e] & 0xffff0000u));
-                pv[e] = kCodes ? pack_f16(w.x * alpha, w.y * alpha) : pack_bf16(w.x * alpha, w.y * alpha);
-            }
-            tmem_st16(colS + c * 16, pv);
+        for (int e = 0; e < 16; ++e) {
+            const float2 w = kCodes ? __half22float2(*reinterpret_cast<const __half2*>(&pv[e]))
+                                    : make_float2(__uint_as_float(pv[e] << 16), __uint_as_float(pv[e] & 0xffff0000u));
+            pv[e] = kCodes ? pack_f16(w.x * alpha, w.y * alpha) : pack_bf16(w.x * alpha, w.y * alpha);
         }
+        tmem_st16(colS + c * 16, pv);
     };
     auto softmax = [&](bool care) {
         ref = -CUDART_INF_F;
@@ -577,8 +579,12 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
                         ref = to;
                     }
                     l *= alpha;
-                    if (i > 0) scale_output(alpha);
-                    if (c > 0) scale_weights(c, alpha);
+                    if (c >= 2) {                             // (the products of the first half are under way)
+                        mbar_wait(barW, uses, P.err, abort);
+                        tc_fence_after();
+                    }
+                    if (i > 0 || c >= 2) scale_output(alpha);
+                    if (c & 1) scale_weights(c - 1, alpha);
                 }
                 const float off = ve - (ref == -CUDART_INF_F ? 0.f : ref);
                 float ps[4] = {0.f, 0.f, 0.f, 0.f};
@@ -597,6 +603,11 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
                 }
                 tmem_st16(colS + c * 16, pk);                 // (over scores that are taken: the thread's own)
                 l = fmaf((ps[0] + ps[1]) + (ps[2] + ps[3]), ex2(-ve), l);
+                if (c == 1) {
+                    tmem_st_wait();
+                    tc_fence_before();
+                    arrive(readyW);
+                }
             }
             tmem_st_wait();
             tc_fence_before();

@@ -91,16 +91,17 @@ class _Call:
                 out[at], lse[:, at] = brc.attend_tree(q64[at], k, v, tree, self.window, there)
         return out, lse
 
-    def check(self, trees=None):
+    def check(self, trees=None, more=(0.0, 0.0)):
+        """`more`: what the outputs and the lse may be off beside TOL."""
         out, lse = self.out.float().cpu().numpy(), self.lse.cpu().numpy()
         want, want_l = self.want(trees)
         tol = TOL[self.dtype]
         for same in (np.isnan, np.isposinf, np.isneginf):
             assert np.array_equal(same(out), same(want)) and np.array_equal(same(lse), same(want_l))
         fine = np.isfinite(want)
-        assert np.all(np.abs(out[fine] - want[fine]) <= tol + tol * np.abs(want[fine]))
+        assert np.all((np.abs(out - want) <= more[0] + tol + tol * np.abs(want))[fine])
         fine = np.isfinite(want_l)
-        assert np.all(np.abs(lse[fine] - want_l[fine]) <= tol * (1 + np.abs(want_l[fine]) * (self.dtype == "f32")))
+        assert np.all(np.abs(lse[fine] - want_l[fine]) <= more[1] + tol * (1 + np.abs(want_l[fine]) * (self.dtype == "f32")))
 
     def sync(self):
         P.lib().c2kv_sync(self.ctx)
@@ -387,5 +388,48 @@ def test_infinite_keys_and_values_over_any_number_of_tiles(shape, n, x):
         call.run()
         call.sync()
         call.check()
+    finally:
+        call.close()
+
+
+@pytest.mark.parametrize("at", [32, 64, 96, 128, 160, 192, 224, 288, 480])
+@pytest.mark.parametrize("shape", [("bf16", "native", 32, 8, 128), ("bf16", "native", 8, 2, 64), ("bf16", "e4m3", 32, 8, 128)], ids=lambda s: "-".join(map(str, s)))
+def test_scores_that_rise_within_a_tile(shape, at):
+    """Keys from `at` on outweigh those before by 2^15, which hold values 2^13 times theirs (16-bit pages): both count, and
+    weights formed before the rise keep their share."""
+    n, x, d = 20, 500, shape[4]
+    rise = 15 * np.log(2) * np.sqrt(d)
+
+    def edit(pg):
+        for key in range(x + n):
+            page, row = int(pg.table_np[0, key // 32]), key % 32
+            if pg.ks is None:
+                pg.k[page, :, row, 0] = rise if key >= at else 0.0
+                if key < at:
+                    pg.v[page, :, row] *= 2.0 ** 13
+            elif key >= at:
+                pg.k.view(torch.uint8)[page, :, row, 0] = 0x7e                    # (448)
+                pg.ks[page, :, row] = rise / 448
+    call = _Call(*shape, 32, [(star(n), x)], turn=False, edit=edit)
+    try:
+        call.q[..., 0] = 1.0
+        call.run()
+        call.sync()
+        # 8-bit rows whose scale is raised have all their channels raised, and scores of a hundred and more.  Operands made
+        # of codes and queries have f16's eleven bits, each off by 2^-11 at most, so a score is off by e = 2^-10 of the sum of
+        # its products' magnitudes, and so may its row's lse be.  Of weights that are off by factors of exp(-e) .. exp(e),
+        # out' - out = sum w_j (exp(e_j) - 1) (v_j - out) / sum w_j exp(e_j), at most (exp(2 e) - exp(e)) sum w_j |v_j - out|.
+        more = 0.0, 0.0
+        if call.pg.ks is not None:
+            k, v = (y[call.pg.table_np[0, :-(-(x + n) // 32)]].swapaxes(1, 2).reshape(-1, shape[3], d)[:x + n] for y in call.pg.host())
+            q = call.q.float().cpu().numpy().astype(np.float64).reshape(n, shape[3], -1, d)
+            score = np.where(brc.sees(star(n), x + n)[:, None, None], np.einsum("nhgd,khd->nhgk", q, k) / np.sqrt(d), -np.inf)
+            e = 2.0 ** -10 * np.einsum("nhgd,khd->nhgk", np.abs(q), np.abs(k)).max(-1) / np.sqrt(d)
+            w = np.exp(score - score.max(-1, keepdims=True))
+            w /= w.sum(-1, keepdims=True)
+            out = np.einsum("nhgk,khd->nhgd", w, v)
+            spread = np.stack([np.einsum("nhg,nhgd->nhgd", w[..., j], np.abs(v[j][None, :, None] - out)) for j in range(x + n)]).sum(0)
+            more = ((np.exp(2 * e) - np.exp(e))[..., None] * spread).reshape(n, -1, d), e.max()
+        call.check(more=more)
     finally:
         call.close()
