@@ -17,7 +17,7 @@
 // A tile of 128 keys takes a CTA 1.4 us: tensor cores are busy for 0.8 us of it (16-bit pages, two terms of the queries) or 0.6,
 // shared memory for 0.9 (products of 128 x 128 read both operands from it at its full rate), the exponentials 0.5.  A stretch
 // takes 5 us before its first scores and after its last.  Eight trees of up to 64 nodes over up to 6000 rows of 16-bit pages
-// take 52 us (2.1 TB/s of pages, which two row tiles read), 32 nodes over 120000 rows of 8-bit pages 100 us (2.5).
+// take 51 us (2.1 TB/s of pages, which two row tiles read), 32 nodes over 120000 rows of 8-bit pages 98 us (2.6).
 // Tried and slower: scores 64 keys at a time in two pieces of tensor memory (62 -> 68 us), the next piece of scores
 // asked for while one is worked on (61 -> 63), all 128 scores of a row held (spills); the largest of a tile first, then its weights
 // (52 -> 54, 103 -> 107).  Nothing is full: the chain scores, weights, products takes most of a group's time for a tile.
@@ -524,9 +524,8 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
         const float row_f = kCodes ? P.scale_log2 * pow2i(s_back[row]) : P.scale_log2;
         for (int i = 0; i < n; ++i, uses ^= 1u) {
             const int key0 = key_of(i);
-            if constexpr (kCodes) mbar_wait(readyC, uses, P.err, abort);
-            mbar_wait(barS, uses, P.err, abort);
-            tc_fence_after();
+            // (codes: what follows is known while the scores are formed)
+            mbar_wait(kCodes ? readyC : barS, uses, P.err, abort);
             const Rows there = rows_of(i);                    // (written ahead of the copies that the scores are behind)
             // of 32 keys (codes): scores in units of 2^[K's exponent], weights of V's
             // (within fp32's normal range: hidden scores of -inf times zero would be no number)
@@ -548,6 +547,8 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
 #pragma unroll
                 for (int c = 0; c < 4; ++c) touched = touched || (s_note[c] & of[c]) != 0u;
             }
+            if constexpr (kCodes) mbar_wait(barS, uses, P.err, abort);
+            tc_fence_after();
             // 32 keys at a time: 128 scores do not fit the registers, and what does not goes through an L1 that shared memory
             // leaves next to nothing of.  The reference is a whole number: where a later piece moves it, weights that are written
             // already take the difference in their exponents.
