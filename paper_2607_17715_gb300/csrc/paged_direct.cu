@@ -17,7 +17,7 @@
 // A tile of 128 keys takes a CTA 1.4 us: tensor cores are busy for 0.8 us of it (16-bit pages, two terms of the queries) or 0.6,
 // shared memory for 0.9 (products of 128 x 128 read both operands from it at its full rate), the exponentials 0.5.  A stretch
 // takes 5 us before its first scores and after its last.  Eight trees of up to 64 nodes over up to 6000 rows of 16-bit pages
-// take 51 us (2.1 TB/s of pages, which two row tiles read), 32 nodes over 120000 rows of 8-bit pages 98 us (2.6).
+// take 51 us (2.1 TB/s of pages, which two row tiles read), 32 nodes over 120000 rows of 8-bit pages 92 us (2.8).
 // Tried and slower: scores 64 keys at a time in two pieces of tensor memory (62 -> 68 us), the next piece of scores
 // asked for while one is worked on (61 -> 63), all 128 scores of a row held (spills); the largest of a tile first, then its weights
 // (52 -> 54, 103 -> 107).  Nothing is full: the chain scores, weights, products takes most of a group's time for a tile.
@@ -42,7 +42,6 @@ constexpr int kDirThreads = 4 * kDirGroup + 64;
 constexpr int kTurned = 16;              // rows of queries that a warp of the softmax turns (32 by half the warps took 4 us)
 constexpr uint32_t kDirTmem = 512;       // a group: S (P over its first half), O
 constexpr int kLeastTiles = 2;           // of a stretch: one a group
-constexpr int kJoinRows = 8;             // rows of a unit that a CTA joins
 constexpr int kItemTiles = 6, kJoinTiles = 3;   // what a stretch takes beside its tiles, and the kernel that joins them, in tiles
 constexpr int kMostCuts = 256;           // stretches of one unit's keys: their weights join in shared memory
 
@@ -856,8 +855,8 @@ cudaError_t launch(const PagedAttnCall& c, const PagedReq* req, int n, cudaStrea
             return cudaErrorInvalidValue;
         e = launch_overlapped(kernel, (unsigned)items, kDirThreads, kSmem, s, X);
         if (e == cudaSuccess && units > 0)
-            e = launch_overlapped(paged_join_kernel<D, BM, kJoinRows, true, DirectLaunch<kReq>>, (unsigned)(units * (BM / kJoinRows)), kJoinThreads,
-                                  (size_t)most * kJoinRows * 4, s, X);
+            e = launch_overlapped(paged_join_kernel<D, BM, true, DirectLaunch<kReq>>, (unsigned)(units * (BM / join_rows(D))), kJoinThreads,
+                                  (size_t)most * join_rows(D) * 4, s, X);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;

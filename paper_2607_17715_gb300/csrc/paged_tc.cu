@@ -27,7 +27,6 @@ namespace c2kv {
 namespace {
 
 constexpr int kPair = 2 * BM;
-constexpr int kJoinRows = 8;             // rows of a unit that a CTA joins
 constexpr int kUnits = 8;                // tiles whose notes are kept: more than K has stages
 
 // Warp 0 issues the products, warp 1 loads, 4..7 and 8..11 are the softmax of tiles A and B, which holds
@@ -622,11 +621,11 @@ cudaError_t launch(const PagedAttnCall& c, const KeyTiles& tiles, const std::vec
         cfg.numAttrs = b0 == 0 && tiles.n > 0;   // (after another kernel than the tiles' it waits for all of that)
         e = cudaLaunchKernelEx(&cfg, kernel, X);
         if (e == cudaSuccess && units > 0) {
-            cfg.gridDim = dim3((unsigned)(units * (kPair / kJoinRows)));
+            cfg.gridDim = dim3((unsigned)(units * (kPair / join_rows(D))));
             cfg.blockDim = dim3(kJoinThreads);
-            cfg.dynamicSmemBytes = (size_t)most * kJoinRows * 4;
+            cfg.dynamicSmemBytes = (size_t)most * join_rows(D) * 4;
             cfg.numAttrs = 1;
-            e = cudaLaunchKernelEx(&cfg, paged_join_kernel<D, kPair, kJoinRows, kTree, TcLaunch<kReq>>, X);
+            e = cudaLaunchKernelEx(&cfg, paged_join_kernel<D, kPair, kTree, TcLaunch<kReq>>, X);
         }
         if (e != cudaSuccess) return e;
     }

@@ -347,18 +347,17 @@ __device__ __forceinline__ void take_in(const Launch& X, const Item& w, uint32_t
     }
 }
 
-// The stretches of cut keys joined: kJoinRows rows of a unit a CTA, eight loads a thread on their way at once,
-// of several stretches where a thread has less than eight rows (one request of 8 KV heads has few units: 64 rows over 30000
-// took 44 us with 8 rows a CTA, 54 with 32, which are 32 CTAs of eight rows a thread).
-// (Joined by the last stretch of a unit instead, 19 partials of 128 KB came through one SM: 72 us for 64
-// tokens over 30000 rows, where this takes 4 of them.)
+// The stretches of cut keys joined: a row a thread, 512 / D rows of a unit a CTA, eight stretches' loads a thread on their
+// way at once (one request of 8 KV heads has few units: with 32 rows a CTA, eight a thread and a stretch at a time, 32 CTAs took 54 us
+// for 64 rows over 30000 where these take 42, attention and all; 32 nodes over 120000 rows took 98 with 8 rows a CTA, and 92 so).
 constexpr int kJoinThreads = 128;
+__host__ __device__ constexpr int join_rows(int d) { return kJoinThreads * 4 / d; }
 
-template <int D, int kUnit, int kJoinRows, bool kTree, class Launch>
+template <int D, int kUnit, bool kTree, class Launch>
 __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_constant__ Launch X) {
     const auto& P = X.a;
     extern __shared__ float weight[];                            // [stretch][row]
-    constexpr int kSlices = kUnit / kJoinRows;
+    constexpr int kJoinRows = join_rows(D), kSlices = kUnit / kJoinRows;
     const int u = blockIdx.x / kSlices, slice = blockIdx.x % kSlices;
     int r = 0;
     while (r + 1 < P.batch && P.req[r + 1].unit0 <= u) ++r;      // (entries that are not cut have no units)
@@ -387,41 +386,29 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
         }
     }
     __syncthreads();
-    constexpr int kLines = D / 4, kStep = kJoinThreads / kLines, kRows = kJoinRows / kStep, kBatch = 8 / kRows;
-    static_assert(kRows >= 1 && kRows * kBatch == 8, "eight loads on their way at once");
-    const int f = threadIdx.x % kLines, row0 = threadIdx.x / kLines;
-    float4 o[kRows];
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int kLines = D / 4, kBatch = 8;
+    const int f = threadIdx.x % kLines, row = threadIdx.x / kLines;
+    if (row >= live) return;
+    const float* const from = X.part_o + (item0 * kUnit + first + row) * D + 4 * f;
+    const int64_t step = (int64_t)P.hkv * kUnit * D;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int k0 = 0; k0 < S; k0 += kBatch) {
-        float4 y[kBatch][kRows];
+        float4 y[kBatch];
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-            const float* const from = X.part_o + ((item0 + (int64_t)min(k0 + b, S - 1) * P.hkv) * kUnit + first) * D + 4 * f;
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) y[b][i] = ld_after_l2(reinterpret_cast<const float4*>(from + (int64_t)min(row0 + i * kStep, live - 1) * D));
-        }
+        for (int b = 0; b < kBatch; ++b) y[b] = ld_after_l2(reinterpret_cast<const float4*>(from + min(k0 + b, S - 1) * step));
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
             if (k0 + b >= S) break;
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                const float a = weight[(k0 + b) * kJoinRows + min(row0 + i * kStep, live - 1)];
-                o[i].x = fmaf(y[b][i].x, a, o[i].x);
-                o[i].y = fmaf(y[b][i].y, a, o[i].y);
-                o[i].z = fmaf(y[b][i].z, a, o[i].z);
-                o[i].w = fmaf(y[b][i].w, a, o[i].w);
-            }
+            const float a = weight[(k0 + b) * kJoinRows + row];
+            o.x = fmaf(y[b].x, a, o.x);
+            o.y = fmaf(y[b].y, a, o.y);
+            o.z = fmaf(y[b].z, a, o.z);
+            o.w = fmaf(y[b].w, a, o.w);
         }
     }
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-        const int row = row0 + i * kStep;
-        if (row >= live) continue;
-        const int all = pr * kUnit + first + row;
-        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(P.out) + ((int64_t)(R.q0 + all / G) * P.hq + hk * G + all % G) * D + 4 * f) =
-            make_uint2(pack_bf16(o[i].x, o[i].y), pack_bf16(o[i].z, o[i].w));
-    }
+    const int all = pr * kUnit + first + row;
+    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(P.out) + ((int64_t)(R.q0 + all / G) * P.hq + hk * G + all % G) * D + 4 * f) =
+        make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
 }
 
 }  // namespace
