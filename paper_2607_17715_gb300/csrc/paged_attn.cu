@@ -20,21 +20,20 @@ constexpr int kMmaRows = 64;
 
 // The same of trees, and the rows up to which tcgen05 takes them straight from the pages instead of making key
 // tiles first.  Measured (us, mma.sync / straight from the pages; one request of 30000 rows, 8 of 4000, 16 of 500): 8-bit
-// pages of 128 channels, 16 rows 32 / 42, 30 / 41, 16 / 18, 32 rows 53 / 42, 44 / 41, 26 / 19; 16-bit ones, 16 rows 39 / 43, 40 / 42,
-// 14 / 18, 32 rows 64 / 43, 66 / 42, 24 / 19; 8-bit ones of 64 channels, 32 rows 32 / 35, 30 / 34, 19 / 15.  24 rows of eight requests
-// of 4000: 35 / 41 from 8-bit pages, 49 / 42 from 16-bit ones.  Straight from the pages / with key tiles: 256 rows 68 / 91, 66 / 89,
-// 40 / 38; 384 rows 87 / 109, 119 / 107, 62 / 56, 12 requests of 3000 rows 105 / 130, 32 of 2000 221 / 263, of up to 2000
-// 117 / 130; 512 rows 120 / 112, 133 / 113, 82 / 59.
+// pages of 128 channels, 16 rows 32 / 38, 30 / 37, 16 / 16, 32 rows 53 / 38, 44 / 38, 26 / 17; 16-bit ones, 16 rows 39 / 39, 40 / 39,
+// 14 / 16, 32 rows 64 / 39, 66 / 40, 24 / 17; 8-bit ones of 64 channels, 32 rows 32 / 33, 30 / 33, 19 / 14.  24 rows of eight requests
+// of 4000: 35 / 37 from 8-bit pages, 49 / 39 from 16-bit ones.  Straight from the pages / with key tiles: 256 rows 60 / 85, 58 / 91,
+// 35 / 38, 384 rows 76 / 107, 111 / 106, 54 / 56, 512 rows 102 / 109, 113 / 112, 71 / 58, of 16-bit pages 100 / 121, 112 / 126, 73 / 62.
 constexpr int tree_mma_rows(int d, bool codes) { return d * (codes ? 1 : 2) == 64 ? 32 : d * (codes ? 1 : 2) == 128 ? 24 : 16; }
-constexpr int kDirectRows = 384;
+constexpr int kDirectRows = 512;
 
 // ... and trees over few keys, which many rows a CTA would leave SMs idle for: mma.sync takes them eight rows a CTA,
 // or 16, where that is one wave of CTAs that read at most so many values of K, counted for eight rows.  Measured (us, eight /
-// 16 / the routes above; 8-bit pages of 128 channels): one request of 1500 rows, 64 rows of queries 13.1 / 16.4 / 18.6, 128 rows (26
-// million values) 17.4 / 18.4 / 18.8; of 6000, 48 rows (38 million) 19.6 / 20.5 / 28, 64 rows (49) 22.7 / 22.2 / 28; four of 500, 64
-// rows 13.2 / 16.6 / 18; 16-bit pages, 64 rows over 1500 15.5 / 16.9 / 19.3, 48 over 6000 26.8 / 24.6 / 28; 64 channels, 256
-// rows over 1500 20 / 18.4 / 18.
-constexpr int64_t kShortValues[2] = {26000000, 38000000};
+// 16 / the routes above; 128 channels): 8-bit pages, one request of 1500 rows, 64 rows of queries (13 million values) 13.1 / 16.5 / 17.0,
+// 128 rows (26) 17.2 / 18.3 / 17.4, of 6000, 32 rows (25) 16.5 / 21.2 / 21.6, 64 rows (50) 22.8 / 22.2 / 21.9; four of 500, 64
+// rows (17) 13.2 / 16.8 / 17.5, 16 of 100, 32 rows (8; eight are more than a wave) - / 10.5 / 12.8; 16-bit pages, 64 rows over 1500
+// 15.5 / 16.8 / 17.4, 96 rows (19) 19.5 / 18.4 / 17.5, 24 rows over 6000 (19) 17.3 / 19.8 / 21.7, 32 (25) 22.1 / 20.0 / 21.8.
+constexpr int64_t short_values(bool codes) { return codes ? 26000000 : 18000000; }
 
 // The same of fp32 contexts, and the keys that some request has to see for it: the lanes' kernel reads keys
 // again for every 4 rows, the register-tiled loop works on 16 rows or, below that, leaves most of its lanes
@@ -113,15 +112,15 @@ cudaError_t launch_many(const PagedAttnCall& c, const PagedReq* req, int n, int 
 // Eights of query rows a CTA for trees that short rows of keys leave SMs free for, 0 for others.
 int short_eights(const PagedAttnCall& c, const std::vector<PagedReq>& req, int d, bool codes) {
     const int64_t G = c.hq / c.hkv;
-    for (int eights = 1; eights <= 2; ++eights) {
-        int64_t units = 0, values = 0;
-        for (const PagedReq& q : req) {
-            if (values > kShortValues[1]) return 0;
-            units += (q.nq * G + 8 * eights - 1) / (8 * eights) * c.hkv;
-            values += (q.nq * G + 7) / 8 * c.hkv * keys_of(c, q) * d;
-        }
-        if (values <= kShortValues[eights - 1] && units <= (int64_t)device_sms() * paged_mma_tree_ctas(d, codes, eights)) return eights;
+    int64_t units[2] = {0, 0}, values = 0;
+    for (const PagedReq& q : req) {
+        values += (q.nq * G + 7) / 8 * c.hkv * keys_of(c, q) * d;
+        if (values > short_values(codes)) return 0;
+        units[0] += (q.nq * G + 7) / 8 * c.hkv;
+        units[1] += (q.nq * G + 15) / 16 * c.hkv;
     }
+    for (int eights = 1; eights <= 2; ++eights)
+        if (units[eights - 1] <= (int64_t)device_sms() * paged_mma_tree_ctas(d, codes, eights)) return eights;
     return 0;
 }
 
