@@ -433,3 +433,12 @@ def test_scores_that_rise_within_a_tile(shape, at):
         call.check(more=more)
     finally:
         call.close()
+
+
+@pytest.mark.parametrize("window", [0, 1500])
+@pytest.mark.parametrize("shape", [("bf16", "native", 8, 2, 64), ("bf16", "e4m3", 8, 2, 128), ("f32", "native", 8, 2, 64)], ids=lambda s: "-".join(map(str, s)))
+def test_uneven_requests(shape, window):
+    """Requests of a few keys beside ones of thousands, in no order: some are cut into stretches, some are not."""
+    r = np.random.default_rng(window)
+    rows = [40, 7000, 3, 900, 5200, 0, 2600, 130, 4100, 61, 1700, 3300]
+    _run(*shape, 64, [(random_tree(r, int(r.integers(9, 40)), near=9), x) for x in rows], window=window)
