@@ -7,6 +7,11 @@
 // 32 keys (a V scale that is NaN makes NaN of the rows that see it, and zero of the row itself).  16-bit pages are operands as they lie,
 // the queries two bf16 terms of them and the weights one, as in paged_mma.cu.
 //
+// Roundings: a code times its scale has eleven bits, as the queries over codes and the weights have, and weights over 16-bit
+// pages have eight.  Outputs are off by 2.2e-3 of their norm from 64 bits, where fp32 in between and the output's own
+// rounding give 1.7e-3.  (Scales met in fp32 by the scores would spare the first; a broadcast from shared memory for every
+// key made the softmax twice as long.  A second term of the weights would add a third to the products of 16-bit pages.)
+//
 // A CTA has an SM to itself, in two groups that take the tiles of 128 keys in turn, each with its own scores and output in
 // tensor memory, and its own warps: four for the softmax (a row a thread), four that convert (8-bit codes) or look after
 // tiles that are not whole, one that issues products and copies.  So a tile's conversions run beside the softmax of the
