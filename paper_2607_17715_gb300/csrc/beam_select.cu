@@ -9,7 +9,7 @@
 // every warp's r-th largest, and the least of those over the warps, is a bound that `best` values reach (8 r >= best).
 // The score rises with the value, so the bound holds for values, less what the score's rounding can hide.  What passes
 // is ranked by counting: 16 x 8 beams over 131072 16-bit logits take 19 us, where a list of every value above the first
-// ones' took 47; four beams over 32000 7.4.  The CTA that ends last joins its request's stretches the same way, the bound from their
+// ones took 47; four beams over 32000 7.4, one request of 16 over 131072 15.  The CTA that ends last joins its request's stretches the same way, the bound from their
 // first ones.
 #include "paged.cuh"
 #include "per_device.cuh"
@@ -48,8 +48,50 @@ __device__ __forceinline__ int ordered(float x) {
 }
 __device__ __forceinline__ float of_ordered(int i) { return __int_as_float(i < 0 ? i ^ 0x7fffffff : i); }
 
+// Appends to the list; past its end nothing is written, and s.n says how many there were.
+__device__ __forceinline__ void append(Best& s, uint32_t key, uint32_t place) {
+    const int at = atomicAdd(&s.n, 1);
+    if (at < kSelList) s.list[at] = make_uint2(key, place);
+}
+
+// Leaves of list[0, n) what a bound does not: of the threads' largest keys every warp's r-th largest, and the least of those
+// over the warps, is a key that `best` reach (8 r >= best).  Returns how many there are.
+__device__ __forceinline__ int shorten(Best& s, int n, int best) {
+    constexpr int kMine = kSelList / kSelThreads;
+    uint2 mine[kMine];
+    uint32_t rest = 0u, bound = 0u;
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+        const int i = threadIdx.x + k * kSelThreads;
+        mine[k] = i < n ? s.list[i] : make_uint2(0u, 0u);
+        rest = max(rest, mine[k].x);
+    }
+    for (int i = (best + kSelWarps - 1) / kSelWarps; i > 0; --i) {
+        bound = __reduce_max_sync(0xffffffffu, rest);
+        const uint32_t at = __ballot_sync(0xffffffffu, rest == bound);
+        if ((int)(threadIdx.x % 32) == __ffs(at) - 1) rest = 0u;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s.sum = 0xffffffffu;
+        s.n = 0;
+    }
+    __syncthreads();
+    if (threadIdx.x % 32 == 0) atomicMin(&s.sum, bound);
+    __syncthreads();
+    bound = s.sum;
+#pragma unroll
+    for (int k = 0; k < kMine; ++k)
+        if (mine[k].x != 0u && mine[k].x >= bound) append(s, mine[k].x, mine[k].y);
+    __syncthreads();
+    return s.n;
+}
+
 // The first `best` of list[0, n), in order; every thread of the CTA.  Returns how many there are.
+// (Every entry meets every other: a long list is shortened first.  Four beams over 50000 values took 42 us without, 512
+// beams over 32000 124.)
 __device__ __forceinline__ int rank_list(Best& s, int n, int best) {
+    if (n > 128) n = shorten(s, n, best);
     for (int i = threadIdx.x; i < n; i += kSelThreads) {
         const uint2 x = s.list[i];
         int rank = 0;
@@ -61,12 +103,6 @@ __device__ __forceinline__ int rank_list(Best& s, int n, int best) {
     }
     __syncthreads();
     return min(n, best);
-}
-
-// Appends to the list; past its end nothing is written, and s.n says how many there were.
-__device__ __forceinline__ void append(Best& s, uint32_t key, uint32_t place) {
-    const int at = atomicAdd(&s.n, 1);
-    if (at < kSelList) s.list[at] = make_uint2(key, place);
 }
 
 // A thread's values of a stretch as they lie in memory: kEach of them, 16 bytes' worth next to one another.
@@ -176,7 +212,8 @@ __global__ void __launch_bounds__(kSelThreads, kEach > 16 && !kBf16 ? 2 : 4) bea
     __shared__ bool s_last;
     const int lane = threadIdx.x % 32, K = P.best, V = P.vocab;
     const int r = blockIdx.x / P.parts, part = blockIdx.x - r * P.parts, of_beam = P.parts / P.width;
-    const int w = part / of_beam, a = (part - w * of_beam) * X::kStretch, n = min(X::kStretch, V - a);
+    const int w = part / of_beam, length = ((V + of_beam - 1) / of_beam + 7) & ~7;     // (whole 16-byte lines: equal stretches but for that)
+    const int a = (part - w * of_beam) * length, n = min(length, V - a);
     const int64_t row = (int64_t)(P.b0 + r) * P.width + w;
     if (threadIdx.x == 0) {
         s.n = 0;
@@ -268,21 +305,30 @@ __global__ void __launch_bounds__(kSelThreads, kEach > 16 && !kBf16 ? 2 : 4) bea
         __syncthreads();
     }
     int total = 0;                                        // the best so far, s.best
-    for (int i0 = 0; i0 < entries; i0 += 2 * kSelThreads) {
+    constexpr int kAhead = 8;                             // entries of a thread on their way at once
+    for (int i0 = 0; i0 < entries; i0 += kAhead * kSelThreads) {
+        uint2 e[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int i = i0 + k * kSelThreads + threadIdx.x;
+            e[k] = i < entries ? __ldcg(all + i) : make_uint2(0u, 0u);
+        }
         // (what is left of the list: no more than was there, and two a thread)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int i = i0 + k * kSelThreads + threadIdx.x;
-            const uint2 e = i < entries ? __ldcg(all + i) : make_uint2(0u, 0u);
-            if (e.x != 0u && !before(bound.x, bound.y, e.x, e.y)) append(s, e.x, e.y);
-        }
-        __syncthreads();
-        if (s.n > kSelList - 2 * kSelThreads || i0 + 2 * kSelThreads >= entries) {
-            total = rank_list(s, s.n, K);
-            if ((int)threadIdx.x < total) s.list[threadIdx.x] = s.best[threadIdx.x];
-            if (total == K) bound = s.best[K - 1];
+        for (int k = 0; k < kAhead; k += 2) {
+            const int past = i0 + (k + 2) * kSelThreads;
+            if (past - 2 * kSelThreads >= entries) break;
+#pragma unroll
+            for (int j = k; j < k + 2; ++j)
+                if (e[j].x != 0u && !before(bound.x, bound.y, e[j].x, e[j].y)) append(s, e[j].x, e[j].y);
             __syncthreads();
-            if (threadIdx.x == 0) s.n = total;
+            if (s.n > kSelList - 2 * kSelThreads || past >= entries) {
+                total = rank_list(s, s.n, K);
+                if ((int)threadIdx.x < total) s.list[threadIdx.x] = s.best[threadIdx.x];
+                if (total == K) bound = s.best[K - 1];
+                __syncthreads();
+                if (threadIdx.x == 0) s.n = total;
+            }
             __syncthreads();
         }
     }
