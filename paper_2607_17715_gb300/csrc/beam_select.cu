@@ -6,11 +6,11 @@
 //
 // Every value is read once, which bounds a batch.  A CTA takes a stretch of one beam, 4096 or 16384 values, all on
 // their way at once and kept in registers as they come.  Few of them need be looked at: of the lanes' largest values
-// every warp's r-th largest, and the least of those over the warps, is a bound that `best` values reach (8 r >= best).
+// every warp's r-th largest, and the least of those over the warps, is a bound that `best` values reach (r times the warps).
 // The score rises with the value, so the bound holds for values, less what the score's rounding can hide.  What passes
-// is ranked by counting: 16 x 8 beams over 131072 16-bit logits take 19 us, where a list of every value above the first
-// ones took 47; four beams over 32000 7.4, one request of 16 over 131072 15.  The CTA that ends last joins its request's stretches the same way, the bound from their
-// first ones.
+// is ranked by counting.  The CTA that ends last joins its request's stretches the same way, the bound from their first ones.
+// 16 x 8 beams over 131072 16-bit logits take 19 us, where a list of every value above the first ones took 47; one request
+// of 16 beams 15, four beams over 32000 7.4.
 #include "paged.cuh"
 #include "per_device.cuh"
 
@@ -238,14 +238,16 @@ __global__ void __launch_bounds__(kSelThreads, kEach > 16 && !kBf16 ? 2 : 4) bea
 #pragma unroll
         for (int u = 0; u < kEach; ++u) top = fmaxf(top, v[u]);
         {
-            int rest = ordered(top), bound = rest;
-            for (int i = (K + kSelWarps - 1) / kSelWarps; i > 0; --i) {
+            // (of warps all of whose lanes have values: a short vocabulary leaves some without)
+            const int full = min(kSelWarps, n / (32 * X::kVec)), rounds = full > 0 ? (K + full - 1) / full : 33;
+            int rest = ordered(top), bound = ordered(-INFINITY);
+            for (int i = rounds <= 32 ? rounds : 0; i > 0; --i) {
                 bound = __reduce_max_sync(0xffffffffu, rest);
                 const uint32_t at = __ballot_sync(0xffffffffu, rest == bound);
                 if (lane == __ffs(at) - 1) rest = ordered(-INFINITY);
             }
             __syncthreads();
-            if (lane == 0) atomicMin(&s.bound, bound);
+            if (lane == 0 && ((int)threadIdx.x / 32 < full || rounds > 32)) atomicMin(&s.bound, bound);
             __syncthreads();
         }
         // Scores of values below the bound may round to the bound's: by 2^-23 of what is added, less than this

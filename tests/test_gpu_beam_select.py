@@ -214,3 +214,20 @@ def test_values_beside_large_scores(ctx):
     x = np.random.default_rng(5).standard_normal((40, 50000))
     _run(ctx, 1, 1, 50000, 16, x=x[:1], score=[[-3.0e6]])
     _run(ctx, 20, 2, 50000, 16, x=x, score=-1.0e5 * np.arange(1, 41).reshape(20, 2))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [31, 255, 257, 511, 513, 1023, 1025, 1279, 1281, 1500, 1791, 1793, 2047, 2049, 2500, 4099, 5000, 8191, 50000])
+def test_stretches_that_leave_lanes_without_values(ctx, vocab, dtype):
+    """Vocabularies that give some warps of a stretch no values, or fewer than lanes; from one continuation to 64."""
+    for best in (1, 5, 33, 64):
+        _run(ctx, 2, 3, vocab, best, dtype, norm=True, seed=best)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_beams_far_apart(ctx, dtype):
+    """One beam's candidates all come before the others': the join meets long lists that its bound does not shorten."""
+    for width, vocab, best in ((16, 40000, 64), (64, 5000, 64), (32, 32000, 32)):
+        score = np.tile(-60.0 * np.arange(width), (2, 1))
+        score[1] = score[1][::-1]
+        _run(ctx, 2, width, vocab, best, dtype, score=score, seed=width)
