@@ -1,0 +1,63 @@
+"""Errors of attention of trees relative to a row's norm: outputs over thousands of rows are too small for an absolute
+tolerance (one of 2e-2 does not notice a key tile that is left out).
+
+The tolerances are those of attention of tokens that follow one another, for the same reasons.  Over random keys and
+values a bf16 output's own rounding is at most 2^-9 of a value, 2.0e-3 of the norm; weights of 8 bits (over 16-bit pages)
+or 11, queries and codes times scales of 11 bits add errors of either sign, 2^-9 / sqrt(3) of the norm together
+at most: 5e-3.  lse: a score moves by 2^-12 |q k| / sqrt(d) for each operand rounded to 11 bits, two of them below 1e-3
+for normal ones: 2e-3.  fp32: 1e-5, lse 2e-5 of its magnitude and one."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import branch_oracle as brc
+from tests import _dense_pages as D
+from tests import _paged_helpers as P
+from tests._tree_helpers import chain, random_tree, star
+
+gpu = pytest.mark.gpu
+TOL = {"bf16": 5e-3, "f32": 1e-5}
+TOL_LSE = {"bf16": 2e-3, "f32": 2e-5}
+
+SHAPES = [("bf16", "e4m3", 32, 8, 128), ("bf16", "native", 32, 8, 128), ("bf16", "e4m3", 28, 4, 64), ("bf16", "native", 8, 2, 64),
+          ("f32", "native", 16, 4, 64), ("f32", "e4m3", 8, 2, 128)]
+# (nodes, rows before) a request: each way that a call may go, of one and several row tiles, odd and even numbers of key
+# tiles, stretches cut and whole
+LENS = {
+    "few": [(2, 9001), (3, 5000), (1, 777)], "short": [(16, 1500), (9, 300)], "tile": [(20, 9001)], "deep": [(120, 4000)],
+    "tiles": [(60, 5000), (100, 2500), (33, 95)], "whole": [(20 + i % 9, 400 + 37 * i) for i in range(40)], "large": [(200, 2500), (300, 700)],
+}
+
+
+@gpu
+@pytest.mark.parametrize("window", [0, 700])
+@pytest.mark.parametrize("lens", LENS, ids=str)
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "-".join(map(str, s)))
+def test_relative_errors(shape, lens, window):
+    dtype, fmt, hq, hkv, d = shape
+    r, gen = np.random.default_rng(5), torch.Generator(device="cuda").manual_seed(5)
+    trees = [chain(n) if lens == "deep" else random_tree(r, n, near=12) for n, _ in LENS[lens]]
+    k, v = ([torch.randn((n + x, hkv, d), generator=gen, device="cuda") for n, x in LENS[lens]] for _ in range(2))
+    T = sum(n for n, _ in LENS[lens])
+    q = torch.randn((T, hq, d), generator=gen, device="cuda").to(P.TDT[dtype])
+    pos = torch.from_numpy(r.integers(0, 100000, T).astype(np.int32)).cuda()
+    call = D.Call(dtype, hq, hkv, d, D.Rows(dtype, fmt, k, v, 64), trees, q, pos, window=window, times=3)
+    assert torch.equal(call.outs[0], call.outs[1]) and torch.equal(call.outs[0], call.outs[2])
+    want, want_l = call.want()
+    assert D.relative(call.out, want) <= TOL[dtype]
+    assert ((call.lse - want_l).abs() <= TOL_LSE[dtype] * (1 + (want_l.abs() if dtype == "f32" else 0))).all()
+
+
+@pytest.mark.parametrize("tree,x", [(star(20), 9001), (chain(60), 5000)], ids=["star", "chain"])
+def test_a_lost_tile_would_show(tree, x):
+    """The tolerances notice a tile of 128 keys left out of thousands: outputs and sums without it are off by more, in most
+    rows."""
+    rng, n = np.random.default_rng(0), len(tree)
+    q, k, v = (rng.standard_normal((m, 1, 128)) for m in (n, x + n, x + n))
+    want, want_l = brc.attend_tree(q, k, v, tree)
+    for lo in (0, 128 * 21, (x - 128) // 128 * 128):
+        there = np.ones(x + n, bool)
+        there[lo:lo + 128] = False
+        out, lse = brc.attend_tree(q, k, v, tree, there=there)
+        assert np.median(np.linalg.norm(out - want, axis=-1) / np.linalg.norm(want, axis=-1)) > 4 * TOL["bf16"]
+        assert np.median(np.abs(lse - want_l)) > 4 * TOL_LSE["bf16"]
