@@ -416,10 +416,11 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
                 v_scale = ld_after(P.pg.v_scale + from);
             }
         };
-        // ... relative to a power of two for 32 keys, the largest to [2^6, 2^7): a code's product is below 2^16
-        auto put_scale = [&](float x, uint32_t* to, int least) {
+        // ... relative to a power of two for 32 keys, the largest to [2^6, 2^7): a code's product is below 2^16.  `none`: the
+        // power of keys that are all zero
+        auto put_scale = [&](float x, uint32_t* to, int least, int none) {
             const uint32_t y = __float_as_uint(x) & 0x7fffffffu, top = __reduce_max_sync(0xffffffffu, y < 0x7f800000u ? y : 0u);
-            const int unit = top == 0u ? 0 : max(least, min(119, (int)(top >> 23) - 126 - 7));
+            const int unit = top == 0u ? none : max(least, min(119, (int)(top >> 23) - 126 - 7));
             const __half2 h = __float2half2_rn(x * pow2i(-unit));
             to[t] = *reinterpret_cast<const uint32_t*>(&h);
             return unit;
@@ -435,8 +436,9 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
                     mbar_wait(barK, uses, P.err, abort);
                     if (i > 0) mbar_wait(barS, uses ^ 1u, P.err, abort);             // the products before have read K's tile, and V's
                     const bool odd = !(fabsf(v_scale) < CUDART_INF_F);       // (V's row becomes zero, and NaN of the rows that see it)
-                    // (V's from -90 on: the sum of weights takes 2^-unit)
-                    const int k_unit = put_scale(k_scale, scales, -120), v_unit = put_scale(odd ? 0.f : v_scale, scales + BN, -90);
+                    // V's from -90 on: the sum of weights takes 2^-unit.  And -90 where all are zero, since a reference takes V's
+                    // unit too: at 0 it rose by 2^15 and more above what other rows' values need, and took their weights' bits
+                    const int k_unit = put_scale(k_scale, scales, -120, 0), v_unit = put_scale(odd ? 0.f : v_scale, scales + BN, -90, -90);
                     if (lane == 0) s_units[(i & 1) * 4 + t / 32] = k_unit;
                     convert_sync(g);
                     ask_scales(i + 1, pages1);
@@ -501,6 +503,11 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
             for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * alpha);
             tmem_st16(colO + c * 16, ov);
         }
+    };
+    // a sum of weights by 2^e, e <= 0: further down than one factor of fp32 reaches (V's units differ by up to 2^209)
+    auto lowered = [](float sum, float e) {
+        if constexpr (kCodes) sum *= ex2(fminf(e + 120.f, 0.f));
+        return sum * ex2(kCodes ? fmaxf(e, -120.f) : e);
     };
     // weights of 32 keys, by a power of two
     auto scale_weights = [&](int c, float alpha) {
@@ -567,7 +574,8 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
                     for (int e = 0; e < 32; ++e)
                         if (!(bits >> e & 1u)) sv[e] = __float_as_uint(-CUDART_INF_F);
                 }
-                const float f = factor(c), ve = exponent(c);
+                const float f = factor(c);
+                float ve = exponent(c);
                 float m = -CUDART_INF_F, m2 = -CUDART_INF_F;
 #pragma unroll
                 for (int e = 0; e < 32; e += 4) {
@@ -581,9 +589,9 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
                     if (moves) {
                         const float to = ceilf(most - kBelow);
                         alpha = ex2(ref - to);
+                        l = lowered(l, ref - to);
                         ref = to;
                     }
-                    l *= alpha;
                     if (c >= 2) {                             // (the products of the first half are under way)
                         mbar_wait(barW, uses, P.err, abort);
                         tc_fence_after();
@@ -591,6 +599,8 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
                     if (i > 0 || c >= 2) scale_output(alpha);
                     if (c & 1) scale_weights(c - 1, alpha);
                 }
+                // weights of 2^-40 and less are nothing in f16: the sum takes them where fp32 still holds them
+                if constexpr (kCodes) ve = fmaxf(ve, fminf(fmaf(-fmaxf(m, m2), f, ref - 40.f), 200.f));
                 const float off = ve - (ref == -CUDART_INF_F ? 0.f : ref);
                 float ps[4] = {0.f, 0.f, 0.f, 0.f};
                 uint32_t pk[16];
@@ -679,7 +689,7 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    l = fmaf(l0, a0, l1 * a1);
+    l = lowered(l0, ref0 - base) + lowered(l1, ref1 - base);
     const bool poisoned = s_touched[row / 32] >> (row & 31) & 1u;            // (codes) by a row of V whose scale is no number
     const float inv = l == 0.f ? 0.f : kCodes && poisoned ? CUDART_NAN_F : 1.0f / l;
     const float lse2 = l == 0.f ? -CUDART_INF_F : top + log2f(l);
