@@ -8,7 +8,9 @@
 // the queries two bf16 terms of them and the weights one, as in paged_mma.cu.
 //
 // Roundings: a code times its scale has eleven bits, as the queries over codes and the weights have, and weights over 16-bit
-// pages have eight.  Outputs are off by 2.2e-3 of their norm from 64 bits, where fp32 in between and the output's own
+// pages have eight.  The scale is rounded too where all of a tile's are within 2^20 of the largest of their 32 keys (rows that a
+// query does not see among them); in other tiles the product alone is, down to 2^-29 of that.  Weights take V's powers of two, and
+// lose bits where those of 32 keys are more than 2^22 above what another 32, which count as much, have.  Outputs are off by 2.2e-3 of their norm from 64 bits, where fp32 in between and the output's own
 // rounding give 1.7e-3.  (Scales met in fp32 by the scores would spare the first; a broadcast from shared memory for every
 // key made the softmax twice as long.  A second term of the weights would add a third to the products of 16-bit pages.)
 //
@@ -69,7 +71,7 @@ struct Dir : TileOf<D> {
     static constexpr int kSmall = kQ + 2 * kGroupBytes;    // [group] (codes) scales of K and V; the join's sums
     static constexpr int kBack = kSmall + 2 * 1024;        // powers of two of the queries' rows: a byte each
     static constexpr int kBars = kBack + BM;               // [group] scores, output, K, V, K's and V's tiles ready, last 64 weights, scales, first 64 weights, their products
-    static constexpr int kWords = kBars + 2 * 10 * 8;       // tensor memory, abort, [group] K not finite, rows touched (four), [group][2] pages, [group][12] units, [group][4] notes
+    static constexpr int kWords = kBars + 2 * 10 * 8;       // tensor memory, abort, [group] K not finite, rows touched (four), [group][2] pages, [group][12] units, [group][4] notes, [group] far
     static constexpr int kSmem = kWords + 192;
 };
 static_assert(Dir<128, true>::kSmem <= 232448 && Dir<128, false>::kSmem <= 232448, "shared memory of a CTA");
@@ -85,7 +87,7 @@ __device__ __forceinline__ bool convert_or(int g, bool x) {
     return any != 0u;
 }
 
-// The queries' rows of a warp (32), turned, as two bf16 terms: the first in place, what it lacks a tile behind.
+// The queries' rows of a warp (kTurned), turned, as two bf16 terms: the first in place, what it lacks a tile behind.
 template <int D, int kReq>
 __device__ __forceinline__ void turn_queries_twice(const PagedAttn<kReq>& P, const QueryRows<D>& k, int warp, int lane, uint32_t sQ) {
     using C = TileOf<D>;
@@ -163,8 +165,9 @@ struct Rows {
 
 // A tile of codes [128][D] times their rows' scales (f16, twice in a word) as f16 in 64-channel blocks under the 128-byte
 // swizzle, by a group's threads; (not `all`) rows that are not there become zero.  The scale's rounding and the product's
-// are 2^-12 of a value each; the output's own is 2^-9.  (Scales in fp32 on the scores and the weights instead, whose rows
-// every thread reads from shared memory, took the softmax twice the time: 3400 clocks a tile for 1600.)
+// are 2^-12 of a value each, where both are f16's normal numbers: scales down to 2^-20 of the largest of their 32 keys, rows
+// that a query does not see among them; others go by wide_codes_to_f16.  The output's own is 2^-9.  (Scales in fp32 on the scores and
+// the weights instead, whose rows every thread reads from shared memory, took the softmax twice the time: 3400 clocks a tile for 1600.)
 template <int D>
 __device__ __forceinline__ void codes_to_f16(uint32_t raw, uint32_t tile, const uint32_t* scale, int t, bool all, const Rows& rows) {
     constexpr int kChunks = D / 16, kStep = kDirGroup / kChunks, kPasses = BN / kStep;
@@ -194,6 +197,30 @@ __device__ __forceinline__ void codes_to_f16(uint32_t raw, uint32_t tile, const 
         const uint4 a = make_uint4(y[0], y[1], y[2], y[3]), b = make_uint4(y[4], y[5], y[6], y[7]);
         sts128_(at + (((q + first) ^ (row & 7)) << 4), first ? b : a);
         sts128_(at + (((q + 1 - first) ^ (row & 7)) << 4), first ? a : b);
+    }
+}
+
+// The same by scales in fp32, for tiles with some that f16 has not as normal numbers: one rounding, of the product, to eleven
+// bits down to 2^-29 of what the largest scale makes of a code of 448.
+template <int D>
+__device__ __noinline__ void wide_codes_to_f16(uint32_t raw, uint32_t tile, const uint32_t* scale, int t, bool all, Rows rows) {
+    constexpr int kChunks = D / 16, kStep = kDirGroup / kChunks;
+    const int chunk = t % kChunks, q = chunk % 4 * 2;
+#pragma unroll 1
+    for (int row = t / kChunks; row < BN; row += kStep) {
+        uint4 w = lds128(raw + row * D + chunk * 16);
+        if (!all && !rows.has(row)) w = make_uint4(0u, 0u, 0u, 0u);
+        const float f = __uint_as_float(scale[row]);
+        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+        uint32_t y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float2 z = codes2(x[e / 2] >> (16 * (e & 1)));
+            y[e] = pack_f16(z.x * f, z.y * f);
+        }
+        const uint32_t at = tile + chunk / 4 * TileOf<D>::kHalf + row * 128;
+        sts128_(at + ((q ^ (row & 7)) << 4), make_uint4(y[0], y[1], y[2], y[3]));
+        sts128_(at + (((q + 1) ^ (row & 7)) << 4), make_uint4(y[4], y[5], y[6], y[7]));
     }
 }
 
@@ -267,6 +294,7 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
     // (codes) exponents that 32 keys lack: K's of every other tile, V's; and rows of V's tile that are not finite, a bit each
     volatile int32_t* const s_units = reinterpret_cast<int32_t*>(words) + 12 + 12 * g;
     volatile uint32_t* const s_note = words + 36 + 4 * g;
+    uint8_t* const s_far = reinterpret_cast<uint8_t*>(words + 44 + g);       // (codes) 32 keys of a tile with scales far apart, a byte each
     if ((sQ & 1023u) != 0u) {                                 // (tiles lie on their swizzle's pattern: it always does)
         if (threadIdx.x == 0) atomicOr(P.err, 2);
         return;
@@ -417,13 +445,29 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
             }
         };
         // ... relative to a power of two for 32 keys, the largest to [2^6, 2^7): a code's product is below 2^16.  `none`: the
-        // power of keys that are all zero
-        auto put_scale = [&](float x, uint32_t* to, int least, int none) {
+        // power of keys that are all zero.  `far`: a scale that is no normal number of f16 then
+        auto put_scale = [&](float x, uint32_t* to, int least, int none, bool& far) {
             const uint32_t y = __float_as_uint(x) & 0x7fffffffu, top = __reduce_max_sync(0xffffffffu, y < 0x7f800000u ? y : 0u);
             const int unit = top == 0u ? none : max(least, min(119, (int)(top >> 23) - 126 - 7));
             const __half2 h = __float2half2_rn(x * pow2i(-unit));
+            far = far || y - 1u < ((uint32_t)max(unit + 113, 1) << 23) - 1u;
             to[t] = *reinterpret_cast<const uint32_t*>(&h);
             return unit;
+        };
+        // K's (V's) tile i, some of whose scales f16 has not, by scales in fp32: over what its threads made of it.  (As another
+        // way instead of a second one it cost tiles that do not take it 1 %.)
+        [[maybe_unused]] auto again = [&](int i, bool v, const Rows& there) {
+            uint32_t* const to = scales + (v ? BN : 0);
+            const int p = __shfl_sync(0xffffffffu, pages_of(i), t >> 4), at = key_of(i) + t, unit = s_units[v ? 8 + t / 32 : (i & 1) * 4 + t / 32];
+            float x = 0.f;
+            if (p >= 0 && at >= w.k_lo && at < hi)
+                x = ld_after((v ? P.pg.v_scale : P.pg.k_scale) + (int64_t)p * P.pg.scale_stride + (w.hk << P.pg.page_shift) +
+                             (t & ((1 << P.pg.page_shift) - 1)));
+            if (v && !(fabsf(x) < CUDART_INF_F)) x = 0.f;
+            convert_sync(g);                                  // (the f16 ones have been read)
+            to[t] = __float_as_uint(x * pow2i(-unit));
+            convert_sync(g);
+            wide_codes_to_f16<D>(v ? inV : inK, v ? sV : sK, to, t, there.all(), there);
         };
         auto all = [&](bool care) {
             if constexpr (kCodes) {
@@ -438,12 +482,17 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
                     const bool odd = !(fabsf(v_scale) < CUDART_INF_F);       // (V's row becomes zero, and NaN of the rows that see it)
                     // V's from -90 on: the sum of weights takes 2^-unit.  And -90 where all are zero, since a reference takes V's
                     // unit too: at 0 it rose by 2^15 and more above what other rows' values need, and took their weights' bits
-                    const int k_unit = put_scale(k_scale, scales, -120, 0), v_unit = put_scale(odd ? 0.f : v_scale, scales + BN, -90, -90);
+                    bool far = false;
+                    const int k_unit = put_scale(k_scale, scales, -120, 0, far), v_unit = put_scale(odd ? 0.f : v_scale, scales + BN, -90, -90, far);
                     if (lane == 0) s_units[(i & 1) * 4 + t / 32] = k_unit;
+                    far = __any_sync(0xffffffffu, far);
+                    if (lane == 0) s_far[t / 32] = far;
                     convert_sync(g);
+                    far = *reinterpret_cast<volatile uint32_t*>(s_far) != 0u;
                     ask_scales(i + 1, pages1);
                     pages1 = pages_of(i + 2);
                     codes_to_f16<D>(inK, sK, scales, t, true, Rows{});               // (hidden keys' scores are replaced)
+                    if (far) again(i, false, Rows{0xffu, 0, BN});
                     fence_proxy_async();
                     arrive(readyK);
                     mbar_wait(barV, uses, P.err, abort);
@@ -456,6 +505,7 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
                     }
                     arrive(readyC);
                     codes_to_f16<D>(inV, sV, scales + BN, t, there.all(), there);
+                    if (far) again(i, true, there);
                     fence_proxy_async();
                     convert_sync(g);                          // (the scales have been read)
                 } else {

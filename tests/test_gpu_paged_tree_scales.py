@@ -89,3 +89,37 @@ def test_values_far_apart_that_count_alike(kind, way, order):
     of = np.arange(rows) // 32
     steps = {"up": of * most // of[-1], "down": most - of * most // of[-1], "mixed": np.random.default_rng(1).integers(0, most + 1, of[-1] + 1)[of]}[order]
     assert _error(kind, way, steps, 2.0 ** -np.round(steps * 64 / 4 / np.sqrt(kind[1]) / np.log(2))) <= TOL
+
+
+@pytest.mark.parametrize("far", [0, 12, 20, 24])
+@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("kind", KINDS, ids=lambda s: "-".join(map(str, s)))
+def test_values_of_a_sibling(kind, way, far):
+    """A node's own values are half of its output and more; a sibling next to it that it does not see holds values 2^far
+    times as large."""
+    n, x = WAYS[way]
+    steps = np.where(np.arange(n + x) < x, 0, 6)
+    assert _error(kind, way, steps, np.ones(n + x), own=8.0, hidden=(1.0, 2.0 ** far)) <= TOL
+
+
+@pytest.mark.parametrize("far", [0, 12, 16])
+@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("kind", KINDS, ids=lambda s: "-".join(map(str, s)))
+def test_keys_of_a_sibling(kind, way, far):
+    """The same of K: a node's own score decides how its value and those before the tree, of the other sign, are mixed.
+
+    Errors are relative to the sum of the terms' magnitudes w_j |v_j|, of which each is off as elsewhere.  The nodes' scores have
+    15 bits, 2^-12 of eight where eleven are kept: e = 2.0e-3.  Rows of weight p that are 4 beside ones of 1 of the other sign move
+    an output by e p (1 - p) 5, at most 0.56 e of 4 p + 1 - p.  With the output's rounding 2.0e-3 + 1.1e-3 + 0.7e-3; over 16-bit
+    pages scores are exact and weights 2^-9, 4.0e-3."""
+    n, x = WAYS[way]
+    steps = np.where(np.arange(n + x) < x, 0, 5 if kind[1] == 128 else 4)
+    assert _error(kind, way, steps, np.ones(n + x), own=-4.0, hidden=(2.0 ** far, 1.0)) <= TOL
+
+
+@pytest.mark.parametrize("way", ["eights", "few", "direct", "direct_long"])
+@pytest.mark.parametrize("kind", KINDS, ids=lambda s: "-".join(map(str, s)))
+def test_keys_of_a_sibling_further(kind, way):
+    n, x = WAYS[way]
+    steps = np.where(np.arange(n + x) < x, 0, 5 if kind[1] == 128 else 4)
+    assert _error(kind, way, steps, np.ones(n + x), own=-4.0, hidden=(2.0 ** 24, 1.0)) <= TOL
