@@ -48,6 +48,11 @@ constexpr int kDirGroup = 128;           // threads of a group's softmax, and of
 constexpr int kDirThreads = 4 * kDirGroup + 64;
 constexpr int kTurned = 16;              // rows of queries that a warp of the softmax turns (32 by half the warps took 4 us)
 constexpr uint32_t kDirTmem = 512;       // a group: S (P over its first half), O
+// What a reference lies below a row's largest score when it is set, and what scores may pass it by before it moves (powers of
+// two).  f16 weights: as far up as their sums of 128 allow.  bf16 ones have fp32's range and meet V as it is: from 2^-8 up to
+// one, so that sums of values near the type's largest are numbers where the values' mean is.
+__host__ __device__ constexpr float below_top(bool codes) { return codes ? kBelow : -7.f; }
+__host__ __device__ constexpr float room_above(bool codes) { return codes ? kRoom : 0.f; }
 constexpr int kLeastTiles = 2;           // of a stretch: one a group
 constexpr int kItemTiles = 6, kJoinTiles = 3;   // what a stretch takes beside its tiles, and the kernel that joins them, in tiles
 constexpr int kMostCuts = 256;           // stretches of one unit's keys: their weights join in shared memory
@@ -633,11 +638,11 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
                     m2 = fmax3(m2, __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
                 }
                 const float most = fmaf(fmaxf(m, m2), f, ve);
-                const bool moves = most > ref + kRoom;        // (from -inf: any number)
+                const bool moves = most > ref + room_above(kCodes);      // (from -inf: any number)
                 if (__any_sync(0xffffffffu, moves)) {
                     float alpha = 1.f;
                     if (moves) {
-                        const float to = ceilf(most - kBelow);
+                        const float to = ceilf(most - below_top(kCodes));
                         alpha = ex2(ref - to);
                         l = lowered(l, ref - to);
                         ref = to;

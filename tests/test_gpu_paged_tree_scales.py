@@ -123,3 +123,11 @@ def test_keys_of_a_sibling_further(kind, way):
     n, x = WAYS[way]
     steps = np.where(np.arange(n + x) < x, 0, 5 if kind[1] == 128 else 4)
     assert _error(kind, way, steps, np.ones(n + x), own=-4.0, hidden=(2.0 ** 24, 1.0)) <= TOL
+
+
+@pytest.mark.parametrize("size", [2.0 ** 114, 2.0 ** 117])
+@pytest.mark.parametrize("way", ["eights", "direct"])
+def test_values_near_the_largest(way, size):
+    """16-bit pages: outputs are numbers where their values are."""
+    steps = np.where(np.arange(_rows(way)) % 500 == 499, 6, 0)       # (scores that rise late, too)
+    assert _error(("native", 128), way, steps, np.full(_rows(way), size)) <= TOL
