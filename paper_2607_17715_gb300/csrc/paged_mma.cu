@@ -290,6 +290,7 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
     __shared__ __align__(16) uint16_t s_q[kTerms][L::KS * NT * 32 * 4];
     __shared__ __align__(8) float s_rs[kRows];
     __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
+    __shared__ int s_unit[kWarps];       // (codes) V's scales are below 2^this
     __shared__ int s_end[kRows];         // (trees: the last key before the tree that a row does not see)
     __shared__ uint32_t s_bits[kTree ? kRows * kTreeWords : 1];
     __shared__ uint32_t s_abort, s_last;
@@ -786,10 +787,17 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
 
     // the warps' results join: O in units of one, rows [row][channel], lines of 16 bytes swapped within
     // groups of eight so that lanes meet fewer banks
+    if (kCodes && lane == 0) s_unit[warp] = unit;
     __syncthreads();                     // every stage has been read
+    // (O is its weights' sum times the output, up to 2^54: of large values in units of 2^lift until it is divided by it)
+    int lift = 0;
+    if constexpr (kCodes) {
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) lift = max(lift, s_unit[w] - 40);
+    }
     float* const joined = reinterpret_cast<float*>(smem);
     auto line = [](int f) { return f ^ (2 * (f >> 3 & 3)); };
-    const float one = kCodes ? pow2i(unit) : 1.f;
+    const float one = kCodes ? pow2i(unit - lift) : 1.f;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -853,6 +861,10 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         if (sum == 0.f) x.x = x.y = x.z = x.w = none(row);
         else x = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+        if constexpr (kCodes) {
+            const float up = pow2i(lift);
+            x = make_float4(x.x * up, x.y * up, x.z * up, x.w * up);
+        }
         if constexpr (!kCodes) {         // values that are not finite, of keys that the row sees
             const uint32_t odd = s_odd[row * (D / 4) + f];
             if (odd != 0u && sum < INFINITY) {
@@ -889,6 +901,7 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
         float top = -INFINITY, sum = 0.f;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
         constexpr int kBatch = 16;
+        constexpr float kLow = 1.f / kMaxStretches;      // (of values near the largest no sum overflows; a power of two changes nothing else)
         for (int k0 = 0; k0 < (int)n_split; k0 += kBatch) {
             float e[kBatch];
             float4 y[kBatch];
@@ -911,7 +924,7 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
             x = make_float4(x.x * a, x.y * a, x.z * a, x.w * a);
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
-                const float w = ex2f(e[k] - base);
+                const float w = ex2f(e[k] - base) * kLow;
                 sum += w;
                 x.x = fmaf(y[k].x, w, x.x);
                 x.y = fmaf(y[k].y, w, x.y);
@@ -924,7 +937,7 @@ __global__ void __launch_bounds__(kWarps * 32, Lay<D, kCodes, NT>::kCtas > 1 ? L
         const uint32_t tok = (row0 + row) / G, h = hk * G + row0 + row - tok * G;
         *reinterpret_cast<uint2*>(out + ((int64_t)(R.q0 + tok) * P.hq + h) * D + 4 * f) =
             make_uint2(pack2<false>(x.x * inv, x.y * inv), pack2<false>(x.z * inv, x.w * inv));
-        if (f == 0 && P.lse) P.lse[(int64_t)h * P.n_tokens + R.q0 + tok] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
+        if (f == 0 && P.lse) P.lse[(int64_t)h * P.n_tokens + R.q0 + tok] = sum == 0.f ? -INFINITY : (top + log2f(sum / kLow)) * 0.69314718055994531f;
     }
 }
 

@@ -131,3 +131,9 @@ def test_values_near_the_largest(way, size):
     """16-bit pages: outputs are numbers where their values are."""
     steps = np.where(np.arange(_rows(way)) % 500 == 499, 6, 0)       # (scores that rise late, too)
     assert _error(("native", 128), way, steps, np.full(_rows(way), size)) <= TOL
+@pytest.mark.parametrize("size", [2.0 ** -98, 2.0 ** -80, 2.0 ** 80, 2.0 ** 111])
+@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("kind", KINDS, ids=lambda s: "-".join(map(str, s)))
+def test_all_values_small_or_large(kind, way, size):
+    """Values near the smallest that 8-bit rows keep, and large ones that thousands of rows add up to 2^126 of."""
+    assert _error(kind, way, np.arange(_rows(way)) % 3, np.full(_rows(way), size)) <= TOL
