@@ -10,9 +10,9 @@
 // Roundings: a code times its scale has eleven bits, as the queries over codes and the weights have, and weights over 16-bit
 // pages have eight.  The scale is rounded too where all of a tile's are within 2^20 of the largest of their 32 keys (rows that a
 // query does not see among them); in other tiles the product alone is, down to 2^-29 of that.  Weights take V's powers of two, and
-// lose bits where those of 32 keys are more than 2^22 above what another 32, which count as much, have.  Outputs are off by 2.2e-3 of their norm from 64 bits, where fp32 in between and the output's own
-// rounding give 1.7e-3.  (Scales met in fp32 by the scores would spare the first; a broadcast from shared memory for every
-// key made the softmax twice as long.  A second term of the weights would add a third to the products of 16-bit pages.)
+// lose bits where those of 32 keys are more than 2^24 above what another 32, which count as much, have.  Outputs over normal keys and
+// values are off by 1.8e-3 of their norm from 64 bits (8-bit pages) and 2.4e-3 (16-bit ones), where the output's own rounding
+// is 1.7e-3.  (A second term of the weights would add a third to the products of 16-bit pages.)
 //
 // A CTA has an SM to itself, in two groups that take the tiles of 128 keys in turn, each with its own scores and output in
 // tensor memory, and its own warps: four for the softmax (a row a thread), four that convert (8-bit codes) or look after
@@ -49,10 +49,11 @@ constexpr int kDirThreads = 4 * kDirGroup + 64;
 constexpr int kTurned = 16;              // rows of queries that a warp of the softmax turns (32 by half the warps took 4 us)
 constexpr uint32_t kDirTmem = 512;       // a group: S (P over its first half), O
 // What a reference lies below a row's largest score when it is set, and what scores may pass it by before it moves (powers of
-// two).  f16 weights: as far up as their sums of 128 allow.  bf16 ones have fp32's range and meet V as it is: from 2^-8 up to
+// two).  f16 weights: up to 2^15; further up at first (2^12, 2^14) references move oftener (32 nodes over 120000 rows 6 and 11 us more),
+// lower (2^8) a tail of small weights has fewer bits.  bf16 ones have fp32's range and meet V as it is: from 2^-8 up to
 // one, so that sums of values near the type's largest are numbers where the values' mean is.
-__host__ __device__ constexpr float below_top(bool codes) { return codes ? kBelow : -7.f; }
-__host__ __device__ constexpr float room_above(bool codes) { return codes ? kRoom : 0.f; }
+__host__ __device__ constexpr float below_top(bool codes) { return codes ? 10.f : -7.f; }
+__host__ __device__ constexpr float room_above(bool codes) { return codes ? 15.f : 0.f; }
 constexpr int kLeastTiles = 2;           // of a stretch: one a group
 constexpr int kItemTiles = 6, kJoinTiles = 3;   // what a stretch takes beside its tiles, and the kernel that joins them, in tiles
 constexpr int kMostCuts = 256;           // stretches of one unit's keys: their weights join in shared memory

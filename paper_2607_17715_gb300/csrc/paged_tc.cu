@@ -195,7 +195,7 @@ __device__ __forceinline__ void issue_products(uint32_t tmem, uint32_t sQ, uint3
 // largest (and a tile of equal weights, 2^15 together, passes for what the guard lets through).  O and the sum
 // are scaled to a new one, before the next tile, only when weights have passed 2^14.  Where a sum shows
 // weights near f16's largest (or the row has no reference yet) the maximum comes first after all.
-constexpr float kMostSum = 61440.f;
+constexpr float kBelow = 8.f, kRoom = 14.f, kMostSum = 61440.f;
 
 template <int D, bool kCodes, bool kTree, int kReq>
 __device__ __forceinline__ void softmax_rows(const TcLaunch<kReq>& X, const Item& w, uint32_t tmem, uint32_t bars, int x, int quad, int lane,

@@ -18,9 +18,6 @@ namespace {
 
 constexpr int BM = 128;                  // rows of a query tile
 constexpr int BN = 128;                  // keys of a tile
-// References of weights lie this far below a row's largest score, and move when weights pass the second (powers of
-// two; see paged_tc.cu).
-constexpr float kBelow = 8.f, kRoom = 14.f;
 
 template <int D>
 struct TileOf {
