@@ -5,14 +5,14 @@
 // two, of 128 rows each, and reading the pages bounds the call: TMA brings them into shared memory, and nothing but
 // partials goes back.  8-bit codes become f16 there, relative to a power of two for every
 // 32 keys (a V scale that is NaN makes NaN of the rows that see it, and zero of the row itself).  16-bit pages are operands as they lie,
-// the queries two bf16 terms of them and the weights one, as in paged_mma.cu.
+// the queries and the weights two bf16 terms each.
 //
-// Roundings: a code times its scale has eleven bits, as the queries over codes and the weights have, and weights over 16-bit
-// pages have eight.  The scale is rounded too where all of a tile's are within 2^20 of the largest of their 32 keys (rows that a
+// Roundings: a code times its scale has eleven bits, as the queries and the weights over codes have; over 16-bit pages both have
+// 16.  The scale is rounded too where all of a tile's are within 2^20 of the largest of their 32 keys (rows that a
 // query does not see among them); in other tiles the product alone is, down to 2^-29 of that.  Weights take V's powers of two, and
 // lose bits where those of 32 keys are more than 2^24 above what another 32, which count as much, have.  Outputs over normal keys and
-// values are off by 1.8e-3 of their norm from 64 bits (8-bit pages) and 2.4e-3 (16-bit ones), where the output's own rounding
-// is 1.7e-3.  (A second term of the weights would add a third to the products of 16-bit pages.)
+// values are off by 1.8e-3 of their norm from 64 bits (8-bit pages), and by their own rounding to bf16, 1.7e-3 (16-bit ones; 2.4e-3
+// with one term of the weights, in 0.89 of the time).
 //
 // A CTA has an SM to itself, in two groups that take the tiles of 128 keys in turn, each with its own scores and output in
 // tensor memory, and its own warps: four for the softmax (a row a thread), four that convert (8-bit codes) or look after
@@ -415,7 +415,13 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
 #pragma unroll
                         for (int kk = 0; kk < BN / 32; ++kk) {
                             const int k = half * (BN / 32) + kk;
-                            mma_bf16_ts(tmemO, tmem + (uint32_t)k * 8u, dv + (uint64_t)((k * 16 * 128) >> 4), idO, k > 0 || i > 0 ? 1u : 0u);
+                            const uint64_t v = dv + (uint64_t)((k * 16 * 128) >> 4);
+                            if constexpr (kCodes) {
+                                mma_bf16_ts(tmemO, tmem + (uint32_t)k * 8u, v, idO, k > 0 || i > 0 ? 1u : 0u);
+                            } else {                          // what the first terms lack, and those
+                                mma_bf16_ts(tmemO, tmem + (uint32_t)(k / 2 * 32 + k % 2 * 8 + 16), v, idO, k > 0 || i > 0 ? 1u : 0u);
+                                mma_bf16_ts(tmemO, tmem + (uint32_t)(k / 2 * 32 + k % 2 * 8), v, idO, 1u);
+                            }
                         }
                         mma_commit(half ? barO : barW);
                     }
@@ -567,17 +573,21 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
     };
     // weights of 32 keys, by a power of two
     auto scale_weights = [&](int c, float alpha) {
-        uint32_t pv[16];
         tmem_st_wait();
-        tmem_ld16(colS + c * 16, pv);
-        tmem_ld_wait();
+#pragma unroll 1
+        for (int x = 0; x < (kCodes ? 1 : 2); ++x) {
+            const uint32_t at = colS + (kCodes ? c * 16 : c * 32 + x * 16);
+            uint32_t pv[16];
+            tmem_ld16(at, pv);
+            tmem_ld_wait();
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const float2 w = kCodes ? __half22float2(*reinterpret_cast<const __half2*>(&pv[e]))
-                                    : make_float2(__uint_as_float(pv[e] << 16), __uint_as_float(pv[e] & 0xffff0000u));
-            pv[e] = kCodes ? pack_f16(w.x * alpha, w.y * alpha) : pack_bf16(w.x * alpha, w.y * alpha);
+            for (int e = 0; e < 16; ++e) {
+                const float2 w = kCodes ? __half22float2(*reinterpret_cast<const __half2*>(&pv[e]))
+                                        : make_float2(__uint_as_float(pv[e] << 16), __uint_as_float(pv[e] & 0xffff0000u));
+                pv[e] = kCodes ? pack_f16(w.x * alpha, w.y * alpha) : pack_bf16(w.x * alpha, w.y * alpha);
+            }
+            tmem_st16(at, pv);
         }
-        tmem_st16(colS + c * 16, pv);
     };
     auto softmax = [&](bool care) {
         ref = -CUDART_INF_F;
@@ -660,6 +670,7 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
                 const float off = ve - (ref == -CUDART_INF_F ? 0.f : ref);
                 float ps[4] = {0.f, 0.f, 0.f, 0.f};
                 uint32_t pk[16];
+                [[maybe_unused]] uint32_t pl[16];             // (16-bit pages) what the first terms, cut off, lack
 #pragma unroll
                 for (int e = 0; e < 32; e += 4) {
                     float a[4];
@@ -669,10 +680,23 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
                     for (int k = 0; k < 4; ++k) a[k] = ex2(a[k]);
                     fadd2(ps[0], ps[1], a[0], a[1]);
                     fadd2(ps[2], ps[3], a[2], a[3]);
-                    pk[e / 2] = kCodes ? pack_f16(a[0], a[1]) : pack_bf16(a[0], a[1]);
-                    pk[e / 2 + 1] = kCodes ? pack_f16(a[2], a[3]) : pack_bf16(a[2], a[3]);
+#pragma unroll
+                    for (int k = 0; k < 4; k += 2) {
+                        if constexpr (kCodes) {
+                            pk[e / 2 + k / 2] = pack_f16(a[k], a[k + 1]);
+                        } else {
+                            const uint32_t x = __float_as_uint(a[k]), y = __float_as_uint(a[k + 1]);
+                            pk[e / 2 + k / 2] = __byte_perm(x, y, 0x7632);
+                            pl[e / 2 + k / 2] = pack_bf16(a[k] - __uint_as_float(x & 0xffff0000u), a[k + 1] - __uint_as_float(y & 0xffff0000u));
+                        }
+                    }
                 }
-                tmem_st16(colS + c * 16, pk);                 // (over scores that are taken: the thread's own)
+                if constexpr (kCodes) {
+                    tmem_st16(colS + c * 16, pk);             // (over scores that are taken: the thread's own)
+                } else {
+                    tmem_st16(colS + c * 32, pk);
+                    tmem_st16(colS + c * 32 + 16, pl);
+                }
                 l = fmaf((ps[0] + ps[1]) + (ps[2] + ps[3]), ex2(-ve), l);
                 if (c == 1) {
                     tmem_st_wait();

@@ -1,11 +1,12 @@
 """Errors of attention of trees relative to a row's norm: outputs over thousands of rows are too small for an absolute
 tolerance (one of 2e-2 does not notice a key tile that is left out).
 
-The tolerances are those of attention of tokens that follow one another, for the same reasons.  Over random keys and
-values a bf16 output's own rounding is at most 2^-9 of a value, 2.0e-3 of the norm; weights of 8 bits (over 16-bit pages)
-or 11, queries and codes times scales of 11 bits add errors of either sign, 2^-9 / sqrt(3) of the norm together
-at most: 5e-3.  lse: a score moves by 2^-12 |q k| / sqrt(d) for each operand rounded to 11 bits, two of them below 1e-3
-for normal ones: 2e-3.  fp32: 1e-5, lse 2e-5 of its magnitude and one."""
+Tolerances.  A rounding to bf16 is off by at most 2^-8 of a value, evenly either way: over a row's channels by 2^-8 / sqrt(3) of its
+norm at most in the mean of squares, 2.3e-3.  The output has one, weights of 8 bits (few rows over 16-bit pages) another, and eleven
+bits of queries, weights, codes times scales an eighth of one each: 3.3e-3 together.  A row's mean of squares over 64 channels
+lies within a half of that: 5e-3 leaves room for it.  lse: an operand's eleven bits move a score by 2^-11 / sqrt(3) of
+(sum q^2 k^2 / d)^(1/2), one for normal rows, two of them by 4e-4: five times that is 2e-3.  fp32: 1e-5, lse 2e-5 of its magnitude and one,
+as the library's other fp32 attentions."""
 import numpy as np
 import pytest
 import torch
@@ -46,6 +47,25 @@ def test_relative_errors(shape, lens, window):
     want, want_l = call.want()
     assert D.relative(call.out, want) <= TOL[dtype]
     assert ((call.lse - want_l).abs() <= TOL_LSE[dtype] * (1 + (want_l.abs() if dtype == "f32" else 0))).all()
+
+
+@gpu
+@pytest.mark.parametrize("lens", ["tile", "deep", "tiles", "whole"])
+@pytest.mark.parametrize("shape", [SHAPES[1], ("bf16", "native", 32, 8, 64)], ids=lambda s: "-".join(map(str, s)))
+def test_operands_of_16_bits(shape, lens):
+    """Trees straight from 16-bit pages: queries and weights have two terms, so an output's own rounding is nearly all of its
+    error.  Second terms are off by 2^-8 of what the first, cut off or rounded, lack: 2^-15 of a weight, 2^-16 of a query's
+    value and so of its scores' sum |q k| / sqrt(d), at most 16 for normal ones.  That is 2^-12 of the output at most, which adds
+    in squares to 1.5e-3 and more of its rounding: 1.3 %."""
+    dtype, fmt, hq, hkv, d = shape
+    r, gen = np.random.default_rng(6), torch.Generator(device="cuda").manual_seed(6)
+    trees = [random_tree(r, n) for n, _ in LENS[lens]]
+    k, v = ([torch.randn((n + x, hkv, d), generator=gen, device="cuda") for n, x in LENS[lens]] for _ in range(2))
+    T = sum(n for n, _ in LENS[lens])
+    q = torch.randn((T, hq, d), generator=gen, device="cuda").to(P.TDT[dtype])
+    call = D.Call(dtype, hq, hkv, d, D.Rows(dtype, fmt, k, v, 64), trees, q)
+    want, _ = call.want()
+    assert (call.out.double() - want).norm() <= 1.02 * (want.bfloat16().double() - want).norm()
 
 
 @pytest.mark.parametrize("tree,x", [(star(20), 9001), (chain(60), 5000)], ids=["star", "chain"])
