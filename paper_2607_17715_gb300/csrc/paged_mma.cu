@@ -19,7 +19,7 @@
 // like the running maximum does.  The largest weight is 2^15, so that f16 keeps 11 bits of weight times scale
 // down to 2^-29 of the largest of both (with a largest weight of one a row whose value is 2^10 times the others',
 // whatever its own weight, left nothing of weights of 2^-15).  Queries are f16 too, each row scaled by a power of two so that its
-// largest value is near 2^6 (2^14 where codes are short of 2^8): their rounding is 2^-12 of a value.  Over
+// largest value is near 2^6 (2^14 where codes are short of 2^8): their rounding is at most 2^-11 of a value.  Over
 // 16-bit pages operands are bf16, and the queries two terms of it each: one alone, 8 bits of a value that
 // RoPE turned, made two thirds of the output's error over long contexts (5.6e-3 of it, against 2e-3).
 //

@@ -1,10 +1,11 @@
 """Attention of trees where most of an output comes from many keys of small weight, where scales are far apart at random, and
 at the ends of the queries' range: the cases of the attention of tokens that follow one another, with trees.
 
-Tolerance: 5e-3 of a row's norm, as there.  Tails: the output's rounding to bf16 is at most 2^-9 of a value, 2.0e-3 of the norm; weights,
-scales and values of 11 bits add 2^-12 each, 0.7e-3, and so does a heavy key's score of up to 11, 2.7e-3 of its weight: at
-most a fourth of that of an output whose other values are one apart.  Weights of 8 bits (16-bit pages; a tail 2^-29 of a heavy
-key and a large value beside it) are all equal ones, with the same error: 2^-9 of the tail's share of at most 3 / 4, 1.5e-3."""
+Tolerance: 5e-3 of a row's norm, as there.  Tails: the output's rounding to bf16 is off by 2^-8 / sqrt(3) of the norm in the mean of
+squares, 2.3e-3.  Weights, scales and values of 11 bits are off by 2^-11 each, and two of a heavy key's score of 11 by 1.1e-2 of its
+weight: at most a fourth of that of an output whose values are one apart, 2.7e-3.  Weights of 8 bits (few rows over 16-bit
+pages; a tail 2^-29 of a heavy key and a large value beside it) are all equal ones, with the same error: 2^-8 of the tail's share of
+at most 3 / 4, 2.9e-3.  In squares 3.7e-3."""
 import numpy as np
 import pytest
 import torch
