@@ -9,8 +9,9 @@
 //
 // Roundings: a code times its scale has eleven bits, as the queries and the weights over codes have; over 16-bit pages both have
 // 16.  The scale is rounded too where all of a tile's are within 2^20 of the largest of their 32 keys (rows that a
-// query does not see among them); in other tiles the product alone is, down to 2^-29 of that.  Weights take V's powers of two, and
-// lose bits where those of 32 keys are more than 2^24 above what another 32, which count as much, have.  Outputs over normal keys and
+// query does not see among them); in other tiles the product alone is, down to 2^-29 of that.  Weights take V's
+// powers of two, one for most tiles as in paged_expand.cu, and lose bits where 32 keys' own is more than 2^24 above another's which
+// count as much.  Outputs over normal keys and
 // values are off by 1.8e-3 of their norm from 64 bits (8-bit pages), and by their own rounding to bf16, 1.7e-3 (16-bit ones; 2.4e-3
 // with one term of the weights, in 0.89 of the time).
 //
@@ -157,6 +158,12 @@ __device__ __forceinline__ void turn_queries_twice(const PagedAttn<kReq>& P, con
     }
 }
 
+// The power of two that brings the largest scale, of these bits, to [2^6, 2^7).
+__device__ __forceinline__ int unit_of(uint32_t top) { return min(119, (int)(top >> 23) - 126 - 7); }
+// V's common power leaves room for rows 2^kCommonRoom above a sample's largest; 32 keys whose own is kCommonDepth below it keep
+// their own: scales are normal numbers of f16 down to 2^-20 of what the power is for.
+constexpr int kCommonRoom = 12, kCommonDepth = 14, kNoUnit = -1000;
+
 // Which rows of a key tile are there: of 16-key groups that lie in pages (bits), from lo to below hi.
 struct Rows {
     uint32_t groups;
@@ -171,8 +178,8 @@ struct Rows {
 
 // A tile of codes [128][D] times their rows' scales (f16, twice in a word) as f16 in 64-channel blocks under the 128-byte
 // swizzle, by a group's threads; (not `all`) rows that are not there become zero.  The scale's rounding and the product's
-// are 2^-12 of a value each, where both are f16's normal numbers: scales down to 2^-20 of the largest of their 32 keys, rows
-// that a query does not see among them; others go by wide_codes_to_f16.  The output's own is 2^-9.  (Scales in fp32 on the scores and
+// are 2^-11 of a value each, where both are f16's normal numbers: scales down to 2^-20 of the largest of their 32 keys, rows
+// that a query does not see among them; others go by wide_codes_to_f16.  The output's own is 2^-8.  (Scales in fp32 on the scores and
 // the weights instead, whose rows every thread reads from shared memory, took the softmax twice the time: 3400 clocks a tile for 1600.)
 template <int D>
 __device__ __forceinline__ void codes_to_f16(uint32_t raw, uint32_t tile, const uint32_t* scale, int t, bool all, const Rows& rows) {
@@ -457,10 +464,13 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
             }
         };
         // ... relative to a power of two for 32 keys, the largest to [2^6, 2^7): a code's product is below 2^16.  `none`: the
-        // power of keys that are all zero.  `far`: a scale that is no normal number of f16 then
-        auto put_scale = [&](float x, uint32_t* to, int least, int none, bool& far) {
+        // power of keys that are all zero; `far`: a scale that is no normal number of f16 then.  V's is `shared` where it may be:
+        // references of weights take it, and where one 32 keys' is above the others' these have fewer bits
+        int common = kNoUnit;
+        auto put_scale = [&](float x, uint32_t* to, int least, int none, int shared, bool& far) {
             const uint32_t y = __float_as_uint(x) & 0x7fffffffu, top = __reduce_max_sync(0xffffffffu, y < 0x7f800000u ? y : 0u);
-            const int unit = top == 0u ? none : max(least, min(119, (int)(top >> 23) - 126 - 7));
+            int unit = top == 0u ? none : max(least, unit_of(top));
+            if (shared != kNoUnit && (top == 0u || (unit <= shared && unit >= shared - kCommonDepth))) unit = shared;
             const __half2 h = __float2half2_rn(x * pow2i(-unit));
             far = far || y - 1u < ((uint32_t)max(unit + 113, 1) << 23) - 1u;
             to[t] = *reinterpret_cast<const uint32_t*>(&h);
@@ -483,8 +493,17 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
         };
         auto all = [&](bool care) {
             if constexpr (kCodes) {
-                ask_scales(0, pages_of(0));
+                // V's common power: room for rows 2^kCommonRoom above the largest of 32 spread over what is seen
+                const int key = w.k_lo + (int)((int64_t)(hi - w.k_lo) * lane / 32);
+                const int page = ld_after(P.pg.table + (int64_t)w.R.row * P.pg.table_stride + (key >> P.pg.page_shift)), pages0 = pages_of(0);
                 pages1 = pages_of(1);
+                uint32_t y = 0u;
+                if (page >= 0 && page < P.pg.n_pages)
+                    y = __float_as_uint(ld_after(P.pg.v_scale + (int64_t)page * P.pg.scale_stride + (w.hk << P.pg.page_shift) +
+                                                 (key & ((1 << P.pg.page_shift) - 1)))) & 0x7fffffffu;
+                ask_scales(0, pages0);
+                const uint32_t top = __reduce_max_sync(0xffffffffu, y < 0x7f800000u ? y : 0u);
+                if (top != 0u) common = max(-90, min(119, unit_of(top) + kCommonRoom));
             }
             if (!care) __syncthreads();
             for (int i = 0; i < n; ++i, uses ^= 1u) {
@@ -492,10 +511,10 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
                     mbar_wait(barK, uses, P.err, abort);
                     if (i > 0) mbar_wait(barS, uses ^ 1u, P.err, abort);             // the products before have read K's tile, and V's
                     const bool odd = !(fabsf(v_scale) < CUDART_INF_F);       // (V's row becomes zero, and NaN of the rows that see it)
-                    // V's from -90 on: the sum of weights takes 2^-unit.  And -90 where all are zero, since a reference takes V's
-                    // unit too: at 0 it rose by 2^15 and more above what other rows' values need, and took their weights' bits
+                    // (V's from -90 on: the sum of weights takes 2^-unit.  And -90 where all are zero, at 0 it would raise references)
                     bool far = false;
-                    const int k_unit = put_scale(k_scale, scales, -120, 0, far), v_unit = put_scale(odd ? 0.f : v_scale, scales + BN, -90, -90, far);
+                    const int k_unit = put_scale(k_scale, scales, -120, 0, kNoUnit, far);
+                    const int v_unit = put_scale(odd ? 0.f : v_scale, scales + BN, -90, -90, common, far);
                     if (lane == 0) s_units[(i & 1) * 4 + t / 32] = k_unit;
                     far = __any_sync(0xffffffffu, far);
                     if (lane == 0) s_far[t / 32] = far;

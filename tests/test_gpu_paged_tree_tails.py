@@ -22,17 +22,18 @@ TOL = 5e-3
 @pytest.mark.parametrize("apart", [0, 6, 10, 13])
 @pytest.mark.parametrize("fmt,hq,hkv,d,batch,n,keys,tail", [
     ("e4m3", 16, 4, 128, 38, 16, 32768, 14), ("native", 16, 4, 128, 38, 16, 32768, 14), ("e4m3", 32, 8, 64, 19, 40, 16384, 13),
-    ("e4m3", 4, 4, 128, 38, 100, 131072, 16), ("e4m3", 32, 8, 128, 1, 40, 131072, 16), ("e4m3", 32, 8, 128, 8, 2, 16384, 13),
+    ("e4m3", 4, 4, 128, 38, 100, 131072, 16), ("e4m3", 4, 4, 128, 38, 100, 131072, 17), ("e4m3", 32, 8, 128, 1, 40, 131072, 16),
+    ("e4m3", 32, 8, 128, 8, 2, 16384, 13),
     ("native", 8, 2, 64, 1, 64, 131072, 16), ("e4m3", 32, 8, 128, 1, 200, 16384, 13)])
 def test_tails(fmt, hq, hkv, d, batch, n, keys, tail, apart, big):
-    """One key of weight 1, one row of V 2^apart times the others at a weight of 2^-40, the rest equal at 2^(0.34 - tail): together
-    as much as the first and more.  Every request has the same pages; of many, none is cut into stretches."""
+    """One key of weight 2^0.5, one row of V 2^apart times the others at a weight of 2^-40, the rest equal at 1.28 2^-tail, which
+    few bits do not have: together as much as the first and more.  Every request has the same pages; of many, none is cut into stretches."""
     gen = torch.Generator(device="cuda").manual_seed(tail)
     per = 16.0 / d ** 0.5 / np.log(2.0)                  # scores in log2: q = 16 in channel 0, nothing else
     k = torch.zeros((keys, hkv, d), device="cuda", dtype=torch.float64)
     v = 1 + 0.25 * torch.randn(k.shape, generator=gen, device="cuda", dtype=torch.float64)
-    k[:, :, 0] = 0.34 / per
-    k[0, :, 0] = tail / per
+    k[:, :, 0] = np.log2(1.28125) / per
+    k[0, :, 0] = (tail + 0.5) / per
     k[big, :, 0] = (tail - 40) / per
     v[0] = 1 + torch.randn((hkv, d), generator=gen, device="cuda", dtype=torch.float64)
     v[big] *= 2.0 ** apart
