@@ -8,11 +8,11 @@
 // the queries and the weights two bf16 terms each.
 //
 // Roundings: a code times its scale has eleven bits, as the queries and the weights over codes have; over 16-bit pages both have
-// 16.  The scale is rounded too where all of a tile's are within 2^20 of the largest of their 32 keys (rows that a
-// query does not see among them); in other tiles the product alone is, down to 2^-29 of that.  Weights take V's
+// 16.  A scale has two terms, or fp32's bits in a tile with one below 2^-20 of the largest of its 32 keys (rows that a query
+// does not see among them), so the product alone is rounded, down to 2^-29 of that largest's.  Weights take V's
 // powers of two, one for most tiles as in paged_expand.cu, and lose bits where 32 keys' own is more than 2^24 above another's which
 // count as much.  Outputs over normal keys and
-// values are off by 1.8e-3 of their norm from 64 bits (8-bit pages), and by their own rounding to bf16, 1.7e-3 (16-bit ones; 2.4e-3
+// values are off by 1.7e-3 of their norm from 64 bits (8-bit pages), and by their own rounding to bf16, 1.7e-3 (16-bit ones; 2.4e-3
 // with one term of the weights, in 0.89 of the time).
 //
 // A CTA has an SM to itself, in two groups that take the tiles of 128 keys in turn, each with its own scores and output in
@@ -176,11 +176,13 @@ struct Rows {
     }
 };
 
-// A tile of codes [128][D] times their rows' scales (f16, twice in a word) as f16 in 64-channel blocks under the 128-byte
-// swizzle, by a group's threads; (not `all`) rows that are not there become zero.  The scale's rounding and the product's
-// are 2^-11 of a value each, where both are f16's normal numbers: scales down to 2^-20 of the largest of their 32 keys, rows
-// that a query does not see among them; others go by wide_codes_to_f16.  The output's own is 2^-8.  (Scales in fp32 on the scores and
-// the weights instead, whose rows every thread reads from shared memory, took the softmax twice the time: 3400 clocks a tile for 1600.)
+// A tile of codes [128][D] times their rows' scales (two f16 terms in a word) as f16 in 64-channel blocks under the 128-byte
+// swizzle, by a group's threads; (not `all`) rows that are not there become zero.  The product is rounded once, by 2^-11 of a value at
+// most, as in key tiles (with one term of the scale, twice: scores over channels eight times the others' were off by 1.6 times as
+// much, and 32 nodes over 120000 rows took 3 % less time).  A second term is itself short of bits where the scale is far below the
+// largest of its 32 keys; where the first would be, below 2^-20 of it, wide_codes_to_f16 has the tile.  (Scales in fp32 on the
+// scores and the weights instead, whose rows every thread reads from shared memory, took the softmax twice the time: 3400 clocks a
+// tile for 1600.)
 template <int D>
 __device__ __forceinline__ void codes_to_f16(uint32_t raw, uint32_t tile, const uint32_t* scale, int t, bool all, const Rows& rows) {
     constexpr int kChunks = D / 16, kStep = kDirGroup / kChunks, kPasses = BN / kStep;
@@ -202,7 +204,8 @@ __device__ __forceinline__ void codes_to_f16(uint32_t raw, uint32_t tile, const 
         for (int e = 0; e < 8; ++e) {
             uint32_t h;
             asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)(x[e / 2] >> (16 * (e & 1)))));
-            const __half2 z = __hmul2(*reinterpret_cast<const __half2*>(&h), *reinterpret_cast<const __half2*>(&f[i]));
+            const __half2 c = *reinterpret_cast<const __half2*>(&h), s = *reinterpret_cast<const __half2*>(&f[i]);
+            const __half2 z = __hfma2(c, __low2half2(s), __hmul2(c, __high2half2(s)));
             y[e] = *reinterpret_cast<const uint32_t*>(&z);
         }
         const uint32_t at = tile + block * TileOf<D>::kHalf + row * 128;
@@ -295,7 +298,7 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
     const int g = role == kIssue ? threadIdx.x / 32 & 1 : threadIdx.x / kDirGroup & 1;
     const uint32_t sQ = smem_u32(smem), sK = sQ + C::kQ + g * C::kGroupBytes, sV = sK + C::kTile;
     const uint32_t inK = kCodes ? sV + C::kTile : sK, inV = kCodes ? inK + C::kRaw : sV;      // where the pages go
-    uint32_t* const scales = reinterpret_cast<uint32_t*>(smem + C::kSmall) + g * BN * 2;      // (codes) [K, V][key], f16 twice
+    uint32_t* const scales = reinterpret_cast<uint32_t*>(smem + C::kSmall) + g * BN * 2;      // (codes) [K, V][key], two f16 terms
     int8_t* const s_back = reinterpret_cast<int8_t*>(smem + C::kBack);
     const uint32_t bars = sQ + C::kBars + g * 80, barS = bars, barO = bars + 8, barK = bars + 16, barV = bars + 24;
     const uint32_t readyK = bars + 32, readyV = bars + 40, readyP = bars + 48, readyC = bars + 56, readyW = bars + 64, barW = bars + 72;     // (an arrival a warp)
@@ -471,7 +474,8 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
             const uint32_t y = __float_as_uint(x) & 0x7fffffffu, top = __reduce_max_sync(0xffffffffu, y < 0x7f800000u ? y : 0u);
             int unit = top == 0u ? none : max(least, unit_of(top));
             if (shared != kNoUnit && (top == 0u || (unit <= shared && unit >= shared - kCommonDepth))) unit = shared;
-            const __half2 h = __float2half2_rn(x * pow2i(-unit));
+            const __half first = __float2half_rn(x * pow2i(-unit));
+            const __half2 h = __halves2half2(first, __float2half_rn(x * pow2i(-unit) - __half2float(first)));
             far = far || y - 1u < ((uint32_t)max(unit + 113, 1) << 23) - 1u;
             to[t] = *reinterpret_cast<const uint32_t*>(&h);
             return unit;

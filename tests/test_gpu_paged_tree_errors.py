@@ -68,6 +68,28 @@ def test_operands_of_16_bits(shape, lens):
     assert (call.out.double() - want).norm() <= 1.02 * (want.bfloat16().double() - want).norm()
 
 
+@gpu
+@pytest.mark.parametrize("lens", ["tile", "tiles", "large"])
+@pytest.mark.parametrize("d", [128, 64])
+def test_codes_times_scales_are_rounded_once(d, lens):
+    """8-bit pages with channels of K eight times the others': outputs are off by what rounding K and V to eleven bits once makes
+    of them, and by their own rounding, in squares.  A quarter more than the first is left for the weights' eleven bits,
+    2^-11 / sqrt(3) of the output at most where K and V make twice that and more."""
+    r, gen = np.random.default_rng(6), torch.Generator(device="cuda").manual_seed(6)
+    trees = [random_tree(r, n) for n, _ in LENS[lens]]
+    k, v = ([torch.randn((n + x, 8, d), generator=gen, device="cuda") for n, x in LENS[lens]] for _ in range(2))
+    for x in k:
+        x[..., [5, d // 2 + 9]] *= 8
+    q = torch.randn((sum(n for n, _ in LENS[lens]), 32, d), generator=gen, device="cuda").bfloat16()
+    rows = D.Rows("bf16", "e4m3", k, v, 64)
+    call = D.Call("bf16", 32, 8, d, rows, trees, q)
+    want, _ = call.want()
+    rows.k, rows.v = ([x.half().double() for x in held] for held in (rows.k, rows.v))
+    once = (call.want()[0] - want).norm().item()
+    own = (want.bfloat16().double() - want).norm().item()
+    assert (call.out.double() - want).norm().item() <= (own ** 2 + (1.25 * once) ** 2) ** 0.5
+
+
 @pytest.mark.parametrize("tree,x", [(star(20), 9001), (chain(60), 5000)], ids=["star", "chain"])
 def test_a_lost_tile_would_show(tree, x):
     """The tolerances notice a tile of 128 keys left out of thousands: outputs and sums without it are off by more, in most
