@@ -4,8 +4,9 @@
 // fp32; the `best` of largest score are kept, of equal ones those of the lowest places.  So the choice does not
 // depend on how the vocabulary is cut.
 //
-// Every value is read once, which bounds a batch.  A CTA takes a stretch of one beam, 4096 or 16384 values, all on
-// their way at once and kept in registers as they come.  Few of them need be looked at: of the lanes' largest values
+// Every value is read once, the least that a batch takes.  A CTA takes a stretch of one beam, 4096 or 16384 values, all on
+// their way at once and kept as they come: in registers, but for 60 bytes a thread of 64 16-bit values, where 64 registers let four CTAs
+// share an SM.  Few of them need be looked at: of the lanes' largest values
 // every warp's r-th largest, and the least of those over the warps, is a bound that `best` values reach (r times the warps).
 // The score rises with the value, so the bound holds for values, less what the score's rounding can hide.  What passes
 // is ranked by counting.  The CTA that ends last joins its request's stretches the same way, the bound from their first ones.

@@ -20,19 +20,19 @@ constexpr int kMmaRows = 64;
 
 // The same of trees, and the rows up to which tcgen05 takes them straight from the pages instead of making key
 // tiles first.  Measured (us, mma.sync / straight from the pages; one request of 30000 rows, 8 of 4000, 16 of 500): 8-bit
-// pages of 128 channels, 16 rows 32 / 38, 30 / 37, 16 / 16, 32 rows 53 / 38, 44 / 38, 26 / 17; 16-bit ones, 16 rows 39 / 39, 40 / 39,
-// 14 / 16, 32 rows 64 / 39, 66 / 40, 24 / 17; 8-bit ones of 64 channels, 32 rows 32 / 33, 30 / 33, 19 / 14.  24 rows of eight requests
-// of 4000: 35 / 37 from 8-bit pages, 49 / 39 from 16-bit ones.  Straight from the pages / with key tiles: 256 rows 60 / 85, 58 / 91,
-// 35 / 38, 384 rows 76 / 107, 111 / 106, 54 / 56, 512 rows 102 / 109, 113 / 112, 71 / 58, of 16-bit pages 100 / 121, 112 / 126, 73 / 62.
+// pages of 128 channels, 16 rows 33 / 39, 29 / 39, 16 / 16, 32 rows 53 / 39, 44 / 40, 26 / 17; 16-bit ones, 16 rows 39 / 43, 40 / 43,
+// 14 / 17, 32 rows 65 / 43, 66 / 44, 24 / 18; 8-bit ones of 64 channels, 32 rows 33 / 34, 30 / 34, 19 / 15.  24 rows of eight requests
+// of 4000: 35 / 39 from 8-bit pages, 49 / 44 from 16-bit ones.  Straight from the pages / with key tiles: 256 rows 63 / 86, 60 / 91,
+// 36 / 38, 384 rows 77 / 107, 113 / 106, 56 / 56, 512 rows 104 / 109, 116 / 112, 74 / 58, of 16-bit pages 116 / 121, 130 / 126, 78 / 62.
 constexpr int tree_mma_rows(int d, bool codes) { return d * (codes ? 1 : 2) == 64 ? 32 : d * (codes ? 1 : 2) == 128 ? 24 : 16; }
 constexpr int kDirectRows = 512;
 
 // ... and trees over few keys, which many rows a CTA would leave SMs idle for: mma.sync takes them eight rows a CTA,
 // or 16, where that is one wave of CTAs that read at most so many values of K, counted for eight rows.  Measured (us, eight /
-// 16 / the routes above; 128 channels): 8-bit pages, one request of 1500 rows, 64 rows of queries (13 million values) 13.1 / 16.5 / 17.0,
-// 128 rows (26) 17.2 / 18.3 / 17.4, of 6000, 32 rows (25) 16.5 / 21.2 / 21.6, 64 rows (50) 22.8 / 22.2 / 21.9; four of 500, 64
-// rows (17) 13.2 / 16.8 / 17.5, 16 of 100, 32 rows (8; eight are more than a wave) - / 10.5 / 12.8; 16-bit pages, 64 rows over 1500
-// 15.5 / 16.8 / 17.4, 96 rows (19) 19.5 / 18.4 / 17.5, 24 rows over 6000 (19) 17.3 / 19.8 / 21.7, 32 (25) 22.1 / 20.0 / 21.8.
+// 16 / the routes above; 128 channels): 8-bit pages, one request of 1500 rows, 64 rows of queries (13 million values) 13.2 / 16.5 / 17.1,
+// 128 rows (26) 17.3 / 18.5 / 17.5, of 6000, 32 rows (25) 16.6 / 21.1 / 22.0, 64 rows (50) 22.7 / 22.3 / 22.2; four of 500, 64
+// rows (17) 13.2 / 16.6 / 17.9, 16 of 100, 32 rows (8; eight are more than a wave) - / 10.6 / 13.3; 16-bit pages, 64 rows over 1500
+// 15.6 / 16.8 / 18.1, 96 rows (19) 19.5 / 18.4 / 18.3, 24 rows over 6000 (19) 17.3 / 19.9 / 22.4, 32 (25) 22.1 / 19.9 / 22.6.
 constexpr int64_t short_values(bool codes) { return codes ? 26000000 : 18000000; }
 
 // The same of fp32 contexts, and the keys that some request has to see for it: the lanes' kernel reads keys

@@ -1032,7 +1032,7 @@ cudaError_t by_rows(const PagedAttnCall& c, const PagedReq* req, int n, cudaStre
     for (int i = 0; i < n; ++i) rows = std::max(rows, req[i].nq * (c.hq / c.hkv));
     const int hold = c.eights ? c.eights : kMostEights;
     const int eights = (rows + 7) / 8, tiles = (eights + hold - 1) / hold, nt = (eights + tiles - 1) / tiles;
-    // (few requests have trees as small as this: their launches take the small block whatever their number)
+    // (trees have kernels of the small block alone: a launch for every 32 requests)
     const bool small = kTree || n <= kPagedFew;
     constexpr int kLarge = kTree ? kPagedFew : kPagedMany;
     if (nt == 1) return small ? launch<D, kCodes, 1, kPagedFew, kTree>(c, req, n, s) : launch<D, kCodes, 1, kLarge, kTree>(c, req, n, s);

@@ -635,7 +635,7 @@ cudaError_t launch(const PagedAttnCall& c, const KeyTiles& tiles, const std::vec
 template <int D, bool kCodes, bool kTree>
 cudaError_t by_count(const PagedAttnCall& c, const KeyTiles& tiles, const PagedReq* req, int n, cudaStream_t s) {
     const std::vector<PagedReq> entries = plan(c, req, n);
-    constexpr int kLarge = kTree ? kPagedFew : kPagedMany;       // (few requests have trees)
+    constexpr int kLarge = kTree ? kPagedFew : kPagedMany;       // (trees: a launch for every 32 requests)
     return (int)entries.size() <= kPagedFew ? launch<D, kCodes, kPagedFew, kTree>(c, tiles, entries, s)
                                             : launch<D, kCodes, kLarge, kTree>(c, tiles, entries, s);
 }
