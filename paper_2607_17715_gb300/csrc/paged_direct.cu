@@ -22,11 +22,11 @@
 // forming of its others.  The groups' results join in shared memory, the
 // stretches' in a kernel of their own.  Stretches go out longest first, as long as lets the last SM end first.
 //
-// A tile of 128 keys takes a CTA 1.4 us: tensor cores are busy for 0.8 us of it (16-bit pages, two terms of the queries) or 0.6,
+// A tile of 128 keys takes a CTA 1.6 us: tensor cores are busy for 1.1 us of it (16-bit pages, two terms of queries and weights) or 0.6,
 // shared memory for 0.9 (products of 128 x 128 read both operands from it at its full rate), the exponentials 0.5.  A stretch
 // takes 5 us before its first scores and after its last.  Eight trees of up to 64 nodes over up to 6000 rows of 16-bit pages
-// take 51 us (2.1 TB/s of pages, which two row tiles read), 32 nodes over 120000 rows of 8-bit pages 92 us (2.8).
-// Tried and slower: scores 64 keys at a time in two pieces of tensor memory (62 -> 68 us), the next piece of scores
+// take 58 us (1.8 TB/s of pages, which two row tiles read), 32 nodes over 120000 rows of 8-bit pages 98 us (2.6).
+// Tried and slower, with fewer terms: scores 64 keys at a time in two pieces of tensor memory (62 -> 68 us), the next piece of scores
 // asked for while one is worked on (61 -> 63), all 128 scores of a row held (spills); the largest of a tile first, then its weights
 // (52 -> 54, 103 -> 107).  Nothing is full: the chain scores, weights, products takes most of a group's time for a tile.
 //

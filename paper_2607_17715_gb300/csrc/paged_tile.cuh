@@ -346,7 +346,7 @@ __device__ __forceinline__ void take_in(const Launch& X, const Item& w, uint32_t
 
 // The stretches of cut keys joined: a row a thread, 512 / D rows of a unit a CTA, eight stretches' loads a thread on their
 // way at once (one request of 8 KV heads has few units: with 32 rows a CTA, eight a thread and a stretch at a time, 32 CTAs took 54 us
-// for 64 rows over 30000 where these take 42, attention and all; 32 nodes over 120000 rows took 98 with 8 rows a CTA, and 92 so).
+// for 64 rows over 30000 where these take 42, attention and all; 32 nodes over 120000 rows took 6 more with 8 rows a CTA).
 constexpr int kJoinThreads = 128;
 __host__ __device__ constexpr int join_rows(int d) { return kJoinThreads * 4 / d; }
 
