@@ -160,9 +160,9 @@ __device__ __forceinline__ void turn_queries_twice(const PagedAttn<kReq>& P, con
 
 // The power of two that brings the largest scale, of these bits, to [2^6, 2^7).
 __device__ __forceinline__ int unit_of(uint32_t top) { return min(119, (int)(top >> 23) - 126 - 7); }
-// V's common power leaves room for rows 2^kCommonRoom above a sample's largest; 32 keys whose own is kCommonDepth below it keep
-// their own: scales are normal numbers of f16 down to 2^-20 of what the power is for.
-constexpr int kCommonRoom = 12, kCommonDepth = 14, kNoUnit = -1000;
+// V's common power leaves room for rows 2^kCommonRoom above a sample's largest.  (Scales are normal numbers of f16 down to 2^-20 of what a
+// power is for: 32 keys with one further down keep their own.)
+constexpr int kCommonRoom = 12, kNoUnit = -1000;
 
 // Which rows of a key tile are there: of 16-key groups that lie in pages (bits), from lo to below hi.
 struct Rows {
@@ -467,16 +467,17 @@ __global__ void __launch_bounds__(kDirThreads, 1) paged_direct_kernel(const __gr
             }
         };
         // ... relative to a power of two for 32 keys, the largest to [2^6, 2^7): a code's product is below 2^16.  `none`: the
-        // power of keys that are all zero; `far`: a scale that is no normal number of f16 then.  V's is `shared` where it may be:
-        // references of weights take it, and where one 32 keys' is above the others' these have fewer bits
+        // power of keys that are all zero; `far`: a scale that is no normal number of f16 then.  V's is `shared` where all of theirs are
+        // normal numbers by it: references of weights take it, and where one 32 keys' is above the others' these have fewer bits
         int common = kNoUnit;
         auto put_scale = [&](float x, uint32_t* to, int least, int none, int shared, bool& far) {
             const uint32_t y = __float_as_uint(x) & 0x7fffffffu, top = __reduce_max_sync(0xffffffffu, y < 0x7f800000u ? y : 0u);
             int unit = top == 0u ? none : max(least, unit_of(top));
-            if (shared != kNoUnit && (top == 0u || (unit <= shared && unit >= shared - kCommonDepth))) unit = shared;
+            auto below = [&](int unit) { return y - 1u < ((uint32_t)max(unit + 113, 1) << 23) - 1u; };      // 2^(unit - 14), and not zero
+            if (shared != kNoUnit && unit <= shared && !__any_sync(0xffffffffu, below(shared))) unit = shared;
             const __half first = __float2half_rn(x * pow2i(-unit));
             const __half2 h = __halves2half2(first, __float2half_rn(x * pow2i(-unit) - __half2float(first)));
-            far = far || y - 1u < ((uint32_t)max(unit + 113, 1) << 23) - 1u;
+            far = far || below(unit);
             to[t] = *reinterpret_cast<const uint32_t*>(&h);
             return unit;
         };

@@ -138,3 +138,12 @@ def test_values_near_the_largest(way, size):
 def test_all_values_small_or_large(kind, way, size):
     """Values near the smallest that 8-bit rows keep, and large ones that thousands of rows add up to 2^126 of."""
     assert _error(kind, way, np.arange(_rows(way)) % 3, np.full(_rows(way), size)) <= TOL
+
+
+@pytest.mark.parametrize("way,far", [(w, f) for w in ("eights", "few", "direct", "direct_long") for f in (12, 20, 24)] + [("large", 12)])
+@pytest.mark.parametrize("kind", KINDS, ids=lambda s: "-".join(map(str, s)))
+def test_small_values_that_count_alone(kind, way, far):
+    """The tree's rows outweigh those before it by e^31 (e^44 with 64 channels), whose values, in the same 32 rows as some of the
+    tree's, are 2^far times theirs."""
+    n, x = WAYS[way]
+    assert _error(kind, way, np.where(np.arange(n + x) < x, 0, 22), np.ones(n + x), own=2.0 ** -far) <= TOL
