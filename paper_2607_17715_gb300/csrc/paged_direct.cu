@@ -8,12 +8,11 @@
 // the queries and the weights two bf16 terms each.
 //
 // Roundings: a code times its scale has eleven bits, as the queries and the weights over codes have; over 16-bit pages both have
-// 16.  A scale has two terms, or fp32's bits in a tile with one below 2^-20 of the largest of its 32 keys (rows that a query
-// does not see among them), so the product alone is rounded, down to 2^-29 of that largest's.  Weights take V's
-// powers of two, one for most tiles as in paged_expand.cu, and lose bits where 32 keys' own is more than 2^24 above another's which
-// count as much.  Outputs over normal keys and
-// values are off by 1.7e-3 of their norm from 64 bits (8-bit pages), and by their own rounding to bf16, 1.7e-3 (16-bit ones; 2.4e-3
-// with one term of the weights, in 0.89 of the time).
+// 16.  A scale has two terms, or fp32's bits in a tile with one below 2^-20 of what its 32 keys' power of two is for (rows that a
+// query does not see among them), so the product alone is rounded, down to 2^-29 of that.  Weights take V's powers of two, one
+// for most keys as in paged_expand.cu, and lose bits where 32 keys' own is more than 2^24 above another's which count as much.
+// Outputs over normal keys and values are off by 1.7e-3 of their norm from 64 bits, which is their own rounding to bf16 (16-bit
+// pages: 2.4e-3 with one term of the weights, in 0.89 of the time).
 //
 // A CTA has an SM to itself, in two groups that take the tiles of 128 keys in turn, each with its own scores and output in
 // tensor memory, and its own warps: four for the softmax (a row a thread), four that convert (8-bit codes) or look after
@@ -48,7 +47,7 @@ namespace {
 constexpr int kDirGroup = 128;           // threads of a group's softmax, and of its conversions
 constexpr int kDirThreads = 4 * kDirGroup + 64;
 constexpr int kTurned = 16;              // rows of queries that a warp of the softmax turns (32 by half the warps took 4 us)
-constexpr uint32_t kDirTmem = 512;       // a group: S (P over its first half), O
+constexpr uint32_t kDirTmem = 512;       // a group: S (P over it), O
 // What a reference lies below a row's largest score when it is set, and what scores may pass it by before it moves (powers of
 // two).  f16 weights: up to 2^15; further up at first (2^12, 2^14) references move oftener (32 nodes over 120000 rows 6 and 11 us more),
 // lower (2^8) a tail of small weights has fewer bits.  bf16 ones have fp32's range and meet V as it is: from 2^-8 up to

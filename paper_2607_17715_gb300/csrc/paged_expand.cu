@@ -5,8 +5,8 @@
 // again and its conversions took twice the time of its products.  And why f16: the products take one type
 // for both operands, and queries turned by RoPE need more than bf16's 8 bits (a score's error of 2^-9 of
 // its terms was two thirds of the output's whole error over long contexts).  f16 keeps 11 bits of queries,
-// weights and E4M3 rows, and all 8 of bf16 values down to 2^-25 of their tile's largest.  What f16 lacks
-// in range the powers of two hold.
+// weights and E4M3 rows, and all 8 of bf16 values down to 2^-25 of their tile's largest (V's, by its common power: 2^-18 of
+// a sample's).  What f16 lacks in range the powers of two hold.
 //
 // V's power of two is one for most tiles of a request's head, since a tile's weights lie that much lower in
 // f16 where its own is smaller than others': with one row 2^10 times the others' the others' weights lost 10
